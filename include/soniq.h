@@ -424,9 +424,142 @@ SONIQ_API soniq_status soniq_mp_conv2d(const soniq_layout *layout, const soniq_c
 SONIQ_API int64_t soniq_mp_conv2d_scratch_bytes(const soniq_layout *layout, const soniq_conv_desc *cd,
                                                 uint32_t flags);
 
+/* ---- key / value cache of a decoder, and attention over it --------------- */
+
+/*
+ * A cache of attention keys and values in SONIQ's two-level form.  The paper
+ * quantizes the inputs of linear layers; the same rules (one precision per
+ * channel, channels re-ordered so that each precision is contiguous, one
+ * max-abs scale per group, Eq. (1) codes) are applied here to the rows that
+ * attention keeps: a row is one token's key (or value) of one head, its K axis
+ * the head's channels.
+ *
+ *   s_g = max|x| over group g's channels of the row (NaN skipped, infinities
+ *         counted as the largest finite value of the type: a cached row is
+ *         always finite); it is one of the inputs, so it is kept exactly in
+ *         the cache's own 16-bit type.
+ *   j   = clamp(round_half_even(x / s_g * 2^(n-1)), -2^(n-1), 2^(n-1) - 1),
+ *         0 for a NaN x and for s_g = 0; it stands for s_g * j / 2^(n-1).
+ *
+ * How the rows of one side (keys or values) are coded:
+ *   D          channels of a head, 1..256.
+ *   n_groups   1 or 2; with 1, count[1] must be 0.
+ *   count[g]   channels in group g: count[0] >= 1, count[0] + count[1] == D.
+ *   bits[g]    2, 4 or 8 (widths whose codes unpack without crossing words;
+ *              others are SONIQ_ERR_UNSUPPORTED).
+ *   perm       DEVICE pointer, int32 [heads][D]: perm[h][p] is the channel of
+ *              head h at packed position p; [0, count[0]) is group 0.
+ * A row holds each group padded with 0 codes to 32-code blocks (layout of a
+ * block: soniq_layout), group 0 first; both groups together at most 256 codes.
+ */
+typedef struct soniq_kv_rows {
+    int32_t D;
+    int32_t n_groups;
+    int32_t count[2];
+    int32_t bits[2];
+    const int32_t *perm;
+} soniq_kv_rows;
+
+/*
+ * The cache: pages of `page_size` tokens (16, 32, 64, 128 or 256).  Token slot
+ * t is token t % page_size of page t / page_size.
+ *   k_codes    device [n_pages][heads][page_size][soniq_kv_row_bytes(&k)], 16-byte aligned.
+ *   k_scales   device [n_pages][heads][page_size][k.n_groups] of `dtype`, 16-byte aligned.
+ *   v_codes, v_scales   the same of the values.
+ *   dtype      SONIQ_OUT_F16 or SONIQ_OUT_BF16: type of keys, values, queries,
+ *              outputs and scales.
+ * Memory that no call has written may hold anything: slots that no sequence
+ * shows are not read into any result.
+ */
+typedef struct soniq_kv_cache {
+    int32_t heads;
+    int32_t page_size;
+    int64_t n_pages;
+    int32_t dtype;
+    soniq_kv_rows k, v;
+    uint8_t *k_codes;
+    void *k_scales;
+    uint8_t *v_codes;
+    void *v_scales;
+} soniq_kv_cache;
+
+/* Bytes of a packed row, a multiple of 16.  -1 on a bad argument.  Host only. */
+SONIQ_API int64_t soniq_kv_row_bytes(const soniq_kv_rows *rows);
+
+/* Checks the fields (not the device pointers); k_perm and v_perm, where not
+ * NULL, are host copies [heads][D] that must hold a permutation per head. */
+SONIQ_API soniq_status soniq_kv_validate(const soniq_kv_cache *cache, const int32_t *k_perm, const int32_t *v_perm);
+
+/*
+ * Quantizes n tokens' keys and values and writes them into their slots.
+ *   K, V       device, `dtype`; element (token i, head h, channel c) of K is
+ *              K[i * k_token_stride + h * k_head_stride + c] (strides in
+ *              elements, so slices of a fused projection need no copy).
+ *   slots      device int64 [n].  A negative slot skips its token; one at or
+ *              beyond n_pages * page_size is skipped and reported by
+ *              soniq_sync_status as SONIQ_ERR_INVALID_ARG.  Slots of one call
+ *              must differ.
+ * Accepted tokens of a drafted tree are moved by writing them again at their
+ * final slots: the same rows give the same bytes.
+ */
+SONIQ_API soniq_status soniq_kv_write(const soniq_kv_cache *cache, const void *K, int64_t k_token_stride,
+                                      int64_t k_head_stride, const void *V, int64_t v_token_stride,
+                                      int64_t v_head_stride, const int64_t *slots, int64_t n, soniq_stream_t stream);
+
+/*
+ * Reads slots back: the values their codes stand for, channels in their own
+ * order, each rounded once to `dtype` (a negative slot gives zeros, one beyond
+ * the cache zeros and the report above).
+ *   K          device out [n][heads][k.D], 2-byte aligned, or NULL.
+ *   V          device out [n][heads][v.D], or NULL.
+ */
+SONIQ_API soniq_status soniq_kv_read(const soniq_kv_cache *cache, const int64_t *slots, int64_t n, void *K, void *V,
+                                     soniq_stream_t stream);
+
+/*
+ * Attention of T query tokens of each of B sequences over the cache:
+ *   out[b][t][h] = sum_p softmax_p(scale * q[b][t][h] . k[p]) v[p]
+ * over the positions p that token t sees: every p < lengths[b] (the context),
+ * and len + j where it sees query token j of its own sequence (the T tokens'
+ * keys and values stand in the cache behind the context, written by
+ * soniq_kv_write).  Query head h reads key head h / (q_heads / heads).
+ * T = 1 is plain decoding; a mask describes a tree of drafted tokens (row t:
+ * its ancestors and itself); without one, token t sees tokens 0..t (a chain:
+ * a piece of a prompt).  A row that sees nothing is zero.
+ *   Q          device, `dtype`; strides in elements as for K above.
+ *   page_table device int32, row b at page_table + b * table_stride: the pages
+ *              of sequence b in order; max_pages entries can be read.  Entries
+ *              that the T + lengths[b] tokens do not reach may hold anything.
+ *              A page outside the cache counts as keys and values of zero and
+ *              is reported by soniq_sync_status (SONIQ_ERR_INVALID_ARG), as are
+ *              tokens beyond max_pages pages, which are not seen.
+ *   lengths    device int32 [B]; a negative length marks an absent sequence,
+ *              whose outputs are zero.
+ *   mask       NULL, or device bytes: query token t of sequence b sees query
+ *              token j where mask[b * mask_stride + t * T + j] is not 0.
+ *   out        device, contiguous [B][T][q_heads][v.D], 2-byte aligned.
+ *   scratch    device, 16-byte aligned, of soniq_kv_attend_scratch_bytes() (SONIQ_ERR_INVALID_ARG
+ *              otherwise).  Its first SONIQ_KV_SCRATCH_ZERO bytes must be zero
+ *              before the first use; every completed call leaves them zero.
+ *              Calls that may overlap on the GPU must use different scratch.
+ * Scores, statistics and sums are fp32; softmax weights (times the value
+ * scale, normalised by a power of two) are rounded to fp16 for the product.
+ */
+SONIQ_API soniq_status soniq_kv_attend(const soniq_kv_cache *cache, const void *Q, int64_t q_seq_stride,
+                                       int64_t q_token_stride, int64_t q_head_stride, const int32_t *page_table,
+                                       int64_t table_stride, int32_t max_pages, const int32_t *lengths,
+                                       const uint8_t *mask, int64_t mask_stride, int32_t B, int32_t T,
+                                       int32_t q_heads, float scale, void *out, void *scratch, size_t scratch_bytes,
+                                       soniq_stream_t stream);
+#define SONIQ_KV_SCRATCH_ZERO 8192
+
+/* Scratch bytes of soniq_kv_attend.  Host only; -1 on a bad argument. */
+SONIQ_API int64_t soniq_kv_attend_scratch_bytes(const soniq_kv_cache *cache, int32_t B, int32_t T, int32_t q_heads);
+
 /* Waits for `stream`, then returns SONIQ_ERR_TIMEOUT if any kernel of this
  * library on the current device recorded a timed-out wait since the last
- * call (and clears that record), SONIQ_ERR_CUDA on a CUDA error, else
+ * call (and clears that record), SONIQ_ERR_INVALID_ARG if none did but a
+ * slot or page outside its cache was met, SONIQ_ERR_CUDA on a CUDA error, else
  * SONIQ_OK.  When the timed-out wait was the grid barrier of
  * soniq_quantize_act_oneshot, it also waits for the whole device and then
  * resets that barrier. */

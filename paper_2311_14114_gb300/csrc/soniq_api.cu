@@ -651,7 +651,7 @@ soniq_status soniq_sync_status(soniq_stream_t stream) {
     }
     const unsigned zero = 0;
     if (cudaMemcpy(addr, &zero, sizeof(zero), cudaMemcpyHostToDevice) != cudaSuccess) return SONIQ_ERR_CUDA;
-    return SONIQ_ERR_TIMEOUT;
+    return (v & ~kErrKvIndex) ? SONIQ_ERR_TIMEOUT : SONIQ_ERR_INVALID_ARG;
 }
 
 void soniq_test_drop_barrier_arrival(int32_t armed) { g_drop_arrival.store(armed != 0 ? 1 : 0); }

@@ -42,10 +42,11 @@ soniq_status make_geom(const soniq_layout* L, int32_t taps, LayoutGeom* geo);
 
 // Device address of the library's error word on the current device (0 on failure).
 unsigned* device_error_word();
-// Bits of the device error word, by the kind of wait that ran out.
+// Bits of the device error word: the kind of wait that ran out, or a bad index met.
 constexpr unsigned kErrWait = 1u;             // a bounded mbarrier wait (tensor-core kernel, GEMV)
 constexpr unsigned kErrQuantBarrier = 2u;     // grid barrier of the one-pass quantize, caller scratch
 constexpr unsigned kErrOneshotBarrier = 4u;   // grid barrier of soniq_quantize_act_oneshot
+constexpr unsigned kErrKvIndex = 8u;          // a slot or page outside its key / value cache
 // Caller scratch of the one-pass per-tensor quantize: the barrier words in the
 // first 256 bytes, then the per-CTA maxima [kMaxGridPartials][2].
 constexpr int kMaxGridPartials = 1024;

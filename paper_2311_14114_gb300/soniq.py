@@ -8,6 +8,7 @@ no GPU is present the calls raise.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -36,7 +37,8 @@ EXPORTED = ["soniq_abi_version", "soniq_status_string", "soniq_group_codes",
             "soniq_pack_weights", "soniq_quantize_act", "soniq_quantize_act_scratch_bytes",
             "soniq_quantize_act_oneshot", "soniq_mp_gemm", "soniq_mp_gemm_path", "soniq_mp_gemm_kernel",
             "soniq_mp_gemm_scratch_bytes", "soniq_mp_conv2d", "soniq_mp_conv2d_scratch_bytes", "soniq_sync_status",
-            "soniq_test_drop_barrier_arrival"]
+            "soniq_test_drop_barrier_arrival", "soniq_kv_row_bytes", "soniq_kv_validate", "soniq_kv_write",
+            "soniq_kv_read", "soniq_kv_attend", "soniq_kv_attend_scratch_bytes"]
 
 _SCALE = {"tensor": SCALE_PER_TENSOR, "row": SCALE_PER_ROW, "calibrated": SCALE_CALIBRATED}
 
@@ -63,6 +65,18 @@ class CConvDesc(ctypes.Structure):
                 ("C_out", ctypes.c_int32), ("R", ctypes.c_int32), ("S", ctypes.c_int32),
                 ("stride_h", ctypes.c_int32), ("stride_w", ctypes.c_int32),
                 ("pad_h", ctypes.c_int32), ("pad_w", ctypes.c_int32)]
+
+
+class CKvRows(ctypes.Structure):
+    _fields_ = [("D", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("count", ctypes.c_int32 * 2),
+                ("bits", ctypes.c_int32 * 2), ("perm", ctypes.c_void_p)]
+
+
+class CKvCache(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("k", CKvRows), ("v", CKvRows),
+                ("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_codes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
 
 
 _lib = None
@@ -112,6 +126,19 @@ def lib() -> ctypes.CDLL:
         L.soniq_sync_status.restype = i32
         L.soniq_test_drop_barrier_arrival.argtypes = [i32]
         L.soniq_test_drop_barrier_arrival.restype = None
+        L.soniq_kv_row_bytes.argtypes = [P]
+        L.soniq_kv_row_bytes.restype = i64
+        L.soniq_kv_validate.argtypes = [P, P, P]
+        L.soniq_kv_validate.restype = i32
+        L.soniq_kv_write.argtypes = [P, P, i64, i64, P, i64, i64, P, i64, P]
+        L.soniq_kv_write.restype = i32
+        L.soniq_kv_read.argtypes = [P, P, i64, P, P, P]
+        L.soniq_kv_read.restype = i32
+        L.soniq_kv_attend.argtypes = [P, P, i64, i64, i64, P, i64, i32, P, P, i64, i32, i32, i32, ctypes.c_float, P, P,
+                                      ctypes.c_size_t, P]
+        L.soniq_kv_attend.restype = i32
+        L.soniq_kv_attend_scratch_bytes.argtypes = [P, i32, i32, i32]
+        L.soniq_kv_attend_scratch_bytes.restype = i64
         _lib = L
     return _lib
 
@@ -155,12 +182,17 @@ def _need(t: torch.Tensor, dtype, name: str):
 # graph's own memory instead: graphs that share a capture stream may be
 # replayed side by side, a later, larger call may replace the cached buffer,
 # and a zero fill that is captured happens only when its graph is replayed.  For
-# the quantize scratch that fill is part of the graph (8.4 KB, one node).
+# the quantize scratch that fill is part of the graph (8.4 KB, one node); of the
+# attention scratch only the leading counters are filled.
 _scratch = {}
+KV_SCRATCH_ZERO = 8192
 
 
 def _graph_scratch(nbytes: int, device, use: str) -> torch.Tensor:
-    return (torch.zeros if use == "quantize" else torch.empty)(nbytes, dtype=torch.uint8, device=device)
+    buf = (torch.zeros if use == "quantize" else torch.empty)(nbytes, dtype=torch.uint8, device=device)
+    if use == "kv":
+        buf[:KV_SCRATCH_ZERO].zero_()
+    return buf
 
 
 def _get_scratch(nbytes: int, device, stream, use: str) -> Optional[torch.Tensor]:
@@ -183,9 +215,9 @@ def _get_scratch(nbytes: int, device, stream, use: str) -> Optional[torch.Tensor
 
 
 def reset_scratch():
-    """Zero every cached quantize scratch buffer (needed after a SONIQ_ERR_TIMEOUT)."""
+    """Zero every cached scratch buffer that a call expects zeroed (needed after a SONIQ_ERR_TIMEOUT)."""
     for key, buf in _scratch.items():
-        if key[0] == "quantize":
+        if key[0] in ("quantize", "kv"):
             buf.zero_()
 
 
@@ -401,6 +433,147 @@ def mp_conv2d(layout: Layout, cd: CConvDesc, Xp: torch.Tensor, s_a: torch.Tensor
                                  ctypes.byref(next.c) if next is not None else None,
                                  _stream(stream)), "soniq_mp_conv2d")
     return Y
+
+
+class KVLayout:
+    """How the keys (or the values) of a cache are coded (soniq_kv_rows).
+
+    perm: int [heads][D], perm[h][p] the channel of head h at packed position
+    p; count: channels of the low and the high group; bits: their widths (2, 4
+    or 8)."""
+
+    def __init__(self, perm, count: Sequence[int], bits: Sequence[int]):
+        perm_t = torch.as_tensor(perm, dtype=torch.int32).cpu().contiguous()
+        if perm_t.dim() != 2:
+            raise ValueError("perm must be [heads][D]")
+        self.heads, self.D = int(perm_t.shape[0]), int(perm_t.shape[1])
+        self.count = [int(c) for c in list(count)[:2]] + [0] * (2 - len(count))
+        self.bits = [int(b) for b in list(bits)[:2]] + [8] * (2 - len(bits))
+        self.n_groups = 2 if self.count[1] != 0 else 1
+        self.perm_host = perm_t.numpy().copy()
+        self.row_bytes = int(lib().soniq_kv_row_bytes(ctypes.byref(self.rows(None))))
+        if self.row_bytes < 0:
+            raise SoniqError(SONIQ_ERR_INVALID_ARG, "soniq_kv_row_bytes")
+
+    def rows(self, perm: Optional[torch.Tensor]) -> CKvRows:
+        """soniq_kv_rows with the permutation `perm` in device memory."""
+        return CKvRows(self.D, self.n_groups, (ctypes.c_int32 * 2)(*self.count), (ctypes.c_int32 * 2)(*self.bits),
+                       _ptr(perm))
+
+
+class KVCache:
+    """Pages of quantized keys and values (soniq_kv_cache) and their memory.
+
+    k_codes, v_codes: uint8 [n_pages][heads][page_size][row bytes]; k_scales,
+    v_scales: dtype [n_pages][heads][page_size][groups].  Token slot t is token
+    t % page_size of page t // page_size."""
+
+    def __init__(self, k: KVLayout, v: KVLayout, n_pages: int, page_size: int, dtype=torch.float16, device="cuda"):
+        if dtype not in (torch.float16, torch.bfloat16):
+            raise ValueError("dtype must be torch.float16 or torch.bfloat16")
+        if k.heads != v.heads:
+            raise ValueError("keys and values have different numbers of heads")
+        self.k, self.v, self.dtype = k, v, dtype
+        self.heads, self.n_pages, self.page_size = k.heads, int(n_pages), int(page_size)
+        c = CKvCache(self.heads, self.page_size, self.n_pages, OUT_BF16 if dtype == torch.bfloat16 else OUT_F16,
+                     k.rows(None), v.rows(None))
+        _check(lib().soniq_kv_validate(ctypes.byref(c), k.perm_host.ctypes.data_as(ctypes.c_void_p),
+                                       v.perm_host.ctypes.data_as(ctypes.c_void_p)), "soniq_kv_validate")
+        for side, lay in (("k", k), ("v", v)):
+            lead = (self.n_pages, self.heads, self.page_size)
+            mem = {"perm": torch.from_numpy(lay.perm_host).to(device),
+                   "codes": torch.zeros(lead + (lay.row_bytes,), dtype=torch.uint8, device=device),
+                   "scales": torch.zeros(lead + (lay.n_groups,), dtype=dtype, device=device)}
+            for name, t in mem.items():
+                setattr(self, f"{side}_{name}", t)
+            setattr(c, side, lay.rows(mem["perm"]))
+            setattr(c, side + "_codes", mem["codes"].data_ptr())
+            setattr(c, side + "_scales", mem["scales"].data_ptr())
+        self.c = c
+        self.ref = ctypes.byref(c)
+
+
+def _new(shape, dtype, device, stream) -> torch.Tensor:
+    """An output of a call on `stream`, from that stream's memory."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _need_rows(t: torch.Tensor, cache: KVCache, shape: tuple, name: str):
+    if not t.is_cuda or t.dtype != cache.dtype or tuple(t.shape) != shape or (t.stride(-1) != 1 and shape[-1] > 1):
+        raise ValueError(f"{name} must be a CUDA {cache.dtype} tensor {list(shape)} with contiguous channels")
+
+
+def kv_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
+    """soniq_kv_write: quantizes keys [n][heads][D] and values [n][heads][Dv]
+    (any token and head strides) into the slots (int64 [n]; negative: skipped)."""
+    _need(slots, torch.int64, "slots")
+    n = slots.numel()
+    _need_rows(k, cache, (n, cache.heads, cache.k.D), "k")
+    _need_rows(v, cache, (n, cache.heads, cache.v.D), "v")
+    _check(lib().soniq_kv_write(cache.ref, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
+                                v.stride(1), slots.data_ptr(), n, _stream(stream)), "soniq_kv_write")
+
+
+def kv_read(cache: KVCache, slots: torch.Tensor, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+            stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """soniq_kv_read: the keys [n][heads][D] and values [n][heads][Dv] that the slots hold."""
+    _need(slots, torch.int64, "slots")
+    n = slots.numel()
+    if k is None:
+        k = _new((n, cache.heads, cache.k.D), cache.dtype, slots.device, stream)
+    if v is None:
+        v = _new((n, cache.heads, cache.v.D), cache.dtype, slots.device, stream)
+    for t, lay, name in ((k, cache.k, "k"), (v, cache.v, "v")):
+        _need(t, cache.dtype, name)
+        if t.numel() != n * cache.heads * lay.D:
+            raise ValueError(f"{name} must hold [{n}][{cache.heads}][{lay.D}]")
+    _check(lib().soniq_kv_read(cache.ref, slots.data_ptr(), n, k.data_ptr(), v.data_ptr(), _stream(stream)),
+           "soniq_kv_read")
+    return k, v
+
+
+def kv_attend(cache: KVCache, q: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
+              mask: Optional[torch.Tensor] = None, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+              stream=None) -> torch.Tensor:
+    """soniq_kv_attend: attention of q [B][T][q_heads][D] over each sequence's
+    cached context (lengths, int32 [B]; negative: absent) and those of the T
+    tokens behind it that mask (bool [B][T][T] or [T][T]; None: a chain) shows.
+    page_table: int32 [B][pages].  scale: 1 / sqrt(D) if left out."""
+    if q.dim() != 4:
+        raise ValueError("q must be [B][T][q_heads][D]")
+    B, T, Hq, D = q.shape
+    _need_rows(q, cache, (B, T, Hq, cache.k.D), "q")
+    if Hq % cache.heads != 0:
+        raise ValueError("q_heads must be a multiple of the cache's heads")
+    _need(lengths, torch.int32, "lengths")
+    if not page_table.is_cuda or page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != B \
+            or (page_table.stride(1) != 1 and page_table.shape[1] > 1) or lengths.numel() != B:
+        raise ValueError("page_table must be a CUDA int32 tensor [B][pages] and lengths [B]")
+    mask_ptr, mask_stride = None, 0
+    if mask is not None:
+        if not mask.is_cuda or mask.dtype not in (torch.bool, torch.uint8) or tuple(mask.shape[-2:]) != (T, T) \
+                or mask.dim() not in (2, 3) or (mask.dim() == 3 and mask.shape[0] != B):
+            raise ValueError("mask must be a CUDA bool tensor [B][T][T] or [T][T]")
+        if not (mask.stride(-1) == 1 or T == 1) or not (mask.stride(-2) == T or T == 1):
+            raise ValueError("each sequence's mask must be contiguous")
+        mask_ptr, mask_stride = mask.data_ptr(), mask.stride(0) if mask.dim() == 3 else 0
+    if out is None:
+        out = _new((B, T, Hq, cache.v.D), cache.dtype, q.device, stream)
+    else:
+        _need(out, cache.dtype, "out")
+        if out.numel() != B * T * Hq * cache.v.D:
+            raise ValueError(f"out must hold [{B}][{T}][{Hq}][{cache.v.D}]")
+    L = lib()
+    need = int(L.soniq_kv_attend_scratch_bytes(cache.ref, B, T, Hq))
+    scratch = _get_scratch(need, q.device, stream, "kv")
+    _check(L.soniq_kv_attend(cache.ref, q.data_ptr(), q.stride(0), q.stride(1), q.stride(2), page_table.data_ptr(),
+                             page_table.stride(0), page_table.shape[1], lengths.data_ptr(), mask_ptr, mask_stride, B, T,
+                             Hq, 1.0 / math.sqrt(D) if scale is None else float(scale), out.data_ptr(),
+                             _ptr(scratch), max(need, 0), _stream(stream)), "soniq_kv_attend")
+    return out
 
 
 def sync_status(stream=None) -> int:
