@@ -39,25 +39,32 @@ constexpr int kChunk = 32;                   // tokens a warp takes at a time
 constexpr int kMergeBytes = 32768;           // outputs of all warps, in as many passes as they need
 constexpr float kLog2e = 1.4426950408889634f;
 
+// How a warp copies 16 packed rows of one side into shared rows whose stride is
+// an odd multiple of 16 bytes (so that lanes reading one place of eight rows
+// meet eight bank groups).  Rows of an odd number of 16-byte pieces go as one
+// run; others with 2^shift >= pieces lanes to a row.
+struct CopyPlan {
+    int stride;          // bytes of a shared row
+    int shift;           // -1: one run
+    int iters, dst_step, src_step;
+    uint32_t page_bytes;         // codes of one page (all heads)
+    uint32_t page_scales;        // scales of one page, bytes
+};
+
 struct RowsPlan {
     int row_tiles;        // tiles of 8 NT query rows per key head
     int rows;             // query rows per key head: T * group
     int stages;
     int stage_bytes;
-    int k_stride, v_stride;      // shared row strides: odd multiples of 16 bytes (no bank conflicts)
+    CopyPlan cp[2];
     int v_off, ks_off, vs_off;   // in a stage
-    int merge_off, q_off, misc_off;
+    int f_off;            // fp32 scales of a warp's chunk, behind its stages
+    int warp_bytes;       // a warp's stages and scales
+    int q_off, misc_off;
     int smem;
     int min_chunks;       // fewest chunks worth a CTA
-    uint32_t k_magic, v_magic;   // ceil(2^16 / 16-byte pieces of a row): pieces are numbered below 512
 };
 
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool on) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp4(uint32_t dst, const void* src, bool on) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(on ? 4 : 0) : "memory");
-}
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 // All but the newest `newer` groups of this thread have landed.
 __device__ __forceinline__ void cp_wait(int newer) {
@@ -67,8 +74,8 @@ __device__ __forceinline__ void cp_wait(int newer) {
 }
 
 __device__ __forceinline__ uint32_t lds16(uint32_t a) {
-    uint16_t v;
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
+    uint32_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
     return v;
 }
 __device__ __forceinline__ uint32_t lds8(uint32_t a) {
@@ -90,6 +97,15 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
     uint4 v;
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
     return v;
+}
+
+__device__ __forceinline__ float4 lds128f(uint32_t a) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts128f(uint32_t a, float x, float y, float z, float w) {
+    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(x), "f"(y), "f"(z), "f"(w) : "memory");
 }
 
 // d (16 x 8, fp32) += a (16 x 16) b (16 x 8)
@@ -124,32 +140,30 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 // The key side: a quad's lane l holds 8 codes of a block as four half pairs
 // h[0..3].  Codes of h[i] and the powers of two their place gives them:
 __device__ __forceinline__ int key_code(int bits, int l, int i, int half) {
-    if (bits == 8) return 8 * l + 2 * i + half;
+    if (bits == 8) return 8 * l + 4 * (i >> 1) + (i & 1) + 2 * half;
     if (bits == 4) return 8 * l + 4 * (i & 1) + (i >> 1) + 2 * half;
     return 16 * (l >> 1) + 4 * i + 2 * (l & 1) + half;
 }
 __device__ __forceinline__ int place_log2(int bits, int i) { return bits == 8 ? 0 : (bits == 4 ? 4 * (i & 1) : 2 * i); }
 
-// ... as u 2^-24 times the place's power, from the block at shared address `at`.
+// ... as u 2^-24 times the place's power; `at`: the lane's bytes of the block.
 template <int BITS>
-__device__ __forceinline__ void key_halves(uint32_t at, int l, uint32_t (&h)[4]) {
+__device__ __forceinline__ void key_halves(uint32_t at, uint32_t (&h)[4]) {
     if constexpr (BITS == 8) {
-        uint2 w = lds64(at + 8 * l);
-        w.x ^= 0x80808080u;
-        w.y ^= 0x80808080u;
-        h[0] = __byte_perm(w.x, 0, 0x4140);
-        h[1] = __byte_perm(w.x, 0, 0x4342);
-        h[2] = __byte_perm(w.y, 0, 0x4140);
-        h[3] = __byte_perm(w.y, 0, 0x4342);
+        const uint2 w = lds64(at);
+        h[0] = (w.x & 0x00FF00FFu) ^ 0x00800080u;
+        h[1] = ((w.x >> 8) & 0x00FF00FFu) ^ 0x00800080u;
+        h[2] = (w.y & 0x00FF00FFu) ^ 0x00800080u;
+        h[3] = ((w.y >> 8) & 0x00FF00FFu) ^ 0x00800080u;
     } else if constexpr (BITS == 4) {
-        uint32_t w = lds32(at + 4 * l);
+        uint32_t w = lds32(at);
         h[0] = (w & 0x000F000Fu) ^ 0x00080008u;
         h[1] = (w & 0x00F000F0u) ^ 0x00800080u;
         w >>= 8;
         h[2] = (w & 0x000F000Fu) ^ 0x00080008u;
         h[3] = (w & 0x00F000F0u) ^ 0x00800080u;
     } else {
-        const uint32_t w = __byte_perm(lds16(at + 2 * l), 0, 0x4140);
+        const uint32_t w = __byte_perm(lds16(at), 0, 0x4140);
         h[0] = (w & 0x00030003u) ^ 0x00020002u;
         h[1] = (w & 0x000C000Cu) ^ 0x00080008u;
         h[2] = (w & 0x00300030u) ^ 0x00200020u;
@@ -158,7 +172,8 @@ __device__ __forceinline__ void key_halves(uint32_t at, int l, uint32_t (&h)[4])
 }
 
 // The value side: lane group g of a warp holds 4 codes of a block, each as the
-// pair (token t, token t + 1), signed, times the place's power.
+// pair (token t, token t + 1), signed, times the place's power; row0, row1: its
+// bytes of the block in the two rows.
 __device__ __forceinline__ int value_code(int bits, int g, int i) {
     if (bits == 8) return 4 * g + i;
     if (bits == 4) return 8 * (g >> 1) + 2 * (g & 1) + 4 * (i & 1) + (i >> 1);
@@ -166,22 +181,22 @@ __device__ __forceinline__ int value_code(int bits, int g, int i) {
 }
 
 template <int BITS>
-__device__ __forceinline__ void value_pairs(uint32_t row0, uint32_t row1, int g, uint32_t (&x)[4]) {
+__device__ __forceinline__ void value_pairs(uint32_t row0, uint32_t row1, uint32_t (&x)[4]) {
     if constexpr (BITS == 8) {
-        const uint32_t a = lds32(row0 + 4 * g), b = lds32(row1 + 4 * g);
+        const uint32_t a = lds32(row0), b = lds32(row1);
         x[0] = sub2((__byte_perm(a, b, 0x4400) & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);
         x[1] = sub2((__byte_perm(a, b, 0x5511) & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);
         x[2] = sub2((__byte_perm(a, b, 0x6622) & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);
         x[3] = sub2((__byte_perm(a, b, 0x7733) & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);
     } else if constexpr (BITS == 4) {
-        uint32_t w = __byte_perm(lds16(row0 + 2 * g), lds16(row1 + 2 * g), 0x5410);
+        uint32_t w = __byte_perm(lds16(row0), lds16(row1), 0x5410);
         x[0] = sub2((w & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);
         x[1] = sub2((w & 0x00F000F0u) ^ 0x64806480u, 0x64806480u);
         w >>= 8;
         x[2] = sub2((w & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);
         x[3] = sub2((w & 0x00F000F0u) ^ 0x64806480u, 0x64806480u);
     } else {
-        const uint32_t w = __byte_perm(lds8(row0 + g), lds8(row1 + g), 0x5410);
+        const uint32_t w = __byte_perm(lds8(row0), lds8(row1), 0x5410);
         x[0] = sub2((w & 0x00030003u) ^ 0x64026402u, 0x64026402u);
         x[1] = sub2((w & 0x000C000Cu) ^ 0x64086408u, 0x64086408u);
         x[2] = sub2((w & 0x00300030u) ^ 0x64206420u, 0x64206420u);
@@ -211,7 +226,9 @@ __device__ __forceinline__ int chunks_of(const KvGeom& geo, const KvAttendArgs& 
 template <int NT, int NVB>
 constexpr int min_ctas() { return NT * NVB <= 4 ? 2 : 1; }
 
-template <int NT, int NVB>
+// WIDE: group 0 of both sides has 4-bit codes and group 1, where there is one,
+// 8-bit codes; otherwise the widths are looked up block by block.
+template <int NT, int NVB, bool WIDE>
 __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(const KvGeom geo, const KvAttendArgs a,
                                                                           const RowsPlan pl) {
     extern __shared__ __align__(128) uint8_t smem[];
@@ -222,8 +239,8 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
     const int nkb = ks.nb[0] + ks.nb[1], nvb = vs.nb[0] + vs.nb[1];
     const bool bf16 = geo.bf16 != 0;
     const uint32_t smem0 = tc::smem_u32(smem);
-    const uint32_t ring = smem0 + warp * pl.stages * pl.stage_bytes;
-    float* merge = reinterpret_cast<float*>(smem + pl.merge_off);
+    const uint32_t ring = smem0 + warp * pl.warp_bytes, fsc = ring + pl.f_off;
+    float* merge = reinterpret_cast<float*>(smem);       // over the rings, which are empty when it is used
     // misc: per (row, group) start value, per row factor, the warps' statistics, the head's value channels
     float* sm_init = reinterpret_cast<float*>(smem + pl.misc_off);   // [2][R]
     float* sm_fac = sm_init + 2 * R;                                 // [R]
@@ -287,8 +304,29 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
         __syncthreads();
     }
 
+    // ---- what a lane copies of 16 rows: its first piece, and its bound on piece numbers ----
+    uint32_t cp_dst[2];
+    int cp_src[2], cp_lim[2];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        const CopyPlan& cp = pl.cp[side];
+        const int pr = geo.s[side].row_bytes >> 4;
+        if (cp.shift < 0) {
+            cp_dst[side] = 16 * lane;
+            cp_src[side] = 16 * lane;
+            cp_lim[side] = 16 * pr;
+        } else {
+            const int row = lane >> cp.shift, col = lane & ((1 << cp.shift) - 1);
+            cp_dst[side] = row * cp.stride + 16 * col;
+            cp_src[side] = (row * pr + col) * 16;
+            cp_lim[side] = col < pr ? 32 * cp.iters : 0;
+        }
+    }
+
     const int qh = geo.heads * a.group;
     const int n_min = ks.ng == 2 && ks.bits[1] < ks.bits[0] ? ks.bits[1] : ks.bits[0];
+    const uint32_t k_lane = g * pl.cp[0].stride + (WIDE ? 4 * l : 0);
+    const uint32_t v_lane = pl.v_off + 2 * l * pl.cp[1].stride + (WIDE ? 2 * g : 0);
     int b = sm_b;
     long long base = sm_base;        // first chunk of sequence b
     long long pos = lo;
@@ -309,45 +347,49 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
         const int row0 = rt * R;
         const int32_t* table = a.table + b * a.table_stride;
 
-        // ---- loads: chunk c into a stage of this warp's ring ----
-        auto page_of = [&](int p) -> int { return p < end ? __ldg(table + (p >> geo.page_shift)) : -1; };
-        auto issue = [&](int c, int stage, int pg0, int pg1) {
-            const int p0 = c * kChunk;
-            const uint32_t st = ring + stage * pl.stage_bytes;
-            const bool on0 = pg0 >= 0 && pg0 < geo.n_pages, on1 = pg1 >= 0 && pg1 < geo.n_pages;
-            if ((!on0 && p0 < end) || (!on1 && p0 + 16 < end)) {
-                if (lane == 0) atomicOr(a.err, kErrKvIndex);
-            }
-            const int in0 = p0 & (geo.page - 1), in1 = (p0 + 16) & (geo.page - 1);
-            const int64_t r0 = on0 ? ((int64_t)pg0 * geo.heads + head) * geo.page + in0 : 0;
-            // rows 16.. of the chunk as if it went on from there
-            const int64_t r1 = on1 ? ((int64_t)pg1 * geo.heads + head) * geo.page + in1 - 16 : 0;
+        // ---- loads: chunk c into a stage of this warp's ring, as two halves of 16 rows ----
+        const uint8_t *src[2], *ssrc[2];       // page 0's rows of this head, this lane's first piece
 #pragma unroll
-            for (int side = 0; side < 2; ++side) {
-                const KvSide& s = side ? vs : ks;
-                const int pr = s.row_bytes >> 4;
-                const uint32_t magic = side ? pl.v_magic : pl.k_magic;
-                const uint8_t* src0 = s.codes + r0 * s.row_bytes;
-                const uint8_t* src1 = s.codes + (on1 ? r1 * s.row_bytes : 0);
-                const int pad = (side ? pl.v_stride : pl.k_stride) - s.row_bytes;   // 0 or 16
-                const uint32_t dst = st + (side ? pl.v_off : 0);
-#pragma unroll 4
-                for (int k = 0; k < pr; ++k) {
-                    const int i = lane + 32 * k;
-                    const int row = (int)((uint32_t)i * magic >> 16);
-                    const bool second = row >= 16;
-                    const bool on = second ? on1 : on0;
-                    cp16(dst + 16 * i + pad * row, (second ? src1 : src0) + (on ? 16 * i : 0), on);
-                }
-                const uint32_t sd = st + (side ? pl.vs_off : pl.ks_off);
-                if (s.ng == 2) {
-                    const bool second = lane >= 16, on = second ? on1 : on0;
-                    cp4(sd + 4 * lane, s.scales + (on ? ((second ? r1 : r0) + lane) * 2 : 0), on);
-                } else if (lane < 16) {
-                    const bool second = lane >= 8, on = second ? on1 : on0;
-                    cp4(sd + 4 * lane, s.scales + (on ? (second ? r1 : r0) + 2 * lane : 0), on);
+        for (int side = 0; side < 2; ++side) {
+            const KvSide& s = geo.s[side];
+            src[side] = s.codes + (int64_t)head * geo.page * s.row_bytes + cp_src[side];
+            ssrc[side] = reinterpret_cast<const uint8_t*>(s.scales) + (int64_t)head * geo.page * 2 * s.ng + 4 * (lane & 15);
+        }
+        auto page_of = [&](int p) -> int { return p < end ? __ldg(table + (p >> geo.page_shift)) : -1; };
+        auto issue = [&](int c, uint32_t st, int pg0, int pg1) {
+            const int p0 = c * kChunk;
+            bool bad = false;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int pg = half ? pg1 : pg0;
+                const bool on = (unsigned)pg < (unsigned)geo.n_pages;
+                bad |= !on && p0 + 16 * half < end;
+                const int in = (p0 + 16 * half) & (geo.page - 1);
+                const uint32_t use = on ? (uint32_t)pg : 0u;
+                const int size = on ? 16 : 0;
+#pragma unroll
+                for (int side = 0; side < 2; ++side) {
+                    const CopyPlan& cp = pl.cp[side];
+                    const KvSide& s = geo.s[side];
+                    const uint8_t* p = src[side] + (uint64_t)use * cp.page_bytes + in * s.row_bytes;
+                    uint32_t dst = st + (side ? pl.v_off : 0) + half * 16 * cp.stride + cp_dst[side];
+                    int i = lane;
+#pragma unroll 2
+                    for (int k = 0; k < cp.iters; ++k) {
+                        if (i < cp_lim[side])
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(p), "r"(size) : "memory");
+                        i += 32;
+                        dst += cp.dst_step;
+                        p += cp.src_step;
+                    }
+                    // 16 tokens' scales: 2 or 4 bytes each
+                    if (lane < 8 * s.ng)
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(st + (side ? pl.vs_off : pl.ks_off) + (half * 8 * s.ng + lane) * 4),
+                                     "l"(ssrc[side] + (uint64_t)use * cp.page_scales + in * 2 * s.ng), "r"(size >> 2)
+                                     : "memory");
                 }
             }
+            if (bad && lane == 0) atomicOr(a.err, kErrKvIndex);
         };
         // page ids are read one issue ahead of their use
         int c_load = c_first + warp, n_pg0 = -1, n_pg1 = -1;
@@ -362,7 +404,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
             const int pg0 = n_pg0, pg1 = n_pg1, c = c_load;
             c_load += n_warps;
             fetch_pages(c_load);
-            if (c < c_end) issue(c, s, pg0, pg1);
+            if (c < c_end) issue(c, ring + s * pl.stage_bytes, pg0, pg1);
             cp_commit();
         }
 
@@ -377,25 +419,20 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
                 const int32_t* perm = ks.perm + head * ks.D;
                 float x[8];
                 uint32_t top = 0;
-                int code[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     x[k] = 0.0f;
-                    code[k] = 0;
                     if (k < nkb) {
                         const int grp = k < ks.nb[0] ? 0 : 1;
                         const int c = key_code(ks.bits[grp], lane >> 3, (lane & 7) >> 1, lane & 1);
                         const int p = 32 * (grp ? k - ks.nb[0] : k) + c;
-                        if (on && p < ks.count[grp]) {
-                            const uint16_t v = q[perm[(grp ? ks.count[0] : 0) + p]];
-                            x[k] = scale_of(v, bf16);
-                        }
+                        if (on && p < ks.count[grp]) x[k] = scale_of(q[perm[(grp ? ks.count[0] : 0) + p]], bf16);
                         top = max(top, __float_as_uint(x[k]) & 0x7FFFFFFFu);
                     }
                 }
                 top = __reduce_max_sync(0xffffffffu, top);
                 const int e = top == 0 ? 0 : min(13 - ((int)(top >> 23) - 127), 120);   // x 2^e: largest in [2^13, 2^14)
-                const float up = pow2(e);
+                const float up = a.scale < 0.0f ? -pow2(e) : pow2(e);
                 float sum0 = 0.0f, sum1 = 0.0f;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
@@ -417,7 +454,8 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
                 if (lane == 0) {
                     sm_init[r] = -sum0;
                     sm_init[R + r] = -sum1;
-                    sm_fac[r] = ldexpf(a.scale * kLog2e, 24 - (n_min - 1) - e);
+                    // positive, so that it can be applied behind the maximum
+                    sm_fac[r] = fmaxf(ldexpf(fabsf(a.scale) * kLog2e, 24 - (n_min - 1) - e), 0x1p-126f);
                 }
             }
             for (int p = tid; p < 32 * NVB; p += blockDim.x) {
@@ -429,14 +467,13 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
         }
         __syncthreads();
 
-        float init0[NT][2], init1[NT][2], fac[NT][2], m[NT][2], lsum[NT][2];
+        // running maximum (of scores before the row's factor), sum and outputs
+        float fac[NT][2], m[NT][2], lsum[NT][2];
         float o[NVB][2][NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-                init0[nt][r] = sm_init[8 * nt + 2 * l + r];
-                init1[nt][r] = sm_init[R + 8 * nt + 2 * l + r];
                 fac[nt][r] = sm_fac[8 * nt + 2 * l + r];
                 m[nt][r] = -INFINITY;
                 lsum[nt][r] = 0.0f;
@@ -453,7 +490,9 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
         int e0 = -100, e1 = -100;     // running powers of two above the value scales
 
         const uint32_t qbase = smem0 + pl.q_off + lane * 16;
-        int stage = 0, load_stage = pl.stages - 1;
+        const int sure = min(len, end);
+        uint32_t st = ring, st_load = ring + (pl.stages - 1) * pl.stage_bytes;
+        const uint32_t ring_end = ring + pl.stages * pl.stage_bytes;
         for (int c = c_first + warp; c < c_end; c += n_warps) {
             cp_wait(pl.stages - 2);
             __syncwarp();
@@ -461,89 +500,132 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
                 const int pg0 = n_pg0, pg1 = n_pg1, cl = c_load;
                 c_load += n_warps;
                 fetch_pages(c_load);
-                if (cl < c_end) issue(cl, load_stage, pg0, pg1);
+                if (cl < c_end) issue(cl, st_load, pg0, pg1);
                 cp_commit();
-                if (++load_stage == pl.stages) load_stage = 0;
+                st_load += pl.stage_bytes;
+                if (st_load == ring_end) st_load = ring;
             }
-            const uint32_t st = ring + stage * pl.stage_bytes;
-            if (++stage == pl.stages) stage = 0;
             const int p0 = c * kChunk;
-            const bool tail = p0 + kChunk > min(len, end);      // some rows may not see some of it
+            const bool tail = p0 + kChunk > sure;      // some rows may not see some of it
+
+            // ---- scales: lane = token; as fp32 for all lanes, the values' relative to the running power of two ----
+            {
+                float k0, k1 = 0.0f, v0, v1 = 0.0f;
+                if (ks.ng == 2) {
+                    const uint32_t w = lds32(st + pl.ks_off + 4 * lane);
+                    k0 = scale_of(w & 0xFFFFu, bf16);
+                    k1 = scale_of(w >> 16, bf16);
+                } else {
+                    k0 = scale_of(lds16(st + pl.ks_off + 2 * lane), bf16);
+                }
+                if (vs.ng == 2) {
+                    const uint32_t w = lds32(st + pl.vs_off + 4 * lane);
+                    v0 = scale_of(w & 0xFFFFu, bf16);
+                    v1 = scale_of(w >> 16, bf16);
+                } else {
+                    v0 = scale_of(lds16(st + pl.vs_off + 2 * lane), bf16);
+                }
+                if (tail && p0 + lane >= end) k0 = k1 = v0 = v1 = 0.0f;
+                // positive floats order as integers; the exponent plus one bounds them
+                const int n0 = max(e0, min((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(v0)) >> 23) - 126, 126));
+                int n1 = e1;
+                if (vs.ng == 2) n1 = max(e1, min((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(v1)) >> 23) - 126, 126));
+                if (n0 > e0 || n1 > e1) {
+                    const float d0 = n0 - e0 > 126 ? 0.0f : pow2(e0 - n0), d1 = n1 - e1 > 126 ? 0.0f : pow2(e1 - n1);
+                    e0 = n0;
+                    e1 = n1;
+#pragma unroll
+                    for (int v = 0; v < NVB; ++v)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) o[v][u][nt][i] *= v < vs.nb[0] ? d0 : d1;
+                }
+                sts128f(fsc + 16 * lane, k0, k1, v0 * pow2(-e0), v1 * pow2(-e1));
+                __syncwarp();
+            }
+            float4 sc[4];      // of tokens g, g + 8, g + 16, g + 24
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sc[j] = lds128f(fsc + 16 * (8 * j + g));
 
             // ---- scores ----
             float x[2][NT][4];
+            const uint32_t krow = st + k_lane;
+            auto key_block = [&](auto width, float(&acc)[2][NT][4], uint32_t at, uint32_t qat) {
+                constexpr int BITS = decltype(width)::value;
+                uint4 q[NT];
 #pragma unroll
-            for (int grp = 0; grp < 2; ++grp) {
-                if (grp == 1 && ks.ng == 1) break;
-                float acc[2][NT][4];
+                for (int nt = 0; nt < NT; ++nt) q[nt] = lds128(qat + nt * 512);
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt) {
+                    uint32_t h[4], k[4];
+                    key_halves<BITS>(at + 16 * mt * pl.cp[0].stride, h);
+                    key_halves<BITS>(at + (16 * mt + 8) * pl.cp[0].stride, k);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        mma(acc[mt][nt], h[0], k[0], h[1], k[1], q[nt].x, q[nt].y);
+                        mma(acc[mt][nt], h[2], k[2], h[3], k[3], q[nt].z, q[nt].w);
+                    }
+                }
+            };
+            auto key_group = [&](auto width, int grp, float(&acc)[2][NT][4]) {
+                constexpr int BITS = decltype(width)::value;
+                float init[NT][2];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) init[nt][r] = sm_init[grp * R + 8 * nt + 2 * l + r];
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[mt][nt][i] = grp ? init1[nt][i & 1] : init0[nt][i & 1];
-                const int bits = ks.bits[grp], nb = ks.nb[grp];
-                const uint32_t krow = st + g * pl.k_stride + ks.off[grp];
-                const uint32_t qb = qbase + (grp ? ks.nb[0] : 0) * NT * 512;
-                auto block = [&](auto width, int blk) {
-                    constexpr int BITS = decltype(width)::value;
-                    uint4 q[NT];
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) q[nt] = lds128(qb + (blk * NT + nt) * 512);
-#pragma unroll
-                    for (int mt = 0; mt < 2; ++mt) {
-                        uint32_t h[4], k[4];
-                        const uint32_t at = krow + 16 * mt * pl.k_stride + 4 * BITS * blk;
-                        key_halves<BITS>(at, l, h);
-                        key_halves<BITS>(at + 8 * pl.k_stride, l, k);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            mma(acc[mt][nt], h[0], k[0], h[1], k[1], q[nt].x, q[nt].y);
-                            mma(acc[mt][nt], h[2], k[2], h[3], k[3], q[nt].z, q[nt].w);
-                        }
-                    }
-                };
-                if (bits == 4) {
-                    for (int blk = 0; blk < nb; ++blk) block(std::integral_constant<int, 4>{}, blk);
-                } else if (bits == 8) {
-                    for (int blk = 0; blk < nb; ++blk) block(std::integral_constant<int, 8>{}, blk);
-                } else {
-                    for (int blk = 0; blk < nb; ++blk) block(std::integral_constant<int, 2>{}, blk);
+                        for (int i = 0; i < 4; ++i) acc[mt][nt][i] = init[nt][i & 1];
+                // a quad's lane starts BITS bytes behind the one before; krow has 4 of them where WIDE
+                uint32_t at = krow + ks.off[grp] + (WIDE ? (BITS == 8 ? 4 * l : 0) : BITS * l);
+                uint32_t qat = qbase + (grp ? ks.nb[0] : 0) * NT * 512;
+                for (int blk = 0; blk < ks.nb[grp]; ++blk) {
+                    key_block(width, acc, at, qat);
+                    at += 4 * BITS;
+                    qat += NT * 512;
                 }
+            };
+            auto key_any = [&](int grp, float(&acc)[2][NT][4]) {
+                if constexpr (WIDE) {
+                    if (grp) key_group(std::integral_constant<int, 8>{}, grp, acc);
+                    else key_group(std::integral_constant<int, 4>{}, grp, acc);
+                } else {
+                    if (ks.bits[grp] == 4) key_group(std::integral_constant<int, 4>{}, grp, acc);
+                    else if (ks.bits[grp] == 8) key_group(std::integral_constant<int, 8>{}, grp, acc);
+                    else key_group(std::integral_constant<int, 2>{}, grp, acc);
+                }
+            };
+            key_any(0, x);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {      // tokens 8 j + g
-                    const int tok = 8 * j + g;
-                    float s = scale_of(lds16(st + pl.ks_off + 2 * (tok * ks.ng + grp)), bf16);
-                    if (tail && p0 + tok >= end) s = 0.0f;
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[mt][nt][i] *= sc[2 * mt + (i >> 1)].x;
+            if (ks.ng == 2) {
+                float acc[2][NT][4];
+                key_any(1, acc);
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int r = 0; r < 2; ++r) {
-                            const float v = acc[j >> 1][nt][2 * (j & 1) + r];
-                            float& d = x[j >> 1][nt][2 * (j & 1) + r];
-                            d = grp ? fmaf(v, s, d) : v * s;
-                        }
-                }
+                        for (int i = 0; i < 4; ++i) x[mt][nt][i] = fmaf(acc[mt][nt][i], sc[2 * mt + (i >> 1)].y, x[mt][nt][i]);
             }
 
             // ---- softmax ----
-            float vsc[2][4];
+            if (tail) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int tok = 8 * j + g;
-                const bool gone = tail && p0 + tok >= end;
-                vsc[0][j] = gone ? 0.0f : scale_of(lds16(st + pl.vs_off + 2 * (tok * vs.ng)), bf16);
-                vsc[1][j] = gone || vs.ng == 1 ? 0.0f : scale_of(lds16(st + pl.vs_off + 2 * (tok * vs.ng) + 2), bf16);
-            }
-            float top[NT][2];
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    top[nt][r] = -INFINITY;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[j >> 1][nt][2 * (j & 1) + r] *= fac[nt][r];
-                    if (tail) {
+                    for (int r = 0; r < 2; ++r) {
                         const int row = row0 + 8 * nt + 2 * l + r;
                         const int t = row < pl.rows ? row / a.group : a.T - 1;
 #pragma unroll
@@ -554,101 +636,100 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
                             if (!see) x[j >> 1][nt][2 * (j & 1) + r] = -INFINITY;
                         }
                     }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) top[nt][r] = fmaxf(top[nt][r], x[j >> 1][nt][2 * (j & 1) + r]);
-                }
+            }
+            float top[NT][2];
             bool grows = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    float& tp = top[nt][r];
+                    float tp = fmaxf(fmaxf(x[0][nt][r], x[0][nt][2 + r]), fmaxf(x[1][nt][r], x[1][nt][2 + r]));
                     tp = fmaxf(tp, __shfl_xor_sync(0xffffffffu, tp, 4));
                     tp = fmaxf(tp, __shfl_xor_sync(0xffffffffu, tp, 8));
                     tp = fmaxf(tp, __shfl_xor_sync(0xffffffffu, tp, 16));
                     grows |= tp > m[nt][r];
+                    top[nt][r] = tp;
                 }
-            // the power of two above every value scale so far (positive floats order as integers)
-            const uint32_t big0 = __reduce_max_sync(0xffffffffu, max(max(__float_as_uint(vsc[0][0]), __float_as_uint(vsc[0][1])),
-                                                                     max(__float_as_uint(vsc[0][2]), __float_as_uint(vsc[0][3]))));
-            uint32_t big1 = 0;
-            if (vs.ng == 2)
-                big1 = __reduce_max_sync(0xffffffffu, max(max(__float_as_uint(vsc[1][0]), __float_as_uint(vsc[1][1])),
-                                                          max(__float_as_uint(vsc[1][2]), __float_as_uint(vsc[1][3]))));
-            const int n0 = max(e0, min((int)(big0 >> 23) - 126, 126)), n1 = max(e1, min((int)(big1 >> 23) - 126, 126));
-            if (__any_sync(0xffffffffu, grows || n0 > e0 || n1 > e1)) {
-                const float d0 = n0 - e0 > 126 ? 0.0f : pow2(e0 - n0), d1 = n1 - e1 > 126 ? 0.0f : pow2(e1 - n1);
-                e0 = n0;
-                e1 = n1;
+            if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
                         const float mn = fmaxf(m[nt][r], top[nt][r]);
-                        const float al = mn == -INFINITY ? 1.0f : ex2(m[nt][r] - mn);
+                        const float al = mn == -INFINITY ? 1.0f : ex2((m[nt][r] - mn) * fac[nt][r]);
                         m[nt][r] = mn;
                         lsum[nt][r] *= al;
 #pragma unroll
-                        for (int v = 0; v < NVB; ++v) {
-                            const float f = al * (v < vs.nb[0] ? d0 : d1);
+                        for (int v = 0; v < NVB; ++v)
 #pragma unroll
                             for (int u = 0; u < 2; ++u) {
-                                o[v][u][nt][r] *= f;
-                                o[v][u][nt][2 + r] *= f;
+                                o[v][u][nt][r] *= al;
+                                o[v][u][nt][2 + r] *= al;
                             }
-                        }
                     }
             }
-            const float f0 = pow2(-e0), f1 = pow2(-e1);
             uint32_t w[2][2][NT][2];      // weights as B fragments: [group][16 tokens][row tile][8 tokens]
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const float ms0 = m[nt][0] == -INFINITY ? 0.0f : m[nt][0], ms1 = m[nt][1] == -INFINITY ? 0.0f : m[nt][1];
+                const float ms0 = m[nt][0] == -INFINITY ? 0.0f : -m[nt][0] * fac[nt][0];
+                const float ms1 = m[nt][1] == -INFINITY ? 0.0f : -m[nt][1] * fac[nt][1];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float pa = ex2(x[j >> 1][nt][2 * (j & 1)] - ms0), pb = ex2(x[j >> 1][nt][2 * (j & 1) + 1] - ms1);
+                    const float pa = ex2(fmaf(x[j >> 1][nt][2 * (j & 1)], fac[nt][0], ms0));
+                    const float pb = ex2(fmaf(x[j >> 1][nt][2 * (j & 1) + 1], fac[nt][1], ms1));
                     lsum[nt][0] += pa;
                     lsum[nt][1] += pb;
-                    const float s0 = vsc[0][j] * f0;
-                    w[0][j >> 1][nt][j & 1] = transpose8(pack2(pa * s0, pb * s0));
-                    if (vs.ng == 2) {
-                        const float s1 = vsc[1][j] * f1;
-                        w[1][j >> 1][nt][j & 1] = transpose8(pack2(pa * s1, pb * s1));
-                    }
+                    w[0][j >> 1][nt][j & 1] = transpose8(pack2(pa * sc[j].z, pb * sc[j].z));
+                    if (vs.ng == 2) w[1][j >> 1][nt][j & 1] = transpose8(pack2(pa * sc[j].w, pb * sc[j].w));
                 }
             }
 
             // ---- outputs ----
+            const uint32_t vrow = st + v_lane;
+            auto value_block = [&](auto width, uint32_t at, const uint32_t(&wg)[2][NT][2], float(&ov)[2][NT][4]) {
+                constexpr int BITS = decltype(width)::value;
+                const int stride = pl.cp[1].stride;
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) {
+                    uint32_t p[4], q[4];
+                    value_pairs<BITS>(at + 16 * kt * stride, at + (16 * kt + 1) * stride, p);
+                    value_pairs<BITS>(at + (16 * kt + 8) * stride, at + (16 * kt + 9) * stride, q);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        mma(ov[0][nt], p[0], p[1], q[0], q[1], wg[kt][nt][0], wg[kt][nt][1]);
+                        mma(ov[1][nt], p[2], p[3], q[2], q[3], wg[kt][nt][0], wg[kt][nt][1]);
+                    }
+                }
+            };
 #pragma unroll
             for (int v = 0; v < NVB; ++v) {
-                if (v >= nvb) break;
-                const int grp = v < vs.nb[0] ? 0 : 1;
-                const int blk = grp ? v - vs.nb[0] : v;
-                auto block = [&](auto width) {
-                    constexpr int BITS = decltype(width)::value;
-#pragma unroll
-                    for (int kt = 0; kt < 2; ++kt) {
-                        const uint32_t at = st + pl.v_off + (16 * kt + 2 * l) * pl.v_stride + vs.off[grp] + 4 * BITS * blk;
-                        uint32_t p[4], q[4];
-                        value_pairs<BITS>(at, at + pl.v_stride, g, p);
-                        value_pairs<BITS>(at + 8 * pl.v_stride, at + 9 * pl.v_stride, g, q);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            const uint32_t b0 = grp ? w[1][kt][nt][0] : w[0][kt][nt][0];
-                            const uint32_t b1 = grp ? w[1][kt][nt][1] : w[0][kt][nt][1];
-                            mma(o[v][0][nt], p[0], p[1], q[0], q[1], b0, b1);
-                            mma(o[v][1][nt], p[2], p[3], q[2], q[3], b0, b1);
-                        }
+                if (v < vs.nb[0]) {
+                    if constexpr (WIDE) {
+                        value_block(std::integral_constant<int, 4>{}, vrow + 16 * v, w[0], o[v]);
+                    } else {
+                        const int bits = vs.bits[0];
+                        const uint32_t at = vrow + 4 * v * bits + (bits * g >> 1);
+                        if (bits == 4) value_block(std::integral_constant<int, 4>{}, at, w[0], o[v]);
+                        else if (bits == 8) value_block(std::integral_constant<int, 8>{}, at, w[0], o[v]);
+                        else value_block(std::integral_constant<int, 2>{}, at, w[0], o[v]);
                     }
-                };
-                const int bits = vs.bits[grp];
-                if (bits == 4) block(std::integral_constant<int, 4>{});
-                else if (bits == 8) block(std::integral_constant<int, 8>{});
-                else block(std::integral_constant<int, 2>{});
+                } else if (v < nvb) {
+                    if constexpr (WIDE) {
+                        value_block(std::integral_constant<int, 8>{}, vrow + 2 * g + vs.off[1] + 32 * (v - vs.nb[0]), w[1], o[v]);
+                    } else {
+                        const int bits = vs.bits[1];
+                        const uint32_t at = vrow + vs.off[1] + 4 * (v - vs.nb[0]) * bits + (bits * g >> 1);
+                        if (bits == 4) value_block(std::integral_constant<int, 4>{}, at, w[1], o[v]);
+                        else if (bits == 8) value_block(std::integral_constant<int, 8>{}, at, w[1], o[v]);
+                        else value_block(std::integral_constant<int, 2>{}, at, w[1], o[v]);
+                    }
+                }
             }
+            st += pl.stage_bytes;
+            if (st == ring_end) st = ring;
         }
 
-        // ---- join the warps ----
+        // ---- join the warps: statistics in units of the softmax's exponent ----
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -657,6 +738,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
                 s += __shfl_xor_sync(0xffffffffu, s, 4);
                 s += __shfl_xor_sync(0xffffffffu, s, 8);
                 s += __shfl_xor_sync(0xffffffffu, s, 16);
+                m[nt][r] *= fac[nt][r];
                 if (g == 0) {
                     sm_m[warp * R + 8 * nt + 2 * l + r] = m[nt][r];
                     sm_l[warp * R + 8 * nt + 2 * l + r] = s;
@@ -774,10 +856,9 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
     }
 }
 
-int odd16(int bytes) { return (bytes / 16) % 2 ? bytes : bytes + 16; }
-
 struct RowsLaunch {
     int nt, nvb, warps, ctas_per_sm;
+    bool wide;
     RowsPlan pl;
 };
 
@@ -794,36 +875,55 @@ RowsLaunch plan_rows(const KvGeom& geo, int64_t T, int64_t group) {
     const int R = 8 * r.nt;
     p.rows = (int)rows;
     p.row_tiles = (int)((rows + R - 1) / R);
-    p.k_stride = odd16(ks.row_bytes);
-    p.v_stride = odd16(vs.row_bytes);
-    p.v_off = kChunk * p.k_stride;
-    p.ks_off = p.v_off + kChunk * p.v_stride;
+    for (int side = 0; side < 2; ++side) {
+        const KvSide& sd = geo.s[side];
+        CopyPlan& cp = p.cp[side];
+        const int pr = sd.row_bytes / 16;
+        if (pr % 2) {
+            cp.shift = -1;
+            cp.stride = sd.row_bytes;
+            cp.iters = (16 * pr + 31) / 32;
+            cp.dst_step = cp.src_step = 512;
+        } else {
+            cp.shift = 1;
+            while ((1 << cp.shift) < pr) ++cp.shift;
+            cp.stride = sd.row_bytes + 16;
+            const int rows_at_once = 32 >> cp.shift;
+            cp.iters = 16 / rows_at_once;
+            cp.dst_step = rows_at_once * cp.stride;
+            cp.src_step = rows_at_once * sd.row_bytes;
+        }
+        cp.page_bytes = (uint32_t)geo.heads * geo.page * sd.row_bytes;
+        cp.page_scales = (uint32_t)geo.heads * geo.page * 2 * sd.ng;
+    }
+    p.v_off = kChunk * p.cp[0].stride;
+    p.ks_off = p.v_off + kChunk * p.cp[1].stride;
     p.vs_off = p.ks_off + kChunk * 2 * ks.ng;
     p.stage_bytes = p.vs_off + kChunk * 2 * vs.ng;
-    const int merge = kMergeBytes, q = nkb * r.nt * 512;
-    const int misc = 4 * (3 * R + 16 * R) + 2 * 32 * r.nvb;
-    const int fixed = merge + q + (misc + 15) / 16 * 16;
-    r.warps = 8;
-    r.ctas_per_sm = r.nt * r.nvb <= 4 ? 2 : 1;
+    const int q = nkb * r.nt * 512, scales = 16 * kChunk;
+    const int misc = (4 * (3 * R + 16 * R) + 2 * 32 * r.nvb + 15) / 16 * 16;
+    const int fixed = q + misc;
     // two stages at least; two CTAs per SM where they and the registers allow it
-    while (r.ctas_per_sm == 2 && fixed + 8 * 2 * p.stage_bytes > kMaxSmem / 2 - 2048) r.ctas_per_sm = 1;
+    r.warps = 8;
+    r.ctas_per_sm = r.nt * r.nvb <= 4 && fixed + 8 * (2 * p.stage_bytes + scales) <= kMaxSmem / 2 - 2048 ? 2 : 1;
     const int budget = r.ctas_per_sm == 2 ? kMaxSmem / 2 - 2048 : kMaxSmem - 1024;
-    if (fixed + 8 * 2 * p.stage_bytes > budget) r.warps = 4;
-    p.stages = (budget - fixed) / (r.warps * p.stage_bytes);
+    if (fixed + 8 * (2 * p.stage_bytes + scales) > budget) r.warps = 4;
+    p.stages = ((budget - fixed) / r.warps - scales) / p.stage_bytes;
     if (p.stages > 4) p.stages = 4;
-    p.merge_off = r.warps * p.stages * p.stage_bytes;
-    p.q_off = p.merge_off + merge;
+    p.f_off = p.stages * p.stage_bytes;
+    p.warp_bytes = p.f_off + scales;
+    p.q_off = r.warps * p.warp_bytes;
+    if (p.q_off < kMergeBytes) p.q_off = kMergeBytes;
     p.misc_off = p.q_off + q;
-    p.smem = p.misc_off + (misc + 15) / 16 * 16;
+    p.smem = p.misc_off + misc;
     p.min_chunks = 8;
-    p.k_magic = (65536u + ks.row_bytes / 16 - 1) / (ks.row_bytes / 16);
-    p.v_magic = (65536u + vs.row_bytes / 16 - 1) / (vs.row_bytes / 16);
+    r.wide = ks.bits[0] == 4 && vs.bits[0] == 4 && ks.bits[1] == 8 && vs.bits[1] == 8;
     return r;
 }
 
 template <int NT, int NVB>
 cudaError_t run_rows(const KvGeom& geo, const KvAttendArgs& a, const RowsLaunch& r, int grid, cudaStream_t st) {
-    auto* kernel = kv_rows_kernel<NT, NVB>;
+    auto* kernel = r.wide ? kv_rows_kernel<NT, NVB, true> : kv_rows_kernel<NT, NVB, false>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, r.pl.smem);
     if (e == cudaSuccess) e = prefer_max_shared(reinterpret_cast<const void*>(kernel));
     if (e != cudaSuccess) return e;
