@@ -540,7 +540,8 @@ SONIQ_API soniq_status soniq_kv_read(const soniq_kv_cache *cache, const int64_t 
  *   out        device, contiguous [B][T][q_heads][v.D], 2-byte aligned.
  *   scratch    device, 16-byte aligned, of soniq_kv_attend_scratch_bytes() (SONIQ_ERR_INVALID_ARG
  *              otherwise).  Its first SONIQ_KV_SCRATCH_ZERO bytes must be zero
- *              before the first use; every completed call leaves them zero.
+ *              before the first use; every completed call leaves them zero (zero
+ *              them again after a SONIQ_ERR_TIMEOUT).
  *              Calls that may overlap on the GPU must use different scratch.
  * Scores, statistics and sums are fp32; softmax weights (times the value
  * scale, normalised by a power of two) are rounded to fp16 for the product.
@@ -566,10 +567,11 @@ SONIQ_API int64_t soniq_kv_attend_scratch_bytes(const soniq_kv_cache *cache, int
 SONIQ_API soniq_status soniq_sync_status(soniq_stream_t stream);
 
 /* Test hook, not for production use.  When armed (armed != 0), the next
+ * soniq_kv_attend leaves out one copy of cached rows, or the next
  * launch of a per-tensor quantize kernel with a grid barrier (one-pass or
  * streamed), from soniq_quantize_act or soniq_quantize_act_oneshot, has its
  * first CTA skip its grid-barrier
- * arrival: the other CTAs' bounded waits run out after 2 s, the outputs are
+ * arrival: the bounded waits run out after 2 s, the outputs are
  * not written, and soniq_sync_status reports SONIQ_ERR_TIMEOUT.  The hook
  * disarms itself at that launch.  No fault, trap or hang is involved. */
 SONIQ_API void soniq_test_drop_barrier_arrival(int32_t armed);

@@ -177,7 +177,7 @@ soniq_status soniq_kv_attend(const soniq_kv_cache* cache, const void* Q, int64_t
     if (err == nullptr) return SONIQ_ERR_CUDA;
     KvAttendArgs a{static_cast<const uint16_t*>(Q), q_seq_stride, q_token_stride, q_head_stride, page_table,
                    table_stride, max_pages, lengths, mask, mask_stride, B, T, q_heads / geo.heads, scale,
-                   static_cast<uint16_t*>(out), scratch, err};
+                   static_cast<uint16_t*>(out), scratch, err, 0};
     return launched(launch_kv_attend(geo, a, reinterpret_cast<cudaStream_t>(stream)));
 }
 

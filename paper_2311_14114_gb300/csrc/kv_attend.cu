@@ -9,9 +9,11 @@
 //    equal contiguous ranges, one per CTA, by lengths read on the device:
 //    ragged batches balance and long sequences spread over all SMs.  A CTA's
 //    warps take the chunks of a range in turn, each with its own ring of
-//    shared-memory stages (cp.async) and its own running maximum, sum and
-//    outputs, joined at the end of a range; ranges that share an item leave
-//    partial results in scratch, and the last of them joins those in order.
+//    shared-memory stages and its own running maximum, sum and outputs, joined
+//    at the end of a range; ranges that share an item leave partial results in
+//    scratch, and the last of them joins those in order.
+//  * A chunk's rows and scales come by TMA (four copies, swizzled so that lanes
+//    reading one place of eight rows meet different banks).
 //  * Products run transposed on mma.sync m16n8k16 (fp16, fp32 sums): scores =
 //    K (16 tokens x 16 channels) x Q^T (8 rows), outputs = V^T (16 channels x
 //    16 tokens) x P^T, so 8 query rows fill the instruction, and codes go
@@ -36,41 +38,35 @@ namespace soniq {
 namespace {
 
 constexpr int kChunk = 32;                   // tokens a warp takes at a time
-constexpr int kMergeBytes = 32768;           // outputs of all warps, in as many passes as they need
 constexpr float kLog2e = 1.4426950408889634f;
-
-// How a warp copies 16 packed rows of one side into shared rows whose stride is
-// an odd multiple of 16 bytes (so that lanes reading one place of eight rows
-// meet eight bank groups).  Rows of an odd number of 16-byte pieces go as one
-// run; others with 2^shift >= pieces lanes to a row.
-struct CopyPlan {
-    int stride;          // bytes of a shared row
-    int shift;           // -1: one run
-    int iters, dst_step, src_step;
-    uint32_t page_bytes;         // codes of one page (all heads)
-    uint32_t page_scales;        // scales of one page, bytes
-};
 
 struct RowsPlan {
     int row_tiles;        // tiles of 8 NT query rows per key head
     int rows;             // query rows per key head: T * group
     int stages;
-    int stage_bytes;
-    CopyPlan cp[2];
-    int v_off, ks_off, vs_off;   // in a stage
-    int f_off;            // fp32 scales of a warp's chunk, behind its stages
-    int warp_bytes;       // a warp's stages and scales
+    int box_rows;         // tokens of one copy: 32, or a page of 16
+    int scale_bytes;      // of a stage: 128 for each copy of keys' or values' scales
+    int warp_bytes;       // a warp's stages
+    int s_off, bar_off;   // the warps' scales, barriers
     int q_off, misc_off;
     int smem;
     int min_chunks;       // fewest chunks worth a CTA
 };
 
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-// All but the newest `newer` groups of this thread have landed.
-__device__ __forceinline__ void cp_wait(int newer) {
-    if (newer >= 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
-    else if (newer == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
-    else asm volatile("cp.async.wait_group 0;" ::: "memory");
+struct RowsMaps {
+    CUtensorMap codes[2], scales[2];     // keys, values
+};
+
+constexpr long long kWaitNs = 2000000000ll;   // bound of a wait for a copy
+
+// Tiled copies of packed rows (x: byte, y: row of the page's heads, z: page) and
+// of scales (x: entry of the page's heads, y: page); a page outside the cache
+// reads as zeros.
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
 }
 
 __device__ __forceinline__ uint32_t lds16(uint32_t a) {
@@ -137,6 +133,13 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return r;
 }
 
+// (x & m) ^ f in one instruction (written out, as two constants otherwise make two)
+__device__ __forceinline__ uint32_t mask_flip(uint32_t x, uint32_t m, uint32_t f) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0x6A;" : "=r"(r) : "r"(x), "r"(m), "r"(f));
+    return r;
+}
+
 // The key side: a quad's lane l holds 8 codes of a block as four half pairs
 // h[0..3].  Codes of h[i] and the powers of two their place gives them:
 __device__ __forceinline__ int key_code(int bits, int l, int i, int half) {
@@ -151,23 +154,23 @@ template <int BITS>
 __device__ __forceinline__ void key_halves(uint32_t at, uint32_t (&h)[4]) {
     if constexpr (BITS == 8) {
         const uint2 w = lds64(at);
-        h[0] = (w.x & 0x00FF00FFu) ^ 0x00800080u;
-        h[1] = ((w.x >> 8) & 0x00FF00FFu) ^ 0x00800080u;
-        h[2] = (w.y & 0x00FF00FFu) ^ 0x00800080u;
-        h[3] = ((w.y >> 8) & 0x00FF00FFu) ^ 0x00800080u;
+        h[0] = mask_flip(w.x, 0x00FF00FFu, 0x00800080u);
+        h[1] = mask_flip(w.x >> 8, 0x00FF00FFu, 0x00800080u);
+        h[2] = mask_flip(w.y, 0x00FF00FFu, 0x00800080u);
+        h[3] = mask_flip(w.y >> 8, 0x00FF00FFu, 0x00800080u);
     } else if constexpr (BITS == 4) {
         uint32_t w = lds32(at);
-        h[0] = (w & 0x000F000Fu) ^ 0x00080008u;
-        h[1] = (w & 0x00F000F0u) ^ 0x00800080u;
+        h[0] = mask_flip(w, 0x000F000Fu, 0x00080008u);
+        h[1] = mask_flip(w, 0x00F000F0u, 0x00800080u);
         w >>= 8;
-        h[2] = (w & 0x000F000Fu) ^ 0x00080008u;
-        h[3] = (w & 0x00F000F0u) ^ 0x00800080u;
+        h[2] = mask_flip(w, 0x000F000Fu, 0x00080008u);
+        h[3] = mask_flip(w, 0x00F000F0u, 0x00800080u);
     } else {
         const uint32_t w = __byte_perm(lds16(at), 0, 0x4140);
-        h[0] = (w & 0x00030003u) ^ 0x00020002u;
-        h[1] = (w & 0x000C000Cu) ^ 0x00080008u;
-        h[2] = (w & 0x00300030u) ^ 0x00200020u;
-        h[3] = (w & 0x00C000C0u) ^ 0x00800080u;
+        h[0] = mask_flip(w, 0x00030003u, 0x00020002u);
+        h[1] = mask_flip(w, 0x000C000Cu, 0x00080008u);
+        h[2] = mask_flip(w, 0x00300030u, 0x00200020u);
+        h[3] = mask_flip(w, 0x00C000C0u, 0x00800080u);
     }
 }
 
@@ -184,23 +187,23 @@ template <int BITS>
 __device__ __forceinline__ void value_pairs(uint32_t row0, uint32_t row1, uint32_t (&x)[4]) {
     if constexpr (BITS == 8) {
         const uint32_t a = lds32(row0), b = lds32(row1);
-        x[0] = sub2((__byte_perm(a, b, 0x4400) & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);
-        x[1] = sub2((__byte_perm(a, b, 0x5511) & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);
-        x[2] = sub2((__byte_perm(a, b, 0x6622) & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);
-        x[3] = sub2((__byte_perm(a, b, 0x7733) & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);
+        x[0] = sub2(mask_flip(__byte_perm(a, b, 0x4400), 0x00FF00FFu, 0x64806480u), 0x64806480u);
+        x[1] = sub2(mask_flip(__byte_perm(a, b, 0x5511), 0x00FF00FFu, 0x64806480u), 0x64806480u);
+        x[2] = sub2(mask_flip(__byte_perm(a, b, 0x6622), 0x00FF00FFu, 0x64806480u), 0x64806480u);
+        x[3] = sub2(mask_flip(__byte_perm(a, b, 0x7733), 0x00FF00FFu, 0x64806480u), 0x64806480u);
     } else if constexpr (BITS == 4) {
         uint32_t w = __byte_perm(lds16(row0), lds16(row1), 0x5410);
-        x[0] = sub2((w & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);
-        x[1] = sub2((w & 0x00F000F0u) ^ 0x64806480u, 0x64806480u);
+        x[0] = sub2(mask_flip(w, 0x000F000Fu, 0x64086408u), 0x64086408u);
+        x[1] = sub2(mask_flip(w, 0x00F000F0u, 0x64806480u), 0x64806480u);
         w >>= 8;
-        x[2] = sub2((w & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);
-        x[3] = sub2((w & 0x00F000F0u) ^ 0x64806480u, 0x64806480u);
+        x[2] = sub2(mask_flip(w, 0x000F000Fu, 0x64086408u), 0x64086408u);
+        x[3] = sub2(mask_flip(w, 0x00F000F0u, 0x64806480u), 0x64806480u);
     } else {
         const uint32_t w = __byte_perm(lds8(row0), lds8(row1), 0x5410);
-        x[0] = sub2((w & 0x00030003u) ^ 0x64026402u, 0x64026402u);
-        x[1] = sub2((w & 0x000C000Cu) ^ 0x64086408u, 0x64086408u);
-        x[2] = sub2((w & 0x00300030u) ^ 0x64206420u, 0x64206420u);
-        x[3] = sub2((w & 0x00C000C0u) ^ 0x64806480u, 0x64806480u);
+        x[0] = sub2(mask_flip(w, 0x00030003u, 0x64026402u), 0x64026402u);
+        x[1] = sub2(mask_flip(w, 0x000C000Cu, 0x64086408u), 0x64086408u);
+        x[2] = sub2(mask_flip(w, 0x00300030u, 0x64206420u), 0x64206420u);
+        x[3] = sub2(mask_flip(w, 0x00C000C0u, 0x64806480u), 0x64806480u);
     }
 }
 
@@ -223,37 +226,72 @@ __device__ __forceinline__ int chunks_of(const KvGeom& geo, const KvAttendArgs& 
     return end == 0 ? 1 : (int)((end + kChunk - 1) / kChunk);
 }
 
+// Byte `x` of a row in shared memory, rows S bytes long: 16-byte pieces swizzled
+// by `sw` (the row's share, swizzle_of), rows of 256 bytes as two tiles of 32
+// half rows.
+template <int S>
+__device__ __forceinline__ uint32_t row_byte(uint32_t x, uint32_t sw) {
+    if constexpr (S == 256) return ((x & 0x80u) << 5) + ((x & 0x7Fu) ^ sw);
+    else return x ^ sw;
+}
+template <int S>
+__device__ __forceinline__ uint32_t swizzle_of(int row) {
+    return S == 64 ? ((row >> 1) & 3) << 4 : (row & 7) << 4;
+}
+// distance of two rows of a tile
+template <int S>
+constexpr int kRowStep = S == 256 ? 128 : S;
+
 template <int NT, int NVB>
 constexpr int min_ctas() { return NT * NVB <= 4 ? 2 : 1; }
 
-// WIDE: group 0 of both sides has 4-bit codes and group 1, where there is one,
-// 8-bit codes; otherwise the widths are looked up block by block.
-template <int NT, int NVB, bool WIDE>
-__global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(const KvGeom geo, const KvAttendArgs a,
-                                                                          const RowsPlan pl) {
-    extern __shared__ __align__(128) uint8_t smem[];
+// KS, VS: bytes of a key and a value row in shared memory.  WIDE: group 0 of
+// both sides has 4-bit codes and group 1, where there is one, 8-bit codes;
+// otherwise the widths are looked up block by block.
+template <int NT, int NVB, int KS, int VS, bool WIDE>
+__global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
+    kv_rows_kernel(const KvGeom geo, const KvAttendArgs a, const RowsPlan pl, const __grid_constant__ RowsMaps maps) {
+    extern __shared__ __align__(1024) uint8_t smem[];
     constexpr int R = 8 * NT;
+    constexpr int KB = kChunk * KS, VB = kChunk * VS;      // bytes of a stage's rows
+    constexpr int KR = kRowStep<KS>, VR = kRowStep<VS>;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
     const int g = lane >> 2, l = lane & 3;
     const KvSide &ks = geo.s[0], &vs = geo.s[1];
     const int nkb = ks.nb[0] + ks.nb[1], nvb = vs.nb[0] + vs.nb[1];
     const bool bf16 = geo.bf16 != 0;
     const uint32_t smem0 = tc::smem_u32(smem);
-    const uint32_t ring = smem0 + warp * pl.warp_bytes, fsc = ring + pl.f_off;
+    // a warp's part: key rows of all stages, value rows; elsewhere its scales and, as fp32, those of the chunk in hand
+    const uint32_t ring = smem0 + warp * pl.warp_bytes;
+    const uint32_t v_ring = ring + pl.stages * KB;
+    const uint32_t s_ring = smem0 + pl.s_off + warp * (pl.stages * pl.scale_bytes + 16 * kChunk);
+    const uint32_t fsc = s_ring + pl.stages * pl.scale_bytes;
+    const uint32_t bars = smem0 + pl.bar_off + warp * 32;
     float* merge = reinterpret_cast<float*>(smem);       // over the rings, which are empty when it is used
-    // misc: per (row, group) start value, per row factor, the warps' statistics, the head's value channels
+    // misc: per (row, group) start value, per row factor, the warps' statistics and the item's, the head's value channels
     float* sm_init = reinterpret_cast<float*>(smem + pl.misc_off);   // [2][R]
     float* sm_fac = sm_init + 2 * R;                                 // [R]
-    float* sm_m = sm_fac + R;                                        // [8][R]
+    float* sm_tm = sm_fac + R;                                       // [R]
+    float* sm_tl = sm_tm + R;                                        // [R]
+    float* sm_m = sm_tl + R;                                         // [8][R]
     float* sm_l = sm_m + 8 * R;                                      // [8][R]
     int16_t* sm_chan = reinterpret_cast<int16_t*>(sm_l + 8 * R);     // [32 NVB]
-    __shared__ long long sm_scan[8];
-    __shared__ long long sm_base;
-    __shared__ int sm_b, sm_last;
+    uint32_t* sm_scan = reinterpret_cast<uint32_t*>(smem + pl.bar_off + 256);      // [8]
+    uint32_t& sm_base = sm_scan[8];
+    int& sm_b = reinterpret_cast<int&>(sm_scan[9]);
+    int& sm_last = reinterpret_cast<int&>(sm_scan[10]);
+    int& sm_abort = reinterpret_cast<int&>(sm_scan[11]);
+    const uint32_t abort_flag = tc::smem_u32(&sm_abort);
+
+    if (lane == 0) {
+        for (int i = 0; i < pl.stages; ++i) tc::mbar_init(bars + 8 * i, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (tid == 0) sm_abort = 0;
 
     // ---- this CTA's range of chunks --------------------------------------
-    const int hr = geo.heads * pl.row_tiles;
-    long long total = 0;
+    const uint32_t hr = geo.heads * pl.row_tiles;
+    uint32_t total = 0;
     for (int b = tid; b < a.B; b += blockDim.x) {
         const int n = chunks_of(geo, a, b);
         total += n;
@@ -266,26 +304,32 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
         const int64_t size = (int64_t)a.T * a.group * geo.heads * vs.D;
         for (int64_t i = tid; i < size; i += blockDim.x) a.out[b * size + i] = 0;
     }
-    for (int i = 16; i; i >>= 1) total += __shfl_xor_sync(0xffffffffu, total, i);
+    total = __reduce_add_sync(0xffffffffu, total);
     if (lane == 0) sm_scan[warp] = total;
     __syncthreads();
     total = 0;
     for (int w = 0; w < n_warps; ++w) total += sm_scan[w];
-    total *= hr;
+    total *= hr;       // below 2^31 (checked on the host)
     if (total == 0) return;
-    const long long by_size = (total + pl.min_chunks - 1) / pl.min_chunks;
-    const long long n_cta = by_size < gridDim.x ? by_size : gridDim.x;
+    const uint32_t n_cta = min((total + pl.min_chunks - 1) / pl.min_chunks, gridDim.x);
     if (blockIdx.x >= n_cta) return;
-    const long long lo = total * blockIdx.x / n_cta, hi = total * (blockIdx.x + 1) / n_cta;
+    // the first `more` CTAs take one chunk more than the others
+    const uint32_t per = total / n_cta, more = total - per * n_cta;
+    auto range_of = [&](uint32_t c) { return per * c + min(c, more); };
+    auto owner_of = [&](uint32_t chunk) {
+        const uint32_t cut = more * (per + 1);
+        return chunk < cut ? chunk / (per + 1) : more + (chunk - cut) / per;
+    };
+    const uint32_t lo = range_of(blockIdx.x), hi = range_of(blockIdx.x + 1);
     // the sequence of chunk lo
     {
-        long long run = 0;
+        uint32_t run = 0;
         for (int b0 = 0; b0 < a.B; b0 += blockDim.x) {
             const int b = b0 + tid;
-            const long long mine = b < a.B ? chunks_of(geo, a, b) : 0;
-            long long incl = mine;
+            const uint32_t mine = b < a.B ? chunks_of(geo, a, b) : 0;
+            uint32_t incl = mine;
             for (int i = 1; i < 32; i <<= 1) {
-                const long long o = __shfl_up_sync(0xffffffffu, incl, i);
+                const uint32_t o = __shfl_up_sync(0xffffffffu, incl, i);
                 if (lane >= i) incl += o;
             }
             __syncthreads();
@@ -294,7 +338,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
             for (int w = 0; w < n_warps; ++w) {
                 if (w < warp) incl += sm_scan[w];
             }
-            const long long at = (run + incl - mine) * hr;
+            const uint32_t at = (run + incl - mine) * hr;
             if (mine > 0 && at <= lo && lo < at + mine * hr) {
                 sm_b = b;
                 sm_base = at;
@@ -304,108 +348,66 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
         __syncthreads();
     }
 
-    // ---- what a lane copies of 16 rows: its first piece, and its bound on piece numbers ----
-    uint32_t cp_dst[2];
-    int cp_src[2], cp_lim[2];
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        const CopyPlan& cp = pl.cp[side];
-        const int pr = geo.s[side].row_bytes >> 4;
-        if (cp.shift < 0) {
-            cp_dst[side] = 16 * lane;
-            cp_src[side] = 16 * lane;
-            cp_lim[side] = 16 * pr;
-        } else {
-            const int row = lane >> cp.shift, col = lane & ((1 << cp.shift) - 1);
-            cp_dst[side] = row * cp.stride + 16 * col;
-            cp_src[side] = (row * pr + col) * 16;
-            cp_lim[side] = col < pr ? 32 * cp.iters : 0;
-        }
-    }
-
     const int qh = geo.heads * a.group;
     const int n_min = ks.ng == 2 && ks.bits[1] < ks.bits[0] ? ks.bits[1] : ks.bits[0];
-    const uint32_t k_lane = g * pl.cp[0].stride + (WIDE ? 4 * l : 0);
-    const uint32_t v_lane = pl.v_off + 2 * l * pl.cp[1].stride + (WIDE ? 2 * g : 0);
+    const uint32_t k_sw = swizzle_of<KS>(g);                                       // rows 8 i + g
+    const uint32_t v_sw0 = swizzle_of<VS>(2 * l), v_sw1 = swizzle_of<VS>(2 * l + 1);   // rows 8 i + 2 l, 8 i + 2 l + 1
+    // token `lane`'s scales in a stage
+    const uint32_t ks_lane = 2 * ks.ng * (lane % pl.box_rows) + 128 * (lane / pl.box_rows);
+    const uint32_t vs_lane = pl.scale_bytes / 2 + 2 * vs.ng * (lane % pl.box_rows) + 128 * (lane / pl.box_rows);
     int b = sm_b;
-    long long base = sm_base;        // first chunk of sequence b
-    long long pos = lo;
+    uint32_t base = sm_base;        // first chunk of sequence b
+    uint32_t pos = lo;
+    uint32_t phases = 0, flying = 0;    // parity of each stage's next completion; stages with copies in flight
     while (pos < hi) {
-        int nch = chunks_of(geo, a, b);
-        while (pos >= base + (long long)nch * hr) {
-            base += (long long)nch * hr;
+        uint32_t nch = chunks_of(geo, a, b);
+        while (pos >= base + nch * hr) {
+            base += nch * hr;
             nch = chunks_of(geo, a, ++b);
         }
-        const long long rel = pos - base;
-        const int item = (int)(rel / nch);
-        const int c_first = (int)(rel % nch);
+        const int item = (int)((pos - base) / nch);
+        const int c_first = (int)(pos - base - item * nch);
         const int head = item / pl.row_tiles, rt = item % pl.row_tiles;
-        const long long left = hi - pos;
-        const int c_end = left < nch - c_first ? c_first + (int)left : nch;
+        const int c_end = min(c_first + (int)(hi - pos), (int)nch);
         const int len = a.lengths[b];
         const int end = (int)seen_end(geo, a, b);
         const int row0 = rt * R;
         const int32_t* table = a.table + b * a.table_stride;
 
-        // ---- loads: chunk c into a stage of this warp's ring, as two halves of 16 rows ----
-        const uint8_t *src[2], *ssrc[2];       // page 0's rows of this head, this lane's first piece
-#pragma unroll
-        for (int side = 0; side < 2; ++side) {
-            const KvSide& s = geo.s[side];
-            src[side] = s.codes + (int64_t)head * geo.page * s.row_bytes + cp_src[side];
-            ssrc[side] = reinterpret_cast<const uint8_t*>(s.scales) + (int64_t)head * geo.page * 2 * s.ng + 4 * (lane & 15);
-        }
+        // ---- loads of chunk c into stage s ----
         auto page_of = [&](int p) -> int { return p < end ? __ldg(table + (p >> geo.page_shift)) : -1; };
-        auto issue = [&](int c, uint32_t st, int pg0, int pg1) {
+        auto issue = [&](int c, int s, int pg0, int pg1) {
             const int p0 = c * kChunk;
-            bool bad = false;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int pg = half ? pg1 : pg0;
-                const bool on = (unsigned)pg < (unsigned)geo.n_pages;
-                bad |= !on && p0 + 16 * half < end;
-                const int in = (p0 + 16 * half) & (geo.page - 1);
-                const uint32_t use = on ? (uint32_t)pg : 0u;
-                const int size = on ? 16 : 0;
-#pragma unroll
-                for (int side = 0; side < 2; ++side) {
-                    const CopyPlan& cp = pl.cp[side];
-                    const KvSide& s = geo.s[side];
-                    const uint8_t* p = src[side] + (uint64_t)use * cp.page_bytes + in * s.row_bytes;
-                    uint32_t dst = st + (side ? pl.v_off : 0) + half * 16 * cp.stride + cp_dst[side];
-                    int i = lane;
-#pragma unroll 2
-                    for (int k = 0; k < cp.iters; ++k) {
-                        if (i < cp_lim[side])
-                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(p), "r"(size) : "memory");
-                        i += 32;
-                        dst += cp.dst_step;
-                        p += cp.src_step;
-                    }
-                    // 16 tokens' scales: 2 or 4 bytes each
-                    if (lane < 8 * s.ng)
-                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(st + (side ? pl.vs_off : pl.ks_off) + (half * 8 * s.ng + lane) * 4),
-                                     "l"(ssrc[side] + (uint64_t)use * cp.page_scales + in * 2 * s.ng), "r"(size >> 2)
-                                     : "memory");
+            const int boxes = p0 < end ? (pl.box_rows == kChunk || p0 + 16 >= end ? 1 : 2) : 0;
+            const int box = pl.box_rows;
+            const uint32_t bar = bars + 8 * s;
+            flying |= 1u << s;
+            const bool ok0 = (unsigned)pg0 < (unsigned)geo.n_pages, ok1 = (unsigned)pg1 < (unsigned)geo.n_pages;
+            if (tc::elect_one()) {
+                const int kx = KS == 256 && ks.row_bytes > 128 ? 2 : 1, vx = VS == 256 && vs.row_bytes > 128 ? 2 : 1;
+                tc::mbar_arrive_expect_tx(bar, boxes * box * (kx * KR + vx * VR + 2 * (ks.ng + vs.ng)));
+                for (int i = 0; i < boxes; ++i) {
+                    const bool ok = i ? ok1 : ok0;
+                    if (!ok) atomicOr(a.err, kErrKvIndex);
+                    const int pg = ok ? (i ? pg1 : pg0) : (int)geo.n_pages;
+                    const int row = head * geo.page + ((p0 + 16 * i) & (geo.page - 1));
+                    const uint32_t kd = ring + s * KB + i * 16 * KR, vd = v_ring + s * VB + i * 16 * VR;
+                    tma_load_3d(kd, &maps.codes[0], 0, row, pg, bar);
+                    if (kx == 2) tma_load_3d(kd + KB / 2, &maps.codes[0], 128, row, pg, bar);
+                    tma_load_3d(vd, &maps.codes[1], 0, row, pg, bar);
+                    if (vx == 2) tma_load_3d(vd + VB / 2, &maps.codes[1], 128, row, pg, bar);
+                    tc::tma_load_2d(s_ring + s * pl.scale_bytes + i * 128, &maps.scales[0], row * ks.ng, pg, bar);
+                    tc::tma_load_2d(s_ring + s * pl.scale_bytes + pl.scale_bytes / 2 + i * 128, &maps.scales[1], row * vs.ng, pg, bar);
                 }
             }
-            if (bad && lane == 0) atomicOr(a.err, kErrKvIndex);
+            __syncwarp();
         };
-        // page ids are read one issue ahead of their use
-        int c_load = c_first + warp, n_pg0 = -1, n_pg1 = -1;
-        auto fetch_pages = [&](int c) {
-            if (c < c_end) {
-                n_pg0 = page_of(c * kChunk);
-                n_pg1 = geo.page == 16 ? page_of(c * kChunk + 16) : (c * kChunk + 16 < end ? n_pg0 : -1);
+        for (int s = 0; s < pl.stages; ++s) {
+            const int c = c_first + warp + s * n_warps;
+            if (c < c_end && !(a.drop && c == 0 && blockIdx.x == 0)) {
+                const int pg0 = page_of(c * kChunk);
+                issue(c, s, pg0, geo.page == 16 ? page_of(c * kChunk + 16) : pg0);
             }
-        };
-        fetch_pages(c_load);
-        for (int s = 0; s < pl.stages - 1; ++s) {
-            const int pg0 = n_pg0, pg1 = n_pg1, c = c_load;
-            c_load += n_warps;
-            fetch_pages(c_load);
-            if (c < c_end) issue(c, ring + s * pl.stage_bytes, pg0, pg1);
-            cp_commit();
         }
 
         // ---- queries of the item: fp16, each row scaled to 2^13, in fragment order ----
@@ -468,13 +470,15 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
         __syncthreads();
 
         // running maximum (of scores before the row's factor), sum and outputs
-        float fac[NT][2], m[NT][2], lsum[NT][2];
+        float fac[NT][2], init[2][NT][2], m[NT][2], lsum[NT][2];
         float o[NVB][2][NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 fac[nt][r] = sm_fac[8 * nt + 2 * l + r];
+                init[0][nt][r] = sm_init[8 * nt + 2 * l + r];
+                init[1][nt][r] = sm_init[R + 8 * nt + 2 * l + r];
                 m[nt][r] = -INFINITY;
                 lsum[nt][r] = 0.0f;
             }
@@ -491,39 +495,38 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
 
         const uint32_t qbase = smem0 + pl.q_off + lane * 16;
         const int sure = min(len, end);
-        uint32_t st = ring, st_load = ring + (pl.stages - 1) * pl.stage_bytes;
-        const uint32_t ring_end = ring + pl.stages * pl.stage_bytes;
+        int stage = 0;
         for (int c = c_first + warp; c < c_end; c += n_warps) {
-            cp_wait(pl.stages - 2);
-            __syncwarp();
-            {
-                const int pg0 = n_pg0, pg1 = n_pg1, cl = c_load;
-                c_load += n_warps;
-                fetch_pages(c_load);
-                if (cl < c_end) issue(cl, st_load, pg0, pg1);
-                cp_commit();
-                st_load += pl.stage_bytes;
-                if (st_load == ring_end) st_load = ring;
+            // the page ids of the chunk that will take this stage
+            const int c_next = c + pl.stages * n_warps;
+            int pg0 = -1, pg1 = -1;
+            if (c_next < c_end) {
+                pg0 = page_of(c_next * kChunk);
+                pg1 = geo.page == 16 ? page_of(c_next * kChunk + 16) : pg0;
             }
             const int p0 = c * kChunk;
             const bool tail = p0 + kChunk > sure;      // some rows may not see some of it
+            const uint32_t s_at = s_ring + stage * pl.scale_bytes;
+            if (!tc::wait_bounded_warp(bars + 8 * stage, (phases >> stage) & 1u, abort_flag, kWaitNs, a.err, kErrWait)) break;
+            phases ^= 1u << stage;
+            flying &= ~(1u << stage);
 
             // ---- scales: lane = token; as fp32 for all lanes, the values' relative to the running power of two ----
             {
                 float k0, k1 = 0.0f, v0, v1 = 0.0f;
                 if (ks.ng == 2) {
-                    const uint32_t w = lds32(st + pl.ks_off + 4 * lane);
+                    const uint32_t w = lds32(s_at + ks_lane);
                     k0 = scale_of(w & 0xFFFFu, bf16);
                     k1 = scale_of(w >> 16, bf16);
                 } else {
-                    k0 = scale_of(lds16(st + pl.ks_off + 2 * lane), bf16);
+                    k0 = scale_of(lds16(s_at + ks_lane), bf16);
                 }
                 if (vs.ng == 2) {
-                    const uint32_t w = lds32(st + pl.vs_off + 4 * lane);
+                    const uint32_t w = lds32(s_at + vs_lane);
                     v0 = scale_of(w & 0xFFFFu, bf16);
                     v1 = scale_of(w >> 16, bf16);
                 } else {
-                    v0 = scale_of(lds16(st + pl.vs_off + 2 * lane), bf16);
+                    v0 = scale_of(lds16(s_at + vs_lane), bf16);
                 }
                 if (tail && p0 + lane >= end) k0 = k1 = v0 = v1 = 0.0f;
                 // positive floats order as integers; the exponent plus one bounds them
@@ -543,6 +546,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) o[v][u][nt][i] *= v < vs.nb[0] ? d0 : d1;
                 }
+                __syncwarp();
                 sts128f(fsc + 16 * lane, k0, k1, v0 * pow2(-e0), v1 * pow2(-e1));
                 __syncwarp();
             }
@@ -552,57 +556,48 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
 
             // ---- scores ----
             float x[2][NT][4];
-            const uint32_t krow = st + k_lane;
-            auto key_block = [&](auto width, float(&acc)[2][NT][4], uint32_t at, uint32_t qat) {
-                constexpr int BITS = decltype(width)::value;
-                uint4 q[NT];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) q[nt] = lds128(qat + nt * 512);
-#pragma unroll
-                for (int mt = 0; mt < 2; ++mt) {
-                    uint32_t h[4], k[4];
-                    key_halves<BITS>(at + 16 * mt * pl.cp[0].stride, h);
-                    key_halves<BITS>(at + (16 * mt + 8) * pl.cp[0].stride, k);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        mma(acc[mt][nt], h[0], k[0], h[1], k[1], q[nt].x, q[nt].y);
-                        mma(acc[mt][nt], h[2], k[2], h[3], k[3], q[nt].z, q[nt].w);
-                    }
-                }
-            };
+            const uint32_t krow = ring + stage * KB + g * KR;
             auto key_group = [&](auto width, int grp, float(&acc)[2][NT][4]) {
                 constexpr int BITS = decltype(width)::value;
-                float init[NT][2];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) init[nt][r] = sm_init[grp * R + 8 * nt + 2 * l + r];
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[mt][nt][i] = init[nt][i & 1];
-                // a quad's lane starts BITS bytes behind the one before; krow has 4 of them where WIDE
-                uint32_t at = krow + ks.off[grp] + (WIDE ? (BITS == 8 ? 4 * l : 0) : BITS * l);
+                        for (int i = 0; i < 4; ++i) acc[mt][nt][i] = init[grp][nt][i & 1];
+                uint32_t byte = ks.off[grp] + BITS * l;
                 uint32_t qat = qbase + (grp ? ks.nb[0] : 0) * NT * 512;
                 for (int blk = 0; blk < ks.nb[grp]; ++blk) {
-                    key_block(width, acc, at, qat);
-                    at += 4 * BITS;
+                    const uint32_t at = krow + row_byte<KS>(byte, k_sw);
+                    uint4 q[NT];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) q[nt] = lds128(qat + nt * 512);
+#pragma unroll
+                    for (int mt = 0; mt < 2; ++mt) {
+                        uint32_t h[4], k[4];
+                        key_halves<BITS>(at + 16 * mt * KR, h);
+                        key_halves<BITS>(at + (16 * mt + 8) * KR, k);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            mma(acc[mt][nt], h[0], k[0], h[1], k[1], q[nt].x, q[nt].y);
+                            mma(acc[mt][nt], h[2], k[2], h[3], k[3], q[nt].z, q[nt].w);
+                        }
+                    }
+                    byte += 4 * BITS;
                     qat += NT * 512;
                 }
             };
-            auto key_any = [&](int grp, float(&acc)[2][NT][4]) {
+            auto key_any = [&](auto grp, float(&acc)[2][NT][4]) {
+                constexpr int G = decltype(grp)::value;
                 if constexpr (WIDE) {
-                    if (grp) key_group(std::integral_constant<int, 8>{}, grp, acc);
-                    else key_group(std::integral_constant<int, 4>{}, grp, acc);
+                    key_group(std::integral_constant<int, G ? 8 : 4>{}, G, acc);
                 } else {
-                    if (ks.bits[grp] == 4) key_group(std::integral_constant<int, 4>{}, grp, acc);
-                    else if (ks.bits[grp] == 8) key_group(std::integral_constant<int, 8>{}, grp, acc);
-                    else key_group(std::integral_constant<int, 2>{}, grp, acc);
+                    if (ks.bits[G] == 4) key_group(std::integral_constant<int, 4>{}, G, acc);
+                    else if (ks.bits[G] == 8) key_group(std::integral_constant<int, 8>{}, G, acc);
+                    else key_group(std::integral_constant<int, 2>{}, G, acc);
                 }
             };
-            key_any(0, x);
+            key_any(std::integral_constant<int, 0>{}, x);
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
@@ -611,7 +606,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
                     for (int i = 0; i < 4; ++i) x[mt][nt][i] *= sc[2 * mt + (i >> 1)].x;
             if (ks.ng == 2) {
                 float acc[2][NT][4];
-                key_any(1, acc);
+                key_any(std::integral_constant<int, 1>{}, acc);
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
@@ -685,15 +680,17 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
             }
 
             // ---- outputs ----
-            const uint32_t vrow = st + v_lane;
-            auto value_block = [&](auto width, uint32_t at, const uint32_t(&wg)[2][NT][2], float(&ov)[2][NT][4]) {
+            const uint32_t vrow = v_ring + stage * VB + 2 * l * VR;
+            auto value_block = [&](auto width, uint32_t byte, const uint32_t(&wg)[2][NT][2], float(&ov)[2][NT][4]) {
                 constexpr int BITS = decltype(width)::value;
-                const int stride = pl.cp[1].stride;
+                byte += BITS * g / 2;
+                const uint32_t at0 = vrow + row_byte<VS>(byte, v_sw0);
+                const uint32_t at1 = VS == 64 ? at0 + VR : vrow + row_byte<VS>(byte, v_sw1) + VR;
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt) {
                     uint32_t p[4], q[4];
-                    value_pairs<BITS>(at + 16 * kt * stride, at + (16 * kt + 1) * stride, p);
-                    value_pairs<BITS>(at + (16 * kt + 8) * stride, at + (16 * kt + 9) * stride, q);
+                    value_pairs<BITS>(at0 + 16 * kt * VR, at1 + 16 * kt * VR, p);
+                    value_pairs<BITS>(at0 + (16 * kt + 8) * VR, at1 + (16 * kt + 8) * VR, q);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         mma(ov[0][nt], p[0], p[1], q[0], q[1], wg[kt][nt][0], wg[kt][nt][1]);
@@ -701,32 +698,28 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
                     }
                 }
             };
+            auto value_any = [&](int grp, uint32_t blk, const uint32_t(&wg)[2][NT][2], float(&ov)[2][NT][4]) {
+                if constexpr (!WIDE) {
+                    const int bits = vs.bits[grp];
+                    const uint32_t byte = vs.off[grp] + 4 * bits * blk;
+                    if (bits == 4) value_block(std::integral_constant<int, 4>{}, byte, wg, ov);
+                    else if (bits == 8) value_block(std::integral_constant<int, 8>{}, byte, wg, ov);
+                    else value_block(std::integral_constant<int, 2>{}, byte, wg, ov);
+                }
+            };
 #pragma unroll
             for (int v = 0; v < NVB; ++v) {
                 if (v < vs.nb[0]) {
-                    if constexpr (WIDE) {
-                        value_block(std::integral_constant<int, 4>{}, vrow + 16 * v, w[0], o[v]);
-                    } else {
-                        const int bits = vs.bits[0];
-                        const uint32_t at = vrow + 4 * v * bits + (bits * g >> 1);
-                        if (bits == 4) value_block(std::integral_constant<int, 4>{}, at, w[0], o[v]);
-                        else if (bits == 8) value_block(std::integral_constant<int, 8>{}, at, w[0], o[v]);
-                        else value_block(std::integral_constant<int, 2>{}, at, w[0], o[v]);
-                    }
+                    if constexpr (WIDE) value_block(std::integral_constant<int, 4>{}, 16 * v, w[0], o[v]);
+                    else value_any(0, v, w[0], o[v]);
                 } else if (v < nvb) {
-                    if constexpr (WIDE) {
-                        value_block(std::integral_constant<int, 8>{}, vrow + 2 * g + vs.off[1] + 32 * (v - vs.nb[0]), w[1], o[v]);
-                    } else {
-                        const int bits = vs.bits[1];
-                        const uint32_t at = vrow + vs.off[1] + 4 * (v - vs.nb[0]) * bits + (bits * g >> 1);
-                        if (bits == 4) value_block(std::integral_constant<int, 4>{}, at, w[1], o[v]);
-                        else if (bits == 8) value_block(std::integral_constant<int, 8>{}, at, w[1], o[v]);
-                        else value_block(std::integral_constant<int, 2>{}, at, w[1], o[v]);
-                    }
+                    if constexpr (WIDE) value_block(std::integral_constant<int, 8>{}, vs.off[1] + 32 * (v - vs.nb[0]), w[1], o[v]);
+                    else value_any(1, v - vs.nb[0], w[1], o[v]);
                 }
             }
-            st += pl.stage_bytes;
-            if (st == ring_end) st = ring;
+            __syncwarp();
+            if (c_next < c_end) issue(c_next, stage, pg0, pg1);
+            if (++stage == pl.stages) stage = 0;
         }
 
         // ---- join the warps: statistics in units of the softmax's exponent ----
@@ -745,29 +738,51 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
                 }
             }
         __syncthreads();
-        float join[NT][2];      // 2^(m - the CTA's m)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                float mm = -INFINITY;
-                for (int wi = 0; wi < n_warps; ++wi) mm = fmaxf(mm, sm_m[wi * R + 8 * nt + 2 * l + r]);
-                join[nt][r] = m[nt][r] == -INFINITY ? 0.0f : ex2(m[nt][r] - mm);
+        if (tc::abort_raised(abort_flag)) {
+            // a copy did not come: wait for the others of this warp, as long again, and leave
+            for (int i = 0; i < pl.stages; ++i) {
+                const long long t0 = tc::globaltimer();
+                while ((flying >> i & 1u) && !tc::mbar_try_wait(bars + 8 * i, (phases >> i) & 1u) &&
+                       tc::globaltimer() - t0 < kWaitNs) {
+                }
             }
-        const bool whole = c_first == 0 && c_end == nch;
+            return;
+        }
+        const bool whole = c_first == 0 && c_end == (int)nch;
         const int segment = pos == lo ? 0 : 1;
         constexpr int PART = R * (32 * NVB + 2);      // floats of a partial result: outputs, then m, then l
         float* parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.scratch) + SONIQ_KV_SCRATCH_ZERO);
         float* part = parts + (int64_t)(2 * blockIdx.x + segment) * PART;
-        // the value blocks of one pass: 8 NT rows x 32 PB outputs of 8 warps in the merge buffer
-        constexpr int PB = NT >= 4 ? 1 : (4 / NT < NVB ? 4 / NT : NVB);
-        auto store = [&](int r, int p, float v) {
+        if (tid < R) {
+            float mm = -INFINITY, ll = 0.0f;
+            for (int wi = 0; wi < n_warps; ++wi) mm = fmaxf(mm, sm_m[wi * R + tid]);
+            for (int wi = 0; wi < n_warps; ++wi) {
+                const float mw = sm_m[wi * R + tid];
+                ll += sm_l[wi * R + tid] * (mw == -INFINITY ? 0.0f : ex2(mw - mm));
+            }
+            sm_tm[tid] = mm;
+            sm_tl[tid] = ll;
+            if (!whole) {
+                part[R * 32 * NVB + tid] = mm;
+                part[R * 32 * NVB + R + tid] = ll;
+            }
+        }
+        __syncthreads();
+        float join[NT][2];      // 2^(m - the CTA's m)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) join[nt][r] = m[nt][r] == -INFINITY ? 0.0f : ex2(m[nt][r] - sm_tm[8 * nt + 2 * l + r]);
+        auto store = [&](int r, int p, float v, float ll) {
             const int row = row0 + r, ch = sm_chan[p];
             if (row < pl.rows && ch >= 0) {
                 const int64_t at = (((int64_t)b * a.T + row / a.group) * qh + head * a.group + row % a.group) * vs.D + ch;
+                v = ll > 0.0f ? v / ll : (ll == 0.0f ? 0.0f : ll);      // nothing seen: 0; NaN stays
                 a.out[at] = bf16 ? kv_round<true>(v) : kv_round<false>(v);
             }
         };
+        // the value blocks of one pass: 8 NT rows x 32 PB outputs of 8 warps in the merge buffer
+        constexpr int PB = NT >= 4 ? 1 : (4 / NT < NVB ? 4 / NT : NVB);
 #pragma unroll
         for (int v0 = 0; v0 < NVB; v0 += PB) {
 #pragma unroll
@@ -794,142 +809,196 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>())) kv_rows_kernel(con
                 if (p >= 32 * nvb) continue;
                 float sum = 0.0f;
                 for (int wi = 0; wi < n_warps; ++wi) sum += merge[wi * R * PB * 32 + i];
-                if (whole) {
-                    float mm = -INFINITY, ll = 0.0f;
-                    for (int wi = 0; wi < n_warps; ++wi) mm = fmaxf(mm, sm_m[wi * R + r]);
-                    for (int wi = 0; wi < n_warps; ++wi) {
-                        const float mw = sm_m[wi * R + r];
-                        ll += sm_l[wi * R + r] * (mw == -INFINITY ? 0.0f : ex2(mw - mm));
-                    }
-                    store(r, p, ll > 0.0f ? sum / ll : (ll == 0.0f ? 0.0f : ll));
-                } else {
-                    part[r * 32 * NVB + p] = sum;
-                }
+                if (whole) store(r, p, sum, sm_tl[r]);
+                else part[r * 32 * NVB + p] = sum;
             }
             __syncthreads();
         }
         if (!whole) {
-            for (int r = tid; r < R; r += blockDim.x) {
-                float mm = -INFINITY, ll = 0.0f;
-                for (int wi = 0; wi < n_warps; ++wi) mm = fmaxf(mm, sm_m[wi * R + r]);
-                for (int wi = 0; wi < n_warps; ++wi) {
-                    const float mw = sm_m[wi * R + r];
-                    ll += sm_l[wi * R + r] * (mw == -INFINITY ? 0.0f : ex2(mw - mm));
-                }
-                part[R * 32 * NVB + r] = mm;
-                part[R * 32 * NVB + R + r] = ll;
-            }
             // the CTAs that share the item: the last to get here joins their parts in order
-            const long long s_first = base + (long long)item * nch, s_last = s_first + nch - 1;
-            const int cta0 = (int)(((s_first + 1) * n_cta - 1) / total), cta1 = (int)(((s_last + 1) * n_cta - 1) / total);
+            const uint32_t s_first = base + item * nch;
+            const int cta0 = (int)owner_of(s_first), cta1 = (int)owner_of(s_first + nch - 1), n_part = cta1 - cta0 + 1;
             unsigned* counter = static_cast<unsigned*>(a.scratch) + cta0;
             __threadfence();
             __syncthreads();
             if (tid == 0) {
                 const unsigned n = atomicAdd(counter, 1u);
-                sm_last = n == (unsigned)(cta1 - cta0);
+                sm_last = n == (unsigned)(n_part - 1);
                 if (sm_last) *counter = 0;
             }
             __syncthreads();
             if (sm_last) {
                 __threadfence();
-                const int head_seg = total * cta0 / n_cta == s_first ? 0 : 1;
-                auto part_of = [&](int c) { return parts + (int64_t)(2 * c + (c == cta0 ? head_seg : 0)) * PART; };
-                for (int i = tid; i < R * 32 * nvb; i += blockDim.x) {
-                    const int r = i / (32 * nvb), p = i % (32 * nvb);
-                    if (row0 + r >= pl.rows) continue;
-                    float mm = -INFINITY, acc = 0.0f, ll = 0.0f;
-                    for (int c = cta0; c <= cta1; ++c) mm = fmaxf(mm, __ldcg(part_of(c) + R * 32 * NVB + r));
-                    for (int c = cta0; c <= cta1; ++c) {
-                        const float* q = part_of(c);
-                        const float mc = __ldcg(q + R * 32 * NVB + r);
-                        const float f = mc == -INFINITY ? 0.0f : ex2(mc - mm);
-                        acc += f * __ldcg(q + r * 32 * NVB + p);
-                        ll += f * __ldcg(q + R * 32 * NVB + R + r);
+                const int head_seg = range_of(cta0) == s_first ? 0 : 1;
+                auto part_of = [&](int i) { return parts + (int64_t)(2 * (cta0 + i) + (i == 0 ? head_seg : 0)) * PART; };
+                float* fp = merge;                      // [n_part][R]: each part's factor
+                for (int i = tid; i < n_part * R; i += blockDim.x) fp[i] = __ldcg(part_of(i / R) + R * 32 * NVB + i % R);
+                __syncthreads();
+                for (int r = warp; r < R; r += n_warps) {
+                    float mm = -INFINITY, ll = 0.0f;
+                    for (int i = lane; i < n_part; i += 32) mm = fmaxf(mm, fp[i * R + r]);
+                    for (int i = 16; i; i >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, i));
+                    for (int i = lane; i < n_part; i += 32) {
+                        const float mc = fp[i * R + r], f = mc == -INFINITY ? 0.0f : ex2(mc - mm);
+                        ll += f * __ldcg(part_of(i) + R * 32 * NVB + R + r);
+                        fp[i * R + r] = f;
                     }
-                    store(r, p, ll > 0.0f ? acc / ll : (ll == 0.0f ? 0.0f : ll));
+                    for (int i = 16; i; i >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, i);
+                    if (lane == 0) sm_tl[r] = ll;
+                }
+                __syncthreads();
+                // four outputs to a thread; parts split over the threads that are left, and joined in order
+                const int rows_used = min(R, pl.rows - row0), per_row = 8 * nvb, n_vec = rows_used * per_row;
+                const int slices = n_vec < (int)blockDim.x ? (int)blockDim.x / n_vec : 1;
+                float4* red = reinterpret_cast<float4*>(fp + (n_part * R + 3) / 4 * 4);
+                for (int v0 = 0; v0 < n_vec; v0 += blockDim.x) {
+                    const int slice = slices > 1 ? tid / n_vec : 0, v = slices > 1 ? tid % n_vec : v0 + tid;
+                    const bool on = slice < slices && v < n_vec;
+                    const int r = on ? v / per_row : 0, p = on ? 4 * (v % per_row) : 0;
+                    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    if (on) {
+#pragma unroll 8
+                        for (int i = slice; i < n_part; i += slices) {
+                            const float4 q = __ldcg(reinterpret_cast<const float4*>(part_of(i) + r * 32 * NVB + p));
+                            const float f = fp[i * R + r];
+                            acc.x = fmaf(f, q.x, acc.x);
+                            acc.y = fmaf(f, q.y, acc.y);
+                            acc.z = fmaf(f, q.z, acc.z);
+                            acc.w = fmaf(f, q.w, acc.w);
+                        }
+                        red[tid] = acc;
+                    }
+                    __syncthreads();
+                    if (on && slice == 0) {
+                        for (int i = 1; i < slices; ++i) {
+                            const float4 q = red[tid + i * n_vec];
+                            acc.x += q.x;
+                            acc.y += q.y;
+                            acc.z += q.z;
+                            acc.w += q.w;
+                        }
+                        const float ll = sm_tl[r];
+                        store(r, p, acc.x, ll);
+                        store(r, p + 1, acc.y, ll);
+                        store(r, p + 2, acc.z, ll);
+                        store(r, p + 3, acc.w, ll);
+                    }
+                    __syncthreads();
                 }
             }
         }
         pos += c_end - c_first;
+        // the next item's copies land where this one's results were joined
+        tc::fence_proxy_async_shared();
         __syncthreads();
     }
 }
 
+constexpr int kMaxSmem = 227 * 1024, kHalfSmem = 228 * 1024 / 2 - 1024;
+
 struct RowsLaunch {
-    int nt, nvb, warps, ctas_per_sm;
+    int nt, nvb, ks, vs, warps, ctas_per_sm;
     bool wide;
     RowsPlan pl;
 };
-
-constexpr int kMaxSmem = 227 * 1024;
 
 RowsLaunch plan_rows(const KvGeom& geo, int64_t T, int64_t group) {
     RowsLaunch r{};
     const KvSide &ks = geo.s[0], &vs = geo.s[1];
     const int nkb = ks.nb[0] + ks.nb[1], nvb = vs.nb[0] + vs.nb[1];
     const int64_t rows = T * group;
-    r.nvb = nvb <= 2 ? 2 : (nvb <= 4 ? 4 : 8);
+    // the smallest of the built shapes that holds the rows
+    if (ks.row_bytes <= 64 && vs.row_bytes <= 64 && nvb <= 2) r.nvb = 2, r.ks = 64, r.vs = 64;
+    else if (ks.row_bytes <= 128 && vs.row_bytes <= 64 && nvb <= 4) r.nvb = 4, r.ks = 128, r.vs = 64;
+    else if (ks.row_bytes <= 128 && vs.row_bytes <= 128 && nvb <= 4) r.nvb = 4, r.ks = 128, r.vs = 128;
+    else r.nvb = 8, r.ks = 256, r.vs = 256;
     r.nt = rows <= 8 ? 1 : (rows <= 16 || r.nvb == 8 ? 2 : 4);
     RowsPlan& p = r.pl;
     const int R = 8 * r.nt;
     p.rows = (int)rows;
     p.row_tiles = (int)((rows + R - 1) / R);
-    for (int side = 0; side < 2; ++side) {
-        const KvSide& sd = geo.s[side];
-        CopyPlan& cp = p.cp[side];
-        const int pr = sd.row_bytes / 16;
-        if (pr % 2) {
-            cp.shift = -1;
-            cp.stride = sd.row_bytes;
-            cp.iters = (16 * pr + 31) / 32;
-            cp.dst_step = cp.src_step = 512;
-        } else {
-            cp.shift = 1;
-            while ((1 << cp.shift) < pr) ++cp.shift;
-            cp.stride = sd.row_bytes + 16;
-            const int rows_at_once = 32 >> cp.shift;
-            cp.iters = 16 / rows_at_once;
-            cp.dst_step = rows_at_once * cp.stride;
-            cp.src_step = rows_at_once * sd.row_bytes;
-        }
-        cp.page_bytes = (uint32_t)geo.heads * geo.page * sd.row_bytes;
-        cp.page_scales = (uint32_t)geo.heads * geo.page * 2 * sd.ng;
-    }
-    p.v_off = kChunk * p.cp[0].stride;
-    p.ks_off = p.v_off + kChunk * p.cp[1].stride;
-    p.vs_off = p.ks_off + kChunk * 2 * ks.ng;
-    p.stage_bytes = p.vs_off + kChunk * 2 * vs.ng;
-    const int q = nkb * r.nt * 512, scales = 16 * kChunk;
-    const int misc = (4 * (3 * R + 16 * R) + 2 * 32 * r.nvb + 15) / 16 * 16;
-    const int fixed = q + misc;
+    p.box_rows = geo.page < kChunk ? geo.page : kChunk;
+    p.scale_bytes = 256 * (kChunk / p.box_rows);
+    const int stage = kChunk * (r.ks + r.vs);
+    const int q = nkb * r.nt * 512;
+    const int misc = (4 * (5 * R + 16 * R) + 2 * 32 * r.nvb + 15) / 16 * 16;
+    const int fixed = q + misc + 256 + 64;
+    auto warp_bytes = [&](int stages) { return stages * (stage + p.scale_bytes) + 16 * kChunk; };
     // two stages at least; two CTAs per SM where they and the registers allow it
     r.warps = 8;
-    r.ctas_per_sm = r.nt * r.nvb <= 4 && fixed + 8 * (2 * p.stage_bytes + scales) <= kMaxSmem / 2 - 2048 ? 2 : 1;
-    const int budget = r.ctas_per_sm == 2 ? kMaxSmem / 2 - 2048 : kMaxSmem - 1024;
-    if (fixed + 8 * (2 * p.stage_bytes + scales) > budget) r.warps = 4;
-    p.stages = ((budget - fixed) / r.warps - scales) / p.stage_bytes;
-    if (p.stages > 4) p.stages = 4;
-    p.f_off = p.stages * p.stage_bytes;
-    p.warp_bytes = p.f_off + scales;
-    p.q_off = r.warps * p.warp_bytes;
-    if (p.q_off < kMergeBytes) p.q_off = kMergeBytes;
+    r.ctas_per_sm = r.nt * r.nvb <= 4 && fixed + 8 * warp_bytes(2) <= kHalfSmem ? 2 : 1;
+    const int budget = r.ctas_per_sm == 2 ? kHalfSmem : kMaxSmem;
+    if (fixed + 8 * warp_bytes(2) > budget) r.warps = 4;
+    p.stages = 2;
+    while (p.stages < 4 && fixed + r.warps * warp_bytes(p.stages + 1) <= budget) ++p.stages;
+    p.warp_bytes = p.stages * stage;
+    p.s_off = r.warps * p.warp_bytes;
+    p.q_off = p.s_off + r.warps * (p.stages * p.scale_bytes + 16 * kChunk);
     p.misc_off = p.q_off + q;
-    p.smem = p.misc_off + misc;
+    p.bar_off = p.misc_off + misc;
+    p.smem = p.bar_off + 256 + 64;
     p.min_chunks = 8;
     r.wide = ks.bits[0] == 4 && vs.bits[0] == 4 && ks.bits[1] == 8 && vs.bits[1] == 8;
     return r;
 }
 
-template <int NT, int NVB>
-cudaError_t run_rows(const KvGeom& geo, const KvAttendArgs& a, const RowsLaunch& r, int grid, cudaStream_t st) {
-    auto* kernel = r.wide ? kv_rows_kernel<NT, NVB, true> : kv_rows_kernel<NT, NVB, false>;
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+    static const EncodeTiledFn fn = [] {
+        void* ptr = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        const bool ok = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &q) ==
+                            cudaSuccess && q == cudaDriverEntryPointSuccess;
+        return ok ? reinterpret_cast<EncodeTiledFn>(ptr) : nullptr;
+    }();
+    return fn;
+}
+
+// Codes as [pages][rows of all heads][row bytes], scales as [pages][entries of
+// all heads]; row_bytes: what a shared row holds of it.
+bool encode_side(const KvGeom& geo, const KvSide& s, int shared_row, int box_rows, CUtensorMap* codes, CUtensorMap* scales) {
+    const EncodeTiledFn enc = encode_fn();
+    if (enc == nullptr) return false;
+    const cuuint32_t step[3] = {1, 1, 1};
+    const cuuint64_t rows = (cuuint64_t)geo.heads * geo.page;
+    const cuuint64_t dims[3] = {(cuuint64_t)s.row_bytes, rows, (cuuint64_t)geo.n_pages};
+    const cuuint64_t strides[2] = {(cuuint64_t)s.row_bytes, rows * s.row_bytes};
+    const cuuint32_t box[3] = {(cuuint32_t)(shared_row < 128 ? shared_row : 128), (cuuint32_t)box_rows, 1};
+    if (enc(codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, s.codes, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            shared_row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return false;
+    const cuuint64_t sdims[2] = {rows * s.ng, (cuuint64_t)geo.n_pages};
+    const cuuint64_t sstrides[1] = {rows * s.ng * 2};
+    const cuuint32_t sbox[2] = {(cuuint32_t)(box_rows * s.ng), 1};
+    return enc(scales, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, s.scales, sdims, sstrides, sbox, step,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int NT, int NVB, int KS, int VS>
+cudaError_t run_rows(const KvGeom& geo, const KvAttendArgs& a, const RowsLaunch& r, const RowsMaps& maps, int grid,
+                     cudaStream_t st) {
+    auto* kernel = r.wide ? kv_rows_kernel<NT, NVB, KS, VS, true> : kv_rows_kernel<NT, NVB, KS, VS, false>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, r.pl.smem);
     if (e == cudaSuccess) e = prefer_max_shared(reinterpret_cast<const void*>(kernel));
     if (e != cudaSuccess) return e;
-    kernel<<<grid, 32 * r.warps, r.pl.smem, st>>>(geo, a, r.pl);
+    kernel<<<grid, 32 * r.warps, r.pl.smem, st>>>(geo, a, r.pl, maps);
     note_launch();
     return cudaGetLastError();
+}
+
+template <int NVB, int KS, int VS>
+cudaError_t run_rows(const KvGeom& geo, const KvAttendArgs& a, const RowsLaunch& r, const RowsMaps& maps, int grid,
+                     cudaStream_t st) {
+    if (r.nt == 1) return run_rows<1, NVB, KS, VS>(geo, a, r, maps, grid, st);
+    if constexpr (NVB <= 4) {
+        if (r.nt == 4) return run_rows<4, NVB, KS, VS>(geo, a, r, maps, grid, st);
+    }
+    return run_rows<2, NVB, KS, VS>(geo, a, r, maps, grid, st);
 }
 
 }  // namespace
@@ -937,26 +1006,29 @@ cudaError_t run_rows(const KvGeom& geo, const KvAttendArgs& a, const RowsLaunch&
 int64_t kv_attend_scratch(const KvGeom& geo, int64_t B, int64_t T, int64_t group) {
     if (B == 0 || T == 0) return 0;
     const RowsLaunch r = plan_rows(geo, T, group);
-    return SONIQ_KV_SCRATCH_ZERO + (int64_t)2 * 2 * num_sms() * 8 * r.nt * (32 * r.nvb + 2) * 4;
+    return SONIQ_KV_SCRATCH_ZERO + (int64_t)2 * r.ctas_per_sm * num_sms() * 8 * r.nt * (32 * r.nvb + 2) * 4;
 }
 
-cudaError_t launch_kv_attend(const KvGeom& geo, const KvAttendArgs& a, cudaStream_t st) {
+cudaError_t launch_kv_attend(const KvGeom& geo, const KvAttendArgs& args, cudaStream_t st) {
+    KvAttendArgs a = args;
+    a.drop = take_drop_arrival();
     const RowsLaunch r = plan_rows(geo, a.T, a.group);
     const int64_t cap = (int64_t)a.max_pages << geo.page_shift;
     const int64_t most = (int64_t)a.B * geo.heads * r.pl.row_tiles * (cap / kChunk + 1);
+    if (most >= 2147483648ll) return cudaErrorNotSupported;      // chunks are numbered in 32 bits
     const int64_t by_size = (most + r.pl.min_chunks - 1) / r.pl.min_chunks;
     const int64_t full = (int64_t)r.ctas_per_sm * num_sms();
     const int grid = (int)(by_size < full ? by_size : full);
-    switch (r.nvb * 8 + r.nt) {
-        case 2 * 8 + 1: return run_rows<1, 2>(geo, a, r, grid, st);
-        case 2 * 8 + 2: return run_rows<2, 2>(geo, a, r, grid, st);
-        case 2 * 8 + 4: return run_rows<4, 2>(geo, a, r, grid, st);
-        case 4 * 8 + 1: return run_rows<1, 4>(geo, a, r, grid, st);
-        case 4 * 8 + 2: return run_rows<2, 4>(geo, a, r, grid, st);
-        case 4 * 8 + 4: return run_rows<4, 4>(geo, a, r, grid, st);
-        case 8 * 8 + 1: return run_rows<1, 8>(geo, a, r, grid, st);
-        default: return run_rows<2, 8>(geo, a, r, grid, st);
+    RowsMaps maps;
+    const int shared_row[2] = {r.ks, r.vs};
+    for (int side = 0; side < 2; ++side) {
+        if (!encode_side(geo, geo.s[side], shared_row[side], r.pl.box_rows, &maps.codes[side], &maps.scales[side]))
+            return cudaErrorUnknown;
     }
+    if (r.nvb == 2) return run_rows<2, 64, 64>(geo, a, r, maps, grid, st);
+    if (r.nvb == 8) return run_rows<8, 256, 256>(geo, a, r, maps, grid, st);
+    if (r.vs == 64) return run_rows<4, 128, 64>(geo, a, r, maps, grid, st);
+    return run_rows<4, 128, 128>(geo, a, r, maps, grid, st);
 }
 
 }  // namespace soniq

@@ -55,6 +55,7 @@ struct KvAttendArgs {
     uint16_t* out;
     void* scratch;
     unsigned* err;
+    int32_t drop;             // test hook: the first copy is left out
 };
 
 soniq_status make_kv_geom(const soniq_kv_cache* c, KvGeom* geo);

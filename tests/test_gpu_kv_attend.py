@@ -254,3 +254,24 @@ def test_refusals(sq):
             sq.kv_attend(p.cache, **args)
     with pytest.raises(sq.SoniqError):
         sq.kv_attend(p.cache, q, p.table, p.dlens, scale=float("nan"))
+
+
+def test_lost_copy_is_reported(sq):
+    """A copy that never comes: the bounded wait runs out, the status says so, and the next call is right."""
+    p = Problem(sq, 34, LAYOUTS[0], [200, 31], 1, 4, 16, torch.float16)
+    want = run(sq, p)
+    sq.test_drop_barrier_arrival()
+    sq.kv_attend(p.cache, p.q.cuda(), p.table, p.dlens)
+    assert sq.sync_status() == sq.SONIQ_ERR_TIMEOUT
+    assert torch.equal(run(sq, p), want)
+
+
+def test_nan_query_stays_in_its_row(sq):
+    p = Problem(sq, 35, LAYOUTS[0], [100], 3, 4, 16, torch.float16)
+    want = run(sq, p)
+    q = p.q.clone()
+    q[0, 1, 6, 3] = float("nan")
+    out = sq.kv_attend(p.cache, q.cuda(), p.table, p.dlens)
+    assert torch.isnan(out[0, 1, 6]).all()
+    out[0, 1, 6] = want[0, 1, 6]
+    assert torch.equal(out, want)
