@@ -153,24 +153,26 @@ __device__ __forceinline__ int place_log2(int bits, int i) { return bits == 8 ? 
 template <int BITS>
 __device__ __forceinline__ void key_halves(uint32_t at, uint32_t (&h)[4]) {
     if constexpr (BITS == 8) {
-        const uint2 w = lds64(at);
-        h[0] = mask_flip(w.x, 0x00FF00FFu, 0x00800080u);
-        h[1] = mask_flip(w.x >> 8, 0x00FF00FFu, 0x00800080u);
-        h[2] = mask_flip(w.y, 0x00FF00FFu, 0x00800080u);
-        h[3] = mask_flip(w.y >> 8, 0x00FF00FFu, 0x00800080u);
+        uint2 w = lds64(at);
+        w.x ^= 0x80808080u;
+        w.y ^= 0x80808080u;
+        h[0] = w.x & 0x00FF00FFu;
+        h[1] = (w.x >> 8) & 0x00FF00FFu;
+        h[2] = w.y & 0x00FF00FFu;
+        h[3] = (w.y >> 8) & 0x00FF00FFu;
     } else if constexpr (BITS == 4) {
-        uint32_t w = lds32(at);
-        h[0] = mask_flip(w, 0x000F000Fu, 0x00080008u);
-        h[1] = mask_flip(w, 0x00F000F0u, 0x00800080u);
+        uint32_t w = lds32(at) ^ 0x88888888u;
+        h[0] = w & 0x000F000Fu;
+        h[1] = w & 0x00F000F0u;
         w >>= 8;
-        h[2] = mask_flip(w, 0x000F000Fu, 0x00080008u);
-        h[3] = mask_flip(w, 0x00F000F0u, 0x00800080u);
+        h[2] = w & 0x000F000Fu;
+        h[3] = w & 0x00F000F0u;
     } else {
-        const uint32_t w = __byte_perm(lds16(at), 0, 0x4140);
-        h[0] = mask_flip(w, 0x00030003u, 0x00020002u);
-        h[1] = mask_flip(w, 0x000C000Cu, 0x00080008u);
-        h[2] = mask_flip(w, 0x00300030u, 0x00200020u);
-        h[3] = mask_flip(w, 0x00C000C0u, 0x00800080u);
+        const uint32_t w = __byte_perm(lds16(at) ^ 0xAAAAu, 0, 0x4140);
+        h[0] = w & 0x00030003u;
+        h[1] = w & 0x000C000Cu;
+        h[2] = w & 0x00300030u;
+        h[3] = w & 0x00C000C0u;
     }
 }
 
@@ -183,29 +185,52 @@ __device__ __forceinline__ int value_code(int bits, int g, int i) {
     return 16 * (g >> 2) + 4 * i + (g & 3);
 }
 
+// The offsets 1024 + 8 and 1024 + 128 as half pairs, in registers: a logic
+// instruction has room for one constant, and the compiler would move the other
+// one in before each use.
+struct Offsets {
+    uint32_t c8, c128;
+    __device__ __forceinline__ Offsets() {
+        asm volatile("mov.b32 %0, 0x64086408;" : "=r"(c8));
+        asm volatile("mov.b32 %0, 0x64806480;" : "=r"(c128));
+    }
+};
+
+// 4-bit codes of two tokens, 4 from each half of w
+__device__ __forceinline__ void nibble_pairs(uint32_t w, const Offsets& f, uint32_t (&x)[4]) {
+    x[0] = sub2(mask_flip(w, 0x000F000Fu, f.c8), f.c8);
+    x[1] = sub2(mask_flip(w, 0x00F000F0u, f.c128), f.c128);
+    w >>= 8;
+    x[2] = sub2(mask_flip(w, 0x000F000Fu, f.c8), f.c8);
+    x[3] = sub2(mask_flip(w, 0x00F000F0u, f.c128), f.c128);
+}
+
 template <int BITS>
-__device__ __forceinline__ void value_pairs(uint32_t row0, uint32_t row1, uint32_t (&x)[4]) {
+__device__ __forceinline__ void value_pairs(uint32_t row0, uint32_t row1, const Offsets& f, uint32_t (&x)[4]) {
     if constexpr (BITS == 8) {
         const uint32_t a = lds32(row0), b = lds32(row1);
-        x[0] = sub2(mask_flip(__byte_perm(a, b, 0x4400), 0x00FF00FFu, 0x64806480u), 0x64806480u);
-        x[1] = sub2(mask_flip(__byte_perm(a, b, 0x5511), 0x00FF00FFu, 0x64806480u), 0x64806480u);
-        x[2] = sub2(mask_flip(__byte_perm(a, b, 0x6622), 0x00FF00FFu, 0x64806480u), 0x64806480u);
-        x[3] = sub2(mask_flip(__byte_perm(a, b, 0x7733), 0x00FF00FFu, 0x64806480u), 0x64806480u);
+        x[0] = sub2(mask_flip(__byte_perm(a, b, 0x4400), 0x00FF00FFu, f.c128), f.c128);
+        x[1] = sub2(mask_flip(__byte_perm(a, b, 0x5511), 0x00FF00FFu, f.c128), f.c128);
+        x[2] = sub2(mask_flip(__byte_perm(a, b, 0x6622), 0x00FF00FFu, f.c128), f.c128);
+        x[3] = sub2(mask_flip(__byte_perm(a, b, 0x7733), 0x00FF00FFu, f.c128), f.c128);
     } else if constexpr (BITS == 4) {
-        uint32_t w = __byte_perm(lds16(row0), lds16(row1), 0x5410);
-        x[0] = sub2(mask_flip(w, 0x000F000Fu, 0x64086408u), 0x64086408u);
-        x[1] = sub2(mask_flip(w, 0x00F000F0u, 0x64806480u), 0x64806480u);
-        w >>= 8;
-        x[2] = sub2(mask_flip(w, 0x000F000Fu, 0x64086408u), 0x64086408u);
-        x[3] = sub2(mask_flip(w, 0x00F000F0u, 0x64806480u), 0x64806480u);
+        nibble_pairs(__byte_perm(lds16(row0), lds16(row1), 0x5410), f, x);
     } else {
         const uint32_t w = __byte_perm(lds8(row0), lds8(row1), 0x5410);
         x[0] = sub2(mask_flip(w, 0x00030003u, 0x64026402u), 0x64026402u);
-        x[1] = sub2(mask_flip(w, 0x000C000Cu, 0x64086408u), 0x64086408u);
+        x[1] = sub2(mask_flip(w, 0x000C000Cu, f.c8), f.c8);
         x[2] = sub2(mask_flip(w, 0x00300030u, 0x64206420u), 0x64206420u);
-        x[3] = sub2(mask_flip(w, 0x00C000C0u, 0x64806480u), 0x64806480u);
+        x[3] = sub2(mask_flip(w, 0x00C000C0u, f.c128), f.c128);
     }
 }
+// Two 4-bit blocks in a row at once: lane group g takes word g of their eight,
+// codes 8 g + 4 (i & 1) + (i >> 1) of 64 into x[i], those 2 later into y[i].
+__device__ __forceinline__ void value_pairs2(uint32_t row0, uint32_t row1, const Offsets& f, uint32_t (&x)[4], uint32_t (&y)[4]) {
+    const uint32_t a = lds32(row0), b = lds32(row1);
+    nibble_pairs(__byte_perm(a, b, 0x5410), f, x);
+    nibble_pairs(__byte_perm(a, b, 0x7632), f, y);
+}
+__device__ __forceinline__ int value_code2(int g, int i) { return 8 * g + 4 * (i & 1) + (i >> 1); }
 
 __device__ __forceinline__ float scale_of(uint32_t bits16, bool bf16) {
     return bf16 ? __uint_as_float(bits16 << 16) : __half2float(__ushort_as_half((uint16_t)bits16));
@@ -290,68 +315,112 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
     if (tid == 0) sm_abort = 0;
 
     // ---- this CTA's range of chunks --------------------------------------
+    if (blockIdx.x == 0) {
+        for (int b = tid; b < a.B; b += blockDim.x)
+            if (a.lengths[b] >= 0 && (int64_t)a.lengths[b] + a.T > ((int64_t)a.max_pages << geo.page_shift))
+                atomicOr(a.err, kErrKvIndex);
+    }
     const uint32_t hr = geo.heads * pl.row_tiles;
-    uint32_t total = 0;
-    for (int b = tid; b < a.B; b += blockDim.x) {
-        const int n = chunks_of(geo, a, b);
-        total += n;
-        if (n != 0 && blockIdx.x == 0 && (int64_t)a.lengths[b] + a.T > ((int64_t)a.max_pages << geo.page_shift))
-            atomicOr(a.err, kErrKvIndex);
+    // exclusive prefix sum over the CTA, and the total
+    auto scan = [&](uint32_t mine, uint32_t& all) {
+        uint32_t incl = mine;
+        for (int i = 1; i < 32; i <<= 1) {
+            const uint32_t o = __shfl_up_sync(0xffffffffu, incl, i);
+            if (lane >= i) incl += o;
+        }
+        __syncthreads();
+        if (lane == 31) sm_scan[warp] = incl;
+        __syncthreads();
+        all = 0;
+        uint32_t before = incl - mine;
+        for (int w = 0; w < n_warps; ++w) {
+            const uint32_t o = sm_scan[w];
+            if (w < warp) before += o;
+            all += o;
+        }
+        return before;
+    };
+    const bool one_scan = a.B <= (int)blockDim.x;
+    uint32_t total, mine = 0, before = 0;
+    int present = 0;
+    if (one_scan) {
+        mine = tid < a.B ? chunks_of(geo, a, tid) : 0;
+        present = __syncthreads_count(mine > 0);
+        before = scan(mine, total);
+    } else {
+        for (int b = tid; b < a.B; b += blockDim.x) mine += chunks_of(geo, a, b);
+        scan(mine, total);
     }
     // outputs of absent sequences
-    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-        if (a.lengths[b] >= 0) continue;
-        const int64_t size = (int64_t)a.T * a.group * geo.heads * vs.D;
-        for (int64_t i = tid; i < size; i += blockDim.x) a.out[b * size + i] = 0;
+    if (!one_scan || present < a.B) {
+        for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+            if (a.lengths[b] >= 0) continue;
+            const int64_t size = (int64_t)a.T * a.group * geo.heads * vs.D;
+            for (int64_t i = tid; i < size; i += blockDim.x) a.out[b * size + i] = 0;
+        }
     }
-    total = __reduce_add_sync(0xffffffffu, total);
-    if (lane == 0) sm_scan[warp] = total;
-    __syncthreads();
-    total = 0;
-    for (int w = 0; w < n_warps; ++w) total += sm_scan[w];
     total *= hr;       // below 2^31 (checked on the host)
     if (total == 0) return;
-    const uint32_t n_cta = min((total + pl.min_chunks - 1) / pl.min_chunks, gridDim.x);
-    if (blockIdx.x >= n_cta) return;
-    // the first `more` CTAs take one chunk more than the others
-    const uint32_t per = total / n_cta, more = total - per * n_cta;
+    // Few items: each is cut in equal parts, a CTA to a part, if that costs no CTA
+    // more than two rounds of its warps over the even split.  Otherwise the list of
+    // all chunks is cut evenly, and a CTA may end one item and begin another.
+    uint32_t n_cta, lo = 0, hi = 0, per = 1, more = 0, part_chunks = 0;
+    if (one_scan) {
+        const uint32_t items = present * hr;
+        if (items <= gridDim.x) {
+            const uint32_t free_cta = gridDim.x - min(items, gridDim.x / 2);
+            const uint32_t want = max((total + free_cta - 1) / free_cta, (uint32_t)pl.min_chunks);
+            uint32_t units;
+            const uint32_t mine_units = (mine + want - 1) / want * hr;
+            const uint32_t u0 = scan(mine_units, units);
+            if (units <= gridDim.x && want <= total / gridDim.x + 2 * n_warps) {
+                part_chunks = want;
+                n_cta = units;
+                if (u0 <= blockIdx.x && blockIdx.x < u0 + mine_units) {
+                    sm_b = tid;
+                    sm_base = u0;
+                }
+            }
+        }
+    }
     auto range_of = [&](uint32_t c) { return per * c + min(c, more); };
     auto owner_of = [&](uint32_t chunk) {
         const uint32_t cut = more * (per + 1);
         return chunk < cut ? chunk / (per + 1) : more + (chunk - cut) / per;
     };
-    const uint32_t lo = range_of(blockIdx.x), hi = range_of(blockIdx.x + 1);
-    // the sequence of chunk lo
-    {
+    if (part_chunks == 0) {
+        n_cta = min((total + pl.min_chunks - 1) / pl.min_chunks, gridDim.x);
+        // the first `more` CTAs take one chunk more than the others
+        per = total / n_cta;
+        more = total - per * n_cta;
+        if (blockIdx.x < n_cta) {
+            lo = range_of(blockIdx.x);
+            hi = range_of(blockIdx.x + 1);
+        }
+        // the sequence of chunk lo
         uint32_t run = 0;
         for (int b0 = 0; b0 < a.B; b0 += blockDim.x) {
-            const int b = b0 + tid;
-            const uint32_t mine = b < a.B ? chunks_of(geo, a, b) : 0;
-            uint32_t incl = mine;
-            for (int i = 1; i < 32; i <<= 1) {
-                const uint32_t o = __shfl_up_sync(0xffffffffu, incl, i);
-                if (lane >= i) incl += o;
+            uint32_t all = 0;
+            if (!one_scan) {
+                mine = b0 + tid < a.B ? chunks_of(geo, a, b0 + tid) : 0;
+                before = scan(mine, all);
             }
-            __syncthreads();
-            if (lane == 31) sm_scan[warp] = incl;
-            __syncthreads();
-            for (int w = 0; w < n_warps; ++w) {
-                if (w < warp) incl += sm_scan[w];
-            }
-            const uint32_t at = (run + incl - mine) * hr;
+            const uint32_t at = (run + before) * hr;
             if (mine > 0 && at <= lo && lo < at + mine * hr) {
-                sm_b = b;
+                sm_b = b0 + tid;
                 sm_base = at;
             }
-            for (int w = 0; w < n_warps; ++w) run += sm_scan[w];
+            run += all;
         }
-        __syncthreads();
     }
+    if (blockIdx.x >= n_cta) return;
+    __syncthreads();
 
     const int qh = geo.heads * a.group;
     const int n_min = ks.ng == 2 && ks.bits[1] < ks.bits[0] ? ks.bits[1] : ks.bits[0];
     const uint32_t k_sw = swizzle_of<KS>(g);                                       // rows 8 i + g
     const uint32_t v_sw0 = swizzle_of<VS>(2 * l), v_sw1 = swizzle_of<VS>(2 * l + 1);   // rows 8 i + 2 l, 8 i + 2 l + 1
+    const Offsets offsets;
     // token `lane`'s scales in a stage
     const uint32_t ks_lane = 2 * ks.ng * (lane % pl.box_rows) + 128 * (lane / pl.box_rows);
     const uint32_t vs_lane = pl.scale_bytes / 2 + 2 * vs.ng * (lane % pl.box_rows) + 128 * (lane / pl.box_rows);
@@ -359,16 +428,33 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
     uint32_t base = sm_base;        // first chunk of sequence b
     uint32_t pos = lo;
     uint32_t phases = 0, flying = 0;    // parity of each stage's next completion; stages with copies in flight
-    while (pos < hi) {
+    while (true) {
         uint32_t nch = chunks_of(geo, a, b);
-        while (pos >= base + nch * hr) {
-            base += nch * hr;
-            nch = chunks_of(geo, a, ++b);
+        int item, c_first, c_end, cta0, n_part, cta0_slot = 0, slot = 2 * blockIdx.x;
+        if (part_chunks != 0) {
+            const uint32_t parts = (nch + part_chunks - 1) / part_chunks, unit = blockIdx.x - base;
+            item = (int)(unit / parts);
+            const uint32_t part = unit - item * parts;
+            c_first = (int)((uint64_t)nch * part / parts);
+            c_end = (int)((uint64_t)nch * (part + 1) / parts);
+            cta0 = (int)(blockIdx.x - part);
+            n_part = (int)parts;
+        } else {
+            while (pos >= base + nch * hr) {
+                base += nch * hr;
+                nch = chunks_of(geo, a, ++b);
+            }
+            item = (int)((pos - base) / nch);
+            const uint32_t first = base + item * nch;
+            c_first = (int)(pos - first);
+            c_end = min(c_first + (int)(hi - pos), (int)nch);
+            cta0 = (int)owner_of(first);
+            n_part = (int)owner_of(first + nch - 1) - cta0 + 1;
+            // a CTA's first range leaves its partial result in the first of its two places
+            slot += pos == lo ? 0 : 1;
+            cta0_slot = range_of(cta0) == first ? 0 : 1;
         }
-        const int item = (int)((pos - base) / nch);
-        const int c_first = (int)(pos - base - item * nch);
         const int head = item / pl.row_tiles, rt = item % pl.row_tiles;
-        const int c_end = min(c_first + (int)(hi - pos), (int)nch);
         const int len = a.lengths[b];
         const int end = (int)seen_end(geo, a, b);
         const int row0 = rt * R;
@@ -402,11 +488,21 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
             }
             __syncwarp();
         };
-        for (int s = 0; s < pl.stages; ++s) {
-            const int c = c_first + warp + s * n_warps;
-            if (c < c_end && !(a.drop && c == 0 && blockIdx.x == 0)) {
-                const int pg0 = page_of(c * kChunk);
-                issue(c, s, pg0, geo.page == 16 ? page_of(c * kChunk + 16) : pg0);
+        {
+            int pg0[4], pg1[4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int c = c_first + warp + s * n_warps;
+                pg0[s] = pg1[s] = -1;
+                if (s < pl.stages && c < c_end) {
+                    pg0[s] = page_of(c * kChunk);
+                    pg1[s] = geo.page == 16 ? page_of(c * kChunk + 16) : pg0[s];
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int c = c_first + warp + s * n_warps;
+                if (s < pl.stages && c < c_end && !(a.drop && c == 0 && blockIdx.x == 0)) issue(c, s, pg0[s], pg1[s]);
             }
         }
 
@@ -419,19 +515,23 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                 const int t = on ? row / a.group : 0, h = head * a.group + (on ? row % a.group : 0);
                 const uint16_t* q = a.Q + b * a.q_seq_stride + t * a.q_token_stride + h * a.q_head_stride;
                 const int32_t* perm = ks.perm + head * ks.D;
+                // all channels' numbers, then all queries: two waits for memory
+                const int code0 = key_code(ks.bits[0], lane >> 3, (lane & 7) >> 1, lane & 1);
+                const int code1 = key_code(ks.bits[1], lane >> 3, (lane & 7) >> 1, lane & 1);
                 float x[8];
+                int ch[8];
                 uint32_t top = 0;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    x[k] = 0.0f;
-                    if (k < nkb) {
-                        const int grp = k < ks.nb[0] ? 0 : 1;
-                        const int c = key_code(ks.bits[grp], lane >> 3, (lane & 7) >> 1, lane & 1);
-                        const int p = 32 * (grp ? k - ks.nb[0] : k) + c;
-                        if (on && p < ks.count[grp]) x[k] = scale_of(q[perm[(grp ? ks.count[0] : 0) + p]], bf16);
-                        top = max(top, __float_as_uint(x[k]) & 0x7FFFFFFFu);
-                    }
+                    const bool hi_group = k >= ks.nb[0];
+                    const int p = hi_group ? 32 * (k - ks.nb[0]) + code1 : 32 * k + code0;
+                    const bool in = on && k < nkb && p < (hi_group ? ks.count[1] : ks.count[0]);
+                    ch[k] = in ? __ldg(perm + (hi_group ? ks.count[0] : 0) + p) : -1;
                 }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = ch[k] >= 0 ? scale_of(q[ch[k]], bf16) : 0.0f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(x[k]) & 0x7FFFFFFFu);
                 top = __reduce_max_sync(0xffffffffu, top);
                 const int e = top == 0 ? 0 : min(13 - ((int)(top >> 23) - 127), 120);   // x 2^e: largest in [2^13, 2^14)
                 const float up = a.scale < 0.0f ? -pow2(e) : pow2(e);
@@ -689,8 +789,8 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt) {
                     uint32_t p[4], q[4];
-                    value_pairs<BITS>(at0 + 16 * kt * VR, at1 + 16 * kt * VR, p);
-                    value_pairs<BITS>(at0 + (16 * kt + 8) * VR, at1 + (16 * kt + 8) * VR, q);
+                    value_pairs<BITS>(at0 + 16 * kt * VR, at1 + 16 * kt * VR, offsets, p);
+                    value_pairs<BITS>(at0 + (16 * kt + 8) * VR, at1 + (16 * kt + 8) * VR, offsets, q);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         mma(ov[0][nt], p[0], p[1], q[0], q[1], wg[kt][nt][0], wg[kt][nt][1]);
@@ -707,14 +807,37 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                     else value_block(std::integral_constant<int, 2>{}, byte, wg, ov);
                 }
             };
+            if constexpr (WIDE) {
 #pragma unroll
-            for (int v = 0; v < NVB; ++v) {
-                if (v < vs.nb[0]) {
-                    if constexpr (WIDE) value_block(std::integral_constant<int, 4>{}, 16 * v, w[0], o[v]);
-                    else value_any(0, v, w[0], o[v]);
-                } else if (v < nvb) {
-                    if constexpr (WIDE) value_block(std::integral_constant<int, 8>{}, vs.off[1] + 32 * (v - vs.nb[0]), w[1], o[v]);
-                    else value_any(1, v - vs.nb[0], w[1], o[v]);
+                for (int v = 0; v < NVB; v += 2) {
+                    if (v + 1 < vs.nb[0]) {
+                        const uint32_t byte = 16 * v + 4 * g;
+                        const uint32_t at0 = vrow + row_byte<VS>(byte, v_sw0);
+                        const uint32_t at1 = VS == 64 ? at0 + VR : vrow + row_byte<VS>(byte, v_sw1) + VR;
+#pragma unroll
+                        for (int kt = 0; kt < 2; ++kt) {
+                            uint32_t p[4], q[4], p2[4], q2[4];
+                            value_pairs2(at0 + 16 * kt * VR, at1 + 16 * kt * VR, offsets, p, p2);
+                            value_pairs2(at0 + (16 * kt + 8) * VR, at1 + (16 * kt + 8) * VR, offsets, q, q2);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                mma(o[v][0][nt], p[0], p[1], q[0], q[1], w[0][kt][nt][0], w[0][kt][nt][1]);
+                                mma(o[v][1][nt], p[2], p[3], q[2], q[3], w[0][kt][nt][0], w[0][kt][nt][1]);
+                                mma(o[v + 1][0][nt], p2[0], p2[1], q2[0], q2[1], w[0][kt][nt][0], w[0][kt][nt][1]);
+                                mma(o[v + 1][1][nt], p2[2], p2[3], q2[2], q2[3], w[0][kt][nt][0], w[0][kt][nt][1]);
+                            }
+                        }
+                    } else {
+                        if (v < vs.nb[0]) value_block(std::integral_constant<int, 4>{}, 16 * v, w[0], o[v]);
+                        else if (v < nvb) value_block(std::integral_constant<int, 8>{}, vs.off[1] + 32 * (v - vs.nb[0]), w[1], o[v]);
+                        if (v + 1 < nvb) value_block(std::integral_constant<int, 8>{}, vs.off[1] + 32 * (v + 1 - vs.nb[0]), w[1], o[v + 1]);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int v = 0; v < NVB; ++v) {
+                    if (v < vs.nb[0]) value_any(0, v, w[0], o[v]);
+                    else if (v < nvb) value_any(1, v - vs.nb[0], w[1], o[v]);
                 }
             }
             __syncwarp();
@@ -748,11 +871,10 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
             }
             return;
         }
-        const bool whole = c_first == 0 && c_end == (int)nch;
-        const int segment = pos == lo ? 0 : 1;
+        const bool whole = n_part == 1;
         constexpr int PART = R * (32 * NVB + 2);      // floats of a partial result: outputs, then m, then l
         float* parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.scratch) + SONIQ_KV_SCRATCH_ZERO);
-        float* part = parts + (int64_t)(2 * blockIdx.x + segment) * PART;
+        float* part = parts + (int64_t)slot * PART;
         if (tid < R) {
             float mm = -INFINITY, ll = 0.0f;
             for (int wi = 0; wi < n_warps; ++wi) mm = fmaxf(mm, sm_m[wi * R + tid]);
@@ -782,7 +904,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
             }
         };
         // the value blocks of one pass: 8 NT rows x 32 PB outputs of 8 warps in the merge buffer
-        constexpr int PB = NT >= 4 ? 1 : (4 / NT < NVB ? 4 / NT : NVB);
+        constexpr int PB = NT >= 2 || NVB == 2 ? 2 : 4;
 #pragma unroll
         for (int v0 = 0; v0 < NVB; v0 += PB) {
 #pragma unroll
@@ -790,10 +912,11 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                 const int v = v0 + vi;
                 if (v < nvb) {
                     const int grp = v < vs.nb[0] ? 0 : 1, bits = vs.bits[grp], e = grp ? e1 : e0;
+                    const bool paired = WIDE && (v | 1) < vs.nb[0];      // value_pairs2's order
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float back = ldexpf(1.0f, e - (bits - 1) - place_log2(bits, i));
-                        const int code = value_code(bits, g, i);
+                        const float back = pow2(e - (bits - 1) - place_log2(bits, i));
+                        const int code = paired ? value_code2(g, i) - 30 * (v & 1) : value_code(bits, g, i);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -816,8 +939,6 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
         }
         if (!whole) {
             // the CTAs that share the item: the last to get here joins their parts in order
-            const uint32_t s_first = base + item * nch;
-            const int cta0 = (int)owner_of(s_first), cta1 = (int)owner_of(s_first + nch - 1), n_part = cta1 - cta0 + 1;
             unsigned* counter = static_cast<unsigned*>(a.scratch) + cta0;
             __threadfence();
             __syncthreads();
@@ -829,8 +950,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
             __syncthreads();
             if (sm_last) {
                 __threadfence();
-                const int head_seg = range_of(cta0) == s_first ? 0 : 1;
-                auto part_of = [&](int i) { return parts + (int64_t)(2 * (cta0 + i) + (i == 0 ? head_seg : 0)) * PART; };
+                auto part_of = [&](int i) { return parts + (int64_t)(2 * (cta0 + i) + (i == 0 ? cta0_slot : 0)) * PART; };
                 float* fp = merge;                      // [n_part][R]: each part's factor
                 for (int i = tid; i < n_part * R; i += blockDim.x) fp[i] = __ldcg(part_of(i / R) + R * 32 * NVB + i % R);
                 __syncthreads();
@@ -888,6 +1008,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
             }
         }
         pos += c_end - c_first;
+        if (part_chunks != 0 || pos >= hi) break;
         // the next item's copies land where this one's results were joined
         tc::fence_proxy_async_shared();
         __syncthreads();
@@ -1016,9 +1137,9 @@ cudaError_t launch_kv_attend(const KvGeom& geo, const KvAttendArgs& args, cudaSt
     const int64_t cap = (int64_t)a.max_pages << geo.page_shift;
     const int64_t most = (int64_t)a.B * geo.heads * r.pl.row_tiles * (cap / kChunk + 1);
     if (most >= 2147483648ll) return cudaErrorNotSupported;      // chunks are numbered in 32 bits
-    const int64_t by_size = (most + r.pl.min_chunks - 1) / r.pl.min_chunks;
-    const int64_t full = (int64_t)r.ctas_per_sm * num_sms();
-    const int grid = (int)(by_size < full ? by_size : full);
+    const int64_t by_size = (most + r.pl.min_chunks - 1) / r.pl.min_chunks, items = (int64_t)a.B * geo.heads * r.pl.row_tiles;
+    const int64_t want = by_size > items ? by_size : items, full = (int64_t)r.ctas_per_sm * num_sms();
+    const int grid = (int)(want < full ? want : full);
     RowsMaps maps;
     const int shared_row[2] = {r.ks, r.vs};
     for (int side = 0; side < 2; ++side) {
