@@ -28,17 +28,16 @@
 //  * Queries are scaled per row by a power of two to 2^13 (bf16 queries are
 //    exact in fp16 then), softmax weights times value scales by a running power
 //    of two (the largest scale met), so no range of either type is lost.
-#include "kv_internal.h"
 #include <type_traits>
 
-#include "tc_ptx.cuh"
+#include "kv_device.cuh"
+#include "kv_split.cuh"
 
 namespace soniq {
 
 namespace {
 
 constexpr int kChunk = 32;                   // tokens a warp takes at a time
-constexpr float kLog2e = 1.4426950408889634f;
 
 struct RowsPlan {
     int row_tiles;        // tiles of 8 NT query rows per key head
@@ -53,102 +52,7 @@ struct RowsPlan {
     int min_chunks;       // fewest chunks worth a CTA
 };
 
-struct RowsMaps {
-    CUtensorMap codes[2], scales[2];     // keys, values
-};
-
-constexpr long long kWaitNs = 2000000000ll;   // bound of a wait for a copy
-
-// Tiled copies of packed rows (x: byte, y: row of the page's heads, z: page) and
-// of scales (x: entry of the page's heads, y: page); a page outside the cache
-// reads as zeros.
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
-        : "memory");
-}
-
-__device__ __forceinline__ uint32_t lds16(uint32_t a) {
-    uint32_t v;
-    asm volatile("ld.shared.u16 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint32_t lds8(uint32_t a) {
-    uint32_t v;
-    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint32_t lds32(uint32_t a) {
-    uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a) {
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-    return v;
-}
-
-__device__ __forceinline__ float4 lds128f(uint32_t a) {
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ void sts128f(uint32_t a, float x, float y, float z, float w) {
-    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(x), "f"(y), "f"(z), "f"(w) : "memory");
-}
-
-// d (16 x 8, fp32) += a (16 x 16) b (16 x 8)
-__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                    uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-// 8 x 8 transpose of halves over the warp
-__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
-    uint32_t r;
-    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
-    return r;
-}
-__device__ __forceinline__ float ex2(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-__device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-
-// (x & m) ^ f in one instruction (written out, as two constants otherwise make two)
-__device__ __forceinline__ uint32_t mask_flip(uint32_t x, uint32_t m, uint32_t f) {
-    uint32_t r;
-    asm("lop3.b32 %0, %1, %2, %3, 0x6A;" : "=r"(r) : "r"(x), "r"(m), "r"(f));
-    return r;
-}
-
-// The key side: a quad's lane l holds 8 codes of a block as four half pairs
-// h[0..3].  Codes of h[i] and the powers of two their place gives them:
-__device__ __forceinline__ int key_code(int bits, int l, int i, int half) {
-    if (bits == 8) return 8 * l + 4 * (i >> 1) + (i & 1) + 2 * half;
-    if (bits == 4) return 8 * l + 4 * (i & 1) + (i >> 1) + 2 * half;
-    return 16 * (l >> 1) + 4 * i + 2 * (l & 1) + half;
-}
-__device__ __forceinline__ int place_log2(int bits, int i) { return bits == 8 ? 0 : (bits == 4 ? 4 * (i & 1) : 2 * i); }
-
+// A quad's lane l holds 8 keys' codes of a block as four half pairs h[0..3] (key_code),
 // ... as u 2^-24 times the place's power; `at`: the lane's bytes of the block.
 template <int BITS>
 __device__ __forceinline__ void key_halves(uint32_t at, uint32_t (&h)[4]) {
@@ -185,26 +89,6 @@ __device__ __forceinline__ int value_code(int bits, int g, int i) {
     return 16 * (g >> 2) + 4 * i + (g & 3);
 }
 
-// The offsets 1024 + 8 and 1024 + 128 as half pairs, in registers: a logic
-// instruction has room for one constant, and the compiler would move the other
-// one in before each use.
-struct Offsets {
-    uint32_t c8, c128;
-    __device__ __forceinline__ Offsets() {
-        asm volatile("mov.b32 %0, 0x64086408;" : "=r"(c8));
-        asm volatile("mov.b32 %0, 0x64806480;" : "=r"(c128));
-    }
-};
-
-// 4-bit codes of two tokens, 4 from each half of w
-__device__ __forceinline__ void nibble_pairs(uint32_t w, const Offsets& f, uint32_t (&x)[4]) {
-    x[0] = sub2(mask_flip(w, 0x000F000Fu, f.c8), f.c8);
-    x[1] = sub2(mask_flip(w, 0x00F000F0u, f.c128), f.c128);
-    w >>= 8;
-    x[2] = sub2(mask_flip(w, 0x000F000Fu, f.c8), f.c8);
-    x[3] = sub2(mask_flip(w, 0x00F000F0u, f.c128), f.c128);
-}
-
 template <int BITS>
 __device__ __forceinline__ void value_pairs(uint32_t row0, uint32_t row1, const Offsets& f, uint32_t (&x)[4]) {
     if constexpr (BITS == 8) {
@@ -232,18 +116,6 @@ __device__ __forceinline__ void value_pairs2(uint32_t row0, uint32_t row1, const
 }
 __device__ __forceinline__ int value_code2(int g, int i) { return 8 * g + 4 * (i & 1) + (i >> 1); }
 
-__device__ __forceinline__ float scale_of(uint32_t bits16, bool bf16) {
-    return bf16 ? __uint_as_float(bits16 << 16) : __half2float(__ushort_as_half((uint16_t)bits16));
-}
-__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
-
-// Chunks of sequence b; the tokens it shows end at `end`.
-__device__ __forceinline__ int64_t seen_end(const KvGeom& geo, const KvAttendArgs& a, int b) {
-    const int len = a.lengths[b];
-    if (len < 0) return 0;
-    const int64_t cap = (int64_t)a.max_pages << geo.page_shift, end = (int64_t)len + a.T;
-    return end < cap ? end : cap;
-}
 // At least one for a present sequence, so that its rows are written.
 __device__ __forceinline__ int chunks_of(const KvGeom& geo, const KvAttendArgs& a, int b) {
     if (a.lengths[b] < 0) return 0;
@@ -275,7 +147,7 @@ constexpr int min_ctas() { return NT * NVB <= 4 ? 2 : 1; }
 // otherwise the widths are looked up block by block.
 template <int NT, int NVB, int KS, int VS, bool WIDE>
 __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
-    kv_rows_kernel(const KvGeom geo, const KvAttendArgs a, const RowsPlan pl, const __grid_constant__ RowsMaps maps) {
+    kv_rows_kernel(const KvGeom geo, const KvAttendArgs a, const RowsPlan pl, const __grid_constant__ KvMaps maps) {
     extern __shared__ __align__(1024) uint8_t smem[];
     constexpr int R = 8 * NT;
     constexpr int KB = kChunk * KS, VB = kChunk * VS;      // bytes of a stage's rows
@@ -301,11 +173,9 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
     float* sm_m = sm_tl + R;                                         // [8][R]
     float* sm_l = sm_m + 8 * R;                                      // [8][R]
     int16_t* sm_chan = reinterpret_cast<int16_t*>(sm_l + 8 * R);     // [32 NVB]
-    uint32_t* sm_scan = reinterpret_cast<uint32_t*>(smem + pl.bar_off + 256);      // [8]
-    uint32_t& sm_base = sm_scan[8];
-    int& sm_b = reinterpret_cast<int&>(sm_scan[9]);
-    int& sm_last = reinterpret_cast<int&>(sm_scan[10]);
-    int& sm_abort = reinterpret_cast<int&>(sm_scan[11]);
+    uint32_t* sm_scan = reinterpret_cast<uint32_t*>(smem + pl.bar_off + 256);      // [16]
+    int& sm_last = reinterpret_cast<int&>(sm_scan[16]);
+    int& sm_abort = reinterpret_cast<int&>(sm_scan[17]);
     const uint32_t abort_flag = tc::smem_u32(&sm_abort);
 
     if (lane == 0) {
@@ -315,106 +185,10 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
     if (tid == 0) sm_abort = 0;
 
     // ---- this CTA's range of chunks --------------------------------------
-    if (blockIdx.x == 0) {
-        for (int b = tid; b < a.B; b += blockDim.x)
-            if (a.lengths[b] >= 0 && (int64_t)a.lengths[b] + a.T > ((int64_t)a.max_pages << geo.page_shift))
-                atomicOr(a.err, kErrKvIndex);
-    }
-    const uint32_t hr = geo.heads * pl.row_tiles;
-    // exclusive prefix sum over the CTA, and the total
-    auto scan = [&](uint32_t mine, uint32_t& all) {
-        uint32_t incl = mine;
-        for (int i = 1; i < 32; i <<= 1) {
-            const uint32_t o = __shfl_up_sync(0xffffffffu, incl, i);
-            if (lane >= i) incl += o;
-        }
-        __syncthreads();
-        if (lane == 31) sm_scan[warp] = incl;
-        __syncthreads();
-        all = 0;
-        uint32_t before = incl - mine;
-        for (int w = 0; w < n_warps; ++w) {
-            const uint32_t o = sm_scan[w];
-            if (w < warp) before += o;
-            all += o;
-        }
-        return before;
-    };
-    const bool one_scan = a.B <= (int)blockDim.x;
-    uint32_t total, mine = 0, before = 0;
-    int present = 0;
-    if (one_scan) {
-        mine = tid < a.B ? chunks_of(geo, a, tid) : 0;
-        present = __syncthreads_count(mine > 0);
-        before = scan(mine, total);
-    } else {
-        for (int b = tid; b < a.B; b += blockDim.x) mine += chunks_of(geo, a, b);
-        scan(mine, total);
-    }
-    // outputs of absent sequences
-    if (!one_scan || present < a.B) {
-        for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-            if (a.lengths[b] >= 0) continue;
-            const int64_t size = (int64_t)a.T * a.group * geo.heads * vs.D;
-            for (int64_t i = tid; i < size; i += blockDim.x) a.out[b * size + i] = 0;
-        }
-    }
-    total *= hr;       // below 2^31 (checked on the host)
-    if (total == 0) return;
-    // Few items: each is cut in equal parts, a CTA to a part, if that costs no CTA
-    // more than two rounds of its warps over the even split.  Otherwise the list of
-    // all chunks is cut evenly, and a CTA may end one item and begin another.
-    uint32_t n_cta, lo = 0, hi = 0, per = 1, more = 0, part_chunks = 0;
-    if (one_scan) {
-        const uint32_t items = present * hr;
-        if (items <= gridDim.x) {
-            const uint32_t free_cta = gridDim.x - min(items, gridDim.x / 2);
-            const uint32_t want = max((total + free_cta - 1) / free_cta, (uint32_t)pl.min_chunks);
-            uint32_t units;
-            const uint32_t mine_units = (mine + want - 1) / want * hr;
-            const uint32_t u0 = scan(mine_units, units);
-            if (units <= gridDim.x && want <= total / gridDim.x + 2 * n_warps) {
-                part_chunks = want;
-                n_cta = units;
-                if (u0 <= blockIdx.x && blockIdx.x < u0 + mine_units) {
-                    sm_b = tid;
-                    sm_base = u0;
-                }
-            }
-        }
-    }
-    auto range_of = [&](uint32_t c) { return per * c + min(c, more); };
-    auto owner_of = [&](uint32_t chunk) {
-        const uint32_t cut = more * (per + 1);
-        return chunk < cut ? chunk / (per + 1) : more + (chunk - cut) / per;
-    };
-    if (part_chunks == 0) {
-        n_cta = min((total + pl.min_chunks - 1) / pl.min_chunks, gridDim.x);
-        // the first `more` CTAs take one chunk more than the others
-        per = total / n_cta;
-        more = total - per * n_cta;
-        if (blockIdx.x < n_cta) {
-            lo = range_of(blockIdx.x);
-            hi = range_of(blockIdx.x + 1);
-        }
-        // the sequence of chunk lo
-        uint32_t run = 0;
-        for (int b0 = 0; b0 < a.B; b0 += blockDim.x) {
-            uint32_t all = 0;
-            if (!one_scan) {
-                mine = b0 + tid < a.B ? chunks_of(geo, a, b0 + tid) : 0;
-                before = scan(mine, all);
-            }
-            const uint32_t at = (run + before) * hr;
-            if (mine > 0 && at <= lo && lo < at + mine * hr) {
-                sm_b = b0 + tid;
-                sm_base = at;
-            }
-            run += all;
-        }
-    }
-    if (blockIdx.x >= n_cta) return;
-    __syncthreads();
+    check_lengths(geo, a);
+    auto chunks = [&](int b) { return (uint32_t)chunks_of(geo, a, b); };
+    Split split;
+    if (!split.begin(chunks, a.B, geo.heads * pl.row_tiles, pl.min_chunks, 2 * n_warps, sm_scan)) return;
 
     const int qh = geo.heads * a.group;
     const int n_min = ks.ng == 2 && ks.bits[1] < ks.bits[0] ? ks.bits[1] : ks.bits[0];
@@ -424,37 +198,11 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
     // token `lane`'s scales in a stage
     const uint32_t ks_lane = 2 * ks.ng * (lane % pl.box_rows) + 128 * (lane / pl.box_rows);
     const uint32_t vs_lane = pl.scale_bytes / 2 + 2 * vs.ng * (lane % pl.box_rows) + 128 * (lane / pl.box_rows);
-    int b = sm_b;
-    uint32_t base = sm_base;        // first chunk of sequence b
-    uint32_t pos = lo;
     uint32_t phases = 0, flying = 0;    // parity of each stage's next completion; stages with copies in flight
     while (true) {
-        uint32_t nch = chunks_of(geo, a, b);
-        int item, c_first, c_end, cta0, n_part, cta0_slot = 0, slot = 2 * blockIdx.x;
-        if (part_chunks != 0) {
-            const uint32_t parts = (nch + part_chunks - 1) / part_chunks, unit = blockIdx.x - base;
-            item = (int)(unit / parts);
-            const uint32_t part = unit - item * parts;
-            c_first = (int)((uint64_t)nch * part / parts);
-            c_end = (int)((uint64_t)nch * (part + 1) / parts);
-            cta0 = (int)(blockIdx.x - part);
-            n_part = (int)parts;
-        } else {
-            while (pos >= base + nch * hr) {
-                base += nch * hr;
-                nch = chunks_of(geo, a, ++b);
-            }
-            item = (int)((pos - base) / nch);
-            const uint32_t first = base + item * nch;
-            c_first = (int)(pos - first);
-            c_end = min(c_first + (int)(hi - pos), (int)nch);
-            cta0 = (int)owner_of(first);
-            n_part = (int)owner_of(first + nch - 1) - cta0 + 1;
-            // a CTA's first range leaves its partial result in the first of its two places
-            slot += pos == lo ? 0 : 1;
-            cta0_slot = range_of(cta0) == first ? 0 : 1;
-        }
-        const int head = item / pl.row_tiles, rt = item % pl.row_tiles;
+        const Segment seg = split.segment(chunks);
+        const int b = seg.entry, c_first = seg.c_first, c_end = seg.c_end, n_part = seg.n_part;
+        const int head = seg.item / pl.row_tiles, rt = seg.item % pl.row_tiles;
         const int len = a.lengths[b];
         const int end = (int)seen_end(geo, a, b);
         const int row0 = rt * R;
@@ -874,7 +622,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
         const bool whole = n_part == 1;
         constexpr int PART = R * (32 * NVB + 2);      // floats of a partial result: outputs, then m, then l
         float* parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.scratch) + SONIQ_KV_SCRATCH_ZERO);
-        float* part = parts + (int64_t)slot * PART;
+        float* part = parts + (int64_t)seg.slot * PART;
         if (tid < R) {
             float mm = -INFINITY, ll = 0.0f;
             for (int wi = 0; wi < n_warps; ++wi) mm = fmaxf(mm, sm_m[wi * R + tid]);
@@ -939,7 +687,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
         }
         if (!whole) {
             // the CTAs that share the item: the last to get here joins their parts in order
-            unsigned* counter = static_cast<unsigned*>(a.scratch) + cta0;
+            unsigned* counter = static_cast<unsigned*>(a.scratch) + seg.cta0;
             __threadfence();
             __syncthreads();
             if (tid == 0) {
@@ -950,7 +698,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
             __syncthreads();
             if (sm_last) {
                 __threadfence();
-                auto part_of = [&](int i) { return parts + (int64_t)(2 * (cta0 + i) + (i == 0 ? cta0_slot : 0)) * PART; };
+                auto part_of = [&](int i) { return parts + (int64_t)part_slot(seg, i) * PART; };
                 float* fp = merge;                      // [n_part][R]: each part's factor
                 for (int i = tid; i < n_part * R; i += blockDim.x) fp[i] = __ldcg(part_of(i / R) + R * 32 * NVB + i % R);
                 __syncthreads();
@@ -1007,8 +755,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                 }
             }
         }
-        pos += c_end - c_first;
-        if (part_chunks != 0 || pos >= hi) break;
+        if (!split.next(seg)) break;
         // the next item's copies land where this one's results were joined
         tc::fence_proxy_async_shared();
         __syncthreads();
@@ -1043,7 +790,7 @@ RowsLaunch plan_rows(const KvGeom& geo, int64_t T, int64_t group) {
     const int stage = kChunk * (r.ks + r.vs);
     const int q = nkb * r.nt * 512;
     const int misc = (4 * (5 * R + 16 * R) + 2 * 32 * r.nvb + 15) / 16 * 16;
-    const int fixed = q + misc + 256 + 64;
+    const int fixed = q + misc + 256 + 128;
     auto warp_bytes = [&](int stages) { return stages * (stage + p.scale_bytes) + 16 * kChunk; };
     // two stages at least; two CTAs per SM where they and the registers allow it
     r.warps = 8;
@@ -1057,51 +804,14 @@ RowsLaunch plan_rows(const KvGeom& geo, int64_t T, int64_t group) {
     p.q_off = p.s_off + r.warps * (p.stages * p.scale_bytes + 16 * kChunk);
     p.misc_off = p.q_off + q;
     p.bar_off = p.misc_off + misc;
-    p.smem = p.bar_off + 256 + 64;
+    p.smem = p.bar_off + 256 + 128;
     p.min_chunks = 8;
     r.wide = ks.bits[0] == 4 && vs.bits[0] == 4 && ks.bits[1] == 8 && vs.bits[1] == 8;
     return r;
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-    static const EncodeTiledFn fn = [] {
-        void* ptr = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        const bool ok = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &q) ==
-                            cudaSuccess && q == cudaDriverEntryPointSuccess;
-        return ok ? reinterpret_cast<EncodeTiledFn>(ptr) : nullptr;
-    }();
-    return fn;
-}
-
-// Codes as [pages][rows of all heads][row bytes], scales as [pages][entries of
-// all heads]; row_bytes: what a shared row holds of it.
-bool encode_side(const KvGeom& geo, const KvSide& s, int shared_row, int box_rows, CUtensorMap* codes, CUtensorMap* scales) {
-    const EncodeTiledFn enc = encode_fn();
-    if (enc == nullptr) return false;
-    const cuuint32_t step[3] = {1, 1, 1};
-    const cuuint64_t rows = (cuuint64_t)geo.heads * geo.page;
-    const cuuint64_t dims[3] = {(cuuint64_t)s.row_bytes, rows, (cuuint64_t)geo.n_pages};
-    const cuuint64_t strides[2] = {(cuuint64_t)s.row_bytes, rows * s.row_bytes};
-    const cuuint32_t box[3] = {(cuuint32_t)(shared_row < 128 ? shared_row : 128), (cuuint32_t)box_rows, 1};
-    if (enc(codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, s.codes, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            shared_row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-        return false;
-    const cuuint64_t sdims[2] = {rows * s.ng, (cuuint64_t)geo.n_pages};
-    const cuuint64_t sstrides[1] = {rows * s.ng * 2};
-    const cuuint32_t sbox[2] = {(cuuint32_t)(box_rows * s.ng), 1};
-    return enc(scales, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, s.scales, sdims, sstrides, sbox, step,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int NT, int NVB, int KS, int VS>
-cudaError_t run_rows(const KvGeom& geo, const KvAttendArgs& a, const RowsLaunch& r, const RowsMaps& maps, int grid,
+cudaError_t run_rows(const KvGeom& geo, const KvAttendArgs& a, const RowsLaunch& r, const KvMaps& maps, int grid,
                      cudaStream_t st) {
     auto* kernel = r.wide ? kv_rows_kernel<NT, NVB, KS, VS, true> : kv_rows_kernel<NT, NVB, KS, VS, false>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, r.pl.smem);
@@ -1113,7 +823,7 @@ cudaError_t run_rows(const KvGeom& geo, const KvAttendArgs& a, const RowsLaunch&
 }
 
 template <int NVB, int KS, int VS>
-cudaError_t run_rows(const KvGeom& geo, const KvAttendArgs& a, const RowsLaunch& r, const RowsMaps& maps, int grid,
+cudaError_t run_rows(const KvGeom& geo, const KvAttendArgs& a, const RowsLaunch& r, const KvMaps& maps, int grid,
                      cudaStream_t st) {
     if (r.nt == 1) return run_rows<1, NVB, KS, VS>(geo, a, r, maps, grid, st);
     if constexpr (NVB <= 4) {
@@ -1122,10 +832,14 @@ cudaError_t run_rows(const KvGeom& geo, const KvAttendArgs& a, const RowsLaunch&
     return run_rows<2, NVB, KS, VS>(geo, a, r, maps, grid, st);
 }
 
+// Whether the rows of a key head go to the tile kernel.
+bool takes_tile(const KvGeom& geo, int64_t T, int64_t group) { return T * group > 16 && kv_tile_supported(geo, T, group); }
+
 }  // namespace
 
 int64_t kv_attend_scratch(const KvGeom& geo, int64_t B, int64_t T, int64_t group) {
     if (B == 0 || T == 0) return 0;
+    if (takes_tile(geo, T, group)) return kv_tile_scratch(geo, T, group);
     const RowsLaunch r = plan_rows(geo, T, group);
     return SONIQ_KV_SCRATCH_ZERO + (int64_t)2 * r.ctas_per_sm * num_sms() * 8 * r.nt * (32 * r.nvb + 2) * 4;
 }
@@ -1133,6 +847,7 @@ int64_t kv_attend_scratch(const KvGeom& geo, int64_t B, int64_t T, int64_t group
 cudaError_t launch_kv_attend(const KvGeom& geo, const KvAttendArgs& args, cudaStream_t st) {
     KvAttendArgs a = args;
     a.drop = take_drop_arrival();
+    if (takes_tile(geo, a.T, a.group)) return launch_kv_tile(geo, a, st);
     const RowsLaunch r = plan_rows(geo, a.T, a.group);
     const int64_t cap = (int64_t)a.max_pages << geo.page_shift;
     const int64_t most = (int64_t)a.B * geo.heads * r.pl.row_tiles * (cap / kChunk + 1);
@@ -1140,10 +855,13 @@ cudaError_t launch_kv_attend(const KvGeom& geo, const KvAttendArgs& args, cudaSt
     const int64_t by_size = (most + r.pl.min_chunks - 1) / r.pl.min_chunks, items = (int64_t)a.B * geo.heads * r.pl.row_tiles;
     const int64_t want = by_size > items ? by_size : items, full = (int64_t)r.ctas_per_sm * num_sms();
     const int grid = (int)(want < full ? want : full);
-    RowsMaps maps;
+    KvMaps maps;
     const int shared_row[2] = {r.ks, r.vs};
     for (int side = 0; side < 2; ++side) {
-        if (!encode_side(geo, geo.s[side], shared_row[side], r.pl.box_rows, &maps.codes[side], &maps.scales[side]))
+        const int row = shared_row[side];
+        if (!encode_side(geo, geo.s[side], row < 128 ? row : 128, r.pl.box_rows,
+                         row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, &maps.codes[side],
+                         &maps.scales[side]))
             return cudaErrorUnknown;
     }
     if (r.nvb == 2) return run_rows<2, 64, 64>(geo, a, r, maps, grid, st);

@@ -1,0 +1,175 @@
+// Device helpers and tensor maps shared by the attention kernels.
+#pragma once
+
+#include <cuda.h>
+
+#include "kv_internal.h"
+#include "tc_ptx.cuh"
+
+namespace soniq {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr long long kWaitNs = 2000000000ll;   // bound of a wait for a copy
+
+// Tiled copies of packed rows (x: byte, y: row of the page's heads, z: page) and
+// of scales (x: entry of the page's heads, y: page); a page outside the cache
+// reads as zeros.
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+
+__device__ __forceinline__ uint32_t lds16(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ float4 lds128f(uint32_t a) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts128f(uint32_t a, float x, float y, float z, float w) {
+    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(x), "f"(y), "f"(z), "f"(w) : "memory");
+}
+
+// d (16 x 8, fp32) += a (16 x 16) b (16 x 8)
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                    uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// 8 x 8 transpose of halves over the warp
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// (x & m) ^ f in one instruction (written out, as two constants otherwise make two)
+__device__ __forceinline__ uint32_t mask_flip(uint32_t x, uint32_t m, uint32_t f) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0x6A;" : "=r"(r) : "r"(x), "r"(m), "r"(f));
+    return r;
+}
+
+__device__ __forceinline__ float scale_of(uint32_t bits16, bool bf16) {
+    return bf16 ? __uint_as_float(bits16 << 16) : __half2float(__ushort_as_half((uint16_t)bits16));
+}
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+
+
+// Eight codes of a block, its l-th quarter, unpack to four half pairs: which codes
+// they are, and the powers of two their places in the word give them.
+__device__ __forceinline__ int key_code(int bits, int l, int i, int half) {
+    if (bits == 8) return 8 * l + 4 * (i >> 1) + (i & 1) + 2 * half;
+    if (bits == 4) return 8 * l + 4 * (i & 1) + (i >> 1) + 2 * half;
+    return 16 * (l >> 1) + 4 * i + 2 * (l & 1) + half;
+}
+__device__ __forceinline__ int place_log2(int bits, int i) { return bits == 8 ? 0 : (bits == 4 ? 4 * (i & 1) : 2 * i); }
+
+// The offsets 1024 + 8 and 1024 + 128 as half pairs, in registers: a logic
+// instruction has room for one constant, and the compiler would move the other
+// one in before each use.
+struct Offsets {
+    uint32_t c8, c128;
+    __device__ __forceinline__ Offsets() {
+        asm volatile("mov.b32 %0, 0x64086408;" : "=r"(c8));
+        asm volatile("mov.b32 %0, 0x64806480;" : "=r"(c128));
+    }
+};
+
+// 4-bit codes of two tokens, 4 from each half of w
+__device__ __forceinline__ void nibble_pairs(uint32_t w, const Offsets& f, uint32_t (&x)[4]) {
+    x[0] = sub2(mask_flip(w, 0x000F000Fu, f.c8), f.c8);
+    x[1] = sub2(mask_flip(w, 0x00F000F0u, f.c128), f.c128);
+    w >>= 8;
+    x[2] = sub2(mask_flip(w, 0x000F000Fu, f.c8), f.c8);
+    x[3] = sub2(mask_flip(w, 0x00F000F0u, f.c128), f.c128);
+}
+
+
+// The cache's tensor maps: keys, values.
+struct KvMaps {
+    CUtensorMap codes[2], scales[2];
+};
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+inline EncodeTiledFn encode_fn() {
+    static const EncodeTiledFn fn = [] {
+        void* ptr = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        const bool ok = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &q) ==
+                            cudaSuccess && q == cudaDriverEntryPointSuccess;
+        return ok ? reinterpret_cast<EncodeTiledFn>(ptr) : nullptr;
+    }();
+    return fn;
+}
+
+// Tensor maps of a side: codes as [pages][rows of all heads][row bytes], in boxes
+// of box_rows rows by box_bytes; scales as [pages][entries of all heads].
+inline bool encode_side(const KvGeom& geo, const KvSide& s, int box_bytes, int box_rows, CUtensorMapSwizzle swizzle,
+                        CUtensorMap* codes, CUtensorMap* scales) {
+    const EncodeTiledFn enc = encode_fn();
+    if (enc == nullptr) return false;
+    const cuuint32_t step[3] = {1, 1, 1};
+    const cuuint64_t rows = (cuuint64_t)geo.heads * geo.page;
+    const cuuint64_t dims[3] = {(cuuint64_t)s.row_bytes, rows, (cuuint64_t)geo.n_pages};
+    const cuuint64_t strides[2] = {(cuuint64_t)s.row_bytes, rows * s.row_bytes};
+    const cuuint32_t box[3] = {(cuuint32_t)box_bytes, (cuuint32_t)box_rows, 1};
+    if (enc(codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, s.codes, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return false;
+    const cuuint64_t sdims[2] = {rows * s.ng, (cuuint64_t)geo.n_pages};
+    const cuuint64_t sstrides[1] = {rows * s.ng * 2};
+    const cuuint32_t sbox[2] = {(cuuint32_t)(box_rows * s.ng), 1};
+    return enc(scales, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, s.scales, sdims, sstrides, sbox, step,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+
+}  // namespace soniq

@@ -66,6 +66,10 @@ cudaError_t launch_kv_read(const KvGeom& geo, const int64_t* slots, int64_t n, u
                            cudaStream_t st);
 cudaError_t launch_kv_attend(const KvGeom& geo, const KvAttendArgs& a, cudaStream_t st);
 int64_t kv_attend_scratch(const KvGeom& geo, int64_t B, int64_t T, int64_t group);
+// Many query rows per key head (kv_tile.cu).
+bool kv_tile_supported(const KvGeom& geo, int64_t T, int64_t group);
+int64_t kv_tile_scratch(const KvGeom& geo, int64_t T, int64_t group);
+cudaError_t launch_kv_tile(const KvGeom& geo, const KvAttendArgs& a, cudaStream_t st);
 
 #ifdef __CUDACC__
 // The cache's 16-bit types as fp32, and back with one rounding.

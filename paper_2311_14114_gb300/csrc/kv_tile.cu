@@ -1,0 +1,804 @@
+// Attention of many query rows per key head over the quantized cache: drafted
+// trees, pieces of prompts.
+//
+//   S = Q K^T, P = softmax(S), O = P V on tcgen05, accumulators in TMEM.
+//
+// With 128 rows to a tile the products (4 x 64 x 128 x 128 multiply-adds per 64
+// tokens at 128 channels) and the exponentials are the work; the cache's bytes
+// are read once per tile of up to 256 rows.  One CTA per SM, 16 warps:
+//   warps 0-3, 4-7  softmax of two row tiles (a thread per row, its scores from
+//                   TMEM), each with its own S, P and O columns;
+//   warps 8-11      unpack a block of 64 tokens into fp16 operand tiles (codes
+//                   exactly, scales as fp32 beside them);
+//   warp 12         issues the MMAs;  warp 13  copies packed rows by TMA.
+// (Registers move to the softmax warps: 2 x 192 + 72 + 56 = 4 x 128 a thread.)
+// While one tile's softmax runs, the tensor cores work for the other.  With at
+// most 128 rows both softmax groups serve the same tile on alternate blocks,
+// as two streams joined at the end.
+//
+// Numerics.  Queries are fp16, each row scaled by a power of two to 2^13; codes
+// are exact in fp16, so S is an exact product summed in fp32, per precision
+// group, and gets its scales in fp32.  P times the value scale (normalised by a
+// running power of two) is rounded to fp16.  The running maximum is raised only
+// when a score exceeds it by more than 2^8: P stays below 2^13.
+//
+// Values keep their row order (tokens x channels) as the MN-major operand of
+// O = P V, so both operand tiles have one layout: 64-code column groups of
+// [token][128 bytes], 16-byte pieces swizzled by the token.
+#include <type_traits>
+
+#include "kv_device.cuh"
+#include "kv_split.cuh"
+#include "soniq_device.cuh"
+
+namespace soniq {
+
+namespace {
+
+constexpr int kTok = 64;                 // tokens of a block
+constexpr int kThreads = 512;
+constexpr int kAtom = kTok * 128;        // bytes of a 64-code column group of a K or V tile
+constexpr int kQAtom = 128 * 128;        // ... of a query tile
+constexpr int kSlotCols = 256;           // TMEM columns of a softmax group: S (and P over it), then O
+constexpr float kLazy = 8.0f;            // a maximum may be exceeded by this (log2) before O is rescaled
+
+struct TilePlan {
+    int rows;               // query rows per key head
+    int tiles;              // row tiles of one CTA: 2, or 1 with two streams
+    int row_units;          // CTA-sized tiles of rows per key head
+    int k_atoms, v_atoms, v_atom1;   // column groups; v_atom1: the second precision group's first
+    int o_cols;
+    int stages, raw_stages;
+    int stage_bytes, raw_bytes, raw_v, raw_s;     // raw_s: scales, 128 bytes or more for each copy
+    int box_rows, scale_step[2];
+    int ring_off, raw_off, misc_off, smem;
+    int out_stride;         // bytes of a staged output row
+    int min_chunks;
+};
+
+struct Bars {               // offsets in 8-byte barriers
+    static constexpr int raw_full = 0, raw_free = 4, k_ready = 8, v_ready = 12, kv_free = 16, s_full = 20, p_full = 22,
+                         o_full = 24, q_full = 26, drain = 27;
+};
+
+__device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(at)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};\n\ttcgen05.wait::st.sync.aligned;" ::"r"(at),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+
+// Values as an MN-major operand: 64-channel column groups kAtom apart, 8-token rows of 1024 bytes.
+__device__ __forceinline__ uint64_t value_desc(uint32_t at) {
+    uint64_t d = (uint64_t)((at & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(kAtom >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc));
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(acc));
+}
+
+// Eight codes at `src` (4, 8 or 2 bytes) as signed halves times their places' powers.
+__device__ __forceinline__ uint4 unpack8(uint32_t src, int bits, const Offsets& f) {
+    uint32_t x[4];
+    if (bits == 4) {
+        nibble_pairs(lds32(src), f, x);
+    } else if (bits == 8) {
+        const uint2 w = lds64(src);
+        x[0] = sub2(mask_flip(w.x, 0x00FF00FFu, f.c128), f.c128);
+        x[1] = sub2(mask_flip(w.x >> 8, 0x00FF00FFu, f.c128), f.c128);
+        x[2] = sub2(mask_flip(w.y, 0x00FF00FFu, f.c128), f.c128);
+        x[3] = sub2(mask_flip(w.y >> 8, 0x00FF00FFu, f.c128), f.c128);
+    } else {
+        const uint32_t w = __byte_perm(lds16(src), 0, 0x4140);
+        x[0] = sub2(mask_flip(w, 0x00030003u, 0x64026402u), 0x64026402u);
+        x[1] = sub2(mask_flip(w, 0x000C000Cu, f.c8), f.c8);
+        x[2] = sub2(mask_flip(w, 0x00300030u, 0x64206420u), 0x64206420u);
+        x[3] = sub2(mask_flip(w, 0x00C000C0u, f.c128), f.c128);
+    }
+    return make_uint4(x[0], x[1], x[2], x[3]);
+}
+
+__device__ __forceinline__ void bar_group(int id, int threads) {
+    asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+// Column `col` (of its group's unpacked codes) -> code of the group.
+__device__ __forceinline__ int column_code(int bits, int col) {
+    return 32 * (col >> 5) + key_code(bits, (col >> 3) & 3, (col & 7) >> 1, col & 1);
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+    kv_tile_kernel(const KvGeom geo, const KvAttendArgs a, const TilePlan pl, const __grid_constant__ KvMaps maps) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const KvSide &ks = geo.s[0], &vs = geo.s[1];
+    const bool bf16 = geo.bf16 != 0;
+    const uint32_t smem0 = tc::smem_u32(smem);
+    const uint32_t ring = smem0 + pl.ring_off, raw = smem0 + pl.raw_off;
+    uint8_t* misc = smem + pl.misc_off;
+    const uint32_t bars = smem0 + pl.misc_off;
+    uint32_t* words = reinterpret_cast<uint32_t*>(misc + 256);       // [16] for the split, then:
+    const uint32_t abort_flag = tc::smem_u32(words + 16);
+    uint32_t* tmem_at = words + 17;
+    uint32_t* sm_last = words + 18;
+    int* sm_e = reinterpret_cast<int*>(words + 20);                  // [4 stages][2]: power of two above the value scales
+    float* sm_fac = reinterpret_cast<float*>(misc + 512);            // [256] factor of a row's scores
+    float* sm_m = sm_fac + 256;                                      // [128], of the second stream
+    float* sm_l = sm_m + 128;
+    int16_t* sm_chan = reinterpret_cast<int16_t*>(sm_l + 128);       // [192] channel of an output column
+    float* sm_back = reinterpret_cast<float*>(sm_chan + 192);        // [192] its power of two
+    auto bar = [&](int i) { return bars + 8u * i; };
+
+    if (tid == 0) {
+        for (int i = 0; i < 4; ++i) {
+            tc::mbar_init(bar(Bars::raw_full + i), 1);
+            tc::mbar_init(bar(Bars::raw_free + i), 4);
+            tc::mbar_init(bar(Bars::k_ready + i), 4);
+            tc::mbar_init(bar(Bars::v_ready + i), 4);
+            tc::mbar_init(bar(Bars::kv_free + i), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            tc::mbar_init(bar(Bars::s_full + i), 1);
+            tc::mbar_init(bar(Bars::p_full + i), 4);
+            tc::mbar_init(bar(Bars::o_full + i), 1);
+        }
+        tc::mbar_init(bar(Bars::q_full), 8);
+        tc::mbar_init(bar(Bars::drain), 1);
+        words[16] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+
+    // ---- this CTA's share: entries are (sequence, unit of row tiles) ----
+    check_lengths(geo, a);
+    const int unit_rows = 128 * pl.tiles;
+    auto last_token = [&](int u) { return (min((u + 1) * unit_rows, pl.rows) - 1) / a.group; };
+    auto end_of = [&](int b, int u) {      // tokens that any row of the unit may see
+        const int64_t end = seen_end(geo, a, b);
+        const int64_t chain = (int64_t)a.lengths[b] + last_token(u) + 1;
+        return (int)(a.mask == nullptr && chain < end ? chain : end);
+    };
+    auto chunks = [&](int e) -> uint32_t {
+        const int b = e / pl.row_units;
+        if (a.lengths[b] < 0) return 0;
+        const int end = end_of(b, e % pl.row_units);
+        return end == 0 ? 1 : (end + kTok - 1) / kTok;      // a present sequence's rows are written even if they see nothing
+    };
+    Split split;
+    if (!split.begin(chunks, a.B * pl.row_units, geo.heads, pl.min_chunks, 8, words)) return;
+
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(tmem_at)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tmem = *tmem_at;
+    const uint32_t o_off = kTok * ks.ng;     // O's first column in a slot
+    const int pa0 = 32 * ks.nb[0], pa1 = 32 * ks.nb[1], va0 = 32 * vs.nb[0], va1 = 32 * vs.nb[1];
+
+    auto wait = [&](int i, uint32_t parity) {
+        return tc::wait_bounded_warp(bar(i), parity & 1u, abort_flag, kWaitNs, a.err, kErrWait);
+    };
+    uint32_t n_block = 0;        // blocks this CTA has gone through (stages and their parities)
+    uint32_t n_s[2] = {0, 0};    // ... of each softmax group
+    uint32_t n_o[2] = {0, 0}, n_seg = 0;      // segments that a softmax group took part in; all
+    bool ok = true;
+
+    auto work = [&](auto role) {
+    constexpr int ROLE = decltype(role)::value;      // 0 softmax, 1 unpacking, 2 MMAs and copies
+    while (true) {
+        const Segment seg = split.segment(chunks);
+        const int b = seg.entry / pl.row_units, unit = seg.entry % pl.row_units, head = seg.item;
+        const int row0 = unit * unit_rows;
+        const int len = a.lengths[b], end = end_of(b, unit);
+        const int nblk = seg.c_end - seg.c_first;
+        // row tiles at work, or streams: group s takes every block of its tile, or every second block
+        const int groups = pl.tiles == 2 ? (row0 + 128 < pl.rows ? 2 : 1) : (nblk > 1 ? 2 : 1);
+        const bool streams = pl.tiles == 1;
+
+        if (ROLE == 2 && warp == 13) {
+            // ---- copies ----
+            const int32_t* table = a.table + b * a.table_stride;
+            for (int j = 0; ok && j < nblk; ++j) {
+                const uint32_t n = n_block + j, r = n % pl.raw_stages;
+                const int p0 = (seg.c_first + j) * kTok;
+                const int boxes = p0 < end ? min(kTok / pl.box_rows, (end - p0 + pl.box_rows - 1) / pl.box_rows) : 0;
+                int page = -1;
+                if (lane < boxes) page = __ldg(table + ((p0 + lane * pl.box_rows) >> geo.page_shift));
+                const bool good = (unsigned)page < (unsigned)geo.n_pages;
+                if (lane < boxes && !good) atomicOr(a.err, kErrKvIndex);
+                if (!good) page = (int)geo.n_pages;        // reads as zeros
+                ok = wait(Bars::raw_free + r, (n / pl.raw_stages) + 1);
+                if (!ok) break;
+                if (a.drop && n == 0 && blockIdx.x == 0) continue;
+                const uint32_t at = raw + r * pl.raw_bytes, full = bar(Bars::raw_full + r);
+                if (tc::elect_one()) tc::mbar_arrive_expect_tx(full, boxes * pl.box_rows * (ks.row_bytes + vs.row_bytes + 2 * (ks.ng + vs.ng)));
+                for (int i = 0; i < boxes; ++i) {
+                    const int pg = __shfl_sync(0xffffffffu, page, i);
+                    const int row = head * geo.page + ((p0 + i * pl.box_rows) & (geo.page - 1));
+                    if (tc::elect_one()) {
+                        tma_load_3d(at + i * pl.box_rows * ks.row_bytes, &maps.codes[0], 0, row, pg, full);
+                        tma_load_3d(at + pl.raw_v + i * pl.box_rows * vs.row_bytes, &maps.codes[1], 0, row, pg, full);
+                        tc::tma_load_2d(at + pl.raw_s + i * pl.scale_step[0], &maps.scales[0], row * ks.ng, pg, full);
+                        tc::tma_load_2d(at + pl.raw_s + kTok / pl.box_rows * pl.scale_step[0] + i * pl.scale_step[1],
+                                        &maps.scales[1], row * vs.ng, pg, full);
+                    }
+                }
+            }
+        } else if (ROLE == 2 && warp == 12) {
+            // ---- MMAs ----
+            constexpr uint32_t fmt = (1u << 4) | ((128u >> 4) << 24);
+            const uint32_t id_s = fmt | ((kTok >> 3) << 17);
+            const uint32_t id_o0 = fmt | (1u << 16) | ((uint32_t)(va0 >> 3) << 17), id_o1 = fmt | (1u << 16) | ((uint32_t)(va1 >> 3) << 17);
+            auto scores = [&](int s, uint32_t n) {
+                const uint32_t st = ring + (n % pl.stages) * pl.stage_bytes, q = smem0 + (streams ? 0 : s * pl.k_atoms * kQAtom);
+                const uint32_t d = tmem + s * kSlotCols;
+                if (tc::elect_one()) {
+                    for (int k = 0; k < (pa0 + pa1) / 16; ++k) {
+                        const bool second = k >= pa0 / 16;
+                        const uint32_t off = (k & 3) * 32;
+                        mma_ss(d + (second ? kTok : 0), tc::sw128_desc(q + (k >> 2) * kQAtom + off),
+                               tc::sw128_desc(st + (k >> 2) * kAtom + off), id_s, k != 0 && k != pa0 / 16);
+                    }
+                    tc::mma_commit(bar(Bars::s_full + s));
+                }
+                __syncwarp();
+            };
+            auto outputs = [&](int s, uint32_t n, bool first, bool frees) {
+                const uint32_t v = ring + (n % pl.stages) * pl.stage_bytes + pl.k_atoms * kAtom;
+                const uint32_t p = tmem + s * kSlotCols, d = p + o_off;
+                if (tc::elect_one()) {
+                    for (int k = 0; k < kTok / 16; ++k) mma_ts(d, p + 8 * k, value_desc(v + k * 2048), id_o0, !(first && k == 0));
+                    if (vs.ng == 2) {
+                        for (int k = 0; k < kTok / 16; ++k)
+                            mma_ts(d + va0, p + 32 + 8 * k, value_desc(v + pl.v_atom1 * kAtom + k * 2048), id_o1, !(first && k == 0));
+                    }
+                    if (frees) tc::mma_commit(bar(Bars::kv_free + n % pl.stages));
+                }
+                __syncwarp();
+            };
+            auto ready = [&](int which, uint32_t n) {
+                ok = ok && wait(which + n % pl.stages, n / pl.stages);
+                tc::tc_fence_after();
+            };
+            ok = wait(Bars::q_full, n_seg);
+            tc::tc_fence_after();
+            for (int s = 0; ok && s < groups; ++s) {
+                const uint32_t n = n_block + (streams ? s : 0);
+                ready(Bars::k_ready, n);
+                if (ok) scores(s, n);
+            }
+            uint32_t done[2] = {0, 0};
+            for (int j = 0; ok && j < nblk; ++j) {
+                const uint32_t n = n_block + j;
+                for (int s = streams ? (j & 1) : 0; ok && s < (streams ? (j & 1) + 1 : groups); ++s) {
+                    ok = wait(Bars::p_full + s, n_s[s] + done[s]);
+                    tc::tc_fence_after();
+                    ready(Bars::v_ready, n);
+                    if (!ok) break;
+                    outputs(s, n, done[s] == 0, streams || s == groups - 1);
+                    ++done[s];
+                    const int next = j + (streams ? 2 : 1);
+                    if (next < nblk) {
+                        ready(Bars::k_ready, n_block + next);
+                        if (ok) scores(s, n_block + next);
+                    } else if (tc::elect_one()) {
+                        tc::mma_commit(bar(Bars::o_full + s));
+                    }
+                    __syncwarp();
+                }
+            }
+        } else if constexpr (ROLE == 1) {
+            // ---- packed rows -> operand tiles ----
+            const int dw = warp - 8;
+            const Offsets f;
+            for (int j = 0; ok && j < nblk; ++j) {
+                const uint32_t n = n_block + j, st = n % pl.stages, r = n % pl.raw_stages;
+                const int p0 = (seg.c_first + j) * kTok;
+                const uint32_t at = ring + st * pl.stage_bytes, src = raw + r * pl.raw_bytes;
+                ok = wait(Bars::kv_free + st, (n / pl.stages) + 1) && wait(Bars::raw_full + r, n / pl.raw_stages);
+                if (!ok) break;
+                // scales as fp32: keys' by warps 0 and 1 (with 2^-(n-1)), values' by 2 and 3, relative to a power of two
+                {
+                    const int side = dw >> 1;
+                    const KvSide& sd = side ? vs : ks;
+                    const uint32_t sc = src + pl.raw_s + (side ? kTok / pl.box_rows * pl.scale_step[0] : 0);
+                    const uint32_t to = at + (pl.k_atoms + pl.v_atoms) * kAtom + side * 512;
+                    const int mine = lane + 32 * (dw & 1);
+                    float x[2][2];        // [this token, the other half's][group]
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int tok = h ? mine ^ 32 : mine;
+                        const uint32_t e = sc + (tok / pl.box_rows) * pl.scale_step[side] + 2 * sd.ng * (tok % pl.box_rows);
+                        const bool in = p0 + tok < end;
+                        x[h][0] = in ? scale_of(lds16(e), bf16) : 0.0f;
+                        x[h][1] = in && sd.ng == 2 ? scale_of(lds16(e + 2), bf16) : 0.0f;
+                    }
+                    float f0 = pow2(1 - sd.bits[0]), f1 = pow2(1 - sd.bits[1]);
+                    if (side) {
+                        const uint32_t big0 = __reduce_max_sync(0xffffffffu, max(__float_as_uint(x[0][0]), __float_as_uint(x[1][0])));
+                        const uint32_t big1 = __reduce_max_sync(0xffffffffu, max(__float_as_uint(x[0][1]), __float_as_uint(x[1][1])));
+                        const int e0 = min(max((int)(big0 >> 23) - 126, -100), 126), e1 = min(max((int)(big1 >> 23) - 126, -100), 126);
+                        f0 = pow2(-e0);
+                        f1 = pow2(-e1);
+                        if (dw == 2 && lane == 0) {
+                            sm_e[2 * st] = e0;
+                            sm_e[2 * st + 1] = e1;
+                        }
+                    }
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 4 * mine), "f"(x[0][0] * f0) : "memory");
+                    if (sd.ng == 2) asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 256 + 4 * mine), "f"(x[0][1] * f1) : "memory");
+                }
+#pragma unroll
+                for (int side = 0; side < 2; ++side) {
+                    const KvSide& sd = side ? vs : ks;
+                    const int c0 = 32 * sd.nb[0], c1 = 32 * sd.nb[1];
+                    const int atom1 = side ? pl.v_atom1 : 0;           // keys: the groups follow each other
+                    const int atoms = side ? pl.v_atoms : pl.k_atoms;
+                    const uint32_t base = src + (side ? pl.raw_v : 0), to = at + (side ? pl.k_atoms * kAtom : 0);
+                    const int piece = lane & 7;
+                    for (int atom = 0; atom < atoms; ++atom) {
+                        int col = 64 * atom + 8 * piece, grp = 0;      // this lane's eight codes of the atom
+                        if (side ? (atom >= atom1 && vs.ng == 2) : col >= c0) {
+                            grp = 1;
+                            col -= side ? 64 * atom1 : c0;
+                        }
+                        if (col >= (grp ? c1 : c0)) continue;
+                        const int bits = sd.bits[grp];
+                        const uint32_t from = base + sd.off[grp] + bits * (col >> 3);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int tok = dw * 16 + 4 * i + (lane >> 3);
+                            const uint4 x = unpack8(from + tok * sd.row_bytes, bits, f);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + atom * kAtom + tok * 128 + ((piece ^ (tok & 7)) << 4)),
+                                         "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w)
+                                         : "memory");
+                        }
+                    }
+                    tc::fence_proxy_async_shared();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tc::mbar_arrive(bar((side ? Bars::v_ready : Bars::k_ready) + st));
+                        if (side) tc::mbar_arrive(bar(Bars::raw_free + r));
+                    }
+                }
+            }
+        } else if constexpr (ROLE == 0) {
+            // ---- softmax ----
+            const int s = warp >> 2, quad = warp & 3;
+            // queries: a warp per row, fp16, scaled to 2^13
+            {
+                const int total = groups == 2 && !streams ? 256 : 128;
+                int ch[8];
+                float down[8];
+                const int cols = pa0 + pa1;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int col = 32 * k + lane, grp = col < pa0 ? 0 : 1, c = grp ? col - pa0 : col;
+                    const int code = column_code(ks.bits[grp], c);
+                    ch[k] = col < cols && code < ks.count[grp] ? __ldg(ks.perm + head * ks.D + (grp ? ks.count[0] : 0) + code) : -1;
+                    down[k] = pow2(-place_log2(ks.bits[grp], (c & 7) >> 1));
+                }
+                for (int c = tid; c < pl.o_cols; c += 256) {
+                    const int grp = c < va0 ? 0 : 1, code = column_code(vs.bits[grp], grp ? c - va0 : c);
+                    sm_chan[c] = code < vs.count[grp] ? (int16_t)__ldg(vs.perm + head * vs.D + (grp ? vs.count[0] : 0) + code) : (int16_t)-1;
+                    sm_back[c] = pow2(1 - vs.bits[grp] - place_log2(vs.bits[grp], (c & 7) >> 1));
+                }
+                for (int r0 = warp * (total / 8); r0 < (warp + 1) * (total / 8); r0 += 4) {
+                    float x[4][8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int row = row0 + r0 + i;
+                        const uint16_t* q = a.Q + b * a.q_seq_stride + (row / a.group) * a.q_token_stride + (head * a.group + row % a.group) * a.q_head_stride;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) x[i][k] = row < pl.rows && ch[k] >= 0 ? scale_of(q[ch[k]], bf16) : 0.0f;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = r0 + i;
+                        uint32_t top = 0;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(x[i][k]) & 0x7FFFFFFFu);
+                        top = __reduce_max_sync(0xffffffffu, top);
+                        const int e = top == 0 ? 0 : min(13 - ((int)(top >> 23) - 127), 120);
+                        const float up = a.scale < 0.0f ? -pow2(e) : pow2(e);
+                        if (lane == 0) sm_fac[r] = fmaxf(ldexpf(fabsf(a.scale) * kLog2e, -e), 0x1p-126f);
+                        uint8_t* q = smem + (r >> 7) * pl.k_atoms * kQAtom + (r & 127) * 128;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const int col = 32 * k + lane;
+                            if (32 * k < cols)
+                                *reinterpret_cast<__half*>(q + (col >> 6) * kQAtom + ((((col & 63) >> 3) ^ (r & 7)) << 4) + 2 * (col & 7)) =
+                                    __float2half_rn(x[i][k] * up * down[k]);
+                        }
+                    }
+                }
+                tc::fence_proxy_async_shared();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(bar(Bars::q_full));
+            }
+            bar_group(1, 256);      // the rows' factors
+            const int r_tile = quad * 32 + lane;                               // row of the tile
+            const int row = row0 + (streams ? 0 : 128 * s) + r_tile;
+            const int t_row = row < pl.rows ? row / a.group : a.T - 1;
+            const float fac = sm_fac[(streams ? 0 : 128 * s) + r_tile];
+            const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+            const uint32_t t_s = tmem + s * kSlotCols + lanes;
+            float m = -INFINITY, l = 0.0f;
+            int e0 = 0, e1 = 0;
+            const int mine = s < groups ? (streams ? (nblk - s + 1) / 2 : nblk) : 0;
+            const int sure = min(len, end);
+            for (int i = 0; ok && i < mine; ++i) {
+                const int j = streams ? 2 * i + s : i;
+                const uint32_t n = n_block + j, st = n % pl.stages;
+                const int p0 = (seg.c_first + j) * kTok;
+                const uint32_t sc = ring + st * pl.stage_bytes + (pl.k_atoms + pl.v_atoms) * kAtom;
+                ok = wait(Bars::k_ready + st, n / pl.stages) && wait(Bars::s_full + s, n_s[s] + i);
+                if (!ok) break;
+                tc::tc_fence_after();
+                float2 x[kTok / 2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t v[32];
+                    tmem_ld32(t_s + 32 * h, v);
+#pragma unroll
+                    for (int k = 0; k < 16; k += 2) {
+                        const float4 kk = lds128f(sc + 128 * h + 8 * k);
+                        x[16 * h + k] = mul2(make_float2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), make_float2(kk.x, kk.y));
+                        x[16 * h + k + 1] = mul2(make_float2(__uint_as_float(v[2 * k + 2]), __uint_as_float(v[2 * k + 3])), make_float2(kk.z, kk.w));
+                    }
+                    if (ks.ng == 2) {
+                        tmem_ld32(t_s + kTok + 32 * h, v);
+#pragma unroll
+                        for (int k = 0; k < 16; k += 2) {
+                            const float4 kk = lds128f(sc + 256 + 128 * h + 8 * k);
+                            x[16 * h + k] = fma2(make_float2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), make_float2(kk.x, kk.y), x[16 * h + k]);
+                            x[16 * h + k + 1] = fma2(make_float2(__uint_as_float(v[2 * k + 2]), __uint_as_float(v[2 * k + 3])), make_float2(kk.z, kk.w), x[16 * h + k + 1]);
+                        }
+                    }
+                }
+                if (p0 + kTok > sure) {
+                    const uint8_t* mask = a.mask ? a.mask + b * a.mask_stride + (int64_t)t_row * a.T : nullptr;
+#pragma unroll
+                    for (int k = 0; k < kTok; ++k) {
+                        const int p = p0 + k, d = p - len;
+                        bool see = p < end;
+                        if (see && d >= 0) see = mask ? mask[d] != 0 : d <= t_row;
+                        if (!see) (k & 1 ? x[k >> 1].y : x[k >> 1].x) = -INFINITY;
+                    }
+                }
+                float top = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < kTok / 2; ++k) top = fmaxf(fmaxf(top, x[k].x), x[k].y);
+                // raise the maximum, and the powers of two of the value scales, where they are left behind by much
+                const int b0 = sm_e[2 * st], b1 = sm_e[2 * st + 1];
+                const bool first = i == 0;
+                const bool raise = m == -INFINITY ? top != -INFINITY : (top - m) * fac > kLazy;
+                const int n0 = first || b0 > e0 + 4 ? b0 : e0, n1 = first || b1 > e1 + 4 ? b1 : e1;
+                if (first) {
+                    m = top;
+                } else if (__any_sync(0xffffffffu, raise) || n0 != e0 || n1 != e1) {
+                    float al = 1.0f;
+                    if (raise) {
+                        al = m == -INFINITY ? 0.0f : ex2((m - top) * fac);
+                        m = top;
+                        l *= al;
+                    }
+                    const float al0 = al * (n0 - e0 > 126 ? 0.0f : pow2(e0 - n0)), al1 = al * (n1 - e1 > 126 ? 0.0f : pow2(e1 - n1));
+                    // the MMAs that wrote O are complete: they came before the ones that wrote these scores
+                    for (int c = 0; c < pl.o_cols; c += 32) {
+                        uint32_t v[32];
+                        tmem_ld32(t_s + o_off + c, v);
+                        const float f = c < va0 ? al0 : al1;
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f);
+                        tmem_st32(t_s + o_off + c, v);
+                    }
+                }
+                e0 = n0;
+                e1 = n1;
+                // weights, times 2^(block's power - running power)
+                const int d0 = max(b0 - e0, -126);
+                const float shift = (m == -INFINITY ? 0.0f : -m * fac) + (float)d0;
+                float2 sum = make_float2(0.0f, 0.0f);
+                uint32_t w[32];
+#pragma unroll
+                for (int k = 0; k < kTok / 2; ++k) {
+                    const float2 y = fma2(x[k], make_float2(fac, fac), make_float2(shift, shift));
+                    x[k] = make_float2(ex2(y.x), ex2(y.y));
+                    sum = fma2(x[k], make_float2(1.0f, 1.0f), sum);
+                }
+                l += (sum.x + sum.y) * pow2(-d0);
+#pragma unroll
+                for (int k = 0; k < 32; k += 2) {
+                    const float4 vv = lds128f(sc + 512 + 8 * k);
+                    const float2 y0 = mul2(x[k], make_float2(vv.x, vv.y)), y1 = mul2(x[k + 1], make_float2(vv.z, vv.w));
+                    w[k] = pack2(y0.x, y0.y);
+                    w[k + 1] = pack2(y1.x, y1.y);
+                }
+                tmem_st32(t_s, w);
+                if (vs.ng == 2) {
+                    const int dd = b1 - e1 - d0;
+                    const float c = dd < -126 ? 0.0f : pow2(min(dd, 127));
+#pragma unroll
+                    for (int k = 0; k < 32; k += 2) {
+                        const float4 vv = lds128f(sc + 768 + 8 * k);
+                        const float2 y0 = mul2(x[k], make_float2(vv.x * c, vv.y * c)), y1 = mul2(x[k + 1], make_float2(vv.z * c, vv.w * c));
+                        w[k] = pack2(y0.x, y0.y);
+                        w[k + 1] = pack2(y1.x, y1.y);
+                    }
+                    tmem_st32(t_s + 32, w);
+                }
+                tc::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(bar(Bars::p_full + s));
+            }
+            // ---- results: both groups' MMAs are complete, so queries' and operands' memory is free ----
+            for (int g = 0; g < groups; ++g) ok = ok && wait(Bars::o_full + g, n_o[g]);
+            tc::tc_fence_after();
+            const bool works = s < (streams ? 1 : groups);          // this group has a tile's results
+            const bool whole = seg.n_part == 1;
+            float m2 = m == -INFINITY ? m : m * fac, keep = 1.0f, other = 0.0f;     // in units of the exponent
+            float* second = reinterpret_cast<float*>(smem);       // [o_cols][128]: the second stream's outputs
+            if (streams && s == 1) {
+                sm_m[r_tile] = mine > 0 ? m2 : -INFINITY;
+                sm_l[r_tile] = l;
+                for (int c = 0; ok && mine > 0 && c < pl.o_cols; c += 32) {
+                    uint32_t v[32];
+                    tmem_ld32(t_s + o_off + c, v);
+                    const int e = c < va0 ? e0 : e1;
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) second[(c + k) * 128 + r_tile] = __uint_as_float(v[k]) * (sm_back[c + k] * pow2(e));
+                }
+            }
+            bar_group(1, 256);
+            if (streams && s == 0 && groups == 2) {
+                const float m1 = sm_m[r_tile], mm = fmaxf(m2, m1);
+                keep = m2 == -INFINITY ? 0.0f : ex2(m2 - mm);
+                other = m1 == -INFINITY ? 0.0f : ex2(m1 - mm);
+                l = l * keep + sm_l[r_tile] * other;
+                m2 = mm;
+            }
+            const int unit_row = (streams ? 0 : 128 * s) + r_tile;
+            const int64_t part_floats = (int64_t)unit_rows * (pl.o_cols + 2);
+            float* parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.scratch) + SONIQ_KV_SCRATCH_ZERO);
+            uint8_t* staged = smem + (streams ? pl.o_cols * 512 : 128 * s * pl.out_stride);
+            auto stage_out = [&](int c, float v) {
+                const int ch = sm_chan[c];
+                if (ch >= 0) *reinterpret_cast<uint16_t*>(staged + r_tile * pl.out_stride + 2 * ch) = bf16 ? kv_round<true>(v) : kv_round<false>(v);
+            };
+            if (works && ok) {
+                const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);     // nothing seen: 0; NaN stays
+                for (int c = 0; c < pl.o_cols; c += 32) {
+                    uint32_t v[32];
+                    tmem_ld32(t_s + o_off + c, v);
+                    const float f = keep * pow2(c < va0 ? e0 : e1);
+                    float x[32];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        x[k] = __uint_as_float(v[k]) * (sm_back[c + k] * f);
+                        if (streams && groups == 2) x[k] = fmaf(second[(c + k) * 128 + r_tile], other, x[k]);
+                    }
+                    if (whole) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) stage_out(c + k, x[k] * inv);
+                    } else {
+                        float4* to = reinterpret_cast<float4*>(parts + seg.slot * part_floats) + (int64_t)(c / 4) * unit_rows + unit_row;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) to[(int64_t)k * unit_rows] = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+                    }
+                }
+                if (!whole) {
+                    float* st = parts + seg.slot * part_floats + (int64_t)unit_rows * pl.o_cols;
+                    st[unit_row] = m2;
+                    st[unit_rows + unit_row] = l;
+                }
+            }
+            bool write = whole;
+            if (!whole) {
+                __threadfence();
+                bar_group(1, 256);
+                if (tid == 0) {
+                    unsigned* counter = static_cast<unsigned*>(a.scratch) + seg.cta0;
+                    *sm_last = !tc::abort_raised(abort_flag) && atomicAdd(counter, 1u) == (unsigned)(seg.n_part - 1);
+                    if (*sm_last) *counter = 0;
+                }
+                bar_group(1, 256);
+                if (*sm_last && works && ok) {
+                    // all parts are there: join them in order
+                    __threadfence();
+                    write = true;
+                    auto stat = [&](int i) { return parts + part_slot(seg, i) * part_floats + (int64_t)unit_rows * pl.o_cols + unit_row; };
+                    float mm = -INFINITY, ll = 0.0f;
+                    for (int i = 0; i < seg.n_part; ++i) mm = fmaxf(mm, __ldcg(stat(i)));
+                    for (int i = 0; i < seg.n_part; ++i) {
+                        const float mi = __ldcg(stat(i));
+                        ll += __ldcg(stat(i) + unit_rows) * (mi == -INFINITY ? 0.0f : ex2(mi - mm));
+                    }
+                    const float inv = ll > 0.0f ? 1.0f / ll : (ll == 0.0f ? 0.0f : ll);
+                    for (int c = 0; c < pl.o_cols; c += 32) {
+                        float x[32] = {};
+                        for (int i = 0; i < seg.n_part; ++i) {
+                            const float mi = __ldcg(stat(i)), f = mi == -INFINITY ? 0.0f : ex2(mi - mm);
+                            const float4* from = reinterpret_cast<const float4*>(parts + part_slot(seg, i) * part_floats) + (int64_t)(c / 4) * unit_rows + unit_row;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                const float4 q = __ldcg(from + (int64_t)k * unit_rows);
+                                x[4 * k] = fmaf(f, q.x, x[4 * k]);
+                                x[4 * k + 1] = fmaf(f, q.y, x[4 * k + 1]);
+                                x[4 * k + 2] = fmaf(f, q.z, x[4 * k + 2]);
+                                x[4 * k + 3] = fmaf(f, q.w, x[4 * k + 3]);
+                            }
+                        }
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) stage_out(c + k, x[k] * inv);
+                    }
+                }
+            }
+            __syncwarp();
+            if (write && works && ok) {
+                // a warp's 32 rows, each in one run
+                const int qh = geo.heads * a.group;
+                const bool pairs = vs.D % 2 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 3u) == 0;
+                for (int i = 0; i < 32; ++i) {
+                    const int r = row0 + (streams ? 0 : 128 * s) + quad * 32 + i;
+                    if (r >= pl.rows) break;
+                    const uint8_t* from = staged + (quad * 32 + i) * pl.out_stride;
+                    uint16_t* to = a.out + (((int64_t)b * a.T + r / a.group) * qh + head * a.group + r % a.group) * vs.D;
+                    if (pairs) {
+                        for (int c = lane; c < vs.D / 2; c += 32) reinterpret_cast<uint32_t*>(to)[c] = reinterpret_cast<const uint32_t*>(from)[c];
+                    } else {
+                        for (int c = lane; c < vs.D; c += 32) to[c] = reinterpret_cast<const uint16_t*>(from)[c];
+                    }
+                }
+            }
+        }
+        n_block += nblk;
+        for (int s = 0; s < groups; ++s) {
+            n_s[s] += streams ? (nblk - s + 1) / 2 : nblk;
+            n_o[s] += 1;
+        }
+        ++n_seg;
+        tc::tc_fence_before();
+        __syncthreads();
+        tc::tc_fence_after();
+        if (tc::abort_raised(abort_flag)) {
+            // a copy did not come: let those on their way land, and the MMAs end, within the same bound
+            const long long t0 = tc::globaltimer();
+            if (warp == 13) {
+                for (uint32_t i = 0; i < (uint32_t)pl.raw_stages; ++i)
+                    while (!tc::mbar_try_wait(bar(Bars::raw_full + i), 0) && !tc::mbar_try_wait(bar(Bars::raw_full + i), 1) &&
+                           tc::globaltimer() - t0 < kWaitNs) {
+                    }
+            } else if (warp == 12) {
+                if (tc::elect_one()) tc::mma_commit(bar(Bars::drain));
+                while (!tc::mbar_try_wait(bar(Bars::drain), 0) && tc::globaltimer() - t0 < kWaitNs) {
+                }
+            }
+            break;
+        }
+        if (!split.next(seg)) break;
+    }
+    };
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        work(std::integral_constant<int, 0>{});
+    } else if (warp < 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        work(std::integral_constant<int, 1>{});
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        work(std::integral_constant<int, 2>{});
+    }
+    __syncthreads();
+    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+struct TileLaunch {
+    bool fits;
+    TilePlan pl;
+};
+
+TileLaunch plan_tile(const KvGeom& geo, int64_t T, int64_t group) {
+    TileLaunch t{};
+    TilePlan& p = t.pl;
+    const KvSide &ks = geo.s[0], &vs = geo.s[1];
+    const int64_t rows = T * group;
+    p.rows = (int)rows;
+    p.tiles = rows > 128 ? 2 : 1;
+    p.row_units = (int)((rows + 128 * p.tiles - 1) / (128 * p.tiles));
+    p.k_atoms = (ks.nb[0] + ks.nb[1] + 1) / 2;
+    p.v_atom1 = (vs.nb[0] + 1) / 2;
+    p.v_atoms = p.v_atom1 + (vs.nb[1] + 1) / 2;
+    p.o_cols = 32 * (vs.nb[0] + vs.nb[1]);
+    if (kTok * ks.ng + p.o_cols > kSlotCols) return t;
+    p.box_rows = geo.page < kTok ? geo.page : kTok;
+    const int copies = kTok / p.box_rows;
+    for (int i = 0; i < 2; ++i) p.scale_step[i] = (p.box_rows * geo.s[i].ng * 2 + 127) / 128 * 128;
+    p.raw_v = kTok * ks.row_bytes;
+    p.raw_s = p.raw_v + kTok * vs.row_bytes;
+    p.raw_bytes = (p.raw_s + copies * (p.scale_step[0] + p.scale_step[1]) + 127) / 128 * 128;
+    p.stage_bytes = (p.k_atoms + p.v_atoms) * kAtom + 1024;
+    p.ring_off = p.tiles * p.k_atoms * kQAtom;
+    p.out_stride = (vs.D + 1) / 2 * 4 + 4;
+    if (p.out_stride / 4 % 2 == 0) p.out_stride += 4;
+    constexpr int misc = 4096, most = 227 * 1024;
+    // two tiles share a block and look one ahead, two streams two
+    static const int choices[][2] = {{4, 4}, {4, 3}, {4, 2}, {3, 4}, {3, 3}, {3, 2}, {2, 3}, {2, 2}};
+    for (const auto& c : choices) {
+        if (p.tiles == 2 && c[0] > 3) continue;
+        p.stages = c[0];
+        p.raw_stages = c[1];
+        p.raw_off = p.ring_off + p.stages * p.stage_bytes;
+        p.misc_off = p.raw_off + (p.raw_stages * p.raw_bytes + 1023) / 1024 * 1024;
+        p.smem = p.misc_off + misc;
+        const int results = p.tiles == 2 ? 256 * p.out_stride : p.o_cols * 512 + 128 * p.out_stride;
+        if (p.smem <= most && results <= p.raw_off) {
+            t.fits = true;
+            break;
+        }
+    }
+    p.min_chunks = 4;
+    return t;
+}
+
+}  // namespace
+
+bool kv_tile_supported(const KvGeom& geo, int64_t T, int64_t group) { return plan_tile(geo, T, group).fits; }
+
+int64_t kv_tile_scratch(const KvGeom& geo, int64_t T, int64_t group) {
+    const TilePlan p = plan_tile(geo, T, group).pl;
+    return SONIQ_KV_SCRATCH_ZERO + (int64_t)2 * num_sms() * 128 * p.tiles * (p.o_cols + 2) * 4;
+}
+
+cudaError_t launch_kv_tile(const KvGeom& geo, const KvAttendArgs& a, cudaStream_t st) {
+    const TileLaunch t = plan_tile(geo, a.T, a.group);
+    if (!t.fits) return cudaErrorNotSupported;
+    const TilePlan& p = t.pl;
+    const int64_t cap = (int64_t)a.max_pages << geo.page_shift;
+    const int64_t items = (int64_t)a.B * geo.heads * p.row_units, most = items * (cap / kTok + 1);
+    if (most >= 2147483648ll) return cudaErrorNotSupported;      // chunks are numbered in 32 bits
+    const int64_t by_size = (most + p.min_chunks - 1) / p.min_chunks, want = by_size > items ? by_size : items;
+    const int grid = (int)(want < num_sms() ? want : num_sms());
+    KvMaps maps;
+    for (int side = 0; side < 2; ++side) {
+        if (!encode_side(geo, geo.s[side], geo.s[side].row_bytes, p.box_rows, CU_TENSOR_MAP_SWIZZLE_NONE, &maps.codes[side],
+                         &maps.scales[side]))
+            return cudaErrorUnknown;
+    }
+    cudaError_t e = cudaFuncSetAttribute(kv_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
+    if (e == cudaSuccess) e = prefer_max_shared(reinterpret_cast<const void*>(kv_tile_kernel));
+    if (e != cudaSuccess) return e;
+    kv_tile_kernel<<<grid, kThreads, p.smem, st>>>(geo, a, p, maps);
+    note_launch();
+    return cudaGetLastError();
+}
+
+}  // namespace soniq
