@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
     if (tid == 0) sm_abort = 0;
 
     // ---- this CTA's range of chunks --------------------------------------
-    check_lengths(geo, a);
+    check_lengths(geo, a, tid, blockDim.x);
     auto chunks = [&](int b) { return (uint32_t)chunks_of(geo, a, b); };
     Split split;
     if (!split.begin(chunks, a.B, geo.heads * pl.row_tiles, pl.min_chunks, 2 * n_warps, sm_scan)) return;

@@ -175,17 +175,18 @@ __device__ __forceinline__ int64_t seen_end(const KvGeom& geo, const KvAttendArg
     return end < cap ? end : cap;
 }
 
-// Reports lengths beyond the page table and writes the outputs of absent sequences.
-__device__ __forceinline__ void check_lengths(const KvGeom& geo, const KvAttendArgs& a) {
+// Reports lengths beyond the page table and writes the outputs of absent
+// sequences; called by `count` threads of each CTA, `rank` among them.
+__device__ __forceinline__ void check_lengths(const KvGeom& geo, const KvAttendArgs& a, int rank, int count) {
     if (blockIdx.x == 0) {
-        for (int b = threadIdx.x; b < a.B; b += blockDim.x)
+        for (int b = rank; b < a.B; b += count)
             if (a.lengths[b] >= 0 && (int64_t)a.lengths[b] + a.T > ((int64_t)a.max_pages << geo.page_shift))
                 atomicOr(a.err, kErrKvIndex);
     }
     for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
         if (a.lengths[b] >= 0) continue;
         const int64_t size = (int64_t)a.T * a.group * geo.heads * geo.s[1].D;
-        for (int64_t i = threadIdx.x; i < size; i += blockDim.x) a.out[b * size + i] = 0;
+        for (int64_t i = rank; i < size; i += count) a.out[b * size + i] = 0;
     }
 }
 

@@ -103,25 +103,58 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
         "r"(a), "l"(b), "r"(idesc), "r"(acc));
 }
 
-// Eight codes at `src` (4, 8 or 2 bytes) as signed halves times their places' powers.
-__device__ __forceinline__ uint4 unpack8(uint32_t src, int bits, const Offsets& f) {
-    uint32_t x[4];
-    if (bits == 4) {
-        nibble_pairs(lds32(src), f, x);
-    } else if (bits == 8) {
-        const uint2 w = lds64(src);
-        x[0] = sub2(mask_flip(w.x, 0x00FF00FFu, f.c128), f.c128);
-        x[1] = sub2(mask_flip(w.x >> 8, 0x00FF00FFu, f.c128), f.c128);
-        x[2] = sub2(mask_flip(w.y, 0x00FF00FFu, f.c128), f.c128);
-        x[3] = sub2(mask_flip(w.y >> 8, 0x00FF00FFu, f.c128), f.c128);
+// Eight codes as signed halves times their places' powers: of 8 bits ...
+__device__ __forceinline__ void bytes8(uint32_t w0, uint32_t w1, const Offsets& f, uint32_t (&x)[4]) {
+    x[0] = sub2(mask_flip(w0, 0x00FF00FFu, f.c128), f.c128);
+    x[1] = sub2(mask_flip(w0 >> 8, 0x00FF00FFu, f.c128), f.c128);
+    x[2] = sub2(mask_flip(w1, 0x00FF00FFu, f.c128), f.c128);
+    x[3] = sub2(mask_flip(w1 >> 8, 0x00FF00FFu, f.c128), f.c128);
+}
+// ... and of 2 bits, from a half word.
+__device__ __forceinline__ void crumbs8(uint32_t h, const Offsets& f, uint32_t (&x)[4]) {
+    const uint32_t w = __byte_perm(h, 0, 0x4140);
+    x[0] = sub2(mask_flip(w, 0x00030003u, 0x64026402u), 0x64026402u);
+    x[1] = sub2(mask_flip(w, 0x000C000Cu, f.c8), f.c8);
+    x[2] = sub2(mask_flip(w, 0x00300030u, 0x64206420u), 0x64206420u);
+    x[3] = sub2(mask_flip(w, 0x00C000C0u, f.c128), f.c128);
+}
+__device__ __forceinline__ void sts128(uint32_t at, const uint32_t (&x)[4]) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+}
+// 16 packed bytes from byte `at` (a multiple of 8) of the row at `row`, whose
+// 16-byte pieces are swizzled by sw.
+__device__ __forceinline__ uint4 packed16(uint32_t row, uint32_t at, uint32_t sw) {
+    if ((at & 8u) == 0) return lds128(row + (at ^ sw));
+    const uint2 a = lds64(row + (at ^ sw)), b = lds64(row + ((at + 8) ^ sw));
+    return make_uint4(a.x, a.y, b.x, b.y);
+}
+// The 32-code block at byte `at` of a packed row -> 16-byte pieces p0 .. p0 + 3 of
+// the operand row at `to`, swizzled by t8 = token % 8.
+template <int BITS>
+__device__ __forceinline__ void unpack_block(uint32_t row, uint32_t at, uint32_t sw, uint32_t to, uint32_t p0, uint32_t t8,
+                                             const Offsets& f) {
+    uint32_t x[4][4];
+    if constexpr (BITS == 4) {
+        const uint4 w = packed16(row, at, sw);
+        nibble_pairs(w.x, f, x[0]);
+        nibble_pairs(w.y, f, x[1]);
+        nibble_pairs(w.z, f, x[2]);
+        nibble_pairs(w.w, f, x[3]);
+    } else if constexpr (BITS == 8) {
+        const uint4 w = packed16(row, at, sw), v = packed16(row, at + 16, sw);
+        bytes8(w.x, w.y, f, x[0]);
+        bytes8(w.z, w.w, f, x[1]);
+        bytes8(v.x, v.y, f, x[2]);
+        bytes8(v.z, v.w, f, x[3]);
     } else {
-        const uint32_t w = __byte_perm(lds16(src), 0, 0x4140);
-        x[0] = sub2(mask_flip(w, 0x00030003u, 0x64026402u), 0x64026402u);
-        x[1] = sub2(mask_flip(w, 0x000C000Cu, f.c8), f.c8);
-        x[2] = sub2(mask_flip(w, 0x00300030u, 0x64206420u), 0x64206420u);
-        x[3] = sub2(mask_flip(w, 0x00C000C0u, f.c128), f.c128);
+        const uint2 w = lds64(row + (at ^ sw));
+        crumbs8(w.x & 0xFFFFu, f, x[0]);
+        crumbs8(w.x >> 16, f, x[1]);
+        crumbs8(w.y & 0xFFFFu, f, x[2]);
+        crumbs8(w.y >> 16, f, x[3]);
     }
-    return make_uint4(x[0], x[1], x[2], x[3]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sts128(to + (((p0 + i) ^ t8) << 4), x[i]);
 }
 
 __device__ __forceinline__ void bar_group(int id, int threads) {
@@ -153,6 +186,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     float* sm_l = sm_m + 128;
     int16_t* sm_chan = reinterpret_cast<int16_t*>(sm_l + 128);       // [192] channel of an output column
     float* sm_back = reinterpret_cast<float*>(sm_chan + 192);        // [192] its power of two
+    int16_t* sm_col = reinterpret_cast<int16_t*>(sm_back + 192);     // [256] column of a key channel
+    Segment* sm_seg = reinterpret_cast<Segment*>(sm_col + 256);      // the next segment, behind a flag that there is one
+    int* sm_more = reinterpret_cast<int*>(sm_seg + 1);
     auto bar = [&](int i) { return bars + 8u * i; };
 
     if (tid == 0) {
@@ -175,7 +211,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 
     // ---- this CTA's share: entries are (sequence, unit of row tiles) ----
-    check_lengths(geo, a);
     const int unit_rows = 128 * pl.tiles;
     auto last_token = [&](int u) { return (min((u + 1) * unit_rows, pl.rows) - 1) / a.group; };
     auto end_of = [&](int b, int u) {      // tokens that any row of the unit may see
@@ -211,10 +246,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t n_o[2] = {0, 0}, n_seg = 0;      // segments that a softmax group took part in; all
     bool ok = true;
 
+    const Segment first = split.segment(chunks);
     auto work = [&](auto role) {
     constexpr int ROLE = decltype(role)::value;      // 0 softmax, 1 unpacking, 2 MMAs and copies
+    Segment seg = first;
     while (true) {
-        const Segment seg = split.segment(chunks);
         const int b = seg.entry / pl.row_units, unit = seg.entry % pl.row_units, head = seg.item;
         const int row0 = unit * unit_rows;
         const int len = a.lengths[b], end = end_of(b, unit);
@@ -257,30 +293,42 @@ __global__ void __launch_bounds__(kThreads, 1)
             constexpr uint32_t fmt = (1u << 4) | ((128u >> 4) << 24);
             const uint32_t id_s = fmt | ((kTok >> 3) << 17);
             const uint32_t id_o0 = fmt | (1u << 16) | ((uint32_t)(va0 >> 3) << 17), id_o1 = fmt | (1u << 16) | ((uint32_t)(va1 >> 3) << 17);
+            // Every lane runs the loops, the elected one issues: descriptors stay in uniform registers.
+            const bool leader = tc::elect_one();
             auto scores = [&](int s, uint32_t n) {
-                const uint32_t st = ring + (n % pl.stages) * pl.stage_bytes, q = smem0 + (streams ? 0 : s * pl.k_atoms * kQAtom);
+                uint64_t q = tc::sw128_desc(smem0 + (streams ? 0 : s * pl.k_atoms * kQAtom));
+                uint64_t k = tc::sw128_desc(ring + (n % pl.stages) * pl.stage_bytes);
                 const uint32_t d = tmem + s * kSlotCols;
-                if (tc::elect_one()) {
-                    for (int k = 0; k < (pa0 + pa1) / 16; ++k) {
-                        const bool second = k >= pa0 / 16;
-                        const uint32_t off = (k & 3) * 32;
-                        mma_ss(d + (second ? kTok : 0), tc::sw128_desc(q + (k >> 2) * kQAtom + off),
-                               tc::sw128_desc(st + (k >> 2) * kAtom + off), id_s, k != 0 && k != pa0 / 16);
+                const int steps0 = pa0 / 32, steps = (pa0 + pa1) / 32;      // of 32 codes: two MMAs
+#pragma unroll 4
+                for (int i = 0; i < steps; ++i) {
+                    const uint32_t to = d + (i >= steps0 ? kTok : 0);
+                    if (leader) {
+                        mma_ss(to, q, k, id_s, i != 0 && i != steps0);
+                        mma_ss(to, q + 2, k + 2, id_s, 1);
                     }
-                    tc::mma_commit(bar(Bars::s_full + s));
+                    // half a column group on, or the next column group
+                    q += i & 1 ? (kQAtom - 64) >> 4 : 4;
+                    k += i & 1 ? (kAtom - 64) >> 4 : 4;
                 }
+                if (leader) tc::mma_commit(bar(Bars::s_full + s));
                 __syncwarp();
             };
-            auto outputs = [&](int s, uint32_t n, bool first, bool frees) {
-                const uint32_t v = ring + (n % pl.stages) * pl.stage_bytes + pl.k_atoms * kAtom;
+            auto outputs = [&](int s, uint32_t n, bool first, bool frees, bool last) {
+                const uint64_t v = value_desc(ring + (n % pl.stages) * pl.stage_bytes + pl.k_atoms * kAtom);
                 const uint32_t p = tmem + s * kSlotCols, d = p + o_off;
-                if (tc::elect_one()) {
-                    for (int k = 0; k < kTok / 16; ++k) mma_ts(d, p + 8 * k, value_desc(v + k * 2048), id_o0, !(first && k == 0));
-                    if (vs.ng == 2) {
-                        for (int k = 0; k < kTok / 16; ++k)
-                            mma_ts(d + va0, p + 32 + 8 * k, value_desc(v + pl.v_atom1 * kAtom + k * 2048), id_o1, !(first && k == 0));
-                    }
+#pragma unroll
+                for (int k = 0; k < kTok / 16; ++k)
+                    if (leader) mma_ts(d, p + 8 * k, v + k * (2048 >> 4), id_o0, !(first && k == 0));
+                if (vs.ng == 2) {
+                    const uint64_t v1 = v + pl.v_atom1 * (kAtom >> 4);
+#pragma unroll
+                    for (int k = 0; k < kTok / 16; ++k)
+                        if (leader) mma_ts(d + va0, p + 32 + 8 * k, v1 + k * (2048 >> 4), id_o1, !(first && k == 0));
+                }
+                if (leader) {
                     if (frees) tc::mma_commit(bar(Bars::kv_free + n % pl.stages));
+                    if (last) tc::mma_commit(bar(Bars::o_full + s));
                 }
                 __syncwarp();
             };
@@ -303,21 +351,25 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tc::tc_fence_after();
                     ready(Bars::v_ready, n);
                     if (!ok) break;
-                    outputs(s, n, done[s] == 0, streams || s == groups - 1);
-                    ++done[s];
                     const int next = j + (streams ? 2 : 1);
+                    outputs(s, n, done[s] == 0, streams || s == groups - 1, next >= nblk);
+                    ++done[s];
                     if (next < nblk) {
                         ready(Bars::k_ready, n_block + next);
                         if (ok) scores(s, n_block + next);
-                    } else if (tc::elect_one()) {
-                        tc::mma_commit(bar(Bars::o_full + s));
                     }
-                    __syncwarp();
                 }
             }
+        } else if (ROLE == 2 && warp == 14) {
+            // ---- the segment after this one ----
+            const bool more = split.next(seg);
+            if (more) *sm_seg = split.segment(chunks);
+            *sm_more = more;
+        } else if (ROLE == 2 && warp == 15) {
+            if (n_seg == 0) check_lengths(geo, a, lane, 32);
         } else if constexpr (ROLE == 1) {
             // ---- packed rows -> operand tiles ----
-            const int dw = warp - 8;
+            const int dw = warp - 8, tok = (dw & 1) * 32 + lane;
             const Offsets f;
             for (int j = 0; ok && j < nblk; ++j) {
                 const uint32_t n = n_block + j, st = n % pl.stages, r = n % pl.raw_stages;
@@ -331,13 +383,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const KvSide& sd = side ? vs : ks;
                     const uint32_t sc = src + pl.raw_s + (side ? kTok / pl.box_rows * pl.scale_step[0] : 0);
                     const uint32_t to = at + (pl.k_atoms + pl.v_atoms) * kAtom + side * 512;
-                    const int mine = lane + 32 * (dw & 1);
                     float x[2][2];        // [this token, the other half's][group]
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const int tok = h ? mine ^ 32 : mine;
-                        const uint32_t e = sc + (tok / pl.box_rows) * pl.scale_step[side] + 2 * sd.ng * (tok % pl.box_rows);
-                        const bool in = p0 + tok < end;
+                        const int t = h ? tok ^ 32 : tok;
+                        const uint32_t e = sc + (t / pl.box_rows) * pl.scale_step[side] + 2 * sd.ng * (t % pl.box_rows);
+                        const bool in = p0 + t < end;
                         x[h][0] = in ? scale_of(lds16(e), bf16) : 0.0f;
                         x[h][1] = in && sd.ng == 2 ? scale_of(lds16(e + 2), bf16) : 0.0f;
                     }
@@ -353,34 +404,25 @@ __global__ void __launch_bounds__(kThreads, 1)
                             sm_e[2 * st + 1] = e1;
                         }
                     }
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 4 * mine), "f"(x[0][0] * f0) : "memory");
-                    if (sd.ng == 2) asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 256 + 4 * mine), "f"(x[0][1] * f1) : "memory");
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 4 * tok), "f"(x[0][0] * f0) : "memory");
+                    if (sd.ng == 2) asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 256 + 4 * tok), "f"(x[0][1] * f1) : "memory");
                 }
 #pragma unroll
                 for (int side = 0; side < 2; ++side) {
                     const KvSide& sd = side ? vs : ks;
-                    const int c0 = 32 * sd.nb[0], c1 = 32 * sd.nb[1];
-                    const int atom1 = side ? pl.v_atom1 : 0;           // keys: the groups follow each other
-                    const int atoms = side ? pl.v_atoms : pl.k_atoms;
-                    const uint32_t base = src + (side ? pl.raw_v : 0), to = at + (side ? pl.k_atoms * kAtom : 0);
-                    const int piece = lane & 7;
-                    for (int atom = 0; atom < atoms; ++atom) {
-                        int col = 64 * atom + 8 * piece, grp = 0;      // this lane's eight codes of the atom
-                        if (side ? (atom >= atom1 && vs.ng == 2) : col >= c0) {
-                            grp = 1;
-                            col -= side ? 64 * atom1 : c0;
-                        }
-                        if (col >= (grp ? c1 : c0)) continue;
-                        const int bits = sd.bits[grp];
-                        const uint32_t from = base + sd.off[grp] + bits * (col >> 3);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int tok = dw * 16 + 4 * i + (lane >> 3);
-                            const uint4 x = unpack8(from + tok * sd.row_bytes, bits, f);
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + atom * kAtom + tok * 128 + ((piece ^ (tok & 7)) << 4)),
-                                         "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w)
-                                         : "memory");
-                        }
+                    const uint32_t base = src + (side ? pl.raw_v : 0) + tok * sd.row_bytes;
+                    const uint32_t to = at + (side ? pl.k_atoms * kAtom : 0) + tok * 128;
+                    const uint32_t raw_sw = sd.row_bytes == 64 ? ((tok >> 1) & 3) << 4 : (sd.row_bytes == 128 ? (tok & 7) << 4 : 0);
+                    // a lane takes a token, two warps every second block
+                    for (int blk = dw >> 1; blk < sd.nb[0] + sd.nb[1]; blk += 2) {
+                        const int grp = blk < sd.nb[0] ? 0 : 1, bb = grp ? blk - sd.nb[0] : blk, bits = sd.bits[grp];
+                        const uint32_t byte = sd.off[grp] + 4 * bits * bb;
+                        // keys' groups follow each other, values' start a column group each
+                        const int col = side && grp ? 64 * pl.v_atom1 + 32 * bb : 32 * blk;
+                        const uint32_t row = to + (col >> 6) * kAtom, p0 = (col >> 3) & 7;
+                        if (bits == 4) unpack_block<4>(base, byte, raw_sw, row, p0, tok & 7, f);
+                        else if (bits == 8) unpack_block<8>(base, byte, raw_sw, row, p0, tok & 7, f);
+                        else unpack_block<2>(base, byte, raw_sw, row, p0, tok & 7, f);
                     }
                     tc::fence_proxy_async_shared();
                     __syncwarp();
@@ -393,53 +435,101 @@ __global__ void __launch_bounds__(kThreads, 1)
         } else if constexpr (ROLE == 0) {
             // ---- softmax ----
             const int s = warp >> 2, quad = warp & 3;
-            // queries: a warp per row, fp16, scaled to 2^13
+            // queries: fp16, each row scaled to 2^13; a lane takes four channels (of 128) of a row
             {
-                const int total = groups == 2 && !streams ? 256 : 128;
-                int ch[8];
-                float down[8];
-                const int cols = pa0 + pa1;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const int col = 32 * k + lane, grp = col < pa0 ? 0 : 1, c = grp ? col - pa0 : col;
-                    const int code = column_code(ks.bits[grp], c);
-                    ch[k] = col < cols && code < ks.count[grp] ? __ldg(ks.perm + head * ks.D + (grp ? ks.count[0] : 0) + code) : -1;
-                    down[k] = pow2(-place_log2(ks.bits[grp], (c & 7) >> 1));
+                const int total = groups == 2 && !streams ? 256 : 128, cols = pa0 + pa1;
+                for (int c = tid; c < cols; c += 256) {
+                    const int grp = c < pa0 ? 0 : 1, code = column_code(ks.bits[grp], grp ? c - pa0 : c);
+                    if (code < ks.count[grp]) sm_col[__ldg(ks.perm + head * ks.D + (grp ? ks.count[0] : 0) + code)] = (int16_t)c;
                 }
                 for (int c = tid; c < pl.o_cols; c += 256) {
                     const int grp = c < va0 ? 0 : 1, code = column_code(vs.bits[grp], grp ? c - va0 : c);
                     sm_chan[c] = code < vs.count[grp] ? (int16_t)__ldg(vs.perm + head * vs.D + (grp ? vs.count[0] : 0) + code) : (int16_t)-1;
                     sm_back[c] = pow2(1 - vs.bits[grp] - place_log2(vs.bits[grp], (c & 7) >> 1));
                 }
-                for (int r0 = warp * (total / 8); r0 < (warp + 1) * (total / 8); r0 += 4) {
-                    float x[4][8];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int row = row0 + r0 + i;
-                        const uint16_t* q = a.Q + b * a.q_seq_stride + (row / a.group) * a.q_token_stride + (head * a.group + row % a.group) * a.q_head_stride;
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) x[i][k] = row < pl.rows && ch[k] >= 0 ? scale_of(q[ch[k]], bf16) : 0.0f;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = r0 + i;
-                        uint32_t top = 0;
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(x[i][k]) & 0x7FFFFFFFu);
-                        top = __reduce_max_sync(0xffffffffu, top);
-                        const int e = top == 0 ? 0 : min(13 - ((int)(top >> 23) - 127), 120);
-                        const float up = a.scale < 0.0f ? -pow2(e) : pow2(e);
-                        if (lane == 0) sm_fac[r] = fmaxf(ldexpf(fabsf(a.scale) * kLog2e, -e), 0x1p-126f);
-                        uint8_t* q = smem + (r >> 7) * pl.k_atoms * kQAtom + (r & 127) * 128;
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const int col = 32 * k + lane;
-                            if (32 * k < cols)
-                                *reinterpret_cast<__half*>(q + (col >> 6) * kQAtom + ((((col & 63) >> 3) ^ (r & 7)) << 4) + 2 * (col & 7)) =
-                                    __float2half_rn(x[i][k] * up * down[k]);
-                        }
+                const int r_first = warp * (total / 8), r_end = r_first + total / 8;
+                if (cols != ks.D) {      // columns without a channel
+                    for (int i = lane; i < (r_end - r_first) * 8 * pl.k_atoms; i += 32) {
+                        const int r = r_first + (i & (total / 8 - 1)), p = i / (total / 8);
+                        *reinterpret_cast<uint4*>(smem + ((r >> 7) * pl.k_atoms + (p >> 3)) * kQAtom + (r & 127) * 128 + (p & 7) * 16) = make_uint4(0, 0, 0, 0);
                     }
                 }
+                bar_group(1, 256);
+                const bool wide = ks.D % 4 == 0 && (((uintptr_t)a.Q | (uintptr_t)(2 * a.q_seq_stride) | (uintptr_t)(2 * a.q_token_stride) |
+                                                     (uintptr_t)(2 * a.q_head_stride)) & 7u) == 0;
+                const float fac0 = fabsf(a.scale) * kLog2e, sign = a.scale < 0.0f ? -1.0f : 1.0f;
+                auto fill = [&](auto halves) {
+                    constexpr int H = decltype(halves)::value;      // 128 channels each
+                    uint32_t to[4 * H];
+                    float down[4 * H];
+#pragma unroll
+                    for (int k = 0; k < 4 * H; ++k) {
+                        const int ch = 128 * (k >> 2) + 4 * lane + (k & 3);
+                        const int col = ch < ks.D ? sm_col[ch] : 0, bits = ks.bits[col < pa0 ? 0 : 1];
+                        to[k] = (col >> 6) * kQAtom + ((col & 63) >> 3) * 16 + 2 * (col & 7);
+                        down[k] = sign * pow2(-place_log2(bits, (col & 7) >> 1));
+                    }
+                    // eight rows' loads go out while the eight before are scaled and stored
+                    int t = (row0 + r_first) / a.group, hq = (row0 + r_first) % a.group, next_row = row0 + r_first;
+                    const uint16_t* q0 = a.Q + b * a.q_seq_stride + (int64_t)head * a.group * a.q_head_stride;
+                    auto load = [&](uint2(&v)[8][H]) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const uint16_t* q = q0 + t * a.q_token_stride + hq * a.q_head_stride;
+#pragma unroll
+                            for (int h = 0; h < H; ++h) {
+                                const int ch = 128 * h + 4 * lane;
+                                v[i][h] = make_uint2(0, 0);
+                                if (next_row < pl.rows && ch < ks.D) {
+                                    if (wide) {
+                                        v[i][h] = *reinterpret_cast<const uint2*>(q + ch);
+                                    } else {
+                                        v[i][h].x = q[ch] | (ch + 1 < ks.D ? (uint32_t)q[ch + 1] << 16 : 0u);
+                                        v[i][h].y = (ch + 2 < ks.D ? q[ch + 2] : 0u) | (ch + 3 < ks.D ? (uint32_t)q[ch + 3] << 16 : 0u);
+                                    }
+                                }
+                            }
+                            ++next_row;
+                            if (++hq == a.group) hq = 0, ++t;
+                        }
+                    };
+                    uint2 v[8][H];
+                    load(v);
+                    for (int r0 = r_first; r0 < r_end; r0 += 8) {
+                        uint2 w[8][H];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+#pragma unroll
+                            for (int h = 0; h < H; ++h) w[i][h] = v[i][h];
+                        if (r0 + 8 < r_end) load(v);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int r = r0 + i;
+                            float x[4 * H];
+                            uint32_t top = 0;
+#pragma unroll
+                            for (int k = 0; k < 4 * H; ++k) {
+                                const uint32_t pair = k & 2 ? w[i][k >> 2].y : w[i][k >> 2].x;
+                                x[k] = scale_of(k & 1 ? pair >> 16 : pair & 0xFFFFu, bf16);
+                                top = max(top, __float_as_uint(x[k]) & 0x7FFFFFFFu);
+                            }
+                            top = __reduce_max_sync(0xffffffffu, top);
+                            const int e = top == 0 ? 0 : min(13 - ((int)(top >> 23) - 127), 120);
+                            const float up = pow2(e);
+                            if (lane == 0) sm_fac[r] = fmaxf(fac0 * pow2(-e), 0x1p-126f);
+                            const uint32_t q = smem0 + (r >> 7) * pl.k_atoms * kQAtom + (r & 127) * 128;
+#pragma unroll
+                            for (int k = 0; k < 4 * H; ++k) {
+                                if (128 * (k >> 2) + 4 * lane + (k & 3) < ks.D)
+                                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(q + (to[k] ^ ((r & 7) << 4))),
+                                                 "h"(__half_as_ushort(__float2half_rn(x[k] * up * down[k])))
+                                                 : "memory");
+                            }
+                        }
+                    }
+                };
+                if (ks.D <= 128) fill(std::integral_constant<int, 1>{});
+                else fill(std::integral_constant<int, 2>{});
                 tc::fence_proxy_async_shared();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(bar(Bars::q_full));
@@ -643,22 +733,26 @@ __global__ void __launch_bounds__(kThreads, 1)
                         ll += __ldcg(stat(i) + unit_rows) * (mi == -INFINITY ? 0.0f : ex2(mi - mm));
                     }
                     const float inv = ll > 0.0f ? 1.0f / ll : (ll == 0.0f ? 0.0f : ll);
-                    for (int c = 0; c < pl.o_cols; c += 32) {
-                        float x[32] = {};
+                    for (int c = 0; c < pl.o_cols; c += 64) {
+                        float x[64] = {};
+                        const int cols = min(64, pl.o_cols - c);       // 32 or 64
                         for (int i = 0; i < seg.n_part; ++i) {
-                            const float mi = __ldcg(stat(i)), f = mi == -INFINITY ? 0.0f : ex2(mi - mm);
                             const float4* from = reinterpret_cast<const float4*>(parts + part_slot(seg, i) * part_floats) + (int64_t)(c / 4) * unit_rows + unit_row;
+                            float4 q[16];
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                const float4 q = __ldcg(from + (int64_t)k * unit_rows);
-                                x[4 * k] = fmaf(f, q.x, x[4 * k]);
-                                x[4 * k + 1] = fmaf(f, q.y, x[4 * k + 1]);
-                                x[4 * k + 2] = fmaf(f, q.z, x[4 * k + 2]);
-                                x[4 * k + 3] = fmaf(f, q.w, x[4 * k + 3]);
+                            for (int k = 0; k < 16; ++k) q[k] = 4 * k < cols ? __ldcg(from + (int64_t)k * unit_rows) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                            const float mi = __ldcg(stat(i)), f = mi == -INFINITY ? 0.0f : ex2(mi - mm);
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) {
+                                x[4 * k] = fmaf(f, q[k].x, x[4 * k]);
+                                x[4 * k + 1] = fmaf(f, q[k].y, x[4 * k + 1]);
+                                x[4 * k + 2] = fmaf(f, q[k].z, x[4 * k + 2]);
+                                x[4 * k + 3] = fmaf(f, q[k].w, x[4 * k + 3]);
                             }
                         }
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) stage_out(c + k, x[k] * inv);
+                        for (int k = 0; k < 64; ++k)
+                            if (k < cols) stage_out(c + k, x[k] * inv);
                     }
                 }
             }
@@ -704,7 +798,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             break;
         }
-        if (!split.next(seg)) break;
+        if (*sm_more == 0) break;
+        seg = *sm_seg;
+        __syncthreads();      // read before it is overwritten
     }
     };
     if (warp < 8) {
@@ -744,12 +840,12 @@ TileLaunch plan_tile(const KvGeom& geo, int64_t T, int64_t group) {
     for (int i = 0; i < 2; ++i) p.scale_step[i] = (p.box_rows * geo.s[i].ng * 2 + 127) / 128 * 128;
     p.raw_v = kTok * ks.row_bytes;
     p.raw_s = p.raw_v + kTok * vs.row_bytes;
-    p.raw_bytes = (p.raw_s + copies * (p.scale_step[0] + p.scale_step[1]) + 127) / 128 * 128;
+    p.raw_bytes = (p.raw_s + copies * (p.scale_step[0] + p.scale_step[1]) + 1023) / 1024 * 1024;     // swizzled tiles start on 1024
     p.stage_bytes = (p.k_atoms + p.v_atoms) * kAtom + 1024;
     p.ring_off = p.tiles * p.k_atoms * kQAtom;
     p.out_stride = (vs.D + 1) / 2 * 4 + 4;
     if (p.out_stride / 4 % 2 == 0) p.out_stride += 4;
-    constexpr int misc = 4096, most = 227 * 1024;
+    constexpr int misc = 5120, most = 227 * 1024;
     // two tiles share a block and look one ahead, two streams two
     static const int choices[][2] = {{4, 4}, {4, 3}, {4, 2}, {3, 4}, {3, 3}, {3, 2}, {2, 3}, {2, 2}};
     for (const auto& c : choices) {
@@ -757,7 +853,7 @@ TileLaunch plan_tile(const KvGeom& geo, int64_t T, int64_t group) {
         p.stages = c[0];
         p.raw_stages = c[1];
         p.raw_off = p.ring_off + p.stages * p.stage_bytes;
-        p.misc_off = p.raw_off + (p.raw_stages * p.raw_bytes + 1023) / 1024 * 1024;
+        p.misc_off = p.raw_off + p.raw_stages * p.raw_bytes;
         p.smem = p.misc_off + misc;
         const int results = p.tiles == 2 ? 256 * p.out_stride : p.o_cols * 512 + 128 * p.out_stride;
         if (p.smem <= most && results <= p.raw_off) {
@@ -789,8 +885,10 @@ cudaError_t launch_kv_tile(const KvGeom& geo, const KvAttendArgs& a, cudaStream_
     const int grid = (int)(want < num_sms() ? want : num_sms());
     KvMaps maps;
     for (int side = 0; side < 2; ++side) {
-        if (!encode_side(geo, geo.s[side], geo.s[side].row_bytes, p.box_rows, CU_TENSOR_MAP_SWIZZLE_NONE, &maps.codes[side],
-                         &maps.scales[side]))
+        // rows whose stride would put eight tokens' pieces on one bank group are swizzled
+        const int row = geo.s[side].row_bytes;
+        const CUtensorMapSwizzle swizzle = row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : (row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE);
+        if (!encode_side(geo, geo.s[side], row, p.box_rows, swizzle, &maps.codes[side], &maps.scales[side]))
             return cudaErrorUnknown;
     }
     cudaError_t e = cudaFuncSetAttribute(kv_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
