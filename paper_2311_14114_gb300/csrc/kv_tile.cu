@@ -166,6 +166,23 @@ __device__ __forceinline__ int column_code(int bits, int col) {
     return 32 * (col >> 5) + key_code(bits, (col >> 3) & 3, (col & 7) >> 1, col & 1);
 }
 
+// Position in a ring of n stages and the parity of its current round.
+struct Ring {
+    int i = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void step(int n) {
+        if (++i == n) {
+            i = 0;
+            phase ^= 1u;
+        }
+    }
+    __device__ __forceinline__ void skip(int by, int n) {
+        const int to = i + by, rounds = to / n;
+        i = to - rounds * n;
+        phase ^= rounds & 1;
+    }
+};
+
 __global__ void __launch_bounds__(kThreads, 1)
     kv_tile_kernel(const KvGeom geo, const KvAttendArgs a, const TilePlan pl, const __grid_constant__ KvMaps maps) {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -241,10 +258,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto wait = [&](int i, uint32_t parity) {
         return tc::wait_bounded_warp(bar(i), parity & 1u, abort_flag, kWaitNs, a.err, kErrWait);
     };
-    uint32_t n_block = 0;        // blocks this CTA has gone through (stages and their parities)
-    uint32_t n_s[2] = {0, 0};    // ... of each softmax group
-    uint32_t n_o[2] = {0, 0}, n_seg = 0;      // segments that a softmax group took part in; all
-    bool ok = true;
+    // where the next segment's blocks begin in the rings; parities of the softmax groups'
+    // barriers (bit s) and of their results', and of the queries'
+    Ring kv0, raw0;
+    uint32_t s_phase = 0, o_phase = 0, q_phase = 0;
+    bool ok = true, checked = false;
 
     const Segment first = split.segment(chunks);
     auto work = [&](auto role) {
@@ -262,8 +280,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (ROLE == 2 && warp == 13) {
             // ---- copies ----
             const int32_t* table = a.table + b * a.table_stride;
-            for (int j = 0; ok && j < nblk; ++j) {
-                const uint32_t n = n_block + j, r = n % pl.raw_stages;
+            Ring ring_r = raw0;
+            for (int j = 0; ok && j < nblk; ++j, ring_r.step(pl.raw_stages)) {
+                const int r = ring_r.i;
                 const int p0 = (seg.c_first + j) * kTok;
                 const int boxes = p0 < end ? min(kTok / pl.box_rows, (end - p0 + pl.box_rows - 1) / pl.box_rows) : 0;
                 int page = -1;
@@ -271,9 +290,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const bool good = (unsigned)page < (unsigned)geo.n_pages;
                 if (lane < boxes && !good) atomicOr(a.err, kErrKvIndex);
                 if (!good) page = (int)geo.n_pages;        // reads as zeros
-                ok = wait(Bars::raw_free + r, (n / pl.raw_stages) + 1);
+                ok = wait(Bars::raw_free + r, ring_r.phase ^ 1u);
                 if (!ok) break;
-                if (a.drop && n == 0 && blockIdx.x == 0) continue;
+                if (a.drop && j == 0 && blockIdx.x == 0) continue;
                 const uint32_t at = raw + r * pl.raw_bytes, full = bar(Bars::raw_full + r);
                 if (tc::elect_one()) tc::mbar_arrive_expect_tx(full, boxes * pl.box_rows * (ks.row_bytes + vs.row_bytes + 2 * (ks.ng + vs.ng)));
                 for (int i = 0; i < boxes; ++i) {
@@ -295,9 +314,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t id_o0 = fmt | (1u << 16) | ((uint32_t)(va0 >> 3) << 17), id_o1 = fmt | (1u << 16) | ((uint32_t)(va1 >> 3) << 17);
             // Every lane runs the loops, the elected one issues: descriptors stay in uniform registers.
             const bool leader = tc::elect_one();
-            auto scores = [&](int s, uint32_t n) {
+            auto scores = [&](int s, int st) {
                 uint64_t q = tc::sw128_desc(smem0 + (streams ? 0 : s * pl.k_atoms * kQAtom));
-                uint64_t k = tc::sw128_desc(ring + (n % pl.stages) * pl.stage_bytes);
+                uint64_t k = tc::sw128_desc(ring + st * pl.stage_bytes);
                 const uint32_t d = tmem + s * kSlotCols;
                 const int steps0 = pa0 / 32, steps = (pa0 + pa1) / 32;      // of 32 codes: two MMAs
 #pragma unroll 4
@@ -314,8 +333,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (leader) tc::mma_commit(bar(Bars::s_full + s));
                 __syncwarp();
             };
-            auto outputs = [&](int s, uint32_t n, bool first, bool frees, bool last) {
-                const uint64_t v = value_desc(ring + (n % pl.stages) * pl.stage_bytes + pl.k_atoms * kAtom);
+            auto outputs = [&](int s, int st, bool first, bool frees, bool last) {
+                const uint64_t v = value_desc(ring + st * pl.stage_bytes + pl.k_atoms * kAtom);
                 const uint32_t p = tmem + s * kSlotCols, d = p + o_off;
 #pragma unroll
                 for (int k = 0; k < kTok / 16; ++k)
@@ -327,38 +346,41 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (leader) mma_ts(d + va0, p + 32 + 8 * k, v1 + k * (2048 >> 4), id_o1, !(first && k == 0));
                 }
                 if (leader) {
-                    if (frees) tc::mma_commit(bar(Bars::kv_free + n % pl.stages));
+                    if (frees) tc::mma_commit(bar(Bars::kv_free + st));
                     if (last) tc::mma_commit(bar(Bars::o_full + s));
                 }
                 __syncwarp();
             };
-            auto ready = [&](int which, uint32_t n) {
-                ok = ok && wait(which + n % pl.stages, n / pl.stages);
+            auto ready = [&](int which, const Ring& at) {
+                ok = ok && wait(which + at.i, at.phase);
                 tc::tc_fence_after();
             };
-            ok = wait(Bars::q_full, n_seg);
+            ok = wait(Bars::q_full, q_phase);
             tc::tc_fence_after();
+            Ring now = kv0, next = kv0;       // the block whose outputs, and whose scores, come next
             for (int s = 0; ok && s < groups; ++s) {
-                const uint32_t n = n_block + (streams ? s : 0);
-                ready(Bars::k_ready, n);
-                if (ok) scores(s, n);
+                ready(Bars::k_ready, next);
+                if (ok) scores(s, next.i);
+                if (streams) next.step(pl.stages);
             }
-            uint32_t done[2] = {0, 0};
+            if (!streams) next.step(pl.stages);
+            uint32_t phase = s_phase;
             for (int j = 0; ok && j < nblk; ++j) {
-                const uint32_t n = n_block + j;
-                for (int s = streams ? (j & 1) : 0; ok && s < (streams ? (j & 1) + 1 : groups); ++s) {
-                    ok = wait(Bars::p_full + s, n_s[s] + done[s]);
-                    tc::tc_fence_after();
-                    ready(Bars::v_ready, n);
+                const int s_begin = streams ? j & 1 : 0, s_end = streams ? s_begin + 1 : groups;
+                const bool more = j + (streams ? 2 : 1) < nblk, first = j < (streams ? 2 : 1);
+                for (int s = s_begin; ok && s < s_end; ++s) {
+                    ok = wait(Bars::p_full + s, phase >> s);
+                    ready(Bars::v_ready, now);
                     if (!ok) break;
-                    const int next = j + (streams ? 2 : 1);
-                    outputs(s, n, done[s] == 0, streams || s == groups - 1, next >= nblk);
-                    ++done[s];
-                    if (next < nblk) {
-                        ready(Bars::k_ready, n_block + next);
-                        if (ok) scores(s, n_block + next);
+                    phase ^= 1u << s;
+                    outputs(s, now.i, first, s == s_end - 1, !more);
+                    if (more) {
+                        ready(Bars::k_ready, next);
+                        if (ok) scores(s, next.i);
                     }
                 }
+                now.step(pl.stages);
+                next.step(pl.stages);
             }
         } else if (ROLE == 2 && warp == 14) {
             // ---- the segment after this one ----
@@ -366,16 +388,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (more) *sm_seg = split.segment(chunks);
             *sm_more = more;
         } else if (ROLE == 2 && warp == 15) {
-            if (n_seg == 0) check_lengths(geo, a, lane, 32);
+            if (!checked) check_lengths(geo, a, lane, 32);
+            checked = true;
         } else if constexpr (ROLE == 1) {
             // ---- packed rows -> operand tiles ----
             const int dw = warp - 8, tok = (dw & 1) * 32 + lane;
             const Offsets f;
-            for (int j = 0; ok && j < nblk; ++j) {
-                const uint32_t n = n_block + j, st = n % pl.stages, r = n % pl.raw_stages;
+            Ring kv = kv0, rw = raw0;
+            for (int j = 0; ok && j < nblk; ++j, kv.step(pl.stages), rw.step(pl.raw_stages)) {
+                const int st = kv.i, r = rw.i;
                 const int p0 = (seg.c_first + j) * kTok;
                 const uint32_t at = ring + st * pl.stage_bytes, src = raw + r * pl.raw_bytes;
-                ok = wait(Bars::kv_free + st, (n / pl.stages) + 1) && wait(Bars::raw_full + r, n / pl.raw_stages);
+                ok = wait(Bars::kv_free + st, kv.phase ^ 1u) && wait(Bars::raw_full + r, rw.phase);
                 if (!ok) break;
                 // scales as fp32: keys' by warps 0 and 1 (with 2^-(n-1)), values' by 2 and 3, relative to a power of two
                 {
@@ -545,13 +569,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             int e0 = 0, e1 = 0;
             const int mine = s < groups ? (streams ? (nblk - s + 1) / 2 : nblk) : 0;
             const int sure = min(len, end);
+            Ring kv = kv0;
+            if (streams && s == 1) kv.step(pl.stages);
+            uint32_t phase = s_phase >> s;
             for (int i = 0; ok && i < mine; ++i) {
-                const int j = streams ? 2 * i + s : i;
-                const uint32_t n = n_block + j, st = n % pl.stages;
+                const int j = streams ? 2 * i + s : i, st = kv.i;
                 const int p0 = (seg.c_first + j) * kTok;
                 const uint32_t sc = ring + st * pl.stage_bytes + (pl.k_atoms + pl.v_atoms) * kAtom;
-                ok = wait(Bars::k_ready + st, n / pl.stages) && wait(Bars::s_full + s, n_s[s] + i);
+                ok = wait(Bars::k_ready + st, kv.phase) && wait(Bars::s_full + s, phase);
                 if (!ok) break;
+                phase ^= 1u;
+                kv.step(pl.stages);
+                if (streams) kv.step(pl.stages);
                 tc::tc_fence_after();
                 float2 x[kTok / 2];
 #pragma unroll
@@ -651,7 +680,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (lane == 0) tc::mbar_arrive(bar(Bars::p_full + s));
             }
             // ---- results: both groups' MMAs are complete, so queries' and operands' memory is free ----
-            for (int g = 0; g < groups; ++g) ok = ok && wait(Bars::o_full + g, n_o[g]);
+            for (int g = 0; g < groups; ++g) ok = ok && wait(Bars::o_full + g, o_phase >> g);
             tc::tc_fence_after();
             const bool works = s < (streams ? 1 : groups);          // this group has a tile's results
             const bool whole = seg.n_part == 1;
@@ -774,12 +803,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
         }
-        n_block += nblk;
-        for (int s = 0; s < groups; ++s) {
-            n_s[s] += streams ? (nblk - s + 1) / 2 : nblk;
-            n_o[s] += 1;
-        }
-        ++n_seg;
+        kv0.skip(nblk, pl.stages);
+        raw0.skip(nblk, pl.raw_stages);
+        // each group's number of blocks, modulo 2
+        const uint32_t odd0 = (streams ? (nblk + 1) / 2 : nblk) & 1, odd1 = (streams ? nblk / 2 : (groups == 2 ? nblk : 0)) & 1;
+        s_phase ^= odd0 | odd1 << 1;
+        o_phase ^= groups == 2 ? 3u : 1u;
+        q_phase ^= 1u;
         tc::tc_fence_before();
         __syncthreads();
         tc::tc_fence_after();
