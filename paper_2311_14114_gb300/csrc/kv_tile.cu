@@ -6,12 +6,12 @@
 // With 128 rows to a tile the products (4 x 64 x 128 x 128 multiply-adds per 64
 // tokens at 128 channels) and the exponentials are the work; the cache's bytes
 // are read once per tile of up to 256 rows.  One CTA per SM, 16 warps:
-//   warps 0-3, 4-7  softmax of two row tiles (a thread per row, its scores from
-//                   TMEM), each with its own S, P and O columns;
-//   warps 8-11      unpack a block of 64 tokens into fp16 operand tiles (codes
+//   warp 0          issues the MMAs;  warp 1  copies packed rows by TMA;
+//   warps 4-7       unpack a block of 64 tokens into fp16 operand tiles (codes
 //                   exactly, scales as fp32 beside them);
-//   warp 12         issues the MMAs;  warp 13  copies packed rows by TMA.
-// (Registers move to the softmax warps: 2 x 192 + 72 + 56 = 4 x 128 a thread.)
+//   warps 8-11, 12-15  softmax of two row tiles (a thread per row, its scores from
+//                   TMEM), each with its own S, P and O columns.
+// (Registers move to the softmax warps: 2 x 184 + 72 + 72 = 4 x 128 a thread.)
 // While one tile's softmax runs, the tensor cores work for the other.  With at
 // most 128 rows both softmax groups serve the same tile on alternate blocks,
 // as two streams joined at the end.
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     Split split;
     if (!split.begin(chunks, a.B * pl.row_units, geo.heads, pl.min_chunks, 8, words)) return;
 
-    if (warp == 12) {
+    if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(tmem_at)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int groups = pl.tiles == 2 ? (row0 + 128 < pl.rows ? 2 : 1) : (nblk > 1 ? 2 : 1);
         const bool streams = pl.tiles == 1;
 
-        if (ROLE == 2 && warp == 13) {
+        if (ROLE == 2 && warp == 1) {
             // ---- copies ----
             const int32_t* table = a.table + b * a.table_stride;
             Ring ring_r = raw0;
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
             }
-        } else if (ROLE == 2 && warp == 12) {
+        } else if (ROLE == 2 && warp == 0) {
             // ---- MMAs ----
             constexpr uint32_t fmt = (1u << 4) | ((128u >> 4) << 24);
             const uint32_t id_s = fmt | ((kTok >> 3) << 17);
@@ -315,36 +315,49 @@ __global__ void __launch_bounds__(kThreads, 1)
             // Every lane runs the loops, the elected one issues: descriptors stay in uniform registers.
             const bool leader = tc::elect_one();
             auto scores = [&](int s, int st) {
-                uint64_t q = tc::sw128_desc(smem0 + (streams ? 0 : s * pl.k_atoms * kQAtom));
-                uint64_t k = tc::sw128_desc(ring + st * pl.stage_bytes);
+                const uint64_t q0 = tc::sw128_desc(smem0 + (streams ? 0 : s * pl.k_atoms * kQAtom));
+                const uint64_t k0 = tc::sw128_desc(ring + st * pl.stage_bytes);
                 const uint32_t d = tmem + s * kSlotCols;
-                const int steps0 = pa0 / 32, steps = (pa0 + pa1) / 32;      // of 32 codes: two MMAs
-#pragma unroll 4
-                for (int i = 0; i < steps; ++i) {
-                    const uint32_t to = d + (i >= steps0 ? kTok : 0);
-                    if (leader) {
-                        mma_ss(to, q, k, id_s, i != 0 && i != steps0);
-                        mma_ss(to, q + 2, k + 2, id_s, 1);
+                // 32-code halves of column groups [h, end): two MMAs each, four in a run where a whole group is left
+                auto group = [&](uint32_t to, int h, int end) {
+                    uint32_t acc = 0;
+                    while (h < end) {
+                        const uint64_t q = q0 + (h >> 1) * (kQAtom >> 4) + (h & 1) * 4, k = k0 + (h >> 1) * (kAtom >> 4) + (h & 1) * 4;
+                        if ((h & 1) == 0 && h + 1 < end) {
+                            if (leader) {
+                                mma_ss(to, q, k, id_s, acc);
+                                mma_ss(to, q + 2, k + 2, id_s, 1);
+                                mma_ss(to, q + 4, k + 4, id_s, 1);
+                                mma_ss(to, q + 6, k + 6, id_s, 1);
+                            }
+                            h += 2;
+                        } else {
+                            if (leader) {
+                                mma_ss(to, q, k, id_s, acc);
+                                mma_ss(to, q + 2, k + 2, id_s, 1);
+                            }
+                            h += 1;
+                        }
+                        acc = 1;
                     }
-                    // half a column group on, or the next column group
-                    q += i & 1 ? (kQAtom - 64) >> 4 : 4;
-                    k += i & 1 ? (kAtom - 64) >> 4 : 4;
-                }
+                };
+                group(d, 0, ks.nb[0]);
+                if (ks.ng == 2) group(d + kTok, ks.nb[0], ks.nb[0] + ks.nb[1]);
                 if (leader) tc::mma_commit(bar(Bars::s_full + s));
                 __syncwarp();
             };
             auto outputs = [&](int s, int st, bool first, bool frees, bool last) {
                 const uint64_t v = value_desc(ring + st * pl.stage_bytes + pl.k_atoms * kAtom);
                 const uint32_t p = tmem + s * kSlotCols, d = p + o_off;
+                auto group = [&](uint32_t to, uint32_t from, uint64_t v, uint32_t id) {
+                    if (leader) {
+                        mma_ts(to, from, v, id, !first);
 #pragma unroll
-                for (int k = 0; k < kTok / 16; ++k)
-                    if (leader) mma_ts(d, p + 8 * k, v + k * (2048 >> 4), id_o0, !(first && k == 0));
-                if (vs.ng == 2) {
-                    const uint64_t v1 = v + pl.v_atom1 * (kAtom >> 4);
-#pragma unroll
-                    for (int k = 0; k < kTok / 16; ++k)
-                        if (leader) mma_ts(d + va0, p + 32 + 8 * k, v1 + k * (2048 >> 4), id_o1, !(first && k == 0));
-                }
+                        for (int k = 1; k < kTok / 16; ++k) mma_ts(to, from + 8 * k, v + k * (2048 >> 4), id, 1);
+                    }
+                };
+                group(d, p, v, id_o0);
+                if (vs.ng == 2) group(d + va0, p + 32, v + pl.v_atom1 * (kAtom >> 4), id_o1);
                 if (leader) {
                     if (frees) tc::mma_commit(bar(Bars::kv_free + st));
                     if (last) tc::mma_commit(bar(Bars::o_full + s));
@@ -369,9 +382,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int s_begin = streams ? j & 1 : 0, s_end = streams ? s_begin + 1 : groups;
                 const bool more = j + (streams ? 2 : 1) < nblk, first = j < (streams ? 2 : 1);
                 for (int s = s_begin; ok && s < s_end; ++s) {
-                    ok = wait(Bars::p_full + s, phase >> s);
                     ready(Bars::v_ready, now);
+                    ok = ok && wait(Bars::p_full + s, phase >> s);
                     if (!ok) break;
+                    tc::tc_fence_after();
                     phase ^= 1u << s;
                     outputs(s, now.i, first, s == s_end - 1, !more);
                     if (more) {
@@ -382,17 +396,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                 now.step(pl.stages);
                 next.step(pl.stages);
             }
-        } else if (ROLE == 2 && warp == 14) {
+        } else if (ROLE == 2 && warp == 2) {
             // ---- the segment after this one ----
             const bool more = split.next(seg);
             if (more) *sm_seg = split.segment(chunks);
             *sm_more = more;
-        } else if (ROLE == 2 && warp == 15) {
+        } else if (ROLE == 2 && warp == 3) {
             if (!checked) check_lengths(geo, a, lane, 32);
             checked = true;
         } else if constexpr (ROLE == 1) {
             // ---- packed rows -> operand tiles ----
-            const int dw = warp - 8, tok = (dw & 1) * 32 + lane;
+            const int dw = warp - 4, tok = (dw & 1) * 32 + lane;
             const Offsets f;
             Ring kv = kv0, rw = raw0;
             for (int j = 0; ok && j < nblk; ++j, kv.step(pl.stages), rw.step(pl.raw_stages)) {
@@ -458,20 +472,20 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         } else if constexpr (ROLE == 0) {
             // ---- softmax ----
-            const int s = warp >> 2, quad = warp & 3;
+            const int s = (warp >> 2) - 2, quad = warp & 3, st_id = tid - 256;
             // queries: fp16, each row scaled to 2^13; a lane takes four channels (of 128) of a row
             {
                 const int total = groups == 2 && !streams ? 256 : 128, cols = pa0 + pa1;
-                for (int c = tid; c < cols; c += 256) {
+                for (int c = st_id; c < cols; c += 256) {
                     const int grp = c < pa0 ? 0 : 1, code = column_code(ks.bits[grp], grp ? c - pa0 : c);
                     if (code < ks.count[grp]) sm_col[__ldg(ks.perm + head * ks.D + (grp ? ks.count[0] : 0) + code)] = (int16_t)c;
                 }
-                for (int c = tid; c < pl.o_cols; c += 256) {
+                for (int c = st_id; c < pl.o_cols; c += 256) {
                     const int grp = c < va0 ? 0 : 1, code = column_code(vs.bits[grp], grp ? c - va0 : c);
                     sm_chan[c] = code < vs.count[grp] ? (int16_t)__ldg(vs.perm + head * vs.D + (grp ? vs.count[0] : 0) + code) : (int16_t)-1;
                     sm_back[c] = pow2(1 - vs.bits[grp] - place_log2(vs.bits[grp], (c & 7) >> 1));
                 }
-                const int r_first = warp * (total / 8), r_end = r_first + total / 8;
+                const int r_first = (warp - 8) * (total / 8), r_end = r_first + total / 8;
                 if (cols != ks.D) {      // columns without a channel
                     for (int i = lane; i < (r_end - r_first) * 8 * pl.k_atoms; i += 32) {
                         const int r = r_first + (i & (total / 8 - 1)), p = i / (total / 8);
@@ -744,7 +758,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!whole) {
                 __threadfence();
                 bar_group(1, 256);
-                if (tid == 0) {
+                if (st_id == 0) {
                     unsigned* counter = static_cast<unsigned*>(a.scratch) + seg.cta0;
                     *sm_last = !tc::abort_raised(abort_flag) && atomicAdd(counter, 1u) == (unsigned)(seg.n_part - 1);
                     if (*sm_last) *counter = 0;
@@ -816,12 +830,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (tc::abort_raised(abort_flag)) {
             // a copy did not come: let those on their way land, and the MMAs end, within the same bound
             const long long t0 = tc::globaltimer();
-            if (warp == 13) {
+            if (warp == 1) {
                 for (uint32_t i = 0; i < (uint32_t)pl.raw_stages; ++i)
                     while (!tc::mbar_try_wait(bar(Bars::raw_full + i), 0) && !tc::mbar_try_wait(bar(Bars::raw_full + i), 1) &&
                            tc::globaltimer() - t0 < kWaitNs) {
                     }
-            } else if (warp == 12) {
+            } else if (warp == 0) {
                 if (tc::elect_one()) tc::mma_commit(bar(Bars::drain));
                 while (!tc::mbar_try_wait(bar(Bars::drain), 0) && tc::globaltimer() - t0 < kWaitNs) {
                 }
@@ -833,18 +847,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncthreads();      // read before it is overwritten
     }
     };
-    if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
         work(std::integral_constant<int, 0>{});
-    } else if (warp < 12) {
+    } else if (warp >= 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         work(std::integral_constant<int, 1>{});
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         work(std::integral_constant<int, 2>{});
     }
     __syncthreads();
-    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
 struct TileLaunch {
