@@ -40,6 +40,9 @@ constexpr int kThreads = 512;
 constexpr int kAtom = kTok * 128;        // bytes of a 64-code column group of a K or V tile
 constexpr int kQAtom = 128 * 128;        // ... of a query tile
 constexpr int kSlotCols = 256;           // TMEM columns of a softmax group: S (and P over it), then O
+// Columns of a softmax group in front of O: scores (the weights of the first value group go over them), and those
+// of the second key group or the weights of the second value group
+__host__ __device__ constexpr int s_cols(int k_groups, int v_groups) { return k_groups == 2 ? 2 * kTok : (v_groups == 2 ? kTok + kTok / 2 : kTok); }
 constexpr float kLazy = 8.0f;            // a maximum may be exceeded by this (log2) before O is rescaled
 
 struct TilePlan {
@@ -70,6 +73,14 @@ __device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
           "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
           "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(at)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16v(uint32_t at, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};\n\t"
+        "tcgen05.wait::st.sync.aligned;" ::"r"(at),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
 __device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) {
@@ -252,7 +263,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncthreads();
     tc::tc_fence_after();
     const uint32_t tmem = *tmem_at;
-    const uint32_t o_off = kTok * ks.ng;     // O's first column in a slot
+    const uint32_t p1_off = kTok;            // the second value group's weights, behind the first scores
+    const uint32_t o_off = s_cols(ks.ng, vs.ng);     // O's first column in a slot
+    const int nkb = ks.nb[0] + ks.nb[1];
     const int pa0 = 32 * ks.nb[0], pa1 = 32 * ks.nb[1], va0 = 32 * vs.nb[0], va1 = 32 * vs.nb[1];
 
     auto wait = [&](int i, uint32_t parity) {
@@ -318,31 +331,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const uint64_t q0 = tc::sw128_desc(smem0 + (streams ? 0 : s * pl.k_atoms * kQAtom));
                 const uint64_t k0 = tc::sw128_desc(ring + st * pl.stage_bytes);
                 const uint32_t d = tmem + s * kSlotCols;
-                // 32-code halves of column groups [h, end): two MMAs each, four in a run where a whole group is left
-                auto group = [&](uint32_t to, int h, int end) {
-                    uint32_t acc = 0;
-                    while (h < end) {
-                        const uint64_t q = q0 + (h >> 1) * (kQAtom >> 4) + (h & 1) * 4, k = k0 + (h >> 1) * (kAtom >> 4) + (h & 1) * 4;
-                        if ((h & 1) == 0 && h + 1 < end) {
-                            if (leader) {
-                                mma_ss(to, q, k, id_s, acc);
-                                mma_ss(to, q + 2, k + 2, id_s, 1);
-                                mma_ss(to, q + 4, k + 4, id_s, 1);
-                                mma_ss(to, q + 6, k + 6, id_s, 1);
-                            }
-                            h += 2;
-                        } else {
-                            if (leader) {
-                                mma_ss(to, q, k, id_s, acc);
-                                mma_ss(to, q + 2, k + 2, id_s, 1);
-                            }
-                            h += 1;
-                        }
-                        acc = 1;
+                // 32-code halves of column groups, two MMAs each
+#pragma unroll 1
+                for (int h = 0; h < nkb; ++h) {
+                    const uint64_t q = q0 + (h >> 1) * (kQAtom >> 4) + (h & 1) * 4, k = k0 + (h >> 1) * (kAtom >> 4) + (h & 1) * 4;
+                    const bool second = h >= ks.nb[0];
+                    const uint32_t to = d + (second ? kTok : 0);
+                    if (leader) {
+                        mma_ss(to, q, k, id_s, h != 0 && h != ks.nb[0]);
+                        mma_ss(to, q + 2, k + 2, id_s, 1);
                     }
-                };
-                group(d, 0, ks.nb[0]);
-                if (ks.ng == 2) group(d + kTok, ks.nb[0], ks.nb[0] + ks.nb[1]);
+                }
                 if (leader) tc::mma_commit(bar(Bars::s_full + s));
                 __syncwarp();
             };
@@ -357,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 };
                 group(d, p, v, id_o0);
-                if (vs.ng == 2) group(d + va0, p + 32, v + pl.v_atom1 * (kAtom >> 4), id_o1);
+                if (vs.ng == 2) group(d + va0, p + p1_off, v + pl.v_atom1 * (kAtom >> 4), id_o1);
                 if (leader) {
                     if (frees) tc::mma_commit(bar(Bars::kv_free + st));
                     if (last) tc::mma_commit(bar(Bars::o_full + s));
@@ -596,40 +595,52 @@ __global__ void __launch_bounds__(kThreads, 1)
                 kv.step(pl.stages);
                 if (streams) kv.step(pl.stages);
                 tc::tc_fence_after();
-                float2 x[kTok / 2];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                // 32 tokens' scores at a time, read twice (for the maximum, for the weights): a short loop keeps
+                // all roles' code in the instruction caches, which a block unrolled as a whole did not (5 us a block)
+                const bool tail = p0 + kTok > sure;
+                auto scores = [&](int h, float2(&x)[16]) {
                     uint32_t v[32];
                     tmem_ld32(t_s + 32 * h, v);
 #pragma unroll
                     for (int k = 0; k < 16; k += 2) {
                         const float4 kk = lds128f(sc + 128 * h + 8 * k);
-                        x[16 * h + k] = mul2(make_float2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), make_float2(kk.x, kk.y));
-                        x[16 * h + k + 1] = mul2(make_float2(__uint_as_float(v[2 * k + 2]), __uint_as_float(v[2 * k + 3])), make_float2(kk.z, kk.w));
+                        x[k] = mul2(make_float2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), make_float2(kk.x, kk.y));
+                        x[k + 1] = mul2(make_float2(__uint_as_float(v[2 * k + 2]), __uint_as_float(v[2 * k + 3])), make_float2(kk.z, kk.w));
                     }
                     if (ks.ng == 2) {
                         tmem_ld32(t_s + kTok + 32 * h, v);
 #pragma unroll
                         for (int k = 0; k < 16; k += 2) {
                             const float4 kk = lds128f(sc + 256 + 128 * h + 8 * k);
-                            x[16 * h + k] = fma2(make_float2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), make_float2(kk.x, kk.y), x[16 * h + k]);
-                            x[16 * h + k + 1] = fma2(make_float2(__uint_as_float(v[2 * k + 2]), __uint_as_float(v[2 * k + 3])), make_float2(kk.z, kk.w), x[16 * h + k + 1]);
+                            x[k] = fma2(make_float2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), make_float2(kk.x, kk.y), x[k]);
+                            x[k + 1] = fma2(make_float2(__uint_as_float(v[2 * k + 2]), __uint_as_float(v[2 * k + 3])), make_float2(kk.z, kk.w), x[k + 1]);
                         }
                     }
-                }
-                if (p0 + kTok > sure) {
-                    const uint8_t* mask = a.mask ? a.mask + b * a.mask_stride + (int64_t)t_row * a.T : nullptr;
+                    if (tail) {
+                        // the tokens of this half that the row sees
+                        uint32_t seen = 0;
+                        const uint8_t* mask = a.mask ? a.mask + b * a.mask_stride + (int64_t)t_row * a.T : nullptr;
+#pragma unroll 1
+                        for (int k = 0; k < 32; ++k) {
+                            const int p = p0 + 32 * h + k, d = p - len;
+                            const bool see = p < end && (d < 0 || (mask ? mask[d] != 0 : d <= t_row));
+                            seen |= (uint32_t)see << k;
+                        }
 #pragma unroll
-                    for (int k = 0; k < kTok; ++k) {
-                        const int p = p0 + k, d = p - len;
-                        bool see = p < end;
-                        if (see && d >= 0) see = mask ? mask[d] != 0 : d <= t_row;
-                        if (!see) (k & 1 ? x[k >> 1].y : x[k >> 1].x) = -INFINITY;
+                        for (int k = 0; k < 16; ++k) {
+                            if (!(seen >> (2 * k) & 1u)) x[k].x = -INFINITY;
+                            if (!(seen >> (2 * k + 1) & 1u)) x[k].y = -INFINITY;
+                        }
                     }
-                }
+                };
                 float top = -INFINITY;
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                    float2 x[16];
+                    scores(h, x);
 #pragma unroll
-                for (int k = 0; k < kTok / 2; ++k) top = fmaxf(fmaxf(top, x[k].x), x[k].y);
+                    for (int k = 0; k < 16; ++k) top = fmaxf(fmaxf(top, x[k].x), x[k].y);
+                }
                 // raise the maximum, and the powers of two of the value scales, where they are left behind by much
                 const int b0 = sm_e[2 * st], b1 = sm_e[2 * st + 1];
                 const bool first = i == 0;
@@ -646,6 +657,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     const float al0 = al * (n0 - e0 > 126 ? 0.0f : pow2(e0 - n0)), al1 = al * (n1 - e1 > 126 ? 0.0f : pow2(e1 - n1));
                     // the MMAs that wrote O are complete: they came before the ones that wrote these scores
+#pragma unroll 1
                     for (int c = 0; c < pl.o_cols; c += 32) {
                         uint32_t v[32];
                         tmem_ld32(t_s + o_off + c, v);
@@ -657,38 +669,42 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 e0 = n0;
                 e1 = n1;
-                // weights, times 2^(block's power - running power)
-                const int d0 = max(b0 - e0, -126);
-                const float shift = (m == -INFINITY ? 0.0f : -m * fac) + (float)d0;
+                // weights, times 2^(block's power - running power); over the scores that are done with: the first
+                // value group's from column 0, the second's from the second key group's place
+                const int d0 = max(b0 - e0, -126), dd = b1 - e1 - d0;
+                const float shift = (m == -INFINITY ? 0.0f : -m * fac) + (float)d0, second = dd < -126 ? 0.0f : pow2(min(dd, 127));
                 float2 sum = make_float2(0.0f, 0.0f);
-                uint32_t w[32];
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                    float2 x[16];
+                    scores(h, x);
+                    uint32_t w[16];
 #pragma unroll
-                for (int k = 0; k < kTok / 2; ++k) {
-                    const float2 y = fma2(x[k], make_float2(fac, fac), make_float2(shift, shift));
-                    x[k] = make_float2(ex2(y.x), ex2(y.y));
-                    sum = fma2(x[k], make_float2(1.0f, 1.0f), sum);
-                }
-                l += (sum.x + sum.y) * pow2(-d0);
+                    for (int k = 0; k < 16; ++k) {
+                        const float2 y = fma2(x[k], make_float2(fac, fac), make_float2(shift, shift));
+                        x[k] = make_float2(ex2(y.x), ex2(y.y));
+                        sum = fma2(x[k], make_float2(1.0f, 1.0f), sum);
+                    }
 #pragma unroll
-                for (int k = 0; k < 32; k += 2) {
-                    const float4 vv = lds128f(sc + 512 + 8 * k);
-                    const float2 y0 = mul2(x[k], make_float2(vv.x, vv.y)), y1 = mul2(x[k + 1], make_float2(vv.z, vv.w));
-                    w[k] = pack2(y0.x, y0.y);
-                    w[k + 1] = pack2(y1.x, y1.y);
-                }
-                tmem_st32(t_s, w);
-                if (vs.ng == 2) {
-                    const int dd = b1 - e1 - d0;
-                    const float c = dd < -126 ? 0.0f : pow2(min(dd, 127));
-#pragma unroll
-                    for (int k = 0; k < 32; k += 2) {
-                        const float4 vv = lds128f(sc + 768 + 8 * k);
-                        const float2 y0 = mul2(x[k], make_float2(vv.x * c, vv.y * c)), y1 = mul2(x[k + 1], make_float2(vv.z * c, vv.w * c));
+                    for (int k = 0; k < 16; k += 2) {
+                        const float4 vv = lds128f(sc + 512 + 128 * h + 8 * k);
+                        const float2 y0 = mul2(x[k], make_float2(vv.x, vv.y)), y1 = mul2(x[k + 1], make_float2(vv.z, vv.w));
                         w[k] = pack2(y0.x, y0.y);
                         w[k + 1] = pack2(y1.x, y1.y);
                     }
-                    tmem_st32(t_s + 32, w);
+                    tmem_st16v(t_s + 16 * h, w);
+                    if (vs.ng == 2) {
+#pragma unroll
+                        for (int k = 0; k < 16; k += 2) {
+                            const float4 vv = lds128f(sc + 768 + 128 * h + 8 * k);
+                            const float2 y0 = mul2(x[k], make_float2(vv.x * second, vv.y * second)), y1 = mul2(x[k + 1], make_float2(vv.z * second, vv.w * second));
+                            w[k] = pack2(y0.x, y0.y);
+                            w[k + 1] = pack2(y1.x, y1.y);
+                        }
+                        tmem_st16v(t_s + p1_off + 16 * h, w);
+                    }
                 }
+                l += (sum.x + sum.y) * pow2(-d0);
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(bar(Bars::p_full + s));
@@ -878,7 +894,7 @@ TileLaunch plan_tile(const KvGeom& geo, int64_t T, int64_t group) {
     p.v_atom1 = (vs.nb[0] + 1) / 2;
     p.v_atoms = p.v_atom1 + (vs.nb[1] + 1) / 2;
     p.o_cols = 32 * (vs.nb[0] + vs.nb[1]);
-    if (kTok * ks.ng + p.o_cols > kSlotCols) return t;
+    if (s_cols(ks.ng, vs.ng) + p.o_cols > kSlotCols) return t;
     p.box_rows = geo.page < kTok ? geo.page : kTok;
     const int copies = kTok / p.box_rows;
     for (int i = 0; i < 2; ++i) p.scale_step[i] = (p.box_rows * geo.s[i].ng * 2 + 127) / 128 * 128;
