@@ -173,9 +173,9 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
     float* sm_m = sm_tl + R;                                         // [8][R]
     float* sm_l = sm_m + 8 * R;                                      // [8][R]
     int16_t* sm_chan = reinterpret_cast<int16_t*>(sm_l + 8 * R);     // [32 NVB]
-    uint32_t* sm_scan = reinterpret_cast<uint32_t*>(smem + pl.bar_off + 256);      // [16]
-    int& sm_last = reinterpret_cast<int&>(sm_scan[16]);
-    int& sm_abort = reinterpret_cast<int&>(sm_scan[17]);
+    uint32_t* sm_scan = reinterpret_cast<uint32_t*>(smem + pl.bar_off + 256);      // [32]
+    int& sm_last = reinterpret_cast<int&>(sm_scan[32]);
+    int& sm_abort = reinterpret_cast<int&>(sm_scan[33]);
     const uint32_t abort_flag = tc::smem_u32(&sm_abort);
 
     if (lane == 0) {
@@ -790,7 +790,7 @@ RowsLaunch plan_rows(const KvGeom& geo, int64_t T, int64_t group) {
     const int stage = kChunk * (r.ks + r.vs);
     const int q = nkb * r.nt * 512;
     const int misc = (4 * (5 * R + 16 * R) + 2 * 32 * r.nvb + 15) / 16 * 16;
-    const int fixed = q + misc + 256 + 128;
+    const int fixed = q + misc + 256 + 192;
     auto warp_bytes = [&](int stages) { return stages * (stage + p.scale_bytes) + 16 * kChunk; };
     // two stages at least; two CTAs per SM where they and the registers allow it
     r.warps = 8;
@@ -804,7 +804,7 @@ RowsLaunch plan_rows(const KvGeom& geo, int64_t T, int64_t group) {
     p.q_off = p.s_off + r.warps * (p.stages * p.scale_bytes + 16 * kChunk);
     p.misc_off = p.q_off + q;
     p.bar_off = p.misc_off + misc;
-    p.smem = p.bar_off + 256 + 128;
+    p.smem = p.bar_off + 256 + 192;
     p.min_chunks = 8;
     r.wide = ks.bits[0] == 4 && vs.bits[0] == 4 && ks.bits[1] == 8 && vs.bits[1] == 8;
     return r;

@@ -27,7 +27,7 @@ struct Split {
     uint32_t n_cta, per, more, pos, hi, lo, base, mult;
     int entry;
 
-    // shared: 16 words.  Every thread of the CTA calls it; false: this CTA has
+    // shared: 32 words (at most 30 warps).  Every thread of the CTA calls it; false: this CTA has
     // nothing to do.  chunks(e) is 0 for an entry without work.
     template <typename F>
     __device__ __forceinline__ bool begin(F chunks, int n_entries, uint32_t mult_, uint32_t min_chunks, uint32_t slack,
@@ -78,8 +78,8 @@ struct Split {
                 part_chunks = want;
                 n_cta = units;
                 if (u0 <= blockIdx.x && blockIdx.x < u0 + mine_units) {
-                    shared[14] = tid;
-                    shared[15] = u0;
+                    shared[30] = tid;
+                    shared[31] = u0;
                 }
             }
         }
@@ -102,16 +102,16 @@ struct Split {
                 }
                 const uint32_t at = (run + before) * mult;
                 if (mine > 0 && at <= lo && lo < at + mine * mult) {
-                    shared[14] = e0 + tid;
-                    shared[15] = at;
+                    shared[30] = e0 + tid;
+                    shared[31] = at;
                 }
                 run += all;
             }
         }
         if (blockIdx.x >= n_cta) return false;
         __syncthreads();
-        entry = (int)shared[14];
-        base = shared[15];
+        entry = (int)shared[30];
+        base = shared[31];
         pos = lo;
         return true;
     }

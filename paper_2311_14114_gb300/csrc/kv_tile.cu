@@ -5,13 +5,14 @@
 //
 // With 128 rows to a tile the products (4 x 64 x 128 x 128 multiply-adds per 64
 // tokens at 128 channels) and the exponentials are the work; the cache's bytes
-// are read once per tile of up to 256 rows.  One CTA per SM, 16 warps:
-//   warp 0          issues the MMAs;  warp 1  copies packed rows by TMA;
-//   warps 4-7       unpack a block of 64 tokens into fp16 operand tiles (codes
-//                   exactly, scales as fp32 beside them);
-//   warps 8-11, 12-15  softmax of two row tiles (a thread per row, its scores from
+// are read once per tile of up to 256 rows.  One CTA per SM, 20 warps:
+//   warps 0, 3      issue the MMAs, each for one softmax group;
+//   warp 1          copies packed rows by TMA;
+//   warps 4-7, 8-11 unpack a block of 64 tokens' keys, and values, into fp16
+//                   operand tiles (codes exactly, scales as fp32 beside them);
+//   warps 12-15, 16-19  softmax of two row tiles (a thread per row, its scores from
 //                   TMEM), each with its own S, P and O columns.
-// (Registers move to the softmax warps: 2 x 184 + 72 + 72 = 4 x 128 a thread.)
+// (Registers move to the softmax warps: 64 + 2 x 56 + 2 x 152 = 5 x 96 a thread.)
 // While one tile's softmax runs, the tensor cores work for the other.  With at
 // most 128 rows both softmax groups serve the same tile on alternate blocks,
 // as two streams joined at the end.
@@ -36,7 +37,7 @@ namespace soniq {
 namespace {
 
 constexpr int kTok = 64;                 // tokens of a block
-constexpr int kThreads = 512;
+constexpr int kThreads = 640;
 constexpr int kAtom = kTok * 128;        // bytes of a 64-code column group of a K or V tile
 constexpr int kQAtom = 128 * 128;        // ... of a query tile
 constexpr int kSlotCols = 256;           // TMEM columns of a softmax group: S (and P over it), then O
@@ -51,7 +52,7 @@ struct TilePlan {
     int row_units;          // CTA-sized tiles of rows per key head
     int k_atoms, v_atoms, v_atom1;   // column groups; v_atom1: the second precision group's first
     int o_cols;
-    int stages, raw_stages;
+    int stages, raw_stages, buffers;
     int stage_bytes, raw_bytes, raw_v, raw_s;     // raw_s: scales, 128 bytes or more for each copy
     int box_rows, scale_step[2];
     int ring_off, raw_off, misc_off, smem;
@@ -60,8 +61,8 @@ struct TilePlan {
 };
 
 struct Bars {               // offsets in 8-byte barriers
-    static constexpr int raw_full = 0, raw_free = 4, k_ready = 8, v_ready = 12, kv_free = 16, s_full = 20, p_full = 22,
-                         o_full = 24, q_full = 26, drain = 27;
+    static constexpr int raw_full = 0, raw_free = 4, k_ready = 8, v_ready = 12, kv_free = 16, s_full = 20, p_full = 24,
+                         pv_done = 26, o_full = 28, q_full = 30, drain = 31;      // s_full: [group][buffer]
 };
 
 __device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
@@ -194,6 +195,34 @@ struct Ring {
     }
 };
 
+// Wait of a whole warp for phase `parity` of `bar`, with one result for its lanes
+// and little code (every role waits in several places, and what all roles run
+// has to stay in the instruction cache): false once the CTA gives up, or after
+// kWaitTries attempts (seconds).
+constexpr uint32_t kWaitTries = 1u << 24;
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, uint32_t abort_flag, unsigned* err) {
+    for (uint32_t i = 1;; ++i) {
+        uint32_t done;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (__all_sync(0xffffffffu, done)) return true;
+        if ((i & 255u) == 0) {
+            if (__any_sync(0xffffffffu, tc::abort_raised(abort_flag))) return false;
+            if (i >= kWaitTries) {
+                tc::set_flag(abort_flag, 1);
+                atomicOr(err, kErrWait);
+                return false;
+            }
+        }
+    }
+}
+
+// KNG, VNG: precision groups of keys and values.  SB: buffers of scores (2 where
+// TMEM has room: the next block's scores are there when this one's softmax ends).
+template <int KNG, int VNG, int SB>
 __global__ void __launch_bounds__(kThreads, 1)
     kv_tile_kernel(const KvGeom geo, const KvAttendArgs a, const TilePlan pl, const __grid_constant__ KvMaps maps) {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -204,11 +233,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t ring = smem0 + pl.ring_off, raw = smem0 + pl.raw_off;
     uint8_t* misc = smem + pl.misc_off;
     const uint32_t bars = smem0 + pl.misc_off;
-    uint32_t* words = reinterpret_cast<uint32_t*>(misc + 256);       // [16] for the split, then:
-    const uint32_t abort_flag = tc::smem_u32(words + 16);
-    uint32_t* tmem_at = words + 17;
-    uint32_t* sm_last = words + 18;
-    int* sm_e = reinterpret_cast<int*>(words + 20);                  // [4 stages][2]: power of two above the value scales
+    uint32_t* words = reinterpret_cast<uint32_t*>(misc + 256);       // [32] for the split, then:
+    const uint32_t abort_flag = tc::smem_u32(words + 32);
+    uint32_t* tmem_at = words + 33;
+    uint32_t* sm_last = words + 34;
+    int* sm_e = reinterpret_cast<int*>(words + 36);                  // [4 stages][2]: power of two above the value scales
     float* sm_fac = reinterpret_cast<float*>(misc + 512);            // [256] factor of a row's scores
     float* sm_m = sm_fac + 256;                                      // [128], of the second stream
     float* sm_l = sm_m + 128;
@@ -222,19 +251,20 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (tid == 0) {
         for (int i = 0; i < 4; ++i) {
             tc::mbar_init(bar(Bars::raw_full + i), 1);
-            tc::mbar_init(bar(Bars::raw_free + i), 4);
+            tc::mbar_init(bar(Bars::raw_free + i), 8);
             tc::mbar_init(bar(Bars::k_ready + i), 4);
             tc::mbar_init(bar(Bars::v_ready + i), 4);
-            tc::mbar_init(bar(Bars::kv_free + i), 1);
+            tc::mbar_init(bar(Bars::kv_free + i), pl.tiles);
+            tc::mbar_init(bar(Bars::s_full + i), 1);
         }
         for (int i = 0; i < 2; ++i) {
-            tc::mbar_init(bar(Bars::s_full + i), 1);
+            tc::mbar_init(bar(Bars::pv_done + i), 1);
             tc::mbar_init(bar(Bars::p_full + i), 4);
             tc::mbar_init(bar(Bars::o_full + i), 1);
         }
         tc::mbar_init(bar(Bars::q_full), 8);
-        tc::mbar_init(bar(Bars::drain), 1);
-        words[16] = 0;
+        tc::mbar_init(bar(Bars::drain), 2);
+        words[32] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
 
@@ -263,18 +293,18 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncthreads();
     tc::tc_fence_after();
     const uint32_t tmem = *tmem_at;
-    const uint32_t p1_off = kTok;            // the second value group's weights, behind the first scores
-    const uint32_t o_off = s_cols(ks.ng, vs.ng);     // O's first column in a slot
+    constexpr uint32_t p1_off = kTok;            // the second value group's weights, behind the first scores
+    constexpr uint32_t o_off = SB * s_cols(KNG, VNG);     // O's first column in a slot
     const int nkb = ks.nb[0] + ks.nb[1];
     const int pa0 = 32 * ks.nb[0], pa1 = 32 * ks.nb[1], va0 = 32 * vs.nb[0], va1 = 32 * vs.nb[1];
 
     auto wait = [&](int i, uint32_t parity) {
-        return tc::wait_bounded_warp(bar(i), parity & 1u, abort_flag, kWaitNs, a.err, kErrWait);
+        return wait_warp(bar(i), parity & 1u, abort_flag, a.err);
     };
     // where the next segment's blocks begin in the rings; parities of the softmax groups'
-    // barriers (bit s) and of their results', and of the queries'
+    // scores, weights and results (bit s), and of the queries'
     Ring kv0, raw0;
-    uint32_t s_phase = 0, o_phase = 0, q_phase = 0;
+    uint32_t s_phase = 0, p_phase = 0, o_phase = 0, q_phase = 0;      // s: bit 2 group + buffer
     bool ok = true, checked = false;
 
     const Segment first = split.segment(chunks);
@@ -320,93 +350,101 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
             }
-        } else if (ROLE == 2 && warp == 0) {
-            // ---- MMAs ----
+        } else if (ROLE == 2 && (warp == 0 || warp == 3)) {
+            // ---- MMAs of softmax group s ----
+            const int s = warp == 0 ? 0 : 1, step = streams ? 2 : 1;
+            const int mine = s < groups ? (streams ? (nblk - s + 1) / 2 : nblk) : 0;
             constexpr uint32_t fmt = (1u << 4) | ((128u >> 4) << 24);
             const uint32_t id_s = fmt | ((kTok >> 3) << 17);
             const uint32_t id_o0 = fmt | (1u << 16) | ((uint32_t)(va0 >> 3) << 17), id_o1 = fmt | (1u << 16) | ((uint32_t)(va1 >> 3) << 17);
-            // Every lane runs the loops, the elected one issues: descriptors stay in uniform registers.
+            const uint32_t t_s = tmem + s * kSlotCols;
+            const uint64_t q_tile = tc::sw128_desc(smem0 + (streams ? 0 : s * pl.k_atoms * kQAtom));
+            // every lane runs the loops, the elected one issues
             const bool leader = tc::elect_one();
-            auto scores = [&](int s, int st) {
-                const uint64_t q0 = tc::sw128_desc(smem0 + (streams ? 0 : s * pl.k_atoms * kQAtom));
-                const uint64_t k0 = tc::sw128_desc(ring + st * pl.stage_bytes);
-                const uint32_t d = tmem + s * kSlotCols;
+            auto scores = [&](int st, int buf) {
+                uint64_t q = q_tile, k = tc::sw128_desc(ring + st * pl.stage_bytes);
+                const uint32_t d = t_s + buf * s_cols(KNG, VNG);
                 // 32-code halves of column groups, two MMAs each
 #pragma unroll 1
                 for (int h = 0; h < nkb; ++h) {
-                    const uint64_t q = q0 + (h >> 1) * (kQAtom >> 4) + (h & 1) * 4, k = k0 + (h >> 1) * (kAtom >> 4) + (h & 1) * 4;
-                    const bool second = h >= ks.nb[0];
-                    const uint32_t to = d + (second ? kTok : 0);
+                    const bool second = KNG == 2 && h >= ks.nb[0];
                     if (leader) {
-                        mma_ss(to, q, k, id_s, h != 0 && h != ks.nb[0]);
-                        mma_ss(to, q + 2, k + 2, id_s, 1);
+                        mma_ss(d + (second ? kTok : 0), q, k, id_s, h != 0 && (KNG == 1 || h != ks.nb[0]));
+                        mma_ss(d + (second ? kTok : 0), q + 2, k + 2, id_s, 1);
                     }
+                    q += h & 1 ? (kQAtom - 64) >> 4 : 4;
+                    k += h & 1 ? (kAtom - 64) >> 4 : 4;
                 }
-                if (leader) tc::mma_commit(bar(Bars::s_full + s));
-                __syncwarp();
-            };
-            auto outputs = [&](int s, int st, bool first, bool frees, bool last) {
-                const uint64_t v = value_desc(ring + st * pl.stage_bytes + pl.k_atoms * kAtom);
-                const uint32_t p = tmem + s * kSlotCols, d = p + o_off;
-                auto group = [&](uint32_t to, uint32_t from, uint64_t v, uint32_t id) {
-                    if (leader) {
-                        mma_ts(to, from, v, id, !first);
-#pragma unroll
-                        for (int k = 1; k < kTok / 16; ++k) mma_ts(to, from + 8 * k, v + k * (2048 >> 4), id, 1);
-                    }
-                };
-                group(d, p, v, id_o0);
-                if (vs.ng == 2) group(d + va0, p + p1_off, v + pl.v_atom1 * (kAtom >> 4), id_o1);
-                if (leader) {
-                    if (frees) tc::mma_commit(bar(Bars::kv_free + st));
-                    if (last) tc::mma_commit(bar(Bars::o_full + s));
-                }
+                if (leader) tc::mma_commit(bar(Bars::s_full + 2 * s + buf));
                 __syncwarp();
             };
             auto ready = [&](int which, const Ring& at) {
                 ok = ok && wait(which + at.i, at.phase);
                 tc::tc_fence_after();
             };
-            ok = wait(Bars::q_full, q_phase);
+            if (mine > 0) ok = wait(Bars::q_full, q_phase);
             tc::tc_fence_after();
             Ring now = kv0, next = kv0;       // the block whose outputs, and whose scores, come next
-            for (int s = 0; ok && s < groups; ++s) {
+            if (streams && s == 1) now.step(pl.stages), next.step(pl.stages);
+            auto advance = [&](Ring& r) {
+                r.step(pl.stages);
+                if (step == 2) r.step(pl.stages);
+            };
+            for (int i = 0; ok && i < min(SB, mine); ++i) {
                 ready(Bars::k_ready, next);
-                if (ok) scores(s, next.i);
-                if (streams) next.step(pl.stages);
+                if (ok) scores(next.i, i);
+                advance(next);
             }
-            if (!streams) next.step(pl.stages);
-            uint32_t phase = s_phase;
-            for (int j = 0; ok && j < nblk; ++j) {
-                const int s_begin = streams ? j & 1 : 0, s_end = streams ? s_begin + 1 : groups;
-                const bool more = j + (streams ? 2 : 1) < nblk, first = j < (streams ? 2 : 1);
-                for (int s = s_begin; ok && s < s_end; ++s) {
-                    ready(Bars::v_ready, now);
-                    ok = ok && wait(Bars::p_full + s, phase >> s);
-                    if (!ok) break;
-                    tc::tc_fence_after();
-                    phase ^= 1u << s;
-                    outputs(s, now.i, first, s == s_end - 1, !more);
-                    if (more) {
-                        ready(Bars::k_ready, next);
-                        if (ok) scores(s, next.i);
+            uint32_t phase = p_phase >> s;
+            for (int i = 0; ok && i < mine; ++i) {
+                const int buf = SB == 2 ? i & 1 : 0;
+                ready(Bars::v_ready, now);
+                ok = ok && wait(Bars::p_full + s, phase);
+                if (!ok) break;
+                tc::tc_fence_after();
+                phase ^= 1u;
+                {
+                    const uint64_t v = value_desc(ring + now.i * pl.stage_bytes + pl.k_atoms * kAtom);
+                    const uint32_t p = t_s + buf * s_cols(KNG, VNG), d = t_s + o_off;
+                    if (leader) {
+                        mma_ts(d, p, v, id_o0, i != 0);
+#pragma unroll
+                        for (int k = 1; k < kTok / 16; ++k) mma_ts(d, p + 8 * k, v + k * (2048 >> 4), id_o0, 1);
+                        if (VNG == 2) {
+                            const uint64_t v1 = v + pl.v_atom1 * (kAtom >> 4);
+                            mma_ts(d + va0, p + p1_off, v1, id_o1, i != 0);
+#pragma unroll
+                            for (int k = 1; k < kTok / 16; ++k) mma_ts(d + va0, p + p1_off + 8 * k, v1 + k * (2048 >> 4), id_o1, 1);
+                        }
+                        tc::mma_commit(bar(Bars::kv_free + now.i));
+                        if (!streams && groups == 1) tc::mma_commit(bar(Bars::kv_free + now.i));     // for the group without rows
+                        if (SB == 2) tc::mma_commit(bar(Bars::pv_done + s));
+                        if (i == mine - 1) tc::mma_commit(bar(Bars::o_full + s));
                     }
+                    __syncwarp();
                 }
-                now.step(pl.stages);
-                next.step(pl.stages);
+                advance(now);
+                if (i + SB < mine) {
+                    ready(Bars::k_ready, next);
+                    if (ok) scores(next.i, buf);
+                    advance(next);
+                }
             }
         } else if (ROLE == 2 && warp == 2) {
             // ---- the segment after this one ----
             const bool more = split.next(seg);
             if (more) *sm_seg = split.segment(chunks);
             *sm_more = more;
-        } else if (ROLE == 2 && warp == 3) {
             if (!checked) check_lengths(geo, a, lane, 32);
             checked = true;
         } else if constexpr (ROLE == 1) {
-            // ---- packed rows -> operand tiles ----
-            const int dw = warp - 4, tok = (dw & 1) * 32 + lane;
+            // ---- packed rows -> operand tiles: keys by one warpgroup, values by the other ----
+            const int side = warp >= 8 ? 1 : 0, dw = warp & 3, tok = (dw & 1) * 32 + lane;
+            const KvSide& sd = geo.s[side];
             const Offsets f;
+            const uint32_t raw_sw = sd.row_bytes == 64 ? ((tok >> 1) & 3) << 4 : (sd.row_bytes == 128 ? (tok & 7) << 4 : 0);
+            const uint32_t sc_at = pl.raw_s + (side ? kTok / pl.box_rows * pl.scale_step[0] : 0);
+            const int ng = side ? VNG : KNG;
             Ring kv = kv0, rw = raw0;
             for (int j = 0; ok && j < nblk; ++j, kv.step(pl.stages), rw.step(pl.raw_stages)) {
                 const int st = kv.i, r = rw.i;
@@ -414,20 +452,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const uint32_t at = ring + st * pl.stage_bytes, src = raw + r * pl.raw_bytes;
                 ok = wait(Bars::kv_free + st, kv.phase ^ 1u) && wait(Bars::raw_full + r, rw.phase);
                 if (!ok) break;
-                // scales as fp32: keys' by warps 0 and 1 (with 2^-(n-1)), values' by 2 and 3, relative to a power of two
-                {
-                    const int side = dw >> 1;
-                    const KvSide& sd = side ? vs : ks;
-                    const uint32_t sc = src + pl.raw_s + (side ? kTok / pl.box_rows * pl.scale_step[0] : 0);
+                // scales as fp32: keys' with 2^-(n-1), values' relative to a power of two
+                if (dw < 2) {
                     const uint32_t to = at + (pl.k_atoms + pl.v_atoms) * kAtom + side * 512;
                     float x[2][2];        // [this token, the other half's][group]
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int t = h ? tok ^ 32 : tok;
-                        const uint32_t e = sc + (t / pl.box_rows) * pl.scale_step[side] + 2 * sd.ng * (t % pl.box_rows);
+                        const uint32_t e = src + sc_at + (t / pl.box_rows) * pl.scale_step[side] + 2 * ng * (t % pl.box_rows);
                         const bool in = p0 + t < end;
                         x[h][0] = in ? scale_of(lds16(e), bf16) : 0.0f;
-                        x[h][1] = in && sd.ng == 2 ? scale_of(lds16(e + 2), bf16) : 0.0f;
+                        x[h][1] = in && ng == 2 ? scale_of(lds16(e + 2), bf16) : 0.0f;
                     }
                     float f0 = pow2(1 - sd.bits[0]), f1 = pow2(1 - sd.bits[1]);
                     if (side) {
@@ -436,42 +471,38 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const int e0 = min(max((int)(big0 >> 23) - 126, -100), 126), e1 = min(max((int)(big1 >> 23) - 126, -100), 126);
                         f0 = pow2(-e0);
                         f1 = pow2(-e1);
-                        if (dw == 2 && lane == 0) {
+                        if (dw == 0 && lane == 0) {
                             sm_e[2 * st] = e0;
                             sm_e[2 * st + 1] = e1;
                         }
                     }
                     asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 4 * tok), "f"(x[0][0] * f0) : "memory");
-                    if (sd.ng == 2) asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 256 + 4 * tok), "f"(x[0][1] * f1) : "memory");
+                    if (ng == 2) asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 256 + 4 * tok), "f"(x[0][1] * f1) : "memory");
                 }
-#pragma unroll
-                for (int side = 0; side < 2; ++side) {
-                    const KvSide& sd = side ? vs : ks;
-                    const uint32_t base = src + (side ? pl.raw_v : 0) + tok * sd.row_bytes;
-                    const uint32_t to = at + (side ? pl.k_atoms * kAtom : 0) + tok * 128;
-                    const uint32_t raw_sw = sd.row_bytes == 64 ? ((tok >> 1) & 3) << 4 : (sd.row_bytes == 128 ? (tok & 7) << 4 : 0);
-                    // a lane takes a token, two warps every second block
-                    for (int blk = dw >> 1; blk < sd.nb[0] + sd.nb[1]; blk += 2) {
-                        const int grp = blk < sd.nb[0] ? 0 : 1, bb = grp ? blk - sd.nb[0] : blk, bits = sd.bits[grp];
-                        const uint32_t byte = sd.off[grp] + 4 * bits * bb;
-                        // keys' groups follow each other, values' start a column group each
-                        const int col = side && grp ? 64 * pl.v_atom1 + 32 * bb : 32 * blk;
-                        const uint32_t row = to + (col >> 6) * kAtom, p0 = (col >> 3) & 7;
-                        if (bits == 4) unpack_block<4>(base, byte, raw_sw, row, p0, tok & 7, f);
-                        else if (bits == 8) unpack_block<8>(base, byte, raw_sw, row, p0, tok & 7, f);
-                        else unpack_block<2>(base, byte, raw_sw, row, p0, tok & 7, f);
-                    }
-                    tc::fence_proxy_async_shared();
-                    __syncwarp();
-                    if (lane == 0) {
-                        tc::mbar_arrive(bar((side ? Bars::v_ready : Bars::k_ready) + st));
-                        if (side) tc::mbar_arrive(bar(Bars::raw_free + r));
-                    }
+                // a lane takes a token, two warps every second block
+                const uint32_t base = src + (side ? pl.raw_v : 0) + tok * sd.row_bytes;
+                const uint32_t to = at + (side ? pl.k_atoms * kAtom : 0) + tok * 128;
+#pragma unroll 1
+                for (int blk = dw >> 1; blk < sd.nb[0] + sd.nb[1]; blk += 2) {
+                    const int grp = blk < sd.nb[0] ? 0 : 1, bb = grp ? blk - sd.nb[0] : blk, bits = sd.bits[grp];
+                    const uint32_t byte = sd.off[grp] + 4 * bits * bb;
+                    // keys' groups follow each other, values' start a column group each
+                    const int col = side && grp ? 64 * pl.v_atom1 + 32 * bb : 32 * blk;
+                    const uint32_t row = to + (col >> 6) * kAtom, p0 = (col >> 3) & 7;
+                    if (bits == 4) unpack_block<4>(base, byte, raw_sw, row, p0, tok & 7, f);
+                    else if (bits == 8) unpack_block<8>(base, byte, raw_sw, row, p0, tok & 7, f);
+                    else unpack_block<2>(base, byte, raw_sw, row, p0, tok & 7, f);
+                }
+                tc::fence_proxy_async_shared();
+                __syncwarp();
+                if (lane == 0) {
+                    tc::mbar_arrive(bar((side ? Bars::v_ready : Bars::k_ready) + st));
+                    tc::mbar_arrive(bar(Bars::raw_free + r));
                 }
             }
         } else if constexpr (ROLE == 0) {
             // ---- softmax ----
-            const int s = (warp >> 2) - 2, quad = warp & 3, st_id = tid - 256;
+            const int s = (warp >> 2) - 3, quad = warp & 3, st_id = tid - 384;
             // queries: fp16, each row scaled to 2^13; a lane takes four channels (of 128) of a row
             {
                 const int total = groups == 2 && !streams ? 256 : 128, cols = pa0 + pa1;
@@ -484,7 +515,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     sm_chan[c] = code < vs.count[grp] ? (int16_t)__ldg(vs.perm + head * vs.D + (grp ? vs.count[0] : 0) + code) : (int16_t)-1;
                     sm_back[c] = pow2(1 - vs.bits[grp] - place_log2(vs.bits[grp], (c & 7) >> 1));
                 }
-                const int r_first = (warp - 8) * (total / 8), r_end = r_first + total / 8;
+                const int r_first = (warp - 12) * (total / 8), r_end = r_first + total / 8;
                 if (cols != ks.D) {      // columns without a channel
                     for (int i = lane; i < (r_end - r_first) * 8 * pl.k_atoms; i += 32) {
                         const int r = r_first + (i & (total / 8 - 1)), p = i / (total / 8);
@@ -506,41 +537,44 @@ __global__ void __launch_bounds__(kThreads, 1)
                         to[k] = (col >> 6) * kQAtom + ((col & 63) >> 3) * 16 + 2 * (col & 7);
                         down[k] = sign * pow2(-place_log2(bits, (col & 7) >> 1));
                     }
-                    // eight rows' loads go out while the eight before are scaled and stored
-                    int t = (row0 + r_first) / a.group, hq = (row0 + r_first) % a.group, next_row = row0 + r_first;
                     const uint16_t* q0 = a.Q + b * a.q_seq_stride + (int64_t)head * a.group * a.q_head_stride;
-                    auto load = [&](uint2(&v)[8][H]) {
+                    // four rows' loads go out while the four before are scaled and stored
+                    auto load = [&](int r, uint2(&v)[4][H]) {
+                        int t = (row0 + r) / a.group, hq = (row0 + r) % a.group;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
+                        for (int i = 0; i < 4; ++i) {
                             const uint16_t* q = q0 + t * a.q_token_stride + hq * a.q_head_stride;
+                            const bool on = row0 + r + i < pl.rows;
 #pragma unroll
                             for (int h = 0; h < H; ++h) {
                                 const int ch = 128 * h + 4 * lane;
                                 v[i][h] = make_uint2(0, 0);
-                                if (next_row < pl.rows && ch < ks.D) {
-                                    if (wide) {
-                                        v[i][h] = *reinterpret_cast<const uint2*>(q + ch);
-                                    } else {
-                                        v[i][h].x = q[ch] | (ch + 1 < ks.D ? (uint32_t)q[ch + 1] << 16 : 0u);
-                                        v[i][h].y = (ch + 2 < ks.D ? q[ch + 2] : 0u) | (ch + 3 < ks.D ? (uint32_t)q[ch + 3] << 16 : 0u);
-                                    }
+                                if (wide && on && ch < ks.D) v[i][h] = *reinterpret_cast<const uint2*>(q + ch);
+                            }
+                            if (!wide && on) {
+#pragma unroll
+                                for (int k = 0; k < 4 * H; ++k) {
+                                    const int ch = 128 * (k >> 2) + 4 * lane + (k & 3);
+                                    const uint32_t x = ch < ks.D ? (uint32_t)q[ch] << (16 * (k & 1)) : 0u;
+                                    if (k & 2) v[i][k >> 2].y |= x;
+                                    else v[i][k >> 2].x |= x;
                                 }
                             }
-                            ++next_row;
                             if (++hq == a.group) hq = 0, ++t;
                         }
                     };
-                    uint2 v[8][H];
-                    load(v);
-                    for (int r0 = r_first; r0 < r_end; r0 += 8) {
-                        uint2 w[8][H];
+                    uint2 v[4][H];
+                    load(r_first, v);
+#pragma unroll 1
+                    for (int r0 = r_first; r0 < r_end; r0 += 4) {
+                        uint2 w[4][H];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
+                        for (int i = 0; i < 4; ++i)
 #pragma unroll
                             for (int h = 0; h < H; ++h) w[i][h] = v[i][h];
-                        if (r0 + 8 < r_end) load(v);
+                        if (r0 + 4 < r_end) load(r0 + 4, v);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
+                        for (int i = 0; i < 4; ++i) {
                             const int r = r0 + i;
                             float x[4 * H];
                             uint32_t top = 0;
@@ -584,14 +618,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int sure = min(len, end);
             Ring kv = kv0;
             if (streams && s == 1) kv.step(pl.stages);
-            uint32_t phase = s_phase >> s;
+            uint32_t phases = s_phase >> (2 * s), done = p_phase >> s;      // of the score buffers, and of the block's MMAs
             for (int i = 0; ok && i < mine; ++i) {
-                const int j = streams ? 2 * i + s : i, st = kv.i;
+                const int j = streams ? 2 * i + s : i, st = kv.i, buf = SB == 2 ? i & 1 : 0;
                 const int p0 = (seg.c_first + j) * kTok;
                 const uint32_t sc = ring + st * pl.stage_bytes + (pl.k_atoms + pl.v_atoms) * kAtom;
-                ok = wait(Bars::k_ready + st, kv.phase) && wait(Bars::s_full + s, phase);
+                ok = wait(Bars::k_ready + st, kv.phase) && wait(Bars::v_ready + st, kv.phase) && wait(Bars::s_full + 2 * s + buf, phases >> buf);
                 if (!ok) break;
-                phase ^= 1u;
+                phases ^= 1u << buf;
+                const uint32_t t_b = t_s + buf * s_cols(KNG, VNG);
                 kv.step(pl.stages);
                 if (streams) kv.step(pl.stages);
                 tc::tc_fence_after();
@@ -600,15 +635,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const bool tail = p0 + kTok > sure;
                 auto scores = [&](int h, float2(&x)[16]) {
                     uint32_t v[32];
-                    tmem_ld32(t_s + 32 * h, v);
+                    tmem_ld32(t_b + 32 * h, v);
 #pragma unroll
                     for (int k = 0; k < 16; k += 2) {
                         const float4 kk = lds128f(sc + 128 * h + 8 * k);
                         x[k] = mul2(make_float2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), make_float2(kk.x, kk.y));
                         x[k + 1] = mul2(make_float2(__uint_as_float(v[2 * k + 2]), __uint_as_float(v[2 * k + 3])), make_float2(kk.z, kk.w));
                     }
-                    if (ks.ng == 2) {
-                        tmem_ld32(t_s + kTok + 32 * h, v);
+                    if (KNG == 2) {
+                        tmem_ld32(t_b + kTok + 32 * h, v);
 #pragma unroll
                         for (int k = 0; k < 16; k += 2) {
                             const float4 kk = lds128f(sc + 256 + 128 * h + 8 * k);
@@ -656,7 +691,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                         l *= al;
                     }
                     const float al0 = al * (n0 - e0 > 126 ? 0.0f : pow2(e0 - n0)), al1 = al * (n1 - e1 > 126 ? 0.0f : pow2(e1 - n1));
-                    // the MMAs that wrote O are complete: they came before the ones that wrote these scores
+                    // The MMAs that wrote O have to be complete: with one buffer they came before those that wrote
+                    // these scores.
+                    if (SB == 2) {
+                        ok = wait(Bars::pv_done + s, done ^ 1u);
+                        if (!ok) break;
+                        tc::tc_fence_after();
+                    }
 #pragma unroll 1
                     for (int c = 0; c < pl.o_cols; c += 32) {
                         uint32_t v[32];
@@ -692,8 +733,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                         w[k] = pack2(y0.x, y0.y);
                         w[k + 1] = pack2(y1.x, y1.y);
                     }
-                    tmem_st16v(t_s + 16 * h, w);
-                    if (vs.ng == 2) {
+                    tmem_st16v(t_b + 16 * h, w);
+                    if (VNG == 2) {
 #pragma unroll
                         for (int k = 0; k < 16; k += 2) {
                             const float4 vv = lds128f(sc + 768 + 128 * h + 8 * k);
@@ -701,13 +742,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                             w[k] = pack2(y0.x, y0.y);
                             w[k + 1] = pack2(y1.x, y1.y);
                         }
-                        tmem_st16v(t_s + p1_off + 16 * h, w);
+                        tmem_st16v(t_b + p1_off + 16 * h, w);
                     }
                 }
                 l += (sum.x + sum.y) * pow2(-d0);
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(bar(Bars::p_full + s));
+                done ^= 1u;
             }
             // ---- results: both groups' MMAs are complete, so queries' and operands' memory is free ----
             for (int g = 0; g < groups; ++g) ok = ok && wait(Bars::o_full + g, o_phase >> g);
@@ -719,12 +761,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (streams && s == 1) {
                 sm_m[r_tile] = mine > 0 ? m2 : -INFINITY;
                 sm_l[r_tile] = l;
-                for (int c = 0; ok && mine > 0 && c < pl.o_cols; c += 32) {
-                    uint32_t v[32];
-                    tmem_ld32(t_s + o_off + c, v);
+#pragma unroll 1
+                for (int c = 0; ok && mine > 0 && c < pl.o_cols; c += 8) {
+                    uint32_t v[8];
+                    tc::tmem_ld8(t_s + o_off + c, v);
                     const int e = c < va0 ? e0 : e1;
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) second[(c + k) * 128 + r_tile] = __uint_as_float(v[k]) * (sm_back[c + k] * pow2(e));
+                    for (int k = 0; k < 8; ++k) second[(c + k) * 128 + r_tile] = __uint_as_float(v[k]) * (sm_back[c + k] * pow2(e));
                 }
             }
             bar_group(1, 256);
@@ -745,23 +788,24 @@ __global__ void __launch_bounds__(kThreads, 1)
             };
             if (works && ok) {
                 const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);     // nothing seen: 0; NaN stays
-                for (int c = 0; c < pl.o_cols; c += 32) {
-                    uint32_t v[32];
-                    tmem_ld32(t_s + o_off + c, v);
+#pragma unroll 1
+                for (int c = 0; c < pl.o_cols; c += 8) {
+                    uint32_t v[8];
+                    tc::tmem_ld8(t_s + o_off + c, v);
                     const float f = keep * pow2(c < va0 ? e0 : e1);
-                    float x[32];
+                    float x[8];
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) {
+                    for (int k = 0; k < 8; ++k) {
                         x[k] = __uint_as_float(v[k]) * (sm_back[c + k] * f);
                         if (streams && groups == 2) x[k] = fmaf(second[(c + k) * 128 + r_tile], other, x[k]);
                     }
                     if (whole) {
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) stage_out(c + k, x[k] * inv);
+                        for (int k = 0; k < 8; ++k) stage_out(c + k, x[k] * inv);
                     } else {
                         float4* to = reinterpret_cast<float4*>(parts + seg.slot * part_floats) + (int64_t)(c / 4) * unit_rows + unit_row;
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) to[(int64_t)k * unit_rows] = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+                        to[0] = make_float4(x[0], x[1], x[2], x[3]);
+                        to[unit_rows] = make_float4(x[4], x[5], x[6], x[7]);
                     }
                 }
                 if (!whole) {
@@ -792,17 +836,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                         ll += __ldcg(stat(i) + unit_rows) * (mi == -INFINITY ? 0.0f : ex2(mi - mm));
                     }
                     const float inv = ll > 0.0f ? 1.0f / ll : (ll == 0.0f ? 0.0f : ll);
-                    for (int c = 0; c < pl.o_cols; c += 64) {
-                        float x[64] = {};
-                        const int cols = min(64, pl.o_cols - c);       // 32 or 64
+#pragma unroll 1
+                    for (int c = 0; c < pl.o_cols; c += 16) {
+                        float x[16] = {};
+#pragma unroll 4
                         for (int i = 0; i < seg.n_part; ++i) {
                             const float4* from = reinterpret_cast<const float4*>(parts + part_slot(seg, i) * part_floats) + (int64_t)(c / 4) * unit_rows + unit_row;
-                            float4 q[16];
+                            float4 q[4];
 #pragma unroll
-                            for (int k = 0; k < 16; ++k) q[k] = 4 * k < cols ? __ldcg(from + (int64_t)k * unit_rows) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                            for (int k = 0; k < 4; ++k) q[k] = __ldcg(from + (int64_t)k * unit_rows);
                             const float mi = __ldcg(stat(i)), f = mi == -INFINITY ? 0.0f : ex2(mi - mm);
 #pragma unroll
-                            for (int k = 0; k < 16; ++k) {
+                            for (int k = 0; k < 4; ++k) {
                                 x[4 * k] = fmaf(f, q[k].x, x[4 * k]);
                                 x[4 * k + 1] = fmaf(f, q[k].y, x[4 * k + 1]);
                                 x[4 * k + 2] = fmaf(f, q[k].z, x[4 * k + 2]);
@@ -810,8 +855,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             }
                         }
 #pragma unroll
-                        for (int k = 0; k < 64; ++k)
-                            if (k < cols) stage_out(c + k, x[k] * inv);
+                        for (int k = 0; k < 16; ++k) stage_out(c + k, x[k] * inv);
                     }
                 }
             }
@@ -835,9 +879,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         kv0.skip(nblk, pl.stages);
         raw0.skip(nblk, pl.raw_stages);
-        // each group's number of blocks, modulo 2
-        const uint32_t odd0 = (streams ? (nblk + 1) / 2 : nblk) & 1, odd1 = (streams ? nblk / 2 : (groups == 2 ? nblk : 0)) & 1;
-        s_phase ^= odd0 | odd1 << 1;
+        // each group's number of blocks, and of uses of its score buffers, modulo 2
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const uint32_t n = s < groups ? (streams ? (nblk - s + 1) / 2 : nblk) : 0;
+            p_phase ^= (n & 1u) << s;
+            if (SB == 2) s_phase ^= (((n + 1) / 2 & 1u) | (n / 2 & 1u) << 1) << (2 * s);
+            else s_phase ^= (n & 1u) << (2 * s);
+        }
         o_phase ^= groups == 2 ? 3u : 1u;
         q_phase ^= 1u;
         tc::tc_fence_before();
@@ -851,7 +900,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     while (!tc::mbar_try_wait(bar(Bars::raw_full + i), 0) && !tc::mbar_try_wait(bar(Bars::raw_full + i), 1) &&
                            tc::globaltimer() - t0 < kWaitNs) {
                     }
-            } else if (warp == 0) {
+            } else if (warp == 0 || warp == 3) {
                 if (tc::elect_one()) tc::mma_commit(bar(Bars::drain));
                 while (!tc::mbar_try_wait(bar(Bars::drain), 0) && tc::globaltimer() - t0 < kWaitNs) {
                 }
@@ -863,14 +912,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncthreads();      // read before it is overwritten
     }
     };
-    if (warp >= 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    if (warp >= 12) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
         work(std::integral_constant<int, 0>{});
     } else if (warp >= 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         work(std::integral_constant<int, 1>{});
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         work(std::integral_constant<int, 2>{});
     }
     __syncthreads();
@@ -918,6 +967,8 @@ TileLaunch plan_tile(const KvGeom& geo, int64_t T, int64_t group) {
         const int results = p.tiles == 2 ? 256 * p.out_stride : p.o_cols * 512 + 128 * p.out_stride;
         if (p.smem <= most && results <= p.raw_off) {
             t.fits = true;
+            // (two streams with two buffers each run up to three blocks ahead)
+            p.buffers = ks.ng == 1 && vs.ng == 1 && 2 * kTok + p.o_cols <= kSlotCols && p.stages >= (p.tiles == 2 ? 2 : 3) ? 2 : 1;
             break;
         }
     }
@@ -951,10 +1002,12 @@ cudaError_t launch_kv_tile(const KvGeom& geo, const KvAttendArgs& a, cudaStream_
         if (!encode_side(geo, geo.s[side], row, p.box_rows, swizzle, &maps.codes[side], &maps.scales[side]))
             return cudaErrorUnknown;
     }
-    cudaError_t e = cudaFuncSetAttribute(kv_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
-    if (e == cudaSuccess) e = prefer_max_shared(reinterpret_cast<const void*>(kv_tile_kernel));
+    auto* kernel = geo.s[0].ng == 1 ? (geo.s[1].ng == 1 ? (p.buffers == 2 ? kv_tile_kernel<1, 1, 2> : kv_tile_kernel<1, 1, 1>) : kv_tile_kernel<1, 2, 1>)
+                                    : (geo.s[1].ng == 1 ? kv_tile_kernel<2, 1, 1> : kv_tile_kernel<2, 2, 1>);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
+    if (e == cudaSuccess) e = prefer_max_shared(reinterpret_cast<const void*>(kernel));
     if (e != cudaSuccess) return e;
-    kv_tile_kernel<<<grid, kThreads, p.smem, st>>>(geo, a, p, maps);
+    kernel<<<grid, kThreads, p.smem, st>>>(geo, a, p, maps);
     note_launch();
     return cudaGetLastError();
 }
