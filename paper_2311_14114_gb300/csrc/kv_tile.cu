@@ -62,7 +62,7 @@ struct TilePlan {
 
 struct Bars {               // offsets in 8-byte barriers
     static constexpr int raw_full = 0, raw_free = 4, k_ready = 8, v_ready = 12, kv_free = 16, s_full = 20, p_full = 24,
-                         pv_done = 26, o_full = 28, q_full = 30, drain = 31;      // s_full: [group][buffer]
+                         pv_done = 28, o_full = 30, q_full = 32, drain = 33;      // s_full, p_full: [group][buffer]
 };
 
 __device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
@@ -195,27 +195,30 @@ struct Ring {
     }
 };
 
-// Wait of a whole warp for phase `parity` of `bar`, with one result for its lanes
-// and little code (every role waits in several places, and what all roles run
-// has to stay in the instruction cache): false once the CTA gives up, or after
-// kWaitTries attempts (seconds).
-constexpr uint32_t kWaitTries = 1u << 24;
+// Wait of a whole warp for phase `parity` of `bar`; one result for its lanes:
+// false once the CTA gives up, or when the wait is given up after 2 s.  (The
+// polling loop is written out: twenty warps' polls took a third of the issue
+// slots, and what all roles run has to stay in the instruction cache.)
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, uint32_t abort_flag, unsigned* err) {
-    for (uint32_t i = 1;; ++i) {
+    long long t0 = 0;
+    while (true) {
         uint32_t done;
         asm volatile(
-            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+            "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 4096;\n"
+            "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra DONE;\n\t"
+            "sub.u32 n, n, 1;\n\tsetp.ne.u32 q, n, 0;\n\t@q bra TRY;\n"
+            "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
             : "=r"(done)
             : "r"(bar), "r"(parity)
             : "memory");
         if (__all_sync(0xffffffffu, done)) return true;
-        if ((i & 255u) == 0) {
-            if (__any_sync(0xffffffffu, tc::abort_raised(abort_flag))) return false;
-            if (i >= kWaitTries) {
-                tc::set_flag(abort_flag, 1);
-                atomicOr(err, kErrWait);
-                return false;
-            }
+        if (__any_sync(0xffffffffu, tc::abort_raised(abort_flag))) return false;
+        const long long t = tc::globaltimer();
+        if (t0 == 0) t0 = t;
+        if (__any_sync(0xffffffffu, t - t0 > kWaitNs)) {
+            tc::set_flag(abort_flag, 1);
+            atomicOr(err, kErrWait);
+            return false;
         }
     }
 }
@@ -233,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t ring = smem0 + pl.ring_off, raw = smem0 + pl.raw_off;
     uint8_t* misc = smem + pl.misc_off;
     const uint32_t bars = smem0 + pl.misc_off;
-    uint32_t* words = reinterpret_cast<uint32_t*>(misc + 256);       // [32] for the split, then:
+    uint32_t* words = reinterpret_cast<uint32_t*>(misc + 320);       // [32] for the split, then:
     const uint32_t abort_flag = tc::smem_u32(words + 32);
     uint32_t* tmem_at = words + 33;
     uint32_t* sm_last = words + 34;
@@ -256,10 +259,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::mbar_init(bar(Bars::v_ready + i), 4);
             tc::mbar_init(bar(Bars::kv_free + i), pl.tiles);
             tc::mbar_init(bar(Bars::s_full + i), 1);
+            tc::mbar_init(bar(Bars::p_full + i), 4);
         }
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(bar(Bars::pv_done + i), 1);
-            tc::mbar_init(bar(Bars::p_full + i), 4);
             tc::mbar_init(bar(Bars::o_full + i), 1);
         }
         tc::mbar_init(bar(Bars::q_full), 8);
@@ -302,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         return wait_warp(bar(i), parity & 1u, abort_flag, a.err);
     };
     // where the next segment's blocks begin in the rings; parities of the softmax groups'
-    // scores, weights and results (bit s), and of the queries'
+    // scores and weights, blocks done and results (bit s), and of the queries'
     Ring kv0, raw0;
     uint32_t s_phase = 0, p_phase = 0, o_phase = 0, q_phase = 0;      // s: bit 2 group + buffer
     bool ok = true, checked = false;
@@ -395,14 +398,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (ok) scores(next.i, i);
                 advance(next);
             }
-            uint32_t phase = p_phase >> s;
+            uint32_t phases = s_phase >> (2 * s);      // of the weights in each buffer, as of the scores
             for (int i = 0; ok && i < mine; ++i) {
                 const int buf = SB == 2 ? i & 1 : 0;
                 ready(Bars::v_ready, now);
-                ok = ok && wait(Bars::p_full + s, phase);
+                ok = ok && wait(Bars::p_full + 2 * s + buf, phases >> buf);
                 if (!ok) break;
                 tc::tc_fence_after();
-                phase ^= 1u;
+                phases ^= 1u << buf;
                 {
                     const uint64_t v = value_desc(ring + now.i * pl.stage_bytes + pl.k_atoms * kAtom);
                     const uint32_t p = t_s + buf * s_cols(KNG, VNG), d = t_s + o_off;
@@ -634,21 +637,23 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // all roles' code in the instruction caches, which a block unrolled as a whole did not (5 us a block)
                 const bool tail = p0 + kTok > sure;
                 auto scores = [&](int h, float2(&x)[16]) {
-                    uint32_t v[32];
-                    tmem_ld32(t_b + 32 * h, v);
+                    uint32_t v[2][16];
+                    tc::tmem_ld16x2(t_b + 32 * h, t_b + 32 * h + 16, v[0], v[1]);
 #pragma unroll
                     for (int k = 0; k < 16; k += 2) {
                         const float4 kk = lds128f(sc + 128 * h + 8 * k);
-                        x[k] = mul2(make_float2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), make_float2(kk.x, kk.y));
-                        x[k + 1] = mul2(make_float2(__uint_as_float(v[2 * k + 2]), __uint_as_float(v[2 * k + 3])), make_float2(kk.z, kk.w));
+                        const uint32_t* y = &v[k >> 3][2 * k & 15];
+                        x[k] = mul2(make_float2(__uint_as_float(y[0]), __uint_as_float(y[1])), make_float2(kk.x, kk.y));
+                        x[k + 1] = mul2(make_float2(__uint_as_float(y[2]), __uint_as_float(y[3])), make_float2(kk.z, kk.w));
                     }
                     if (KNG == 2) {
-                        tmem_ld32(t_b + kTok + 32 * h, v);
+                        tc::tmem_ld16x2(t_b + kTok + 32 * h, t_b + kTok + 32 * h + 16, v[0], v[1]);
 #pragma unroll
                         for (int k = 0; k < 16; k += 2) {
                             const float4 kk = lds128f(sc + 256 + 128 * h + 8 * k);
-                            x[k] = fma2(make_float2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), make_float2(kk.x, kk.y), x[k]);
-                            x[k + 1] = fma2(make_float2(__uint_as_float(v[2 * k + 2]), __uint_as_float(v[2 * k + 3])), make_float2(kk.z, kk.w), x[k + 1]);
+                            const uint32_t* y = &v[k >> 3][2 * k & 15];
+                            x[k] = fma2(make_float2(__uint_as_float(y[0]), __uint_as_float(y[1])), make_float2(kk.x, kk.y), x[k]);
+                            x[k + 1] = fma2(make_float2(__uint_as_float(y[2]), __uint_as_float(y[3])), make_float2(kk.z, kk.w), x[k + 1]);
                         }
                     }
                     if (tail) {
@@ -748,7 +753,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 l += (sum.x + sum.y) * pow2(-d0);
                 tc::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) tc::mbar_arrive(bar(Bars::p_full + s));
+                // (by buffer: with two, a warp may be a block ahead of the others of its group)
+                if (lane == 0) tc::mbar_arrive(bar(Bars::p_full + 2 * s + buf));
                 done ^= 1u;
             }
             // ---- results: both groups' MMAs are complete, so queries' and operands' memory is free ----
