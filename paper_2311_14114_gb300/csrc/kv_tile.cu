@@ -327,6 +327,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             // ---- copies ----
             const int32_t* table = a.table + b * a.table_stride;
             Ring ring_r = raw0;
+#pragma unroll 1
             for (int j = 0; ok && j < nblk; ++j, ring_r.step(pl.raw_stages)) {
                 const int r = ring_r.i;
                 const int p0 = (seg.c_first + j) * kTok;
@@ -341,6 +342,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (a.drop && j == 0 && blockIdx.x == 0) continue;
                 const uint32_t at = raw + r * pl.raw_bytes, full = bar(Bars::raw_full + r);
                 if (tc::elect_one()) tc::mbar_arrive_expect_tx(full, boxes * pl.box_rows * (ks.row_bytes + vs.row_bytes + 2 * (ks.ng + vs.ng)));
+#pragma unroll 1
                 for (int i = 0; i < boxes; ++i) {
                     const int pg = __shfl_sync(0xffffffffu, page, i);
                     const int row = head * geo.page + ((p0 + i * pl.box_rows) & (geo.page - 1));
@@ -364,23 +366,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint64_t q_tile = tc::sw128_desc(smem0 + (streams ? 0 : s * pl.k_atoms * kQAtom));
             // every lane runs the loops, the elected one issues
             const bool leader = tc::elect_one();
-            auto scores = [&](int st, int buf) {
-                uint64_t q = q_tile, k = tc::sw128_desc(ring + st * pl.stage_bytes);
-                const uint32_t d = t_s + buf * s_cols(KNG, VNG);
-                // 32-code halves of column groups, two MMAs each
-#pragma unroll 1
-                for (int h = 0; h < nkb; ++h) {
-                    const bool second = KNG == 2 && h >= ks.nb[0];
-                    if (leader) {
-                        mma_ss(d + (second ? kTok : 0), q, k, id_s, h != 0 && (KNG == 1 || h != ks.nb[0]));
-                        mma_ss(d + (second ? kTok : 0), q + 2, k + 2, id_s, 1);
-                    }
-                    q += h & 1 ? (kQAtom - 64) >> 4 : 4;
-                    k += h & 1 ? (kAtom - 64) >> 4 : 4;
-                }
-                if (leader) tc::mma_commit(bar(Bars::s_full + 2 * s + buf));
-                __syncwarp();
-            };
             auto ready = [&](int which, const Ring& at) {
                 ok = ok && wait(which + at.i, at.phase);
                 tc::tc_fence_after();
@@ -393,43 +378,61 @@ __global__ void __launch_bounds__(kThreads, 1)
                 r.step(pl.stages);
                 if (step == 2) r.step(pl.stages);
             };
-            for (int i = 0; ok && i < min(SB, mine); ++i) {
-                ready(Bars::k_ready, next);
-                if (ok) scores(next.i, i);
-                advance(next);
-            }
             uint32_t phases = s_phase >> (2 * s);      // of the weights in each buffer, as of the scores
-            for (int i = 0; ok && i < mine; ++i) {
+            // scores run SB blocks ahead of the outputs
+#pragma unroll 1
+            for (int i = -SB; ok && i < mine; ++i) {
                 const int buf = SB == 2 ? i & 1 : 0;
-                ready(Bars::v_ready, now);
-                ok = ok && wait(Bars::p_full + 2 * s + buf, phases >> buf);
-                if (!ok) break;
-                tc::tc_fence_after();
-                phases ^= 1u << buf;
-                {
-                    const uint64_t v = value_desc(ring + now.i * pl.stage_bytes + pl.k_atoms * kAtom);
-                    const uint32_t p = t_s + buf * s_cols(KNG, VNG), d = t_s + o_off;
-                    if (leader) {
-                        mma_ts(d, p, v, id_o0, i != 0);
-#pragma unroll
-                        for (int k = 1; k < kTok / 16; ++k) mma_ts(d, p + 8 * k, v + k * (2048 >> 4), id_o0, 1);
-                        if (VNG == 2) {
-                            const uint64_t v1 = v + pl.v_atom1 * (kAtom >> 4);
-                            mma_ts(d + va0, p + p1_off, v1, id_o1, i != 0);
-#pragma unroll
-                            for (int k = 1; k < kTok / 16; ++k) mma_ts(d + va0, p + p1_off + 8 * k, v1 + k * (2048 >> 4), id_o1, 1);
+                if (i >= 0) {
+                    ready(Bars::v_ready, now);
+                    ok = ok && wait(Bars::p_full + 2 * s + buf, phases >> buf);
+                    if (!ok) break;
+                    tc::tc_fence_after();
+                    phases ^= 1u << buf;
+                    uint64_t v = value_desc(ring + now.i * pl.stage_bytes + pl.k_atoms * kAtom);
+                    uint32_t p = t_s + buf * s_cols(KNG, VNG);
+                    const uint32_t d = t_s + o_off;
+#pragma unroll 1
+                    for (int k = 0; k < kTok / 16; k += 2) {
+                        if (leader) {
+                            mma_ts(d, p, v, id_o0, i != 0 || k != 0);
+                            mma_ts(d, p + 8, v + (2048 >> 4), id_o0, 1);
+                            if (VNG == 2) {
+                                const uint64_t v1 = v + pl.v_atom1 * (kAtom >> 4);
+                                mma_ts(d + va0, p + p1_off, v1, id_o1, i != 0 || k != 0);
+                                mma_ts(d + va0, p + p1_off + 8, v1 + (2048 >> 4), id_o1, 1);
+                            }
                         }
+                        v += 2 * (2048 >> 4);
+                        p += 16;
+                    }
+                    if (leader) {
                         tc::mma_commit(bar(Bars::kv_free + now.i));
                         if (!streams && groups == 1) tc::mma_commit(bar(Bars::kv_free + now.i));     // for the group without rows
                         if (SB == 2) tc::mma_commit(bar(Bars::pv_done + s));
                         if (i == mine - 1) tc::mma_commit(bar(Bars::o_full + s));
                     }
                     __syncwarp();
+                    advance(now);
                 }
-                advance(now);
                 if (i + SB < mine) {
                     ready(Bars::k_ready, next);
-                    if (ok) scores(next.i, buf);
+                    if (!ok) break;
+                    uint64_t q = q_tile, k = tc::sw128_desc(ring + next.i * pl.stage_bytes);
+                    const uint32_t d = t_s + buf * s_cols(KNG, VNG);
+                    // 32-code halves of column groups, two MMAs each
+#pragma unroll 1
+                    for (int h = 0; h < nkb; ++h) {
+                        const bool second = KNG == 2 && h >= ks.nb[0];
+                        if (leader) {
+                            mma_ss(d + (second ? kTok : 0), q, k, id_s, h != 0 && (KNG == 1 || h != ks.nb[0]));
+                            mma_ss(d + (second ? kTok : 0), q + 2, k + 2, id_s, 1);
+                        }
+                        q += h & 1 ? (kQAtom - 64) >> 4 : 4;
+                        k += h & 1 ? (kAtom - 64) >> 4 : 4;
+                    }
+                    if (leader) tc::mma_commit(bar(Bars::s_full + 2 * s + buf));
+                    __syncwarp();
                     advance(next);
                 }
             }
@@ -449,6 +452,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t sc_at = pl.raw_s + (side ? kTok / pl.box_rows * pl.scale_step[0] : 0);
             const int ng = side ? VNG : KNG;
             Ring kv = kv0, rw = raw0;
+#pragma unroll 1
             for (int j = 0; ok && j < nblk; ++j, kv.step(pl.stages), rw.step(pl.raw_stages)) {
                 const int st = kv.i, r = rw.i;
                 const int p0 = (seg.c_first + j) * kTok;
@@ -633,18 +637,30 @@ __global__ void __launch_bounds__(kThreads, 1)
                 kv.step(pl.stages);
                 if (streams) kv.step(pl.stages);
                 tc::tc_fence_after();
-                // 32 tokens' scores at a time, read twice (for the maximum, for the weights): a short loop keeps
-                // all roles' code in the instruction caches, which a block unrolled as a whole did not (5 us a block)
                 const bool tail = p0 + kTok > sure;
-                auto scores = [&](int h, float2(&x)[16]) {
+                uint32_t seen[2] = {0xffffffffu, 0xffffffffu};      // of the block, by the row
+                if (tail) {
+                    const uint8_t* mask = a.mask ? a.mask + b * a.mask_stride + (int64_t)t_row * a.T : nullptr;
+#pragma unroll 1
+                    for (int k = 0; k < kTok; ++k) {
+                        const int p = p0 + k, d = p - len;
+                        if (p < end && (d < 0 || (mask ? mask[d] != 0 : d <= t_row))) continue;
+                        if (k < 32) seen[0] &= ~(1u << k);
+                        else seen[1] &= ~(1u << (k - 32));
+                    }
+                }
+                const int b0 = sm_e[2 * st], b1 = sm_e[2 * st + 1];
+                float2 x[kTok / 2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
                     uint32_t v[2][16];
                     tc::tmem_ld16x2(t_b + 32 * h, t_b + 32 * h + 16, v[0], v[1]);
 #pragma unroll
                     for (int k = 0; k < 16; k += 2) {
                         const float4 kk = lds128f(sc + 128 * h + 8 * k);
                         const uint32_t* y = &v[k >> 3][2 * k & 15];
-                        x[k] = mul2(make_float2(__uint_as_float(y[0]), __uint_as_float(y[1])), make_float2(kk.x, kk.y));
-                        x[k + 1] = mul2(make_float2(__uint_as_float(y[2]), __uint_as_float(y[3])), make_float2(kk.z, kk.w));
+                        x[16 * h + k] = mul2(make_float2(__uint_as_float(y[0]), __uint_as_float(y[1])), make_float2(kk.x, kk.y));
+                        x[16 * h + k + 1] = mul2(make_float2(__uint_as_float(y[2]), __uint_as_float(y[3])), make_float2(kk.z, kk.w));
                     }
                     if (KNG == 2) {
                         tc::tmem_ld16x2(t_b + kTok + 32 * h, t_b + kTok + 32 * h + 16, v[0], v[1]);
@@ -652,37 +668,23 @@ __global__ void __launch_bounds__(kThreads, 1)
                         for (int k = 0; k < 16; k += 2) {
                             const float4 kk = lds128f(sc + 256 + 128 * h + 8 * k);
                             const uint32_t* y = &v[k >> 3][2 * k & 15];
-                            x[k] = fma2(make_float2(__uint_as_float(y[0]), __uint_as_float(y[1])), make_float2(kk.x, kk.y), x[k]);
-                            x[k + 1] = fma2(make_float2(__uint_as_float(y[2]), __uint_as_float(y[3])), make_float2(kk.z, kk.w), x[k + 1]);
+                            x[16 * h + k] = fma2(make_float2(__uint_as_float(y[0]), __uint_as_float(y[1])), make_float2(kk.x, kk.y), x[16 * h + k]);
+                            x[16 * h + k + 1] = fma2(make_float2(__uint_as_float(y[2]), __uint_as_float(y[3])), make_float2(kk.z, kk.w), x[16 * h + k + 1]);
                         }
                     }
                     if (tail) {
-                        // the tokens of this half that the row sees
-                        uint32_t seen = 0;
-                        const uint8_t* mask = a.mask ? a.mask + b * a.mask_stride + (int64_t)t_row * a.T : nullptr;
-#pragma unroll 1
-                        for (int k = 0; k < 32; ++k) {
-                            const int p = p0 + 32 * h + k, d = p - len;
-                            const bool see = p < end && (d < 0 || (mask ? mask[d] != 0 : d <= t_row));
-                            seen |= (uint32_t)see << k;
-                        }
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
-                            if (!(seen >> (2 * k) & 1u)) x[k].x = -INFINITY;
-                            if (!(seen >> (2 * k + 1) & 1u)) x[k].y = -INFINITY;
+                            if (!(seen[h] >> (2 * k) & 1u)) x[16 * h + k].x = -INFINITY;
+                            if (!(seen[h] >> (2 * k + 1) & 1u)) x[16 * h + k].y = -INFINITY;
                         }
                     }
-                };
-                float top = -INFINITY;
-#pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                    float2 x[16];
-                    scores(h, x);
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) top = fmaxf(fmaxf(top, x[k].x), x[k].y);
                 }
+                float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int k = 0; k < kTok / 2; ++k) tops[k & 3] = fmaxf(fmaxf(tops[k & 3], x[k].x), x[k].y);
+                const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                 // raise the maximum, and the powers of two of the value scales, where they are left behind by much
-                const int b0 = sm_e[2 * st], b1 = sm_e[2 * st + 1];
                 const bool first = i == 0;
                 const bool raise = m == -INFINITY ? top != -INFINITY : (top - m) * fac > kLazy;
                 const int n0 = first || b0 > e0 + 4 ? b0 : e0, n1 = first || b1 > e1 + 4 ? b1 : e1;
@@ -704,13 +706,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                         tc::tc_fence_after();
                     }
 #pragma unroll 1
-                    for (int c = 0; c < pl.o_cols; c += 32) {
-                        uint32_t v[32];
-                        tmem_ld32(t_s + o_off + c, v);
+                    for (int c = 0; c < pl.o_cols; c += 16) {
+                        uint32_t v[16];
+                        tc::tmem_ld16(t_s + o_off + c, v);
                         const float f = c < va0 ? al0 : al1;
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f);
-                        tmem_st32(t_s + o_off + c, v);
+                        for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f);
+                        tmem_st16v(t_s + o_off + c, v);
                     }
                 }
                 e0 = n0;
@@ -718,39 +720,39 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // weights, times 2^(block's power - running power); over the scores that are done with: the first
                 // value group's from column 0, the second's from the second key group's place
                 const int d0 = max(b0 - e0, -126), dd = b1 - e1 - d0;
-                const float shift = (m == -INFINITY ? 0.0f : -m * fac) + (float)d0, second = dd < -126 ? 0.0f : pow2(min(dd, 127));
-                float2 sum = make_float2(0.0f, 0.0f);
-#pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                    float2 x[16];
-                    scores(h, x);
-                    uint32_t w[16];
+                const float shift = (m == -INFINITY ? 0.0f : -m * fac) + (float)d0;
+                const float second = dd < -126 ? 0.0f : pow2(min(dd, 127));
+                float2 sums[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const float2 y = fma2(x[k], make_float2(fac, fac), make_float2(shift, shift));
-                        x[k] = make_float2(ex2(y.x), ex2(y.y));
-                        sum = fma2(x[k], make_float2(1.0f, 1.0f), sum);
-                    }
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t w[16];
 #pragma unroll
                     for (int k = 0; k < 16; k += 2) {
                         const float4 vv = lds128f(sc + 512 + 128 * h + 8 * k);
-                        const float2 y0 = mul2(x[k], make_float2(vv.x, vv.y)), y1 = mul2(x[k + 1], make_float2(vv.z, vv.w));
-                        w[k] = pack2(y0.x, y0.y);
-                        w[k + 1] = pack2(y1.x, y1.y);
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            float2& y = x[16 * h + k + j];
+                            y = fma2(y, make_float2(fac, fac), make_float2(shift, shift));
+                            y = make_float2(ex2(y.x), ex2(y.y));
+                            sums[j] = fma2(y, make_float2(1.0f, 1.0f), sums[j]);
+                            const float2 z = mul2(y, j ? make_float2(vv.z, vv.w) : make_float2(vv.x, vv.y));
+                            w[k + j] = pack2(z.x, z.y);
+                        }
                     }
                     tmem_st16v(t_b + 16 * h, w);
                     if (VNG == 2) {
 #pragma unroll
                         for (int k = 0; k < 16; k += 2) {
                             const float4 vv = lds128f(sc + 768 + 128 * h + 8 * k);
-                            const float2 y0 = mul2(x[k], make_float2(vv.x * second, vv.y * second)), y1 = mul2(x[k + 1], make_float2(vv.z * second, vv.w * second));
+                            const float2 y0 = mul2(x[16 * h + k], make_float2(vv.x * second, vv.y * second));
+                            const float2 y1 = mul2(x[16 * h + k + 1], make_float2(vv.z * second, vv.w * second));
                             w[k] = pack2(y0.x, y0.y);
                             w[k + 1] = pack2(y1.x, y1.y);
                         }
                         tmem_st16v(t_b + p1_off + 16 * h, w);
                     }
                 }
-                l += (sum.x + sum.y) * pow2(-d0);
+                l += (sums[0].x + sums[0].y + sums[1].x + sums[1].y) * pow2(-d0);
                 tc::tc_fence_before();
                 __syncwarp();
                 // (by buffer: with two, a warp may be a block ahead of the others of its group)
