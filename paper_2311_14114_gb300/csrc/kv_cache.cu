@@ -103,25 +103,37 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(const KvGeom geo, co
     uint8_t* staged = rows[warp][lane / LPR];
     if (mode == kStaged && ql == 0) *reinterpret_cast<uint16_t*>(staged + 2 * s.D) = 0;      // what padding reads
     const uint16_t* base = in.p + head * in.head_stride;
-    const int64_t t_end = min(n, ((int64_t)blockIdx.x * kWarps + warp + 1) * per_warp);
-    int64_t t = ((int64_t)blockIdx.x * kWarps + warp) * per_warp + lane / LPR;
+    // a warp's tokens, at most 32: t_first .. t_first + count - 1; lane i holds the slot of the i-th
+    const int64_t t_first = ((int64_t)blockIdx.x * kWarps + warp) * per_warp;
+    if (t_first >= n) return;
+    const int count = (int)min((int64_t)per_warp, n - t_first);
+    const int64_t my_slot = lane < count ? __ldg(slots + t_first + lane) : -1;
     const float half = (float)(1 << (me.bits - 1));
     // the 16 bytes this lane loads of a row: its channels, or its share of the row
     const int ch16 = mode == kRun ? me.ch[0] : 8 * ql;
     const bool loads = mode != kSingle && ch16 >= 0 && ch16 < s.D;
-    uint4 next = make_uint4(0, 0, 0, 0);
-    int64_t slot_next = -1;
-    if (t < t_end) {
-        slot_next = slots[t];
-        if (loads) next = __ldg(reinterpret_cast<const uint4*>(base + t * in.token_stride + ch16));
-    }
-    for (int64_t t0 = t - lane / LPR; t0 < t_end; t0 += RPW, t += RPW) {
-        const uint4 raw = next;
-        const int64_t slot = t < t_end ? slot_next : -1;
-        if (t + RPW < t_end) {
-            slot_next = slots[t + RPW];
-            if (loads) next = __ldg(reinterpret_cast<const uint4*>(base + (t + RPW) * in.token_stride + ch16));
-        }
+    // rows are loaded four steps ahead of their use (the loop stays rolled: unrolled four times, with all its
+    // loads at the top, it took twice as long, for its instructions)
+    const uint16_t* load_at = base + (t_first + lane / LPR) * in.token_stride + ch16;
+    int i_load = lane / LPR;
+    auto load = [&]() {
+        uint4 r = make_uint4(0, 0, 0, 0);
+        if (loads && i_load < count) r = __ldg(reinterpret_cast<const uint4*>(load_at));
+        load_at += RPW * in.token_stride;
+        i_load += RPW;
+        return r;
+    };
+    uint4 ahead0 = load(), ahead1 = load(), ahead2 = load(), ahead3 = load();
+#pragma unroll 1
+    for (int i0 = 0; i0 < count; i0 += RPW) {
+        const int i_tok = i0 + lane / LPR;
+        const int64_t t = t_first + i_tok;
+        const uint4 raw = ahead0;
+        ahead0 = ahead1;
+        ahead1 = ahead2;
+        ahead2 = ahead3;
+        ahead3 = load();
+        const int64_t slot = __shfl_sync(0xffffffffu, my_slot, i_tok & 31);
         uint32_t x[4] = {raw.x, raw.y, raw.z, raw.w};
         if (mode == kStaged) {
             __syncwarp();
@@ -140,8 +152,8 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(const KvGeom geo, co
             const uint16_t* src = base + t * in.token_stride;
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
-                const uint32_t a = t < t_end && me.ch[i] >= 0 ? src[me.ch[i]] : 0u;
-                const uint32_t b = t < t_end && me.ch[i + 1] >= 0 ? src[me.ch[i + 1]] : 0u;
+                const uint32_t a = i_tok < count && me.ch[i] >= 0 ? src[me.ch[i]] : 0u;
+                const uint32_t b = i_tok < count && me.ch[i + 1] >= 0 ? src[me.ch[i + 1]] : 0u;
                 x[i >> 1] = a | b << 16;
             }
         }
@@ -187,7 +199,7 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(const KvGeom geo, co
         pack8(j, me.bits, w);
         const uint32_t other = __shfl_xor_sync(0xffffffffu, w[0], 1);
         if (me.bits == 2) w[0] |= other << 4;      // pairs of lanes share a word
-        if (slot < 0 || !me.valid) continue;
+        if (i_tok >= count || slot < 0 || !me.valid) continue;
         if (slot >= geo.n_pages * geo.page) {
             if (ql == 0) atomicOr(err, kErrKvIndex);
             continue;
@@ -233,39 +245,45 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(const KvGeom geo, con
     const bool wide = ((uintptr_t)out & 15u) == 0 && s.D % 8 == 0;
     const int mode = !wide ? kSingle : (__all_sync(0xffffffffu, me.run) ? kRun : kStaged);
     uint8_t* staged = rows[warp][lane / LPR];
-    const int64_t t_end = min(n, ((int64_t)blockIdx.x * kWarps + warp + 1) * per_warp);
-    int64_t t = ((int64_t)blockIdx.x * kWarps + warp) * per_warp + lane / LPR;
+    const int64_t t_first = ((int64_t)blockIdx.x * kWarps + warp) * per_warp;
+    if (t_first >= n) return;
+    const int count = (int)min((int64_t)per_warp, n - t_first);
+    const int64_t my_slot = lane < count ? __ldg(slots + t_first + lane) : -1;
     const float unit = 1.0f / (float)(1 << (me.bits - 1));
     const int at = s.off[me.grp] + (me.bits == 2 ? 4 * (me.q >> 1) : me.bits * me.q);
-    // a token's packed word(s) and scale are loaded while the one before is written
-    uint32_t next[2] = {0u, 0u};
-    uint16_t sc_next = 0;
-    auto load = [&](int64_t i) {
-        next[0] = next[1] = 0u;
-        sc_next = 0;
-        if (i >= t_end || !me.valid) return;
-        const int64_t slot = slots[i];
-        if (slot < 0) return;
-        if (slot >= geo.n_pages * geo.page) {
-            if (ql == 0) atomicOr(err, kErrKvIndex);
-            return;
-        }
-        const int64_t row = ((slot >> geo.page_shift) * geo.heads + head) * geo.page + (slot & (geo.page - 1));
-        const uint8_t* src = s.codes + row * s.row_bytes + at;
-        if (me.bits == 8) {
-            const uint2 w = *reinterpret_cast<const uint2*>(src);
-            next[0] = w.x;
-            next[1] = w.y;
-        } else {
-            next[0] = *reinterpret_cast<const uint32_t*>(src);
-        }
-        sc_next = s.scales[row * s.ng + me.grp];
+    // packed words and scales are loaded four steps ahead of their use
+    struct Packed {
+        uint32_t w0, w1, sc;
     };
-    load(t);
-    for (int64_t t0 = t - lane / LPR; t0 < t_end; t0 += RPW, t += RPW) {
-        uint32_t w[2] = {next[0], next[1]};
-        const float u = kv_load<BF16>(sc_next) * unit;
-        load(t + RPW);
+    int i_load = lane / LPR;
+    auto load = [&]() {
+        Packed r{0u, 0u, 0u};
+        const int64_t slot = __shfl_sync(0xffffffffu, my_slot, i_load & 31);
+        if (i_load < count && me.valid && slot >= 0) {
+            if (slot >= geo.n_pages * geo.page) {
+                if (ql == 0) atomicOr(err, kErrKvIndex);
+            } else {
+                const int64_t row = ((slot >> geo.page_shift) * geo.heads + head) * geo.page + (slot & (geo.page - 1));
+                const uint8_t* src = s.codes + row * s.row_bytes + at;
+                r.w0 = *reinterpret_cast<const uint32_t*>(src);
+                if (me.bits == 8) r.w1 = *reinterpret_cast<const uint32_t*>(src + 4);
+                r.sc = s.scales[row * s.ng + me.grp];
+            }
+        }
+        i_load += RPW;
+        return r;
+    };
+    Packed ahead0 = load(), ahead1 = load(), ahead2 = load(), ahead3 = load();
+#pragma unroll 1
+    for (int i0 = 0; i0 < count; i0 += RPW) {
+        const int i_tok = i0 + lane / LPR;
+        const int64_t t = t_first + i_tok;
+        uint32_t w[2] = {ahead0.w0, ahead0.w1};
+        const float u = kv_load<BF16>((uint16_t)ahead0.sc) * unit;
+        ahead0 = ahead1;
+        ahead1 = ahead2;
+        ahead2 = ahead3;
+        ahead3 = load();
         if (me.bits == 2) w[0] = w[0] >> (4 * (me.q & 1)) & 0x0F0F0F0Fu;
         float f[8];
         unpack8(w, me.bits, f);
@@ -276,7 +294,7 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(const KvGeom geo, con
             y[i] = kv_round<BF16>(z.x) | (uint32_t)kv_round<BF16>(z.y) << 16;
         }
         uint16_t* dst = out + (t * geo.heads + head) * s.D;
-        const bool on = t < t_end && me.valid;
+        const bool on = i_tok < count && me.valid;
         if (mode == kRun) {
             if (on && me.ch[0] >= 0) *reinterpret_cast<uint4*>(dst + me.ch[0]) = make_uint4(y[0], y[1], y[2], y[3]);
         } else if (mode == kStaged) {
@@ -285,7 +303,7 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(const KvGeom geo, con
             for (int i = 0; i < 8; ++i)
                 if (me.ch[i] >= 0) *reinterpret_cast<uint16_t*>(staged + 2 * me.ch[i]) = (uint16_t)pattern(y, i);
             __syncwarp();
-            if (t < t_end && 8 * ql < s.D) {
+            if (i_tok < count && 8 * ql < s.D) {
                 const uint2 a = *reinterpret_cast<const uint2*>(staged + 16 * ql), b = *reinterpret_cast<const uint2*>(staged + 16 * ql + 8);
                 *reinterpret_cast<uint4*>(dst + 8 * ql) = make_uint4(a.x, a.y, b.x, b.y);
             }
@@ -310,8 +328,7 @@ bool make_shape(const KvGeom& geo, int64_t n, Shape* sh) {
     while (sh->lpr < eighths) sh->lpr *= 2;
     const int64_t rpw = 32 / sh->lpr, steps = (n + rpw - 1) / rpw * geo.heads * 2;
     int64_t iters = steps / ((int64_t)num_sms() * 64);
-    iters = iters < 1 ? 1 : (iters > 32 ? 32 : iters);
-    sh->per_warp = (int)(iters * rpw);
+    sh->per_warp = (int)(iters * rpw < rpw ? rpw : (iters * rpw > 32 ? 32 : iters * rpw));      // a warp holds 32 slots
     const int64_t blocks = (n + (int64_t)kWarps * sh->per_warp - 1) / ((int64_t)kWarps * sh->per_warp);
     if (blocks > 2147483647) return false;
     sh->grid = dim3((unsigned)blocks, (unsigned)geo.heads, 2);
