@@ -60,22 +60,19 @@ struct TilePlan {
     int min_chunks;
 };
 
+// An item whose parts the join kernel puts together: written by the CTA that has
+// the first of them (n_part 0: none), one place per CTA behind the zeroed words
+// of the scratch, in front of the parts.
+struct JoinItem {
+    int entry, item, n_part, cta0, cta0_slot;
+};
+constexpr int kJoinBytes = 8192;
+
 struct Bars {               // offsets in 8-byte barriers
     static constexpr int raw_full = 0, raw_free = 4, k_ready = 8, v_ready = 12, kv_free = 16, s_full = 20, p_full = 24,
                          pv_done = 28, o_full = 30, q_full = 32, drain = 33;      // s_full, p_full: [group][buffer]
 };
 
-__device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
-        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(at)
-        : "memory");
-}
 __device__ __forceinline__ void tmem_st16v(uint32_t at, const uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};\n\t"
@@ -84,17 +81,6 @@ __device__ __forceinline__ void tmem_st16v(uint32_t at, const uint32_t (&r)[16])
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
-        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};\n\ttcgen05.wait::st.sync.aligned;" ::"r"(at),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-        : "memory");
-}
-
 // Values as an MN-major operand: 64-channel column groups kAtom apart, 8-token rows of 1024 bytes.
 __device__ __forceinline__ uint64_t value_desc(uint32_t at) {
     uint64_t d = (uint64_t)((at & 0x3FFFFu) >> 4);
@@ -239,7 +225,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t* words = reinterpret_cast<uint32_t*>(misc + 320);       // [32] for the split, then:
     const uint32_t abort_flag = tc::smem_u32(words + 32);
     uint32_t* tmem_at = words + 33;
-    uint32_t* sm_last = words + 34;
     int* sm_e = reinterpret_cast<int*>(words + 36);                  // [4 stages][2]: power of two above the value scales
     float* sm_fac = reinterpret_cast<float*>(misc + 512);            // [256] factor of a row's scores
     float* sm_m = sm_fac + 256;                                      // [128], of the second stream
@@ -286,7 +271,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         return end == 0 ? 1 : (end + kTok - 1) / kTok;      // a present sequence's rows are written even if they see nothing
     };
     Split split;
-    if (!split.begin(chunks, a.B * pl.row_units, geo.heads, pl.min_chunks, 8, words)) return;
+    JoinItem* join = reinterpret_cast<JoinItem*>(static_cast<uint8_t*>(a.scratch) + SONIQ_KV_SCRATCH_ZERO) + blockIdx.x;
+    const bool any = split.begin(chunks, a.B * pl.row_units, geo.heads, pl.min_chunks, 8, words);
+    if (tid == 0) join->n_part = 0;
+    if (!any) return;
 
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(tmem_at)), "r"(512) : "memory");
@@ -788,7 +776,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             const int unit_row = (streams ? 0 : 128 * s) + r_tile;
             const int64_t part_floats = (int64_t)unit_rows * (pl.o_cols + 2);
-            float* parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.scratch) + SONIQ_KV_SCRATCH_ZERO);
+            float* parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.scratch) + SONIQ_KV_SCRATCH_ZERO + kJoinBytes);
             uint8_t* staged = smem + (streams ? pl.o_cols * 512 : 128 * s * pl.out_stride);
             auto stage_out = [&](int c, float v) {
                 const int ch = sm_chan[c];
@@ -822,53 +810,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                     st[unit_rows + unit_row] = l;
                 }
             }
-            bool write = whole;
-            if (!whole) {
-                __threadfence();
-                bar_group(1, 256);
-                if (st_id == 0) {
-                    unsigned* counter = static_cast<unsigned*>(a.scratch) + seg.cta0;
-                    *sm_last = !tc::abort_raised(abort_flag) && atomicAdd(counter, 1u) == (unsigned)(seg.n_part - 1);
-                    if (*sm_last) *counter = 0;
-                }
-                bar_group(1, 256);
-                if (*sm_last && works && ok) {
-                    // all parts are there: join them in order
-                    __threadfence();
-                    write = true;
-                    auto stat = [&](int i) { return parts + part_slot(seg, i) * part_floats + (int64_t)unit_rows * pl.o_cols + unit_row; };
-                    float mm = -INFINITY, ll = 0.0f;
-                    for (int i = 0; i < seg.n_part; ++i) mm = fmaxf(mm, __ldcg(stat(i)));
-                    for (int i = 0; i < seg.n_part; ++i) {
-                        const float mi = __ldcg(stat(i));
-                        ll += __ldcg(stat(i) + unit_rows) * (mi == -INFINITY ? 0.0f : ex2(mi - mm));
-                    }
-                    const float inv = ll > 0.0f ? 1.0f / ll : (ll == 0.0f ? 0.0f : ll);
-#pragma unroll 1
-                    for (int c = 0; c < pl.o_cols; c += 16) {
-                        float x[16] = {};
-#pragma unroll 4
-                        for (int i = 0; i < seg.n_part; ++i) {
-                            const float4* from = reinterpret_cast<const float4*>(parts + part_slot(seg, i) * part_floats) + (int64_t)(c / 4) * unit_rows + unit_row;
-                            float4 q[4];
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) q[k] = __ldcg(from + (int64_t)k * unit_rows);
-                            const float mi = __ldcg(stat(i)), f = mi == -INFINITY ? 0.0f : ex2(mi - mm);
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                x[4 * k] = fmaf(f, q[k].x, x[4 * k]);
-                                x[4 * k + 1] = fmaf(f, q[k].y, x[4 * k + 1]);
-                                x[4 * k + 2] = fmaf(f, q[k].z, x[4 * k + 2]);
-                                x[4 * k + 3] = fmaf(f, q[k].w, x[4 * k + 3]);
-                            }
-                        }
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) stage_out(c + k, x[k] * inv);
-                    }
-                }
-            }
+            // (thread 0 cleared the place; it and this one are apart by a barrier of all threads)
+            if (!whole && seg.c_first == 0 && st_id == 0)
+                *join = JoinItem{seg.entry, seg.item, tc::abort_raised(abort_flag) ? 0 : seg.n_part, seg.cta0, seg.cta0_slot};
             __syncwarp();
-            if (write && works && ok) {
+            if (whole && works && ok) {
                 // a warp's 32 rows, each in one run
                 const int qh = geo.heads * a.group;
                 const bool pairs = vs.D % 2 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 3u) == 0;
@@ -934,6 +880,70 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
+// Joins the parts of split items, in order: 32 rows of one to a CTA.  (Joined by
+// the last CTA of the item to finish, inside the kernel above, five parts of 256
+// rows took 33 us.)
+constexpr int kJoinThreads = 256;
+__global__ void __launch_bounds__(kJoinThreads) kv_join_kernel(const KvGeom geo, const KvAttendArgs a, const TilePlan pl) {
+    extern __shared__ __align__(16) uint8_t staged[];      // 32 output rows
+    __shared__ int16_t chan[192];
+    tc::pdl_wait();
+    const uint8_t* scratch = static_cast<const uint8_t*>(a.scratch) + SONIQ_KV_SCRATCH_ZERO;
+    const JoinItem it = reinterpret_cast<const JoinItem*>(scratch)[blockIdx.x];
+    if (it.n_part == 0) return;
+    const KvSide& vs = geo.s[1];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int unit_rows = 128 * pl.tiles, unit_row = 32 * blockIdx.y + lane;
+    const int b = it.entry / pl.row_units, row0 = it.entry % pl.row_units * unit_rows + 32 * blockIdx.y, head = it.item;
+    if (row0 >= pl.rows) return;
+    const bool bf16 = geo.bf16 != 0;
+    const int va0 = 32 * vs.nb[0];
+    for (int c = tid; c < pl.o_cols; c += kJoinThreads) {
+        const int grp = c < va0 ? 0 : 1, code = column_code(vs.bits[grp], grp ? c - va0 : c);
+        chan[c] = code < vs.count[grp] ? (int16_t)vs.perm[head * vs.D + (grp ? vs.count[0] : 0) + code] : (int16_t)-1;
+    }
+    const int64_t part_floats = (int64_t)unit_rows * (pl.o_cols + 2);
+    auto part = [&](int i) {
+        return reinterpret_cast<const float*>(scratch + kJoinBytes) + (int64_t)(2 * (it.cta0 + i) + (i == 0 ? it.cta0_slot : 0)) * part_floats;
+    };
+    auto m_of = [&](int i) { return part(i)[(int64_t)unit_rows * pl.o_cols + unit_row]; };
+    float mm = -INFINITY, ll = 0.0f;
+#pragma unroll 4
+    for (int i = 0; i < it.n_part; ++i) mm = fmaxf(mm, m_of(i));
+#pragma unroll 4
+    for (int i = 0; i < it.n_part; ++i) {
+        const float mi = m_of(i);
+        ll += part(i)[(int64_t)unit_rows * (pl.o_cols + 1) + unit_row] * (mi == -INFINITY ? 0.0f : ex2(mi - mm));
+    }
+    const float inv = ll > 0.0f ? 1.0f / ll : (ll == 0.0f ? 0.0f : ll);      // nothing seen: 0; NaN stays
+    __syncthreads();
+    for (int c = 4 * warp; c < pl.o_cols; c += 4 * (kJoinThreads / 32)) {
+        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+        for (int i = 0; i < it.n_part; ++i) {
+            const float4 q = *(reinterpret_cast<const float4*>(part(i)) + (int64_t)(c / 4) * unit_rows + unit_row);
+            const float mi = m_of(i), f = mi == -INFINITY ? 0.0f : ex2(mi - mm);
+            x.x = fmaf(f, q.x, x.x);
+            x.y = fmaf(f, q.y, x.y);
+            x.z = fmaf(f, q.z, x.z);
+            x.w = fmaf(f, q.w, x.w);
+        }
+        const float y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int ch = chan[c + k];
+            if (ch >= 0) *reinterpret_cast<uint16_t*>(staged + lane * pl.out_stride + 2 * ch) = bf16 ? kv_round<true>(y[k] * inv) : kv_round<false>(y[k] * inv);
+        }
+    }
+    __syncthreads();
+    const int qh = geo.heads * a.group;
+    for (int i = warp; i < 32 && row0 + i < pl.rows; i += kJoinThreads / 32) {
+        const int r = row0 + i;
+        uint16_t* to = a.out + (((int64_t)b * a.T + r / a.group) * qh + head * a.group + r % a.group) * vs.D;
+        for (int c = lane; c < vs.D; c += 32) to[c] = *reinterpret_cast<const uint16_t*>(staged + i * pl.out_stride + 2 * c);
+    }
+}
+
 struct TileLaunch {
     bool fits;
     TilePlan pl;
@@ -990,7 +1000,7 @@ bool kv_tile_supported(const KvGeom& geo, int64_t T, int64_t group) { return pla
 
 int64_t kv_tile_scratch(const KvGeom& geo, int64_t T, int64_t group) {
     const TilePlan p = plan_tile(geo, T, group).pl;
-    return SONIQ_KV_SCRATCH_ZERO + (int64_t)2 * num_sms() * 128 * p.tiles * (p.o_cols + 2) * 4;
+    return SONIQ_KV_SCRATCH_ZERO + kJoinBytes + (int64_t)2 * num_sms() * 128 * p.tiles * (p.o_cols + 2) * 4;
 }
 
 cudaError_t launch_kv_tile(const KvGeom& geo, const KvAttendArgs& a, cudaStream_t st) {
@@ -1017,7 +1027,11 @@ cudaError_t launch_kv_tile(const KvGeom& geo, const KvAttendArgs& a, cudaStream_
     if (e != cudaSuccess) return e;
     kernel<<<grid, kThreads, p.smem, st>>>(geo, a, p, maps);
     note_launch();
-    return cudaGetLastError();
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    e = launch_pdl(kv_join_kernel, dim3((unsigned)grid, 4u * p.tiles), dim3(kJoinThreads), (size_t)(32 * p.out_stride), st, geo, a, p);
+    if (e == cudaSuccess) note_launch();
+    return e;
 }
 
 }  // namespace soniq
