@@ -4,11 +4,12 @@ GEMV and implicit-GEMM convolution behind a C-ABI library (``include/soniq.h``).
 
 ``paper_2311_14114_gb300.soniq`` is the thin ctypes binding over
 ``libsoniq.so``; ``paper_2311_14114_gb300.workloads`` draws seeded synthetic
-inputs.  Importing this package does not load the CUDA library; the binding
+inputs; ``paper_2311_14114_gb300.decode`` runs an attention layer over a
+quantized key / value cache.  Importing this package does not load the CUDA library; the binding
 loads it on first use and raises if it is missing.
 """
 
-__all__ = ["soniq", "workloads"]
+__all__ = ["soniq", "workloads", "decode"]
 
 
 def __getattr__(name):
