@@ -44,7 +44,10 @@ constexpr int kSlotCols = 256;           // TMEM columns of a softmax group: S (
 // Columns of a softmax group in front of O: scores (the weights of the first value group go over them), and those
 // of the second key group or the weights of the second value group
 __host__ __device__ constexpr int s_cols(int k_groups, int v_groups) { return k_groups == 2 ? 2 * kTok : (v_groups == 2 ? kTok + kTok / 2 : kTok); }
-constexpr float kLazy = 8.0f;            // a maximum may be exceeded by this (log2) before O is rescaled
+// A row's running maximum may be exceeded by kLazy (log2), and the running powers of the value scales by kLazyScale,
+// before O is rescaled: weights stay below 2^15 in fp16.
+constexpr float kLazy = 13.0f;
+constexpr int kLazyScale = 2;
 
 struct TilePlan {
     int rows;               // query rows per key head
@@ -185,19 +188,11 @@ struct Ring {
 // false once the CTA gives up, or when the wait is given up after 2 s.  (The
 // polling loop is written out: twenty warps' polls took a third of the issue
 // slots, and what all roles run has to stay in the instruction cache.)
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, uint32_t abort_flag, unsigned* err) {
+template <typename F>
+__device__ __forceinline__ bool wait_until(F poll, uint32_t abort_flag, unsigned* err) {
     long long t0 = 0;
     while (true) {
-        uint32_t done;
-        asm volatile(
-            "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 4096;\n"
-            "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra DONE;\n\t"
-            "sub.u32 n, n, 1;\n\tsetp.ne.u32 q, n, 0;\n\t@q bra TRY;\n"
-            "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done)
-            : "r"(bar), "r"(parity)
-            : "memory");
-        if (__all_sync(0xffffffffu, done)) return true;
+        if (__all_sync(0xffffffffu, poll())) return true;
         if (__any_sync(0xffffffffu, tc::abort_raised(abort_flag))) return false;
         const long long t = tc::globaltimer();
         if (t0 == 0) t0 = t;
@@ -207,6 +202,40 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, uint32_
             return false;
         }
     }
+}
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, uint32_t abort_flag, unsigned* err) {
+    return wait_until([&]() {
+        uint32_t done;
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 4096;\n"
+            "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra DONE;\n\t"
+            "sub.u32 n, n, 1;\n\tsetp.ne.u32 q, n, 0;\n\t@q bra TRY;\n"
+            "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        return done;
+    }, abort_flag, err);
+}
+// The same for three barriers, whose phases stay complete until this warp has gone on.  (One
+// after the other, three waits that were over took 870 cycles of a block's 3550.)
+__device__ __forceinline__ bool wait_warp3(uint32_t b0, uint32_t parity0, uint32_t b1, uint32_t parity1, uint32_t b2, uint32_t parity2,
+                                           uint32_t abort_flag, unsigned* err) {
+    return wait_until([&]() {
+        uint32_t done;
+        asm volatile(
+            "{\n\t.reg .pred p, q, r;\n\t.reg .u32 n;\n\tmov.u32 n, 4096;\n"
+            "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 q, [%3], %4;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 r, [%5], %6;\n\t"
+            "and.pred p, p, q;\n\tand.pred p, p, r;\n\t@p bra DONE;\n\t"
+            "sub.u32 n, n, 1;\n\tsetp.ne.u32 q, n, 0;\n\t@q bra TRY;\n"
+            "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(b0), "r"(parity0), "r"(b1), "r"(parity1), "r"(b2), "r"(parity2)
+            : "memory");
+        return done;
+    }, abort_flag, err);
 }
 
 // KNG, VNG: precision groups of keys and values.  SB: buffers of scores (2 where
@@ -292,6 +321,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto wait = [&](int i, uint32_t parity) {
         return wait_warp(bar(i), parity & 1u, abort_flag, a.err);
     };
+    auto wait3 = [&](int i, uint32_t pi, int j, uint32_t pj, int k, uint32_t pk) {
+        return wait_warp3(bar(i), pi & 1u, bar(j), pj & 1u, bar(k), pk & 1u, abort_flag, a.err);
+    };
     // where the next segment's blocks begin in the rings; parities of the softmax groups'
     // scores and weights, blocks done and results (bit s), and of the queries'
     Ring kv0, raw0;
@@ -354,10 +386,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint64_t q_tile = tc::sw128_desc(smem0 + (streams ? 0 : s * pl.k_atoms * kQAtom));
             // every lane runs the loops, the elected one issues
             const bool leader = tc::elect_one();
-            auto ready = [&](int which, const Ring& at) {
-                ok = ok && wait(which + at.i, at.phase);
-                tc::tc_fence_after();
-            };
             if (mine > 0) ok = wait(Bars::q_full, q_phase);
             tc::tc_fence_after();
             Ring now = kv0, next = kv0;       // the block whose outputs, and whose scores, come next
@@ -367,13 +395,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (step == 2) r.step(pl.stages);
             };
             uint32_t phases = s_phase >> (2 * s);      // of the weights in each buffer, as of the scores
-            // scores run SB blocks ahead of the outputs
+            // Scores run SB blocks ahead of the outputs.  Where the ring has a place for the next scores' keys that no
+            // outputs of this block or later free, one wait covers both.
+            const bool early = pl.stages > SB * step;
 #pragma unroll 1
             for (int i = -SB; ok && i < mine; ++i) {
                 const int buf = SB == 2 ? i & 1 : 0;
                 if (i >= 0) {
-                    ready(Bars::v_ready, now);
-                    ok = ok && wait(Bars::p_full + 2 * s + buf, phases >> buf);
+                    const int nx = i + SB < mine && early ? Bars::k_ready + next.i : Bars::v_ready + now.i;
+                    ok = wait3(Bars::p_full + 2 * s + buf, phases >> buf, Bars::v_ready + now.i, now.phase, nx,
+                               i + SB < mine && early ? next.phase : now.phase);
                     if (!ok) break;
                     tc::tc_fence_after();
                     phases ^= 1u << buf;
@@ -404,8 +435,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                     advance(now);
                 }
                 if (i + SB < mine) {
-                    ready(Bars::k_ready, next);
-                    if (!ok) break;
+                    if (i < 0 || !early) {
+                        ok = wait(Bars::k_ready + next.i, next.phase);
+                        if (!ok) break;
+                        tc::tc_fence_after();
+                    }
                     uint64_t q = q_tile, k = tc::sw128_desc(ring + next.i * pl.stage_bytes);
                     const uint32_t d = t_s + buf * s_cols(KNG, VNG);
                     // 32-code halves of column groups, two MMAs each
@@ -618,7 +652,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int j = streams ? 2 * i + s : i, st = kv.i, buf = SB == 2 ? i & 1 : 0;
                 const int p0 = (seg.c_first + j) * kTok;
                 const uint32_t sc = ring + st * pl.stage_bytes + (pl.k_atoms + pl.v_atoms) * kAtom;
-                ok = wait(Bars::k_ready + st, kv.phase) && wait(Bars::v_ready + st, kv.phase) && wait(Bars::s_full + 2 * s + buf, phases >> buf);
+                ok = wait3(Bars::s_full + 2 * s + buf, phases >> buf, Bars::k_ready + st, kv.phase, Bars::v_ready + st, kv.phase);
                 if (!ok) break;
                 phases ^= 1u << buf;
                 const uint32_t t_b = t_s + buf * s_cols(KNG, VNG);
@@ -629,12 +663,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                 uint32_t seen[2] = {0xffffffffu, 0xffffffffu};      // of the block, by the row
                 if (tail) {
                     const uint8_t* mask = a.mask ? a.mask + b * a.mask_stride + (int64_t)t_row * a.T : nullptr;
-#pragma unroll 1
-                    for (int k = 0; k < kTok; ++k) {
-                        const int p = p0 + k, d = p - len;
-                        if (p < end && (d < 0 || (mask ? mask[d] != 0 : d <= t_row))) continue;
-                        if (k < 32) seen[0] &= ~(1u << k);
-                        else seen[1] &= ~(1u << (k - 32));
+                    const int upto = (mask ? sure : min(end, len + t_row + 1)) - p0;      // shown without a look at the mask
+                    seen[0] = upto >= 32 ? 0xffffffffu : (upto <= 0 ? 0u : (1u << upto) - 1u);
+                    seen[1] = upto >= 64 ? 0xffffffffu : (upto <= 32 ? 0u : (1u << (upto - 32)) - 1u);
+                    if (mask) {
+#pragma unroll 8
+                        for (int k = max(upto, 0); k < min(kTok, end - p0); ++k) {
+                            const uint32_t shown = mask[p0 + k - len] != 0;
+                            if (k < 32) seen[0] |= shown << k;
+                            else seen[1] |= shown << (k - 32);
+                        }
                     }
                 }
                 const int b0 = sm_e[2 * st], b1 = sm_e[2 * st + 1];
@@ -668,14 +706,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                     }
                 }
-                float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                float tops[8];
 #pragma unroll
-                for (int k = 0; k < kTok / 2; ++k) tops[k & 3] = fmaxf(fmaxf(tops[k & 3], x[k].x), x[k].y);
-                const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+                for (int k = 0; k < 8; ++k) tops[k] = fmaxf(x[k].x, x[k].y);
+#pragma unroll
+                for (int k = 8; k < kTok / 2; ++k) tops[k & 7] = fmaxf(fmaxf(tops[k & 7], x[k].x), x[k].y);
+                const float top = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
                 // raise the maximum, and the powers of two of the value scales, where they are left behind by much
                 const bool first = i == 0;
                 const bool raise = m == -INFINITY ? top != -INFINITY : (top - m) * fac > kLazy;
-                const int n0 = first || b0 > e0 + 4 ? b0 : e0, n1 = first || b1 > e1 + 4 ? b1 : e1;
+                const int n0 = first || b0 > e0 + kLazyScale ? b0 : e0, n1 = first || b1 > e1 + kLazyScale ? b1 : e1;
                 if (first) {
                     m = top;
                 } else if (__any_sync(0xffffffffu, raise) || n0 != e0 || n1 != e1) {
