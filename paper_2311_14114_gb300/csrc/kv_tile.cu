@@ -217,8 +217,24 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, uint32_
         return done;
     }, abort_flag, err);
 }
-// The same for three barriers, whose phases stay complete until this warp has gone on.  (One
-// after the other, three waits that were over took 870 cycles of a block's 3550.)
+// The same for two or three barriers, whose phases stay complete until this warp has gone
+// on.  (One after the other, three waits that were over took 870 cycles of a block's 3550.)
+__device__ __forceinline__ bool wait_warp2(uint32_t b0, uint32_t parity0, uint32_t b1, uint32_t parity1, uint32_t abort_flag, unsigned* err) {
+    return wait_until([&]() {
+        uint32_t done;
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 4096;\n"
+            "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 q, [%3], %4;\n\t"
+            "and.pred p, p, q;\n\t@p bra DONE;\n\t"
+            "sub.u32 n, n, 1;\n\tsetp.ne.u32 q, n, 0;\n\t@q bra TRY;\n"
+            "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(b0), "r"(parity0), "r"(b1), "r"(parity1)
+            : "memory");
+        return done;
+    }, abort_flag, err);
+}
 __device__ __forceinline__ bool wait_warp3(uint32_t b0, uint32_t parity0, uint32_t b1, uint32_t parity1, uint32_t b2, uint32_t parity2,
                                            uint32_t abort_flag, unsigned* err) {
     return wait_until([&]() {
@@ -268,9 +284,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (tid == 0) {
         for (int i = 0; i < 4; ++i) {
             tc::mbar_init(bar(Bars::raw_full + i), 1);
-            tc::mbar_init(bar(Bars::raw_free + i), 8);
-            tc::mbar_init(bar(Bars::k_ready + i), 4);
-            tc::mbar_init(bar(Bars::v_ready + i), 4);
+            tc::mbar_init(bar(Bars::raw_free + i), 9);
+            tc::mbar_init(bar(Bars::k_ready + i), 5);
+            tc::mbar_init(bar(Bars::v_ready + i), 5);
             tc::mbar_init(bar(Bars::kv_free + i), pl.tiles);
             tc::mbar_init(bar(Bars::s_full + i), 1);
             tc::mbar_init(bar(Bars::p_full + i), 4);
@@ -320,6 +336,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     auto wait = [&](int i, uint32_t parity) {
         return wait_warp(bar(i), parity & 1u, abort_flag, a.err);
+    };
+    auto wait2 = [&](int i, uint32_t pi, int j, uint32_t pj) {
+        return wait_warp2(bar(i), pi & 1u, bar(j), pj & 1u, abort_flag, a.err);
     };
     auto wait3 = [&](int i, uint32_t pi, int j, uint32_t pj, int k, uint32_t pk) {
         return wait_warp3(bar(i), pi & 1u, bar(j), pj & 1u, bar(k), pk & 1u, abort_flag, a.err);
@@ -459,10 +478,56 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
         } else if (ROLE == 2 && warp == 2) {
-            // ---- the segment after this one ----
+            // ---- the segment after this one, and scales ----
             const bool more = split.next(seg);
             if (more) *sm_seg = split.segment(chunks);
             *sm_more = more;
+            // ---- scales as fp32: keys' with 2^-(n-1), values' relative to a power of two; two tokens to a lane ----
+            uint32_t from[2][2];        // [side][token]
+#pragma unroll
+            for (int side = 0; side < 2; ++side) {
+                const int ng = side ? VNG : KNG, at0 = pl.raw_s + (side ? kTok / pl.box_rows * pl.scale_step[0] : 0);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int t = lane + 32 * h;
+                    from[side][h] = at0 + (t / pl.box_rows) * pl.scale_step[side] + 2 * ng * (t % pl.box_rows);
+                }
+            }
+            Ring kv = kv0, rw = raw0;
+#pragma unroll 1
+            for (int j = 0; ok && j < nblk; ++j, kv.step(pl.stages), rw.step(pl.raw_stages)) {
+                const int st = kv.i, r = rw.i, p0 = (seg.c_first + j) * kTok;
+                ok = wait2(Bars::kv_free + st, kv.phase ^ 1u, Bars::raw_full + r, rw.phase);
+                if (!ok) break;
+                const uint32_t src = raw + r * pl.raw_bytes, to = ring + st * pl.stage_bytes + (pl.k_atoms + pl.v_atoms) * kAtom + 4 * lane;
+#pragma unroll
+                for (int side = 0; side < 2; ++side) {
+#pragma unroll
+                    for (int grp = 0; grp < (side ? VNG : KNG); ++grp) {
+                        float x[2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            x[h] = p0 + lane + 32 * h < end ? scale_of(lds16(src + from[side][h] + 2 * grp), bf16) : 0.0f;
+                        float f = pow2(1 - geo.s[side].bits[grp]);
+                        if (side) {
+                            const uint32_t big = __reduce_max_sync(0xffffffffu, max(__float_as_uint(x[0]), __float_as_uint(x[1])));
+                            const int e = min(max((int)(big >> 23) - 126, -100), 126);
+                            f = pow2(-e);
+                            if (lane == 0) sm_e[2 * st + grp] = e;
+                        }
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 512 * side + 256 * grp + 128 * h), "f"(x[h] * f) : "memory");
+                    }
+                }
+                if (VNG == 1 && lane == 0) sm_e[2 * st + 1] = -100;
+                __syncwarp();
+                if (lane == 0) {
+                    tc::mbar_arrive(bar(Bars::k_ready + st));
+                    tc::mbar_arrive(bar(Bars::v_ready + st));
+                    tc::mbar_arrive(bar(Bars::raw_free + r));
+                }
+            }
             if (!checked) check_lengths(geo, a, lane, 32);
             checked = true;
         } else if constexpr (ROLE == 1) {
@@ -471,43 +536,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             const KvSide& sd = geo.s[side];
             const Offsets f;
             const uint32_t raw_sw = sd.row_bytes == 64 ? ((tok >> 1) & 3) << 4 : (sd.row_bytes == 128 ? (tok & 7) << 4 : 0);
-            const uint32_t sc_at = pl.raw_s + (side ? kTok / pl.box_rows * pl.scale_step[0] : 0);
-            const int ng = side ? VNG : KNG;
             Ring kv = kv0, rw = raw0;
 #pragma unroll 1
             for (int j = 0; ok && j < nblk; ++j, kv.step(pl.stages), rw.step(pl.raw_stages)) {
                 const int st = kv.i, r = rw.i;
-                const int p0 = (seg.c_first + j) * kTok;
                 const uint32_t at = ring + st * pl.stage_bytes, src = raw + r * pl.raw_bytes;
-                ok = wait(Bars::kv_free + st, kv.phase ^ 1u) && wait(Bars::raw_full + r, rw.phase);
+                ok = wait2(Bars::kv_free + st, kv.phase ^ 1u, Bars::raw_full + r, rw.phase);
                 if (!ok) break;
-                // scales as fp32: keys' with 2^-(n-1), values' relative to a power of two
-                if (dw < 2) {
-                    const uint32_t to = at + (pl.k_atoms + pl.v_atoms) * kAtom + side * 512;
-                    float x[2][2];        // [this token, the other half's][group]
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int t = h ? tok ^ 32 : tok;
-                        const uint32_t e = src + sc_at + (t / pl.box_rows) * pl.scale_step[side] + 2 * ng * (t % pl.box_rows);
-                        const bool in = p0 + t < end;
-                        x[h][0] = in ? scale_of(lds16(e), bf16) : 0.0f;
-                        x[h][1] = in && ng == 2 ? scale_of(lds16(e + 2), bf16) : 0.0f;
-                    }
-                    float f0 = pow2(1 - sd.bits[0]), f1 = pow2(1 - sd.bits[1]);
-                    if (side) {
-                        const uint32_t big0 = __reduce_max_sync(0xffffffffu, max(__float_as_uint(x[0][0]), __float_as_uint(x[1][0])));
-                        const uint32_t big1 = __reduce_max_sync(0xffffffffu, max(__float_as_uint(x[0][1]), __float_as_uint(x[1][1])));
-                        const int e0 = min(max((int)(big0 >> 23) - 126, -100), 126), e1 = min(max((int)(big1 >> 23) - 126, -100), 126);
-                        f0 = pow2(-e0);
-                        f1 = pow2(-e1);
-                        if (dw == 0 && lane == 0) {
-                            sm_e[2 * st] = e0;
-                            sm_e[2 * st + 1] = e1;
-                        }
-                    }
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 4 * tok), "f"(x[0][0] * f0) : "memory");
-                    if (ng == 2) asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 256 + 4 * tok), "f"(x[0][1] * f1) : "memory");
-                }
                 // a lane takes a token, two warps every second block
                 const uint32_t base = src + (side ? pl.raw_v : 0) + tok * sd.row_bytes;
                 const uint32_t to = at + (side ? pl.k_atoms * kAtom : 0) + tok * 128;
