@@ -38,6 +38,7 @@ namespace soniq {
 namespace {
 
 constexpr int kChunk = 32;                   // tokens a warp takes at a time
+constexpr int kLead = 16;            // an item's queries and results take about as long as this many chunks
 
 struct RowsPlan {
     int row_tiles;        // tiles of 8 NT query rows per key head
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
     check_lengths(geo, a, tid, blockDim.x);
     auto chunks = [&](int b) { return (uint32_t)chunks_of(geo, a, b); };
     Split split;
-    if (!split.begin(chunks, a.B, geo.heads * pl.row_tiles, pl.min_chunks, 2 * n_warps, sm_scan)) return;
+    if (!split.begin(chunks, a.B, geo.heads * pl.row_tiles, pl.min_chunks, kLead, 2 * n_warps, sm_scan)) return;
 
     const int qh = geo.heads * a.group;
     const int n_min = ks.ng == 2 && ks.bits[1] < ks.bits[0] ? ks.bits[1] : ks.bits[0];
@@ -850,9 +851,9 @@ cudaError_t launch_kv_attend(const KvGeom& geo, const KvAttendArgs& args, cudaSt
     if (takes_tile(geo, a.T, a.group)) return launch_kv_tile(geo, a, st);
     const RowsLaunch r = plan_rows(geo, a.T, a.group);
     const int64_t cap = (int64_t)a.max_pages << geo.page_shift;
-    const int64_t most = (int64_t)a.B * geo.heads * r.pl.row_tiles * (cap / kChunk + 1);
-    if (most >= 2147483648ll) return cudaErrorNotSupported;      // chunks are numbered in 32 bits
-    const int64_t by_size = (most + r.pl.min_chunks - 1) / r.pl.min_chunks, items = (int64_t)a.B * geo.heads * r.pl.row_tiles;
+    const int64_t items = (int64_t)a.B * geo.heads * r.pl.row_tiles, most = items * (cap / kChunk + 1);
+    if (most + items * kLead >= 2147483648ll) return cudaErrorNotSupported;      // chunks are numbered in 32 bits
+    const int64_t by_size = (most + r.pl.min_chunks - 1) / r.pl.min_chunks;
     const int64_t want = by_size > items ? by_size : items, full = (int64_t)r.ctas_per_sm * num_sms();
     const int grid = (int)(want < full ? want : full);
     KvMaps maps;

@@ -6,9 +6,10 @@
 // for `mult` items of chunks(e) chunks each.  Few items: each is cut in equal
 // parts, a CTA to a part, if that costs no CTA more than `slack` chunks over the
 // even split.  Otherwise the list is cut evenly, and a CTA may end one item and
-// begin another.  CTAs that share an item leave partial results, each in a
-// place of its own, and the last to finish joins them in order, so the outputs
-// do not depend on which CTA that is.
+// begin another; there an item counts `lead` units more than its chunks, in front
+// of them, for what it costs whatever its length.  CTAs that share an item leave
+// partial results, each in a place of its own, which are joined in order, so the
+// outputs do not depend on which CTA was first.
 #pragma once
 
 #include "kv_internal.h"
@@ -24,16 +25,17 @@ struct Segment {
 
 struct Split {
     uint32_t part_chunks;              // 0: the even cut
-    uint32_t n_cta, per, more, pos, hi, lo, base, mult;
+    uint32_t n_cta, per, more, pos, hi, lo, base, mult, lead;
     int entry;
 
     // shared: 32 words (at most 30 warps).  Every thread of the CTA calls it; false: this CTA has
     // nothing to do.  chunks(e) is 0 for an entry without work.
     template <typename F>
-    __device__ __forceinline__ bool begin(F chunks, int n_entries, uint32_t mult_, uint32_t min_chunks, uint32_t slack,
-                                          uint32_t* shared) {
+    __device__ __forceinline__ bool begin(F chunks, int n_entries, uint32_t mult_, uint32_t min_chunks, uint32_t lead_,
+                                          uint32_t slack, uint32_t* shared) {
         const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
         mult = mult_;
+        lead = lead_;
         part_chunks = lo = hi = 0;
         per = 1;
         more = 0;
@@ -57,21 +59,25 @@ struct Split {
             return before;
         };
         const bool one_scan = n_entries <= (int)blockDim.x;
+        auto units_of = [&](int e) {
+            const uint32_t n = chunks(e);
+            return n == 0 ? 0u : n + lead;
+        };
         uint32_t total, mine = 0, before = 0, items = 0xffffffffu;
         if (one_scan) {
-            mine = tid < n_entries ? chunks(tid) : 0;
+            mine = tid < n_entries ? units_of(tid) : 0;
             items = __syncthreads_count(mine > 0) * mult;
             before = scan(mine, total);
         } else {
-            for (int e = tid; e < n_entries; e += blockDim.x) mine += chunks(e);
+            for (int e = tid; e < n_entries; e += blockDim.x) mine += units_of(e);
             scan(mine, total);
         }
         total *= mult;      // below 2^31 (checked on the host)
         if (total == 0) return false;
         if (items <= gridDim.x) {
             const uint32_t free_cta = gridDim.x - min(items, gridDim.x / 2);
-            const uint32_t want = max((total + free_cta - 1) / free_cta, min_chunks);
-            const uint32_t mine_units = (mine + want - 1) / want * mult;
+            const uint32_t want = max((total - items * lead + free_cta - 1) / free_cta, min_chunks);
+            const uint32_t mine_units = mine == 0 ? 0 : (mine - lead + want - 1) / want * mult;
             uint32_t units;
             const uint32_t u0 = scan(mine_units, units);
             if (units <= gridDim.x && want <= total / gridDim.x + slack) {
@@ -97,7 +103,7 @@ struct Split {
             for (int e0 = 0; e0 < n_entries; e0 += blockDim.x) {
                 uint32_t all = 0;
                 if (!one_scan) {
-                    mine = e0 + tid < n_entries ? chunks(e0 + tid) : 0;
+                    mine = e0 + tid < n_entries ? units_of(e0 + tid) : 0;
                     before = scan(mine, all);
                 }
                 const uint32_t at = (run + before) * mult;
@@ -113,7 +119,8 @@ struct Split {
         entry = (int)shared[30];
         base = shared[31];
         pos = lo;
-        return true;
+        // a range within an item's lead has no chunks
+        return part_chunks != 0 || hi - lo > left_of_lead(lo, chunks(entry) + lead);
     }
 
     template <typename F>
@@ -131,19 +138,21 @@ struct Split {
             s.n_part = (int)parts;
             s.cta0_slot = 0;
         } else {
-            while (pos >= base + nch * mult) {
-                base += nch * mult;
+            // (an entry without chunks has no units)
+            while (nch == 0 || pos >= base + (nch + lead) * mult) {
+                base += nch == 0 ? 0 : (nch + lead) * mult;
                 nch = chunks(++entry);
             }
-            s.item = (int)((pos - base) / nch);
-            const uint32_t first = base + s.item * nch;
-            s.c_first = (int)(pos - first);
-            s.c_end = min(s.c_first + (int)(hi - pos), (int)nch);
+            s.item = (int)((pos - base) / (nch + lead));
+            const uint32_t first = base + s.item * (nch + lead) + lead;      // unit of its first chunk
+            s.c_first = pos > first ? (int)(pos - first) : 0;
+            s.c_end = min((int)(hi - first), (int)nch);
             s.cta0 = (int)owner_of(first);
             s.n_part = (int)owner_of(first + nch - 1) - s.cta0 + 1;
             // a CTA's first range leaves its partial result in the first of its two places
             s.slot += pos == lo ? 0 : 1;
-            s.cta0_slot = range_of(s.cta0) == first ? 0 : 1;
+            s.cta0_slot = range_of(s.cta0) + lead >= first ? 0 : 1;
+            pos = first + s.c_first;
         }
         s.entry = entry;
         s.n_chunks = (int)nch;
@@ -153,10 +162,15 @@ struct Split {
     // Behind a segment; false: it was the last.
     __device__ __forceinline__ bool next(const Segment& s) {
         pos += s.c_end - s.c_first;
-        return part_chunks == 0 && pos < hi;
+        return part_chunks == 0 && hi > pos + lead;       // a next item's chunks come behind its lead
     }
 
 private:
+    // Units from u to the first chunk of its item (0: u is a chunk).
+    __device__ __forceinline__ uint32_t left_of_lead(uint32_t u, uint32_t item_units) const {
+        const uint32_t at = (u - base) % item_units;
+        return at < lead ? lead - at : 0;
+    }
     __device__ __forceinline__ uint32_t range_of(uint32_t c) const { return per * c + min(c, more); }
     __device__ __forceinline__ uint32_t owner_of(uint32_t chunk) const {
         const uint32_t cut = more * (per + 1);

@@ -70,6 +70,7 @@ struct JoinItem {
     int entry, item, n_part, cta0, cta0_slot;
 };
 constexpr int kJoinBytes = 8192;
+constexpr int kLead = 8;                 // an item's queries and results take about as long as this many blocks
 
 struct Bars {               // offsets in 8-byte barriers
     static constexpr int raw_full = 0, raw_free = 4, k_ready = 8, v_ready = 12, kv_free = 16, s_full = 20, p_full = 24,
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
     Split split;
     JoinItem* join = reinterpret_cast<JoinItem*>(static_cast<uint8_t*>(a.scratch) + SONIQ_KV_SCRATCH_ZERO) + blockIdx.x;
-    const bool any = split.begin(chunks, a.B * pl.row_units, geo.heads, pl.min_chunks, 8, words);
+    const bool any = split.begin(chunks, a.B * pl.row_units, geo.heads, pl.min_chunks, kLead, 8, words);
     if (tid == 0) join->n_part = 0;
     if (!any) return;
 
@@ -567,7 +568,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         } else if constexpr (ROLE == 0) {
             // ---- softmax ----
             const int s = (warp >> 2) - 3, quad = warp & 3, st_id = tid - 384;
-            // queries: fp16, each row scaled to 2^13; a lane takes four channels (of 128) of a row
+            // queries: fp16, each row scaled to 2^13; a lane takes eight channels (of 128) of a row
             {
                 const int total = groups == 2 && !streams ? 256 : 128, cols = pa0 + pa1;
                 for (int c = st_id; c < cols; c += 256) {
@@ -587,77 +588,83 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
                 bar_group(1, 256);
-                const bool wide = ks.D % 4 == 0 && (((uintptr_t)a.Q | (uintptr_t)(2 * a.q_seq_stride) | (uintptr_t)(2 * a.q_token_stride) |
-                                                     (uintptr_t)(2 * a.q_head_stride)) & 7u) == 0;
+                const bool wide = ks.D % 8 == 0 && (((uintptr_t)a.Q | (uintptr_t)(2 * a.q_seq_stride) | (uintptr_t)(2 * a.q_token_stride) |
+                                                     (uintptr_t)(2 * a.q_head_stride)) & 15u) == 0;
                 const float fac0 = fabsf(a.scale) * kLog2e, sign = a.scale < 0.0f ? -1.0f : 1.0f;
                 auto fill = [&](auto halves) {
                     constexpr int H = decltype(halves)::value;      // 128 channels each
-                    uint32_t to[4 * H];
-                    float down[4 * H];
+                    const int half = lane >> 4, l16 = lane & 15;
+                    uint32_t to[8 * H];
+                    float down[8 * H];
 #pragma unroll
-                    for (int k = 0; k < 4 * H; ++k) {
-                        const int ch = 128 * (k >> 2) + 4 * lane + (k & 3);
+                    for (int k = 0; k < 8 * H; ++k) {
+                        const int ch = 128 * (k >> 3) + 8 * l16 + (k & 7);
                         const int col = ch < ks.D ? sm_col[ch] : 0, bits = ks.bits[col < pa0 ? 0 : 1];
                         to[k] = (col >> 6) * kQAtom + ((col & 63) >> 3) * 16 + 2 * (col & 7);
                         down[k] = sign * pow2(-place_log2(bits, (col & 7) >> 1));
                     }
+                    // each half of the warp takes every second row: two rows' loads go out while the two before are
+                    // scaled and stored
+                    int row = row0 + r_first + half, t = row / a.group, hq = row - t * a.group;
                     const uint16_t* q0 = a.Q + b * a.q_seq_stride + (int64_t)head * a.group * a.q_head_stride;
-                    // four rows' loads go out while the four before are scaled and stored
-                    auto load = [&](int r, uint2(&v)[4][H]) {
-                        int t = (row0 + r) / a.group, hq = (row0 + r) % a.group;
+                    auto load = [&](uint4(&v)[2][H]) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint16_t* q = q0 + t * a.q_token_stride + hq * a.q_head_stride;
-                            const bool on = row0 + r + i < pl.rows;
+                        for (int i = 0; i < 2; ++i) {
+                            const uint16_t* q = q0 + t * a.q_token_stride + hq * a.q_head_stride + 8 * l16;
+                            const bool on = row < pl.rows;
 #pragma unroll
                             for (int h = 0; h < H; ++h) {
-                                const int ch = 128 * h + 4 * lane;
-                                v[i][h] = make_uint2(0, 0);
-                                if (wide && on && ch < ks.D) v[i][h] = *reinterpret_cast<const uint2*>(q + ch);
-                            }
-                            if (!wide && on) {
+                                const int left = ks.D - 128 * h - 8 * l16;      // channels from this lane's on
+                                v[i][h] = make_uint4(0, 0, 0, 0);
+                                if (wide && on && left > 0) {
+                                    v[i][h] = *reinterpret_cast<const uint4*>(q + 128 * h);
+                                } else if (on && !wide) {
+                                    uint32_t x[8];
 #pragma unroll
-                                for (int k = 0; k < 4 * H; ++k) {
-                                    const int ch = 128 * (k >> 2) + 4 * lane + (k & 3);
-                                    const uint32_t x = ch < ks.D ? (uint32_t)q[ch] << (16 * (k & 1)) : 0u;
-                                    if (k & 2) v[i][k >> 2].y |= x;
-                                    else v[i][k >> 2].x |= x;
+                                    for (int k = 0; k < 8; ++k) x[k] = k < left ? (uint32_t)q[128 * h + k] : 0u;
+                                    v[i][h] = make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
                                 }
                             }
-                            if (++hq == a.group) hq = 0, ++t;
+                            row += 2;
+                            hq += 2;
+#pragma unroll
+                            for (int k = 0; k < 2; ++k)
+                                if (hq >= a.group) hq -= a.group, ++t;
                         }
                     };
-                    uint2 v[4][H];
-                    load(r_first, v);
+                    uint4 v[2][H];
+                    load(v);
 #pragma unroll 1
-                    for (int r0 = r_first; r0 < r_end; r0 += 4) {
-                        uint2 w[4][H];
+                    for (int r0 = r_first + half; r0 < r_end; r0 += 4) {
+                        uint4 w[2][H];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
+                        for (int i = 0; i < 2; ++i)
 #pragma unroll
                             for (int h = 0; h < H; ++h) w[i][h] = v[i][h];
-                        if (r0 + 4 < r_end) load(r0 + 4, v);
+                        if (r0 + 4 < r_end) load(v);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int r = r0 + i;
-                            float x[4 * H];
-                            uint32_t top = 0;
+                        for (int i = 0; i < 2; ++i) {
+                            const int r = r0 + 2 * i;
+                            uint32_t most = 0;      // magnitudes order as their patterns
 #pragma unroll
-                            for (int k = 0; k < 4 * H; ++k) {
-                                const uint32_t pair = k & 2 ? w[i][k >> 2].y : w[i][k >> 2].x;
-                                x[k] = scale_of(k & 1 ? pair >> 16 : pair & 0xFFFFu, bf16);
-                                top = max(top, __float_as_uint(x[k]) & 0x7FFFFFFFu);
-                            }
-                            top = __reduce_max_sync(0xffffffffu, top);
+                            for (int h = 0; h < H; ++h)
+                                most = __vmaxu2(__vmaxu2(__vmaxu2(most, w[i][h].x & 0x7FFF7FFFu), w[i][h].y & 0x7FFF7FFFu),
+                                                __vmaxu2(w[i][h].z & 0x7FFF7FFFu, w[i][h].w & 0x7FFF7FFFu));
+#pragma unroll
+                            for (int k = 8; k; k >>= 1) most = __vmaxu2(most, __shfl_xor_sync(0xffffffffu, most, k));
+                            const uint32_t top = __float_as_uint(scale_of(max(most & 0xFFFFu, most >> 16), bf16));
                             const int e = top == 0 ? 0 : min(13 - ((int)(top >> 23) - 127), 120);
                             const float up = pow2(e);
-                            if (lane == 0) sm_fac[r] = fmaxf(fac0 * pow2(-e), 0x1p-126f);
-                            const uint32_t q = smem0 + (r >> 7) * pl.k_atoms * kQAtom + (r & 127) * 128;
+                            if (l16 == 0) sm_fac[r] = fmaxf(fac0 * pow2(-e), 0x1p-126f);
+                            const uint32_t q = smem0 + (r >> 7) * pl.k_atoms * kQAtom + (r & 127) * 128, sw = (r & 7) << 4;
 #pragma unroll
-                            for (int k = 0; k < 4 * H; ++k) {
-                                if (128 * (k >> 2) + 4 * lane + (k & 3) < ks.D)
-                                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(q + (to[k] ^ ((r & 7) << 4))),
-                                                 "h"(__half_as_ushort(__float2half_rn(x[k] * up * down[k])))
+                            for (int k = 0; k < 8 * H; ++k) {
+                                const uint4& u = w[i][k >> 3];
+                                const uint32_t pair = (k >> 1 & 3) == 0 ? u.x : ((k >> 1 & 3) == 1 ? u.y : ((k >> 1 & 3) == 2 ? u.z : u.w));
+                                const float x = scale_of(k & 1 ? pair >> 16 : pair & 0xFFFFu, bf16);
+                                if (128 * (k >> 3) + 8 * l16 + (k & 7) < ks.D)
+                                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(q + (to[k] ^ sw)),
+                                                 "h"(__half_as_ushort(__float2half_rn(x * (up * down[k]))))
                                                  : "memory");
                             }
                         }
@@ -833,12 +840,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 sm_m[r_tile] = mine > 0 ? m2 : -INFINITY;
                 sm_l[r_tile] = l;
 #pragma unroll 1
-                for (int c = 0; ok && mine > 0 && c < pl.o_cols; c += 8) {
-                    uint32_t v[8];
-                    tc::tmem_ld8(t_s + o_off + c, v);
-                    const int e = c < va0 ? e0 : e1;
+                for (int c = 0; ok && mine > 0 && c < pl.o_cols; c += 16) {
+                    uint32_t v[16];
+                    tc::tmem_ld16(t_s + o_off + c, v);
+                    const float f = pow2(c < va0 ? e0 : e1);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) second[(c + k) * 128 + r_tile] = __uint_as_float(v[k]) * (sm_back[c + k] * pow2(e));
+                    for (int k = 0; k < 16; ++k) second[(c + k) * 128 + r_tile] = __uint_as_float(v[k]) * (sm_back[c + k] * f);
                 }
             }
             bar_group(1, 256);
@@ -860,23 +867,23 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (works && ok) {
                 const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);     // nothing seen: 0; NaN stays
 #pragma unroll 1
-                for (int c = 0; c < pl.o_cols; c += 8) {
-                    uint32_t v[8];
-                    tc::tmem_ld8(t_s + o_off + c, v);
+                for (int c = 0; c < pl.o_cols; c += 16) {
+                    uint32_t v[16];
+                    tc::tmem_ld16(t_s + o_off + c, v);
                     const float f = keep * pow2(c < va0 ? e0 : e1);
-                    float x[8];
+                    float x[16];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
+                    for (int k = 0; k < 16; ++k) {
                         x[k] = __uint_as_float(v[k]) * (sm_back[c + k] * f);
                         if (streams && groups == 2) x[k] = fmaf(second[(c + k) * 128 + r_tile], other, x[k]);
                     }
                     if (whole) {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) stage_out(c + k, x[k] * inv);
+                        for (int k = 0; k < 16; ++k) stage_out(c + k, x[k] * inv);
                     } else {
                         float4* to = reinterpret_cast<float4*>(parts + seg.slot * part_floats) + (int64_t)(c / 4) * unit_rows + unit_row;
-                        to[0] = make_float4(x[0], x[1], x[2], x[3]);
-                        to[unit_rows] = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) to[k * unit_rows] = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
                     }
                 }
                 if (!whole) {
@@ -1084,7 +1091,7 @@ cudaError_t launch_kv_tile(const KvGeom& geo, const KvAttendArgs& a, cudaStream_
     const TilePlan& p = t.pl;
     const int64_t cap = (int64_t)a.max_pages << geo.page_shift;
     const int64_t items = (int64_t)a.B * geo.heads * p.row_units, most = items * (cap / kTok + 1);
-    if (most >= 2147483648ll) return cudaErrorNotSupported;      // chunks are numbered in 32 bits
+    if (most + items * kLead >= 2147483648ll) return cudaErrorNotSupported;      // chunks are numbered in 32 bits
     const int64_t by_size = (most + p.min_chunks - 1) / p.min_chunks, want = by_size > items ? by_size : items;
     const int grid = (int)(want < num_sms() ? want : num_sms());
     KvMaps maps;
