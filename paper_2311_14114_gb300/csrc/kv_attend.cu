@@ -38,7 +38,7 @@ namespace soniq {
 namespace {
 
 constexpr int kChunk = 32;                   // tokens a warp takes at a time
-constexpr int kLead = 16;            // an item's queries and results take about as long as this many chunks
+constexpr int kLead = 32;            // an item's queries and results take about as long as this many chunks
 
 struct RowsPlan {
     int row_tiles;        // tiles of 8 NT query rows per key head
