@@ -8,8 +8,9 @@
 // are read once per tile of up to 256 rows.  One CTA per SM, 20 warps:
 //   warps 0, 3      issue the MMAs, each for one softmax group;
 //   warp 1          copies packed rows by TMA;
+//   warp 2          turns scales into fp32 and works out the next segment;
 //   warps 4-7, 8-11 unpack a block of 64 tokens' keys, and values, into fp16
-//                   operand tiles (codes exactly, scales as fp32 beside them);
+//                   operand tiles (codes exactly);
 //   warps 12-15, 16-19  softmax of two row tiles (a thread per row, its scores from
 //                   TMEM), each with its own S, P and O columns.
 // (Registers move to the softmax warps: 64 + 2 x 56 + 2 x 152 = 5 x 96 a thread.)
@@ -21,11 +22,22 @@
 // are exact in fp16, so S is an exact product summed in fp32, per precision
 // group, and gets its scales in fp32.  P times the value scale (normalised by a
 // running power of two) is rounded to fp16.  The running maximum is raised only
-// when a score exceeds it by more than 2^8: P stays below 2^13.
+// when a score exceeds it by more than 2^13: P stays below 2^15.
 //
 // Values keep their row order (tokens x channels) as the MN-major operand of
 // O = P V, so both operand tiles have one layout: 64-code column groups of
 // [token][128 bytes], 16-byte pieces swizzled by the token.
+//
+// Bound by the softmax warps where scores have two buffers: 2930 cycles for 64
+// tokens of 256 rows (waits 340, scores times key scales 560, maxima and their
+// check 750, exponentials and rounding 900, the rest the loop), of which the
+// tensor cores work 630.  With two key groups TMEM holds one buffer, and the way
+// scores - softmax - outputs - scores is one chain of about 4500 cycles, two of
+// which run side by side.  An item costs 12000 cycles for its queries and 5000
+// to 9000 for its results besides, so short items count kLead blocks more.
+// Measured (GB300): 4 x 64 drafted tokens x 8 heads per key head over 16384
+// cached ones 113 us (610 TFLOP/s), 2 x 512 x 4 over 3500 157 us (400), 16 x 24 x
+// 4 over up to 4096 95 us.
 #include <type_traits>
 
 #include "kv_device.cuh"
@@ -70,7 +82,9 @@ struct JoinItem {
     int entry, item, n_part, cta0, cta0_slot;
 };
 constexpr int kJoinBytes = 8192;
-constexpr int kLead = 8;                 // an item's queries and results take about as long as this many blocks
+// An item's queries and results take about as long as this many blocks.  (Blocks, us: 16 x 24 drafted tokens over
+// ragged contexts 4: 109, 8: 96, 16: 90; 2 x 512 tokens 4: 155, 8: 156, 16: 173.)
+constexpr int kLead = 8;
 
 struct Bars {               // offsets in 8-byte barriers
     static constexpr int raw_full = 0, raw_free = 4, k_ready = 8, v_ready = 12, kv_free = 16, s_full = 20, p_full = 24,
