@@ -334,7 +334,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     JoinItem* join = reinterpret_cast<JoinItem*>(static_cast<uint8_t*>(a.scratch) + SONIQ_KV_SCRATCH_ZERO) + blockIdx.x;
     const bool any = split.begin(chunks, a.B * pl.row_units, geo.heads, pl.min_chunks, kLead, 8, words);
     if (tid == 0) join->n_part = 0;
-    if (!any) return;
+    if (!any) {
+        check_lengths(geo, a, tid, kThreads);
+        return;
+    }
 
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(tmem_at)), "r"(512) : "memory");
