@@ -543,6 +543,8 @@ SONIQ_API soniq_status soniq_kv_read(const soniq_kv_cache *cache, const int64_t 
  *              before the first use; every completed call leaves them zero (zero
  *              them again after a SONIQ_ERR_TIMEOUT).
  *              Calls that may overlap on the GPU must use different scratch.
+ * What the cache holds of a token that no row sees does not matter; a value scale
+ * that soniq_kv_write cannot have left (negative, not finite) counts as 0.
  * Scores, statistics and sums are fp32; softmax weights (times the value
  * scale, normalised by a power of two) are rounded to fp16 for the product.
  */

@@ -380,10 +380,10 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                 }
                 if (vs.ng == 2) {
                     const uint32_t w = lds32(s_at + vs_lane);
-                    v0 = scale_of(w & 0xFFFFu, bf16);
-                    v1 = scale_of(w >> 16, bf16);
+                    v0 = value_scale(w & 0xFFFFu, bf16);
+                    v1 = value_scale(w >> 16, bf16);
                 } else {
-                    v0 = scale_of(lds16(s_at + vs_lane), bf16);
+                    v0 = value_scale(lds16(s_at + vs_lane), bf16);
                 }
                 if (tail && p0 + lane >= end) k0 = k1 = v0 = v1 = 0.0f;
                 // positive floats order as integers; the exponent plus one bounds them

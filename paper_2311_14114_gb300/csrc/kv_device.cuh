@@ -95,6 +95,12 @@ __device__ __forceinline__ uint32_t mask_flip(uint32_t x, uint32_t m, uint32_t f
 __device__ __forceinline__ float scale_of(uint32_t bits16, bool bf16) {
     return bf16 ? __uint_as_float(bits16 << 16) : __half2float(__ushort_as_half((uint16_t)bits16));
 }
+// A cached value scale.  One that no write leaves (negative, not finite) counts as 0: it may stand behind a token
+// that no row sees, and would spread through the common power of two of its block.
+__device__ __forceinline__ float value_scale(uint32_t bits16, bool bf16) {
+    const float x = scale_of(bits16, bf16);
+    return x >= 0.0f && x < INFINITY ? x : 0.0f;
+}
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
 
 

@@ -524,8 +524,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int grp = 0; grp < (side ? VNG : KNG); ++grp) {
                         float x[2];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            x[h] = p0 + lane + 32 * h < end ? scale_of(lds16(src + from[side][h] + 2 * grp), bf16) : 0.0f;
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t raw16 = lds16(src + from[side][h] + 2 * grp);
+                            x[h] = p0 + lane + 32 * h >= end ? 0.0f : (side ? value_scale(raw16, bf16) : scale_of(raw16, bf16));
+                        }
                         float f = pow2(1 - geo.s[side].bits[grp]);
                         if (side) {
                             const uint32_t big = __reduce_max_sync(0xffffffffu, max(__float_as_uint(x[0]), __float_as_uint(x[1])));

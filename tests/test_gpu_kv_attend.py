@@ -275,3 +275,21 @@ def test_nan_query_stays_in_its_row(sq):
     assert torch.isnan(out[0, 1, 6]).all()
     out[0, 1, 6] = want[0, 1, 6]
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("poison", [float("nan"), float("inf"), -1.0])
+@pytest.mark.parametrize("shape", [0, 1])
+@pytest.mark.parametrize("T,group", [(4, 1), (40, 4)])
+def test_hidden_drafts_may_hold_anything(sq, T, group, shape, poison):
+    """A draft that no row sees: whatever stands in its slot, the outputs are those without it."""
+    p = Problem(sq, 36, LAYOUTS[shape], [70, 0], T, group, 16, torch.float16)
+    m = tree(p.rng, 2, T)
+    m[:, :, 2] = False
+    run(sq, p, m)
+    for b in range(2):
+        pos = int(p.lens[b]) + 2
+        page, at = int(p.table[b, pos // 16]), pos % 16
+        for codes, scales in ((p.cache.k_codes, p.cache.k_scales), (p.cache.v_codes, p.cache.v_scales)):
+            codes[page, :, at] = 0x81
+            scales[page, :, at] = poison
+    run(sq, p, m)
