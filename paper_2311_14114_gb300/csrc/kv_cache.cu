@@ -20,7 +20,7 @@
 // which is why the loop is compiled once for each way to reach a row) and, when
 // reading, by the latency of the packed words.  Measured (GB300, bf16, 8 heads of
 // 128 channels, mostly 4 bits): 16384 tokens written 33 us (2.6 TB/s of rows and
-// codes), 65536 read 134 us (2.6 TB/s); 777 tokens read 4.8 us.
+// codes), 65536 read 123 us (2.8 TB/s); 777 tokens read 4.8 us.
 #include "kv_internal.h"
 #include "soniq_device.cuh"
 
@@ -124,12 +124,12 @@ __device__ __forceinline__ float2 load2(uint32_t x) {
 template <int LPR, bool BF16>
 __global__ void __launch_bounds__(kThreads, 3) kv_write_kernel(const KvGeom geo, const KvRowsArg k, const KvRowsArg v,
                                                             const int64_t* __restrict__ slots, int64_t n, int per_warp,
-                                                            unsigned* err) {
+                                                            int side0, unsigned* err) {
     constexpr int RPW = 32 / LPR;
     constexpr uint32_t INF = BF16 ? 0x7F80u : 0x7C00u;
     __shared__ __align__(16) uint8_t rows[kWarps][RPW][kStride];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int head = blockIdx.y, side = blockIdx.z, ql = lane & (LPR - 1);
+    const int head = blockIdx.y, side = side0 + blockIdx.z, ql = lane & (LPR - 1);
     const KvSide s = side ? geo.s[1] : geo.s[0];
     const KvRowsArg in = side ? v : k;
     const Lane me = make_lane<LPR>(s, head);
@@ -275,11 +275,11 @@ __device__ __forceinline__ void unpack8(const uint32_t (&w)[2], int bits, float 
 
 template <int LPR, bool BF16>
 __global__ void __launch_bounds__(kThreads) kv_read_kernel(const KvGeom geo, const int64_t* __restrict__ slots, int64_t n,
-                                                           int per_warp, uint16_t* k, uint16_t* v, unsigned* err) {
+                                                           int per_warp, int side0, uint16_t* k, uint16_t* v, unsigned* err) {
     constexpr int RPW = 32 / LPR;
     __shared__ __align__(16) uint8_t rows[kWarps][RPW][kStride];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int head = blockIdx.y, side = blockIdx.z, ql = lane & (LPR - 1);
+    const int head = blockIdx.y, side = side0 + blockIdx.z, ql = lane & (LPR - 1);
     const KvSide s = side ? geo.s[1] : geo.s[0];
     uint16_t* out = side ? v : k;
     if (out == nullptr) return;
@@ -371,61 +371,79 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(const KvGeom geo, con
 // as many tokens to each as there are.  16384 tokens written and read, us: 59 so,
 // 68 with twice as many warps, 78 with a wave for writing and two for reading.
 struct Shape {
-    int lpr, per_warp;
+    int lpr, per_warp, side0;
     dim3 grid;
 };
-bool make_shape(const KvGeom& geo, int64_t n, int warps_per_sm, Shape* sh) {
-    int eighths = 0;
-    for (const KvSide& s : geo.s) eighths = 4 * (s.nb[0] + s.nb[1]) > eighths ? 4 * (s.nb[0] + s.nb[1]) : eighths;
-    sh->lpr = 4;
-    while (sh->lpr < eighths) sh->lpr *= 2;
-    const int64_t rpw = 32 / sh->lpr, steps = (n + rpw - 1) / rpw * geo.heads * 2;
-    int64_t iters = (steps + (int64_t)num_sms() * warps_per_sm - 1) / ((int64_t)num_sms() * warps_per_sm);
-    const int64_t most = 1024;
-    iters = iters < 1 ? 1 : (iters > most ? most : iters);
-    sh->per_warp = (int)(iters * rpw);
-    const int64_t blocks = (n + (int64_t)kWarps * sh->per_warp - 1) / ((int64_t)kWarps * sh->per_warp);
-    if (blocks > 2147483647) return false;
-    sh->grid = dim3((unsigned)blocks, (unsigned)geo.heads, 2);
-    return true;
+int lanes_of(const KvSide& s) {
+    int lpr = 4;
+    while (lpr < 4 * (s.nb[0] + s.nb[1])) lpr *= 2;
+    return lpr;
+}
+// Keys and values in one launch, or, where their rows take different numbers of
+// lanes and there are enough of them to repay it, in one each (20 and 16 lanes, 8
+// heads, together and apart, us: 8192 tokens written and read 50 and 54, 16384 93
+// and 89, 65536 336 and 290, read alone 134 and 123).
+constexpr int64_t kApart = 131072;
+int make_shapes(const KvGeom& geo, int64_t n, int warps_per_sm, Shape (&shapes)[2]) {
+    const int lpr[2] = {lanes_of(geo.s[0]), lanes_of(geo.s[1])};
+    const int launches = lpr[0] != lpr[1] && n * geo.heads >= kApart ? 2 : 1, sides = 2 / launches;
+    for (int i = 0; i < launches; ++i) {
+        Shape* sh = &shapes[i];
+        sh->side0 = i;
+        sh->lpr = launches == 2 ? lpr[i] : (lpr[0] > lpr[1] ? lpr[0] : lpr[1]);
+        const int64_t rpw = 32 / sh->lpr, steps = (n + rpw - 1) / rpw * geo.heads * sides;
+        int64_t iters = (steps + (int64_t)num_sms() * warps_per_sm - 1) / ((int64_t)num_sms() * warps_per_sm);
+        iters = iters < 1 ? 1 : (iters > 1024 ? 1024 : iters);
+        sh->per_warp = (int)(iters * rpw);
+        const int64_t blocks = (n + (int64_t)kWarps * sh->per_warp - 1) / ((int64_t)kWarps * sh->per_warp);
+        if (blocks > 2147483647) return 0;
+        sh->grid = dim3((unsigned)blocks, (unsigned)geo.heads, (unsigned)sides);
+    }
+    return launches;
 }
 
 template <bool BF16>
 void run_write(const Shape& sh, const KvGeom& geo, const KvRowsArg& k, const KvRowsArg& v, const int64_t* slots, int64_t n,
                unsigned* err, cudaStream_t st) {
-    if (sh.lpr == 32) kv_write_kernel<32, BF16><<<sh.grid, kThreads, 0, st>>>(geo, k, v, slots, n, sh.per_warp, err);
-    else if (sh.lpr == 16) kv_write_kernel<16, BF16><<<sh.grid, kThreads, 0, st>>>(geo, k, v, slots, n, sh.per_warp, err);
-    else if (sh.lpr == 8) kv_write_kernel<8, BF16><<<sh.grid, kThreads, 0, st>>>(geo, k, v, slots, n, sh.per_warp, err);
-    else kv_write_kernel<4, BF16><<<sh.grid, kThreads, 0, st>>>(geo, k, v, slots, n, sh.per_warp, err);
+    if (sh.lpr == 32) kv_write_kernel<32, BF16><<<sh.grid, kThreads, 0, st>>>(geo, k, v, slots, n, sh.per_warp, sh.side0, err);
+    else if (sh.lpr == 16) kv_write_kernel<16, BF16><<<sh.grid, kThreads, 0, st>>>(geo, k, v, slots, n, sh.per_warp, sh.side0, err);
+    else if (sh.lpr == 8) kv_write_kernel<8, BF16><<<sh.grid, kThreads, 0, st>>>(geo, k, v, slots, n, sh.per_warp, sh.side0, err);
+    else kv_write_kernel<4, BF16><<<sh.grid, kThreads, 0, st>>>(geo, k, v, slots, n, sh.per_warp, sh.side0, err);
 }
 template <bool BF16>
 void run_read(const Shape& sh, const KvGeom& geo, const int64_t* slots, int64_t n, uint16_t* k, uint16_t* v, unsigned* err,
               cudaStream_t st) {
-    if (sh.lpr == 32) kv_read_kernel<32, BF16><<<sh.grid, kThreads, 0, st>>>(geo, slots, n, sh.per_warp, k, v, err);
-    else if (sh.lpr == 16) kv_read_kernel<16, BF16><<<sh.grid, kThreads, 0, st>>>(geo, slots, n, sh.per_warp, k, v, err);
-    else if (sh.lpr == 8) kv_read_kernel<8, BF16><<<sh.grid, kThreads, 0, st>>>(geo, slots, n, sh.per_warp, k, v, err);
-    else kv_read_kernel<4, BF16><<<sh.grid, kThreads, 0, st>>>(geo, slots, n, sh.per_warp, k, v, err);
+    if (sh.lpr == 32) kv_read_kernel<32, BF16><<<sh.grid, kThreads, 0, st>>>(geo, slots, n, sh.per_warp, sh.side0, k, v, err);
+    else if (sh.lpr == 16) kv_read_kernel<16, BF16><<<sh.grid, kThreads, 0, st>>>(geo, slots, n, sh.per_warp, sh.side0, k, v, err);
+    else if (sh.lpr == 8) kv_read_kernel<8, BF16><<<sh.grid, kThreads, 0, st>>>(geo, slots, n, sh.per_warp, sh.side0, k, v, err);
+    else kv_read_kernel<4, BF16><<<sh.grid, kThreads, 0, st>>>(geo, slots, n, sh.per_warp, sh.side0, k, v, err);
 }
 
 }  // namespace
 
 cudaError_t launch_kv_write(const KvGeom& geo, const KvRowsArg& k, const KvRowsArg& v, const int64_t* slots, int64_t n,
                             unsigned* err, cudaStream_t st) {
-    Shape sh;
-    if (!make_shape(geo, n, 48, &sh)) return cudaErrorNotSupported;
-    if (geo.bf16) run_write<true>(sh, geo, k, v, slots, n, err, st);
-    else run_write<false>(sh, geo, k, v, slots, n, err, st);
-    note_launch();
+    Shape shapes[2];
+    const int launches = make_shapes(geo, n, 48, shapes);
+    if (launches == 0) return cudaErrorNotSupported;
+    for (int i = 0; i < launches; ++i) {
+        if (geo.bf16) run_write<true>(shapes[i], geo, k, v, slots, n, err, st);
+        else run_write<false>(shapes[i], geo, k, v, slots, n, err, st);
+        note_launch();
+    }
     return cudaGetLastError();
 }
 
 cudaError_t launch_kv_read(const KvGeom& geo, const int64_t* slots, int64_t n, uint16_t* k, uint16_t* v, unsigned* err,
                            cudaStream_t st) {
-    Shape sh;
-    if (!make_shape(geo, n, 32, &sh)) return cudaErrorNotSupported;
-    if (geo.bf16) run_read<true>(sh, geo, slots, n, k, v, err, st);
-    else run_read<false>(sh, geo, slots, n, k, v, err, st);
-    note_launch();
+    Shape shapes[2];
+    const int launches = make_shapes(geo, n, 32, shapes);
+    if (launches == 0) return cudaErrorNotSupported;
+    for (int i = 0; i < launches; ++i) {
+        if (geo.bf16) run_read<true>(shapes[i], geo, slots, n, k, v, err, st);
+        else run_read<false>(shapes[i], geo, slots, n, k, v, err, st);
+        note_launch();
+    }
     return cudaGetLastError();
 }
 

@@ -232,3 +232,25 @@ def test_refusals(sq):
             sq.kv_write(cache, *bad_args)
     with pytest.raises(ValueError):
         sq.kv_read(cache, slots, k=torch.empty(2, 1, 64, dtype=torch.float16, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_many_rows_of_unequal_sides(sq, dtype):
+    """Keys' rows take more lanes than values': many tokens at once equal the same tokens in small calls."""
+    rng = np.random.default_rng(16)
+    n, shape = 16384 + 21, (8, 128, 128, ([112, 16], [4, 8]), ([128], [4]))
+    caches = [make_cache(sq, np.random.default_rng(17), shape, n // 16 + 2, 16, dtype) for _ in range(2)]
+    k, v = (torch.from_numpy(rng.standard_normal((n, 8, 128)).astype(np.float32)).to(dtype).cuda() for _ in range(2))
+    slots = torch.from_numpy(rng.permutation(n + 16)[:n]).cuda()
+    slots[5] = -1
+    sq.kv_write(caches[0], k, v, slots)
+    for i in range(0, n, 4001):
+        sq.kv_write(caches[1], k[i:i + 4001], v[i:i + 4001], slots[i:i + 4001])
+    for name in ("k_codes", "k_scales", "v_codes", "v_scales"):
+        assert torch.equal(getattr(caches[0], name), getattr(caches[1], name))
+    got = sq.kv_read(caches[0], slots)
+    for i in range(0, n, 4001):
+        part = sq.kv_read(caches[1], slots[i:i + 4001].contiguous())
+        for a, b in zip(got, part):
+            assert torch.equal(a[i:i + 4001], b)
+    assert sq.sync_status() == 0

@@ -71,3 +71,12 @@ def test_one_group_a_side_over_long_contexts(sq):
                                               128 ** -0.5)
         tol = base.plain.tolerance(o, mag, ds, total, n + t + 1, np.abs(vv).max(), torch.float16)
         assert (np.abs(first[:, t:t + 1].double().cpu().numpy() - o) <= tol).all()
+
+
+@pytest.mark.parametrize("T,group", [(40, 4), (9, 16)])
+@pytest.mark.parametrize("shape", [(1, 256, 64, ([256], [2]), ([64], [4])), (2, 256, 128, ([256], [4]), ([128], [4])),
+                                   (1, 256, 128, ([256], [4]), ([128], [8])), (1, 256, 256, ([192, 64], [4, 8]), ([256], [8]))])
+def test_many_rows_of_wide_heads(sq, shape, T, group):
+    """More than 128 rows per key head of 256 channels: two tiles of queries leave no room for a ring of operands."""
+    p = base.Problem(sq, 45, shape, [0, 130, 777], T, group, 16, torch.float16)
+    attend_into_nan(sq, p)
