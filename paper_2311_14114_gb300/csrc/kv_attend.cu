@@ -32,8 +32,8 @@
 // Bound by instructions, about 800 for a chunk of 32 tokens (keys 4/8 bits,
 // values 4, 128 channels, 8 rows) at 2.5 a cycle, and for short contexts by what
 // comes before and after: the split, queries, and the joins take 10 to 20 us.
-// Measured (GB300): 131071 tokens of one sequence, 8 key heads: 57 us (2.8 TB/s);
-// 64 sequences of up to 8192 tokens: 119 us (2.8 TB/s); 97 tokens: 12 us.
+// Measured (GB300): 131071 tokens of one sequence, 8 key heads: 58 us (2.7 TB/s);
+// 64 sequences of up to 8192 tokens: 121 us (2.8 TB/s); 97 tokens: 12 us.
 #include <type_traits>
 
 #include "kv_device.cuh"

@@ -36,8 +36,8 @@
 // which run side by side.  An item costs 12000 cycles for its queries and 5000
 // to 9000 for its results besides, so short items count kLead blocks more.
 // Measured (GB300): 4 x 64 drafted tokens x 8 heads per key head over 16384
-// cached ones 113 us (610 TFLOP/s), 2 x 512 x 4 over 3500 157 us (400), 16 x 24 x
-// 4 over up to 4096 95 us.
+// cached ones 114 us (600 TFLOP/s), 2 x 512 x 4 over 3500 158 us (400), 16 x 24 x
+// 4 over up to 4096 96 us.
 #include <type_traits>
 
 #include "kv_device.cuh"
