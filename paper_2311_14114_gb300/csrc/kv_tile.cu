@@ -807,8 +807,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 e0 = n0;
                 e1 = n1;
                 // weights, times 2^(block's power - running power); over the scores that are done with: the first
-                // value group's from column 0, the second's from the second key group's place
-                const int d0 = max(b0 - e0, -126), dd = b1 - e1 - d0;
+                // value group's from column 0, the second's from the second key group's place.  The sum and the second
+                // group are made of the same numbers, so the power stops where the first group's round to 0 in fp16
+                // (below 2^(13 - 40)): a block of small or zero values still counts.
+                const int d0 = max(b0 - e0, -40), dd = b1 - e1 - d0;
                 const float shift = (m == -INFINITY ? 0.0f : -m * fac) + (float)d0;
                 const float second = dd < -126 ? 0.0f : pow2(min(dd, 127));
                 float2 sums[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
