@@ -629,7 +629,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
             return;
         }
         const bool whole = n_part == 1;
-        constexpr int PART = R * (32 * NVB + 2);      // floats of a partial result: outputs, then m, then l
+        constexpr int PART = R * (32 * NVB + 2);      // floats of a partial result: outputs (divided by l), then m, then l
         float* parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.scratch) + SONIQ_KV_SCRATCH_ZERO);
         float* part = parts + (int64_t)seg.slot * PART;
         if (tid < R) {
@@ -640,23 +640,27 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                 ll += sm_l[wi * R + tid] * (mw == -INFINITY ? 0.0f : ex2(mw - mm));
             }
             sm_tm[tid] = mm;
-            sm_tl[tid] = ll;
+            sm_tl[tid] = inverse(ll);
             if (!whole) {
                 part[R * 32 * NVB + tid] = mm;
                 part[R * 32 * NVB + R + tid] = ll;
             }
         }
         __syncthreads();
-        float join[NT][2];      // 2^(m - the CTA's m)
+        // 2^(m - the CTA's m) / the CTA's sum: results are averages from here on, which are representable where sums
+        // of values near the end of the type's range are not
+        float join[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int r = 0; r < 2; ++r) join[nt][r] = m[nt][r] == -INFINITY ? 0.0f : ex2(m[nt][r] - sm_tm[8 * nt + 2 * l + r]);
-        auto store = [&](int r, int p, float v, float ll) {
+            for (int r = 0; r < 2; ++r) {
+                const int row = 8 * nt + 2 * l + r;
+                join[nt][r] = (m[nt][r] == -INFINITY ? 0.0f : ex2(m[nt][r] - sm_tm[row])) * sm_tl[row];
+            }
+        auto store = [&](int r, int p, float v) {
             const int row = row0 + r, ch = sm_chan[p];
             if (row < pl.rows && ch >= 0) {
                 const int64_t at = (((int64_t)b * a.T + row / a.group) * qh + head * a.group + row % a.group) * vs.D + ch;
-                v = ll > 0.0f ? v / ll : (ll == 0.0f ? 0.0f : ll);      // nothing seen: 0; NaN stays
                 a.out[at] = bf16 ? kv_round<true>(v) : kv_round<false>(v);
             }
         };
@@ -689,7 +693,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                 if (p >= 32 * nvb) continue;
                 float sum = 0.0f;
                 for (int wi = 0; wi < n_warps; ++wi) sum += merge[wi * R * PB * 32 + i];
-                if (whole) store(r, p, sum, sm_tl[r]);
+                if (whole) store(r, p, sum);
                 else part[r * 32 * NVB + p] = sum;
             }
             __syncthreads();
@@ -708,7 +712,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
             if (sm_last) {
                 __threadfence();
                 auto part_of = [&](int i) { return parts + (int64_t)part_slot(seg, i) * PART; };
-                float* fp = merge;                      // [n_part][R]: each part's factor
+                float* fp = merge;                      // [n_part][R]: each part's share of the sum
                 for (int i = tid; i < n_part * R; i += blockDim.x) fp[i] = __ldcg(part_of(i / R) + R * 32 * NVB + i % R);
                 __syncthreads();
                 for (int r = warp; r < R; r += n_warps) {
@@ -716,12 +720,13 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                     for (int i = lane; i < n_part; i += 32) mm = fmaxf(mm, fp[i * R + r]);
                     for (int i = 16; i; i >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, i));
                     for (int i = lane; i < n_part; i += 32) {
-                        const float mc = fp[i * R + r], f = mc == -INFINITY ? 0.0f : ex2(mc - mm);
-                        ll += f * __ldcg(part_of(i) + R * 32 * NVB + R + r);
+                        const float mc = fp[i * R + r];
+                        const float f = (mc == -INFINITY ? 0.0f : ex2(mc - mm)) * __ldcg(part_of(i) + R * 32 * NVB + R + r);
+                        ll += f;
                         fp[i * R + r] = f;
                     }
                     for (int i = 16; i; i >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, i);
-                    if (lane == 0) sm_tl[r] = ll;
+                    for (int i = lane; i < n_part; i += 32) fp[i * R + r] *= inverse(ll);
                 }
                 __syncthreads();
                 // four outputs to a thread; parts split over the threads that are left, and joined in order
@@ -754,11 +759,10 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                             acc.z += q.z;
                             acc.w += q.w;
                         }
-                        const float ll = sm_tl[r];
-                        store(r, p, acc.x, ll);
-                        store(r, p + 1, acc.y, ll);
-                        store(r, p + 2, acc.z, ll);
-                        store(r, p + 3, acc.w, ll);
+                        store(r, p, acc.x);
+                        store(r, p + 1, acc.y);
+                        store(r, p + 2, acc.z);
+                        store(r, p + 3, acc.w);
                     }
                     __syncthreads();
                 }

@@ -101,6 +101,8 @@ __device__ __forceinline__ float value_scale(uint32_t bits16, bool bf16) {
     const float x = scale_of(bits16, bf16);
     return x >= 0.0f && x < INFINITY ? x : 0.0f;
 }
+// 1 / a softmax sum; nothing seen: 0; NaN stays.
+__device__ __forceinline__ float inverse(float l) { return l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l); }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
 
 

@@ -855,7 +855,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::tc_fence_after();
             const bool works = s < (streams ? 1 : groups);          // this group has a tile's results
             const bool whole = seg.n_part == 1;
-            float m2 = m == -INFINITY ? m : m * fac, keep = 1.0f, other = 0.0f;     // in units of the exponent
+            // Results are averages from here on, which are representable where sums of values near the end of the type's
+            // range are not.
+            float m2 = m == -INFINITY ? m : m * fac, inv = inverse(l), other = 0.0f;     // m2: in units of the exponent
             float* second = reinterpret_cast<float*>(smem);       // [o_cols][128]: the second stream's outputs
             if (streams && s == 1) {
                 sm_m[r_tile] = mine > 0 ? m2 : -INFINITY;
@@ -866,15 +868,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tc::tmem_ld16(t_s + o_off + c, v);
                     const float f = pow2(c < va0 ? e0 : e1);
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) second[(c + k) * 128 + r_tile] = __uint_as_float(v[k]) * (sm_back[c + k] * f);
+                    for (int k = 0; k < 16; ++k) second[(c + k) * 128 + r_tile] = (__uint_as_float(v[k]) * inv) * (sm_back[c + k] * f);
                 }
             }
             bar_group(1, 256);
             if (streams && s == 0 && groups == 2) {
                 const float m1 = sm_m[r_tile], mm = fmaxf(m2, m1);
-                keep = m2 == -INFINITY ? 0.0f : ex2(m2 - mm);
-                other = m1 == -INFINITY ? 0.0f : ex2(m1 - mm);
-                l = l * keep + sm_l[r_tile] * other;
+                const float keep = m2 == -INFINITY ? 0.0f : ex2(m2 - mm);
+                other = (m1 == -INFINITY ? 0.0f : ex2(m1 - mm)) * sm_l[r_tile];
+                l = l * keep + other;
+                inv = inverse(l) * keep;
+                other *= inverse(l);
                 m2 = mm;
             }
             const int unit_row = (streams ? 0 : 128 * s) + r_tile;
@@ -886,21 +890,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (ch >= 0) *reinterpret_cast<uint16_t*>(staged + r_tile * pl.out_stride + 2 * ch) = bf16 ? kv_round<true>(v) : kv_round<false>(v);
             };
             if (works && ok) {
-                const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);     // nothing seen: 0; NaN stays
 #pragma unroll 1
                 for (int c = 0; c < pl.o_cols; c += 16) {
                     uint32_t v[16];
                     tc::tmem_ld16(t_s + o_off + c, v);
-                    const float f = keep * pow2(c < va0 ? e0 : e1);
+                    const float f = pow2(c < va0 ? e0 : e1);
                     float x[16];
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
-                        x[k] = __uint_as_float(v[k]) * (sm_back[c + k] * f);
+                        x[k] = (__uint_as_float(v[k]) * inv) * (sm_back[c + k] * f);
                         if (streams && groups == 2) x[k] = fmaf(second[(c + k) * 128 + r_tile], other, x[k]);
                     }
                     if (whole) {
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) stage_out(c + k, x[k] * inv);
+                        for (int k = 0; k < 16; ++k) stage_out(c + k, x[k]);
                     } else {
                         float4* to = reinterpret_cast<float4*>(parts + seg.slot * part_floats) + (int64_t)(c / 4) * unit_rows + unit_row;
 #pragma unroll
@@ -1011,21 +1014,23 @@ __global__ void __launch_bounds__(kJoinThreads) kv_join_kernel(const KvGeom geo,
     };
     auto m_of = [&](int i) { return part(i)[(int64_t)unit_rows * pl.o_cols + unit_row]; };
     float mm = -INFINITY, ll = 0.0f;
+    // a part's sum in units of the item's maximum
+    auto sum_of = [&](int i) {
+        const float mi = m_of(i);
+        return part(i)[(int64_t)unit_rows * (pl.o_cols + 1) + unit_row] * (mi == -INFINITY ? 0.0f : ex2(mi - mm));
+    };
 #pragma unroll 4
     for (int i = 0; i < it.n_part; ++i) mm = fmaxf(mm, m_of(i));
 #pragma unroll 4
-    for (int i = 0; i < it.n_part; ++i) {
-        const float mi = m_of(i);
-        ll += part(i)[(int64_t)unit_rows * (pl.o_cols + 1) + unit_row] * (mi == -INFINITY ? 0.0f : ex2(mi - mm));
-    }
-    const float inv = ll > 0.0f ? 1.0f / ll : (ll == 0.0f ? 0.0f : ll);      // nothing seen: 0; NaN stays
+    for (int i = 0; i < it.n_part; ++i) ll += sum_of(i);
+    const float inv = inverse(ll);
     __syncthreads();
     for (int c = 4 * warp; c < pl.o_cols; c += 4 * (kJoinThreads / 32)) {
         float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
         for (int i = 0; i < it.n_part; ++i) {
             const float4 q = *(reinterpret_cast<const float4*>(part(i)) + (int64_t)(c / 4) * unit_rows + unit_row);
-            const float mi = m_of(i), f = mi == -INFINITY ? 0.0f : ex2(mi - mm);
+            const float f = sum_of(i) * inv;
             x.x = fmaf(f, q.x, x.x);
             x.y = fmaf(f, q.y, x.y);
             x.z = fmaf(f, q.z, x.z);
@@ -1035,7 +1040,7 @@ __global__ void __launch_bounds__(kJoinThreads) kv_join_kernel(const KvGeom geo,
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int ch = chan[c + k];
-            if (ch >= 0) *reinterpret_cast<uint16_t*>(staged + lane * pl.out_stride + 2 * ch) = bf16 ? kv_round<true>(y[k] * inv) : kv_round<false>(y[k] * inv);
+            if (ch >= 0) *reinterpret_cast<uint16_t*>(staged + lane * pl.out_stride + 2 * ch) = bf16 ? kv_round<true>(y[k]) : kv_round<false>(y[k]);
         }
     }
     __syncthreads();
