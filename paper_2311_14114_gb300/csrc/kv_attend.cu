@@ -26,8 +26,8 @@
 //    instruction): their sums run over tokens, where the offset would swamp a
 //    small average.
 //  * Queries are scaled per row by a power of two to 2^13 (bf16 queries are
-//    exact in fp16 then), softmax weights times value scales by a running power
-//    of two (the largest scale met), so no range of either type is lost.
+//    exact in fp16 then).  Softmax weights times value scales are rounded to fp16
+//    relative to a power of two of the row's own (kv_device.cuh).
 //
 // Bound by instructions, about 800 for a chunk of 32 tokens (keys 4/8 bits,
 // values 4, 128 channels, 8 rows) at 2.5 a cycle, and for short contexts by what
@@ -326,8 +326,9 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
         }
         __syncthreads();
 
-        // running maximum (of scores before the row's factor), sum and outputs
-        float fac[NT][2], init[2][NT][2], m[NT][2], lsum[NT][2];
+        // A row's running maximum (a whole number, in units of the exponent), sum, outputs and, for each value group, the
+        // power of two that its outputs and weights are relative to, counted from the maximum (RowPower).
+        float fac[NT][2], init[2][NT][2], m[NT][2], lsum[NT][2], power[2][NT][2];
         float o[NVB][2][NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -336,7 +337,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                 fac[nt][r] = sm_fac[8 * nt + 2 * l + r];
                 init[0][nt][r] = sm_init[8 * nt + 2 * l + r];
                 init[1][nt][r] = sm_init[R + 8 * nt + 2 * l + r];
-                m[nt][r] = -INFINITY;
+                m[nt][r] = power[0][nt][r] = power[1][nt][r] = kUnset;
                 lsum[nt][r] = 0.0f;
             }
         }
@@ -348,7 +349,6 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[v][u][nt][i] = 0.0f;
-        int e0 = -100, e1 = -100;     // running powers of two above the value scales
 
         const uint32_t qbase = smem0 + pl.q_off + lane * 16;
         const int sure = min(len, end);
@@ -368,7 +368,8 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
             phases ^= 1u << stage;
             flying &= ~(1u << stage);
 
-            // ---- scales: lane = token; as fp32 for all lanes, the values' relative to the running power of two ----
+            // ---- scales: lane = token; as fp32 for all lanes ----
+            float room[2];      // of a row's largest weight over its power, for each value group
             {
                 float k0, k1 = 0.0f, v0, v1 = 0.0f;
                 if (ks.ng == 2) {
@@ -386,25 +387,10 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                     v0 = value_scale(lds16(s_at + vs_lane), bf16);
                 }
                 if (tail && p0 + lane >= end) k0 = k1 = v0 = v1 = 0.0f;
-                // positive floats order as integers; the exponent plus one bounds them
-                const int n0 = max(e0, min((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(v0)) >> 23) - 126, 126));
-                int n1 = e1;
-                if (vs.ng == 2) n1 = max(e1, min((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(v1)) >> 23) - 126, 126));
-                if (n0 > e0 || n1 > e1) {
-                    const float d0 = n0 - e0 > 126 ? 0.0f : pow2(e0 - n0), d1 = n1 - e1 > 126 ? 0.0f : pow2(e1 - n1);
-                    e0 = n0;
-                    e1 = n1;
-#pragma unroll
-                    for (int v = 0; v < NVB; ++v)
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) o[v][u][nt][i] *= v < vs.nb[0] ? d0 : d1;
-                }
+                room[0] = kRoom - scale_bound(__reduce_max_sync(0xffffffffu, __float_as_uint(v0)));
+                room[1] = vs.ng == 2 ? kRoom - scale_bound(__reduce_max_sync(0xffffffffu, __float_as_uint(v1))) : INFINITY;
                 __syncwarp();
-                sts128f(fsc + 16 * lane, k0, k1, v0 * pow2(-e0), v1 * pow2(-e1));
+                sts128f(fsc + 16 * lane, k0, k1, v0, v1);
                 __syncwarp();
             }
             float4 sc[4];      // of tokens g, g + 8, g + 16, g + 24
@@ -499,40 +485,72 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                     tp = fmaxf(tp, __shfl_xor_sync(0xffffffffu, tp, 4));
                     tp = fmaxf(tp, __shfl_xor_sync(0xffffffffu, tp, 8));
                     tp = fmaxf(tp, __shfl_xor_sync(0xffffffffu, tp, 16));
-                    grows |= tp > m[nt][r];
-                    top[nt][r] = tp;
+                    top[nt][r] = tp * fac[nt][r];
+                    grows |= top[nt][r] > m[nt][r];
                 }
             if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const float mn = fmaxf(m[nt][r], top[nt][r]);
-                        const float al = mn == -INFINITY ? 1.0f : ex2((m[nt][r] - mn) * fac[nt][r]);
-                        m[nt][r] = mn;
-                        lsum[nt][r] *= al;
-#pragma unroll
-                        for (int v = 0; v < NVB; ++v)
-#pragma unroll
-                            for (int u = 0; u < 2; ++u) {
-                                o[v][u][nt][r] *= al;
-                                o[v][u][nt][2 + r] *= al;
-                            }
+                        const float by = raise(m[nt][r], top[nt][r]);
+                        lsum[nt][r] *= ex2(-by);
+                        power[0][nt][r] -= by;
+                        power[1][nt][r] -= by;
                     }
+            }
+            // where a row's weights times scales might leave fp16: the power that those it sees need
+            bool over = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const float lead = top[nt][r] - m[nt][r];
+                    over |= lead - power[0][nt][r] > room[0];
+                    if (vs.ng == 2) over |= lead - power[1][nt][r] > room[1];
+                }
+            if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+                for (int grp = 0; grp < 2; ++grp) {
+                    if (grp >= vs.ng) break;
+                    float down[NT][2];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            float z = -INFINITY;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                z = fmaxf(z, fmaf(x[j >> 1][nt][2 * (j & 1) + r], fac[nt][r], -m[nt][r]) + lg2(grp ? sc[j].w : sc[j].z));
+                            z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, 4));
+                            z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, 8));
+                            z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, 16));
+                            down[nt][r] = raise_power(power[grp][nt][r], z);
+                        }
+#pragma unroll
+                    for (int v = 0; v < NVB; ++v)
+                        if ((v < vs.nb[0]) == (grp == 0))
+#pragma unroll
+                            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) o[v][u][nt][i] *= down[nt][i & 1];
+                }
             }
             uint32_t w[2][2][NT][2];      // weights as B fragments: [group][16 tokens][row tile][8 tokens]
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const float ms0 = m[nt][0] == -INFINITY ? 0.0f : -m[nt][0] * fac[nt][0];
-                const float ms1 = m[nt][1] == -INFINITY ? 0.0f : -m[nt][1] * fac[nt][1];
+                const float a0 = unit_of(power[0][nt][0]), b0 = unit_of(power[0][nt][1]);
+                const float a1 = unit_of(power[1][nt][0]), b1 = unit_of(power[1][nt][1]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float pa = ex2(fmaf(x[j >> 1][nt][2 * (j & 1)], fac[nt][0], ms0));
-                    const float pb = ex2(fmaf(x[j >> 1][nt][2 * (j & 1) + 1], fac[nt][1], ms1));
+                    const float pa = ex2(fmaf(x[j >> 1][nt][2 * (j & 1)], fac[nt][0], -m[nt][0]));
+                    const float pb = ex2(fmaf(x[j >> 1][nt][2 * (j & 1) + 1], fac[nt][1], -m[nt][1]));
                     lsum[nt][0] += pa;
                     lsum[nt][1] += pb;
-                    w[0][j >> 1][nt][j & 1] = transpose8(pack2(pa * sc[j].z, pb * sc[j].z));
-                    if (vs.ng == 2) w[1][j >> 1][nt][j & 1] = transpose8(pack2(pa * sc[j].w, pb * sc[j].w));
+                    w[0][j >> 1][nt][j & 1] = transpose8(pack2(pa * sc[j].z * a0, pb * sc[j].z * b0));
+                    if (vs.ng == 2) w[1][j >> 1][nt][j & 1] = transpose8(pack2(pa * sc[j].w * a1, pb * sc[j].w * b1));
                 }
             }
 
@@ -611,7 +629,6 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                 s += __shfl_xor_sync(0xffffffffu, s, 4);
                 s += __shfl_xor_sync(0xffffffffu, s, 8);
                 s += __shfl_xor_sync(0xffffffffu, s, 16);
-                m[nt][r] *= fac[nt][r];
                 if (g == 0) {
                     sm_m[warp * R + 8 * nt + 2 * l + r] = m[nt][r];
                     sm_l[warp * R + 8 * nt + 2 * l + r] = s;
@@ -633,12 +650,9 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
         float* parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.scratch) + SONIQ_KV_SCRATCH_ZERO);
         float* part = parts + (int64_t)seg.slot * PART;
         if (tid < R) {
-            float mm = -INFINITY, ll = 0.0f;
+            float mm = kUnset, ll = 0.0f;
             for (int wi = 0; wi < n_warps; ++wi) mm = fmaxf(mm, sm_m[wi * R + tid]);
-            for (int wi = 0; wi < n_warps; ++wi) {
-                const float mw = sm_m[wi * R + tid];
-                ll += sm_l[wi * R + tid] * (mw == -INFINITY ? 0.0f : ex2(mw - mm));
-            }
+            for (int wi = 0; wi < n_warps; ++wi) ll += sm_l[wi * R + tid] * ex2(sm_m[wi * R + tid] - mm);
             sm_tm[tid] = mm;
             sm_tl[tid] = inverse(ll);
             if (!whole) {
@@ -655,7 +669,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 const int row = 8 * nt + 2 * l + r;
-                join[nt][r] = (m[nt][r] == -INFINITY ? 0.0f : ex2(m[nt][r] - sm_tm[row])) * sm_tl[row];
+                join[nt][r] = ex2(m[nt][r] - sm_tm[row]) * sm_tl[row];
             }
         auto store = [&](int r, int p, float v) {
             const int row = row0 + r, ch = sm_chan[p];
@@ -672,18 +686,18 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
             for (int vi = 0; vi < PB; ++vi) {
                 const int v = v0 + vi;
                 if (v < nvb) {
-                    const int grp = v < vs.nb[0] ? 0 : 1, bits = vs.bits[grp], e = grp ? e1 : e0;
+                    const int grp = v < vs.nb[0] ? 0 : 1, bits = vs.bits[grp];
                     const bool paired = WIDE && (v | 1) < vs.nb[0];      // value_pairs2's order
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float back = pow2(e - (bits - 1) - place_log2(bits, i));
+                        const float back = pow2(1 - bits - place_log2(bits, i));
                         const int code = paired ? value_code2(g, i) - 30 * (v & 1) : value_code(bits, g, i);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int r = 0; r < 2; ++r)
                                 merge[((warp * R + 8 * nt + 2 * l + r) * PB + vi) * 32 + code] =
-                                    o[v][i >> 1][nt][2 * (i & 1) + r] * join[nt][r] * back;
+                                    (o[v][i >> 1][nt][2 * (i & 1) + r] * join[nt][r]) * (back * power_of(grp ? power[1][nt][r] : power[0][nt][r]));
                     }
                 }
             }
@@ -716,12 +730,11 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                 for (int i = tid; i < n_part * R; i += blockDim.x) fp[i] = __ldcg(part_of(i / R) + R * 32 * NVB + i % R);
                 __syncthreads();
                 for (int r = warp; r < R; r += n_warps) {
-                    float mm = -INFINITY, ll = 0.0f;
+                    float mm = kUnset, ll = 0.0f;
                     for (int i = lane; i < n_part; i += 32) mm = fmaxf(mm, fp[i * R + r]);
                     for (int i = 16; i; i >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, i));
                     for (int i = lane; i < n_part; i += 32) {
-                        const float mc = fp[i * R + r];
-                        const float f = (mc == -INFINITY ? 0.0f : ex2(mc - mm)) * __ldcg(part_of(i) + R * 32 * NVB + R + r);
+                        const float f = ex2(fp[i * R + r] - mm) * __ldcg(part_of(i) + R * 32 * NVB + R + r);
                         ll += f;
                         fp[i * R + r] = f;
                     }

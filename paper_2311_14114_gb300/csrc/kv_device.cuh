@@ -96,7 +96,7 @@ __device__ __forceinline__ float scale_of(uint32_t bits16, bool bf16) {
     return bf16 ? __uint_as_float(bits16 << 16) : __half2float(__ushort_as_half((uint16_t)bits16));
 }
 // A cached value scale.  One that no write leaves (negative, not finite) counts as 0: it may stand behind a token
-// that no row sees, and would spread through the common power of two of its block.
+// that no row sees, and 0 times it would not be 0.
 __device__ __forceinline__ float value_scale(uint32_t bits16, bool bf16) {
     const float x = scale_of(bits16, bf16);
     return x >= 0.0f && x < INFINITY ? x : 0.0f;
@@ -104,7 +104,50 @@ __device__ __forceinline__ float value_scale(uint32_t bits16, bool bf16) {
 // 1 / a softmax sum; nothing seen: 0; NaN stays.
 __device__ __forceinline__ float inverse(float l) { return l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l); }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+__device__ __forceinline__ float lg2(float x) {
+    float r;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 
+// How weights become fp16.  With a row's running maximum m (of scores in units of
+// the exponent, rounded up, so that changes of it are exact) a token's weight is
+// p = 2^(score - m) <= 1; its products with the codes carry the value scale s.  A
+// row (and value group) rounds p s 2^-power to fp16 and sums outputs in that
+// unit.  The power follows the products p s of the tokens that the row sees: it
+// is raised to the largest where that exceeds 2^15 of it, and shrinks as m grows.
+// So rounding costs a row 2^-11 of each product, or 2^-25 of its largest, whatever
+// stands in tokens that it does not see, or hardly weighs.  (With a power common to
+// all rows of a block, over all of its scales, one scale of 2^16 times the others'
+// cost the rest 2 % of their weights.)
+// Finding the largest product takes a logarithm per token, so it is done only
+// where the bound from the largest scale of the block and the largest score
+// leaves the range.
+constexpr float kUnset = -3.402823466e+38f;      // no token seen, no product met
+constexpr float kRoom = 15.0f;
+
+// log2 of the largest value scale of a block, from its bits (none: far below any product), at most 0.09 too large:
+// log2(1 + f) is f to f + 0.0861.
+__device__ __forceinline__ float scale_bound(uint32_t bits) { return fmaf((float)bits, 0x1p-23f, -126.91f); }
+// Raises a row's maximum to its block's `top`; returns by how much.
+__device__ __forceinline__ float raise(float& m, float top) {
+    const float to = fmaxf(m, ceilf(top)), by = to - m;
+    m = to;
+    return by;
+}
+// Raises a power to the largest product, 2^most, where that leaves the room; returns the factor of what is summed so far.
+// (126 at most: products reach 2^128, and both 2^power and its inverse are floats.)
+__device__ __forceinline__ float raise_power(float& power, float most) {
+    if (!(most - power > kRoom)) return 1.0f;
+    const float to = fminf(ceilf(most), 126.0f), by = power - to;
+    power = to;
+    return by < -126.0f ? 0.0f : pow2((int)by);
+}
+// 2^power, and 2^-power through the integer in a float's low bits.  (Below 2^-126, products are 0 as weights are.)
+__device__ __forceinline__ float power_of(float power) { return pow2((int)fmaxf(power, -126.0f)); }
+__device__ __forceinline__ float unit_of(float power) {
+    return __uint_as_float(__float_as_uint(12582912.0f + 127.0f - fmaxf(power, -126.0f)) << 23);
+}
 
 // Eight codes of a block, its l-th quarter, unpack to four half pairs: which codes
 // they are, and the powers of two their places in the word give them.
