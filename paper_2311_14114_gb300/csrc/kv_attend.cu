@@ -525,7 +525,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                             z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, 4));
                             z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, 8));
                             z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, 16));
-                            down[nt][r] = raise_power(power[grp][nt][r], z);
+                            down[nt][r] = raise_power(power[grp][nt][r], z, z - power[grp][nt][r] > kRoom);
                         }
 #pragma unroll
                     for (int v = 0; v < NVB; ++v)

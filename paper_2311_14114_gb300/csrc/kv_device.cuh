@@ -47,6 +47,11 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
     return v;
 }
 
+__device__ __forceinline__ float lds32f(uint32_t a) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    return v;
+}
 __device__ __forceinline__ float4 lds128f(uint32_t a) {
     float4 v;
     asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
@@ -120,8 +125,8 @@ __device__ __forceinline__ float lg2(float x) {
 // stands in tokens that it does not see, or hardly weighs.  (With a power common to
 // all rows of a block, over all of its scales, one scale of 2^16 times the others'
 // cost the rest 2 % of their weights.)
-// Finding the largest product takes a logarithm per token, so it is done only
-// where the bound from the largest scale of the block and the largest score
+// Finding the largest product takes a pass over the tokens, so it is done only
+// where the bound from the largest scale of the block and the row's largest score
 // leaves the range.
 constexpr float kUnset = -3.402823466e+38f;      // no token seen, no product met
 constexpr float kRoom = 15.0f;
@@ -129,17 +134,18 @@ constexpr float kRoom = 15.0f;
 // log2 of the largest value scale of a block, from its bits (none: far below any product), at most 0.09 too large:
 // log2(1 + f) is f to f + 0.0861.
 __device__ __forceinline__ float scale_bound(uint32_t bits) { return fmaf((float)bits, 0x1p-23f, -126.91f); }
+// ... and at most that of the smallest.
+__device__ __forceinline__ float scale_floor(uint32_t bits) { return fmaf((float)bits, 0x1p-23f, -127.0f); }
 // Raises a row's maximum to its block's `top`; returns by how much.
 __device__ __forceinline__ float raise(float& m, float top) {
     const float to = fmaxf(m, ceilf(top)), by = to - m;
     m = to;
     return by;
 }
-// Raises a power to the largest product, 2^most, where that leaves the room; returns the factor of what is summed so far.
+// Raises a power to the largest product, 2^most, if it is to; returns the factor of what is summed so far.
 // (126 at most: products reach 2^128, and both 2^power and its inverse are floats.)
-__device__ __forceinline__ float raise_power(float& power, float most) {
-    if (!(most - power > kRoom)) return 1.0f;
-    const float to = fminf(ceilf(most), 126.0f), by = power - to;
+__device__ __forceinline__ float raise_power(float& power, float most, bool is_to) {
+    const float to = is_to ? fminf(ceilf(most), 126.0f) : power, by = power - to;
     power = to;
     return by < -126.0f ? 0.0f : pow2((int)by);
 }

@@ -20,9 +20,9 @@
 //
 // Numerics.  Queries are fp16, each row scaled by a power of two to 2^13; codes
 // are exact in fp16, so S is an exact product summed in fp32, per precision
-// group, and gets its scales in fp32.  P times the value scale (normalised by a
-// running power of two) is rounded to fp16.  The running maximum is raised only
-// when a score exceeds it by more than 2^13: P stays below 2^15.
+// group, and gets its scales in fp32.  P times the value scale is rounded to fp16
+// relative to a power of two of the row's own, which O is relative to (kv_device.cuh):
+// O is rescaled only when a product leaves fp16's range above it.
 //
 // Values keep their row order (tokens x channels) as the MN-major operand of
 // O = P V, so both operand tiles have one layout: 64-code column groups of
@@ -56,10 +56,6 @@ constexpr int kSlotCols = 256;           // TMEM columns of a softmax group: S (
 // Columns of a softmax group in front of O: scores (the weights of the first value group go over them), and those
 // of the second key group or the weights of the second value group
 __host__ __device__ constexpr int s_cols(int k_groups, int v_groups) { return k_groups == 2 ? 2 * kTok : (v_groups == 2 ? kTok + kTok / 2 : kTok); }
-// A row's running maximum may be exceeded by kLazy (log2), and the running powers of the value scales by kLazyScale,
-// before O is rescaled: weights stay below 2^15 in fp16.
-constexpr float kLazy = 13.0f;
-constexpr int kLazyScale = 2;
 
 struct TilePlan {
     int rows;               // query rows per key head
@@ -285,7 +281,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t* words = reinterpret_cast<uint32_t*>(misc + 320);       // [32] for the split, then:
     const uint32_t abort_flag = tc::smem_u32(words + 32);
     uint32_t* tmem_at = words + 33;
-    int* sm_e = reinterpret_cast<int*>(words + 36);                  // [4 stages][2]: power of two above the value scales
     float* sm_fac = reinterpret_cast<float*>(misc + 512);            // [256] factor of a row's scores
     float* sm_m = sm_fac + 256;                                      // [128], of the second stream
     float* sm_l = sm_m + 128;
@@ -294,6 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     int16_t* sm_col = reinterpret_cast<int16_t*>(sm_back + 192);     // [256] column of a key channel
     Segment* sm_seg = reinterpret_cast<Segment*>(sm_col + 256);      // the next segment, behind a flag that there is one
     int* sm_more = reinterpret_cast<int*>(sm_seg + 1);
+    float2* sm_span = reinterpret_cast<float2*>(misc + 4608);        // [4 stages][2]: log2 of the largest and smallest value scale
     auto bar = [&](int i) { return bars + 8u * i; };
 
     if (tid == 0) {
@@ -500,7 +496,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool more = split.next(seg);
             if (more) *sm_seg = split.segment(chunks);
             *sm_more = more;
-            // ---- scales as fp32: keys' with 2^-(n-1), values' relative to a power of two; two tokens to a lane ----
+            // ---- scales as fp32, keys' with 2^-(n-1); two tokens to a lane ----
             uint32_t from[2][2];        // [side][token]
 #pragma unroll
             for (int side = 0; side < 2; ++side) {
@@ -528,19 +524,19 @@ __global__ void __launch_bounds__(kThreads, 1)
                             const uint32_t raw16 = lds16(src + from[side][h] + 2 * grp);
                             x[h] = p0 + lane + 32 * h >= end ? 0.0f : (side ? value_scale(raw16, bf16) : scale_of(raw16, bf16));
                         }
-                        float f = pow2(1 - geo.s[side].bits[grp]);
+                        const float f = side ? 1.0f : pow2(1 - geo.s[0].bits[grp]);
                         if (side) {
                             const uint32_t big = __reduce_max_sync(0xffffffffu, max(__float_as_uint(x[0]), __float_as_uint(x[1])));
-                            const int e = min(max((int)(big >> 23) - 126, -100), 126);
-                            f = pow2(-e);
-                            if (lane == 0) sm_e[2 * st + grp] = e;
+                            // (beyond the end: none)
+                            const uint32_t a0 = p0 + lane >= end ? big : __float_as_uint(x[0]), a1 = p0 + lane + 32 >= end ? big : __float_as_uint(x[1]);
+                            const uint32_t least = __reduce_min_sync(0xffffffffu, min(a0, a1));
+                            if (lane == 0) sm_span[2 * st + grp] = make_float2(scale_bound(big), scale_floor(least));
                         }
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
                             asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 512 * side + 256 * grp + 128 * h), "f"(x[h] * f) : "memory");
                     }
                 }
-                if (VNG == 1 && lane == 0) sm_e[2 * st + 1] = -100;
                 __syncwarp();
                 if (lane == 0) {
                     tc::mbar_arrive(bar(Bars::k_ready + st));
@@ -702,8 +698,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float fac = sm_fac[(streams ? 0 : 128 * s) + r_tile];
             const uint32_t lanes = (uint32_t)(quad * 32) << 16;
             const uint32_t t_s = tmem + s * kSlotCols + lanes;
-            float m = -INFINITY, l = 0.0f;
-            int e0 = 0, e1 = 0;
+            // the maximum (a whole number, in units of the exponent), the sum, and each value group's power of two
+            // (kv_device.cuh) that weights and outputs are relative to
+            float m = kUnset, l = 0.0f, power0 = kUnset, power1 = kUnset;
             const int mine = s < groups ? (streams ? (nblk - s + 1) / 2 : nblk) : 0;
             const int sure = min(len, end);
             Ring kv = kv0;
@@ -736,7 +733,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                     }
                 }
-                const int b0 = sm_e[2 * st], b1 = sm_e[2 * st + 1];
+                const float2 span0 = sm_span[2 * st], span1 = VNG == 2 ? sm_span[2 * st + 1] : span0;
                 float2 x[kTok / 2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -772,47 +769,70 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int k = 0; k < 8; ++k) tops[k] = fmaxf(x[k].x, x[k].y);
 #pragma unroll
                 for (int k = 8; k < kTok / 2; ++k) tops[k & 7] = fmaxf(fmaxf(tops[k & 7], x[k].x), x[k].y);
-                const float top = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
-                // raise the maximum, and the powers of two of the value scales, where they are left behind by much
-                const bool first = i == 0;
-                const bool raise = m == -INFINITY ? top != -INFINITY : (top - m) * fac > kLazy;
-                const int n0 = first || b0 > e0 + kLazyScale ? b0 : e0, n1 = first || b1 > e1 + kLazyScale ? b1 : e1;
-                if (first) {
-                    m = top;
-                } else if (__any_sync(0xffffffffu, raise) || n0 != e0 || n1 != e1) {
-                    float al = 1.0f;
-                    if (raise) {
-                        al = m == -INFINITY ? 0.0f : ex2((m - top) * fac);
-                        m = top;
-                        l *= al;
-                    }
-                    const float al0 = al * (n0 - e0 > 126 ? 0.0f : pow2(e0 - n0)), al1 = al * (n1 - e1 > 126 ? 0.0f : pow2(e1 - n1));
-                    // The MMAs that wrote O have to be complete: with one buffer they came before those that wrote
-                    // these scores.
-                    if (SB == 2) {
-                        ok = wait(Bars::pv_done + s, done ^ 1u);
-                        if (!ok) break;
-                        tc::tc_fence_after();
-                    }
-#pragma unroll 1
-                    for (int c = 0; c < pl.o_cols; c += 16) {
-                        uint32_t v[16];
-                        tc::tmem_ld16(t_s + o_off + c, v);
-                        const float f = c < va0 ? al0 : al1;
+                const float top = fac * fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
+                // (the distance to a power is the same before and after the maximum is raised)
+                bool over0 = (top - m) + span0.x - power0 > kRoom, over1 = VNG == 2 && (top - m) + span1.x - power1 > kRoom;
+                if (__any_sync(0xffffffffu, top > m || over0 || over1)) {
+                    const float by = raise(m, top);
+                    l *= ex2(-by);
+                    power0 -= by;
+                    power1 -= by;
+                    if (__any_sync(0xffffffffu, over0 || over1)) {
+                        const float lead = top - m;
+                        // Weights times scales might leave fp16: the power becomes that of the largest product that the row
+                        // sees, or of its largest weight and the smallest scale where scales are within 2^14 of each other.
+                        float most0 = lead + span0.y, most1 = lead + span1.y;
+                        if (fmaxf(span0.x - span0.y, span1.x - span1.y) > kRoom - 1.0f) {
+                            // (through TMEM, where scores can be indexed by a loop: unrolled over registers, these rare lines
+                            // cost the common ones 2 to 5 %)
+                            float z0 = 0.0f, z1 = 0.0f;
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f);
-                        tmem_st16v(t_s + o_off + c, v);
+                            for (int c = 0; c < kTok; c += 16) {
+                                uint32_t v[16];
+#pragma unroll
+                                for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(k & 1 ? x[(c + k) / 2].y : x[(c + k) / 2].x);
+                                tmem_st16v(t_b + c, v);
+                            }
+#pragma unroll 1
+                            for (int c = 0; c < kTok; c += 8) {
+                                uint32_t v[8];
+                                tc::tmem_ld8(t_b + c, v);
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) {
+                                    const float p = ex2(fmaf(__uint_as_float(v[k]), fac, -m));
+                                    z0 = fmaxf(z0, p * lds32f(sc + 512 + 4 * (c + k)));
+                                    if (VNG == 2) z1 = fmaxf(z1, p * lds32f(sc + 768 + 4 * (c + k)));
+                                }
+                            }
+                            most0 = lg2(z0);
+                            most1 = lg2(z1);
+                            over0 = most0 - power0 > kRoom;
+                            over1 = VNG == 2 && most1 - power1 > kRoom;
+                        }
+                        const float down0 = raise_power(power0, most0, over0), down1 = raise_power(power1, most1, over1);
+                        if (i != 0 && __any_sync(0xffffffffu, down0 != 1.0f || down1 != 1.0f)) {
+                            // The MMAs that wrote O have to be complete: with one buffer they came before those that wrote
+                            // these scores.
+                            if (SB == 2) {
+                                ok = wait(Bars::pv_done + s, done ^ 1u);
+                                if (!ok) break;
+                                tc::tc_fence_after();
+                            }
+#pragma unroll 1
+                            for (int c = 0; c < pl.o_cols; c += 16) {
+                                uint32_t v[16];
+                                tc::tmem_ld16(t_s + o_off + c, v);
+                                const float f = c < va0 ? down0 : down1;
+#pragma unroll
+                                for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f);
+                                tmem_st16v(t_s + o_off + c, v);
+                            }
+                        }
                     }
                 }
-                e0 = n0;
-                e1 = n1;
-                // weights, times 2^(block's power - running power); over the scores that are done with: the first
-                // value group's from column 0, the second's from the second key group's place.  The sum and the second
-                // group are made of the same numbers, so the power stops where the first group's round to 0 in fp16
-                // (below 2^(13 - 40)): a block of small or zero values still counts.
-                const int d0 = max(b0 - e0, -40), dd = b1 - e1 - d0;
-                const float shift = (m == -INFINITY ? 0.0f : -m * fac) + (float)d0;
-                const float second = dd < -126 ? 0.0f : pow2(min(dd, 127));
+                // weights, over the scores that are done with: the first value group's from column 0, the second's from
+                // the second key group's place
+                const float unit0 = unit_of(power0), unit1 = unit_of(power1);
                 float2 sums[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -823,10 +843,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
                             float2& y = x[16 * h + k + j];
-                            y = fma2(y, make_float2(fac, fac), make_float2(shift, shift));
+                            y = fma2(y, make_float2(fac, fac), make_float2(-m, -m));
                             y = make_float2(ex2(y.x), ex2(y.y));
                             sums[j] = fma2(y, make_float2(1.0f, 1.0f), sums[j]);
-                            const float2 z = mul2(y, j ? make_float2(vv.z, vv.w) : make_float2(vv.x, vv.y));
+                            const float2 z = mul2(mul2(y, j ? make_float2(vv.z, vv.w) : make_float2(vv.x, vv.y)), make_float2(unit0, unit0));
                             w[k + j] = pack2(z.x, z.y);
                         }
                     }
@@ -835,15 +855,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int k = 0; k < 16; k += 2) {
                             const float4 vv = lds128f(sc + 768 + 128 * h + 8 * k);
-                            const float2 y0 = mul2(x[16 * h + k], make_float2(vv.x * second, vv.y * second));
-                            const float2 y1 = mul2(x[16 * h + k + 1], make_float2(vv.z * second, vv.w * second));
+                            const float2 y0 = mul2(mul2(x[16 * h + k], make_float2(vv.x, vv.y)), make_float2(unit1, unit1));
+                            const float2 y1 = mul2(mul2(x[16 * h + k + 1], make_float2(vv.z, vv.w)), make_float2(unit1, unit1));
                             w[k] = pack2(y0.x, y0.y);
                             w[k + 1] = pack2(y1.x, y1.y);
                         }
                         tmem_st16v(t_b + p1_off + 16 * h, w);
                     }
                 }
-                l += (sums[0].x + sums[0].y + sums[1].x + sums[1].y) * pow2(-d0);
+                l += sums[0].x + sums[0].y + sums[1].x + sums[1].y;
                 tc::tc_fence_before();
                 __syncwarp();
                 // (by buffer: with two, a warp may be a block ahead of the others of its group)
@@ -857,29 +877,29 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool whole = seg.n_part == 1;
             // Results are averages from here on, which are representable where sums of values near the end of the type's
             // range are not.
-            float m2 = m == -INFINITY ? m : m * fac, inv = inverse(l), other = 0.0f;     // m2: in units of the exponent
+            float inv = inverse(l), other = 0.0f;
+            const float unit_power0 = power_of(power0), unit_power1 = power_of(power1);
             float* second = reinterpret_cast<float*>(smem);       // [o_cols][128]: the second stream's outputs
             if (streams && s == 1) {
-                sm_m[r_tile] = mine > 0 ? m2 : -INFINITY;
+                sm_m[r_tile] = m;
                 sm_l[r_tile] = l;
 #pragma unroll 1
                 for (int c = 0; ok && mine > 0 && c < pl.o_cols; c += 16) {
                     uint32_t v[16];
                     tc::tmem_ld16(t_s + o_off + c, v);
-                    const float f = pow2(c < va0 ? e0 : e1);
+                    const float f = c < va0 ? unit_power0 : unit_power1;
 #pragma unroll
                     for (int k = 0; k < 16; ++k) second[(c + k) * 128 + r_tile] = (__uint_as_float(v[k]) * inv) * (sm_back[c + k] * f);
                 }
             }
             bar_group(1, 256);
             if (streams && s == 0 && groups == 2) {
-                const float m1 = sm_m[r_tile], mm = fmaxf(m2, m1);
-                const float keep = m2 == -INFINITY ? 0.0f : ex2(m2 - mm);
-                other = (m1 == -INFINITY ? 0.0f : ex2(m1 - mm)) * sm_l[r_tile];
+                const float m1 = sm_m[r_tile], mm = fmaxf(m, m1), keep = ex2(m - mm);
+                other = ex2(m1 - mm) * sm_l[r_tile];
                 l = l * keep + other;
                 inv = inverse(l) * keep;
                 other *= inverse(l);
-                m2 = mm;
+                m = mm;
             }
             const int unit_row = (streams ? 0 : 128 * s) + r_tile;
             const int64_t part_floats = (int64_t)unit_rows * (pl.o_cols + 2);
@@ -894,7 +914,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int c = 0; c < pl.o_cols; c += 16) {
                     uint32_t v[16];
                     tc::tmem_ld16(t_s + o_off + c, v);
-                    const float f = pow2(c < va0 ? e0 : e1);
+                    const float f = c < va0 ? unit_power0 : unit_power1;
                     float x[16];
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
@@ -912,7 +932,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 if (!whole) {
                     float* st = parts + seg.slot * part_floats + (int64_t)unit_rows * pl.o_cols;
-                    st[unit_row] = m2;
+                    st[unit_row] = m;
                     st[unit_rows + unit_row] = l;
                 }
             }
@@ -1013,12 +1033,9 @@ __global__ void __launch_bounds__(kJoinThreads) kv_join_kernel(const KvGeom geo,
         return reinterpret_cast<const float*>(scratch + kJoinBytes) + (int64_t)(2 * (it.cta0 + i) + (i == 0 ? it.cta0_slot : 0)) * part_floats;
     };
     auto m_of = [&](int i) { return part(i)[(int64_t)unit_rows * pl.o_cols + unit_row]; };
-    float mm = -INFINITY, ll = 0.0f;
+    float mm = kUnset, ll = 0.0f;
     // a part's sum in units of the item's maximum
-    auto sum_of = [&](int i) {
-        const float mi = m_of(i);
-        return part(i)[(int64_t)unit_rows * (pl.o_cols + 1) + unit_row] * (mi == -INFINITY ? 0.0f : ex2(mi - mm));
-    };
+    auto sum_of = [&](int i) { return part(i)[(int64_t)unit_rows * (pl.o_cols + 1) + unit_row] * ex2(m_of(i) - mm); };
 #pragma unroll 4
     for (int i = 0; i < it.n_part; ++i) mm = fmaxf(mm, m_of(i));
 #pragma unroll 4

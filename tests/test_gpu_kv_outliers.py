@@ -18,11 +18,11 @@ TOP = {F16: 65504.0, BF16: float(torch.finfo(BF16).max)}
 ONE = (2, 128, 128, ([128], [8]), ([128], [4]))
 MIXED = (2, 128, 128, ([96, 32], [4, 8]), ([128], [4]))
 TWO = (2, 64, 64, ([51, 13], [4, 8]), ([51, 13], [4, 8]))
-WIDE = (1, 192, 192, ([187, 5], [4, 8]), ([160, 32], [2, 8]))
+WIDE = (1, 192, 192, ([187, 5], [4, 8]), ([160, 32], [2, 8]))       # values that no tile kernel takes
 SHAPES = [ONE, MIXED, TWO, WIDE]
-# T, group: 4 and 12 query rows per key head
+# T, group: 4 and 12 query rows per key head, and 40, 160 and 264
 FEW = [(4, 1), (3, 4)]
-MANY = []
+MANY = [(40, 1), (40, 4), (33, 8)]
 
 
 def attend(sq, p, mask=None, scale=None):
