@@ -41,6 +41,7 @@
 #include <type_traits>
 
 #include "kv_device.cuh"
+#include "kv_flights.h"
 #include "kv_split.cuh"
 #include "soniq_device.cuh"
 
@@ -367,6 +368,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto work = [&](auto role) {
     constexpr int ROLE = decltype(role)::value;      // 0 softmax, 1 unpacking, 2 MMAs and copies
     Segment seg = first;
+    Flights flights;        // of the copying warp
     while (true) {
         const int b = seg.entry / pl.row_units, unit = seg.entry % pl.row_units, head = seg.item;
         const int row0 = unit * unit_rows;
@@ -393,6 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ok = wait(Bars::raw_free + r, ring_r.phase ^ 1u);
                 if (!ok) break;
                 if (a.drop && j == 0 && blockIdx.x == 0) continue;
+                flights.issue(r, ring_r.phase);
                 const uint32_t at = raw + r * pl.raw_bytes, full = bar(Bars::raw_full + r);
                 if (tc::elect_one()) tc::mbar_arrive_expect_tx(full, boxes * pl.box_rows * (ks.row_bytes + vs.row_bytes + 2 * (ks.ng + vs.ng)));
 #pragma unroll 1
@@ -976,10 +979,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             // a copy did not come: let those on their way land, and the MMAs end, within the same bound
             const long long t0 = tc::globaltimer();
             if (warp == 1) {
-                for (uint32_t i = 0; i < (uint32_t)pl.raw_stages; ++i)
-                    while (!tc::mbar_try_wait(bar(Bars::raw_full + i), 0) && !tc::mbar_try_wait(bar(Bars::raw_full + i), 1) &&
-                           tc::globaltimer() - t0 < kWaitNs) {
-                    }
+                flights.land([&](int i, uint32_t parity) { return tc::mbar_try_wait(bar(Bars::raw_full + i), parity); },
+                             [&]() { return tc::globaltimer() - t0 < kWaitNs; });
             } else if (warp == 0 || warp == 3) {
                 if (tc::elect_one()) tc::mma_commit(bar(Bars::drain));
                 while (!tc::mbar_try_wait(bar(Bars::drain), 0) && tc::globaltimer() - t0 < kWaitNs) {
