@@ -199,7 +199,9 @@ struct Ring {
 // Wait of a whole warp for phase `parity` of `bar`; one result for its lanes:
 // false once the CTA gives up, or when the wait is given up after 2 s.  (The
 // polling loop is written out: twenty warps' polls took a third of the issue
-// slots, and what all roles run has to stay in the instruction cache.)
+// slots, and what all roles run has to stay in the instruction cache.  A poll may
+// suspend the warp for a time that the hardware sets, so the clock is read every
+// 64 of them.)
 template <typename F>
 __device__ __forceinline__ bool wait_until(F poll, uint32_t abort_flag, unsigned* err) {
     long long t0 = 0;
@@ -219,7 +221,7 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, uint32_
     return wait_until([&]() {
         uint32_t done;
         asm volatile(
-            "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 4096;\n"
+            "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 64;\n"
             "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra DONE;\n\t"
             "sub.u32 n, n, 1;\n\tsetp.ne.u32 q, n, 0;\n\t@q bra TRY;\n"
             "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
@@ -235,7 +237,7 @@ __device__ __forceinline__ bool wait_warp2(uint32_t b0, uint32_t parity0, uint32
     return wait_until([&]() {
         uint32_t done;
         asm volatile(
-            "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 4096;\n"
+            "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 64;\n"
             "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
             "mbarrier.try_wait.parity.shared::cta.b64 q, [%3], %4;\n\t"
             "and.pred p, p, q;\n\t@p bra DONE;\n\t"
@@ -252,7 +254,7 @@ __device__ __forceinline__ bool wait_warp3(uint32_t b0, uint32_t parity0, uint32
     return wait_until([&]() {
         uint32_t done;
         asm volatile(
-            "{\n\t.reg .pred p, q, r;\n\t.reg .u32 n;\n\tmov.u32 n, 4096;\n"
+            "{\n\t.reg .pred p, q, r;\n\t.reg .u32 n;\n\tmov.u32 n, 64;\n"
             "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
             "mbarrier.try_wait.parity.shared::cta.b64 q, [%3], %4;\n\t"
             "mbarrier.try_wait.parity.shared::cta.b64 r, [%5], %6;\n\t"
