@@ -726,7 +726,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 uint32_t seen[2] = {0xffffffffu, 0xffffffffu};      // of the block, by the row
                 if (tail) {
                     const uint8_t* mask = a.mask ? a.mask + b * a.mask_stride + (int64_t)t_row * a.T : nullptr;
-                    const int upto = (mask ? sure : min(end, len + t_row + 1)) - p0;      // shown without a look at the mask
+                    // shown without a look at the mask (a length may be near 2^31)
+                    const int upto = (mask ? sure : (int)min((int64_t)end, (int64_t)len + t_row + 1)) - p0;
                     seen[0] = upto >= 32 ? 0xffffffffu : (upto <= 0 ? 0u : (1u << upto) - 1u);
                     seen[1] = upto >= 64 ? 0xffffffffu : (upto <= 32 ? 0u : (1u << (upto - 32)) - 1u);
                     if (mask) {
