@@ -18,7 +18,7 @@ namespace soniq {
 
 struct Segment {
     int entry, item;         // item: 0 .. mult - 1 of the entry
-    int c_first, c_end, n_chunks;
+    int c_first, c_end;
     int cta0, n_part;        // the CTAs that share the item
     int slot, cta0_slot;     // places of this part and (0 or 1) of the first CTA's
 };
@@ -155,7 +155,6 @@ struct Split {
             pos = first + s.c_first;
         }
         s.entry = entry;
-        s.n_chunks = (int)nch;
         return s;
     }
 
