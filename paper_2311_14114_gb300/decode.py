@@ -53,13 +53,14 @@ class CachedAttention:
 
     def slots(self, page_table: torch.Tensor, lengths: torch.Tensor, T: int) -> torch.Tensor:
         """Slots (int64 [B][T]) of the T tokens behind each context; -1 in absent
-        sequences; beyond the table one that is no slot, which the library reports."""
+        sequences; beyond the table, or where its page is none of the cache's, one that
+        is no slot, which the library reports."""
         page = self.cache.page_size
         pos = lengths.long()[:, None] + torch.arange(T, device=lengths.device)
         entry = pos.clamp(min=0) // page
         inside = entry < page_table.shape[1]
         pages = page_table.long().gather(1, entry.clamp(max=page_table.shape[1] - 1))
-        slot = torch.where(inside, pages * page + pos % page, self.cache.n_pages * page)
+        slot = torch.where(inside & (pages >= 0), pages * page + pos % page, self.cache.n_pages * page)
         return torch.where(lengths[:, None] >= 0, slot, -1)
 
     def step(self, X: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
