@@ -475,7 +475,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                         }
                     }
             }
-            float top[NT][2];
+            float best[NT][2], to_exp[NT][2];       // a row's largest score, and the factor to units of the exponent
             bool grows = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -485,15 +485,16 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                     tp = fmaxf(tp, __shfl_xor_sync(0xffffffffu, tp, 4));
                     tp = fmaxf(tp, __shfl_xor_sync(0xffffffffu, tp, 8));
                     tp = fmaxf(tp, __shfl_xor_sync(0xffffffffu, tp, 16));
-                    top[nt][r] = tp * fac[nt][r];
-                    grows |= top[nt][r] > m[nt][r];
+                    best[nt][r] = tp;
+                    to_exp[nt][r] = exponent_factor(fac[nt][r], tp);
+                    grows |= tp * to_exp[nt][r] > m[nt][r];
                 }
             if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const float by = raise(m[nt][r], top[nt][r]);
+                        const float by = raise(m[nt][r], best[nt][r] * to_exp[nt][r]);
                         lsum[nt][r] *= ex2(-by);
                         power[0][nt][r] -= by;
                         power[1][nt][r] -= by;
@@ -505,7 +506,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    const float lead = top[nt][r] - m[nt][r];
+                    const float lead = fmaf(best[nt][r], to_exp[nt][r], -m[nt][r]);
                     over |= lead - power[0][nt][r] > room[0];
                     if (vs.ng == 2) over |= lead - power[1][nt][r] > room[1];
                 }
@@ -521,7 +522,7 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                             float z = -INFINITY;
 #pragma unroll
                             for (int j = 0; j < 4; ++j)
-                                z = fmaxf(z, fmaf(x[j >> 1][nt][2 * (j & 1) + r], fac[nt][r], -m[nt][r]) + lg2(grp ? sc[j].w : sc[j].z));
+                                z = fmaxf(z, fmaf(x[j >> 1][nt][2 * (j & 1) + r], to_exp[nt][r], -m[nt][r]) + lg2(grp ? sc[j].w : sc[j].z));
                             z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, 4));
                             z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, 8));
                             z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, 16));
@@ -545,8 +546,8 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                 const float a1 = unit_of(power[1][nt][0]), b1 = unit_of(power[1][nt][1]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float pa = ex2(fmaf(x[j >> 1][nt][2 * (j & 1)], fac[nt][0], -m[nt][0]));
-                    const float pb = ex2(fmaf(x[j >> 1][nt][2 * (j & 1) + 1], fac[nt][1], -m[nt][1]));
+                    const float pa = ex2(fmaf(x[j >> 1][nt][2 * (j & 1)], to_exp[nt][0], -m[nt][0]));
+                    const float pb = ex2(fmaf(x[j >> 1][nt][2 * (j & 1) + 1], to_exp[nt][1], -m[nt][1]));
                     lsum[nt][0] += pa;
                     lsum[nt][1] += pb;
                     w[0][j >> 1][nt][j & 1] = transpose8(pack2(pa * sc[j].z * a0, pb * sc[j].z * b0));

@@ -136,6 +136,15 @@ constexpr float kRoom = 15.0f;
 __device__ __forceinline__ float scale_bound(uint32_t bits) { return fmaf((float)bits, 0x1p-23f, -126.91f); }
 // ... and at most that of the smallest.
 __device__ __forceinline__ float scale_floor(uint32_t bits) { return fmaf((float)bits, 0x1p-23f, -127.0f); }
+// The factor of a row's scores, whose largest in the block is `best`, that takes them to units of the exponent.
+// score * factor - m is one rounding; m is that of a rounded product.  Up to 2^30 the two are within 2^5 of each other,
+// which weights have room for, and which the row's lead over m counts.  Beyond, different scores are 2^6 or more apart,
+// so any factor of that size leaves one weight, or equal ones: a power of two makes the products exact.  (The next one
+// above, so that scores stay in order with those of other blocks.)
+__device__ __forceinline__ float exponent_factor(float factor, float best) {
+    const float whole = __uint_as_float((__float_as_uint(factor) + 0x007FFFFFu) & 0x7F800000u);
+    return fabsf(best * factor) > 0x1p30f ? whole : factor;
+}
 // Raises a row's maximum to its block's `top`; returns by how much.
 __device__ __forceinline__ float raise(float& m, float top) {
     const float to = fmaxf(m, ceilf(top)), by = to - m;

@@ -293,6 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     Segment* sm_seg = reinterpret_cast<Segment*>(sm_col + 256);      // the next segment, behind a flag that there is one
     int* sm_more = reinterpret_cast<int*>(sm_seg + 1);
     float2* sm_span = reinterpret_cast<float2*>(misc + 4608);        // [4 stages][2]: log2 of the largest and smallest value scale
+    float* sm_up = reinterpret_cast<float*>(sm_span + 8);            // [4 stages]: what the keys' scales were divided by
     auto bar = [&](int i) { return bars + 8u * i; };
 
     if (tid == 0) {
@@ -501,7 +502,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool more = split.next(seg);
             if (more) *sm_seg = split.segment(chunks);
             *sm_more = more;
-            // ---- scales as fp32, keys' with 2^-(n-1); two tokens to a lane ----
+            // ---- scales as fp32, keys' with 2^-(n-1); two tokens to a lane.  Exact products reach 2^28 before they get
+            // their scales, so those above 2^90 are brought down to it with the block, and scores stay in fp32's range where
+            // their softmax argument does. ----
             uint32_t from[2][2];        // [side][token]
 #pragma unroll
             for (int side = 0; side < 2; ++side) {
@@ -519,28 +522,38 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ok = wait2(Bars::kv_free + st, kv.phase ^ 1u, Bars::raw_full + r, rw.phase);
                 if (!ok) break;
                 const uint32_t src = raw + r * pl.raw_bytes, to = ring + st * pl.stage_bytes + (pl.k_atoms + pl.v_atoms) * kAtom + 4 * lane;
+                auto scale = [&](int side, int grp, int h) {
+                    const uint32_t raw16 = lds16(src + from[side][h] + 2 * grp);
+                    return p0 + lane + 32 * h >= end ? 0.0f : (side ? value_scale(raw16, bf16) : scale_of(raw16, bf16));
+                };
+                auto put = [&](int side, int grp, float x0, float x1) {
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 512 * side + 256 * grp), "f"(x0) : "memory");
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 512 * side + 256 * grp + 128), "f"(x1) : "memory");
+                };
+                float k[KNG][2];
+                uint32_t top = 0;       // (a token that no row sees may hold anything: not finite, it does not count)
 #pragma unroll
-                for (int side = 0; side < 2; ++side) {
+                for (int i = 0; i < 2 * KNG; ++i) {
+                    k[i >> 1][i & 1] = scale(0, i >> 1, i & 1);
+                    const uint32_t mag = __float_as_uint(k[i >> 1][i & 1]) & 0x7FFFFFFFu;
+                    top = max(top, mag < 0x7F800000u ? mag : 0u);
+                }
+                const int by = max((int)ceilf(scale_bound(__reduce_max_sync(0xffffffffu, top))) - 90, 0);
+                if (lane == 0) sm_up[st] = pow2(by);
 #pragma unroll
-                    for (int grp = 0; grp < (side ? VNG : KNG); ++grp) {
-                        float x[2];
+                for (int grp = 0; grp < KNG; ++grp) {
+                    const float f = pow2(1 - ks.bits[grp] - by);
+                    put(0, grp, k[grp][0] * f, k[grp][1] * f);
+                }
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const uint32_t raw16 = lds16(src + from[side][h] + 2 * grp);
-                            x[h] = p0 + lane + 32 * h >= end ? 0.0f : (side ? value_scale(raw16, bf16) : scale_of(raw16, bf16));
-                        }
-                        const float f = side ? 1.0f : pow2(1 - geo.s[0].bits[grp]);
-                        if (side) {
-                            const uint32_t big = __reduce_max_sync(0xffffffffu, max(__float_as_uint(x[0]), __float_as_uint(x[1])));
-                            // (beyond the end: none)
-                            const uint32_t a0 = p0 + lane >= end ? big : __float_as_uint(x[0]), a1 = p0 + lane + 32 >= end ? big : __float_as_uint(x[1]);
-                            const uint32_t least = __reduce_min_sync(0xffffffffu, min(a0, a1));
-                            if (lane == 0) sm_span[2 * st + grp] = make_float2(scale_bound(big), scale_floor(least));
-                        }
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 512 * side + 256 * grp + 128 * h), "f"(x[h] * f) : "memory");
-                    }
+                for (int grp = 0; grp < VNG; ++grp) {
+                    const float x0 = scale(1, grp, 0), x1 = scale(1, grp, 1);
+                    const uint32_t big = __reduce_max_sync(0xffffffffu, max(__float_as_uint(x0), __float_as_uint(x1)));
+                    // (beyond the end: none)
+                    const uint32_t a0 = p0 + lane >= end ? big : __float_as_uint(x0), a1 = p0 + lane + 32 >= end ? big : __float_as_uint(x1);
+                    const uint32_t least = __reduce_min_sync(0xffffffffu, min(a0, a1));
+                    if (lane == 0) sm_span[2 * st + grp] = make_float2(scale_bound(big), scale_floor(least));
+                    put(1, grp, x0, x1);
                 }
                 __syncwarp();
                 if (lane == 0) {
@@ -775,16 +788,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int k = 0; k < 8; ++k) tops[k] = fmaxf(x[k].x, x[k].y);
 #pragma unroll
                 for (int k = 8; k < kTok / 2; ++k) tops[k & 7] = fmaxf(fmaxf(tops[k & 7], x[k].x), x[k].y);
-                const float top = fac * fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
+                const float best = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
+                const float to_exp = exponent_factor(fac * sm_up[st], best), top = best * to_exp;
                 // (the distance to a power is the same before and after the maximum is raised)
-                bool over0 = (top - m) + span0.x - power0 > kRoom, over1 = VNG == 2 && (top - m) + span1.x - power1 > kRoom;
+                const float ahead = fmaf(best, to_exp, -m);
+                bool over0 = ahead + span0.x - power0 > kRoom, over1 = VNG == 2 && ahead + span1.x - power1 > kRoom;
                 if (__any_sync(0xffffffffu, top > m || over0 || over1)) {
                     const float by = raise(m, top);
                     l *= ex2(-by);
                     power0 -= by;
                     power1 -= by;
                     if (__any_sync(0xffffffffu, over0 || over1)) {
-                        const float lead = top - m;
+                        const float lead = fmaf(best, to_exp, -m);
                         // Weights times scales might leave fp16: the power becomes that of the largest product that the row
                         // sees, or of its largest weight and the smallest scale where scales are within 2^14 of each other.
                         float most0 = lead + span0.y, most1 = lead + span1.y;
@@ -805,7 +820,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 tc::tmem_ld8(t_b + c, v);
 #pragma unroll
                                 for (int k = 0; k < 8; ++k) {
-                                    const float p = ex2(fmaf(__uint_as_float(v[k]), fac, -m));
+                                    const float p = ex2(fmaf(__uint_as_float(v[k]), to_exp, -m));
                                     z0 = fmaxf(z0, p * lds32f(sc + 512 + 4 * (c + k)));
                                     if (VNG == 2) z1 = fmaxf(z1, p * lds32f(sc + 768 + 4 * (c + k)));
                                 }
@@ -849,7 +864,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
                             float2& y = x[16 * h + k + j];
-                            y = fma2(y, make_float2(fac, fac), make_float2(-m, -m));
+                            y = fma2(y, make_float2(to_exp, to_exp), make_float2(-m, -m));
                             y = make_float2(ex2(y.x), ex2(y.y));
                             sums[j] = fma2(y, make_float2(1.0f, 1.0f), sums[j]);
                             const float2 z = mul2(mul2(y, j ? make_float2(vv.z, vv.w) : make_float2(vv.x, vv.y)), make_float2(unit0, unit0));
