@@ -326,8 +326,8 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
         }
         __syncthreads();
 
-        // A row's running maximum (a whole number, in units of the exponent), sum, outputs and, for each value group, the
-        // power of two that its outputs and weights are relative to, counted from the maximum (RowPower).
+        // A row's running maximum (in units of the exponent), sum, outputs and, for each value group, the power of two that
+        // its outputs and weights are relative to, counted from the maximum (kv_device.cuh).
         float fac[NT][2], init[2][NT][2], m[NT][2], lsum[NT][2], power[2][NT][2];
         float o[NVB][2][NT][4];
 #pragma unroll
@@ -494,10 +494,17 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const float by = raise(m[nt][r], best[nt][r] * to_exp[nt][r]);
+                        const float top = best[nt][r] * to_exp[nt][r], by = raise(m[nt][r], top, top > m[nt][r]), rest = rest_of(by);
                         lsum[nt][r] *= ex2(-by);
-                        power[0][nt][r] -= by;
-                        power[1][nt][r] -= by;
+                        power[0][nt][r] -= whole_steps(by);
+                        power[1][nt][r] -= whole_steps(by);
+#pragma unroll
+                        for (int v = 0; v < NVB; ++v)
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                o[v][u][nt][r] *= rest;
+                                o[v][u][nt][2 + r] *= rest;
+                            }
                     }
             }
             // where a row's weights times scales might leave fp16: the power that those it sees need
@@ -550,8 +557,8 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                     const float pb = ex2(fmaf(x[j >> 1][nt][2 * (j & 1) + 1], to_exp[nt][1], -m[nt][1]));
                     lsum[nt][0] += pa;
                     lsum[nt][1] += pb;
-                    w[0][j >> 1][nt][j & 1] = transpose8(pack2(pa * sc[j].z * a0, pb * sc[j].z * b0));
-                    if (vs.ng == 2) w[1][j >> 1][nt][j & 1] = transpose8(pack2(pa * sc[j].w * a1, pb * sc[j].w * b1));
+                    w[0][j >> 1][nt][j & 1] = transpose8(pack2(pa * a0 * sc[j].z, pb * b0 * sc[j].z));
+                    if (vs.ng == 2) w[1][j >> 1][nt][j & 1] = transpose8(pack2(pa * a1 * sc[j].w, pb * b1 * sc[j].w));
                 }
             }
 

@@ -116,13 +116,14 @@ __device__ __forceinline__ float lg2(float x) {
 }
 
 // How weights become fp16.  With a row's running maximum m (of scores in units of
-// the exponent, rounded up, so that changes of it are exact) a token's weight is
-// p = 2^(score - m) <= 1; its products with the codes carry the value scale s.  A
-// row (and value group) rounds p s 2^-power to fp16 and sums outputs in that
-// unit.  The power follows the products p s of the tokens that the row sees: it
-// is raised to the largest where that exceeds 2^15 of it, and shrinks as m grows.
-// So rounding costs a row 2^-11 of each product, or 2^-25 of its largest, whatever
-// stands in tokens that it does not see, or hardly weighs.  (With a power common to
+// the exponent) a token's weight is p = 2^(score - m); its products with the codes
+// carry the value scale s.  A row (and value group) rounds p s 2^-power to fp16 and
+// sums outputs in that unit.  The power is a whole number that follows the products
+// p s of the tokens that the row sees: it is raised to the largest where that
+// exceeds 2^15 of it, and falls by m's raises, in whole steps; the outputs take the
+// rest.  So a weight of 1 costs its scale nothing, and rounding costs a
+// row 2^-11 of each other product, or 2^-25 of its largest, whatever stands in
+// tokens that it does not see, or hardly weighs.  (With a power common to
 // all rows of a block, over all of its scales, one scale of 2^16 times the others'
 // cost the rest 2 % of their weights.)
 // Finding the largest product takes a pass over the tokens, so it is done only
@@ -145,12 +146,15 @@ __device__ __forceinline__ float exponent_factor(float factor, float best) {
     const float whole = __uint_as_float((__float_as_uint(factor) + 0x007FFFFFu) & 0x7F800000u);
     return fabsf(best * factor) > 0x1p30f ? whole : factor;
 }
-// Raises a row's maximum to its block's `top`; returns by how much.
-__device__ __forceinline__ float raise(float& m, float top) {
-    const float to = fmaxf(m, ceilf(top)), by = to - m;
+// Raises a row's maximum to its block's `top` if it is to; returns by how much.
+__device__ __forceinline__ float raise(float& m, float top, bool is_to) {
+    const float to = is_to ? top : m, by = to - m;
     m = to;
     return by;
 }
+// The whole steps of a raise, and the factor that makes them of it.  (Rounded up: the unit never rises but to a product.)
+__device__ __forceinline__ float whole_steps(float by) { return by < 0x1p23f ? ceilf(by) : by; }
+__device__ __forceinline__ float rest_of(float by) { return by < 0x1p23f ? ex2(ceilf(by) - by) : 1.0f; }
 // Raises a power to the largest product, 2^most, if it is to; returns the factor of what is summed so far.
 // (126 at most: products reach 2^128, and both 2^power and its inverse are floats.)
 __device__ __forceinline__ float raise_power(float& power, float most, bool is_to) {
@@ -158,10 +162,11 @@ __device__ __forceinline__ float raise_power(float& power, float most, bool is_t
     power = to;
     return by < -126.0f ? 0.0f : pow2((int)by);
 }
-// 2^power, and 2^-power through the integer in a float's low bits.  (Below 2^-126, products are 0 as weights are.)
-__device__ __forceinline__ float power_of(float power) { return pow2((int)fmaxf(power, -126.0f)); }
+// 2^power, and 2^-power through the integer in a float's low bits.  (Not below 2^-110, so that weights times the latter
+// stay floats.)
+__device__ __forceinline__ float power_of(float power) { return pow2((int)fmaxf(power, -110.0f)); }
 __device__ __forceinline__ float unit_of(float power) {
-    return __uint_as_float(__float_as_uint(12582912.0f + 127.0f - fmaxf(power, -126.0f)) << 23);
+    return __uint_as_float(__float_as_uint(12582912.0f + 127.0f - fmaxf(power, -110.0f)) << 23);
 }
 
 // Eight codes of a block, its l-th quarter, unpack to four half pairs: which codes

@@ -54,6 +54,8 @@ constexpr int kThreads = 640;
 constexpr int kAtom = kTok * 128;        // bytes of a 64-code column group of a K or V tile
 constexpr int kQAtom = 128 * 128;        // ... of a query tile
 constexpr int kSlotCols = 256;           // TMEM columns of a softmax group: S (and P over it), then O
+// A row's running maximum may be exceeded by 2^kLazy before it is raised, and O with it.
+constexpr float kLazy = 13.0f;
 // Columns of a softmax group in front of O: scores (the weights of the first value group go over them), and those
 // of the second key group or the weights of the second value group
 __host__ __device__ constexpr int s_cols(int k_groups, int v_groups) { return k_groups == 2 ? 2 * kTok : (v_groups == 2 ? kTok + kTok / 2 : kTok); }
@@ -716,8 +718,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float fac = sm_fac[(streams ? 0 : 128 * s) + r_tile];
             const uint32_t lanes = (uint32_t)(quad * 32) << 16;
             const uint32_t t_s = tmem + s * kSlotCols + lanes;
-            // the maximum (a whole number, in units of the exponent), the sum, and each value group's power of two
-            // (kv_device.cuh) that weights and outputs are relative to
+            // the maximum (in units of the exponent), the sum, and each value group's power of two (kv_device.cuh) that
+            // weights and outputs are relative to
             float m = kUnset, l = 0.0f, power0 = kUnset, power1 = kUnset;
             const int mine = s < groups ? (streams ? (nblk - s + 1) / 2 : nblk) : 0;
             const int sure = min(len, end);
@@ -789,17 +791,17 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int k = 8; k < kTok / 2; ++k) tops[k & 7] = fmaxf(fmaxf(tops[k & 7], x[k].x), x[k].y);
                 const float best = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
-                const float to_exp = exponent_factor(fac * sm_up[st], best), top = best * to_exp;
-                // (the distance to a power is the same before and after the maximum is raised)
+                const float to_exp = exponent_factor(fac * sm_up[st], best);
                 const float ahead = fmaf(best, to_exp, -m);
-                bool over0 = ahead + span0.x - power0 > kRoom, over1 = VNG == 2 && ahead + span1.x - power1 > kRoom;
-                if (__any_sync(0xffffffffu, top > m || over0 || over1)) {
-                    const float by = raise(m, top);
+                if (__any_sync(0xffffffffu, ahead > kLazy || ahead + span0.x - power0 > kRoom ||
+                                                (VNG == 2 && ahead + span1.x - power1 > kRoom))) {
+                    const float by = raise(m, best * to_exp, ahead > kLazy), lead = fmaf(best, to_exp, -m);
+                    float down0 = rest_of(by), down1 = down0;       // of what is summed so far
                     l *= ex2(-by);
-                    power0 -= by;
-                    power1 -= by;
+                    power0 -= whole_steps(by);
+                    power1 -= whole_steps(by);
+                    bool over0 = lead + span0.x - power0 > kRoom, over1 = VNG == 2 && lead + span1.x - power1 > kRoom;
                     if (__any_sync(0xffffffffu, over0 || over1)) {
-                        const float lead = fmaf(best, to_exp, -m);
                         // Weights times scales might leave fp16: the power becomes that of the largest product that the row
                         // sees, or of its largest weight and the smallest scale where scales are within 2^14 of each other.
                         float most0 = lead + span0.y, most1 = lead + span1.y;
@@ -830,24 +832,25 @@ __global__ void __launch_bounds__(kThreads, 1)
                             over0 = most0 - power0 > kRoom;
                             over1 = VNG == 2 && most1 - power1 > kRoom;
                         }
-                        const float down0 = raise_power(power0, most0, over0), down1 = raise_power(power1, most1, over1);
-                        if (i != 0 && __any_sync(0xffffffffu, down0 != 1.0f || down1 != 1.0f)) {
-                            // The MMAs that wrote O have to be complete: with one buffer they came before those that wrote
-                            // these scores.
-                            if (SB == 2) {
-                                ok = wait(Bars::pv_done + s, done ^ 1u);
-                                if (!ok) break;
-                                tc::tc_fence_after();
-                            }
+                        down0 *= raise_power(power0, most0, over0);
+                        down1 *= raise_power(power1, most1, over1);
+                    }
+                    if (i != 0 && __any_sync(0xffffffffu, down0 != 1.0f || down1 != 1.0f)) {
+                        // The MMAs that wrote O have to be complete: with one buffer they came before those that wrote
+                        // these scores.
+                        if (SB == 2) {
+                            ok = wait(Bars::pv_done + s, done ^ 1u);
+                            if (!ok) break;
+                            tc::tc_fence_after();
+                        }
 #pragma unroll 1
-                            for (int c = 0; c < pl.o_cols; c += 16) {
-                                uint32_t v[16];
-                                tc::tmem_ld16(t_s + o_off + c, v);
-                                const float f = c < va0 ? down0 : down1;
+                        for (int c = 0; c < pl.o_cols; c += 16) {
+                            uint32_t v[16];
+                            tc::tmem_ld16(t_s + o_off + c, v);
+                            const float f = c < va0 ? down0 : down1;
 #pragma unroll
-                                for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f);
-                                tmem_st16v(t_s + o_off + c, v);
-                            }
+                            for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f);
+                            tmem_st16v(t_s + o_off + c, v);
                         }
                     }
                 }
@@ -867,7 +870,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             y = fma2(y, make_float2(to_exp, to_exp), make_float2(-m, -m));
                             y = make_float2(ex2(y.x), ex2(y.y));
                             sums[j] = fma2(y, make_float2(1.0f, 1.0f), sums[j]);
-                            const float2 z = mul2(mul2(y, j ? make_float2(vv.z, vv.w) : make_float2(vv.x, vv.y)), make_float2(unit0, unit0));
+                            const float2 z = mul2(mul2(y, make_float2(unit0, unit0)), j ? make_float2(vv.z, vv.w) : make_float2(vv.x, vv.y));
                             w[k + j] = pack2(z.x, z.y);
                         }
                     }
@@ -876,8 +879,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int k = 0; k < 16; k += 2) {
                             const float4 vv = lds128f(sc + 768 + 128 * h + 8 * k);
-                            const float2 y0 = mul2(mul2(x[16 * h + k], make_float2(vv.x, vv.y)), make_float2(unit1, unit1));
-                            const float2 y1 = mul2(mul2(x[16 * h + k + 1], make_float2(vv.z, vv.w)), make_float2(unit1, unit1));
+                            const float2 y0 = mul2(mul2(x[16 * h + k], make_float2(unit1, unit1)), make_float2(vv.x, vv.y));
+                            const float2 y1 = mul2(mul2(x[16 * h + k + 1], make_float2(unit1, unit1)), make_float2(vv.z, vv.w));
                             w[k] = pack2(y0.x, y0.y);
                             w[k + 1] = pack2(y1.x, y1.y);
                         }
