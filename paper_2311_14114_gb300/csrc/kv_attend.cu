@@ -814,7 +814,8 @@ RowsLaunch plan_rows(const KvGeom& geo, int64_t T, int64_t group) {
     else if (ks.row_bytes <= 128 && vs.row_bytes <= 64 && nvb <= 4) r.nvb = 4, r.ks = 128, r.vs = 64;
     else if (ks.row_bytes <= 128 && vs.row_bytes <= 128 && nvb <= 4) r.nvb = 4, r.ks = 128, r.vs = 128;
     else r.nvb = 8, r.ks = 256, r.vs = 256;
-    r.nt = rows <= 8 ? 1 : (rows <= 16 || r.nvb == 8 ? 2 : 4);
+    // (Four tiles of 8 rows to a warp do not fit its registers: 32 rows over 131071 tokens 270 us, as two tiles of 16 158.)
+    r.nt = rows <= 8 ? 1 : 2;
     RowsPlan& p = r.pl;
     const int R = 8 * r.nt;
     p.rows = (int)rows;
@@ -860,16 +861,15 @@ template <int NVB, int KS, int VS>
 cudaError_t run_rows(const KvGeom& geo, const KvAttendArgs& a, const RowsLaunch& r, const KvMaps& maps, int grid,
                      cudaStream_t st) {
     if (r.nt == 1) return run_rows<1, NVB, KS, VS>(geo, a, r, maps, grid, st);
-    if constexpr (NVB <= 4) {
-        if (r.nt == 4) return run_rows<4, NVB, KS, VS>(geo, a, r, maps, grid, st);
-    }
     return run_rows<2, NVB, KS, VS>(geo, a, r, maps, grid, st);
 }
 
-// Whether the rows of a key head go to the tile kernel: more than 16, where its operands fit.  (This kernel and that
-// one, us: 16 sequences over up to 4096 tokens 8 rows 33 and 80, 16 rows 48 and 84, 32 rows 94 and 92; one over
-// 131071 tokens 16 rows 86 and 169, 32 rows 199 and 168; over 500, 32 rows 38 and 29.)
-bool takes_tile(const KvGeom& geo, int64_t T, int64_t group) { return T * group > 16 && kv_tile_supported(geo, T, group); }
+// Whether the rows of a key head go to the tile kernel: more than 32, where its operands fit.  (This kernel and that
+// one, us, key groups of 96 and 32 channels: 16 sequences over up to 4096 tokens 16 rows 51 and 87, 32 rows 80 and 94,
+// 48 rows 113 and 95; one over 131071 tokens 32 rows 158 and 175, 48 rows 216 and 179; over 500, 32 rows 22 and 30,
+// 64 rows 25 and 31.  One key group, or heads of 64: the same side wins, 32 and 48 rows included, but for 64 channels
+// over 131071, 32 rows 154 and 152.)
+bool takes_tile(const KvGeom& geo, int64_t T, int64_t group) { return T * group > 32 && kv_tile_supported(geo, T, group); }
 
 }  // namespace
 
