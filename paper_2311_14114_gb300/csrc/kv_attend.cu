@@ -148,8 +148,11 @@ __device__ __forceinline__ uint32_t swizzle_of(int row) {
 template <int S>
 constexpr int kRowStep = S == 256 ? 128 : S;
 
+// Two CTAs per SM where 128 registers do: 8 rows, up to 128 value channels.  (16 rows of 64 channels, two CTAs with
+// 432 bytes spilled and one, us: 3 x 13 drafts over 1501 tokens 24.1 and 20.9, 16 sequences over 4096 48.5 and 41.3,
+// one over 131071 92.5 and 76.6.)
 template <int NT, int NVB>
-constexpr int min_ctas() { return NT * NVB <= 4 ? 2 : 1; }
+constexpr int min_ctas() { return NT == 1 && NVB <= 4 ? 2 : 1; }
 
 // KS, VS: bytes of a key and a value row in shared memory.  WIDE: group 0 of
 // both sides has 4-bit codes and group 1, where there is one, 8-bit codes;
@@ -829,7 +832,7 @@ RowsLaunch plan_rows(const KvGeom& geo, int64_t T, int64_t group) {
     auto warp_bytes = [&](int stages) { return stages * (stage + p.scale_bytes) + 16 * kChunk; };
     // two stages at least; two CTAs per SM where they and the registers allow it
     r.warps = 8;
-    r.ctas_per_sm = r.nt * r.nvb <= 4 && fixed + 8 * warp_bytes(2) <= kHalfSmem ? 2 : 1;
+    r.ctas_per_sm = r.nt == 1 && r.nvb <= 4 && fixed + 8 * warp_bytes(2) <= kHalfSmem ? 2 : 1;
     const int budget = r.ctas_per_sm == 2 ? kHalfSmem : kMaxSmem;
     if (fixed + 8 * warp_bytes(2) > budget) r.warps = 4;
     p.stages = 2;
