@@ -316,8 +316,9 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                 if (lane == 0) {
                     sm_init[r] = -sum0;
                     sm_init[R + r] = -sum1;
-                    // positive, so that it can be applied behind the maximum
-                    sm_fac[r] = fmaxf(ldexpf(fabsf(a.scale) * kLog2e, 24 - (n_min - 1) - e), 0x1p-126f);
+                    // positive, so that it can be applied behind the maximum; finite where queries are (of scores that
+                    // large one takes the whole weight)
+                    sm_fac[r] = fminf(fmaxf(ldexpf(fabsf(a.scale) * kLog2e, 24 - (n_min - 1) - e), 0x1p-126f), 0x1p126f);
                 }
             }
             for (int p = tid; p < 32 * NVB; p += blockDim.x) {
