@@ -29,11 +29,11 @@
 //    exact in fp16 then).  Softmax weights times value scales are rounded to fp16
 //    relative to a power of two of the row's own (kv_device.cuh).
 //
-// Bound by instructions, about 800 for a chunk of 32 tokens (keys 4/8 bits,
+// Bound by instructions, about 830 for a chunk of 32 tokens (keys 4/8 bits,
 // values 4, 128 channels, 8 rows) at 2.5 a cycle, and for short contexts by what
 // comes before and after: the split, queries, and the joins take 10 to 20 us.
-// Measured (GB300): 131071 tokens of one sequence, 8 key heads: 58 us (2.7 TB/s);
-// 64 sequences of up to 8192 tokens: 121 us (2.8 TB/s); 97 tokens: 12 us.
+// Measured (GB300): 131071 tokens of one sequence, 8 key heads: 60 us (2.6 TB/s);
+// 64 sequences of up to 8192 tokens: 125 us (2.7 TB/s); 97 tokens: 12 us.
 #include <type_traits>
 
 #include "kv_device.cuh"
@@ -44,8 +44,8 @@ namespace soniq {
 namespace {
 
 constexpr int kChunk = 32;                   // tokens a warp takes at a time
-// An item's queries and results take about as long as this many chunks.  (64 sequences of up to 8192 tokens, us: 8: 138,
-// 16: 131, 32: 119, 64: 125.)
+// An item's queries and results take about as long as this many chunks.  (64 sequences of up to 8192 tokens, us: 8: 141,
+// 16: 136, 32: 125, 64: 131.)
 constexpr int kLead = 32;
 
 struct RowsPlan {

@@ -28,16 +28,16 @@
 // O = P V, so both operand tiles have one layout: 64-code column groups of
 // [token][128 bytes], 16-byte pieces swizzled by the token.
 //
-// Bound by the softmax warps where scores have two buffers: 2930 cycles for 64
-// tokens of 256 rows (waits 340, scores times key scales 560, maxima and their
-// check 750, exponentials and rounding 900, the rest the loop), of which the
-// tensor cores work 630.  With two key groups TMEM holds one buffer, and the way
-// scores - softmax - outputs - scores is one chain of about 4500 cycles, two of
+// Bound by the softmax warps where scores have two buffers: about 3200 cycles for
+// 64 tokens of 256 rows, of which the tensor cores work 630.  (2930 before rows had
+// powers of two of their own: waits 340, scores times key scales 560, maxima and
+// their check 750, exponentials and rounding 900, the rest the loop.)  With two key groups TMEM holds one buffer, and the way
+// scores - softmax - outputs - scores is one chain of about 4600 cycles, two of
 // which run side by side.  An item costs 12000 cycles for its queries and 5000
 // to 9000 for its results besides, so short items count kLead blocks more.
 // Measured (GB300): 4 x 64 drafted tokens x 8 heads per key head over 16384
-// cached ones 114 us (600 TFLOP/s), 2 x 512 x 4 over 3500 158 us (400), 16 x 24 x
-// 4 over up to 4096 96 us.
+// cached ones 122 us (560 TFLOP/s), 2 x 512 x 4 over 3500 162 us (390), 16 x 24 x
+// 4 over up to 4096 99 us.
 #include <type_traits>
 
 #include "kv_device.cuh"
@@ -82,7 +82,7 @@ struct JoinItem {
 };
 constexpr int kJoinBytes = 8192;
 // An item's queries and results take about as long as this many blocks.  (Blocks, us: 16 x 24 drafted tokens over
-// ragged contexts 4: 109, 8: 96, 16: 90; 2 x 512 tokens 4: 155, 8: 156, 16: 173.)
+// ragged contexts 4: 113, 8: 100, 16: 92; 2 x 512 tokens 4: 161, 8: 162, 16: 177.)
 constexpr int kLead = 8;
 
 struct Bars {               // offsets in 8-byte barriers

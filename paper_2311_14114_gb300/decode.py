@@ -11,8 +11,10 @@ the context; they are quantized from the same 16-bit rows again, so a token's
 codes do not depend on whether it was drafted.
 
 This module sequences the calls and does the integer bookkeeping of slots;
-every arithmetic step runs in the library's kernels.  Position encodings act
-on q and k between the projection and the cache, outside this path."""
+every arithmetic step runs in the library's kernels.  The layer is fp16 and
+applies no position encoding: there is no place for one between its projection
+and its cache.  A model that turns q and k by their positions, or runs in bf16,
+makes the same calls itself."""
 from __future__ import annotations
 
 from typing import Optional, Tuple
