@@ -31,10 +31,11 @@
 // Bound by the softmax warps where scores have two buffers: about 3200 cycles for
 // 64 tokens of 256 rows, of which the tensor cores work 630.  (2930 before rows had
 // powers of two of their own: waits 340, scores times key scales 560, maxima and
-// their check 750, exponentials and rounding 900, the rest the loop.)  With two key groups TMEM holds one buffer, and the way
-// scores - softmax - outputs - scores is one chain of about 4600 cycles, two of
-// which run side by side.  An item costs 12000 cycles for its queries and 5000
-// to 9000 for its results besides, so short items count kLead blocks more.
+// their check 750, exponentials and rounding 900, the rest the loop.)  With two key
+// groups TMEM holds one buffer, and the way scores - softmax - outputs - scores is
+// one chain of about 4600 cycles, two of which run side by side.  An item costs
+// 12000 cycles for its queries and 5000 to 9000 for its results besides, so short
+// items count kLead blocks more.
 // Measured (GB300): 4 x 64 drafted tokens x 8 heads per key head over 16384
 // cached ones 122 us (560 TFLOP/s), 2 x 512 x 4 over 3500 162 us (390), 16 x 24 x
 // 4 over up to 4096 99 us.
