@@ -341,7 +341,8 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                 fac[nt][r] = sm_fac[8 * nt + 2 * l + r];
                 init[0][nt][r] = sm_init[8 * nt + 2 * l + r];
                 init[1][nt][r] = sm_init[R + 8 * nt + 2 * l + r];
-                m[nt][r] = power[0][nt][r] = power[1][nt][r] = kUnset;
+                m[nt][r] = kUnset;
+                power[0][nt][r] = power[1][nt][r] = kLeast;
                 lsum[nt][r] = 0.0f;
             }
         }
@@ -498,10 +499,11 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const float top = best[nt][r] * to_exp[nt][r], by = raise(m[nt][r], top, top > m[nt][r]), rest = rest_of(by);
+                        const float top = best[nt][r] * to_exp[nt][r], by = raise(m[nt][r], top, top > m[nt][r]);
                         lsum[nt][r] *= ex2(-by);
-                        power[0][nt][r] -= whole_steps(by);
-                        power[1][nt][r] -= whole_steps(by);
+                        const float rest = rest_of(by), steps = whole_steps(by);
+                        power[0][nt][r] -= steps;
+                        if (vs.ng == 2) power[1][nt][r] -= steps;
 #pragma unroll
                         for (int v = 0; v < NVB; ++v)
 #pragma unroll
@@ -511,15 +513,15 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                             }
                     }
             }
-            // where a row's weights times scales might leave fp16: the power that those it sees need
+            // where a row's weights times scales might leave fp16: the power that those it sees need; and the least one
             bool over = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     const float lead = fmaf(best[nt][r], to_exp[nt][r], -m[nt][r]);
-                    over |= lead - power[0][nt][r] > room[0];
-                    if (vs.ng == 2) over |= lead - power[1][nt][r] > room[1];
+                    over |= lead - power[0][nt][r] > room[0] || power[0][nt][r] < kLeast;
+                    if (vs.ng == 2) over |= lead - power[1][nt][r] > room[1] || power[1][nt][r] < kLeast;
                 }
             if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
@@ -537,7 +539,8 @@ __global__ void __launch_bounds__(256, (min_ctas<NT, NVB>()))
                             z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, 4));
                             z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, 8));
                             z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, 16));
-                            down[nt][r] = raise_power(power[grp][nt][r], z, z - power[grp][nt][r] > kRoom);
+                            down[nt][r] = floor_power(power[grp][nt][r]);
+                            down[nt][r] *= raise_power(power[grp][nt][r], z, z - power[grp][nt][r] > kRoom);
                         }
 #pragma unroll
                     for (int v = 0; v < NVB; ++v)

@@ -121,16 +121,17 @@ __device__ __forceinline__ float lg2(float x) {
 // sums outputs in that unit.  The power is a whole number that follows the products
 // p s of the tokens that the row sees: it is raised to the largest where that
 // exceeds 2^15 of it, and falls by m's raises, in whole steps; the outputs take the
-// rest.  So a weight of 1 costs its scale nothing, and rounding costs a
-// row 2^-11 of each other product, or 2^-25 of its largest, whatever stands in
-// tokens that it does not see, or hardly weighs.  (With a power common to
-// all rows of a block, over all of its scales, one scale of 2^16 times the others'
-// cost the rest 2 % of their weights.)
+// rest.  (It is -110 at least, where a row begins.)  So a weight of 1 costs its
+// scale nothing, and rounding costs a row 2^-11 of each other product, or 2^-25 of
+// its largest, whatever stands in tokens that it does not see, or hardly weighs.
+// (With a power common to all rows of a block, over all of its scales, one scale of
+// 2^16 times the others' cost the rest 2 % of their weights.)
 // Finding the largest product takes a pass over the tokens, so it is done only
 // where the bound from the largest scale of the block and the row's largest score
 // leaves the range.
-constexpr float kUnset = -3.402823466e+38f;      // no token seen, no product met
+constexpr float kUnset = -3.402823466e+38f;      // maximum of no token seen
 constexpr float kRoom = 15.0f;
+constexpr float kLeast = -110.0f;                // smallest power: weights (up to 2^13) times its inverse stay floats
 
 // log2 of the largest value scale of a block, from its bits (none: far below any product), at most 0.09 too large:
 // log2(1 + f) is f to f + 0.0861.
@@ -152,22 +153,27 @@ __device__ __forceinline__ float raise(float& m, float top, bool is_to) {
     m = to;
     return by;
 }
-// The whole steps of a raise, and the factor that makes them of it.  (Rounded up: the unit never rises but to a product.)
+__device__ __forceinline__ float factor_of(float by) { return by < -126.0f ? 0.0f : pow2((int)by); }      // 2^by, a whole by <= 0
+// A raise of the maximum in whole steps, and the factor that is too much.  (Rounded up: the unit never rises but to a
+// product, or to stay above the smallest.  From 2^23 on floats are whole.)
 __device__ __forceinline__ float whole_steps(float by) { return by < 0x1p23f ? ceilf(by) : by; }
 __device__ __forceinline__ float rest_of(float by) { return by < 0x1p23f ? ex2(ceilf(by) - by) : 1.0f; }
+// Brings a lowered power up to the smallest; returns the factor of what is summed so far.
+__device__ __forceinline__ float floor_power(float& power) {
+    const float from = power;
+    power = fmaxf(from, kLeast);
+    return factor_of(from - power);
+}
 // Raises a power to the largest product, 2^most, if it is to; returns the factor of what is summed so far.
 // (126 at most: products reach 2^128, and both 2^power and its inverse are floats.)
 __device__ __forceinline__ float raise_power(float& power, float most, bool is_to) {
     const float to = is_to ? fminf(ceilf(most), 126.0f) : power, by = power - to;
     power = to;
-    return by < -126.0f ? 0.0f : pow2((int)by);
+    return factor_of(by);
 }
-// 2^power, and 2^-power through the integer in a float's low bits.  (Not below 2^-110, so that weights times the latter
-// stay floats.)
-__device__ __forceinline__ float power_of(float power) { return pow2((int)fmaxf(power, -110.0f)); }
-__device__ __forceinline__ float unit_of(float power) {
-    return __uint_as_float(__float_as_uint(12582912.0f + 127.0f - fmaxf(power, -110.0f)) << 23);
-}
+// 2^power, and 2^-power through the integer in a float's low bits.
+__device__ __forceinline__ float power_of(float power) { return pow2((int)power); }
+__device__ __forceinline__ float unit_of(float power) { return __uint_as_float(__float_as_uint(12582912.0f + 127.0f - power) << 23); }
 
 // Eight codes of a block, its l-th quarter, unpack to four half pairs: which codes
 // they are, and the powers of two their places in the word give them.

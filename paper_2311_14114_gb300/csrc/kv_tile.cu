@@ -721,7 +721,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t t_s = tmem + s * kSlotCols + lanes;
             // the maximum (in units of the exponent), the sum, and each value group's power of two (kv_device.cuh) that
             // weights and outputs are relative to
-            float m = kUnset, l = 0.0f, power0 = kUnset, power1 = kUnset;
+            float m = kUnset, l = 0.0f, power0 = kLeast, power1 = kLeast;
             const int mine = s < groups ? (streams ? (nblk - s + 1) / 2 : nblk) : 0;
             const int sure = min(len, end);
             Ring kv = kv0;
@@ -797,10 +797,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (__any_sync(0xffffffffu, ahead > kLazy || ahead + span0.x - power0 > kRoom ||
                                                 (VNG == 2 && ahead + span1.x - power1 > kRoom))) {
                     const float by = raise(m, best * to_exp, ahead > kLazy), lead = fmaf(best, to_exp, -m);
-                    float down0 = rest_of(by), down1 = down0;       // of what is summed so far
+                    const float rest = rest_of(by), steps = whole_steps(by);
+                    power0 -= steps;
+                    if (VNG == 2) power1 -= steps;
+                    float down0 = rest * floor_power(power0), down1 = rest * floor_power(power1);       // of what is summed so far
                     l *= ex2(-by);
-                    power0 -= whole_steps(by);
-                    power1 -= whole_steps(by);
                     bool over0 = lead + span0.x - power0 > kRoom, over1 = VNG == 2 && lead + span1.x - power1 > kRoom;
                     if (__any_sync(0xffffffffu, over0 || over1)) {
                         // Weights times scales might leave fp16: the power becomes that of the largest product that the row
