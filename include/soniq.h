@@ -548,7 +548,7 @@ SONIQ_API soniq_status soniq_kv_read(const soniq_kv_cache *cache, const int64_t 
  * Scores, statistics and sums are fp32; softmax weights times the value scale
  * are rounded to fp16 for the product, relative to a power of two that each row
  * (and value group) takes from the tokens that it sees: by 2^-11, or 2^-25 of
- * the row's largest.
+ * the row's largest (of 2^-110 at least).
  */
 SONIQ_API soniq_status soniq_kv_attend(const soniq_kv_cache *cache, const void *Q, int64_t q_seq_stride,
                                        int64_t q_token_stride, int64_t q_head_stride, const int32_t *page_table,
