@@ -561,6 +561,105 @@ SONIQ_API soniq_status soniq_kv_attend(const soniq_kv_cache *cache, const void *
 /* Scratch bytes of soniq_kv_attend.  Host only; -1 on a bad argument. */
 SONIQ_API int64_t soniq_kv_attend_scratch_bytes(const soniq_kv_cache *cache, int32_t B, int32_t T, int32_t q_heads);
 
+/* ---- a step over packed prompts and new tokens --------------------------- */
+
+/*
+ * A step holds tokens of B sequences back to back ("packed"): those of
+ * sequence b are starts[b] .. starts[b + 1] - 1.  soniq_kv_plan says where they
+ * go; per layer, soniq_rotate_heads turns the projection's queries and keys by
+ * their positions, soniq_kv_write puts keys and values into their slots, and
+ * soniq_prompt_attend is the attention of whole prompts over themselves (in 16
+ * bits, before the cache rounds them), soniq_kv_attend that of tokens behind a
+ * cached context.
+ */
+
+/*
+ * The pages, slots and positions of a step, from the lengths of its sequences.
+ * Sequence b has max(lengths[b], 0) tokens in the cache and is to have
+ * max(targets[b], 0): what it lacks are its tokens of this step.  A sequence
+ * that grows takes pages from a pool, one that shrinks (drafts that were not
+ * accepted) or leaves (a negative target) gives back those that it no longer
+ * reaches.
+ *   - Pages given back are numbered by sequence and place, 0 .. R - 1.  A page
+ *     that is needed is the lowest of them that is left, and once there is none
+ *     the pool's last.  Pages are needed in the same order.  What was given back
+ *     and not needed goes behind the pool's pages, the lowest number last: so
+ *     shrinking undoes growing.
+ *   - A sequence is served if its pages fit its row of the table, its tokens lie
+ *     below max_tokens, and the pool lasts; the first for which it does not last
+ *     has all later ones that need pages wait too.  One that is not served
+ *     changes nothing: no page, its length kept, its tokens' slots -1.
+ * page_size 16 to 256, a power of two; B <= 8192, B * max_pages < 2^31
+ * (SONIQ_ERR_UNSUPPORTED otherwise).
+ *   table       device int32, row b at table + b * table_stride, max_pages entries:
+ *               the pages of sequence b in order.  Entries of pages taken are
+ *               written, all others left as they are (also those given back).
+ *   free_pages  device int32 [n_pages]: the pool's pages, *count of them.  Entries
+ *               from the new count on are left as they are.
+ *   count       device int32 [2]: pages in the pool, and a word that must be zero
+ *               before the first call and is zero after each.
+ *   count_out   device int32: the new count; may be count.
+ *   lengths, targets   device int32 [B].
+ *   starts      device out int32 [B + 1], at most max_tokens each.
+ *   positions   device out int32 [max_tokens], 0 behind the step's tokens.
+ *   slots       device out int64 [max_tokens], -1 there (soniq_kv_write skips them).
+ *   lengths_out device out int32 [B]: the target of a sequence that was served (-1
+ *               where it is negative), else the length; may be lengths or targets.
+ * Outputs must not overlap inputs or each other otherwise.  Pages outside the
+ * cache, or a count that is, are reported by soniq_sync_status as
+ * SONIQ_ERR_INVALID_ARG; a token in such a page gets a slot beyond the cache, which
+ * soniq_kv_write skips and reports.  Calls that share a pool must not overlap.
+ */
+SONIQ_API soniq_status soniq_kv_plan(int32_t page_size, int64_t n_pages, int32_t *table, int64_t table_stride,
+                                     int32_t max_pages, int32_t *free_pages, int32_t *count, int32_t *count_out,
+                                     const int32_t *lengths, const int32_t *targets, int32_t B, int32_t max_tokens,
+                                     int32_t *starts, int32_t *positions, int64_t *slots, int32_t *lengths_out,
+                                     soniq_stream_t stream);
+
+/*
+ * A rotation by position: of a head's first `channels` channels (even), pair p
+ * at position t turns by the angle t * 2 pi * turns[p] / 2^64:
+ *   (a, b) -> magnitude * (a cos - b sin, b cos + a sin).
+ * Pair p is channels (p, p + channels / 2), or, interleaved, (2 p, 2 p + 1).
+ *   turns      device uint64 [channels / 2]: turns a position in units of 2^-64,
+ *              modulo 1.  The product with a position is exact modulo a turn.
+ */
+typedef struct soniq_rotary {
+    int32_t channels;
+    int32_t interleaved;
+    float magnitude;
+    const uint64_t *turns;
+} soniq_rotary;
+
+/* Heads [token][head][D] to normalise and turn.  Strides in elements; `out` may
+ * be `in` with the same strides, else must not overlap it.  gain: device fp32 [D],
+ * or NULL for no norm. */
+typedef struct soniq_heads {
+    int32_t heads;
+    const void *in;
+    int64_t in_token_stride, in_head_stride;
+    void *out;
+    int64_t out_token_stride, out_head_stride;
+    const float *gain;
+} soniq_heads;
+
+/*
+ * For each of n tokens and each head of q and of k (either may be NULL):
+ *   y = x * gain / sqrt(mean(x^2) + eps)      (where there is a gain; over all D channels)
+ * then the rotation (rotary NULL or of 0 channels: none), in fp32, rounded once
+ * to `dtype` (SONIQ_OUT_F16 or SONIQ_OUT_BF16).
+ *   positions  device int32 [n], any value; NULL where nothing is turned.
+ *   D          1..256 (SONIQ_ERR_UNSUPPORTED above); at most 4096 heads a side.
+ *   eps        finite, not negative.
+ * Pointers need the alignment of their elements.  Rows that are 16-byte pieces (D
+ * and strides multiples of 8, pointers on 16 bytes) whose pairs lie whole pieces
+ * apart (interleaved, or channels a multiple of 16) are moved in those; others by
+ * a slower kernel.
+ */
+SONIQ_API soniq_status soniq_rotate_heads(const soniq_rotary *rotary, const int32_t *positions, int64_t n, int32_t D,
+                                          int32_t dtype, const soniq_heads *q, const soniq_heads *k, float eps,
+                                          soniq_stream_t stream);
+
 /* Waits for `stream`, then returns SONIQ_ERR_TIMEOUT if any kernel of this
  * library on the current device recorded a timed-out wait since the last
  * call (and clears that record), SONIQ_ERR_INVALID_ARG if none did but a

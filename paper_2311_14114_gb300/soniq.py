@@ -10,7 +10,8 @@ from __future__ import annotations
 import ctypes
 import math
 import os
-from typing import Optional, Sequence, Tuple
+from fractions import Fraction
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
@@ -38,7 +39,7 @@ EXPORTED = ["soniq_abi_version", "soniq_status_string", "soniq_group_codes",
             "soniq_quantize_act_oneshot", "soniq_mp_gemm", "soniq_mp_gemm_path", "soniq_mp_gemm_kernel",
             "soniq_mp_gemm_scratch_bytes", "soniq_mp_conv2d", "soniq_mp_conv2d_scratch_bytes", "soniq_sync_status",
             "soniq_test_drop_barrier_arrival", "soniq_kv_row_bytes", "soniq_kv_validate", "soniq_kv_write",
-            "soniq_kv_read", "soniq_kv_attend", "soniq_kv_attend_scratch_bytes"]
+            "soniq_kv_read", "soniq_kv_attend", "soniq_kv_attend_scratch_bytes", "soniq_kv_plan", "soniq_rotate_heads"]
 
 _SCALE = {"tensor": SCALE_PER_TENSOR, "row": SCALE_PER_ROW, "calibrated": SCALE_CALIBRATED}
 
@@ -77,6 +78,17 @@ class CKvCache(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("k", CKvRows), ("v", CKvRows),
                 ("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
                 ("v_codes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+
+
+class CRotary(ctypes.Structure):
+    _fields_ = [("channels", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("turns", ctypes.c_void_p)]
+
+
+class CHeads(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("in_", ctypes.c_void_p), ("in_token_stride", ctypes.c_int64),
+                ("in_head_stride", ctypes.c_int64), ("out", ctypes.c_void_p), ("out_token_stride", ctypes.c_int64),
+                ("out_head_stride", ctypes.c_int64), ("gain", ctypes.c_void_p)]
 
 
 _lib = None
@@ -139,6 +151,10 @@ def lib() -> ctypes.CDLL:
         L.soniq_kv_attend.restype = i32
         L.soniq_kv_attend_scratch_bytes.argtypes = [P, i32, i32, i32]
         L.soniq_kv_attend_scratch_bytes.restype = i64
+        L.soniq_kv_plan.argtypes = [i32, i64, P, i64, i32, P, P, P, P, P, i32, i32, P, P, P, P, P]
+        L.soniq_kv_plan.restype = i32
+        L.soniq_rotate_heads.argtypes = [P, P, i64, i32, i32, P, P, ctypes.c_float, P]
+        L.soniq_rotate_heads.restype = i32
         _lib = L
     return _lib
 
@@ -574,6 +590,168 @@ def kv_attend(cache: KVCache, q: torch.Tensor, page_table: torch.Tensor, lengths
                              Hq, 1.0 / math.sqrt(D) if scale is None else float(scale), out.data_ptr(),
                              _ptr(scratch), max(need, 0), _stream(stream)), "soniq_kv_attend")
     return out
+
+
+def _need_here(t: torch.Tensor, dtype, shape: Optional[tuple], name: str):
+    """A contiguous tensor on the current device, whose streams the library launches on."""
+    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
+        of = "" if shape is None else f" {list(shape)}"
+        raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor{of}")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is not on the current CUDA device")
+
+
+class KVPages:
+    """Which pages each sequence of a cache holds, and the pool of the others, for kv_plan.
+
+    table: int32 [sequences][max_pages], row b the pages of sequence b in order
+    (page_table of kv_attend); free: int32 [n_pages], the pool; count: int32 [2],
+    its size and a word that stays zero.  A new pool holds every page."""
+
+    def __init__(self, n_pages: int, page_size: int, sequences: int, max_pages: int, device="cuda"):
+        self.n_pages, self.page_size = int(n_pages), int(page_size)
+        self.table = torch.full((sequences, max_pages), -1, dtype=torch.int32, device=device)
+        self.free = torch.arange(self.n_pages - 1, -1, -1, dtype=torch.int32, device=device)
+        self.count = torch.tensor([self.n_pages, 0], dtype=torch.int32, device=device)
+
+
+class KVStep(NamedTuple):
+    """What kv_plan says of a step (soniq_kv_plan)."""
+    starts: torch.Tensor       # int32 [B + 1]
+    positions: torch.Tensor    # int32 [max_tokens]
+    slots: torch.Tensor        # int64 [max_tokens]
+    lengths: torch.Tensor      # int32 [B]
+
+
+def kv_plan(pages: KVPages, lengths: torch.Tensor, targets: torch.Tensor, max_tokens: int,
+            count_out: Optional[torch.Tensor] = None, out: Optional[KVStep] = None, stream=None) -> KVStep:
+    """soniq_kv_plan: takes and gives back pages so that sequence b of lengths[b]
+    tokens (int32 [B]; negative: none yet) holds targets[b] (negative: it leaves);
+    pages.table and pages.free are updated, and pages.count, unless count_out (int32)
+    is to get the pool's new size.  max_tokens: rows of the step's buffers, at least
+    its tokens (those of sequences beyond it are not served)."""
+    B, dev = lengths.numel(), lengths.device
+    _need_here(lengths, torch.int32, (B,), "lengths")
+    _need_here(targets, torch.int32, (B,), "targets")
+    table = pages.table
+    if table.shape[0] < B:
+        raise ValueError("pages.table has fewer rows than there are sequences")
+    _need_here(table, torch.int32, None, "pages.table")
+    _need_here(pages.free, torch.int32, (pages.n_pages,), "pages.free")
+    _need_here(pages.count, torch.int32, (2,), "pages.count")
+    if count_out is None:
+        count_out = pages.count
+    elif count_out.numel() < 1:
+        raise ValueError("count_out must hold a number")
+    else:
+        _need_here(count_out, torch.int32, None, "count_out")
+    max_tokens = int(max_tokens)
+    if out is None:
+        out = KVStep(_new((B + 1,), torch.int32, dev, stream), _new((max(max_tokens, 0),), torch.int32, dev, stream),
+                     _new((max(max_tokens, 0),), torch.int64, dev, stream), _new((B,), torch.int32, dev, stream))
+    else:
+        for t, dtype, n, name in zip(out, (torch.int32, torch.int32, torch.int64, torch.int32),
+                                     (B + 1, max_tokens, max_tokens, B), KVStep._fields):
+            _need_here(t, dtype, (n,), "out." + name)
+    _check(lib().soniq_kv_plan(pages.page_size, pages.n_pages, table.data_ptr(), table.stride(0), table.shape[1],
+                               pages.free.data_ptr(), pages.count.data_ptr(), count_out.data_ptr(), lengths.data_ptr(),
+                               targets.data_ptr(), B, max_tokens, out.starts.data_ptr(), out.positions.data_ptr(),
+                               out.slots.data_ptr(), out.lengths.data_ptr(), _stream(stream)), "soniq_kv_plan")
+    return out
+
+
+class Rotary:
+    """A rotation by position (soniq_rotary) of a head's first `channels` channels.
+
+    Pair p turns by base^(-2 p / channels) radians a position; pairs are
+    neighbours (interleaved) or stand half of `channels` apart.  scaling, for
+    contexts longer than those that a model was made for: ("linear", factor), all
+    frequencies divided by factor; or ("wavelength", factor, low, high, length), only
+    those that make fewer than `low` turns over `length` positions, those of more
+    than `high` kept, and those between blended.  magnitude: a factor of what is
+    turned.  frequencies: radians a position of each pair, in place of all that."""
+
+    def __init__(self, channels: int, base: float = 10000.0, interleaved: bool = False, scaling: Optional[tuple] = None,
+                 magnitude: float = 1.0, frequencies: Optional[Sequence[float]] = None, device="cuda"):
+        if channels < 0 or channels % 2 != 0:
+            raise ValueError("channels must be even")
+        self.channels, self.interleaved, self.magnitude = int(channels), bool(interleaved), float(magnitude)
+        if frequencies is None:
+            frequencies = self._scaled([base ** (-2.0 * p / channels) for p in range(channels // 2)], scaling)
+        self.frequencies = [float(f) for f in frequencies]
+        if len(self.frequencies) != channels // 2 or not all(math.isfinite(f) for f in self.frequencies):
+            raise ValueError("frequencies must be one finite number for each pair")
+        # turns of 2^64 parts, from the doubles exactly, as signed words
+        turns = [round(Fraction(f) / _TWO_PI * 2 ** 64) % 2 ** 64 for f in self.frequencies]
+        self.turns = torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turns], dtype=torch.int64, device=device)
+        self.c = CRotary(self.channels, int(self.interleaved), self.magnitude, self.turns.data_ptr() if turns else None)
+        self.ref = ctypes.byref(self.c)
+
+    @staticmethod
+    def _scaled(freq, scaling):
+        if scaling is None:
+            return freq
+        kind, factor = scaling[0], float(scaling[1])
+        if not factor > 0.0:
+            raise ValueError("the scaling's factor must be positive")
+        if kind == "linear" and len(scaling) == 2:
+            return [f / factor for f in freq]
+        if kind == "wavelength" and len(scaling) == 5:
+            low, high, length = (float(x) for x in scaling[2:])
+            if not (0.0 <= low < high and length > 0.0):
+                raise ValueError("the scaling needs 0 <= low < high and a positive length")
+            keep = [min(max((length * f / (2.0 * math.pi) - low) / (high - low), 0.0), 1.0) for f in freq]
+            return [k * f + (1.0 - k) * f / factor for k, f in zip(keep, freq)]
+        raise ValueError("scaling must be ('linear', factor) or ('wavelength', factor, low, high, length)")
+
+
+_TWO_PI = Fraction("6.283185307179586476925286766559005768394338798750211641949889")
+
+
+def _heads(x: torch.Tensor, n: int, D: int, dtype, gain: Optional[torch.Tensor], out: Optional[torch.Tensor], name: str, stream):
+    if not x.is_cuda or x.dtype != dtype or x.dim() != 3 or x.shape[0] != n or x.shape[2] != D or \
+            (x.stride(2) != 1 and D > 1) or x.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} must be a {dtype} tensor [{n}][heads][{D}] with contiguous channels on the current CUDA device")
+    if out is None:
+        out = _new(x.shape, dtype, x.device, stream)
+    elif not out.is_cuda or out.dtype != dtype or out.shape != x.shape or (out.stride(2) != 1 and D > 1) or \
+            out.get_device() != x.get_device():
+        raise ValueError(f"{name}_out must be a tensor like {name} with contiguous channels")
+    if gain is not None:
+        _need_here(gain, torch.float32, (D,), name + "_gain")
+    sx, so = x.stride(), out.stride()
+    return out, CHeads(x.shape[1], x.data_ptr(), sx[0], sx[1], out.data_ptr(), so[0], so[1], _ptr(gain))
+
+
+def rotate_heads(rotary: Optional[Rotary], q: Optional[torch.Tensor], k: Optional[torch.Tensor],
+                 positions: Optional[torch.Tensor] = None, q_gain: Optional[torch.Tensor] = None,
+                 k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6, q_out: Optional[torch.Tensor] = None,
+                 k_out: Optional[torch.Tensor] = None, stream=None) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """soniq_rotate_heads: each head of q and k ([n][heads][D], any token and head
+    strides; either may be None) divided by its root mean square and multiplied by
+    its gain (fp32 [D]; None: neither), then turned by the token's position (int32
+    [n]; rotary None: not turned).  q_out, k_out: where to, e.g. q and k themselves."""
+    some = q if q is not None else k
+    if some is None:
+        return None, None
+    if some.dim() != 3 or some.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("q and k must be float16 or bfloat16 tensors [n][heads][D]")
+    n, _, D = some.shape
+    if rotary is not None and rotary.channels > 0:
+        if positions is None:
+            raise ValueError("positions are needed to turn by")
+        _need_here(positions, torch.int32, (n,), "positions")
+    cq = ck = None
+    if q is not None:
+        q_out, cq = _heads(q, n, D, some.dtype, q_gain, q_out, "q", stream)
+    if k is not None:
+        k_out, ck = _heads(k, n, D, some.dtype, k_gain, k_out, "k", stream)
+    _check(lib().soniq_rotate_heads(rotary.ref if rotary is not None else None, _ptr(positions), n, D,
+                                    OUT_BF16 if some.dtype == torch.bfloat16 else OUT_F16,
+                                    ctypes.byref(cq) if cq is not None else None,
+                                    ctypes.byref(ck) if ck is not None else None, float(eps), _stream(stream)),
+           "soniq_rotate_heads")
+    return (q_out if q is not None else None), (k_out if k is not None else None)
 
 
 def sync_status(stream=None) -> int:
