@@ -660,6 +660,35 @@ SONIQ_API soniq_status soniq_rotate_heads(const soniq_rotary *rotary, const int3
                                           int32_t dtype, const soniq_heads *q, const soniq_heads *k, float eps,
                                           soniq_stream_t stream);
 
+/*
+ * Attention of B packed prompts over themselves: for token t and query head h
+ * of sequence b
+ *   out[t][h] = sum_j softmax_j(scale * q[t][h] . k[j]) v[j]
+ * over the tokens j of the sequence, up to t if causal.  Query head h reads key
+ * head h / (q_heads / k_heads).
+ *   Q, K, V    device, `dtype` (SONIQ_OUT_F16 or SONIQ_OUT_BF16), n tokens; strides
+ *              in elements as for soniq_kv_write.
+ *   starts     device int32 [B + 1], not falling: sequence b is tokens starts[b] ..
+ *              starts[b + 1] - 1 (it may be empty).  One that is not within 0 .. n is
+ *              left out and reported by soniq_sync_status (SONIQ_ERR_INVALID_ARG).
+ *   out        device, contiguous [n][q_heads][Dv]; rows of no sequence are left as
+ *              they were.
+ *   D, Dv      1..256 (SONIQ_ERR_UNSUPPORTED above); n < 2^31.
+ *   scale      finite, not negative.
+ * Scores, statistics and sums are fp32; a row's weights are rounded to `dtype`
+ * for the product (fp16: by 2^-11, or 2^-33 of its largest; bf16: by 2^-8), and the
+ * output once.  What a row does not see does not matter, whatever it holds.
+ * Pointers need the alignment of their elements.  The tensor cores are used where
+ * D and Dv are multiples of 8 and rows are on 16 bytes (pointers, and token and
+ * head strides); other rows take a slow kernel.
+ */
+SONIQ_API soniq_status soniq_prompt_attend(const void *Q, int64_t q_token_stride, int64_t q_head_stride, const void *K,
+                                           int64_t k_token_stride, int64_t k_head_stride, const void *V,
+                                           int64_t v_token_stride, int64_t v_head_stride, const int32_t *starts,
+                                           int32_t B, int64_t n, int32_t q_heads, int32_t k_heads, int32_t D,
+                                           int32_t Dv, int32_t dtype, int32_t causal, float scale, void *out,
+                                           soniq_stream_t stream);
+
 /* Waits for `stream`, then returns SONIQ_ERR_TIMEOUT if any kernel of this
  * library on the current device recorded a timed-out wait since the last
  * call (and clears that record), SONIQ_ERR_INVALID_ARG if none did but a

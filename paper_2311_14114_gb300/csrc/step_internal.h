@@ -46,4 +46,21 @@ struct RotateArgs {
 };
 cudaError_t launch_rotate_heads(const RotateArgs& a, bool bf16, cudaStream_t st);
 
+struct PromptSide {
+    const uint16_t* p;
+    int64_t token, head;           // strides in elements
+};
+struct PromptArgs {
+    PromptSide q, k, v;
+    const int32_t* starts;
+    int32_t B, n;
+    int32_t k_heads, group;        // group: query heads per key head
+    int32_t D, Dv;
+    int32_t causal;
+    float scale;
+    uint16_t* out;
+    unsigned* err;
+};
+cudaError_t launch_prompt_rows(const PromptArgs& a, bool bf16, cudaStream_t st);
+
 }  // namespace soniq

@@ -39,7 +39,8 @@ EXPORTED = ["soniq_abi_version", "soniq_status_string", "soniq_group_codes",
             "soniq_quantize_act_oneshot", "soniq_mp_gemm", "soniq_mp_gemm_path", "soniq_mp_gemm_kernel",
             "soniq_mp_gemm_scratch_bytes", "soniq_mp_conv2d", "soniq_mp_conv2d_scratch_bytes", "soniq_sync_status",
             "soniq_test_drop_barrier_arrival", "soniq_kv_row_bytes", "soniq_kv_validate", "soniq_kv_write",
-            "soniq_kv_read", "soniq_kv_attend", "soniq_kv_attend_scratch_bytes", "soniq_kv_plan", "soniq_rotate_heads"]
+            "soniq_kv_read", "soniq_kv_attend", "soniq_kv_attend_scratch_bytes", "soniq_kv_plan", "soniq_rotate_heads",
+            "soniq_prompt_attend"]
 
 _SCALE = {"tensor": SCALE_PER_TENSOR, "row": SCALE_PER_ROW, "calibrated": SCALE_CALIBRATED}
 
@@ -155,6 +156,9 @@ def lib() -> ctypes.CDLL:
         L.soniq_kv_plan.restype = i32
         L.soniq_rotate_heads.argtypes = [P, P, i64, i32, i32, P, P, ctypes.c_float, P]
         L.soniq_rotate_heads.restype = i32
+        L.soniq_prompt_attend.argtypes = [P, i64, i64, P, i64, i64, P, i64, i64, P, i32, i64, i32, i32, i32, i32, i32, i32,
+                                          ctypes.c_float, P, P]
+        L.soniq_prompt_attend.restype = i32
         _lib = L
     return _lib
 
@@ -752,6 +756,38 @@ def rotate_heads(rotary: Optional[Rotary], q: Optional[torch.Tensor], k: Optiona
                                     ctypes.byref(ck) if ck is not None else None, float(eps), _stream(stream)),
            "soniq_rotate_heads")
     return (q_out if q is not None else None), (k_out if k is not None else None)
+
+
+def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, causal: bool = True,
+                  scale: Optional[float] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """soniq_prompt_attend: attention of packed prompts over themselves.  q [n][q_heads][D],
+    k [n][heads][D], v [n][heads][Dv] (any token and head strides); sequence b is
+    tokens starts[b] .. starts[b + 1] - 1 (int32 [B + 1]).  scale: 1 / sqrt(D) if left
+    out.  Returns out [n][q_heads][Dv], whose rows of no sequence are left as they were."""
+    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3 or q.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("q, k and v must be float16 or bfloat16 tensors [n][heads][channels]")
+    (n, Hq, D), (_, Hk, Dv) = q.shape, v.shape
+    here = torch.cuda.current_device() if q.is_cuda else -1
+    for t, shape, name in ((q, (n, Hq, D), "q"), (k, (n, Hk, D), "k"), (v, (n, Hk, Dv), "v")):
+        if not t.is_cuda or t.dtype != q.dtype or tuple(t.shape) != shape or (t.stride(2) != 1 and shape[2] > 1) or \
+                t.get_device() != here:
+            raise ValueError(f"{name} must be a {q.dtype} tensor {list(shape)} with contiguous channels on the current CUDA device")
+    if Hk == 0 or Hq % Hk != 0:
+        raise ValueError("q's heads must be a multiple of k's")
+    if starts.dim() != 1 or starts.numel() < 1:
+        raise ValueError("starts must be [B + 1]")
+    _need_here(starts, torch.int32, None, "starts")
+    if out is None:
+        out = _new((n, Hq, Dv), q.dtype, q.device, stream)
+    else:
+        _need_here(out, q.dtype, (n, Hq, Dv), "out")
+    sq, sk, sv = q.stride(), k.stride(), v.stride()
+    _check(lib().soniq_prompt_attend(q.data_ptr(), sq[0], sq[1], k.data_ptr(), sk[0], sk[1], v.data_ptr(), sv[0], sv[1],
+                                     starts.data_ptr(), starts.numel() - 1, n, Hq, Hk, D, Dv,
+                                     OUT_BF16 if q.dtype == torch.bfloat16 else OUT_F16, int(bool(causal)),
+                                     1.0 / math.sqrt(D) if scale is None else float(scale), out.data_ptr(), _stream(stream)),
+           "soniq_prompt_attend")
+    return out
 
 
 def sync_status(stream=None) -> int:

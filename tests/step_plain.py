@@ -73,3 +73,43 @@ def rotate_tolerance(ref, mag, dtype):
     turn, 2^-23.3 radians, and the functions' own 2^-24): below 2^-20 of the summed
     magnitudes."""
     return HALF_STEP[dtype] * np.abs(ref) + (1 + HALF_STEP[dtype]) * 2.0 ** -20 * mag + LEAST[dtype]
+
+
+def attend(q, k, v, starts, causal, scale):
+    """q [n][Hq][D], k, v [n][Hk][..] torch fp64.  Returns outputs and, for the
+    tolerance, sum of p |v|, the largest summed magnitudes of a score, and of a row the
+    softmax sum and the largest |v| that it sees."""
+    n, Hq, _ = q.shape
+    G = Hq // k.shape[1]
+    o = torch.zeros(n, Hq, v.shape[2], dtype=torch.float64, device=q.device)
+    mag, dscore = torch.zeros_like(o), torch.zeros(n, Hq, 1, dtype=torch.float64, device=q.device)
+    total, v_max = torch.ones_like(dscore), torch.zeros_like(dscore)
+    for s, e in zip(starts[:-1], starts[1:]):
+        if e <= s:
+            continue
+        hide = torch.ones(e - s, e - s, dtype=torch.bool, device=q.device).triu(1) if causal else None
+        for h in range(k.shape[1]):
+            hq = slice(h * G, (h + 1) * G)
+            x, y, z = q[s:e, hq].transpose(0, 1), k[s:e, h], v[s:e, h]
+            sc, big = x @ y.T * scale, x.abs() @ y.abs().T * scale
+            if causal:
+                sc, big = sc.masked_fill(hide, -math.inf), big.masked_fill(hide, 0)
+            p = torch.exp(sc - sc.amax(-1, keepdim=True))
+            l = p.sum(-1, keepdim=True)
+            o[s:e, hq] = (p / l @ z).transpose(0, 1)
+            mag[s:e, hq] = (p / l @ z.abs()).transpose(0, 1)
+            dscore[s:e, hq] = big.amax(-1, keepdim=True).transpose(0, 1)
+            total[s:e, hq] = l.transpose(0, 1)
+            top = z.abs().amax(-1, keepdim=True)
+            v_max[s:e, hq] = (torch.cummax(top, 0).values if causal else top.amax().expand(e - s, 1))[:, None]
+    return o, mag, dscore, total, v_max
+
+
+def attend_tolerance(ref, mag, dscore, total, v_max, n, dtype):
+    """|error| allowed: weights are rounded to the type (half a step each; fp16: or 2^-33 of
+    the row's largest weight where they are subnormal, n of them at most); scores carry
+    2^-21 of the summed magnitudes of their products (sums of at most 256 in fp32), which
+    the exponential doubles over row and sum; exponentials and sums 2^-19; one rounding."""
+    half = HALF_STEP[dtype]
+    sub = 2.0 ** -33 * n * v_max / total if dtype == torch.float16 else 0.0
+    return (1 + half) * (mag * (half + 2.0 ** -20 * dscore + 2.0 ** -19) + sub) + half * ref.abs() + LEAST[dtype]

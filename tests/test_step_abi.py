@@ -96,3 +96,30 @@ def test_the_binding_refuses(sq):
         with pytest.raises(ValueError):
             call()
     assert sq.rotate_heads(None, None, None) == (None, None)
+
+
+def attend(sq, **kw):
+    a = dict(Q=FAKE, qt=512, qh=64, K=FAKE, kt=128, kh=64, V=FAKE, vt=128, vh=64, starts=FAKE, B=1, n=4, q_heads=8, k_heads=2,
+             D=64, Dv=64, dtype=0, causal=1, scale=0.1, out=FAKE)
+    assert set(kw) <= set(a)
+    a.update(kw)
+    return sq.lib().soniq_prompt_attend(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(B=0), OK), (dict(n=0), OK), (dict(B=-1), INVALID), (dict(n=-1), INVALID), (dict(n=1 << 31), UNSUPPORTED),
+    (dict(q_heads=7), INVALID), (dict(q_heads=0), INVALID), (dict(k_heads=0), INVALID), (dict(q_heads=4098), UNSUPPORTED),
+    (dict(D=0), INVALID), (dict(Dv=0), INVALID), (dict(D=257), UNSUPPORTED), (dict(Dv=264), UNSUPPORTED), (dict(dtype=3), INVALID),
+    (dict(scale=math.inf), INVALID), (dict(scale=math.nan), INVALID), (dict(scale=-0.1), INVALID), (dict(Q=None), INVALID),
+    (dict(K=None), INVALID), (dict(V=None), INVALID), (dict(starts=None), INVALID), (dict(out=None), INVALID),
+    (dict(Q=FAKE + 1), ALIGNMENT), (dict(K=FAKE + 1), ALIGNMENT), (dict(V=FAKE + 1), ALIGNMENT), (dict(out=FAKE + 1), ALIGNMENT),
+    (dict(starts=FAKE + 2), ALIGNMENT)])
+def test_bad_prompts(sq, kw, want):
+    assert attend(sq, **kw) == want
+
+
+def test_the_binding_refuses_prompts(sq):
+    x, st = torch.zeros(4, 2, 16, dtype=torch.float16), torch.zeros(2, dtype=torch.int32)
+    for args in ((x, x, x, st), (x.float(), x, x, st), (x[0], x, x, st), (x, x[:3], x, st), (x, x[:, :0], x[:, :0], st)):
+        with pytest.raises(ValueError):
+            sq.prompt_attend(*args)
