@@ -673,8 +673,13 @@ SONIQ_API soniq_status soniq_rotate_heads(const soniq_rotary *rotary, const int3
  *              left out and reported by soniq_sync_status (SONIQ_ERR_INVALID_ARG).
  *   out        device, contiguous [n][q_heads][Dv]; rows of no sequence are left as
  *              they were.
- *   D, Dv      1..256 (SONIQ_ERR_UNSUPPORTED above); n < 2^31.
+ *   D, Dv      1..256, at most 4096 query heads and 2^30 tokens (SONIQ_ERR_UNSUPPORTED above).
  *   scale      finite, not negative.
+ *   scratch    device, 16-byte aligned, of soniq_prompt_attend_scratch_bytes()
+ *              (SONIQ_ERR_INVALID_ARG otherwise), zero before the first use; every
+ *              completed call leaves it zero (zero it again after a
+ *              SONIQ_ERR_TIMEOUT).  Calls that may overlap on the GPU must use
+ *              different scratch.
  * Scores, statistics and sums are fp32; a row's weights are rounded to `dtype`
  * for the product (fp16: by 2^-11, or 2^-33 of its largest; bf16: by 2^-8), and the
  * output once.  What a row does not see does not matter, whatever it holds.
@@ -687,7 +692,10 @@ SONIQ_API soniq_status soniq_prompt_attend(const void *Q, int64_t q_token_stride
                                            int64_t v_token_stride, int64_t v_head_stride, const int32_t *starts,
                                            int32_t B, int64_t n, int32_t q_heads, int32_t k_heads, int32_t D,
                                            int32_t Dv, int32_t dtype, int32_t causal, float scale, void *out,
-                                           soniq_stream_t stream);
+                                           void *scratch, size_t scratch_bytes, soniq_stream_t stream);
+
+/* Scratch bytes of soniq_prompt_attend, for any arguments.  Host only. */
+SONIQ_API int64_t soniq_prompt_attend_scratch_bytes(void);
 
 /* Waits for `stream`, then returns SONIQ_ERR_TIMEOUT if any kernel of this
  * library on the current device recorded a timed-out wait since the last
@@ -700,6 +708,7 @@ SONIQ_API soniq_status soniq_sync_status(soniq_stream_t stream);
 
 /* Test hook, not for production use.  When armed (armed != 0), the next
  * soniq_kv_attend leaves out one copy of cached rows, or the next
+ * soniq_prompt_attend on the tensor cores one of keys and values, or the next
  * launch of a per-tensor quantize kernel with a grid barrier (one-pass or
  * streamed), from soniq_quantize_act or soniq_quantize_act_oneshot, has its
  * first CTA skip its grid-barrier

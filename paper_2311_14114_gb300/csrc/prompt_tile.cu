@@ -1,0 +1,569 @@
+// Attention of packed prompts on tcgen05:
+//
+//   S = Q K^T, P = softmax(scale S), O = P V, accumulators in TMEM.
+//
+// A tile is 128 rows: the query heads of one key head (128 at most) at as many
+// neighbouring tokens as fit, so a key block serves all of them.  A CTA works at
+// one unit at a time, TILES neighbouring tiles of one prompt and key head, over
+// blocks of 64 tokens.  Its warps:
+//   warp 0 (and 2)   issue the MMAs, each for one tile;
+//   warp 1           copies queries, keys and values by TMA;
+//   warp 3           finds the next unit;
+//   warps 4-7, 8-11  softmax of a tile, a thread to a row.
+// Scores have two buffers a tile: the next block's are there when this one's
+// softmax ends, and weights go over the scores that they come from.  Units are
+// handed out by a counter, the longest of a prompt first, and one unit's scores
+// begin while the one before leaves its outputs.
+//
+// Numerics.  Scores are fp32.  A row's weights are 2^(score - m), held at most
+// 2^15: m is raised, and O with it, only when a weight would pass that, to where
+// the largest is 2^8.  (So fp16 weights have their full 11 bits down to 2^-22 of
+// the row's largest.)  Weights are rounded to the type for the product.
+//
+// What no rounding of that kind holds ends in an output that is not finite: NaN
+// and infinities in the values of later tokens, which a row does not see (0 times
+// them is not 0), sums that pass fp32, scores so large that their products with
+// the exponent's factor are off.  Rows with such an output are done again, from
+// the definition, by prompt_row.  So the blocks need no look at what is hidden;
+// only what stands behind a prompt, where a buffer's padding may hold anything, is
+// cleared in its last block.
+#include "kv_flights.h"
+#include "prompt_rows.cuh"
+#include "soniq_device.cuh"
+#include "tile_ops.cuh"
+
+namespace soniq {
+
+namespace {
+
+constexpr int kTok = 64;                 // tokens of a block
+constexpr int kAtom = kTok * 128;        // bytes of a 64-channel column group of a key or value block
+constexpr int kQAtom = 128 * 128;        // ... of a query tile
+constexpr int kOCol = 2 * kTok;          // O's first column in a tile's TMEM columns, behind two buffers of scores
+constexpr int kMaxStages = 8;
+constexpr float kMost = 15.0f, kBegin = 8.0f;      // log2 of the largest weight, and of a row's largest when m is raised
+
+struct PromptPlan {
+    int row_heads;           // query heads of a tile
+    int tile_tokens;
+    int head_parts;          // tiles that share a key head's query heads
+    int k_atoms, v_atoms;
+    int o_cols;              // Dv rounded up to whole MMA columns
+    int slot_cols, tmem_cols;
+    int stages, stage_bytes;
+    int ring_off, misc_off, smem;
+};
+
+struct PromptMaps {
+    CUtensorMap q, k, v;
+};
+
+struct Unit {
+    int start, len;          // the prompt
+    int token;               // first token of the unit, within it; negative: there is no unit
+    int kv_head, part;
+    int blocks0, blocks1;    // of each tile; 0: the tile is empty
+    __device__ __forceinline__ int blocks_of(int s) const { return s ? blocks1 : blocks0; }
+    __device__ __forceinline__ int blocks() const { return max(blocks0, blocks1); }
+};
+
+struct Bars {                // offsets in 8-byte barriers; the first 17 are those of copies (Flights)
+    static constexpr int k_full = 0, v_full = kMaxStages, q_full = 2 * kMaxStages, kv_free = q_full + 1,
+                         q_free = kv_free + kMaxStages, s_full = q_free + 1, p_full = s_full + 4, pv_done = p_full + 4,
+                         o_full = pv_done + 2, o_free = o_full + 2, unit_full = o_free + 2, unit_free = unit_full + 2,
+                         drain = unit_free + 2, count = drain + 1;      // s_full, p_full: [tile][buffer]
+};
+constexpr int kMisc = 1024;
+static_assert(8 * Bars::count <= 512, "barriers");
+
+__device__ __forceinline__ void tmem_ld64(uint32_t at, uint32_t (&r)[64]) {
+#define SONIQ_R4(i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3])
+#define SONIQ_R16(i) SONIQ_R4(i), SONIQ_R4(i + 4), SONIQ_R4(i + 8), SONIQ_R4(i + 12)
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+        "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,"
+        "%62,%63}, [%64];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : SONIQ_R16(0), SONIQ_R16(16), SONIQ_R16(32), SONIQ_R16(48)
+        : "r"(at)
+        : "memory");
+#undef SONIQ_R16
+#undef SONIQ_R4
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+template <bool BF16, int TILES>
+__global__ void __launch_bounds__(128 + 128 * TILES, 1)
+    prompt_tile_kernel(const PromptArgs a, const PromptPlan pl, const __grid_constant__ PromptMaps maps, unsigned* counters, const int drop) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t smem0 = tc::smem_u32(smem), ring = smem0 + pl.ring_off, bars = smem0 + pl.misc_off;
+    uint8_t* misc = smem + pl.misc_off;
+    Unit* units = reinterpret_cast<Unit*>(misc + 512);                // [2]
+    uint32_t* words = reinterpret_cast<uint32_t*>(misc + 640);
+    const uint32_t abort_flag = tc::smem_u32(words);
+    uint32_t* tmem_at = words + 1;
+    auto bar = [&](int i) { return bars + 8u * i; };
+    const int unit_tokens = TILES * pl.tile_tokens;
+
+    if (tid == 0) {
+        auto init = [&](int first, int n, int arrivals) {
+            for (int i = 0; i < n; ++i) tc::mbar_init(bar(first + i), arrivals);
+        };
+        init(Bars::k_full, 2 * kMaxStages + 1, 1);
+        init(Bars::kv_free, kMaxStages + 1, TILES);      // and q_free
+        init(Bars::s_full, 4, 1);
+        init(Bars::p_full, 4, 4);
+        init(Bars::pv_done, 4, 1);                       // and o_full
+        init(Bars::o_free, 2, 4);
+        init(Bars::unit_full, 2, 1);
+        init(Bars::unit_free, 2, 1 + 5 * TILES);
+        init(Bars::drain, 1, TILES);
+        words[0] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(tmem_at)), "r"(pl.tmem_cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tmem = *tmem_at;
+    auto wait = [&](int i, uint32_t parity) { return wait_warp(bar(i), parity & 1u, abort_flag, a.err); };
+
+    // The next unit, as the warps of other roles read it; they release it (`done`) when they have gone on.
+    auto next_unit = [&](uint32_t n, Unit* u) {
+        if (!wait(Bars::unit_full + (n & 1), n >> 1)) return false;
+        *u = units[n & 1];
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(bar(Bars::unit_free + (n & 1)));
+        return u->token >= 0;
+    };
+
+    Flights flights;       // of the copying warp
+    if (warp == 3) {
+        // ---- units: numbered prompt by prompt, later tokens first, key heads side by side ----
+        const int per_unit = a.k_heads * pl.head_parts;
+        int64_t base = 0;              // units of the prompts before b0
+        int b0 = 0;
+        unsigned id = blockIdx.x;
+        bool ok = true;
+        for (uint32_t n = 0;; ++n) {
+            // the prompt that holds it: 32 at a time, from the last one on
+            int found = -1, s = 0, len = 0;
+            int64_t before = 0;
+            while (b0 < a.B) {
+                const int b = b0 + lane;
+                int s_b = 0, e_b = 0;
+                if (b < a.B && !(blockIdx.x == 0 ? prompt_span(a, b, &s_b, &e_b)
+                                                 : (s_b = a.starts[b], e_b = a.starts[b + 1], s_b >= 0 && s_b <= e_b && e_b <= a.n)))
+                    s_b = e_b = 0;
+                const int64_t mine = (int64_t)((e_b - s_b + unit_tokens - 1) / unit_tokens) * per_unit;
+                int64_t upto = mine;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int64_t x = __shfl_up_sync(0xffffffffu, upto, d);
+                    if (lane >= d) upto += x;
+                }
+                const unsigned in = __ballot_sync(0xffffffffu, (int64_t)id < base + upto);
+                if (in != 0) {
+                    const int at = __ffs(in) - 1;
+                    found = b0 + at;
+                    s = __shfl_sync(0xffffffffu, s_b, at);
+                    len = __shfl_sync(0xffffffffu, e_b - s_b, at);
+                    before = base + __shfl_sync(0xffffffffu, upto - mine, at);
+                    break;
+                }
+                base += __shfl_sync(0xffffffffu, upto, 31);
+                b0 += 32;
+            }
+            ok = wait(Bars::unit_free + (n & 1), (n >> 1) ^ 1u);
+            Unit u{};
+            u.token = -1;
+            if (found >= 0) {
+                const int r = (int)(id - before), of = (len + unit_tokens - 1) / unit_tokens;
+                const int head = r % per_unit;
+                u.start = s;
+                u.len = len;
+                u.token = (of - 1 - r / per_unit) * unit_tokens;
+                u.kv_head = head / pl.head_parts;
+                u.part = head % pl.head_parts;
+                auto blocks = [&](int first) {
+                    const int end = a.causal ? min(first + pl.tile_tokens, len) : len;
+                    return first < len ? (end + kTok - 1) / kTok : 0;
+                };
+                u.blocks0 = blocks(u.token);
+                if (TILES == 2) u.blocks1 = blocks(u.token + pl.tile_tokens);
+            }
+            if (ok && lane == 0) {
+                units[n & 1] = u;
+                tc::mbar_arrive(bar(Bars::unit_full + (n & 1)));
+            }
+            __syncwarp();
+            if (!ok || found < 0) break;
+            if (lane == 0) id = gridDim.x + atomicAdd(counters, 1u);
+            id = __shfl_sync(0xffffffffu, id, 0);
+        }
+        // the last CTA to have asked leaves the counters as it found them
+        if (ok && lane == 0) {
+            __threadfence();
+            if (atomicAdd(counters + 1, 1u) == gridDim.x - 1) {
+                counters[0] = 0;
+                counters[1] = 0;
+            }
+        }
+    } else if (warp == 1) {
+        // ---- copies ----
+        Ring kv;
+        Unit u;
+        bool ok = true;
+        for (uint32_t n = 0; ok && next_unit(n, &u); ++n) {
+            const int blocks = u.blocks();
+            const int head = (u.kv_head * a.group + u.part * pl.row_heads);
+            ok = wait(Bars::q_free, n ^ 1u);
+            if (!ok) break;
+            flights.issue(Bars::q_full, n);
+            const int box_bytes = pl.row_heads * pl.tile_tokens * 128, tiles = u.blocks_of(TILES - 1) > 0 ? TILES : 1;
+            if (tc::elect_one()) tc::mbar_arrive_expect_tx(bar(Bars::q_full), tiles * pl.k_atoms * box_bytes);
+            for (int i = 0; i < tiles * pl.k_atoms; ++i) {
+                const int tile = i / pl.k_atoms, atom = i % pl.k_atoms;
+                if (tc::elect_one())
+                    tma_load_3d(smem0 + i * kQAtom, &maps.q, 64 * atom, a.q.head ? head : 0, u.start + u.token + tile * pl.tile_tokens, bar(Bars::q_full));
+            }
+#pragma unroll 1
+            for (int j = 0; j < blocks; ++j, kv.step(pl.stages)) {
+                ok = wait(Bars::kv_free + kv.i, kv.phase ^ 1u);
+                if (!ok) break;
+                const uint32_t at = ring + kv.i * pl.stage_bytes;
+                const int token = u.start + j * kTok;
+                if (drop && blockIdx.x == 0 && n == 0 && j == 0) continue;
+                flights.issue(Bars::k_full + kv.i, kv.phase);
+                flights.issue(Bars::v_full + kv.i, kv.phase);
+                if (tc::elect_one()) {
+                    tc::mbar_arrive_expect_tx(bar(Bars::k_full + kv.i), pl.k_atoms * kAtom);
+                    for (int i = 0; i < pl.k_atoms; ++i)
+                        tma_load_3d(at + i * kAtom, &maps.k, 64 * i, a.k.head ? u.kv_head : 0, token, bar(Bars::k_full + kv.i));
+                    tc::mbar_arrive_expect_tx(bar(Bars::v_full + kv.i), pl.v_atoms * kAtom);
+                    for (int i = 0; i < pl.v_atoms; ++i)
+                        tma_load_3d(at + (pl.k_atoms + i) * kAtom, &maps.v, 64 * i, a.v.head ? u.kv_head : 0, token, bar(Bars::v_full + kv.i));
+                }
+                __syncwarp();
+            }
+        }
+    } else if (warp == 0 || (TILES == 2 && warp == 2)) {
+        // ---- MMAs of tile s ----
+        const int s = warp >> 1;
+        constexpr uint32_t fmt = (1u << 4) | (BF16 ? (1u << 7) | (1u << 10) : 0u) | ((128u >> 4) << 24);
+        const uint32_t id_s = fmt | ((kTok >> 3) << 17), id_o = fmt | (1u << 16) | ((uint32_t)(pl.o_cols >> 3) << 17);
+        const uint32_t t_s = tmem + s * pl.slot_cols;
+        const uint64_t q_tile = tc::sw128_desc(smem0 + s * pl.k_atoms * kQAtom);
+        const int steps = (a.D + 15) / 16;      // of 16 channels
+        const bool leader = tc::elect_one();
+        Ring now, next;                          // the block whose outputs, and whose scores, come next
+        uint32_t done = 0, tiles = 0;            // blocks and tiles so far
+        Unit u;
+        bool ok = true;
+        for (uint32_t n = 0; ok && next_unit(n, &u); ++n) {
+            const int blocks = u.blocks(), mine = u.blocks_of(s);
+            ok = wait(Bars::q_full, n);
+            if (!ok) break;
+            tc::tc_fence_after();
+            next = now;
+#pragma unroll 1
+            for (int i = -2; i < mine; ++i) {
+                const uint32_t buf = (done + (i & 1)) & 1u;
+                if (i >= 0) {
+                    ok = wait(Bars::p_full + 2 * s + buf, (done + i) >> 1) && wait(Bars::v_full + now.i, now.phase) &&
+                         (i > 0 || wait(Bars::o_free + s, tiles ^ 1u));
+                    if (!ok) break;
+                    tc::tc_fence_after();
+                    const uint32_t values = ring + now.i * pl.stage_bytes + pl.k_atoms * kAtom;
+                    if ((i + 1) * kTok > u.len) {
+                        // Tokens behind the prompt, whose weights are 0, may hold anything (a buffer's padding): 0 times
+                        // that is to be 0.  (The other tile's warp writes the same zeros.)
+                        const int first = u.len - i * kTok, rows = kTok - first;
+                        for (int k = lane; k < 8 * rows * pl.v_atoms; k += 32) {
+                            const uint32_t at = values + (k / (8 * rows)) * kAtom + 128 * first + 16 * (k % (8 * rows));
+                            sts128f(at, 0.0f, 0.0f, 0.0f, 0.0f);
+                        }
+                        tc::fence_proxy_async_shared();
+                        __syncwarp();
+                    }
+                    const uint64_t v = value_desc(values, kAtom);
+                    const uint32_t p = t_s + buf * kTok;
+                    if (leader) {
+#pragma unroll
+                        for (int k = 0; k < kTok / 16; ++k) mma_ts(t_s + kOCol, p + 8 * k, v + k * (2048 >> 4), id_o, i != 0 || k != 0);
+                        tc::mma_commit(bar(Bars::kv_free + now.i));
+                        tc::mma_commit(bar(Bars::pv_done + s));
+                        if (i == mine - 1) tc::mma_commit(bar(Bars::o_full + s));
+                    }
+                    __syncwarp();
+                    now.step(pl.stages);
+                }
+                if (i + 2 < mine) {
+                    ok = wait(Bars::k_full + next.i, next.phase);
+                    if (!ok) break;
+                    tc::tc_fence_after();
+                    uint64_t q = q_tile, k = tc::sw128_desc(ring + next.i * pl.stage_bytes);
+                    const uint32_t d = t_s + buf * kTok;
+                    // column groups of four steps
+#pragma unroll 1
+                    for (int c = 0; c < steps; c += 4) {
+                        if (leader) {
+                            mma_ss(d, q, k, id_s, c != 0);
+                            if (c + 1 < steps) mma_ss(d, q + 2, k + 2, id_s, 1);
+                            if (c + 2 < steps) mma_ss(d, q + 4, k + 4, id_s, 1);
+                            if (c + 3 < steps) mma_ss(d, q + 6, k + 6, id_s, 1);
+                        }
+                        q += kQAtom >> 4;
+                        k += kAtom >> 4;
+                    }
+                    if (leader) {
+                        tc::mma_commit(bar(Bars::s_full + 2 * s + buf));
+                        if (i + 3 == mine) tc::mma_commit(bar(Bars::q_free));
+                    }
+                    __syncwarp();
+                    next.step(pl.stages);
+                }
+            }
+            if (!ok) break;
+            if (mine == 0 && lane == 0) tc::mbar_arrive(bar(Bars::q_free));
+            done += mine;
+            tiles += mine > 0;
+            // blocks that only the other tile sees: each is released when it is there, so that no release runs ahead
+#pragma unroll 1
+            for (int i = mine; i < blocks; ++i, now.step(pl.stages)) {
+                ok = wait(Bars::k_full + now.i, now.phase) && wait(Bars::v_full + now.i, now.phase);
+                if (!ok) break;
+                if (lane == 0) tc::mbar_arrive(bar(Bars::kv_free + now.i));
+                __syncwarp();
+            }
+        }
+    } else if (warp >= 4) {
+        // ---- softmax of tile s ----
+        const int s = (warp >> 2) - 1, quad = warp & 3, row = quad * 32 + lane;
+        const uint32_t t_s = tmem + s * pl.slot_cols + ((uint32_t)(quad * 32) << 16);
+        const int row_token = row / pl.row_heads, row_head = row - row_token * pl.row_heads;
+        const int heads = a.k_heads * a.group;
+        // (never 0: a score that is masked, minus infinity, has no weight at any scale)
+        const float factor = fmaxf(a.scale * kLog2e, 1.4e-45f);
+        uint32_t done = 0, tiles = 0;
+        Unit u;
+        bool ok = true;
+        for (uint32_t n = 0; ok && next_unit(n, &u); ++n) {
+            const int mine = u.blocks_of(s);
+            if (mine == 0) continue;
+            const int token = u.token + s * pl.tile_tokens + row_token, head = u.part * pl.row_heads + row_head;
+            const bool live = row_token < pl.tile_tokens && token < u.len && head < a.group;
+            // keys that the row sees, and those that all of the warp's do (rows of no token do not matter)
+            const int end = live && a.causal ? token + 1 : u.len;
+            const int sure = __reduce_min_sync(0xffffffffu, end);
+            float m = kUnset, l = 0.0f;
+#pragma unroll 1
+            for (int i = 0; i < mine; ++i, ++done) {
+                const uint32_t buf = done & 1u, t_b = t_s + buf * kTok;
+                ok = wait(Bars::s_full + 2 * s + buf, done >> 1);
+                if (!ok) break;
+                tc::tc_fence_after();
+                uint32_t raw[64];
+                tmem_ld64(t_b, raw);
+                float2 x[kTok / 2];
+#pragma unroll
+                for (int k = 0; k < kTok / 2; ++k) x[k] = make_float2(__uint_as_float(raw[2 * k]), __uint_as_float(raw[2 * k + 1]));
+                const int p0 = i * kTok;
+                if (p0 + kTok > sure) {
+                    const int upto = end - p0;
+#pragma unroll
+                    for (int k = 0; k < kTok / 2; ++k) {
+                        if (2 * k >= upto) x[k].x = -INFINITY;
+                        if (2 * k + 1 >= upto) x[k].y = -INFINITY;
+                    }
+                }
+                float tops[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) tops[k] = fmaxf(x[k].x, x[k].y);
+#pragma unroll
+                for (int k = 8; k < kTok / 2; ++k) tops[k & 7] = fmaxf(fmaxf(tops[k & 7], x[k].x), x[k].y);
+                const float best = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
+                const bool over = fmaf(best, factor, -m) > kMost;
+                if (__any_sync(0xffffffffu, over)) {
+                    const float to = over ? best * factor - kBegin : m, by = ex2(m - to);
+                    m = to;
+                    l *= by;
+                    // scores whose products are off by their rounding: the row is done again
+                    if (over && !(fabsf(fmaf(best, factor, -m) - kBegin) <= 4.0f)) l = NAN;
+                    if (i != 0) {
+                        // the MMAs that wrote O have to be complete
+                        ok = wait(Bars::pv_done + s, done ^ 1u);
+                        if (!ok) break;
+                        tc::tc_fence_after();
+#pragma unroll 1
+                        for (int c = 0; c < pl.o_cols; c += 16) {
+                            uint32_t v[16];
+                            tc::tmem_ld16(t_s + kOCol + c, v);
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * by);
+                            tmem_st16v(t_s + kOCol + c, v);
+                        }
+                    }
+                }
+                float2 sums[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        float2 y = fma2(x[16 * h + k], make_float2(factor, factor), make_float2(-m, -m));
+                        y = make_float2(ex2(y.x), ex2(y.y));
+                        sums[k & 1] = fma2(y, make_float2(1.0f, 1.0f), sums[k & 1]);
+                        w[k] = BF16 ? pack_bf16(y.x, y.y) : pack2(y.x, y.y);
+                    }
+                    tmem_st16v(t_b + 16 * h, w);
+                }
+                l += sums[0].x + sums[0].y + sums[1].x + sums[1].y;
+                tc::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(bar(Bars::p_full + 2 * s + buf));
+            }
+            if (!ok) break;
+            // ---- outputs ----
+            ok = wait(Bars::o_full + s, tiles);
+            if (!ok) break;
+            tc::tc_fence_after();
+            const float inv = 1.0f / l;
+            float odd = 0.0f;              // NaN once an output is not finite
+            const int64_t out_row = (int64_t)(u.start + token) * heads + u.kv_head * a.group + head;
+            uint16_t* out = a.out + out_row * a.Dv;
+            constexpr float top = BF16 ? 3.3895313892515355e38f : 65504.0f;
+#pragma unroll 1
+            for (int c = 0; c < pl.o_cols; c += 16) {
+                uint32_t v[16], w[8];
+                tc::tmem_ld16(t_s + kOCol + c, v);
+#pragma unroll
+                for (int k = 0; k < 16; k += 2) {
+                    const float y0 = __uint_as_float(v[k]) * inv, y1 = __uint_as_float(v[k + 1]) * inv;
+                    odd = fmaf(y0, 0.0f, fmaf(y1, 0.0f, odd));
+                    // (an average of values of the type is not beyond it, though rounded weights may say so)
+                    const float z0 = fminf(fmaxf(y0, -top), top), z1 = fminf(fmaxf(y1, -top), top);
+                    w[k / 2] = BF16 ? pack_bf16(z0, z1) : pack2(z0, z1);
+                }
+                if (live) {
+                    *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
+                    if (c + 8 < a.Dv) *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                }
+            }
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(bar(Bars::o_free + s));
+            ++tiles;
+            unsigned again = __ballot_sync(0xffffffffu, live && odd != 0.0f);
+            while (again != 0) {
+                const int from = __ffs(again) - 1;
+                again &= again - 1;
+                const int t = __shfl_sync(0xffffffffu, u.start + token, from), h = __shfl_sync(0xffffffffu, u.kv_head * a.group + head, from);
+                const int e = __shfl_sync(0xffffffffu, end, from);
+                prompt_row<BF16, true>(a, h, t, u.start, u.start + e);
+                __syncwarp();
+            }
+        }
+    }
+    __syncthreads();
+    if (tc::abort_raised(abort_flag)) {
+        // a copy did not come: let those on their way land, and the MMAs end, within the same bound
+        const long long t0 = tc::globaltimer();
+        if (warp == 1) {
+            flights.land([&](int i, uint32_t parity) { return tc::mbar_try_wait(bar(i), parity); },
+                         [&]() { return tc::globaltimer() - t0 < kWaitNs; });
+        } else if (warp == 0 || (TILES == 2 && warp == 2)) {
+            if (tc::elect_one()) tc::mma_commit(bar(Bars::drain));
+            while (!tc::mbar_try_wait(bar(Bars::drain), 0) && tc::globaltimer() - t0 < kWaitNs) {
+            }
+        }
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(pl.tmem_cols) : "memory");
+}
+
+// [tokens][heads][channels] in boxes of 64 channels.
+bool encode(const PromptSide& x, bool bf16, int64_t n, int heads, int D, int box_heads, int box_tokens, CUtensorMap* map) {
+    const EncodeTiledFn enc = encode_fn();
+    if (enc == nullptr) return false;
+    // (strides of dimensions of one are not used, but have to be some)
+    if (x.head == 0) heads = 1;
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)n};
+    const cuuint64_t strides[2] = {heads > 1 ? (cuuint64_t)(2 * x.head) : 512, n > 1 ? (cuuint64_t)(2 * x.token) : 512};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens}, step[3] = {1, 1, 1};
+    return enc(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<uint16_t*>(x.p), dims, strides,
+               box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Rows on 16 bytes, no further apart than a tensor map reaches; a row of all tokens, or (queries) of all heads, has none.
+bool mapped(const PromptSide& x, int64_t n, int heads, bool shared_heads) {
+    const int64_t far = (int64_t)1 << 39;
+    return (uintptr_t)x.p % 16 == 0 && (n == 1 || (x.token > 0 && x.token % 8 == 0 && x.token < far / 2)) &&
+           (heads == 1 || (x.head == 0 ? shared_heads : x.head > 0 && x.head % 8 == 0 && x.head < far / 2));
+}
+
+bool make_plan(const PromptArgs& a, int tiles, PromptPlan* p) {
+    p->row_heads = a.group < 128 ? a.group : 128;
+    p->tile_tokens = 128 / p->row_heads;
+    p->head_parts = (a.group + p->row_heads - 1) / p->row_heads;
+    p->k_atoms = (a.D + 63) / 64;
+    p->v_atoms = (a.Dv + 63) / 64;
+    p->o_cols = (a.Dv + 15) / 16 * 16;
+    p->slot_cols = tiles == 2 ? 256 : 512;
+    p->tmem_cols = 512;
+    if (tiles == 2 && kOCol + p->o_cols > 256) return false;
+    p->stage_bytes = (p->k_atoms + p->v_atoms) * kAtom;
+    p->ring_off = tiles * p->k_atoms * kQAtom;
+    p->stages = (227 * 1024 - kMisc - p->ring_off) / p->stage_bytes;
+    if (p->stages > kMaxStages) p->stages = kMaxStages;
+    p->misc_off = p->ring_off + p->stages * p->stage_bytes;
+    p->smem = p->misc_off + kMisc;
+    return p->stages >= 2;
+}
+
+}  // namespace
+
+bool prompt_tile_supported(const PromptArgs& a) {
+    return a.D % 8 == 0 && a.Dv % 8 == 0 && (uintptr_t)a.out % 16 == 0 && mapped(a.q, a.n, a.k_heads * a.group, false) &&
+           mapped(a.k, a.n, a.k_heads, true) && mapped(a.v, a.n, a.k_heads, true);
+}
+
+cudaError_t launch_prompt_tile(const PromptArgs& a, bool bf16, unsigned* counters, cudaStream_t st) {
+    PromptPlan p{};
+    int tiles = 2;
+    if (!make_plan(a, 2, &p)) {
+        tiles = 1;
+        if (!make_plan(a, 1, &p)) return cudaErrorNotSupported;
+    }
+    PromptMaps maps;
+    if (!encode(a.q, bf16, a.n, a.k_heads * a.group, a.D, p.row_heads, p.tile_tokens, &maps.q) ||
+        !encode(a.k, bf16, a.n, a.k_heads, a.D, 1, kTok, &maps.k) || !encode(a.v, bf16, a.n, a.k_heads, a.Dv, 1, kTok, &maps.v))
+        return cudaErrorUnknown;
+    // as many units as the prompts can make, each of which ends one
+    const int64_t unit_tokens = tiles * p.tile_tokens;
+    const int64_t units = ((int64_t)a.n / unit_tokens + (a.B < a.n ? a.B : a.n)) * a.k_heads * p.head_parts;
+    if (units > 2000000000) return cudaErrorNotSupported;      // they are numbered in 32 bits
+    const int grid = (int)(units < num_sms() ? units : num_sms());
+    auto* kernel = tiles == 2 ? (bf16 ? prompt_tile_kernel<true, 2> : prompt_tile_kernel<false, 2>)
+                              : (bf16 ? prompt_tile_kernel<true, 1> : prompt_tile_kernel<false, 1>);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
+    if (e == cudaSuccess) e = prefer_max_shared(reinterpret_cast<const void*>(kernel));
+    if (e != cudaSuccess) return e;
+    kernel<<<grid, 128 + 128 * tiles, p.smem, st>>>(a, p, maps, counters, take_drop_arrival() ? 1 : 0);
+    note_launch();
+    return cudaGetLastError();
+}
+
+}  // namespace soniq

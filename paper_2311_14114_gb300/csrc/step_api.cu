@@ -93,15 +93,17 @@ soniq_status soniq_prompt_attend(const void* Q, int64_t q_token_stride, int64_t 
                                  int64_t k_token_stride, int64_t k_head_stride, const void* V, int64_t v_token_stride,
                                  int64_t v_head_stride, const int32_t* starts, int32_t B, int64_t n, int32_t q_heads,
                                  int32_t k_heads, int32_t D, int32_t Dv, int32_t dtype, int32_t causal, float scale,
-                                 void* out, soniq_stream_t stream) {
+                                 void* out, void* scratch, size_t scratch_bytes, soniq_stream_t stream) {
     if (B < 0 || n < 0 || q_heads < 1 || k_heads < 1 || q_heads % k_heads != 0 || D < 1 || Dv < 1 ||
         (dtype != SONIQ_OUT_F16 && dtype != SONIQ_OUT_BF16) || !std::isfinite(scale) || scale < 0.0f)
         return SONIQ_ERR_INVALID_ARG;
-    if (D > kMaxChannels || Dv > kMaxChannels || q_heads > kMaxHeads || n >= kMaxTokens) return SONIQ_ERR_UNSUPPORTED;
+    if (D > kMaxChannels || Dv > kMaxChannels || q_heads > kMaxHeads || n > kMaxTokens / 2) return SONIQ_ERR_UNSUPPORTED;
     if (B == 0 || n == 0) return SONIQ_OK;
     if (Q == nullptr || K == nullptr || V == nullptr || starts == nullptr || out == nullptr) return SONIQ_ERR_INVALID_ARG;
     if (!aligned_to(Q, 2) || !aligned_to(K, 2) || !aligned_to(V, 2) || !aligned_to(out, 2) || !aligned_to(starts, 4))
         return SONIQ_ERR_ALIGNMENT;
+    if (scratch == nullptr || (int64_t)scratch_bytes < kPromptScratchBytes) return SONIQ_ERR_INVALID_ARG;
+    if (!aligned_to(scratch, 16)) return SONIQ_ERR_ALIGNMENT;
     unsigned* err = device_error_word();
     if (err == nullptr) return SONIQ_ERR_CUDA;
     const PromptArgs a{{static_cast<const uint16_t*>(Q), q_token_stride, q_head_stride},
@@ -109,7 +111,12 @@ soniq_status soniq_prompt_attend(const void* Q, int64_t q_token_stride, int64_t 
                        {static_cast<const uint16_t*>(V), v_token_stride, v_head_stride},
                        starts, B, (int32_t)n, k_heads, q_heads / k_heads, D, Dv, causal != 0, scale,
                        static_cast<uint16_t*>(out), err};
-    return launched(launch_prompt_rows(a, dtype == SONIQ_OUT_BF16, reinterpret_cast<cudaStream_t>(stream)));
+    const bool bf16 = dtype == SONIQ_OUT_BF16;
+    const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (!prompt_tile_supported(a)) return launched(launch_prompt_rows(a, bf16, st));
+    return launched(launch_prompt_tile(a, bf16, static_cast<unsigned*>(scratch), st));
 }
+
+int64_t soniq_prompt_attend_scratch_bytes(void) { return kPromptScratchBytes; }
 
 }  // extern "C"

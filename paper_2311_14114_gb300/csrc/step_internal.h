@@ -61,6 +61,11 @@ struct PromptArgs {
     uint16_t* out;
     unsigned* err;
 };
+// A warp to a row, of any kind; and tensor-core tiles, of rows on 16 bytes.  counters: two
+// words that are zero between launches.
 cudaError_t launch_prompt_rows(const PromptArgs& a, bool bf16, cudaStream_t st);
+bool prompt_tile_supported(const PromptArgs& a);
+cudaError_t launch_prompt_tile(const PromptArgs& a, bool bf16, unsigned* counters, cudaStream_t st);
+constexpr int64_t kPromptScratchBytes = 256;
 
 }  // namespace soniq

@@ -40,7 +40,7 @@ EXPORTED = ["soniq_abi_version", "soniq_status_string", "soniq_group_codes",
             "soniq_mp_gemm_scratch_bytes", "soniq_mp_conv2d", "soniq_mp_conv2d_scratch_bytes", "soniq_sync_status",
             "soniq_test_drop_barrier_arrival", "soniq_kv_row_bytes", "soniq_kv_validate", "soniq_kv_write",
             "soniq_kv_read", "soniq_kv_attend", "soniq_kv_attend_scratch_bytes", "soniq_kv_plan", "soniq_rotate_heads",
-            "soniq_prompt_attend"]
+            "soniq_prompt_attend", "soniq_prompt_attend_scratch_bytes"]
 
 _SCALE = {"tensor": SCALE_PER_TENSOR, "row": SCALE_PER_ROW, "calibrated": SCALE_CALIBRATED}
 
@@ -157,8 +157,10 @@ def lib() -> ctypes.CDLL:
         L.soniq_rotate_heads.argtypes = [P, P, i64, i32, i32, P, P, ctypes.c_float, P]
         L.soniq_rotate_heads.restype = i32
         L.soniq_prompt_attend.argtypes = [P, i64, i64, P, i64, i64, P, i64, i64, P, i32, i64, i32, i32, i32, i32, i32, i32,
-                                          ctypes.c_float, P, P]
+                                          ctypes.c_float, P, P, ctypes.c_size_t, P]
         L.soniq_prompt_attend.restype = i32
+        L.soniq_prompt_attend_scratch_bytes.argtypes = []
+        L.soniq_prompt_attend_scratch_bytes.restype = i64
         _lib = L
     return _lib
 
@@ -202,14 +204,16 @@ def _need(t: torch.Tensor, dtype, name: str):
 # graph's own memory instead: graphs that share a capture stream may be
 # replayed side by side, a later, larger call may replace the cached buffer,
 # and a zero fill that is captured happens only when its graph is replayed.  For
-# the quantize scratch that fill is part of the graph (8.4 KB, one node); of the
-# attention scratch only the leading counters are filled.
+# the quantize scratch that fill is part of the graph (8.4 KB, one node), as for
+# the prompts' counters (256 bytes); of the cache's attention scratch only the
+# leading counters are filled.
 _scratch = {}
 KV_SCRATCH_ZERO = 8192
+PROMPT_SCRATCH = 256            # soniq_prompt_attend_scratch_bytes
 
 
 def _graph_scratch(nbytes: int, device, use: str) -> torch.Tensor:
-    buf = (torch.zeros if use == "quantize" else torch.empty)(nbytes, dtype=torch.uint8, device=device)
+    buf = (torch.zeros if use in ("quantize", "prompt") else torch.empty)(nbytes, dtype=torch.uint8, device=device)
     if use == "kv":
         buf[:KV_SCRATCH_ZERO].zero_()
     return buf
@@ -237,7 +241,7 @@ def _get_scratch(nbytes: int, device, stream, use: str) -> Optional[torch.Tensor
 def reset_scratch():
     """Zero every cached scratch buffer that a call expects zeroed (needed after a SONIQ_ERR_TIMEOUT)."""
     for key, buf in _scratch.items():
-        if key[0] in ("quantize", "kv"):
+        if key[0] in ("quantize", "kv", "prompt"):
             buf.zero_()
 
 
@@ -782,11 +786,12 @@ def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: tor
     else:
         _need_here(out, q.dtype, (n, Hq, Dv), "out")
     sq, sk, sv = q.stride(), k.stride(), v.stride()
+    scratch = _get_scratch(PROMPT_SCRATCH, q.device, stream, "prompt")
     _check(lib().soniq_prompt_attend(q.data_ptr(), sq[0], sq[1], k.data_ptr(), sk[0], sk[1], v.data_ptr(), sv[0], sv[1],
                                      starts.data_ptr(), starts.numel() - 1, n, Hq, Hk, D, Dv,
                                      OUT_BF16 if q.dtype == torch.bfloat16 else OUT_F16, int(bool(causal)),
-                                     1.0 / math.sqrt(D) if scale is None else float(scale), out.data_ptr(), _stream(stream)),
-           "soniq_prompt_attend")
+                                     1.0 / math.sqrt(D) if scale is None else float(scale), out.data_ptr(), scratch.data_ptr(),
+                                     PROMPT_SCRATCH, _stream(stream)), "soniq_prompt_attend")
     return out
 
 

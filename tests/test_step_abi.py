@@ -100,22 +100,26 @@ def test_the_binding_refuses(sq):
 
 def attend(sq, **kw):
     a = dict(Q=FAKE, qt=512, qh=64, K=FAKE, kt=128, kh=64, V=FAKE, vt=128, vh=64, starts=FAKE, B=1, n=4, q_heads=8, k_heads=2,
-             D=64, Dv=64, dtype=0, causal=1, scale=0.1, out=FAKE)
+             D=64, Dv=64, dtype=0, causal=1, scale=0.1, out=FAKE, scratch=FAKE, bytes=256)
     assert set(kw) <= set(a)
     a.update(kw)
     return sq.lib().soniq_prompt_attend(*a.values(), None)
 
 
 @pytest.mark.parametrize("kw,want", [
-    (dict(B=0), OK), (dict(n=0), OK), (dict(B=-1), INVALID), (dict(n=-1), INVALID), (dict(n=1 << 31), UNSUPPORTED),
+    (dict(B=0), OK), (dict(n=0), OK), (dict(B=-1), INVALID), (dict(n=-1), INVALID), (dict(n=(1 << 30) + 1), UNSUPPORTED),
     (dict(q_heads=7), INVALID), (dict(q_heads=0), INVALID), (dict(k_heads=0), INVALID), (dict(q_heads=4098), UNSUPPORTED),
     (dict(D=0), INVALID), (dict(Dv=0), INVALID), (dict(D=257), UNSUPPORTED), (dict(Dv=264), UNSUPPORTED), (dict(dtype=3), INVALID),
     (dict(scale=math.inf), INVALID), (dict(scale=math.nan), INVALID), (dict(scale=-0.1), INVALID), (dict(Q=None), INVALID),
     (dict(K=None), INVALID), (dict(V=None), INVALID), (dict(starts=None), INVALID), (dict(out=None), INVALID),
     (dict(Q=FAKE + 1), ALIGNMENT), (dict(K=FAKE + 1), ALIGNMENT), (dict(V=FAKE + 1), ALIGNMENT), (dict(out=FAKE + 1), ALIGNMENT),
-    (dict(starts=FAKE + 2), ALIGNMENT)])
+    (dict(starts=FAKE + 2), ALIGNMENT), (dict(scratch=None), INVALID), (dict(bytes=255), INVALID), (dict(scratch=FAKE + 8), ALIGNMENT)])
 def test_bad_prompts(sq, kw, want):
     assert attend(sq, **kw) == want
+
+
+def test_prompt_scratch(sq):
+    assert sq.lib().soniq_prompt_attend_scratch_bytes() == sq.PROMPT_SCRATCH
 
 
 def test_the_binding_refuses_prompts(sq):
