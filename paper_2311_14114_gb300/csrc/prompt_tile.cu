@@ -5,15 +5,16 @@
 // A tile is 128 rows: the query heads of one key head (128 at most) at as many
 // neighbouring tokens as fit, so a key block serves all of them.  A CTA works at
 // one unit at a time, TILES neighbouring tiles of one prompt and key head, over
-// blocks of 64 tokens.  Its warps:
+// blocks of 128 tokens.  Its warps:
 //   warp 0 (and 2)   issue the MMAs, each for one tile;
 //   warp 1           copies queries, keys and values by TMA;
 //   warp 3           finds the next unit;
-//   warps 4-7, 8-11  softmax of a tile, a thread to a row.
-// Scores have two buffers a tile: the next block's are there when this one's
-// softmax ends, and weights go over the scores that they come from.  Units are
-// handed out by a counter, the longest of a prompt first, and one unit's scores
-// begin while the one before leaves its outputs.
+//   warps 4-11 and 12-19  softmax of a tile, two threads to a row.
+// Weights go over the scores that they come from.  While one tile's softmax runs,
+// the tensor cores work for the other; a lone tile has two buffers of scores.
+// Keys and values come in pieces of 128 tokens by 128 channels, in the order in
+// which the MMAs take them.  Units are handed out by a counter, the longest of a
+// prompt first, and one unit's scores begin while the one before leaves its outputs.
 //
 // Numerics.  Scores are fp32.  A row's weights are 2^(score - m), held at most
 // 2^15: m is raised, and O with it, only when a weight would pass that, to where
@@ -36,11 +37,9 @@ namespace soniq {
 
 namespace {
 
-constexpr int kTok = 64;                 // tokens of a block
-constexpr int kAtom = kTok * 128;        // bytes of a 64-channel column group of a key or value block
-constexpr int kQAtom = 128 * 128;        // ... of a query tile
-constexpr int kOCol = 2 * kTok;          // O's first column in a tile's TMEM columns, behind two buffers of scores
-constexpr int kMaxStages = 8;
+constexpr int kTok = 128;                // tokens of a block
+constexpr int kAtom = kTok * 128;        // bytes of a 64-channel column group of a key or value block, or of a query tile
+constexpr int kMaxSlots = 12;
 constexpr float kMost = 15.0f, kBegin = 8.0f;      // log2 of the largest weight, and of a row's largest when m is raised
 
 struct PromptPlan {
@@ -49,8 +48,7 @@ struct PromptPlan {
     int head_parts;          // tiles that share a key head's query heads
     int k_atoms, v_atoms;
     int o_cols;              // Dv rounded up to whole MMA columns
-    int slot_cols, tmem_cols;
-    int stages, stage_bytes;
+    int slots, slot_bytes;   // of the ring of pieces
     int ring_off, misc_off, smem;
 };
 
@@ -67,15 +65,16 @@ struct Unit {
     __device__ __forceinline__ int blocks() const { return max(blocks0, blocks1); }
 };
 
-struct Bars {                // offsets in 8-byte barriers; the first 17 are those of copies (Flights)
-    static constexpr int k_full = 0, v_full = kMaxStages, q_full = 2 * kMaxStages, kv_free = q_full + 1,
-                         q_free = kv_free + kMaxStages, s_full = q_free + 1, p_full = s_full + 4, pv_done = p_full + 4,
+struct Bars {                // offsets in 8-byte barriers; the first ones are those of copies (Flights)
+    static constexpr int full = 0, q_full = kMaxSlots, free = q_full + 1,
+                         q_free = free + kMaxSlots, s_full = q_free + 1, p_full = s_full + 4, pv_done = p_full + 4,
                          o_full = pv_done + 2, o_free = o_full + 2, unit_full = o_free + 2, unit_free = unit_full + 2,
-                         drain = unit_free + 2, count = drain + 1;      // s_full, p_full: [tile][buffer]
+                         turn = unit_free + 2, drain = turn + 2, count = drain + 1;      // s_full, p_full: [tile][buffer]
 };
-constexpr int kMisc = 1024;
+constexpr int kMisc = 3072;
 static_assert(8 * Bars::count <= 512, "barriers");
 
+// 64 consecutive TMEM columns of this thread's lane (load + wait in one statement).
 __device__ __forceinline__ void tmem_ld64(uint32_t at, uint32_t (&r)[64]) {
 #define SONIQ_R4(i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3])
 #define SONIQ_R16(i) SONIQ_R4(i), SONIQ_R4(i + 4), SONIQ_R4(i + 8), SONIQ_R4(i + 12)
@@ -83,14 +82,45 @@ __device__ __forceinline__ void tmem_ld64(uint32_t at, uint32_t (&r)[64]) {
         "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
         "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
         "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,"
-        "%62,%63}, [%64];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
+        "%62,%63}, [%64];\n\ttcgen05.wait::ld.sync.aligned;"
         : SONIQ_R16(0), SONIQ_R16(16), SONIQ_R16(32), SONIQ_R16(48)
         : "r"(at)
         : "memory");
+}
 #undef SONIQ_R16
 #undef SONIQ_R4
+// 16 columns without the wait.
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
 }
+// MMAs and commits of a whole warp, issued by one of its lanes, which the instruction
+// itself elects: control flow stays that of the warp, and what it works out in uniform
+// registers.  (Under a branch of one lane each operand is moved there first, and
+// waits for the MMA before to have read it: 90 to 130 cycles an MMA.)
+__device__ __forceinline__ void warp_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc));
+}
+__device__ __forceinline__ void warp_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(acc));
+}
+__device__ __forceinline__ void warp_commit(uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar)
+        : "memory");
+}
+// A value that is the same in all lanes, so that the compiler knows.
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -98,55 +128,66 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 
 template <bool BF16, int TILES>
-__global__ void __launch_bounds__(128 + 128 * TILES, 1)
+__global__ void __launch_bounds__(128 + 256 * TILES, 1)
     prompt_tile_kernel(const PromptArgs a, const PromptPlan pl, const __grid_constant__ PromptMaps maps, unsigned* counters, const int drop) {
     extern __shared__ __align__(1024) uint8_t smem[];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
     const uint32_t smem0 = tc::smem_u32(smem), ring = smem0 + pl.ring_off, bars = smem0 + pl.misc_off;
     uint8_t* misc = smem + pl.misc_off;
     Unit* units = reinterpret_cast<Unit*>(misc + 512);                // [2]
     uint32_t* words = reinterpret_cast<uint32_t*>(misc + 640);
     const uint32_t abort_flag = tc::smem_u32(words);
     uint32_t* tmem_at = words + 1;
+    float* halves = reinterpret_cast<float*>(misc + 1024);            // [tile][half][128]: what the two threads of a row tell each other
     auto bar = [&](int i) { return bars + 8u * i; };
     const int unit_tokens = TILES * pl.tile_tokens;
+    constexpr int SB = 3 - TILES;                       // buffers of scores
+    constexpr int slot_cols = 512 / TILES, o_col = SB * kTok;      // TMEM columns of a tile; where its outputs begin
 
     if (tid == 0) {
         auto init = [&](int first, int n, int arrivals) {
             for (int i = 0; i < n; ++i) tc::mbar_init(bar(first + i), arrivals);
         };
-        init(Bars::k_full, 2 * kMaxStages + 1, 1);
-        init(Bars::kv_free, kMaxStages + 1, TILES);      // and q_free
+        init(Bars::full, kMaxSlots + 1, 1);              // and q_full
+        init(Bars::free, kMaxSlots + 1, TILES);          // and q_free
         init(Bars::s_full, 4, 1);
-        init(Bars::p_full, 4, 4);
+        init(Bars::p_full, 4, 8);
         init(Bars::pv_done, 4, 1);                       // and o_full
-        init(Bars::o_free, 2, 4);
+        init(Bars::o_free, 2, 8);
         init(Bars::unit_full, 2, 1);
-        init(Bars::unit_free, 2, 1 + 5 * TILES);
+        init(Bars::unit_free, 2, 1 + 9 * TILES);
+        init(Bars::turn, 2, 1);
         init(Bars::drain, 1, TILES);
         words[0] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(tmem_at)), "r"(pl.tmem_cols) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(tmem_at)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
-    const uint32_t tmem = *tmem_at;
-    auto wait = [&](int i, uint32_t parity) { return wait_warp(bar(i), parity & 1u, abort_flag, a.err); };
+    const uint32_t tmem = uniform(*tmem_at);
+    // (most waits are over when they begin: one look at those costs 20 cycles, the loop 160)
+    auto wait = [&](int i, uint32_t parity) {
+        return __all_sync(0xffffffffu, tc::mbar_try_wait(bar(i), parity & 1u)) || wait_warp(bar(i), parity & 1u, abort_flag, a.err);
+    };
 
     // The next unit, as the warps of other roles read it; they release it (`done`) when they have gone on.
     auto next_unit = [&](uint32_t n, Unit* u) {
         if (!wait(Bars::unit_full + (n & 1), n >> 1)) return false;
-        *u = units[n & 1];
-        __syncwarp();
+        const Unit x = units[n & 1];
+        *u = Unit{uniform(x.start), uniform(x.len), uniform(x.token), uniform(x.kv_head), uniform(x.part), uniform(x.blocks0), uniform(x.blocks1)};
         if (lane == 0) tc::mbar_arrive(bar(Bars::unit_free + (n & 1)));
         return u->token >= 0;
     };
 
     Flights flights;       // of the copying warp
+    // Registers move to the softmax warps: 4 x 104 + 64 = 5 x 96 a thread.  (All four warps of a group give up theirs, or
+    // the others wait for them without end.)
+    if (warp < 4) {
+        if constexpr (TILES == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 3) {
         // ---- units: numbered prompt by prompt, later tokens first, key heads side by side ----
         const int per_unit = a.k_heads * pl.head_parts;
@@ -234,130 +275,194 @@ __global__ void __launch_bounds__(128 + 128 * TILES, 1)
             for (int i = 0; i < tiles * pl.k_atoms; ++i) {
                 const int tile = i / pl.k_atoms, atom = i % pl.k_atoms;
                 if (tc::elect_one())
-                    tma_load_3d(smem0 + i * kQAtom, &maps.q, 64 * atom, a.q.head ? head : 0, u.start + u.token + tile * pl.tile_tokens, bar(Bars::q_full));
+                    tma_load_3d(smem0 + i * kAtom, &maps.q, 64 * atom, a.q.head ? head : 0, u.start + u.token + tile * pl.tile_tokens, bar(Bars::q_full));
             }
+            // a block's pieces of keys or of values
+            auto pieces = [&](int j, int atoms, const CUtensorMap* map, int kv_head) {
 #pragma unroll 1
-            for (int j = 0; j < blocks; ++j, kv.step(pl.stages)) {
-                ok = wait(Bars::kv_free + kv.i, kv.phase ^ 1u);
-                if (!ok) break;
-                const uint32_t at = ring + kv.i * pl.stage_bytes;
-                const int token = u.start + j * kTok;
-                if (drop && blockIdx.x == 0 && n == 0 && j == 0) continue;
-                flights.issue(Bars::k_full + kv.i, kv.phase);
-                flights.issue(Bars::v_full + kv.i, kv.phase);
-                if (tc::elect_one()) {
-                    tc::mbar_arrive_expect_tx(bar(Bars::k_full + kv.i), pl.k_atoms * kAtom);
-                    for (int i = 0; i < pl.k_atoms; ++i)
-                        tma_load_3d(at + i * kAtom, &maps.k, 64 * i, a.k.head ? u.kv_head : 0, token, bar(Bars::k_full + kv.i));
-                    tc::mbar_arrive_expect_tx(bar(Bars::v_full + kv.i), pl.v_atoms * kAtom);
-                    for (int i = 0; i < pl.v_atoms; ++i)
-                        tma_load_3d(at + (pl.k_atoms + i) * kAtom, &maps.v, 64 * i, a.v.head ? u.kv_head : 0, token, bar(Bars::v_full + kv.i));
+                for (int c = 0; ok && c < atoms; c += 2, kv.step(pl.slots)) {
+                    ok = wait(Bars::free + kv.i, kv.phase ^ 1u);
+                    if (!ok) break;
+                    if (drop && blockIdx.x == 0 && n == 0 && j == 0) continue;
+                    flights.issue(Bars::full + kv.i, kv.phase);
+                    const uint32_t at = ring + kv.i * pl.slot_bytes;
+                    if (tc::elect_one()) {
+                        tc::mbar_arrive_expect_tx(bar(Bars::full + kv.i), (c + 1 < atoms ? 2 : 1) * kAtom);
+                        tma_load_3d(at, map, 64 * c, kv_head, u.start + j * kTok, bar(Bars::full + kv.i));
+                        if (c + 1 < atoms) tma_load_3d(at + kAtom, map, 64 * c + 64, kv_head, u.start + j * kTok, bar(Bars::full + kv.i));
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
+            };
+#pragma unroll 1
+            for (int j = -SB; ok && j < blocks; ++j) {
+                if (j >= 0) pieces(j, pl.v_atoms, &maps.v, a.v.head ? u.kv_head : 0);
+                if (j + SB < blocks) pieces(j + SB, pl.k_atoms, &maps.k, a.k.head ? u.kv_head : 0);
             }
         }
-    } else if (warp == 0 || (TILES == 2 && warp == 2)) {
+    } else if (warp == 0 || TILES == 2) {
         // ---- MMAs of tile s ----
-        const int s = warp >> 1;
+        const int s = TILES == 2 ? warp >> 1 : 0;
         constexpr uint32_t fmt = (1u << 4) | (BF16 ? (1u << 7) | (1u << 10) : 0u) | ((128u >> 4) << 24);
-        const uint32_t id_s = fmt | ((kTok >> 3) << 17), id_o = fmt | (1u << 16) | ((uint32_t)(pl.o_cols >> 3) << 17);
-        const uint32_t t_s = tmem + s * pl.slot_cols;
-        const uint64_t q_tile = tc::sw128_desc(smem0 + s * pl.k_atoms * kQAtom);
+        auto columns = [](int n) { return (uint32_t)(n >> 3) << 17; };
         const int steps = (a.D + 15) / 16;      // of 16 channels
-        const bool leader = tc::elect_one();
-        Ring now, next;                          // the block whose outputs, and whose scores, come next
-        uint32_t done = 0, tiles = 0;            // blocks and tiles so far
-        Unit u;
+        const int k_pieces = (pl.k_atoms + 1) / 2, v_pieces = (pl.v_atoms + 1) / 2;
         bool ok = true;
+        // the ring's next n pieces are there
+        auto arrived = [&](Ring r, int n) {
+            for (int i = 0; ok && i < n; ++i, r.step(pl.slots)) ok = wait(Bars::full + r.i, r.phase);
+            tc::tc_fence_after();
+        };
+        const uint32_t t_s = tmem + s * slot_cols;
+        const uint64_t q_tile = tc::sw128_desc(smem0 + s * pl.k_atoms * kAtom);
+        // scores of a block, `keys` of it, whose pieces begin at r
+        auto scores = [&](uint32_t buf, int keys, Ring r) {
+            const uint32_t d = t_s + buf * kTok, id = fmt | columns(keys);
+            uint64_t q = q_tile;
+#pragma unroll 1
+            for (int c = 0; c < k_pieces; ++c, r.step(pl.slots), q += 2 * (kAtom >> 4)) {
+                const uint64_t k = tc::sw128_desc(ring + r.i * pl.slot_bytes);
+                const int some = steps - 8 * c;
+                if (some >= 8) {
+#pragma unroll
+                    for (int h = 0; h < 8; ++h)
+                        warp_mma_ss(d, q + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), k + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), id, h == 0 ? c : 1);
+                } else {
+                    if (some >= 4) {
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) warp_mma_ss(d, q + 2 * h, k + 2 * h, id, h == 0 ? c : 1);
+                    }
+#pragma unroll 1
+                    for (int h = some >= 4 ? 4 : 0; h < some; ++h)
+                        warp_mma_ss(d, q + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), k + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), id, c | h);
+                }
+                warp_commit(bar(Bars::free + r.i));
+            }
+            warp_commit(bar(Bars::s_full + 2 * s + buf));
+        };
+        // outputs over block i, `keys` of it, of which `first` are the prompt's
+        auto outputs = [&](int i, uint32_t buf, int keys, int first, Ring r) {
+            const uint32_t p = t_s + buf * kTok;
+#pragma unroll 1
+            for (int c = 0; c < v_pieces; ++c, r.step(pl.slots)) {
+                const uint32_t values = ring + r.i * pl.slot_bytes, d = t_s + o_col + 128 * c;
+                if (keys > first) {
+                    // Tokens behind the prompt, whose weights are 0, may hold anything (a buffer's padding): 0 times
+                    // that is to be 0.  (The other tile's warp writes the same zeros.)
+                    const int n16 = 8 * (keys - first), atoms = min(pl.v_atoms - 2 * c, 2);
+                    for (int k = lane; k < atoms * n16; k += 32)
+                        sts128f(values + (k >= n16 ? kAtom - 16 * n16 : 0) + 128 * first + 16 * k, 0.0f, 0.0f, 0.0f, 0.0f);
+                    tc::fence_proxy_async_shared();
+                    __syncwarp();
+                }
+                const uint64_t v = value_desc(values, kAtom);
+                const uint32_t id = fmt | (1u << 16) | columns(min(pl.o_cols - 128 * c, 128));
+                if (keys == kTok) {
+#pragma unroll
+                    for (int k = 0; k < kTok / 16; ++k) warp_mma_ts(d, p + 8 * k, v + k * (2048 >> 4), id, k == 0 ? i : 1);
+                } else {
+#pragma unroll 1
+                    for (int k = 0; k < keys / 16; ++k) warp_mma_ts(d, p + 8 * k, v + k * (2048 >> 4), id, i | k);
+                }
+                warp_commit(bar(Bars::free + r.i));
+            }
+            warp_commit(bar(Bars::pv_done + s));
+        };
+        auto skip = [&](Ring& r, int n) {
+            for (int i = 0; i < n; ++i) r.step(pl.slots);
+        };
+        // Pieces that only the other tile uses are released when they are there, so that no release runs ahead.
+        auto leave = [&](Ring r, int n) {
+            for (int i = 0; ok && i < n; ++i, r.step(pl.slots)) {
+                ok = wait(Bars::full + r.i, r.phase);
+                if (ok && lane == 0) tc::mbar_arrive(bar(Bars::free + r.i));
+                __syncwarp();
+            }
+        };
+        Ring kv;                                 // the next piece
+        uint32_t done = 0, tiles = 0, turns = 0; // blocks, tiles and turns so far
+        Unit u;
         for (uint32_t n = 0; ok && next_unit(n, &u); ++n) {
             const int blocks = u.blocks(), mine = u.blocks_of(s);
+            // keys of the last block, in whole steps of 16
+            const int end = a.causal ? min(u.token + (s + 1) * pl.tile_tokens, u.len) : u.len;
+            const int last_keys = (end - (mine - 1) * kTok + 15) / 16 * 16;
             ok = wait(Bars::q_full, n);
-            if (!ok) break;
-            tc::tc_fence_after();
-            next = now;
+            if (mine == 0 && lane == 0) tc::mbar_arrive(bar(Bars::q_free));
+            __syncwarp();
 #pragma unroll 1
-            for (int i = -2; i < mine; ++i) {
-                const uint32_t buf = (done + (i & 1)) & 1u;
-                if (i >= 0) {
-                    ok = wait(Bars::p_full + 2 * s + buf, (done + i) >> 1) && wait(Bars::v_full + now.i, now.phase) &&
-                         (i > 0 || wait(Bars::o_free + s, tiles ^ 1u));
-                    if (!ok) break;
-                    tc::tc_fence_after();
-                    const uint32_t values = ring + now.i * pl.stage_bytes + pl.k_atoms * kAtom;
-                    if ((i + 1) * kTok > u.len) {
-                        // Tokens behind the prompt, whose weights are 0, may hold anything (a buffer's padding): 0 times
-                        // that is to be 0.  (The other tile's warp writes the same zeros.)
-                        const int first = u.len - i * kTok, rows = kTok - first;
-                        for (int k = lane; k < 8 * rows * pl.v_atoms; k += 32) {
-                            const uint32_t at = values + (k / (8 * rows)) * kAtom + 128 * first + 16 * (k % (8 * rows));
-                            sts128f(at, 0.0f, 0.0f, 0.0f, 0.0f);
-                        }
-                        tc::fence_proxy_async_shared();
-                        __syncwarp();
-                    }
-                    const uint64_t v = value_desc(values, kAtom);
-                    const uint32_t p = t_s + buf * kTok;
-                    if (leader) {
-#pragma unroll
-                        for (int k = 0; k < kTok / 16; ++k) mma_ts(t_s + kOCol, p + 8 * k, v + k * (2048 >> 4), id_o, i != 0 || k != 0);
-                        tc::mma_commit(bar(Bars::kv_free + now.i));
-                        tc::mma_commit(bar(Bars::pv_done + s));
-                        if (i == mine - 1) tc::mma_commit(bar(Bars::o_full + s));
-                    }
-                    __syncwarp();
-                    now.step(pl.stages);
+            for (int i = -SB; ok && i < blocks; ++i) {
+                const uint32_t buf = SB == 2 ? (done + (i & 1)) & 1u : 0u;
+                const bool out = i >= 0 && i < mine, in = i + SB < mine;
+                Ring keys_at = kv;
+                if (i >= 0) skip(keys_at, v_pieces);
+                // (what is there already, before what has to be waited for)
+                if (out) arrived(kv, v_pieces);
+                if (ok && in) arrived(keys_at, k_pieces);
+                if (ok && out) {
+                    ok = wait(Bars::p_full + 2 * s + buf, SB == 2 ? (done + i) >> 1 : done + i) && (i > 0 || wait(Bars::o_free + s, tiles ^ 1u));
                 }
-                if (i + 2 < mine) {
-                    ok = wait(Bars::k_full + next.i, next.phase);
-                    if (!ok) break;
-                    tc::tc_fence_after();
-                    uint64_t q = q_tile, k = tc::sw128_desc(ring + next.i * pl.stage_bytes);
-                    const uint32_t d = t_s + buf * kTok;
-                    // column groups of four steps
-#pragma unroll 1
-                    for (int c = 0; c < steps; c += 4) {
-                        if (leader) {
-                            mma_ss(d, q, k, id_s, c != 0);
-                            if (c + 1 < steps) mma_ss(d, q + 2, k + 2, id_s, 1);
-                            if (c + 2 < steps) mma_ss(d, q + 4, k + 4, id_s, 1);
-                            if (c + 3 < steps) mma_ss(d, q + 6, k + 6, id_s, 1);
-                        }
-                        q += kQAtom >> 4;
-                        k += kAtom >> 4;
-                    }
-                    if (leader) {
-                        tc::mma_commit(bar(Bars::s_full + 2 * s + buf));
-                        if (i + 3 == mine) tc::mma_commit(bar(Bars::q_free));
-                    }
+                // The two tiles take turns: the softmax of one has the time of the other's MMAs.  (Without, the two ran in
+                // step, both softmaxes and then both tiles' MMAs: 5200 cycles a block instead of 2700.)
+                if (TILES == 2 && i >= 0 && ok) ok = wait(Bars::turn + s, turns ^ (s ^ 1u));
+                if (!ok) break;
+                tc::tc_fence_after();
+                if (out) {
+                    outputs(i, buf, i == mine - 1 ? last_keys : kTok, u.len - i * kTok, kv);
+                    if (i == mine - 1) warp_commit(bar(Bars::o_full + s));
+                }
+                if (in) {
+                    scores(buf, i + SB == mine - 1 ? last_keys : kTok, keys_at);
+                    if (i + SB == mine - 1) warp_commit(bar(Bars::q_free));
+                }
+                if (TILES == 2 && i >= 0) {
+                    if (lane == 0) tc::mbar_arrive(bar(Bars::turn + (s ^ 1)));
                     __syncwarp();
-                    next.step(pl.stages);
+                    ++turns;
+                }
+                if (i >= 0) {
+                    if (!out) leave(kv, v_pieces);
+                    kv = keys_at;
+                }
+                if (i + SB < blocks) {
+                    if (!in) leave(kv, k_pieces);
+                    skip(kv, k_pieces);
                 }
             }
-            if (!ok) break;
-            if (mine == 0 && lane == 0) tc::mbar_arrive(bar(Bars::q_free));
             done += mine;
             tiles += mine > 0;
-            // blocks that only the other tile sees: each is released when it is there, so that no release runs ahead
-#pragma unroll 1
-            for (int i = mine; i < blocks; ++i, now.step(pl.stages)) {
-                ok = wait(Bars::k_full + now.i, now.phase) && wait(Bars::v_full + now.i, now.phase);
-                if (!ok) break;
-                if (lane == 0) tc::mbar_arrive(bar(Bars::kv_free + now.i));
-                __syncwarp();
-            }
         }
-    } else if (warp >= 4) {
-        // ---- softmax of tile s ----
-        const int s = (warp >> 2) - 1, quad = warp & 3, row = quad * 32 + lane;
-        const uint32_t t_s = tmem + s * pl.slot_cols + ((uint32_t)(quad * 32) << 16);
+    }
+    } else {
+        if constexpr (TILES == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        // ---- softmax of tile s: two threads to a row, each with half of a block's keys ----
+        const int s = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1, quad = warp & 3, row = quad * 32 + lane;
+        const uint32_t t_s = tmem + s * slot_cols + ((uint32_t)(quad * 32) << 16);
         const int row_token = row / pl.row_heads, row_head = row - row_token * pl.row_heads;
         const int heads = a.k_heads * a.group;
+        float* mine_at = halves + (2 * s + half) * 128 + row;
+        const float* other_at = halves + (2 * s + 1 - half) * 128 + row;
+        // Whether it is so in any row of the two warps that share these 32.  (Waits are bounded, but this is not: a warp
+        // whose wait was given up goes on to the next such point, and both leave there.)
+        auto either = [&](bool x) {
+            uint32_t r;
+            asm volatile(
+                "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                : "=r"(r)
+                : "r"((uint32_t)x), "r"(1 + 4 * s + quad)
+                : "memory");
+            return r != 0;
+        };
         // (never 0: a score that is masked, minus infinity, has no weight at any scale)
         const float factor = fmaxf(a.scale * kLog2e, 1.4e-45f);
+        // this half's share of the outputs' columns
+        const int chunks = pl.o_cols / 16, c_first = half ? (chunks + 1) / 2 * 16 : 0, c_end = half ? pl.o_cols : (chunks + 1) / 2 * 16;
         uint32_t done = 0, tiles = 0;
         Unit u;
         bool ok = true;
-        for (uint32_t n = 0; ok && next_unit(n, &u); ++n) {
+        for (uint32_t n = 0;; ++n) {
+            ok = next_unit(n, &u);
+            if (either(!ok)) break;
             const int mine = u.blocks_of(s);
             if (mine == 0) continue;
             const int token = u.token + s * pl.tile_tokens + row_token, head = u.part * pl.row_heads + row_head;
@@ -368,49 +473,51 @@ __global__ void __launch_bounds__(128 + 128 * TILES, 1)
             float m = kUnset, l = 0.0f;
 #pragma unroll 1
             for (int i = 0; i < mine; ++i, ++done) {
-                const uint32_t buf = done & 1u, t_b = t_s + buf * kTok;
-                ok = wait(Bars::s_full + 2 * s + buf, done >> 1);
-                if (!ok) break;
+                const uint32_t buf = SB == 2 ? done & 1u : 0u, t_b = t_s + buf * kTok;
+                ok = ok && wait(Bars::s_full + 2 * s + buf, SB == 2 ? done >> 1 : done);
                 tc::tc_fence_after();
                 uint32_t raw[64];
-                tmem_ld64(t_b, raw);
-                float2 x[kTok / 2];
+                tmem_ld64(t_b + 64 * half, raw);
+                float2 x[32];
 #pragma unroll
-                for (int k = 0; k < kTok / 2; ++k) x[k] = make_float2(__uint_as_float(raw[2 * k]), __uint_as_float(raw[2 * k + 1]));
-                const int p0 = i * kTok;
-                if (p0 + kTok > sure) {
-                    const int upto = end - p0;
+                for (int k = 0; k < 32; ++k) x[k] = make_float2(__uint_as_float(raw[2 * k]), __uint_as_float(raw[2 * k + 1]));
+                if ((i + 1) * kTok > sure) {
+                    const int upto = end - i * kTok - 64 * half;
 #pragma unroll
-                    for (int k = 0; k < kTok / 2; ++k) {
+                    for (int k = 0; k < 32; ++k) {
                         if (2 * k >= upto) x[k].x = -INFINITY;
                         if (2 * k + 1 >= upto) x[k].y = -INFINITY;
                     }
                 }
                 float tops[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) tops[k] = fmaxf(x[k].x, x[k].y);
-#pragma unroll
-                for (int k = 8; k < kTok / 2; ++k) tops[k & 7] = fmaxf(fmaxf(tops[k & 7], x[k].x), x[k].y);
+                for (int k = 0; k < 32; ++k) tops[k & 7] = k < 8 ? fmaxf(x[k].x, x[k].y) : fmaxf(fmaxf(tops[k & 7], x[k].x), x[k].y);
                 const float best = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
-                const bool over = fmaf(best, factor, -m) > kMost;
-                if (__any_sync(0xffffffffu, over)) {
-                    const float to = over ? best * factor - kBegin : m, by = ex2(m - to);
+                // (behind this both have read their scores, and weights may go over them)
+                if (either(!ok || fmaf(best, factor, -m) > kMost)) {
+                    *mine_at = best;
+                    if (either(!ok)) {
+                        ok = false;
+                        break;
+                    }
+                    const float both = fmaxf(best, *other_at);
+                    const bool over = fmaf(both, factor, -m) > kMost;
+                    const float to = over ? both * factor - kBegin : m, by = ex2(m - to);
                     m = to;
                     l *= by;
                     // scores whose products are off by their rounding: the row is done again
-                    if (over && !(fabsf(fmaf(best, factor, -m) - kBegin) <= 4.0f)) l = NAN;
+                    if (over && !(fabsf(fmaf(both, factor, -m) - kBegin) <= 4.0f)) l = NAN;
                     if (i != 0) {
                         // the MMAs that wrote O have to be complete
                         ok = wait(Bars::pv_done + s, done ^ 1u);
-                        if (!ok) break;
                         tc::tc_fence_after();
 #pragma unroll 1
-                        for (int c = 0; c < pl.o_cols; c += 16) {
+                        for (int c = c_first; c < c_end; c += 16) {
                             uint32_t v[16];
-                            tc::tmem_ld16(t_s + kOCol + c, v);
+                            tc::tmem_ld16(t_s + o_col + c, v);
 #pragma unroll
                             for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * by);
-                            tmem_st16v(t_s + kOCol + c, v);
+                            tmem_st16v(t_s + o_col + c, v);
                         }
                     }
                 }
@@ -425,27 +532,28 @@ __global__ void __launch_bounds__(128 + 128 * TILES, 1)
                         sums[k & 1] = fma2(y, make_float2(1.0f, 1.0f), sums[k & 1]);
                         w[k] = BF16 ? pack_bf16(y.x, y.y) : pack2(y.x, y.y);
                     }
-                    tmem_st16v(t_b + 16 * h, w);
+                    tmem_st16(t_b + 32 * half + 16 * h, w);
                 }
                 l += sums[0].x + sums[0].y + sums[1].x + sums[1].y;
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(bar(Bars::p_full + 2 * s + buf));
             }
-            if (!ok) break;
-            // ---- outputs ----
-            ok = wait(Bars::o_full + s, tiles);
-            if (!ok) break;
+            // ---- outputs, half of the columns each ----
+            ok = ok && wait(Bars::o_full + s, tiles);
+            *mine_at = l;
+            if (either(!ok)) break;
             tc::tc_fence_after();
-            const float inv = 1.0f / l;
+            const float inv = 1.0f / (half ? *other_at + l : l + *other_at);
             float odd = 0.0f;              // NaN once an output is not finite
             const int64_t out_row = (int64_t)(u.start + token) * heads + u.kv_head * a.group + head;
             uint16_t* out = a.out + out_row * a.Dv;
             constexpr float top = BF16 ? 3.3895313892515355e38f : 65504.0f;
 #pragma unroll 1
-            for (int c = 0; c < pl.o_cols; c += 16) {
+            for (int c = c_first; c < c_end; c += 16) {
                 uint32_t v[16], w[8];
-                tc::tmem_ld16(t_s + kOCol + c, v);
+                tc::tmem_ld16(t_s + o_col + c, v);
 #pragma unroll
                 for (int k = 0; k < 16; k += 2) {
                     const float y0 = __uint_as_float(v[k]) * inv, y1 = __uint_as_float(v[k + 1]) * inv;
@@ -463,14 +571,21 @@ __global__ void __launch_bounds__(128 + 128 * TILES, 1)
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(bar(Bars::o_free + s));
             ++tiles;
-            unsigned again = __ballot_sync(0xffffffffu, live && odd != 0.0f);
-            while (again != 0) {
-                const int from = __ffs(again) - 1;
-                again &= again - 1;
-                const int t = __shfl_sync(0xffffffffu, u.start + token, from), h = __shfl_sync(0xffffffffu, u.kv_head * a.group + head, from);
-                const int e = __shfl_sync(0xffffffffu, end, from);
-                prompt_row<BF16, true>(a, h, t, u.start, u.start + e);
-                __syncwarp();
+            // rows to be done again, behind both halves' stores
+            if (either(live && odd != 0.0f)) {
+                *mine_at = odd;
+                either(false);
+                const bool row_odd = live && (odd != 0.0f || *other_at != 0.0f);
+                // (every second one each)
+                unsigned again = __ballot_sync(0xffffffffu, row_odd && (lane & 1) == half);
+                while (again != 0) {
+                    const int from = __ffs(again) - 1;
+                    again &= again - 1;
+                    const int t = __shfl_sync(0xffffffffu, u.start + token, from), h = __shfl_sync(0xffffffffu, u.kv_head * a.group + head, from);
+                    const int e = __shfl_sync(0xffffffffu, end, from);
+                    prompt_row<BF16, true>(a, h, t, u.start, u.start + e);
+                    __syncwarp();
+                }
             }
         }
     }
@@ -490,7 +605,7 @@ __global__ void __launch_bounds__(128 + 128 * TILES, 1)
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
-    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(pl.tmem_cols) : "memory");
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
 // [tokens][heads][channels] in boxes of 64 channels.
@@ -521,16 +636,14 @@ bool make_plan(const PromptArgs& a, int tiles, PromptPlan* p) {
     p->k_atoms = (a.D + 63) / 64;
     p->v_atoms = (a.Dv + 63) / 64;
     p->o_cols = (a.Dv + 15) / 16 * 16;
-    p->slot_cols = tiles == 2 ? 256 : 512;
-    p->tmem_cols = 512;
-    if (tiles == 2 && kOCol + p->o_cols > 256) return false;
-    p->stage_bytes = (p->k_atoms + p->v_atoms) * kAtom;
-    p->ring_off = tiles * p->k_atoms * kQAtom;
-    p->stages = (227 * 1024 - kMisc - p->ring_off) / p->stage_bytes;
-    if (p->stages > kMaxStages) p->stages = kMaxStages;
-    p->misc_off = p->ring_off + p->stages * p->stage_bytes;
+    if ((3 - tiles) * kTok + p->o_cols > 512 / tiles) return false;
+    p->slot_bytes = (p->k_atoms > 1 || p->v_atoms > 1 ? 2 : 1) * kAtom;
+    p->ring_off = tiles * p->k_atoms * kAtom;
+    p->slots = (227 * 1024 - kMisc - p->ring_off) / p->slot_bytes;
+    if (p->slots > kMaxSlots) p->slots = kMaxSlots;
+    p->misc_off = p->ring_off + p->slots * p->slot_bytes;
     p->smem = p->misc_off + kMisc;
-    return p->stages >= 2;
+    return p->slots >= 3;
 }
 
 }  // namespace
@@ -561,7 +674,7 @@ cudaError_t launch_prompt_tile(const PromptArgs& a, bool bf16, unsigned* counter
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
     if (e == cudaSuccess) e = prefer_max_shared(reinterpret_cast<const void*>(kernel));
     if (e != cudaSuccess) return e;
-    kernel<<<grid, 128 + 128 * tiles, p.smem, st>>>(a, p, maps, counters, take_drop_arrival() ? 1 : 0);
+    kernel<<<grid, 128 + 256 * tiles, p.smem, st>>>(a, p, maps, counters, take_drop_arrival() ? 1 : 0);
     note_launch();
     return cudaGetLastError();
 }
