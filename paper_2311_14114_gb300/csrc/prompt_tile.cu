@@ -69,7 +69,7 @@ struct Bars {                // offsets in 8-byte barriers; the first ones are t
     static constexpr int full = 0, q_full = kMaxSlots, free = q_full + 1,
                          q_free = free + kMaxSlots, s_full = q_free + 1, p_full = s_full + 4, pv_done = p_full + 4,
                          o_full = pv_done + 2, o_free = o_full + 2, unit_full = o_free + 2, unit_free = unit_full + 2,
-                         turn = unit_free + 2, drain = turn + 2, count = drain + 1;      // s_full, p_full: [tile][buffer]
+                         turn = unit_free + 2, drain = turn + 2, count = drain + 1;      // s_full: [tile][buffer]; p_full: [tile or buffer][half]
 };
 constexpr int kMisc = 3072;
 static_assert(8 * Bars::count <= 512, "barriers");
@@ -117,6 +117,13 @@ __device__ __forceinline__ void warp_commit(uint32_t bar) {
     asm volatile(
         "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
         "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar)
+        : "memory");
+}
+// Arrival of a whole warp as one.
+__device__ __forceinline__ void warp_arrive(uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\t.reg .b64 st;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e mbarrier.arrive.shared::cta.b64 st, [%0];\n\t}" ::"r"(bar)
         : "memory");
 }
 // A value that is the same in all lanes, so that the compiler knows.
@@ -313,6 +320,8 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
             for (int i = 0; ok && i < n; ++i, r.step(pl.slots)) ok = wait(Bars::full + r.i, r.phase);
             tc::tc_fence_after();
         };
+        // steps of 16 keys in the order in which their weights come: the first quarter of each half, then the second
+        auto step_of = [](int h) { return (h & 1) + 4 * (h >> 1 & 1) + 2 * (h >> 2); };
         const uint32_t t_s = tmem + s * slot_cols;
         const uint64_t q_tile = tc::sw128_desc(smem0 + s * pl.k_atoms * kAtom);
         // scores of a block, `keys` of it, whose pieces begin at r
@@ -340,8 +349,8 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
             }
             warp_commit(bar(Bars::s_full + 2 * s + buf));
         };
-        // outputs over block i, `keys` of it, of which `first` are the prompt's
-        auto outputs = [&](int i, uint32_t buf, int keys, int first, Ring r) {
+        // outputs over block i, `keys` of it, of which `first` are the prompt's, once weights of the parity are there
+        auto outputs = [&](int i, uint32_t buf, uint32_t parity, int keys, int first, Ring r) {
             const uint32_t p = t_s + buf * kTok;
 #pragma unroll 1
             for (int c = 0; c < v_pieces; ++c, r.step(pl.slots)) {
@@ -357,16 +366,18 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
                 }
                 const uint64_t v = value_desc(values, kAtom);
                 const uint32_t id = fmt | (1u << 16) | columns(min(pl.o_cols - 128 * c, 128));
-                if (keys == kTok) {
 #pragma unroll
-                    for (int k = 0; k < kTok / 16; ++k) warp_mma_ts(d, p + 8 * k, v + k * (2048 >> 4), id, k == 0 ? i : 1);
-                } else {
-#pragma unroll 1
-                    for (int k = 0; k < keys / 16; ++k) warp_mma_ts(d, p + 8 * k, v + k * (2048 >> 4), id, i | k);
+                for (int h = 0; h < kTok / 16; ++h) {
+                    const int k = step_of(h);
+                    if (c == 0 && h == 4) {
+                        ok = ok && wait(Bars::p_full + 2 * (SB == 2 ? buf : s) + 1, parity);
+                        tc::tc_fence_after();
+                    }
+                    if (16 * k < keys) warp_mma_ts(d, p + 8 * k, v + k * (2048 >> 4), id, h == 0 ? i : 1);
                 }
                 warp_commit(bar(Bars::free + r.i));
             }
-            warp_commit(bar(Bars::pv_done + s));
+            if (SB == 2) warp_commit(bar(Bars::pv_done + s));
         };
         auto skip = [&](Ring& r, int n) {
             for (int i = 0; i < n; ++i) r.step(pl.slots);
@@ -375,10 +386,10 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
         auto leave = [&](Ring r, int n) {
             for (int i = 0; ok && i < n; ++i, r.step(pl.slots)) {
                 ok = wait(Bars::full + r.i, r.phase);
-                if (ok && lane == 0) tc::mbar_arrive(bar(Bars::free + r.i));
-                __syncwarp();
+                if (ok) warp_arrive(bar(Bars::free + r.i));
             }
         };
+        const bool plain = k_pieces == 1 && steps == 8;
         Ring kv;                                 // the next piece
         uint32_t done = 0, tiles = 0, turns = 0; // blocks, tiles and turns so far
         Unit u;
@@ -388,11 +399,49 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
             const int end = a.causal ? min(u.token + (s + 1) * pl.tile_tokens, u.len) : u.len;
             const int last_keys = (end - (mine - 1) * kTok + 15) / 16 * 16;
             ok = wait(Bars::q_full, n);
-            if (mine == 0 && lane == 0) tc::mbar_arrive(bar(Bars::q_free));
-            __syncwarp();
+            if (mine == 0) warp_arrive(bar(Bars::q_free));
 #pragma unroll 1
             for (int i = -SB; ok && i < blocks; ++i) {
+                if (TILES == 2 && plain && i == 0 && mine > 2) {
+                    // Whole blocks of 128 channels, without a question on the way: the warp's instructions come from the
+                    // cache that the softmax warps sweep, some 5 cycles each.
+                    ok = wait(Bars::o_free + s, tiles ^ 1u);
+                    uint32_t at = kv.i, phase = kv.phase;
+#pragma unroll 1
+                    for (; ok && i + 2 < mine; ++i) {
+                        const uint32_t v_at = at, v_phase = phase;
+                        if (++at == (uint32_t)pl.slots) at = 0, phase ^= 1u;
+                        const uint32_t k_at = at, k_phase = phase;
+                        if (++at == (uint32_t)pl.slots) at = 0, phase ^= 1u;
+                        ok = wait(Bars::full + v_at, v_phase) && wait(Bars::full + k_at, k_phase) && wait(Bars::turn + s, turns ^ (s ^ 1u)) &&
+                             wait(Bars::p_full + 2 * s, done + i);
+                        if (!ok) break;
+                        tc::tc_fence_after();
+                        const uint64_t v = value_desc(ring + v_at * pl.slot_bytes, kAtom), k = tc::sw128_desc(ring + k_at * pl.slot_bytes);
+                        const uint32_t id = fmt | (1u << 16) | columns(pl.o_cols);
+#pragma unroll
+                        for (int h = 0; h < 8; ++h) {
+                            if (h == 4) {
+                                ok = wait(Bars::p_full + 2 * s + 1, done + i);
+                                tc::tc_fence_after();
+                            }
+                            warp_mma_ts(t_s + o_col, t_s + 8 * step_of(h), v + step_of(h) * (2048 >> 4), id, h == 0 ? i : 1);
+                        }
+                        warp_commit(bar(Bars::free + v_at));
+#pragma unroll
+                        for (int h = 0; h < 8; ++h)
+                            warp_mma_ss(t_s, q_tile + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), k + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), fmt | columns(kTok), h != 0);
+                        warp_commit(bar(Bars::free + k_at));
+                        warp_commit(bar(Bars::s_full + 2 * s));
+                        warp_arrive(bar(Bars::turn + (s ^ 1)));
+                        ++turns;
+                    }
+                    kv.i = at;
+                    kv.phase = phase;
+                    if (!ok) break;
+                }
                 const uint32_t buf = SB == 2 ? (done + (i & 1)) & 1u : 0u;
+                const uint32_t parity = SB == 2 ? (done + i) >> 1 : done + i;
                 const bool out = i >= 0 && i < mine, in = i + SB < mine;
                 Ring keys_at = kv;
                 if (i >= 0) skip(keys_at, v_pieces);
@@ -400,7 +449,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
                 if (out) arrived(kv, v_pieces);
                 if (ok && in) arrived(keys_at, k_pieces);
                 if (ok && out) {
-                    ok = wait(Bars::p_full + 2 * s + buf, SB == 2 ? (done + i) >> 1 : done + i) && (i > 0 || wait(Bars::o_free + s, tiles ^ 1u));
+                    ok = (i > 0 || wait(Bars::o_free + s, tiles ^ 1u)) && wait(Bars::p_full + 2 * (SB == 2 ? buf : s), parity);
                 }
                 // The two tiles take turns: the softmax of one has the time of the other's MMAs.  (Without, the two ran in
                 // step, both softmaxes and then both tiles' MMAs: 5200 cycles a block instead of 2700.)
@@ -408,7 +457,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
                 if (!ok) break;
                 tc::tc_fence_after();
                 if (out) {
-                    outputs(i, buf, i == mine - 1 ? last_keys : kTok, u.len - i * kTok, kv);
+                    outputs(i, buf, parity, i == mine - 1 ? last_keys : kTok, u.len - i * kTok, kv);
                     if (i == mine - 1) warp_commit(bar(Bars::o_full + s));
                 }
                 if (in) {
@@ -416,8 +465,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
                     if (i + SB == mine - 1) warp_commit(bar(Bars::q_free));
                 }
                 if (TILES == 2 && i >= 0) {
-                    if (lane == 0) tc::mbar_arrive(bar(Bars::turn + (s ^ 1)));
-                    __syncwarp();
+                    warp_arrive(bar(Bars::turn + (s ^ 1)));
                     ++turns;
                 }
                 if (i >= 0) {
@@ -493,7 +541,28 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
 #pragma unroll
                 for (int k = 0; k < 32; ++k) tops[k & 7] = k < 8 ? fmaxf(x[k].x, x[k].y) : fmaxf(fmaxf(tops[k & 7], x[k].x), x[k].y);
                 const float best = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
-                // (behind this both have read their scores, and weights may go over them)
+                float2 sums[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+                uint32_t w[16];
+                // weights of a quarter of the block's keys
+                auto weigh = [&](int h) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        float2 y = fma2(x[16 * h + k], make_float2(factor, factor), make_float2(-m, -m));
+                        y = make_float2(ex2(y.x), ex2(y.y));
+                        sums[k & 1] = fma2(y, make_float2(1.0f, 1.0f), sums[k & 1]);
+                        w[k] = BF16 ? pack_bf16(y.x, y.y) : pack2(y.x, y.y);
+                    }
+                };
+                auto leave = [&](int h) {
+                    tmem_st16(t_b + 32 * half + 16 * h, w);
+                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                    tc::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(bar(Bars::p_full + 2 * (SB == 2 ? buf : s) + h));
+                };
+                // (the first quarter as if m stays, which it mostly does: the two warps are not asked before it)
+                weigh(0);
+                // Behind this both have read their scores, and weights may go over them.
                 if (either(!ok || fmaf(best, factor, -m) > kMost)) {
                     *mine_at = best;
                     if (either(!ok)) {
@@ -508,9 +577,11 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
                     // scores whose products are off by their rounding: the row is done again
                     if (over && !(fabsf(fmaf(both, factor, -m) - kBegin) <= 4.0f)) l = NAN;
                     if (i != 0) {
-                        // the MMAs that wrote O have to be complete
-                        ok = wait(Bars::pv_done + s, done ^ 1u);
-                        tc::tc_fence_after();
+                        // the MMAs that wrote O have to be complete: with one buffer they came before those of these scores
+                        if (SB == 2) {
+                            ok = wait(Bars::pv_done + s, done ^ 1u);
+                            tc::tc_fence_after();
+                        }
 #pragma unroll 1
                         for (int c = c_first; c < c_end; c += 16) {
                             uint32_t v[16];
@@ -520,25 +591,13 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
                             tmem_st16v(t_s + o_col + c, v);
                         }
                     }
+                    sums[0] = sums[1] = make_float2(0.0f, 0.0f);
+                    weigh(0);
                 }
-                float2 sums[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t w[16];
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        float2 y = fma2(x[16 * h + k], make_float2(factor, factor), make_float2(-m, -m));
-                        y = make_float2(ex2(y.x), ex2(y.y));
-                        sums[k & 1] = fma2(y, make_float2(1.0f, 1.0f), sums[k & 1]);
-                        w[k] = BF16 ? pack_bf16(y.x, y.y) : pack2(y.x, y.y);
-                    }
-                    tmem_st16(t_b + 32 * half + 16 * h, w);
-                }
+                leave(0);
+                weigh(1);
+                leave(1);
                 l += sums[0].x + sums[0].y + sums[1].x + sums[1].y;
-                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                tc::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(bar(Bars::p_full + 2 * s + buf));
             }
             // ---- outputs, half of the columns each ----
             ok = ok && wait(Bars::o_full + s, tiles);
