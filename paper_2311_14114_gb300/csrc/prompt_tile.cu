@@ -50,6 +50,7 @@ struct PromptPlan {
     int o_cols;              // Dv rounded up to whole MMA columns
     int slots, slot_bytes;   // of the ring of pieces
     int ring_off, misc_off, smem;
+    int wide_rows;           // output rows are whole 32-byte pieces
 };
 
 struct PromptMaps {
@@ -126,6 +127,14 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar) {
         "@e mbarrier.arrive.shared::cta.b64 st, [%0];\n\t}" ::"r"(bar)
         : "memory");
 }
+// Rounded to the type, values beyond its range to its largest.
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack_finite(float lo, float hi) {
+    uint32_t r;
+    if constexpr (BF16) asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
 // A value that is the same in all lanes, so that the compiler knows.
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -176,7 +185,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
     __syncthreads();
     tc::tc_fence_after();
     const uint32_t tmem = uniform(*tmem_at);
-    // (most waits are over when they begin: one look at those costs 20 cycles, the loop 160)
+    // (one look at a wait that is over costs 20 cycles, the loop 160)
     auto wait = [&](int i, uint32_t parity) {
         return __all_sync(0xffffffffu, tc::mbar_try_wait(bar(i), parity & 1u)) || wait_warp(bar(i), parity & 1u, abort_flag, a.err);
     };
@@ -561,9 +570,9 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
                     if (lane == 0) tc::mbar_arrive(bar(Bars::p_full + 2 * (SB == 2 ? buf : s) + h));
                 };
                 // (the first quarter as if m stays, which it mostly does: the two warps are not asked before it)
-                weigh(0);
+                if (i != 0) weigh(0);
                 // Behind this both have read their scores, and weights may go over them.
-                if (either(!ok || fmaf(best, factor, -m) > kMost)) {
+                if (i == 0 || either(!ok || fmaf(best, factor, -m) > kMost)) {
                     *mine_at = best;
                     if (either(!ok)) {
                         ok = false;
@@ -605,31 +614,38 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
             if (either(!ok)) break;
             tc::tc_fence_after();
             const float inv = 1.0f / (half ? *other_at + l : l + *other_at);
-            float odd = 0.0f;              // NaN once an output is not finite
-            const int64_t out_row = (int64_t)(u.start + token) * heads + u.kv_head * a.group + head;
-            uint16_t* out = a.out + out_row * a.Dv;
-            constexpr float top = BF16 ? 3.3895313892515355e38f : 65504.0f;
+            uint16_t* out = a.out + ((int64_t)(u.start + token) * heads + u.kv_head * a.group + head) * a.Dv;
+            // (Rows of their own are 32 of them to an instruction, 32 bytes each.  Four lanes that first exchange pieces, to
+            // write 64 bytes of a row together, halve what the memory pipe does but take 300 instructions instead of 120, in
+            // all warps at about the same time.)
+            float2 odd2 = make_float2(0.0f, 0.0f);
 #pragma unroll 1
             for (int c = c_first; c < c_end; c += 16) {
                 uint32_t v[16], w[8];
                 tc::tmem_ld16(t_s + o_col + c, v);
 #pragma unroll
                 for (int k = 0; k < 16; k += 2) {
-                    const float y0 = __uint_as_float(v[k]) * inv, y1 = __uint_as_float(v[k + 1]) * inv;
-                    odd = fmaf(y0, 0.0f, fmaf(y1, 0.0f, odd));
+                    const float2 y = mul2(make_float2(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), make_float2(inv, inv));
+                    odd2 = fma2(y, make_float2(0.0f, 0.0f), odd2);
                     // (an average of values of the type is not beyond it, though rounded weights may say so)
-                    const float z0 = fminf(fmaxf(y0, -top), top), z1 = fminf(fmaxf(y1, -top), top);
-                    w[k / 2] = BF16 ? pack_bf16(z0, z1) : pack2(z0, z1);
+                    w[k / 2] = pack_finite<BF16>(y.x, y.y);
                 }
                 if (live) {
-                    *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
-                    if (c + 8 < a.Dv) *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                    if (pl.wide_rows) {
+                        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + c), "r"(w[0]), "r"(w[1]),
+                                     "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                                     : "memory");
+                    } else {
+                        *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
+                        if (c + 8 < a.Dv) *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                    }
                 }
             }
             tc::tc_fence_before();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(bar(Bars::o_free + s));
             ++tiles;
+            const float odd = odd2.x + odd2.y;      // NaN where an output is not finite
             // rows to be done again, behind both halves' stores
             if (either(live && odd != 0.0f)) {
                 *mine_at = odd;
@@ -695,6 +711,7 @@ bool make_plan(const PromptArgs& a, int tiles, PromptPlan* p) {
     p->k_atoms = (a.D + 63) / 64;
     p->v_atoms = (a.Dv + 63) / 64;
     p->o_cols = (a.Dv + 15) / 16 * 16;
+    p->wide_rows = a.Dv % 16 == 0 && (uintptr_t)a.out % 32 == 0;
     if ((3 - tiles) * kTok + p->o_cols > 512 / tiles) return false;
     p->slot_bytes = (p->k_atoms > 1 || p->v_atoms > 1 ? 2 : 1) * kAtom;
     p->ring_off = tiles * p->k_atoms * kAtom;
