@@ -28,6 +28,8 @@
 // the definition, by prompt_row.  So the blocks need no look at what is hidden;
 // only what stands behind a prompt, where a buffer's padding may hold anything, is
 // cleared in its last block.
+#include <atomic>
+
 #include "kv_flights.h"
 #include "prompt_rows.cuh"
 #include "soniq_device.cuh"
@@ -145,7 +147,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 
 template <bool BF16, int TILES>
 __global__ void __launch_bounds__(128 + 256 * TILES, 1)
-    prompt_tile_kernel(const PromptArgs a, const PromptPlan pl, const __grid_constant__ PromptMaps maps, unsigned* counters, const int drop) {
+    prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ PromptPlan pl, const __grid_constant__ PromptMaps maps, unsigned* counters, const int drop) {
     extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
     const uint32_t smem0 = tc::smem_u32(smem), ring = smem0 + pl.ring_off, bars = smem0 + pl.misc_off;
@@ -539,11 +541,16 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
 #pragma unroll
                 for (int k = 0; k < 32; ++k) x[k] = make_float2(__uint_as_float(raw[2 * k]), __uint_as_float(raw[2 * k + 1]));
                 if ((i + 1) * kTok > sure) {
+                    // (by sixteen keys, most of which all rows of the warp see)
                     const int upto = end - i * kTok - 64 * half;
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        if (2 * k >= upto) x[k].x = -INFINITY;
-                        if (2 * k + 1 >= upto) x[k].y = -INFINITY;
+                    for (int k = 0; k < 32; k += 8) {
+                        if (i * kTok + 64 * half + 2 * k + 16 <= sure) continue;
+#pragma unroll
+                        for (int e = k; e < k + 8; ++e) {
+                            if (2 * e >= upto) x[e].x = -INFINITY;
+                            if (2 * e + 1 >= upto) x[e].y = -INFINITY;
+                        }
                     }
                 }
                 float tops[8];
@@ -704,6 +711,20 @@ bool mapped(const PromptSide& x, int64_t n, int heads, bool shared_heads) {
            (heads == 1 || (x.head == 0 ? shared_heads : x.head > 0 && x.head % 8 == 0 && x.head < far / 2));
 }
 
+// Asks for all of the shared memory, once per device and kernel (`which`).
+cudaError_t prepared(const void* kernel, int which) {
+    static std::atomic<uint32_t> done[64];
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const bool known = device >= 0 && device < 64;
+    if (known && (done[device].load(std::memory_order_relaxed) >> which & 1u) != 0) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+    if (e == cudaSuccess) e = prefer_max_shared(kernel);
+    if (e == cudaSuccess && known) done[device].fetch_or(1u << which, std::memory_order_relaxed);
+    return e;
+}
+
 bool make_plan(const PromptArgs& a, int tiles, PromptPlan* p) {
     p->row_heads = a.group < 128 ? a.group : 128;
     p->tile_tokens = 128 / p->row_heads;
@@ -747,8 +768,7 @@ cudaError_t launch_prompt_tile(const PromptArgs& a, bool bf16, unsigned* counter
     const int grid = (int)(units < num_sms() ? units : num_sms());
     auto* kernel = tiles == 2 ? (bf16 ? prompt_tile_kernel<true, 2> : prompt_tile_kernel<false, 2>)
                               : (bf16 ? prompt_tile_kernel<true, 1> : prompt_tile_kernel<false, 1>);
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
-    if (e == cudaSuccess) e = prefer_max_shared(reinterpret_cast<const void*>(kernel));
+    const cudaError_t e = prepared(reinterpret_cast<const void*>(kernel), 2 * (tiles - 1) + bf16);
     if (e != cudaSuccess) return e;
     kernel<<<grid, 128 + 256 * tiles, p.smem, st>>>(a, p, maps, counters, take_drop_arrival() ? 1 : 0);
     note_launch();

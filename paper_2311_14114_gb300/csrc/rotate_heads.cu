@@ -11,8 +11,8 @@
 // that a float product of a million positions has.  Its upper half goes to
 // sincospi.
 //
-// A warp takes a token, or a share of its heads; each lane keeps the cosines and
-// sines of its eight channels for all of the token's heads.  Rows are read and
+// A warp takes a token, or a share of its heads; its lanes work out the token's
+// cosines and sines, and each keeps those of its eight channels for all heads.  Rows are read and
 // written in 16-byte pieces, two rows of 128 channels to a warp; in the half
 // layout partners stand in lanes a fixed distance apart and come by shuffles.
 // Rows that are no 16-byte pieces, or whose partners are not whole pieces apart,
@@ -20,6 +20,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include "soniq_device.cuh"
 #include "step_internal.h"
 
 namespace soniq {
@@ -53,130 +54,134 @@ __device__ __forceinline__ float2 turn(const RotateArgs& a, int position, int pa
     return make_float2(c * a.magnitude, s * a.magnitude);
 }
 
-// Divides a row, N of whose channels each of its LANES lanes holds, by its root
-// mean square.  Where the squares' sum leaves fp32 (above; or below, with no eps
-// to speak of) the row is brought to about 1 first.
+// 1 / the root mean square of a row, of which each of its LANES lanes holds N pairs
+// of channels.  Where the squares' sum leaves fp32 (above; or below, with no eps to
+// speak of) it is that of the row times *up, a power of two.
 template <int LANES, int N>
-__device__ __forceinline__ void normalise(float (&x)[N], const RotateArgs& a) {
-    auto squares = [&]() {
-        float sum = 0.0f;
+__device__ __forceinline__ float norm_factor(const float2 (&x)[N], const RotateArgs& a, float* up) {
+    auto squares = [&](float by) {
+        float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
-        for (int k = 0; k < N; ++k) sum = fmaf(x[k], x[k], sum);
+        for (int k = 0; k < N; ++k) {
+            const float2 y = by == 1.0f ? x[k] : mul2(x[k], make_float2(by, by));
+            sum = fma2(y, y, sum);
+        }
+        float all = sum.x + sum.y;
 #pragma unroll
-        for (int d = LANES / 2; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        return sum;
+        for (int d = LANES / 2; d; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
+        return all;
     };
-    const float sum = squares(), mean = sum / (float)a.D + a.eps;
+    const float sum = squares(1.0f), mean = fmaf(sum, 1.0f / (float)a.D, a.eps);
     float f = rsqrtf(mean);
     const bool out = !(sum <= 1e37f && mean >= 1e-30f);
     if (__any_sync(0xffffffffu, out)) {
         float most = 0.0f;
 #pragma unroll
-        for (int k = 0; k < N; ++k) most = fmaxf(most, fabsf(x[k]));
+        for (int k = 0; k < N; ++k) most = fmaxf(most, fmaxf(fabsf(x[k].x), fabsf(x[k].y)));
 #pragma unroll
         for (int d = LANES / 2; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-        // a power of two, 2^100 at most so that eps stays in range with it; none for rows of zeros or infinities
+        // to about 1; 2^100 at most so that eps stays in range with it; none for rows of zeros or infinities
         const int e = out && most > 0.0f && most < INFINITY ? min(127 - (int)(__float_as_uint(most) >> 23), 100) : 0;
-        const float up = __uint_as_float((uint32_t)(max(e, -126) + 127) << 23);
-#pragma unroll
-        for (int k = 0; k < N; ++k) x[k] *= up;
-        const float better = rsqrtf(squares() / (float)a.D + a.eps * up * up);
+        *up = __uint_as_float((uint32_t)(max(e, -126) + 127) << 23);
+        const float better = rsqrtf(fmaf(squares(*up), 1.0f / (float)a.D, a.eps * *up * *up));
         if (e != 0) f = better;
     }
-#pragma unroll
-    for (int k = 0; k < N; ++k) x[k] *= f;
+    return f;
 }
 
-// LANES: lanes of a row, eight channels each.
+// LANES: lanes of a row, eight channels each.  A row's factor f comes last: with
+// the gains in the cosines and sines, out = f (x A + y B) for a channel x and its
+// partner y.
 template <bool BF16, int LANES>
-__global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a, const int parts) {
+__global__ void __launch_bounds__(kThreads, 3) rotate_kernel(const __grid_constant__ RotateArgs a, const int parts) {
     constexpr int ROWS = 32 / LANES, STEPS = 4;
     const int lane = threadIdx.x & 31, sub = lane / LANES, l = lane % LANES;
     const int64_t task = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     const int64_t token = task / parts;
-    const int part = (int)(task % parts);
+    const int part = (int)(task - token * parts);
     if (token >= a.n) return;
     const int c0 = 8 * l, half = a.channels / 2;
     const bool in_row = c0 < a.D;
-    // ---- this lane's cosines and sines: pairs (c, c + half), or neighbours ----
-    float cs[8], sn[8];
-    int partner = 0;
+    // `parts` warps share a token's groups of rows
+    auto first_of = [&](const RotateSide& side, int p) { return (int)((int64_t)((side.heads + ROWS - 1) / ROWS) * p / parts); };
+    uint4 raw[STEPS];
+    auto load = [&](const RotateSide& side, int g, int g1) {
+        const uint16_t* in = side.in + token * side.in_token + c0;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const int h = (g + i) * ROWS + sub;
+            raw[i] = make_uint4(0, 0, 0, 0);
+            if (g + i < g1 && h < side.heads && in_row) raw[i] = *reinterpret_cast<const uint4*>(in + h * side.in_head);
+        }
+    };
+    const int s0 = first_of(a.side[0], part) < first_of(a.side[0], part + 1) ? 0 : 1;
+    load(a.side[s0], first_of(a.side[s0], part), first_of(a.side[s0], part + 1));     // on its way while angles are worked out
+    // ---- the token's cosines and sines, a pair to a lane ----
+    __shared__ float2 turns[kThreads / 32][128];
+    float2* mine = turns[threadIdx.x >> 5];
     if (half > 0) {
         const int position = a.positions[token];
-        if (a.interleaved) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 t = turn(a, position, c0 / 2 + i);
-                cs[2 * i] = cs[2 * i + 1] = t.x;
-                sn[2 * i] = -t.y;
-                sn[2 * i + 1] = t.y;
-            }
-        } else {
-            partner = c0 < half ? half / 8 : (c0 < a.channels ? -half / 8 : 0);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float2 t = turn(a, position, c0 < half ? c0 + i : (c0 < a.channels ? c0 - half + i : half));
-                cs[i] = t.x;
-                sn[i] = c0 < half ? -t.y : t.y;
-            }
-        }
-    }
-    const int from = sub * LANES + l + partner, turned = a.channels - c0;      // of this lane's channels, the first `turned`
-    // ---- the heads: queries, then keys; `parts` warps share a token's groups of rows ----
 #pragma unroll 1
-    for (int s = 0; s < 2; ++s) {
+        for (int p = lane; p < half; p += 32) mine[p] = turn(a, position, p);
+        __syncwarp();
+    }
+    // Pairs are (c, c + half), or neighbours.  The partner's words of channels that are not turned do not count (0 times an
+    // infinity is not 0).
+    uint32_t turned[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) turned[i] = c0 + 2 * i < a.channels ? 0xffffffffu : 0u;
+    const int partner = a.interleaved || c0 >= a.channels ? 0 : (c0 < half ? half / 8 : -half / 8);
+    const int from = sub * LANES + l + partner;
+    // ---- the heads: queries, then keys ----
+#pragma unroll 1
+    for (int s = s0; s < 2; ++s) {
         const RotateSide& side = a.side[s];
-        const int groups = (side.heads + ROWS - 1) / ROWS;
-        const int g0 = (int)((int64_t)groups * part / parts), g1 = (int)((int64_t)groups * (part + 1) / parts);
+        const int g0 = first_of(side, part), g1 = first_of(side, part + 1);
         if (g0 == g1) continue;
-        const uint16_t* in = side.in + token * side.in_token + c0;
-        uint16_t* out = side.out + token * side.out_token + c0;
+        if (s != s0) load(side, g0, g1);
         const bool norm = side.gain != nullptr;
-        float gain[8] = {};
-        if (norm && in_row) {
-            const float4 x = *reinterpret_cast<const float4*>(side.gain + c0), y = *reinterpret_cast<const float4*>(side.gain + c0 + 4);
-            gain[0] = x.x, gain[1] = x.y, gain[2] = x.z, gain[3] = x.w;
-            gain[4] = y.x, gain[5] = y.y, gain[6] = y.z, gain[7] = y.w;
+        float2 A[4], B[4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = c0 + i, other = a.interleaved ? c ^ 1 : c + 8 * partner;
+            const bool gains = norm && in_row, second = a.interleaved ? (c & 1) != 0 : c >= half;
+            const float2 t = c < a.channels ? mine[a.interleaved ? c / 2 : (second ? c - half : c)] : make_float2(1.0f, 0.0f);
+            const float own = t.x * (gains ? side.gain[c] : 1.0f);
+            const float with = (second ? t.y : -t.y) * (gains && turned[i / 2] != 0 ? side.gain[other] : 1.0f);
+            if (i & 1) A[i / 2].y = own, B[i / 2].y = with;
+            else A[i / 2].x = own, B[i / 2].x = with;
         }
+        uint16_t* out = side.out + token * side.out_token + c0;
 #pragma unroll 1
         for (int g = g0; g < g1; g += STEPS) {
-            uint4 raw[STEPS];
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                const int h = (g + i) * ROWS + sub;
-                raw[i] = make_uint4(0, 0, 0, 0);
-                if (g + i < g1 && h < side.heads && in_row) raw[i] = *reinterpret_cast<const uint4*>(in + h * side.in_head);
-            }
+            if (g != g0) load(side, g, g1);
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
                 if (g + i >= g1) break;
                 const int h = (g + i) * ROWS + sub;
-                float x[8];
                 const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+                float2 x[4], y[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const float2 v = load2<BF16>(w[k]);
-                    x[2 * k] = v.x;
-                    x[2 * k + 1] = v.y;
+                    x[k] = load2<BF16>(w[k]);
+                    y[k] = load2<BF16>((a.interleaved ? __byte_perm(w[k], 0, 0x1032) : __shfl_sync(0xffffffffu, w[k], from)) & turned[k]);
                 }
-                if (norm) {
-                    normalise<LANES>(x, a);
+                float f = 1.0f, up = 1.0f;
+                if (norm) f = norm_factor<LANES>(x, a, &up);
+                if (up != 1.0f) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) x[k] *= gain[k];
+                    for (int k = 0; k < 4; ++k) {
+                        x[k] = mul2(x[k], make_float2(up, up));
+                        y[k] = mul2(y[k], make_float2(up, up));
+                    }
                 }
-                if (half > 0) {
-                    float y[8];
+                uint32_t z[4];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) y[k] = a.interleaved ? x[k ^ 1] : __shfl_sync(0xffffffffu, x[k], from);
-                    // (a channel that is not turned has no partner: 0 times an infinity would not be 0)
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) y[k] = k < turned ? y[k] : 0.0f;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) x[k] = fmaf(y[k], sn[k], x[k] * cs[k]);
+                for (int k = 0; k < 4; ++k) {
+                    const float2 v = mul2(fma2(y[k], B[k], mul2(x[k], A[k])), make_float2(f, f));
+                    z[k] = round2<BF16>(v.x, v.y);
                 }
-                if (h < side.heads && in_row)
-                    *reinterpret_cast<uint4*>(out + h * side.out_head) =
-                        make_uint4(round2<BF16>(x[0], x[1]), round2<BF16>(x[2], x[3]), round2<BF16>(x[4], x[5]), round2<BF16>(x[6], x[7]));
+                if (h < side.heads && in_row) *reinterpret_cast<uint4*>(out + h * side.out_head) = make_uint4(z[0], z[1], z[2], z[3]);
             }
         }
     }
@@ -184,7 +189,7 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a, co
 
 // A channel to a lane, eight times: any D, channels and strides.
 template <bool BF16>
-__global__ void __launch_bounds__(kThreads) rotate_scalar_kernel(const RotateArgs a, const int parts) {
+__global__ void __launch_bounds__(kThreads) rotate_scalar_kernel(const __grid_constant__ RotateArgs a, const int parts) {
     const int lane = threadIdx.x & 31;
     const int64_t task = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     const int64_t token = task / parts;
@@ -214,37 +219,29 @@ __global__ void __launch_bounds__(kThreads) rotate_scalar_kernel(const RotateArg
         for (int h = h0; h < h1; ++h) {
             const uint16_t* in = side.in + token * side.in_token + h * side.in_head;
             uint16_t* out = side.out + token * side.out_token + h * side.out_head;
-            float x[8], y[8];
+            float2 x[4], y[4];
+            auto at = [](float2 (&v)[4], int i) -> float& { return i & 1 ? v[i / 2].y : v[i / 2].x; };
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int c = lane + 32 * i;
-                x[i] = c < a.D ? value(in[c]) : 0.0f;
-                y[i] = partner[i] >= 0 ? value(in[partner[i]]) : 0.0f;
+                at(x, i) = c < a.D ? value(in[c]) : 0.0f;
+                at(y, i) = partner[i] >= 0 ? value(in[partner[i]]) : 0.0f;
             }
             __syncwarp();       // the whole row is read before any of it is written: out may be in
             if (side.gain != nullptr) {
-                normalise<32>(x, a);
+                float up = 1.0f;
+                const float f = norm_factor<32>(x, a, &up);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int c = lane + 32 * i;
-                    x[i] = c < a.D ? x[i] * side.gain[c] : 0.0f;
-                }
-                // the lane that holds the partner has its value now
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float p = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float v = __shfl_sync(0xffffffffu, x[j], partner[i] & 31);
-                        if (partner[i] >> 5 == j) p = v;
-                    }
-                    y[i] = p;
+                    at(x, i) = c < a.D ? at(x, i) * up * f * side.gain[c] : 0.0f;
+                    at(y, i) = partner[i] >= 0 ? at(y, i) * up * f * side.gain[partner[i]] : 0.0f;
                 }
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int c = lane + 32 * i;
-                if (c < a.D) out[c] = (uint16_t)round2<BF16>(fmaf(y[i], sn[i], x[i] * cs[i]), 0.0f);
+                if (c < a.D) out[c] = (uint16_t)round2<BF16>(fmaf(at(y, i), sn[i], at(x, i) * cs[i]), 0.0f);
             }
             __syncwarp();
         }

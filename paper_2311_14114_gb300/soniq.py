@@ -600,13 +600,14 @@ def kv_attend(cache: KVCache, q: torch.Tensor, page_table: torch.Tensor, lengths
     return out
 
 
-def _need_here(t: torch.Tensor, dtype, shape: Optional[tuple], name: str):
-    """A contiguous tensor on the current device, whose streams the library launches on."""
-    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
-        of = "" if shape is None else f" {list(shape)}"
-        raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor{of}")
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} is not on the current CUDA device")
+# The current device without torch's initialisation checks (0.1 us instead of 0.3; a small call takes 15).
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _need_here(t: torch.Tensor, dtype, n: int, here: int, name: str):
+    """n contiguous elements on the current device (`here`), whose streams the library launches on."""
+    if t.get_device() != here or t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be {n} contiguous {dtype} elements on the current CUDA device")
 
 
 class KVPages:
@@ -638,30 +639,28 @@ def kv_plan(pages: KVPages, lengths: torch.Tensor, targets: torch.Tensor, max_to
     pages.table and pages.free are updated, and pages.count, unless count_out (int32)
     is to get the pool's new size.  max_tokens: rows of the step's buffers, at least
     its tokens (those of sequences beyond it are not served)."""
-    B, dev = lengths.numel(), lengths.device
-    _need_here(lengths, torch.int32, (B,), "lengths")
-    _need_here(targets, torch.int32, (B,), "targets")
-    table = pages.table
-    if table.shape[0] < B:
+    B, here = lengths.numel(), _device() if lengths.is_cuda else -2
+    i32, table, max_tokens = torch.int32, pages.table, int(max_tokens)
+    rows, width = table.shape
+    if rows < B:
         raise ValueError("pages.table has fewer rows than there are sequences")
-    _need_here(table, torch.int32, None, "pages.table")
-    _need_here(pages.free, torch.int32, (pages.n_pages,), "pages.free")
-    _need_here(pages.count, torch.int32, (2,), "pages.count")
+    _need_here(lengths, i32, B, here, "lengths")
+    _need_here(targets, i32, B, here, "targets")
+    _need_here(table, i32, rows * width, here, "pages.table")
+    _need_here(pages.free, i32, pages.n_pages, here, "pages.free")
+    _need_here(pages.count, i32, 2, here, "pages.count")
     if count_out is None:
         count_out = pages.count
-    elif count_out.numel() < 1:
-        raise ValueError("count_out must hold a number")
-    else:
-        _need_here(count_out, torch.int32, None, "count_out")
-    max_tokens = int(max_tokens)
+    elif count_out.numel() < 1 or count_out.dtype is not i32 or count_out.get_device() != here:
+        raise ValueError("count_out must be an int32 tensor on the current CUDA device")
     if out is None:
-        out = KVStep(_new((B + 1,), torch.int32, dev, stream), _new((max(max_tokens, 0),), torch.int32, dev, stream),
-                     _new((max(max_tokens, 0),), torch.int64, dev, stream), _new((B,), torch.int32, dev, stream))
+        dev, cap = lengths.device, max(max_tokens, 0)
+        out = KVStep(_new((B + 1,), i32, dev, stream), _new((cap,), i32, dev, stream), _new((cap,), torch.int64, dev, stream),
+                     _new((B,), i32, dev, stream))
     else:
-        for t, dtype, n, name in zip(out, (torch.int32, torch.int32, torch.int64, torch.int32),
-                                     (B + 1, max_tokens, max_tokens, B), KVStep._fields):
-            _need_here(t, dtype, (n,), "out." + name)
-    _check(lib().soniq_kv_plan(pages.page_size, pages.n_pages, table.data_ptr(), table.stride(0), table.shape[1],
+        for t, dtype, n, name in zip(out, (i32, i32, torch.int64, i32), (B + 1, max_tokens, max_tokens, B), KVStep._fields):
+            _need_here(t, dtype, n, here, "out." + name)
+    _check(lib().soniq_kv_plan(pages.page_size, pages.n_pages, table.data_ptr(), width, width,
                                pages.free.data_ptr(), pages.count.data_ptr(), count_out.data_ptr(), lengths.data_ptr(),
                                targets.data_ptr(), B, max_tokens, out.starts.data_ptr(), out.positions.data_ptr(),
                                out.slots.data_ptr(), out.lengths.data_ptr(), _stream(stream)), "soniq_kv_plan")
@@ -716,19 +715,23 @@ class Rotary:
 _TWO_PI = Fraction("6.283185307179586476925286766559005768394338798750211641949889")
 
 
-def _heads(x: torch.Tensor, n: int, D: int, dtype, gain: Optional[torch.Tensor], out: Optional[torch.Tensor], name: str, stream):
-    if not x.is_cuda or x.dtype != dtype or x.dim() != 3 or x.shape[0] != n or x.shape[2] != D or \
-            (x.stride(2) != 1 and D > 1) or x.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} must be a {dtype} tensor [{n}][heads][{D}] with contiguous channels on the current CUDA device")
-    if out is None:
-        out = _new(x.shape, dtype, x.device, stream)
-    elif not out.is_cuda or out.dtype != dtype or out.shape != x.shape or (out.stride(2) != 1 and D > 1) or \
-            out.get_device() != x.get_device():
-        raise ValueError(f"{name}_out must be a tensor like {name} with contiguous channels")
+def _heads(x: torch.Tensor, n: int, D: int, dtype, gain: Optional[torch.Tensor], out: Optional[torch.Tensor], here: int,
+           name: str, stream):
+    if x.dim() != 3 or x.get_device() != here or x.dtype is not dtype:
+        raise ValueError(f"{name} must be a {dtype} tensor [{n}][heads][{D}] on the current CUDA device")
+    shape, stride = x.shape, x.stride()
+    if shape[0] != n or shape[2] != D or (stride[2] != 1 and D > 1):
+        raise ValueError(f"{name} must be [{n}][heads][{D}] with contiguous channels")
     if gain is not None:
-        _need_here(gain, torch.float32, (D,), name + "_gain")
-    sx, so = x.stride(), out.stride()
-    return out, CHeads(x.shape[1], x.data_ptr(), sx[0], sx[1], out.data_ptr(), so[0], so[1], _ptr(gain))
+        _need_here(gain, torch.float32, D, here, name + "_gain")
+    if out is None:
+        out = _new(shape, dtype, x.device, stream)
+        to = (shape[1] * D, D)
+    else:
+        to = out.stride()
+        if out.dtype is not dtype or out.shape != shape or (to[2] != 1 and D > 1) or out.get_device() != here:
+            raise ValueError(f"{name}_out must be a tensor like {name} with contiguous channels")
+    return out, CHeads(shape[1], x.data_ptr(), stride[0], stride[1], out.data_ptr(), to[0], to[1], _ptr(gain))
 
 
 def rotate_heads(rotary: Optional[Rotary], q: Optional[torch.Tensor], k: Optional[torch.Tensor],
@@ -742,24 +745,23 @@ def rotate_heads(rotary: Optional[Rotary], q: Optional[torch.Tensor], k: Optiona
     some = q if q is not None else k
     if some is None:
         return None, None
-    if some.dim() != 3 or some.dtype not in (torch.float16, torch.bfloat16):
+    dtype, here = some.dtype, _device() if some.is_cuda else -2
+    if some.dim() != 3 or (dtype is not torch.float16 and dtype is not torch.bfloat16):
         raise ValueError("q and k must be float16 or bfloat16 tensors [n][heads][D]")
     n, _, D = some.shape
     if rotary is not None and rotary.channels > 0:
         if positions is None:
             raise ValueError("positions are needed to turn by")
-        _need_here(positions, torch.int32, (n,), "positions")
+        _need_here(positions, torch.int32, n, here, "positions")
     cq = ck = None
     if q is not None:
-        q_out, cq = _heads(q, n, D, some.dtype, q_gain, q_out, "q", stream)
+        q_out, cq = _heads(q, n, D, dtype, q_gain, q_out, here, "q", stream)
     if k is not None:
-        k_out, ck = _heads(k, n, D, some.dtype, k_gain, k_out, "k", stream)
-    _check(lib().soniq_rotate_heads(rotary.ref if rotary is not None else None, _ptr(positions), n, D,
-                                    OUT_BF16 if some.dtype == torch.bfloat16 else OUT_F16,
-                                    ctypes.byref(cq) if cq is not None else None,
-                                    ctypes.byref(ck) if ck is not None else None, float(eps), _stream(stream)),
-           "soniq_rotate_heads")
-    return (q_out if q is not None else None), (k_out if k is not None else None)
+        k_out, ck = _heads(k, n, D, dtype, k_gain, k_out, here, "k", stream)
+    _check(lib().soniq_rotate_heads(None if rotary is None else rotary.ref, _ptr(positions), n, D,
+                                    OUT_BF16 if dtype is torch.bfloat16 else OUT_F16, None if cq is None else ctypes.byref(cq),
+                                    None if ck is None else ctypes.byref(ck), eps, _stream(stream)), "soniq_rotate_heads")
+    return (None if q is None else q_out), (None if k is None else k_out)
 
 
 def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, causal: bool = True,
@@ -768,29 +770,30 @@ def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: tor
     k [n][heads][D], v [n][heads][Dv] (any token and head strides); sequence b is
     tokens starts[b] .. starts[b + 1] - 1 (int32 [B + 1]).  scale: 1 / sqrt(D) if left
     out.  Returns out [n][q_heads][Dv], whose rows of no sequence are left as they were."""
-    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3 or q.dtype not in (torch.float16, torch.bfloat16):
+    dtype, here = q.dtype, _device() if q.is_cuda else -2
+    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3 or (dtype is not torch.float16 and dtype is not torch.bfloat16):
         raise ValueError("q, k and v must be float16 or bfloat16 tensors [n][heads][channels]")
-    (n, Hq, D), (_, Hk, Dv) = q.shape, v.shape
-    here = torch.cuda.current_device() if q.is_cuda else -1
-    for t, shape, name in ((q, (n, Hq, D), "q"), (k, (n, Hk, D), "k"), (v, (n, Hk, Dv), "v")):
-        if not t.is_cuda or t.dtype != q.dtype or tuple(t.shape) != shape or (t.stride(2) != 1 and shape[2] > 1) or \
-                t.get_device() != here:
-            raise ValueError(f"{name} must be a {q.dtype} tensor {list(shape)} with contiguous channels on the current CUDA device")
+    (n, Hq, D), (nk, Hk, Dk), (nv, Hv, Dv) = q.shape, k.shape, v.shape
     if Hk == 0 or Hq % Hk != 0:
         raise ValueError("q's heads must be a multiple of k's")
+    sq, sk, sv = q.stride(), k.stride(), v.stride()
+    for t, stride, good, name in ((q, sq, True, "q"), (k, sk, nk == n and Dk == D, "k"), (v, sv, nv == n and Hv == Hk, "v")):
+        if not good or t.dtype is not dtype or t.get_device() != here or (stride[2] != 1 and t.shape[2] > 1):
+            raise ValueError(f"{name} must match q ([{n}][heads][channels], {dtype}), with contiguous channels, on the current CUDA device")
     if starts.dim() != 1 or starts.numel() < 1:
         raise ValueError("starts must be [B + 1]")
-    _need_here(starts, torch.int32, None, "starts")
+    _need_here(starts, torch.int32, starts.numel(), here, "starts")
     if out is None:
-        out = _new((n, Hq, Dv), q.dtype, q.device, stream)
+        out = _new((n, Hq, Dv), dtype, q.device, stream)
+    elif out.shape != (n, Hq, Dv):
+        raise ValueError(f"out must be [{n}][{Hq}][{Dv}]")
     else:
-        _need_here(out, q.dtype, (n, Hq, Dv), "out")
-    sq, sk, sv = q.stride(), k.stride(), v.stride()
+        _need_here(out, dtype, n * Hq * Dv, here, "out")
     scratch = _get_scratch(PROMPT_SCRATCH, q.device, stream, "prompt")
     _check(lib().soniq_prompt_attend(q.data_ptr(), sq[0], sq[1], k.data_ptr(), sk[0], sk[1], v.data_ptr(), sv[0], sv[1],
                                      starts.data_ptr(), starts.numel() - 1, n, Hq, Hk, D, Dv,
-                                     OUT_BF16 if q.dtype == torch.bfloat16 else OUT_F16, int(bool(causal)),
-                                     1.0 / math.sqrt(D) if scale is None else float(scale), out.data_ptr(), scratch.data_ptr(),
+                                     OUT_BF16 if dtype is torch.bfloat16 else OUT_F16, 1 if causal else 0,
+                                     1.0 / math.sqrt(D) if scale is None else scale, out.data_ptr(), scratch.data_ptr(),
                                      PROMPT_SCRATCH, _stream(stream)), "soniq_prompt_attend")
     return out
 
