@@ -326,11 +326,6 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
         const int steps = (a.D + 15) / 16;      // of 16 channels
         const int k_pieces = (pl.k_atoms + 1) / 2, v_pieces = (pl.v_atoms + 1) / 2;
         bool ok = true;
-        // the ring's next n pieces are there
-        auto arrived = [&](Ring r, int n) {
-            for (int i = 0; ok && i < n; ++i, r.step(pl.slots)) ok = wait(Bars::full + r.i, r.phase);
-            tc::tc_fence_after();
-        };
         // steps of 16 keys in the order in which their weights come: the first quarter of each half, then the second
         auto step_of = [](int h) { return (h & 1) + 4 * (h >> 1 & 1) + 2 * (h >> 2); };
         const uint32_t t_s = tmem + s * slot_cols;
@@ -341,6 +336,9 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
             uint64_t q = q_tile;
 #pragma unroll 1
             for (int c = 0; c < k_pieces; ++c, r.step(pl.slots), q += 2 * (kAtom >> 4)) {
+                ok = ok && wait(Bars::full + r.i, r.phase);
+                if (!ok) break;
+                tc::tc_fence_after();
                 const uint64_t k = tc::sw128_desc(ring + r.i * pl.slot_bytes);
                 const int some = steps - 8 * c;
                 if (some >= 8) {
@@ -365,6 +363,9 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
             const uint32_t p = t_s + buf * kTok;
 #pragma unroll 1
             for (int c = 0; c < v_pieces; ++c, r.step(pl.slots)) {
+                ok = ok && wait(Bars::full + r.i, r.phase) && (c > 0 || wait(Bars::p_full + 2 * (SB == 2 ? buf : s), parity));
+                if (!ok) break;
+                tc::tc_fence_after();
                 const uint32_t values = ring + r.i * pl.slot_bytes, d = t_s + o_col + 128 * c;
                 if (keys > first) {
                     // Tokens behind the prompt, whose weights are 0, may hold anything (a buffer's padding): 0 times
@@ -400,7 +401,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
                 if (ok) warp_arrive(bar(Bars::free + r.i));
             }
         };
-        const bool plain = k_pieces == 1 && steps == 8;
+        const bool plain = k_pieces == 1;
         Ring kv;                                 // the next piece
         uint32_t done = 0, tiles = 0, turns = 0; // blocks, tiles and turns so far
         Unit u;
@@ -414,7 +415,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
 #pragma unroll 1
             for (int i = -SB; ok && i < blocks; ++i) {
                 if (TILES == 2 && plain && i == 0 && mine > 2) {
-                    // Whole blocks of 128 channels, without a question on the way: the warp's instructions come from the
+                    // Whole blocks of up to 128 channels, with few questions on the way: the warp's instructions come from the
                     // cache that the softmax warps sweep, some 5 cycles each.
                     ok = wait(Bars::o_free + s, tiles ^ 1u);
                     uint32_t at = kv.i, phase = kv.phase;
@@ -439,9 +440,22 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
                             warp_mma_ts(t_s + o_col, t_s + 8 * step_of(h), v + step_of(h) * (2048 >> 4), id, h == 0 ? i : 1);
                         }
                         warp_commit(bar(Bars::free + v_at));
-#pragma unroll
-                        for (int h = 0; h < 8; ++h)
+                        auto step = [&](int h) {
                             warp_mma_ss(t_s, q_tile + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), k + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), fmt | columns(kTok), h != 0);
+                        };
+                        int h = 0;
+                        if (steps >= 4) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) step(e);
+                            h = 4;
+                        }
+                        if (steps == 8) {
+#pragma unroll
+                            for (int e = 4; e < 8; ++e) step(e);
+                        } else {
+#pragma unroll 1
+                            for (; h < steps; ++h) step(h);
+                        }
                         warp_commit(bar(Bars::free + k_at));
                         warp_commit(bar(Bars::s_full + 2 * s));
                         warp_arrive(bar(Bars::turn + (s ^ 1)));
@@ -456,21 +470,16 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
                 const bool out = i >= 0 && i < mine, in = i + SB < mine;
                 Ring keys_at = kv;
                 if (i >= 0) skip(keys_at, v_pieces);
-                // (what is there already, before what has to be waited for)
-                if (out) arrived(kv, v_pieces);
-                if (ok && in) arrived(keys_at, k_pieces);
-                if (ok && out) {
-                    ok = (i > 0 || wait(Bars::o_free + s, tiles ^ 1u)) && wait(Bars::p_full + 2 * (SB == 2 ? buf : s), parity);
-                }
+                if (out && i == 0) ok = wait(Bars::o_free + s, tiles ^ 1u);
                 // The two tiles take turns: the softmax of one has the time of the other's MMAs.  (Without, the two ran in
                 // step, both softmaxes and then both tiles' MMAs: 5200 cycles a block instead of 2700.)
                 if (TILES == 2 && i >= 0 && ok) ok = wait(Bars::turn + s, turns ^ (s ^ 1u));
                 if (!ok) break;
-                tc::tc_fence_after();
                 if (out) {
                     outputs(i, buf, parity, i == mine - 1 ? last_keys : kTok, u.len - i * kTok, kv);
                     if (i == mine - 1) warp_commit(bar(Bars::o_full + s));
                 }
+                if (!ok) break;
                 if (in) {
                     scores(buf, i + SB == mine - 1 ? last_keys : kTok, keys_at);
                     if (i + SB == mine - 1) warp_commit(bar(Bars::q_free));
