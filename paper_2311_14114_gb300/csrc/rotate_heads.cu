@@ -12,9 +12,8 @@
 // sincospi.
 //
 // A warp takes a token, or a share of its heads; its lanes work out the token's
-// cosines and sines, and each keeps those of its eight channels for all heads.  Rows are read and
-// written in 16-byte pieces, two rows of 128 channels to a warp; in the half
-// layout partners stand in lanes a fixed distance apart and come by shuffles.
+// cosines and sines, and each keeps those of its sixteen channels for all heads.
+// Rows are read and written in 16-byte pieces, four rows of 128 channels to a warp.
 // Rows that are no 16-byte pieces, or whose partners are not whole pieces apart,
 // take rotate_scalar_kernel, a channel to a lane.
 #include <cuda_bf16.h>
@@ -89,29 +88,41 @@ __device__ __forceinline__ float norm_factor(const float2 (&x)[N], const RotateA
     return f;
 }
 
-// LANES: lanes of a row, eight channels each.  A row's factor f comes last: with
-// the gains in the cosines and sines, out = f (x A + y B) for a channel x and its
-// partner y.
-template <bool BF16, int LANES>
-__global__ void __launch_bounds__(kThreads, 3) rotate_kernel(const __grid_constant__ RotateArgs a, const int parts) {
-    constexpr int ROWS = 32 / LANES, STEPS = 4;
+// LANES: lanes of a row, two pieces of eight channels each, so that a pair's two
+// channels are in one lane: in the half layout the pieces stand half of the turned
+// channels apart, interleaved they follow each other.  Of a pair (x, y) the kernel
+// keeps x in a[] and y in b[], and writes
+//   f (x cx + y sx), f (y cy + x sy)
+// with the gains in the coefficients; f is the row's norm.
+template <bool BF16, int LANES, bool INTERLEAVED>
+__global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const __grid_constant__ RotateArgs a, const int parts) {
+    constexpr int ROWS = 32 / LANES, STEPS = 2;
     const int lane = threadIdx.x & 31, sub = lane / LANES, l = lane % LANES;
     const int64_t task = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     const int64_t token = task / parts;
     const int part = (int)(task - token * parts);
     if (token >= a.n) return;
-    const int c0 = 8 * l, half = a.channels / 2;
-    const bool in_row = c0 < a.D;
+    const int half = a.channels / 2;
+    // this lane's pieces: of the turned ones in the half layout a pair, of the others two neighbours
+    int c0 = 16 * l, c1 = 16 * l + 8;
+    bool turned = c0 < a.channels;
+    if (!INTERLEAVED && turned) {
+        c0 = 8 * l;
+        c1 = half + 8 * l;
+    }
+    const bool in0 = c0 < a.D, in1 = c1 < a.D;
     // `parts` warps share a token's groups of rows
     auto first_of = [&](const RotateSide& side, int p) { return (int)((int64_t)((side.heads + ROWS - 1) / ROWS) * p / parts); };
-    uint4 raw[STEPS];
+    uint4 raw[STEPS][2];
     auto load = [&](const RotateSide& side, int g, int g1) {
-        const uint16_t* in = side.in + token * side.in_token + c0;
+        const uint16_t* in = side.in + token * side.in_token;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             const int h = (g + i) * ROWS + sub;
-            raw[i] = make_uint4(0, 0, 0, 0);
-            if (g + i < g1 && h < side.heads && in_row) raw[i] = *reinterpret_cast<const uint4*>(in + h * side.in_head);
+            const bool on = g + i < g1 && h < side.heads;
+            raw[i][0] = raw[i][1] = make_uint4(0, 0, 0, 0);
+            if (on && in0) raw[i][0] = *reinterpret_cast<const uint4*>(in + h * side.in_head + c0);
+            if (on && in1) raw[i][1] = *reinterpret_cast<const uint4*>(in + h * side.in_head + c1);
         }
     };
     const int s0 = first_of(a.side[0], part) < first_of(a.side[0], part + 1) ? 0 : 1;
@@ -125,13 +136,12 @@ __global__ void __launch_bounds__(kThreads, 3) rotate_kernel(const __grid_consta
         for (int p = lane; p < half; p += 32) mine[p] = turn(a, position, p);
         __syncwarp();
     }
-    // Pairs are (c, c + half), or neighbours.  The partner's words of channels that are not turned do not count (0 times an
-    // infinity is not 0).
-    uint32_t turned[4];
+    // what a channel's partner counts for: nothing where it is not turned, even if it is an infinity
+    auto pair_of = [&](int i) { return INTERLEAVED ? c0 / 2 + i : c0 + i; };
+    uint32_t counts = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) turned[i] = c0 + 2 * i < a.channels ? 0xffffffffu : 0u;
-    const int partner = a.interleaved || c0 >= a.channels ? 0 : (c0 < half ? half / 8 : -half / 8);
-    const int from = sub * LANES + l + partner;
+    for (int i = 0; i < 8; ++i) counts |= (uint32_t)(turned && pair_of(i) < half) << i;
+    const bool all = __all_sync(0xffffffffu, counts == 0xffu || !in0);
     // ---- the heads: queries, then keys ----
 #pragma unroll 1
     for (int s = s0; s < 2; ++s) {
@@ -140,18 +150,16 @@ __global__ void __launch_bounds__(kThreads, 3) rotate_kernel(const __grid_consta
         if (g0 == g1) continue;
         if (s != s0) load(side, g0, g1);
         const bool norm = side.gain != nullptr;
-        float2 A[4], B[4];
+        float cx[8], sx[8], cy[8], sy[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int c = c0 + i, other = a.interleaved ? c ^ 1 : c + 8 * partner;
-            const bool gains = norm && in_row, second = a.interleaved ? (c & 1) != 0 : c >= half;
-            const float2 t = c < a.channels ? mine[a.interleaved ? c / 2 : (second ? c - half : c)] : make_float2(1.0f, 0.0f);
-            const float own = t.x * (gains ? side.gain[c] : 1.0f);
-            const float with = (second ? t.y : -t.y) * (gains && turned[i / 2] != 0 ? side.gain[other] : 1.0f);
-            if (i & 1) A[i / 2].y = own, B[i / 2].y = with;
-            else A[i / 2].x = own, B[i / 2].x = with;
+            const int x = INTERLEAVED ? c0 + 2 * i : c0 + i, y = INTERLEAVED ? c0 + 2 * i + 1 : c1 + i;
+            const float gx = norm && x < a.D ? side.gain[x] : 1.0f, gy = norm && y < a.D ? side.gain[y] : 1.0f;
+            const float2 t = counts >> i & 1u ? mine[pair_of(i)] : make_float2(1.0f, 0.0f);
+            cx[i] = t.x * gx, sx[i] = -t.y * gy;
+            cy[i] = t.x * gy, sy[i] = t.y * gx;
         }
-        uint16_t* out = side.out + token * side.out_token + c0;
+        uint16_t* out = side.out + token * side.out_token;
 #pragma unroll 1
         for (int g = g0; g < g1; g += STEPS) {
             if (g != g0) load(side, g, g1);
@@ -159,29 +167,43 @@ __global__ void __launch_bounds__(kThreads, 3) rotate_kernel(const __grid_consta
             for (int i = 0; i < STEPS; ++i) {
                 if (g + i >= g1) break;
                 const int h = (g + i) * ROWS + sub;
-                const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-                float2 x[4], y[4];
+                const uint32_t w[8] = {raw[i][0].x, raw[i][0].y, raw[i][0].z, raw[i][0].w, raw[i][1].x, raw[i][1].y, raw[i][1].z, raw[i][1].w};
+                float2 v[8];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    x[k] = load2<BF16>(w[k]);
-                    y[k] = load2<BF16>((a.interleaved ? __byte_perm(w[k], 0, 0x1032) : __shfl_sync(0xffffffffu, w[k], from)) & turned[k]);
-                }
+                for (int k = 0; k < 8; ++k) v[k] = load2<BF16>(w[k]);
                 float f = 1.0f, up = 1.0f;
-                if (norm) f = norm_factor<LANES>(x, a, &up);
+                if (norm) f = norm_factor<LANES>(v, a, &up);
                 if (up != 1.0f) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        x[k] = mul2(x[k], make_float2(up, up));
-                        y[k] = mul2(y[k], make_float2(up, up));
+                    for (int k = 0; k < 8; ++k) v[k] = mul2(v[k], make_float2(up, up));
+                }
+                float x[8], y[8], z[8], u[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    x[k] = INTERLEAVED ? v[k].x : (k & 1 ? v[k / 2].y : v[k / 2].x);
+                    y[k] = INTERLEAVED ? v[k].y : (k & 1 ? v[4 + k / 2].y : v[4 + k / 2].x);
+                }
+                if (all) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        z[k] = fmaf(y[k], sx[k], x[k] * cx[k]) * f;
+                        u[k] = fmaf(x[k], sy[k], y[k] * cy[k]) * f;
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const bool on = counts >> k & 1u;
+                        z[k] = fmaf(on ? y[k] : 0.0f, sx[k], x[k] * cx[k]) * f;
+                        u[k] = fmaf(on ? x[k] : 0.0f, sy[k], y[k] * cy[k]) * f;
                     }
                 }
-                uint32_t z[4];
+                uint32_t r[8];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float2 v = mul2(fma2(y[k], B[k], mul2(x[k], A[k])), make_float2(f, f));
-                    z[k] = round2<BF16>(v.x, v.y);
-                }
-                if (h < side.heads && in_row) *reinterpret_cast<uint4*>(out + h * side.out_head) = make_uint4(z[0], z[1], z[2], z[3]);
+                for (int k = 0; k < 8; ++k)
+                    r[k] = INTERLEAVED ? round2<BF16>(z[k], u[k]) : (k < 4 ? round2<BF16>(z[2 * k], z[2 * k + 1]) : round2<BF16>(u[2 * k - 8], u[2 * k - 7]));
+                uint16_t* to = out + h * side.out_head;
+                if (h < side.heads && in0) *reinterpret_cast<uint4*>(to + c0) = make_uint4(r[0], r[1], r[2], r[3]);
+                if (h < side.heads && in1) *reinterpret_cast<uint4*>(to + c1) = make_uint4(r[4], r[5], r[6], r[7]);
             }
         }
     }
@@ -250,15 +272,17 @@ __global__ void __launch_bounds__(kThreads) rotate_scalar_kernel(const __grid_co
 
 template <bool BF16>
 cudaError_t launch(const RotateArgs& a, bool vectors, cudaStream_t st) {
-    const int lanes = !vectors ? 32 : (a.D <= 64 ? 8 : (a.D <= 128 ? 16 : 32)), rows = 32 / lanes;
+    const int lanes = !vectors ? 32 : (a.D <= 64 ? 4 : (a.D <= 128 ? 8 : 16)), rows = 32 / lanes;
     const int groups = (a.side[0].heads + rows - 1) / rows + (a.side[1].heads + rows - 1) / rows;
     // a token's heads are shared by warps until there are eight for each scheduler
     const int64_t want = ((int64_t)num_sms() * 32 + a.n - 1) / a.n;
     const int parts = (int)(want < groups ? want : groups);
     const int64_t grid = (a.n * parts + kThreads / 32 - 1) / (kThreads / 32);
     if (grid > 2147483647) return cudaErrorNotSupported;
+    auto pick = [&](auto* by4, auto* by8, auto* by16) { return lanes == 4 ? by4 : (lanes == 8 ? by8 : by16); };
     auto* kernel = !vectors ? rotate_scalar_kernel<BF16>
-                            : (lanes == 8 ? rotate_kernel<BF16, 8> : (lanes == 16 ? rotate_kernel<BF16, 16> : rotate_kernel<BF16, 32>));
+                            : (a.interleaved ? pick(rotate_kernel<BF16, 4, true>, rotate_kernel<BF16, 8, true>, rotate_kernel<BF16, 16, true>)
+                                             : pick(rotate_kernel<BF16, 4, false>, rotate_kernel<BF16, 8, false>, rotate_kernel<BF16, 16, false>));
     kernel<<<(unsigned)grid, kThreads, 0, st>>>(a, parts);
     note_launch();
     return cudaGetLastError();

@@ -1,20 +1,22 @@
-"""Attention over a quantized cache, as a decoder runs it with drafted tokens.
+"""Attention over a quantized cache, as a decoder runs it with whole prompts and
+drafted tokens.
 
-A step takes the hidden states of T tokens of each sequence: a piece of a
-prompt, one new token, or a tree of drafted ones.  The fused projection runs on
-the library's quantized matmul (signed activations, Eq. (1), one scale per
-token), its keys and values go to the cache (soniq_kv_write), the queries
-attend over the cached context and over the drafts their mask shows
-(soniq_kv_attend), and the output projection closes the layer.  When the
-drafts have been judged, `accept` moves the rows of the accepted path behind
-the context; they are quantized from the same 16-bit rows again, so a token's
-codes do not depend on whether it was drafted.
+Whole prompts come packed, back to back: soniq_kv_plan has said where their
+tokens go, they attend to themselves in 16 bits (soniq_prompt_attend), and their
+keys and values are put into the cache.  A later step takes the hidden states of
+T tokens of each sequence: a piece of a prompt, one new token, or a tree of
+drafted ones.  The fused projection runs on the library's quantized matmul (signed
+activations, Eq. (1), one scale per token), queries and keys are normalised and
+turned by their positions where the layer does so (soniq_rotate_heads), keys and
+values go to the cache (soniq_kv_write), the queries attend over the cached
+context and over the drafts their mask shows (soniq_kv_attend), and the output
+projection closes the layer.  When the drafts have been judged, `accept` moves the
+rows of the accepted path behind the context; they are quantized from the same
+16-bit rows again, so a token's codes do not depend on whether it was drafted.
 
-This module sequences the calls and does the integer bookkeeping of slots;
-every arithmetic step runs in the library's kernels.  The layer is fp16 and
-applies no position encoding: there is no place for one between its projection
-and its cache.  A model that turns q and k by their positions, or runs in bf16,
-makes the same calls itself."""
+This module sequences the calls and does the integer bookkeeping of drafts; every
+arithmetic step runs in the library's kernels.  The layer is fp16; a model that
+runs in bf16 makes the same calls itself."""
 from __future__ import annotations
 
 from typing import Optional, Tuple
@@ -30,10 +32,13 @@ class CachedAttention:
     qkv, out: dicts with W (fp32 [N][K], numpy or torch), perm, count, bits (as
     the workloads module makes them).  qkv's rows are the query heads (q_heads
     of k.D), the key heads and the value heads; out's channels the query heads
-    (of v.D).  The cache has n_pages pages of page_size tokens."""
+    (of v.D).  The cache has n_pages pages of page_size tokens.  rotary, gains,
+    eps: sq.rotate_heads' of the queries and keys (gains: a pair, fp32 [k.D] each),
+    left out: queries and keys stay as projected."""
 
     def __init__(self, qkv: dict, out: dict, q_heads: int, k: sq.KVLayout, v: sq.KVLayout, n_pages: int,
-                 page_size: int = 64, device="cuda"):
+                 page_size: int = 64, device="cuda", rotary: Optional[sq.Rotary] = None,
+                 gains: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, eps: float = 1e-6):
         self.q_heads = int(q_heads)
         self.cache = sq.KVCache(k, v, n_pages, page_size, torch.float16, device=device)
         self.weights = []
@@ -47,11 +52,33 @@ class CachedAttention:
             raise ValueError("the projections' sizes differ from the heads'")
         self.widths = widths
         self.q = self.k = self.v = self.o = None
+        self.rotary, self.gains, self.eps = rotary, gains or (None, None), eps
 
     def _project(self, which: int, x: torch.Tensor) -> torch.Tensor:
         layout, Wp, s_w = self.weights[which]
         Ap, s_a = sq.quantize_act(layout, x, "row")
         return sq.mp_gemm(layout, Ap, s_a, Wp, s_w, scale_mode="row")
+
+    def _heads(self, X: torch.Tensor, positions):
+        """Queries, keys and values [n][heads][..] of the rows X [n][K]; positions: a
+        function that gives the rows' (called where they are used)."""
+        q, k, v = self._project(0, X).split(self.widths, dim=-1)
+        q = q.unflatten(-1, (self.q_heads, self.cache.k.D))
+        k = k.unflatten(-1, (self.cache.heads, self.cache.k.D))
+        if self.rotary is not None or self.gains[0] is not None or self.gains[1] is not None:
+            sq.rotate_heads(self.rotary, q, k, positions() if self.rotary is not None else None, *self.gains, self.eps,
+                            q_out=q, k_out=k)
+        return q, k, v.unflatten(-1, (self.cache.heads, self.cache.v.D))
+
+    def prompt(self, X: torch.Tensor, step: sq.KVStep) -> torch.Tensor:
+        """Whole prompts, packed.  X: fp16 [n][K], as many rows as the step's buffers
+        (sq.kv_plan from lengths of 0 or less; sequences that add nothing may stand
+        among them); rows behind the step's tokens are padding.  Returns fp16 [n][N]."""
+        self.q, self.k, self.v = self._heads(X, lambda: step.positions)
+        sq.kv_write(self.cache, self.k, self.v, step.slots)
+        self.o = torch.zeros(X.shape[0], self.q_heads, self.cache.v.D, dtype=X.dtype, device=X.device)
+        sq.prompt_attend(self.q, self.k, self.v, step.starts, out=self.o)
+        return self._project(1, self.o.view(X.shape[0], -1))
 
     def slots(self, page_table: torch.Tensor, lengths: torch.Tensor, T: int) -> torch.Tensor:
         """Slots (int64 [B][T]) of the T tokens behind each context; -1 in absent
@@ -66,18 +93,23 @@ class CachedAttention:
         return torch.where(lengths[:, None] >= 0, slot, -1)
 
     def step(self, X: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
-             mask: Optional[torch.Tensor] = None) -> torch.Tensor:
+             mask: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+             slots: Optional[torch.Tensor] = None) -> torch.Tensor:
         """X: fp16 [B][T][K]; page_table int32 [B][pages]; lengths int32 [B] (the
-        context in front of the T tokens); mask as sq.kv_attend's.  Returns fp16
-        [B][T][N]; q, k, v and the attention's output stay in self."""
+        context in front of the T tokens); mask as sq.kv_attend's.  positions: int32
+        [B][T], what a layer with a rotary turns by (left out: one after the other
+        behind the context; of a tree's drafts those with the same depth share one).
+        slots: int64, the B * T tokens' where they are known (sq.kv_plan's).  Returns
+        fp16 [B][T][N]; q, k, v and the attention's output stay in self."""
         B, T, K = X.shape
-        y = self._project(0, X.reshape(B * T, K)).view(B, T, -1)
-        q, k, v = y.split(self.widths, dim=-1)
-        self.q = q.unflatten(-1, (self.q_heads, self.cache.k.D))
-        self.k = k.unflatten(-1, (self.cache.heads, self.cache.k.D))
-        self.v = v.unflatten(-1, (self.cache.heads, self.cache.v.D))
-        sq.kv_write(self.cache, self.k.flatten(0, 1), self.v.flatten(0, 1),
-                    self.slots(page_table, lengths, T).view(-1))
+
+        def where():
+            p = lengths[:, None] + torch.arange(T, dtype=torch.int32, device=X.device) if positions is None else positions
+            return p.to(torch.int32).reshape(-1)
+
+        q, k, v = self._heads(X.reshape(B * T, K), where)
+        self.q, self.k, self.v = (t.unflatten(0, (B, T)) for t in (q, k, v))
+        sq.kv_write(self.cache, k, v, self.slots(page_table, lengths, T).view(-1) if slots is None else slots)
         self.o = sq.kv_attend(self.cache, self.q, page_table, lengths, mask)
         return self._project(1, self.o.view(B * T, -1)).view(B, T, -1)
 

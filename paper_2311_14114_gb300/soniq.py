@@ -10,7 +10,6 @@ from __future__ import annotations
 import ctypes
 import math
 import os
-from fractions import Fraction
 from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
@@ -688,8 +687,9 @@ class Rotary:
         self.frequencies = [float(f) for f in frequencies]
         if len(self.frequencies) != channels // 2 or not all(math.isfinite(f) for f in self.frequencies):
             raise ValueError("frequencies must be one finite number for each pair")
-        # turns of 2^64 parts, from the doubles exactly, as signed words
-        turns = [round(Fraction(f) / _TWO_PI * 2 ** 64) % 2 ** 64 for f in self.frequencies]
+        # turns of 2^64 parts, to the nearest from the doubles' own values, as signed words
+        ratios = [f.as_integer_ratio() for f in self.frequencies]
+        turns = [(2 * n * _PI_SCALE * 2 ** 63 + d * _PI) // (2 * d * _PI) % 2 ** 64 for n, d in ratios]
         self.turns = torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turns], dtype=torch.int64, device=device)
         self.c = CRotary(self.channels, int(self.interleaved), self.magnitude, self.turns.data_ptr() if turns else None)
         self.ref = ctypes.byref(self.c)
@@ -712,7 +712,8 @@ class Rotary:
         raise ValueError("scaling must be ('linear', factor) or ('wavelength', factor, low, high, length)")
 
 
-_TWO_PI = Fraction("6.283185307179586476925286766559005768394338798750211641949889")
+# pi with 60 decimals
+_PI, _PI_SCALE = 3141592653589793238462643383279502884197169399375105820974944, 10 ** 60
 
 
 def _heads(x: torch.Tensor, n: int, D: int, dtype, gain: Optional[torch.Tensor], out: Optional[torch.Tensor], here: int,
