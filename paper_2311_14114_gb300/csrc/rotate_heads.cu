@@ -19,7 +19,6 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include "soniq_device.cuh"
 #include "step_internal.h"
 
 namespace soniq {
@@ -27,6 +26,17 @@ namespace soniq {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kAhead = 8;      // groups of rows, 1 KB each, that a warp has on their way
+
+// 16 bytes into shared memory, or zeros; this thread sees them after cp.async.wait_group.
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool on) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ uint4 read16(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
 
 template <bool BF16>
 __device__ __forceinline__ float2 load2(uint32_t x) {
@@ -53,37 +63,35 @@ __device__ __forceinline__ float2 turn(const RotateArgs& a, int position, int pa
     return make_float2(c * a.magnitude, s * a.magnitude);
 }
 
-// 1 / the root mean square of a row, of which each of its LANES lanes holds N pairs
-// of channels.  Where the squares' sum leaves fp32 (above; or below, with no eps to
+// 1 / the root mean square of a row, of which each of its LANES lanes holds N
+// channels.  Where the squares' sum leaves fp32 (above; or below, with no eps to
 // speak of) it is that of the row times *up, a power of two.
 template <int LANES, int N>
-__device__ __forceinline__ float norm_factor(const float2 (&x)[N], const RotateArgs& a, float* up) {
-    auto squares = [&](float by) {
-        float2 sum = make_float2(0.0f, 0.0f);
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const float2 y = by == 1.0f ? x[k] : mul2(x[k], make_float2(by, by));
-            sum = fma2(y, y, sum);
-        }
-        float all = sum.x + sum.y;
+__device__ __forceinline__ float norm_factor(const float (&x)[N], const RotateArgs& a, float* up) {
+    auto over_lanes = [&](float all) {
 #pragma unroll
         for (int d = LANES / 2; d; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
         return all;
     };
-    const float sum = squares(1.0f), mean = fmaf(sum, 1.0f / (float)a.D, a.eps);
+    float part[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < N; ++k) part[k & 1] = fmaf(x[k], x[k], part[k & 1]);
+    const float sum = over_lanes(part[0] + part[1]), mean = fmaf(sum, a.inverse_D, a.eps);
     float f = rsqrtf(mean);
     const bool out = !(sum <= 1e37f && mean >= 1e-30f);
     if (__any_sync(0xffffffffu, out)) {
-        float most = 0.0f;
+        float most = 0.0f, again = 0.0f;
 #pragma unroll
-        for (int k = 0; k < N; ++k) most = fmaxf(most, fmaxf(fabsf(x[k].x), fabsf(x[k].y)));
+        for (int k = 0; k < N; ++k) most = fmaxf(most, fabsf(x[k]));
 #pragma unroll
         for (int d = LANES / 2; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
         // to about 1; 2^100 at most so that eps stays in range with it; none for rows of zeros or infinities
         const int e = out && most > 0.0f && most < INFINITY ? min(127 - (int)(__float_as_uint(most) >> 23), 100) : 0;
         *up = __uint_as_float((uint32_t)(max(e, -126) + 127) << 23);
-        const float better = rsqrtf(fmaf(squares(*up), 1.0f / (float)a.D, a.eps * *up * *up));
-        if (e != 0) f = better;
+#pragma unroll
+        for (int k = 0; k < N; ++k) again = fmaf(x[k] * *up, x[k] * *up, again);
+        again = over_lanes(again);
+        if (e != 0) f = rsqrtf(fmaf(again, a.inverse_D, a.eps * *up * *up));
     }
     return f;
 }
@@ -96,7 +104,7 @@ __device__ __forceinline__ float norm_factor(const float2 (&x)[N], const RotateA
 // with the gains in the coefficients; f is the row's norm.
 template <bool BF16, int LANES, bool INTERLEAVED>
 __global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const __grid_constant__ RotateArgs a, const int parts) {
-    constexpr int ROWS = 32 / LANES, STEPS = 2;
+    constexpr int ROWS = 32 / LANES;
     const int lane = threadIdx.x & 31, sub = lane / LANES, l = lane % LANES;
     const int64_t task = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     const int64_t token = task / parts;
@@ -113,20 +121,34 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const __grid_consta
     const bool in0 = c0 < a.D, in1 = c1 < a.D;
     // `parts` warps share a token's groups of rows
     auto first_of = [&](const RotateSide& side, int p) { return (int)((int64_t)((side.heads + ROWS - 1) / ROWS) * p / parts); };
-    uint4 raw[STEPS][2];
-    auto load = [&](const RotateSide& side, int g, int g1) {
-        const uint16_t* in = side.in + token * side.in_token;
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            const int h = (g + i) * ROWS + sub;
-            const bool on = g + i < g1 && h < side.heads;
-            raw[i][0] = raw[i][1] = make_uint4(0, 0, 0, 0);
-            if (on && in0) raw[i][0] = *reinterpret_cast<const uint4*>(in + h * side.in_head + c0);
-            if (on && in1) raw[i][1] = *reinterpret_cast<const uint4*>(in + h * side.in_head + c1);
+    // ---- groups of rows on their way: kAhead of them, each lane's pieces in places of its own ----
+    extern __shared__ __align__(16) uint8_t ring[];
+    const int first0 = first_of(a.side[0], part), n0 = first_of(a.side[0], part + 1) - first0;
+    const int first1 = first_of(a.side[1], part), n1 = first_of(a.side[1], part + 1) - first1;
+    const uint32_t place = (uint32_t)__cvta_generic_to_shared(ring) + (threadIdx.x >> 5) * (kAhead * 1024) + 16 * lane;
+    const uint16_t* next = a.side[0].in + token * a.side[0].in_token + (int64_t)(first0 * ROWS + sub) * a.side[0].in_head;
+    int next_left = n0, next_rows = a.side[0].heads - first0 * ROWS - sub;      // groups to come of this side, rows from this lane's on
+    bool last_side = false;
+    uint32_t put = 0;
+    auto fetch = [&]() {
+        if (next_left == 0 && !last_side) {
+            last_side = true;
+            next = a.side[1].in + token * a.side[1].in_token + (int64_t)(first1 * ROWS + sub) * a.side[1].in_head;
+            next_left = n1;
+            next_rows = a.side[1].heads - first1 * ROWS - sub;
         }
+        if (next_left > 0) {
+            copy16(place + put, next + (in0 ? c0 : 0), in0 && next_rows > 0);
+            copy16(place + put + 512, next + (in1 ? c1 : 0), in1 && next_rows > 0);
+            next += ROWS * a.side[last_side ? 1 : 0].in_head;
+            next_rows -= ROWS;
+            --next_left;
+            put = (put + 1024) % (kAhead * 1024);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    const int s0 = first_of(a.side[0], part) < first_of(a.side[0], part + 1) ? 0 : 1;
-    load(a.side[s0], first_of(a.side[s0], part), first_of(a.side[s0], part + 1));     // on its way while angles are worked out
+#pragma unroll 1
+    for (int t = 0; t < kAhead; ++t) fetch();
     // ---- the token's cosines and sines, a pair to a lane ----
     __shared__ float2 turns[kThreads / 32][128];
     float2* mine = turns[threadIdx.x >> 5];
@@ -143,70 +165,85 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const __grid_consta
     for (int i = 0; i < 8; ++i) counts |= (uint32_t)(turned && pair_of(i) < half) << i;
     const bool all = __all_sync(0xffffffffu, counts == 0xffu || !in0);
     // ---- the heads: queries, then keys ----
+    uint32_t get = 0;
 #pragma unroll 1
-    for (int s = s0; s < 2; ++s) {
+    for (int s = 0; s < 2; ++s) {
         const RotateSide& side = a.side[s];
-        const int g0 = first_of(side, part), g1 = first_of(side, part + 1);
-        if (g0 == g1) continue;
-        if (s != s0) load(side, g0, g1);
+        const int n = s ? n1 : n0, first = s ? first1 : first0;
+        if (n == 0) continue;
         const bool norm = side.gain != nullptr;
+        float g0[8], g1[8];        // gains of this lane's pieces
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+            const float4 one = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+            const float4 p = norm && in0 ? *reinterpret_cast<const float4*>(side.gain + c0 + i) : one;
+            const float4 q = norm && in1 ? *reinterpret_cast<const float4*>(side.gain + c1 + i) : one;
+            g0[i] = p.x, g0[i + 1] = p.y, g0[i + 2] = p.z, g0[i + 3] = p.w;
+            g1[i] = q.x, g1[i + 1] = q.y, g1[i + 2] = q.z, g1[i + 3] = q.w;
+        }
         float cx[8], sx[8], cy[8], sy[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int x = INTERLEAVED ? c0 + 2 * i : c0 + i, y = INTERLEAVED ? c0 + 2 * i + 1 : c1 + i;
-            const float gx = norm && x < a.D ? side.gain[x] : 1.0f, gy = norm && y < a.D ? side.gain[y] : 1.0f;
+            const float gx = INTERLEAVED ? (i < 4 ? g0[2 * i] : g1[2 * i - 8]) : g0[i];
+            const float gy = INTERLEAVED ? (i < 4 ? g0[2 * i + 1] : g1[2 * i - 7]) : g1[i];
             const float2 t = counts >> i & 1u ? mine[pair_of(i)] : make_float2(1.0f, 0.0f);
             cx[i] = t.x * gx, sx[i] = -t.y * gy;
             cy[i] = t.x * gy, sy[i] = t.y * gx;
         }
-        uint16_t* out = side.out + token * side.out_token;
+        uint16_t* to = side.out + token * side.out_token + (int64_t)(first * ROWS + sub) * side.out_head;
+        const int64_t to_step = ROWS * side.out_head;
+        int rows = side.heads - first * ROWS - sub;        // from this lane's on
 #pragma unroll 1
-        for (int g = g0; g < g1; g += STEPS) {
-            if (g != g0) load(side, g, g1);
+        for (int g = 0; g < n; ++g, to += to_step, rows -= ROWS) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+            const uint4 p0 = read16(place + get), p1 = read16(place + get + 512);
+            get = (get + 1024) % (kAhead * 1024);
+            const uint32_t w[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
+            float v[16];
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                if (g + i >= g1) break;
-                const int h = (g + i) * ROWS + sub;
-                const uint32_t w[8] = {raw[i][0].x, raw[i][0].y, raw[i][0].z, raw[i][0].w, raw[i][1].x, raw[i][1].y, raw[i][1].z, raw[i][1].w};
-                float2 v[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = load2<BF16>(w[k]);
-                float f = 1.0f, up = 1.0f;
-                if (norm) f = norm_factor<LANES>(v, a, &up);
+            for (int k = 0; k < 8; ++k) {
+                const float2 pair = load2<BF16>(w[k]);
+                v[2 * k] = pair.x;
+                v[2 * k + 1] = pair.y;
+            }
+            fetch();
+            float f = 1.0f, up = 1.0f;
+            if (norm) {
+                f = norm_factor<LANES>(v, a, &up);
                 if (up != 1.0f) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k] = mul2(v[k], make_float2(up, up));
+                    for (int k = 0; k < 16; ++k) v[k] *= up;
                 }
-                float x[8], y[8], z[8], u[8];
+            }
+            float x[8], y[8], z[8], u[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                x[k] = INTERLEAVED ? v[2 * k] : v[k];
+                y[k] = INTERLEAVED ? v[2 * k + 1] : v[8 + k];
+            }
+            if (all) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    x[k] = INTERLEAVED ? v[k].x : (k & 1 ? v[k / 2].y : v[k / 2].x);
-                    y[k] = INTERLEAVED ? v[k].y : (k & 1 ? v[4 + k / 2].y : v[4 + k / 2].x);
+                    z[k] = fmaf(y[k], sx[k], x[k] * cx[k]) * f;
+                    u[k] = fmaf(x[k], sy[k], y[k] * cy[k]) * f;
                 }
-                if (all) {
+            } else {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        z[k] = fmaf(y[k], sx[k], x[k] * cx[k]) * f;
-                        u[k] = fmaf(x[k], sy[k], y[k] * cy[k]) * f;
-                    }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const bool on = counts >> k & 1u;
-                        z[k] = fmaf(on ? y[k] : 0.0f, sx[k], x[k] * cx[k]) * f;
-                        u[k] = fmaf(on ? x[k] : 0.0f, sy[k], y[k] * cy[k]) * f;
-                    }
+                for (int k = 0; k < 8; ++k) {
+                    const bool on = counts >> k & 1u;
+                    z[k] = fmaf(on ? y[k] : 0.0f, sx[k], x[k] * cx[k]) * f;
+                    u[k] = fmaf(on ? x[k] : 0.0f, sy[k], y[k] * cy[k]) * f;
                 }
-                uint32_t r[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    r[k] = INTERLEAVED ? round2<BF16>(z[k], u[k]) : (k < 4 ? round2<BF16>(z[2 * k], z[2 * k + 1]) : round2<BF16>(u[2 * k - 8], u[2 * k - 7]));
-                uint16_t* to = out + h * side.out_head;
-                if (h < side.heads && in0) *reinterpret_cast<uint4*>(to + c0) = make_uint4(r[0], r[1], r[2], r[3]);
-                if (h < side.heads && in1) *reinterpret_cast<uint4*>(to + c1) = make_uint4(r[4], r[5], r[6], r[7]);
             }
+            uint32_t r[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                r[k] = INTERLEAVED ? round2<BF16>(z[k], u[k]) : (k < 4 ? round2<BF16>(z[2 * k], z[2 * k + 1]) : round2<BF16>(u[2 * k - 8], u[2 * k - 7]));
+            if (rows > 0 && in0) *reinterpret_cast<uint4*>(to + c0) = make_uint4(r[0], r[1], r[2], r[3]);
+            if (rows > 0 && in1) *reinterpret_cast<uint4*>(to + c1) = make_uint4(r[4], r[5], r[6], r[7]);
         }
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 // A channel to a lane, eight times: any D, channels and strides.
@@ -241,13 +278,12 @@ __global__ void __launch_bounds__(kThreads) rotate_scalar_kernel(const __grid_co
         for (int h = h0; h < h1; ++h) {
             const uint16_t* in = side.in + token * side.in_token + h * side.in_head;
             uint16_t* out = side.out + token * side.out_token + h * side.out_head;
-            float2 x[4], y[4];
-            auto at = [](float2 (&v)[4], int i) -> float& { return i & 1 ? v[i / 2].y : v[i / 2].x; };
+            float x[8], y[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int c = lane + 32 * i;
-                at(x, i) = c < a.D ? value(in[c]) : 0.0f;
-                at(y, i) = partner[i] >= 0 ? value(in[partner[i]]) : 0.0f;
+                x[i] = c < a.D ? value(in[c]) : 0.0f;
+                y[i] = partner[i] >= 0 ? value(in[partner[i]]) : 0.0f;
             }
             __syncwarp();       // the whole row is read before any of it is written: out may be in
             if (side.gain != nullptr) {
@@ -256,14 +292,14 @@ __global__ void __launch_bounds__(kThreads) rotate_scalar_kernel(const __grid_co
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int c = lane + 32 * i;
-                    at(x, i) = c < a.D ? at(x, i) * up * f * side.gain[c] : 0.0f;
-                    at(y, i) = partner[i] >= 0 ? at(y, i) * up * f * side.gain[partner[i]] : 0.0f;
+                    x[i] = c < a.D ? x[i] * up * f * side.gain[c] : 0.0f;
+                    y[i] = partner[i] >= 0 ? y[i] * up * f * side.gain[partner[i]] : 0.0f;
                 }
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int c = lane + 32 * i;
-                if (c < a.D) out[c] = (uint16_t)round2<BF16>(fmaf(at(y, i), sn[i], at(x, i) * cs[i]), 0.0f);
+                if (c < a.D) out[c] = (uint16_t)round2<BF16>(fmaf(y[i], sn[i], x[i] * cs[i]), 0.0f);
             }
             __syncwarp();
         }
@@ -283,7 +319,12 @@ cudaError_t launch(const RotateArgs& a, bool vectors, cudaStream_t st) {
     auto* kernel = !vectors ? rotate_scalar_kernel<BF16>
                             : (a.interleaved ? pick(rotate_kernel<BF16, 4, true>, rotate_kernel<BF16, 8, true>, rotate_kernel<BF16, 16, true>)
                                              : pick(rotate_kernel<BF16, 4, false>, rotate_kernel<BF16, 8, false>, rotate_kernel<BF16, 16, false>));
-    kernel<<<(unsigned)grid, kThreads, 0, st>>>(a, parts);
+    const int smem = vectors ? kThreads / 32 * kAhead * 1024 : 0;
+    if (smem > 0) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+    }
+    kernel<<<(unsigned)grid, kThreads, smem, st>>>(a, parts);
     note_launch();
     return cudaGetLastError();
 }

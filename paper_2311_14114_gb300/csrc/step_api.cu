@@ -86,6 +86,7 @@ soniq_status soniq_rotate_heads(const soniq_rotary* rotary, const int32_t* posit
     a.n = n;
     a.D = D;
     a.eps = eps;
+    a.inverse_D = 1.0f / (float)D;
     return launched(launch_rotate_heads(a, dtype == SONIQ_OUT_BF16, reinterpret_cast<cudaStream_t>(stream)));
 }
 

@@ -42,7 +42,7 @@ struct RotateArgs {
     const uint64_t* turns;         // [channels / 2]
     int64_t n;
     int32_t D, channels, interleaved;
-    float magnitude, eps;
+    float magnitude, eps, inverse_D;
 };
 cudaError_t launch_rotate_heads(const RotateArgs& a, bool bf16, cudaStream_t st);
 
