@@ -670,7 +670,8 @@ SONIQ_API soniq_status soniq_rotate_heads(const soniq_rotary *rotary, const int3
  *              in elements as for soniq_kv_write.
  *   starts     device int32 [B + 1], not falling: sequence b is tokens starts[b] ..
  *              starts[b + 1] - 1 (it may be empty).  One that is not within 0 .. n is
- *              left out and reported by soniq_sync_status (SONIQ_ERR_INVALID_ARG).
+ *              left out and reported by soniq_sync_status (SONIQ_ERR_INVALID_ARG); of
+ *              rows that two sequences share, either's output may stay.
  *   out        device, contiguous [n][q_heads][Dv]; rows of no sequence are left as
  *              they were.
  *   D, Dv      1..256, at most 4096 query heads and 2^30 tokens (SONIQ_ERR_UNSUPPORTED above).

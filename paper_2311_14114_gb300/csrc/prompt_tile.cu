@@ -465,8 +465,63 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
                     kv.phase = phase;
                     if (!ok) break;
                 }
-                const uint32_t buf = SB == 2 ? (done + (i & 1)) & 1u : 0u;
-                const uint32_t parity = SB == 2 ? (done + i) >> 1 : done + i;
+                if (TILES == 1 && i == 0 && mine > 3) {
+                    // whole blocks, likewise
+                    ok = wait(Bars::o_free, tiles ^ 1u);
+                    uint32_t at = kv.i, phase = kv.phase;
+                    auto go_on = [&] {
+                        if (++at == (uint32_t)pl.slots) at = 0, phase ^= 1u;
+                    };
+#pragma unroll 1
+                    for (; ok && i + 3 < mine; ++i) {
+                        const uint32_t b = (done + i) & 1u, t_b = t_s + b * kTok, half_round = (done + i) >> 1;
+#pragma unroll 1
+                        for (int c = 0; c < v_pieces; ++c) {
+                            ok = wait(Bars::full + at, phase) && (c > 0 || wait(Bars::p_full + 2 * b, half_round));
+                            if (!ok) break;
+                            tc::tc_fence_after();
+                            const uint64_t v = value_desc(ring + at * pl.slot_bytes, kAtom);
+                            const uint32_t id = fmt | (1u << 16) | columns(min(pl.o_cols - 128 * c, 128));
+#pragma unroll
+                            for (int h = 0; h < 8; ++h) {
+                                if (h == 4 && c == 0) {
+                                    ok = wait(Bars::p_full + 2 * b + 1, half_round);
+                                    tc::tc_fence_after();
+                                }
+                                warp_mma_ts(t_s + o_col + 128 * c, t_b + 8 * step_of(h), v + step_of(h) * (2048 >> 4), id, h == 0 ? i : 1);
+                            }
+                            warp_commit(bar(Bars::free + at));
+                            go_on();
+                        }
+                        if (!ok) break;
+                        warp_commit(bar(Bars::pv_done));
+#pragma unroll 1
+                        for (int c = 0; c < k_pieces; ++c) {
+                            ok = wait(Bars::full + at, phase);
+                            if (!ok) break;
+                            tc::tc_fence_after();
+                            const uint64_t k = tc::sw128_desc(ring + at * pl.slot_bytes), q = q_tile + c * 2 * (kAtom >> 4);
+                            auto step = [&](int h, uint32_t acc) {
+                                warp_mma_ss(t_b, q + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), k + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), fmt | columns(kTok), acc);
+                            };
+                            if (steps - 8 * c >= 8) {
+#pragma unroll
+                                for (int h = 0; h < 8; ++h) step(h, h == 0 ? c : 1);
+                            } else {
+#pragma unroll 1
+                                for (int h = 0; h < steps - 8 * c; ++h) step(h, c | h);
+                            }
+                            warp_commit(bar(Bars::free + at));
+                            go_on();
+                        }
+                        if (!ok) break;
+                        warp_commit(bar(Bars::s_full + b));
+                    }
+                    kv.i = at;
+                    kv.phase = phase;
+                    if (!ok) break;
+                }
+                const uint32_t buf = SB == 2 ? (done + (i & 1)) & 1u : 0u, parity = SB == 2 ? (done + i) >> 1 : done + i;
                 const bool out = i >= 0 && i < mine, in = i + SB < mine;
                 Ring keys_at = kv;
                 if (i >= 0) skip(keys_at, v_pieces);
