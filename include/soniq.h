@@ -669,11 +669,11 @@ SONIQ_API soniq_status soniq_rotate_heads(const soniq_rotary *rotary, const int3
  *   Q, K, V    device, `dtype` (SONIQ_OUT_F16 or SONIQ_OUT_BF16), n tokens; strides
  *              in elements as for soniq_kv_write.
  *   starts     device int32 [B + 1], not falling: sequence b is tokens starts[b] ..
- *              starts[b + 1] - 1 (it may be empty).  One that is not within 0 .. n is
- *              left out and reported by soniq_sync_status (SONIQ_ERR_INVALID_ARG); of
- *              rows that two sequences share, either's output may stay.
- *   out        device, contiguous [n][q_heads][Dv]; rows of no sequence are left as
- *              they were.
+ *              starts[b + 1] - 1 (it may be empty).  One that is not within 0 .. n, or
+ *              begins in front of the end of any before it that is, is left out and
+ *              reported by soniq_sync_status (SONIQ_ERR_INVALID_ARG).
+ *   out        device, contiguous [n][q_heads][Dv], apart from the inputs; rows of no
+ *              sequence are left as they were.
  *   D, Dv      1..256, at most 4096 query heads and 2^30 tokens (SONIQ_ERR_UNSUPPORTED above).
  *   scale      finite, not negative.
  *   scratch    device, 16-byte aligned, of soniq_prompt_attend_scratch_bytes()

@@ -14,9 +14,15 @@ __global__ void __launch_bounds__(kThreads) prompt_rows_kernel(const PromptArgs 
     // sequences one after the other, in every warp
     int64_t done = 0;      // rows of those before
     int64_t mine = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    int taken = 0;
     for (int b = 0; b < a.B; ++b) {
-        int s, e;
-        if (!prompt_span(a, b, &s, &e)) continue;
+        const int s = a.starts[b], e = a.starts[b + 1];
+        const bool good = prompt_good(a, s, e, taken);
+        if (prompt_good(a, s, e, 0)) taken = max(taken, e);
+        if (!good) {
+            if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.err, kErrKvIndex);
+            continue;
+        }
         const int64_t rows = (int64_t)(e - s) * heads;
         for (; mine < done + rows; mine += warps) {
             const int t = s + (int)((mine - done) / heads), head = (int)((mine - done) % heads);

@@ -77,13 +77,7 @@ __device__ __noinline__ void prompt_row(const PromptArgs& a, int head, int t, in
         if (c0 + k < a.Dv) out[k] = kv_round<BF16>(acc[k] * back);
 }
 
-// Sequence b's tokens; false (and reported) where they are not within the batch.
-__device__ __forceinline__ bool prompt_span(const PromptArgs& a, int b, int* s, int* e) {
-    *s = a.starts[b];
-    *e = a.starts[b + 1];
-    if (*s >= 0 && *s <= *e && *e <= a.n) return true;
-    atomicOr(a.err, kErrKvIndex);
-    return false;
-}
+// A prompt's tokens lie within the batch, and behind those of all before it (`taken`: the end of those within the batch).
+__device__ __forceinline__ bool prompt_good(const PromptArgs& a, int s, int e, int taken) { return s >= taken && s <= e && e <= a.n; }
 
 }  // namespace soniq

@@ -42,6 +42,7 @@ namespace {
 constexpr int kTok = 128;                // tokens of a block
 constexpr int kAtom = kTok * 128;        // bytes of a 64-channel column group of a key or value block, or of a query tile
 constexpr int kMaxSlots = 12;
+constexpr int shared_of(int ctas) { return (ctas == 1 ? 227 : 113) * 1024; }      // (each CTA of an SM's 228 KB has 1 KB that it does not see)
 constexpr float kMost = 15.0f, kBegin = 8.0f;      // log2 of the largest weight, and of a row's largest when m is raised
 
 struct PromptPlan {
@@ -82,12 +83,13 @@ __device__ __forceinline__ void tmem_ld64(uint32_t at, uint32_t (&r)[64]) {
 #define SONIQ_R4(i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3])
 #define SONIQ_R16(i) SONIQ_R4(i), SONIQ_R4(i + 4), SONIQ_R4(i + 8), SONIQ_R4(i + 12)
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
-        "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,"
-        "%62,%63}, [%64];\n\ttcgen05.wait::ld.sync.aligned;"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%64];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+        "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%65];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
         : SONIQ_R16(0), SONIQ_R16(16), SONIQ_R16(32), SONIQ_R16(48)
-        : "r"(at)
+        : "r"(at), "r"(at + 32)
         : "memory");
 }
 #undef SONIQ_R16
@@ -145,8 +147,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return r;
 }
 
-template <bool BF16, int TILES>
-__global__ void __launch_bounds__(128 + 256 * TILES, 1)
+// CTAS: resident on an SM.  Two of one tile each take turns at the SM's units where prompts are short.
+template <bool BF16, int TILES, int CTAS>
+__global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
     prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ PromptPlan pl, const __grid_constant__ PromptMaps maps, unsigned* counters, const int drop) {
     extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
@@ -159,8 +162,8 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
     float* halves = reinterpret_cast<float*>(misc + 1024);            // [tile][half][128]: what the two threads of a row tell each other
     auto bar = [&](int i) { return bars + 8u * i; };
     const int unit_tokens = TILES * pl.tile_tokens;
-    constexpr int SB = 3 - TILES;                       // buffers of scores
-    constexpr int slot_cols = 512 / TILES, o_col = SB * kTok;      // TMEM columns of a tile; where its outputs begin
+    constexpr int SB = TILES * CTAS == 1 ? 2 : 1;       // buffers of scores
+    constexpr int tmem_cols = 512 / CTAS, slot_cols = tmem_cols / TILES, o_col = SB * kTok;      // TMEM columns of a tile; where its outputs begin
 
     if (tid == 0) {
         auto init = [&](int first, int n, int arrivals) {
@@ -180,7 +183,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(tmem_at)), "r"(512) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(tmem_at)), "r"(tmem_cols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc::tc_fence_before();
@@ -202,15 +205,16 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
     };
 
     Flights flights;       // of the copying warp
-    // Registers move to the softmax warps: 4 x 104 + 64 = 5 x 96 a thread.  (All four warps of a group give up theirs, or
-    // the others wait for them without end.)
+    // Registers move to the softmax warps: 4 x 104 + 64 = 5 x 96 a thread, of two CTAs 2 x 96 + 48 = 3 x 80.  (All four
+    // warps of a group give up theirs, or the others wait for them without end.)
     if (warp < 4) {
         if constexpr (TILES == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if constexpr (CTAS == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (warp == 3) {
         // ---- units: numbered prompt by prompt, later tokens first, key heads side by side ----
         const int per_unit = a.k_heads * pl.head_parts;
         int64_t base = 0;              // units of the prompts before b0
-        int b0 = 0;
+        int b0 = 0, taken = 0;         // and the end of them
         unsigned id = blockIdx.x;
         bool ok = true;
         for (uint32_t n = 0;; ++n) {
@@ -219,10 +223,19 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
             int64_t before = 0;
             while (b0 < a.B) {
                 const int b = b0 + lane;
-                int s_b = 0, e_b = 0;
-                if (b < a.B && !(blockIdx.x == 0 ? prompt_span(a, b, &s_b, &e_b)
-                                                 : (s_b = a.starts[b], e_b = a.starts[b + 1], s_b >= 0 && s_b <= e_b && e_b <= a.n)))
+                int s_b = b < a.B ? a.starts[b] : 0, e_b = b < a.B ? a.starts[b + 1] : 0;
+                // the end of the prompts before: a start that fell leaves out what begins in front of it
+                int upmost = b < a.B && prompt_good(a, s_b, e_b, 0) ? e_b : 0;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int x = __shfl_up_sync(0xffffffffu, upmost, d);
+                    if (lane >= d) upmost = max(upmost, x);
+                }
+                const int before_me = __shfl_up_sync(0xffffffffu, upmost, 1);
+                if (b < a.B && !prompt_good(a, s_b, e_b, lane ? max(before_me, taken) : taken)) {
+                    if (blockIdx.x == 0) atomicOr(a.err, kErrKvIndex);
                     s_b = e_b = 0;
+                }
                 const int64_t mine = (int64_t)((e_b - s_b + unit_tokens - 1) / unit_tokens) * per_unit;
                 int64_t upto = mine;
 #pragma unroll
@@ -240,6 +253,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
                     break;
                 }
                 base += __shfl_sync(0xffffffffu, upto, 31);
+                taken = max(taken, __shfl_sync(0xffffffffu, upmost, 31));
                 b0 += 32;
             }
             ok = wait(Bars::unit_free + (n & 1), (n >> 1) ^ 1u);
@@ -465,7 +479,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
                     kv.phase = phase;
                     if (!ok) break;
                 }
-                if (TILES == 1 && i == 0 && mine > 3) {
+                if (SB == 2 && i == 0 && mine > 3) {
                     // whole blocks, likewise
                     ok = wait(Bars::o_free, tiles ^ 1u);
                     uint32_t at = kv.i, phase = kv.phase;
@@ -558,6 +572,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
     }
     } else {
         if constexpr (TILES == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        if constexpr (CTAS == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
         // ---- softmax of tile s: two threads to a row, each with half of a block's keys ----
         const int s = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1, quad = warp & 3, row = quad * 32 + lane;
         const uint32_t t_s = tmem + s * slot_cols + ((uint32_t)(quad * 32) << 16);
@@ -751,7 +766,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, 1)
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
-    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols) : "memory");
 }
 
 // [tokens][heads][channels] in boxes of 64 channels.
@@ -775,21 +790,21 @@ bool mapped(const PromptSide& x, int64_t n, int heads, bool shared_heads) {
            (heads == 1 || (x.head == 0 ? shared_heads : x.head > 0 && x.head % 8 == 0 && x.head < far / 2));
 }
 
-// Asks for all of the shared memory, once per device and kernel (`which`).
-cudaError_t prepared(const void* kernel, int which) {
+// Asks for the shared memory, once per device and kernel (`which`).
+cudaError_t prepared(const void* kernel, int which, int shared) {
     static std::atomic<uint32_t> done[64];
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
     const bool known = device >= 0 && device < 64;
     if (known && (done[device].load(std::memory_order_relaxed) >> which & 1u) != 0) return cudaSuccess;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
     if (e == cudaSuccess) e = prefer_max_shared(kernel);
     if (e == cudaSuccess && known) done[device].fetch_or(1u << which, std::memory_order_relaxed);
     return e;
 }
 
-bool make_plan(const PromptArgs& a, int tiles, PromptPlan* p) {
+bool make_plan(const PromptArgs& a, int tiles, int ctas, PromptPlan* p) {
     p->row_heads = a.group < 128 ? a.group : 128;
     p->tile_tokens = 128 / p->row_heads;
     p->head_parts = (a.group + p->row_heads - 1) / p->row_heads;
@@ -797,14 +812,14 @@ bool make_plan(const PromptArgs& a, int tiles, PromptPlan* p) {
     p->v_atoms = (a.Dv + 63) / 64;
     p->o_cols = (a.Dv + 15) / 16 * 16;
     p->wide_rows = a.Dv % 16 == 0 && (uintptr_t)a.out % 32 == 0;
-    if ((3 - tiles) * kTok + p->o_cols > 512 / tiles) return false;
+    if ((tiles * ctas == 1 ? 2 : 1) * kTok + p->o_cols > 512 / (tiles * ctas)) return false;
     p->slot_bytes = (p->k_atoms > 1 || p->v_atoms > 1 ? 2 : 1) * kAtom;
     p->ring_off = tiles * p->k_atoms * kAtom;
-    p->slots = (227 * 1024 - kMisc - p->ring_off) / p->slot_bytes;
+    p->slots = (shared_of(ctas) - kMisc - p->ring_off) / p->slot_bytes;
     if (p->slots > kMaxSlots) p->slots = kMaxSlots;
     p->misc_off = p->ring_off + p->slots * p->slot_bytes;
     p->smem = p->misc_off + kMisc;
-    return p->slots >= 3;
+    return p->slots >= 3 || (ctas == 2 && p->slots >= 2);
 }
 
 }  // namespace
@@ -816,10 +831,15 @@ bool prompt_tile_supported(const PromptArgs& a) {
 
 cudaError_t launch_prompt_tile(const PromptArgs& a, bool bf16, unsigned* counters, cudaStream_t st) {
     PromptPlan p{};
-    int tiles = 2;
-    if (!make_plan(a, 2, &p)) {
-        tiles = 1;
-        if (!make_plan(a, 1, &p)) return cudaErrorNotSupported;
+    int tiles = 1, ctas = 2;
+    const bool small = (int64_t)a.n * (a.group < 128 ? a.group : 128) <= 128 * (int64_t)a.B;
+    if (!small || !make_plan(a, 1, 2, &p)) {
+        ctas = 1;
+        tiles = 2;
+        if (!make_plan(a, 2, 1, &p)) {
+            tiles = 1;
+            if (!make_plan(a, 1, 1, &p)) return cudaErrorNotSupported;
+        }
     }
     PromptMaps maps;
     if (!encode(a.q, bf16, a.n, a.k_heads * a.group, a.D, p.row_heads, p.tile_tokens, &maps.q) ||
@@ -829,10 +849,11 @@ cudaError_t launch_prompt_tile(const PromptArgs& a, bool bf16, unsigned* counter
     const int64_t unit_tokens = tiles * p.tile_tokens;
     const int64_t units = ((int64_t)a.n / unit_tokens + (a.B < a.n ? a.B : a.n)) * a.k_heads * p.head_parts;
     if (units > 2000000000) return cudaErrorNotSupported;      // they are numbered in 32 bits
-    const int grid = (int)(units < num_sms() ? units : num_sms());
-    auto* kernel = tiles == 2 ? (bf16 ? prompt_tile_kernel<true, 2> : prompt_tile_kernel<false, 2>)
-                              : (bf16 ? prompt_tile_kernel<true, 1> : prompt_tile_kernel<false, 1>);
-    const cudaError_t e = prepared(reinterpret_cast<const void*>(kernel), 2 * (tiles - 1) + bf16);
+    const int most = ctas * num_sms(), grid = (int)(units < most ? units : most);
+    auto* kernel = ctas == 2 ? (bf16 ? prompt_tile_kernel<true, 1, 2> : prompt_tile_kernel<false, 1, 2>)
+                             : (tiles == 2 ? (bf16 ? prompt_tile_kernel<true, 2, 1> : prompt_tile_kernel<false, 2, 1>)
+                                           : (bf16 ? prompt_tile_kernel<true, 1, 1> : prompt_tile_kernel<false, 1, 1>));
+    const cudaError_t e = prepared(reinterpret_cast<const void*>(kernel), 2 * (tiles - 1 + 2 * (ctas - 1)) + bf16, shared_of(ctas));
     if (e != cudaSuccess) return e;
     kernel<<<grid, 128 + 256 * tiles, p.smem, st>>>(a, p, maps, counters, take_drop_arrival() ? 1 : 0);
     note_launch();
