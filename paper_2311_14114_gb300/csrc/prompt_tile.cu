@@ -428,13 +428,13 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
             if (mine == 0) warp_arrive(bar(Bars::q_free));
 #pragma unroll 1
             for (int i = -SB; ok && i < blocks; ++i) {
-                if (TILES == 2 && plain && i == 0 && mine > 2) {
+                if (TILES == 2 && plain && i == 0 && mine > 1) {
                     // Whole blocks of up to 128 channels, with few questions on the way: the warp's instructions come from the
                     // cache that the softmax warps sweep, some 5 cycles each.
                     ok = wait(Bars::o_free + s, tiles ^ 1u);
                     uint32_t at = kv.i, phase = kv.phase;
 #pragma unroll 1
-                    for (; ok && i + 2 < mine; ++i) {
+                    for (; ok && i + 1 < mine; ++i) {
                         const uint32_t v_at = at, v_phase = phase;
                         if (++at == (uint32_t)pl.slots) at = 0, phase ^= 1u;
                         const uint32_t k_at = at, k_phase = phase;
@@ -444,7 +444,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
                         if (!ok) break;
                         tc::tc_fence_after();
                         const uint64_t v = value_desc(ring + v_at * pl.slot_bytes, kAtom), k = tc::sw128_desc(ring + k_at * pl.slot_bytes);
-                        const uint32_t id = fmt | (1u << 16) | columns(pl.o_cols);
+                        const uint32_t id = fmt | (1u << 16) | columns(pl.o_cols), id_s = fmt | columns(i + 2 == mine ? last_keys : kTok);
 #pragma unroll
                         for (int h = 0; h < 8; ++h) {
                             if (h == 4) {
@@ -455,7 +455,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
                         }
                         warp_commit(bar(Bars::free + v_at));
                         auto step = [&](int h) {
-                            warp_mma_ss(t_s, q_tile + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), k + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), fmt | columns(kTok), h != 0);
+                            warp_mma_ss(t_s, q_tile + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), k + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), id_s, h != 0);
                         };
                         int h = 0;
                         if (steps >= 4) {
@@ -472,6 +472,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
                         }
                         warp_commit(bar(Bars::free + k_at));
                         warp_commit(bar(Bars::s_full + 2 * s));
+                        if (i + 2 == mine) warp_commit(bar(Bars::q_free));
                         warp_arrive(bar(Bars::turn + (s ^ 1)));
                         ++turns;
                     }
@@ -479,7 +480,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
                     kv.phase = phase;
                     if (!ok) break;
                 }
-                if (SB == 2 && i == 0 && mine > 3) {
+                if (SB == 2 && i == 0 && mine > 2) {
                     // whole blocks, likewise
                     ok = wait(Bars::o_free, tiles ^ 1u);
                     uint32_t at = kv.i, phase = kv.phase;
@@ -487,7 +488,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
                         if (++at == (uint32_t)pl.slots) at = 0, phase ^= 1u;
                     };
 #pragma unroll 1
-                    for (; ok && i + 3 < mine; ++i) {
+                    for (; ok && i + 2 < mine; ++i) {
                         const uint32_t b = (done + i) & 1u, t_b = t_s + b * kTok, half_round = (done + i) >> 1;
 #pragma unroll 1
                         for (int c = 0; c < v_pieces; ++c) {
@@ -509,6 +510,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
                         }
                         if (!ok) break;
                         warp_commit(bar(Bars::pv_done));
+                        const uint32_t id_s = fmt | columns(i + 3 == mine ? last_keys : kTok);
 #pragma unroll 1
                         for (int c = 0; c < k_pieces; ++c) {
                             ok = wait(Bars::full + at, phase);
@@ -516,7 +518,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
                             tc::tc_fence_after();
                             const uint64_t k = tc::sw128_desc(ring + at * pl.slot_bytes), q = q_tile + c * 2 * (kAtom >> 4);
                             auto step = [&](int h, uint32_t acc) {
-                                warp_mma_ss(t_b, q + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), k + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), fmt | columns(kTok), acc);
+                                warp_mma_ss(t_b, q + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), k + (h >> 2) * (kAtom >> 4) + 2 * (h & 3), id_s, acc);
                             };
                             if (steps - 8 * c >= 8) {
 #pragma unroll
@@ -530,6 +532,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
                         }
                         if (!ok) break;
                         warp_commit(bar(Bars::s_full + b));
+                        if (i + 3 == mine) warp_commit(bar(Bars::q_free));
                     }
                     kv.i = at;
                     kv.phase = phase;
@@ -699,7 +702,8 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
             *mine_at = l;
             if (either(!ok)) break;
             tc::tc_fence_after();
-            const float inv = 1.0f / (half ? *other_at + l : l + *other_at);
+            float inv;                     // (sums are 2^8 or more: their reciprocals are normal numbers)
+            asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(l + *other_at));
             uint16_t* out = a.out + ((int64_t)(u.start + token) * heads + u.kv_head * a.group + head) * a.Dv;
             // (Rows of their own are 32 of them to an instruction, 32 bytes each.  Four lanes that first exchange pieces, to
             // write 64 bytes of a row together, halve what the memory pipe does but take 300 instructions instead of 120, in
