@@ -71,8 +71,11 @@ struct Grow {
         const int64_t page = (int64_t)1 << a.page_shift;
         old = max(n, 0);
         goal = max(t, 0);
-        has = (int)min((old + page - 1) >> a.page_shift, (int64_t)a.max_pages);
+        has = pages(a, old);
         to = (int)((goal + page - 1) >> a.page_shift);
+    }
+    __device__ __forceinline__ static int pages(const KvPlanArgs& a, int old) {
+        return (int)min((old + ((int64_t)1 << a.page_shift) - 1) >> a.page_shift, (int64_t)a.max_pages);
     }
     __device__ __forceinline__ int tokens() const { return max(goal - old, 0); }
     __device__ __forceinline__ int back() const { return max(has - to, 0); }
@@ -88,7 +91,9 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a) {
     int32_t* start = mem;                    // [B + 1] first token, at most max_tokens
     int32_t* back0 = start + B + 1;          // [B + 1] first page given back
     int32_t* need0 = back0 + B + 1;          // [B + 1] first page needed
-    uint8_t* served = reinterpret_cast<uint8_t*>(need0 + B + 1);
+    int32_t* old_of = need0 + B + 1;         // [B] tokens before
+    int32_t* to_of = old_of + B;             // [B] pages after
+    uint8_t* served = reinterpret_cast<uint8_t*>(to_of + B);
 
     // ---- tokens and pages given back, pages needed; a thread takes neighbouring sequences ----
     const int per = (B + kThreads - 1) / kThreads, b0 = min(tid * per, B), b1 = min(b0 + per, B);
@@ -106,6 +111,8 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a) {
         const Grow g(a, b);
         start[b] = (int32_t)min(at.a, cap);
         back0[b] = (int32_t)at.b;
+        old_of[b] = g.old;
+        to_of[b] = g.to;
         at.a += g.tokens();
         at.b += g.back();
         const bool fits = g.to <= a.max_pages && at.a <= cap;
@@ -139,15 +146,16 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a) {
         if ((unsigned)page >= (unsigned)a.n_pages) atomicOr(a.err, kErrKvIndex);
         return page;
     };
+    auto has_of = [&](int b) { return Grow::pages(a, old_of[b]); };
     auto released = [&](int k) {
         const int b = last_upto(back0, B, k);
-        return checked(a.table[b * a.table_stride + Grow(a, b).to + k - back0[b]]);
+        return checked(a.table[b * a.table_stride + to_of[b] + k - back0[b]]);
     };
     auto given = [&](int k) { return k < R ? released(k) : checked(a.free_pages[pool - 1 - (k - (int)R)]); };
     const int first = blockIdx.x * kThreads + tid, step = gridDim.x * kThreads;
     for (int k = first; k < taken; k += step) {
         const int b = last_upto(need0, B, k);
-        a.table[b * a.table_stride + Grow(a, b).has + k - need0[b]] = given(k);
+        a.table[b * a.table_stride + has_of(b) + k - need0[b]] = given(k);
     }
     for (int64_t k = (int64_t)taken + first; k < R; k += step) {
         const int64_t to = pool + R - 1 - k;
@@ -161,11 +169,10 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a) {
         if (t < tokens) {
             // (of the sequences that start at t, the last: the others have no tokens)
             const int b = last_upto(start, B - 1, (int)t);
-            const Grow g(a, b);
-            pos = g.old + ((int)t - start[b]);
+            pos = old_of[b] + ((int)t - start[b]);
             if (served[b]) {
-                const int i = pos >> a.page_shift;
-                const int page = i < g.has ? a.table[b * a.table_stride + i] : given(need0[b] + i - g.has);
+                const int i = pos >> a.page_shift, has = has_of(b);
+                const int page = i < has ? a.table[b * a.table_stride + i] : given(need0[b] + i - has);
                 const int64_t size = (int64_t)1 << a.page_shift;
                 slot = (unsigned)page < (unsigned)a.n_pages ? page * size + (pos & (size - 1)) : a.n_pages * size;
             }
@@ -199,13 +206,13 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a) {
 }  // namespace
 
 cudaError_t launch_kv_plan(const KvPlanArgs& a, cudaStream_t st) {
-    const int smem = 12 * (a.B + 1) + a.B;
-    if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kv_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return e;
-    }
-    // two tokens to a thread, or eight sequences, whose pages are not known here, to a warp
-    const int64_t by_tokens = ((int64_t)a.max_tokens + 2 * kThreads - 1) / (2 * kThreads), by_pages = (a.B + 127) / 128;
+    const int smem = 12 * (a.B + 1) + 9 * a.B;
+    cudaError_t e = prefer_max_shared(reinterpret_cast<const void*>(kv_plan_kernel));
+    if (e == cudaSuccess && smem > 48 * 1024)
+        e = cudaFuncSetAttribute(kv_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    // two tokens to a thread, or one sequence, whose pages are not known here, to a warp
+    const int64_t by_tokens = ((int64_t)a.max_tokens + 2 * kThreads - 1) / (2 * kThreads), by_pages = (a.B + 15) / 16;
     const int64_t want = by_tokens > by_pages ? by_tokens : by_pages;
     const int grid = (int)(want < 1 ? 1 : (want < num_sms() ? want : num_sms()));
     kv_plan_kernel<<<grid, kThreads, smem, st>>>(a);

@@ -26,7 +26,7 @@ namespace soniq {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kAhead = 8;      // groups of rows, 1 KB each, that a warp has on their way
+constexpr int kAhead = 4;      // groups of rows, 1 KB each, that a warp has on their way (8: 72 us for 16384 tokens x 40 heads, not 67)
 
 // 16 bytes into shared memory, or zeros; this thread sees them after cp.async.wait_group.
 __device__ __forceinline__ void copy16(uint32_t to, const void* from, bool on) {
@@ -310,9 +310,9 @@ template <bool BF16>
 cudaError_t launch(const RotateArgs& a, bool vectors, cudaStream_t st) {
     const int lanes = !vectors ? 32 : (a.D <= 64 ? 4 : (a.D <= 128 ? 8 : 16)), rows = 32 / lanes;
     const int groups = (a.side[0].heads + rows - 1) / rows + (a.side[1].heads + rows - 1) / rows;
-    // a token's heads are shared by warps until there are eight for each scheduler
-    const int64_t want = ((int64_t)num_sms() * 32 + a.n - 1) / a.n;
-    const int parts = (int)(want < groups ? want : groups);
+    // a token's heads are shared by warps as long as all of them are at work at once
+    const int64_t want = (int64_t)num_sms() * (2 * kThreads / 32) / a.n;
+    const int parts = (int)(want < 1 ? 1 : (want < groups ? want : groups));
     const int64_t grid = (a.n * parts + kThreads / 32 - 1) / (kThreads / 32);
     if (grid > 2147483647) return cudaErrorNotSupported;
     auto pick = [&](auto* by4, auto* by8, auto* by16) { return lanes == 4 ? by4 : (lanes == 8 ? by8 : by16); };
@@ -320,10 +320,8 @@ cudaError_t launch(const RotateArgs& a, bool vectors, cudaStream_t st) {
                             : (a.interleaved ? pick(rotate_kernel<BF16, 4, true>, rotate_kernel<BF16, 8, true>, rotate_kernel<BF16, 16, true>)
                                              : pick(rotate_kernel<BF16, 4, false>, rotate_kernel<BF16, 8, false>, rotate_kernel<BF16, 16, false>));
     const int smem = vectors ? kThreads / 32 * kAhead * 1024 : 0;
-    if (smem > 0) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return e;
-    }
+    const cudaError_t e = prefer_max_shared(reinterpret_cast<const void*>(kernel));
+    if (e != cudaSuccess) return e;
     kernel<<<(unsigned)grid, kThreads, smem, st>>>(a, parts);
     note_launch();
     return cudaGetLastError();
