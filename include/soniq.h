@@ -652,9 +652,8 @@ typedef struct soniq_heads {
  *   D          1..256 (SONIQ_ERR_UNSUPPORTED above); at most 4096 heads a side.
  *   eps        finite, not negative.
  * Pointers need the alignment of their elements.  Rows that are 16-byte pieces (D
- * and strides multiples of 8, pointers on 16 bytes) whose pairs lie whole pieces
- * apart (interleaved, or channels a multiple of 16) are moved in those; others by
- * a slower kernel.
+ * and strides multiples of 8, pointers on 16 bytes) are moved in those, others by a
+ * slower kernel.
  */
 SONIQ_API soniq_status soniq_rotate_heads(const soniq_rotary *rotary, const int32_t *positions, int64_t n, int32_t D,
                                           int32_t dtype, const soniq_heads *q, const soniq_heads *k, float eps,

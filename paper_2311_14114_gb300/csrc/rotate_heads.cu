@@ -14,8 +14,12 @@
 // A warp takes a token, or a share of its heads; its lanes work out the token's
 // cosines and sines, and each keeps those of its sixteen channels for all heads.
 // Rows are read and written in 16-byte pieces, four rows of 128 channels to a warp.
-// Rows that are no 16-byte pieces, or whose partners are not whole pieces apart,
-// take rotate_scalar_kernel, a channel to a lane.
+// Rows that are no 16-byte pieces take rotate_scalar_kernel, a channel to a lane.
+//
+// Bound by memory where there are many tokens: 16384 tokens x 40 heads of 128, bf16,
+// slices of a fused projection, take 67 us (335 MB, 5.0 TB/s; a copy of as many
+// bytes takes 56).  Few tokens are bound by the chain position - turns - cosines -
+// rows - squares - stores: 8 tokens 6 us, 1001 x 24 heads of 80 8 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -31,6 +35,11 @@ constexpr int kAhead = 4;      // groups of rows, 1 KB each, that a warp has on 
 // 16 bytes into shared memory, or zeros; this thread sees them after cp.async.wait_group.
 __device__ __forceinline__ void copy16(uint32_t to, const void* from, bool on) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ uint32_t read2(uint32_t at) {
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at) : "memory");
+    return v;
 }
 __device__ __forceinline__ uint4 read16(uint32_t at) {
     uint4 v;
@@ -96,13 +105,17 @@ __device__ __forceinline__ float norm_factor(const float (&x)[N], const RotateAr
     return f;
 }
 
-// LANES: lanes of a row, two pieces of eight channels each, so that a pair's two
-// channels are in one lane: in the half layout the pieces stand half of the turned
-// channels apart, interleaved they follow each other.  Of a pair (x, y) the kernel
-// keeps x in a[] and y in b[], and writes
+enum Pairs { kApart, kNeighbours, kAnywhere };
+
+// LANES: lanes of a row, two pieces of eight channels each.  Where they can a
+// pair's two channels are in one lane: apart by whole pieces (kApart), the pieces
+// stand half of the turned channels apart; neighbours are in one piece.  Of such a
+// pair (x, y) the kernel writes
 //   f (x cx + y sx), f (y cy + x sy)
-// with the gains in the coefficients; f is the row's norm.
-template <bool BF16, int LANES, bool INTERLEAVED>
+// with the gains in the coefficients; f is the row's norm.  Of pairs that stand
+// otherwise (kAnywhere) a lane reads the partners of its channels from the rows in
+// shared memory.
+template <bool BF16, int LANES, int PAIRS>
 __global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const __grid_constant__ RotateArgs a, const int parts) {
     constexpr int ROWS = 32 / LANES;
     const int lane = threadIdx.x & 31, sub = lane / LANES, l = lane % LANES;
@@ -111,10 +124,12 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const __grid_consta
     const int part = (int)(task - token * parts);
     if (token >= a.n) return;
     const int half = a.channels / 2;
-    // this lane's pieces: of the turned ones in the half layout a pair, of the others two neighbours
-    int c0 = 16 * l, c1 = 16 * l + 8;
-    bool turned = c0 < a.channels;
-    if (!INTERLEAVED && turned) {
+    // This lane's pieces: of channels turned in kApart a pair of pieces; else one each of the first and the second half of
+    // the row's (of those that are not turned), so that neighbouring lanes have neighbouring pieces.
+    const bool turned = PAIRS != kApart || 16 * l < a.channels;
+    const int base = PAIRS == kApart ? a.channels : 0, l0 = l - base / 16, pieces = (a.D - base) / 8, upper = (pieces + 1) / 2;
+    int c0 = l0 < upper ? base + 8 * l0 : a.D, c1 = l0 < upper && l0 + upper < pieces ? base + 8 * (l0 + upper) : a.D;
+    if (PAIRS == kApart && turned) {
         c0 = 8 * l;
         c1 = half + 8 * l;
     }
@@ -159,11 +174,22 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const __grid_consta
         __syncwarp();
     }
     // what a channel's partner counts for: nothing where it is not turned, even if it is an infinity
-    auto pair_of = [&](int i) { return INTERLEAVED ? c0 / 2 + i : c0 + i; };
-    uint32_t counts = 0;
+    auto pair_of = [&](int i) { return PAIRS == kNeighbours ? (i < 4 ? c0 / 2 + i : c1 / 2 + i - 4) : c0 + i; };
+    auto channel = [&](int k) { return k < 8 ? c0 + k : c1 + k - 8; };
+    uint32_t counts = 0;       // by pair, or (kAnywhere) by channel
+    uint16_t mate[PAIRS == kAnywhere ? 16 : 1];        // where the partner's value stands in the group's 1 KB
+    if constexpr (PAIRS == kAnywhere) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) counts |= (uint32_t)(turned && pair_of(i) < half) << i;
-    const bool all = __all_sync(0xffffffffu, counts == 0xffu || !in0);
+        for (int k = 0; k < 16; ++k) {
+            const int c = channel(k), p = c < half ? c + half : c - half, j = p >> 3;
+            counts |= (uint32_t)(c < a.channels) << k;
+            mate[k] = (uint16_t)(c < a.channels ? (j < upper ? 16 * (sub * LANES + j) : 512 + 16 * (sub * LANES + j - upper)) + 2 * (p & 7) : 0);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) counts |= (uint32_t)(turned && pair_of(i) < half) << i;
+    }
+    const bool all = PAIRS != kAnywhere && __all_sync(0xffffffffu, (counts | (in1 ? 0u : 0xf0u)) == 0xffu || !in0);
     // ---- the heads: queries, then keys ----
     uint32_t get = 0;
 #pragma unroll 1
@@ -181,14 +207,27 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const __grid_consta
             g0[i] = p.x, g0[i + 1] = p.y, g0[i + 2] = p.z, g0[i + 3] = p.w;
             g1[i] = q.x, g1[i + 1] = q.y, g1[i + 2] = q.z, g1[i + 3] = q.w;
         }
+        // of pairs: (cx, sx) and (cy, sy); of channels: cx and sx of the first eight, cy and sy of the others
         float cx[8], sx[8], cy[8], sy[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float gx = INTERLEAVED ? (i < 4 ? g0[2 * i] : g1[2 * i - 8]) : g0[i];
-            const float gy = INTERLEAVED ? (i < 4 ? g0[2 * i + 1] : g1[2 * i - 7]) : g1[i];
-            const float2 t = counts >> i & 1u ? mine[pair_of(i)] : make_float2(1.0f, 0.0f);
-            cx[i] = t.x * gx, sx[i] = -t.y * gy;
-            cy[i] = t.x * gy, sy[i] = t.y * gx;
+            if constexpr (PAIRS == kAnywhere) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int c = channel(8 * h + i);
+                    const bool on = c < a.channels, first = c < half;
+                    const float2 t = on ? mine[first ? c : c - half] : make_float2(1.0f, 0.0f);
+                    const float mates = on && norm ? side.gain[first ? c + half : c - half] : 1.0f;
+                    (h ? cy : cx)[i] = t.x * (h ? g1 : g0)[i];
+                    (h ? sy : sx)[i] = (first ? -t.y : t.y) * mates;
+                }
+            } else {
+                const float gx = PAIRS == kNeighbours ? (i < 4 ? g0[2 * i] : g1[2 * i - 8]) : g0[i];
+                const float gy = PAIRS == kNeighbours ? (i < 4 ? g0[2 * i + 1] : g1[2 * i - 7]) : g1[i];
+                const float2 t = counts >> i & 1u ? mine[pair_of(i)] : make_float2(1.0f, 0.0f);
+                cx[i] = t.x * gx, sx[i] = -t.y * gy;
+                cy[i] = t.x * gy, sy[i] = t.y * gx;
+            }
         }
         uint16_t* to = side.out + token * side.out_token + (int64_t)(first * ROWS + sub) * side.out_head;
         const int64_t to_step = ROWS * side.out_head;
@@ -196,6 +235,13 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const __grid_consta
 #pragma unroll 1
         for (int g = 0; g < n; ++g, to += to_step, rows -= ROWS) {
             asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+            float mates[PAIRS == kAnywhere ? 16 : 1];
+            if constexpr (PAIRS == kAnywhere) {
+                __syncwarp();       // all of the group's rows are there
+#pragma unroll
+                for (int k = 0; k < 16; ++k)
+                    mates[k] = counts >> k & 1u ? load2<BF16>(read2(place - 16 * lane + get + mate[k])).x : 0.0f;
+            }
             const uint4 p0 = read16(place + get), p1 = read16(place + get + 512);
             get = (get + 1024) % (kAhead * 1024);
             const uint32_t w[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
@@ -206,39 +252,41 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const __grid_consta
                 v[2 * k] = pair.x;
                 v[2 * k + 1] = pair.y;
             }
+            if constexpr (PAIRS == kAnywhere) __syncwarp();       // their places are read
             fetch();
             float f = 1.0f, up = 1.0f;
             if (norm) {
                 f = norm_factor<LANES>(v, a, &up);
                 if (up != 1.0f) {
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) v[k] *= up;
-                }
-            }
-            float x[8], y[8], z[8], u[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                x[k] = INTERLEAVED ? v[2 * k] : v[k];
-                y[k] = INTERLEAVED ? v[2 * k + 1] : v[8 + k];
-            }
-            if (all) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    z[k] = fmaf(y[k], sx[k], x[k] * cx[k]) * f;
-                    u[k] = fmaf(x[k], sy[k], y[k] * cy[k]) * f;
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const bool on = counts >> k & 1u;
-                    z[k] = fmaf(on ? y[k] : 0.0f, sx[k], x[k] * cx[k]) * f;
-                    u[k] = fmaf(on ? x[k] : 0.0f, sy[k], y[k] * cy[k]) * f;
+                    for (int k = 0; k < 16; ++k) {
+                        v[k] *= up;
+                        if constexpr (PAIRS == kAnywhere) mates[k] *= up;
+                    }
                 }
             }
             uint32_t r[8];
+            if constexpr (PAIRS == kAnywhere) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                r[k] = INTERLEAVED ? round2<BF16>(z[k], u[k]) : (k < 4 ? round2<BF16>(z[2 * k], z[2 * k + 1]) : round2<BF16>(u[2 * k - 8], u[2 * k - 7]));
+                for (int k = 0; k < 16; k += 2) {
+                    const float* c = k < 8 ? cx + k : cy + k - 8;
+                    const float* d = k < 8 ? sx + k : sy + k - 8;
+                    r[k / 2] = round2<BF16>(fmaf(mates[k], d[0], v[k] * c[0]) * f, fmaf(mates[k + 1], d[1], v[k + 1] * c[1]) * f);
+                }
+            } else {
+                float z[8], u[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float x = PAIRS == kNeighbours ? v[2 * k] : v[k], y = PAIRS == kNeighbours ? v[2 * k + 1] : v[8 + k];
+                    const bool on = all || (counts >> k & 1u) != 0;
+                    z[k] = fmaf(on ? y : 0.0f, sx[k], x * cx[k]) * f;
+                    u[k] = fmaf(on ? x : 0.0f, sy[k], y * cy[k]) * f;
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    r[k] = PAIRS == kNeighbours ? round2<BF16>(z[k], u[k])
+                                                : (k < 4 ? round2<BF16>(z[2 * k], z[2 * k + 1]) : round2<BF16>(u[2 * k - 8], u[2 * k - 7]));
+            }
             if (rows > 0 && in0) *reinterpret_cast<uint4*>(to + c0) = make_uint4(r[0], r[1], r[2], r[3]);
             if (rows > 0 && in1) *reinterpret_cast<uint4*>(to + c1) = make_uint4(r[4], r[5], r[6], r[7]);
         }
@@ -306,6 +354,11 @@ __global__ void __launch_bounds__(kThreads) rotate_scalar_kernel(const __grid_co
     }
 }
 
+template <bool BF16, int PAIRS>
+auto* kernel_of(int lanes) {
+    return lanes == 4 ? rotate_kernel<BF16, 4, PAIRS> : (lanes == 8 ? rotate_kernel<BF16, 8, PAIRS> : rotate_kernel<BF16, 16, PAIRS>);
+}
+
 template <bool BF16>
 cudaError_t launch(const RotateArgs& a, bool vectors, cudaStream_t st) {
     const int lanes = !vectors ? 32 : (a.D <= 64 ? 4 : (a.D <= 128 ? 8 : 16)), rows = 32 / lanes;
@@ -315,10 +368,9 @@ cudaError_t launch(const RotateArgs& a, bool vectors, cudaStream_t st) {
     const int parts = (int)(want < 1 ? 1 : (want < groups ? want : groups));
     const int64_t grid = (a.n * parts + kThreads / 32 - 1) / (kThreads / 32);
     if (grid > 2147483647) return cudaErrorNotSupported;
-    auto pick = [&](auto* by4, auto* by8, auto* by16) { return lanes == 4 ? by4 : (lanes == 8 ? by8 : by16); };
     auto* kernel = !vectors ? rotate_scalar_kernel<BF16>
-                            : (a.interleaved ? pick(rotate_kernel<BF16, 4, true>, rotate_kernel<BF16, 8, true>, rotate_kernel<BF16, 16, true>)
-                                             : pick(rotate_kernel<BF16, 4, false>, rotate_kernel<BF16, 8, false>, rotate_kernel<BF16, 16, false>));
+                            : (a.interleaved ? kernel_of<BF16, kNeighbours>(lanes)
+                                             : (a.channels % 16 == 0 ? kernel_of<BF16, kApart>(lanes) : kernel_of<BF16, kAnywhere>(lanes)));
     const int smem = vectors ? kThreads / 32 * kAhead * 1024 : 0;
     const cudaError_t e = prefer_max_shared(reinterpret_cast<const void*>(kernel));
     if (e != cudaSuccess) return e;
@@ -334,7 +386,7 @@ bool pieces(const void* p, int64_t token, int64_t head, int64_t n, int heads) {
 }  // namespace
 
 cudaError_t launch_rotate_heads(const RotateArgs& a, bool bf16, cudaStream_t st) {
-    bool vectors = a.D % 8 == 0 && (a.interleaved || a.channels % 16 == 0);
+    bool vectors = a.D % 8 == 0;
     for (const RotateSide& s : a.side)
         if (s.heads > 0)
             vectors = vectors && pieces(s.in, s.in_token, s.in_head, a.n, s.heads) &&

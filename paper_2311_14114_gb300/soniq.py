@@ -7,6 +7,7 @@ no GPU is present the calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -654,8 +655,9 @@ def kv_plan(pages: KVPages, lengths: torch.Tensor, targets: torch.Tensor, max_to
         raise ValueError("count_out must be an int32 tensor on the current CUDA device")
     if out is None:
         dev, cap = lengths.device, max(max_tokens, 0)
-        out = KVStep(_new((B + 1,), i32, dev, stream), _new((cap,), i32, dev, stream), _new((cap,), torch.int64, dev, stream),
-                     _new((B,), i32, dev, stream))
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            out = KVStep(torch.empty(B + 1, dtype=i32, device=dev), torch.empty(cap, dtype=i32, device=dev),
+                         torch.empty(cap, dtype=torch.int64, device=dev), torch.empty(B, dtype=i32, device=dev))
     else:
         for t, dtype, n, name in zip(out, (i32, i32, torch.int64, i32), (B + 1, max_tokens, max_tokens, B), KVStep._fields):
             _need_here(t, dtype, n, here, "out." + name)
