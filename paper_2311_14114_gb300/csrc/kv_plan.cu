@@ -15,8 +15,10 @@
 // entries below `has` are read, the others written.  Lengths and the count, which
 // may be updated in place, are written by the last CTA to have read them.
 //
-// Bound by latency: 8 sequences 1 CTA, two dependent reads (lengths, then table
-// entries), the prefix sums' four barriers and the launch.
+// Bound by latency: the launch, two dependent reads (lengths, then table entries),
+// the prefix sums' barriers, bisections.  Measured, replayed from a graph (GB300): 8
+// sequences that decode 6.2 us, 1000 of which some leave 12.3, 32 prompts of up to
+// 4000 tokens 10.3.
 #include "step_internal.h"
 
 namespace soniq {
