@@ -77,8 +77,9 @@ __device__ __noinline__ void prompt_row(const PromptArgs& a, int head, int t, in
         best = fmaxf(best, top);
         nan = __any_sync(0xffffffffu, mine != mine) || best == INFINITY;
         if (nan) break;
-        if (best == -INFINITY) continue;
-        const float down = exp2f((top - best) * factor), w = exp2f((mine - best) * factor), part = ldexpf(w, -spare);
+        // (keys of scores minus infinity alone: no weight, and 0 times a value that is not finite is NaN here too)
+        const float from = best == -INFINITY ? 0.0f : best;
+        const float down = exp2f((top - from) * factor), w = exp2f((mine - from) * factor), part = ldexpf(w, -spare);
         top = best;
         sum = fmaf(sum, down, w);
 #pragma unroll

@@ -182,6 +182,31 @@ def test_what_a_row_does_not_see(sq, D, dtype, bad):
     assert got[100, 1].isnan().all() and got[300].isnan().all()
 
 
+@pytest.mark.parametrize("D", [64, 128, 256, 33])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_tokens_of_no_weight(sq, D, dtype):
+    """The first 100 tokens' scores are minus infinity: they add nothing, the rows that
+    see no others are NaN, and so is what sees a NaN or an infinity in their values
+    (0 times it), wherever that stands among them."""
+    lens = [170, 5]
+    q, k, v, starts = draw(15, lens, 2, 2, D, D, dtype)
+    q[:, :, 0] = 1.0
+    k[:100, :, 0] = -float("inf")
+    for t in (None, 0, 31, 63, 64, 96, 99):
+        for bad in (float("nan"), float("inf")):
+            y = v.clone()
+            if t is not None:
+                y[t, :, 0] = bad
+            got = sq.prompt_attend(q, k, y, ints(starts))
+            assert got[:100].isnan().all()
+            ref = step_plain.attend(q[100:].double(), k[100:].double(), v[100:].double(), [0, 70, 75], True, D ** -0.5)
+            ok = (got[100:].double() - ref[0]).abs() <= step_plain.attend_tolerance(*ref, 170, dtype)
+            seen = torch.zeros_like(ok)
+            if t is not None:
+                seen[:70, :, 0] = True
+            assert ok[~seen].all() and got[100:][seen].isnan().all()
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("D", [64, 128, 256])
 def test_scores_of_any_size(sq, dtype, D):
