@@ -756,6 +756,8 @@ def rotate_heads(rotary: Optional[Rotary], q: Optional[torch.Tensor], k: Optiona
         if positions is None:
             raise ValueError("positions are needed to turn by")
         _need_here(positions, torch.int32, n, here, "positions")
+        if rotary.turns.get_device() != here:
+            raise ValueError("rotary must have been made for the current CUDA device")
     cq = ck = None
     if q is not None:
         q_out, cq = _heads(q, n, D, dtype, q_gain, q_out, here, "q", stream)

@@ -178,3 +178,10 @@ def test_offsets_past_32_bits(sq):
     want = check(sq, x.contiguous(), None, rotary, pos)[0]
     sq.rotate_heads(rotary, x, None, pos, q_out=x)
     assert torch.equal(x, want)
+
+
+def test_a_rotary_made_elsewhere_is_refused(sq):
+    x, pos = torch.zeros(2, 3, 16, dtype=F16, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        sq.rotate_heads(sq.Rotary(4, device="cpu"), x, None, pos)
+    sq.rotate_heads(sq.Rotary(0, device="cpu"), x, None)        # turns nothing
