@@ -1,6 +1,6 @@
 // Attention of packed prompts, a warp to a row: for rows that are no 16-byte
-// pieces.  Bound by the instructions of its products, a key to a lane: 2048 tokens x
-// 8 heads of 50 channels take 4.0 ms, where prompt_tile_kernel would take 0.03.
+// pieces.  Bound by the instructions of its products, eight channels to a lane: 2048 tokens x
+// 8 heads of 50 channels take 1.2 ms, where prompt_tile_kernel would take 0.03.
 #include "prompt_rows.cuh"
 
 namespace soniq {

@@ -89,7 +89,7 @@ struct Bars {                // offsets in 8-byte barriers; the first ones are t
                          o_full = pv_done + 2, o_free = o_full + 2, unit_full = o_free + 2, unit_free = unit_full + 2,
                          turn = unit_free + 2, drain = turn + 2, count = drain + 1;      // s_full: [tile][buffer]; p_full: [tile or buffer][half]
 };
-constexpr int kMisc = 3072;
+constexpr int kMisc = 3 * 1024;
 static_assert(8 * Bars::count <= 512, "barriers");
 
 // 64 consecutive TMEM columns of this thread's lane (load + wait in one statement).
