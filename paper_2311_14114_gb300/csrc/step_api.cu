@@ -23,8 +23,11 @@ soniq_status check_heads(const soniq_heads* h, RotateSide* s) {
     if (h->heads < 0 || h->in == nullptr || h->out == nullptr) return SONIQ_ERR_INVALID_ARG;
     if (h->heads > kMaxHeads) return SONIQ_ERR_UNSUPPORTED;
     if (!aligned_to(h->in, 2) || !aligned_to(h->out, 2) || !aligned_to(h->gain, 4)) return SONIQ_ERR_ALIGNMENT;
-    *s = RotateSide{static_cast<const uint16_t*>(h->in), h->in_token_stride, h->in_head_stride,
-                    static_cast<uint16_t*>(h->out), h->out_token_stride, h->out_head_stride, h->gain, h->heads};
+    // A lone head's stride is any number, but lanes without a row form addresses with it, and a copy of no bytes needs an
+    // aligned one too: 0.
+    const bool one = h->heads == 1;
+    *s = RotateSide{static_cast<const uint16_t*>(h->in), h->in_token_stride, one ? 0 : h->in_head_stride,
+                    static_cast<uint16_t*>(h->out), h->out_token_stride, one ? 0 : h->out_head_stride, h->gain, h->heads};
     return SONIQ_OK;
 }
 
