@@ -717,6 +717,11 @@ SONIQ_API soniq_status soniq_sync_status(soniq_stream_t stream);
  * disarms itself at that launch.  No fault, trap or hang is involved. */
 SONIQ_API void soniq_test_drop_barrier_arrival(int32_t armed);
 
+/* Test hook, not for production use.  In the next soniq_prompt_attend on the
+ * tensor cores a wait is given up after `ns` nanoseconds in which its CTA did
+ * nothing, not after 2 s (0 or less: 2 s). */
+SONIQ_API void soniq_test_wait_limit(int64_t ns);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,7 +27,7 @@ __global__ void __launch_bounds__(kThreads) prompt_rows_kernel(const PromptArgs 
         const int64_t rows = (int64_t)(e - s) * heads;
         for (; mine < done + rows; mine += warps) {
             const int t = s + (int)((mine - done) / heads), head = (int)((mine - done) % heads);
-            prompt_row<BF16, false>(a, head, t, s, a.causal ? t + 1 : e);
+            prompt_row<BF16, false>(a, head, t, s, a.causal ? t + 1 : e, [] {});
         }
         done += rows;
     }

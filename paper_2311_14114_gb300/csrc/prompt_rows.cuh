@@ -13,9 +13,9 @@ namespace soniq {
 // score so far, and what is summed follows it; they are in units of 2^spare, the
 // next power of two from their number, so that sums of values near the end of
 // bf16's range stay in fp32's.  (A score that is NaN makes the row NaN, as do two
-// infinities.)
-template <bool BF16, bool VEC>
-__device__ __noinline__ void prompt_row(const PromptArgs& a, int head, int t, int first, int end) {
+// infinities.)  tick() is called by one lane for every 32 keys.
+template <bool BF16, bool VEC, typename Tick>
+__device__ __noinline__ void prompt_row(const PromptArgs& a, int head, int t, int first, int end, Tick tick) {
     const int lane = threadIdx.x & 31, kv = head / a.group;
     auto width = [](int pieces) { return pieces <= 8 ? 8 : (pieces <= 16 ? 16 : 32); };
     const int k_pieces = (a.D + 7) / 8, v_pieces = (a.Dv + 7) / 8;
@@ -52,6 +52,7 @@ __device__ __noinline__ void prompt_row(const PromptArgs& a, int head, int t, in
     float top = -INFINITY, sum = 0.0f, acc[8] = {};
     bool nan = false;
     for (int j0 = first; j0 < end; j0 += 32) {
+        if (lane == 0) tick();
         float mine = -INFINITY;        // the score of key j0 + lane
 #pragma unroll 1
         for (int i0 = 0; i0 < k_wide; i0 += 4) {

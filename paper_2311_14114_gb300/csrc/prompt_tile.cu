@@ -164,14 +164,14 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 // CTAS: resident on an SM.  Two of one tile each take turns at the SM's units where prompts are short.
 template <bool BF16, int TILES, int CTAS>
 __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
-    prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ PromptPlan pl, const __grid_constant__ PromptMaps maps, unsigned* counters, const int drop) {
+    prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ PromptPlan pl, const __grid_constant__ PromptMaps maps, unsigned* counters, const int drop, const long long wait_ns) {
     extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
     const uint32_t smem0 = tc::smem_u32(smem), ring = smem0 + pl.ring_off, bars = smem0 + pl.misc_off;
     uint8_t* misc = smem + pl.misc_off;
     Unit* units = reinterpret_cast<Unit*>(misc + 512);                // [2]
     uint32_t* words = reinterpret_cast<uint32_t*>(misc + 640);
-    const uint32_t abort_flag = tc::smem_u32(words);
+    const uint32_t abort_flag = tc::smem_u32(words), progress = abort_flag + 8;
     uint32_t* tmem_at = words + 1;
     float* halves = reinterpret_cast<float*>(misc + 1024);            // [tile][half][128]: what the two threads of a row tell each other
     auto bar = [&](int i) { return bars + 8u * i; };
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
         init(Bars::unit_free, 2, 1 + 9 * TILES);
         init(Bars::turn, 2, 1);
         init(Bars::drain, 1, TILES);
-        words[0] = 0;
+        words[0] = words[2] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
@@ -204,9 +204,15 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
     __syncthreads();
     tc::tc_fence_after();
     const uint32_t tmem = uniform(*tmem_at);
+    // Waits are bounded: the warp that finds units is there until all others have seen the last of them, and raises the
+    // abort flag, which every wait looks at, once none of them has got on for `wait_ns`.  (Not before: a role may wait for
+    // as long as the others take over a unit, which with prompts of 2^28 tokens, or rows done again, is longer than any
+    // limit.)  These say that they get on: the warp that copies, with each piece, and those that do rows again, with
+    // each 32 keys.
+    auto tick = [progress]() { asm volatile("red.relaxed.cta.shared::cta.add.u32 [%0], 1;" ::"r"(progress) : "memory"); };
     // (one look at a wait that is over costs 20 cycles, the loop 160)
     auto wait = [&](int i, uint32_t parity) {
-        return __all_sync(0xffffffffu, tc::mbar_try_wait(bar(i), parity & 1u)) || wait_warp(bar(i), parity & 1u, abort_flag, a.err);
+        return __all_sync(0xffffffffu, tc::mbar_try_wait(bar(i), parity & 1u)) || wait_watched(bar(i), parity & 1u, abort_flag);
     };
 
     // The next unit, as the warps of other roles read it; they release it (`done`) when they have gone on.
@@ -231,6 +237,10 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
         int b0 = 0, taken = 0;         // and the end of them
         unsigned id = blockIdx.x;
         bool ok = true;
+        auto watch = [&](int i, uint32_t parity) {
+            return wait_watching(bar(i), parity & 1u, abort_flag, a.err, [&]() { return lds32(progress); }, wait_ns);
+        };
+        uint32_t last = 0;
         for (uint32_t n = 0;; ++n) {
             // the prompt that holds it: 32 at a time, from the last one on
             int found = -1, s = 0, len = 0;
@@ -270,7 +280,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
                 taken = max(taken, __shfl_sync(0xffffffffu, upmost, 31));
                 b0 += 32;
             }
-            ok = wait(Bars::unit_free + (n & 1), (n >> 1) ^ 1u);
+            ok = watch(Bars::unit_free + (n & 1), (n >> 1) ^ 1u);
             Unit u{};
             u.token = -1;
             if (found >= 0) {
@@ -293,7 +303,11 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
                 tc::mbar_arrive(bar(Bars::unit_full + (n & 1)));
             }
             __syncwarp();
-            if (!ok || found < 0) break;
+            if (!ok) break;
+            if (found < 0) {
+                last = n;
+                break;
+            }
             if (lane == 0) id = gridDim.x + atomicAdd(counters, 1u);
             id = __shfl_sync(0xffffffffu, id, 0);
         }
@@ -305,6 +319,9 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
                 counters[1] = 0;
             }
         }
+        // until all others have seen that there are no more
+        __syncwarp();
+        if (ok) watch(Bars::unit_free + (last & 1), last >> 1);
     } else if (warp == 1) {
         // ---- copies ----
         Ring kv;
@@ -336,6 +353,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
                         tc::mbar_arrive_expect_tx(bar(Bars::full + kv.i), (c + 1 < atoms ? 2 : 1) * kAtom);
                         tma_load_3d(at, map, 64 * c, kv_head, u.start + j * kTok, bar(Bars::full + kv.i));
                         if (c + 1 < atoms) tma_load_3d(at + kAtom, map, 64 * c + 64, kv_head, u.start + j * kTok, bar(Bars::full + kv.i));
+                        tick();
                     }
                     __syncwarp();
                 }
@@ -762,7 +780,7 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
                     again &= again - 1;
                     const int t = __shfl_sync(0xffffffffu, u.start + token, from), h = __shfl_sync(0xffffffffu, u.kv_head * a.group + head, from);
                     const int e = __shfl_sync(0xffffffffu, end, from);
-                    prompt_row<BF16, true>(a, h, t, u.start, u.start + e);
+                    prompt_row<BF16, true>(a, h, t, u.start, u.start + e, tick);
                     __syncwarp();
                 }
             }
@@ -876,7 +894,8 @@ cudaError_t launch_prompt_tile(const PromptArgs& a, bool bf16, unsigned* counter
                                            : (bf16 ? prompt_tile_kernel<true, 1, 1> : prompt_tile_kernel<false, 1, 1>));
     const cudaError_t e = prepared(reinterpret_cast<const void*>(kernel), 2 * (tiles - 1 + 2 * (ctas - 1)) + bf16, shared_of(ctas));
     if (e != cudaSuccess) return e;
-    kernel<<<grid, 128 + 256 * tiles, p.smem, st>>>(a, p, maps, counters, take_drop_arrival() ? 1 : 0);
+    const long long limit = take_wait_limit();
+    kernel<<<grid, 128 + 256 * tiles, p.smem, st>>>(a, p, maps, counters, take_drop_arrival() ? 1 : 0, limit > 0 ? limit : kWaitNs);
     note_launch();
     return cudaGetLastError();
 }

@@ -32,6 +32,7 @@ static __device__ __align__(256) float g_oneshot_partials[2 * kOneShotMaxCtas];
 // Test hook (soniq_test_drop_barrier_arrival): the next one-pass quantize
 // launch drops one grid-barrier arrival.
 std::atomic<int> g_drop_arrival{0};
+std::atomic<int64_t> g_wait_limit{0};      // soniq_test_wait_limit
 
 std::atomic<int64_t> g_launches{0};
 
@@ -91,6 +92,7 @@ bool oneshot_scratch(unsigned** bar, float** part) {
 }
 
 bool take_drop_arrival() { return g_drop_arrival.exchange(0) != 0; }
+int64_t take_wait_limit() { return g_wait_limit.exchange(0); }
 
 void note_launch(int n) { g_launches.fetch_add(n, std::memory_order_relaxed); }
 
@@ -655,5 +657,7 @@ soniq_status soniq_sync_status(soniq_stream_t stream) {
 }
 
 void soniq_test_drop_barrier_arrival(int32_t armed) { g_drop_arrival.store(armed != 0 ? 1 : 0); }
+
+void soniq_test_wait_limit(int64_t ns) { g_wait_limit.store(ns > 0 ? ns : 0); }
 
 }  // extern "C"

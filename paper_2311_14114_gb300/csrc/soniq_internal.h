@@ -57,6 +57,8 @@ constexpr int64_t kQuantScratchBytes = 256 + 8 * kMaxGridPartials;
 constexpr int64_t kKeepInL2Bytes = 80ll << 20;
 // True once for the launch that the test hook soniq_test_drop_barrier_arrival armed.
 bool take_drop_arrival();
+// What soniq_test_wait_limit set for this launch, 0 for the next ones.
+int64_t take_wait_limit();
 void note_launch(int n = 1);
 int num_sms();
 // Asks for the largest shared-memory carve-out for `func` (once per device):

@@ -76,19 +76,47 @@ __device__ __forceinline__ bool wait_until(F poll, uint32_t abort_flag, unsigned
         }
     }
 }
+__device__ __forceinline__ uint32_t poll64(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 64;\n"
+        "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra DONE;\n\t"
+        "sub.u32 n, n, 1;\n\tsetp.ne.u32 q, n, 0;\n\t@q bra TRY;\n"
+        "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done;
+}
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, uint32_t abort_flag, unsigned* err) {
-    return wait_until([&]() {
-        uint32_t done;
-        asm volatile(
-            "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 64;\n"
-            "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra DONE;\n\t"
-            "sub.u32 n, n, 1;\n\tsetp.ne.u32 q, n, 0;\n\t@q bra TRY;\n"
-            "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done)
-            : "r"(bar), "r"(parity)
-            : "memory");
-        return done;
-    }, abort_flag, err);
+    return wait_until([&]() { return poll64(bar, parity); }, abort_flag, err);
+}
+// One that looks at no clock: another warp of the CTA does, for all of them, and raises the flag.
+__device__ __forceinline__ bool wait_watched(uint32_t bar, uint32_t parity, uint32_t abort_flag) {
+    while (true) {
+        if (__all_sync(0xffffffffu, poll64(bar, parity))) return true;
+        if (__any_sync(0xffffffffu, tc::abort_raised(abort_flag))) return false;
+    }
+}
+// That warp's: given up after `limit` in which sign(), a word that others change as they get on, stayed the same.
+template <typename Sign>
+__device__ __forceinline__ bool wait_watching(uint32_t bar, uint32_t parity, uint32_t abort_flag, unsigned* err, Sign sign, long long limit) {
+    long long t0 = 0;
+    uint32_t seen = 0;
+    while (true) {
+        if (__all_sync(0xffffffffu, poll64(bar, parity))) return true;
+        const long long t = tc::globaltimer();
+        const uint32_t now = __shfl_sync(0xffffffffu, sign(), 0);
+        if (t0 == 0 || now != seen) {
+            t0 = t;
+            seen = now;
+        }
+        if (__any_sync(0xffffffffu, t - t0 > limit)) {
+            tc::set_flag(abort_flag, 1);
+            atomicOr(err, kErrWait);
+            return false;
+        }
+    }
 }
 // The same for two or three barriers, whose phases stay complete until this warp has gone
 // on.  (One after the other, three waits that were over took 870 cycles of a block's 3550.)

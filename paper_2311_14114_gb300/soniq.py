@@ -40,7 +40,7 @@ EXPORTED = ["soniq_abi_version", "soniq_status_string", "soniq_group_codes",
             "soniq_mp_gemm_scratch_bytes", "soniq_mp_conv2d", "soniq_mp_conv2d_scratch_bytes", "soniq_sync_status",
             "soniq_test_drop_barrier_arrival", "soniq_kv_row_bytes", "soniq_kv_validate", "soniq_kv_write",
             "soniq_kv_read", "soniq_kv_attend", "soniq_kv_attend_scratch_bytes", "soniq_kv_plan", "soniq_rotate_heads",
-            "soniq_prompt_attend", "soniq_prompt_attend_scratch_bytes"]
+            "soniq_prompt_attend", "soniq_prompt_attend_scratch_bytes", "soniq_test_wait_limit"]
 
 _SCALE = {"tensor": SCALE_PER_TENSOR, "row": SCALE_PER_ROW, "calibrated": SCALE_CALIBRATED}
 
@@ -139,6 +139,8 @@ def lib() -> ctypes.CDLL:
         L.soniq_sync_status.restype = i32
         L.soniq_test_drop_barrier_arrival.argtypes = [i32]
         L.soniq_test_drop_barrier_arrival.restype = None
+        L.soniq_test_wait_limit.argtypes = [i64]
+        L.soniq_test_wait_limit.restype = None
         L.soniq_kv_row_bytes.argtypes = [P]
         L.soniq_kv_row_bytes.restype = i64
         L.soniq_kv_validate.argtypes = [P, P, P]
@@ -818,6 +820,11 @@ def sync_status(stream=None) -> int:
 def test_drop_barrier_arrival(armed: bool = True):
     """soniq_test_drop_barrier_arrival (test hook)."""
     lib().soniq_test_drop_barrier_arrival(1 if armed else 0)
+
+
+def test_wait_limit(ns: int):
+    """soniq_test_wait_limit (test hook)."""
+    lib().soniq_test_wait_limit(ns)
 
 
 def launch_count() -> int:
