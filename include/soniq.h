@@ -588,7 +588,9 @@ SONIQ_API int64_t soniq_kv_attend_scratch_bytes(const soniq_kv_cache *cache, int
  *   - A sequence is served if its pages fit its row of the table, its tokens lie
  *     below max_tokens, and the pool lasts; the first for which it does not last
  *     has all later ones that need pages wait too.  One that is not served
- *     changes nothing: no page, its length kept, its tokens' slots -1.
+ *     changes nothing: no page, its length kept, its tokens' slots -1.  (The page
+ *     behind its context may be none, or one that it gave back and another has by
+ *     now: soniq_kv_attend is to get a negative length for it in that step.)
  * page_size 16 to 256, a power of two; B <= 8192, B * max_pages < 2^31
  * (SONIQ_ERR_UNSUPPORTED otherwise).
  *   table       device int32, row b at table + b * table_stride, max_pages entries:

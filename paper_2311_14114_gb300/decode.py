@@ -19,7 +19,7 @@ arithmetic step runs in the library's kernels.  The layer is fp16; a model that
 runs in bf16 makes the same calls itself."""
 from __future__ import annotations
 
-from typing import Optional, Tuple
+from typing import Optional, Tuple, Union
 
 import torch
 
@@ -92,16 +92,49 @@ class CachedAttention:
         slot = torch.where(inside & (pages >= 0), pages * page + pos % page, self.cache.n_pages * page)
         return torch.where(lengths[:, None] >= 0, slot, -1)
 
+    def planned(self, plan: sq.KVStep, B: int, T: int) -> torch.Tensor:
+        """The slots of a plan's tokens, which stand packed, as int64 [B][T]: row b those of
+        its sequence b; -1 in sequences that add none or were not served.  One that adds
+        another number than T has no place in such a step: its slots are beyond the cache,
+        which the library reports."""
+        if plan.starts.numel() <= B:
+            raise ValueError("the plan has fewer sequences than the step")
+        none = self.cache.n_pages * self.cache.page_size
+        n = plan.slots.numel()
+        if n == 0:
+            return torch.full((B, T), -1, dtype=torch.int64, device=plan.slots.device)
+        first, count = plan.starts[:B, None].long(), (plan.starts[1:B + 1] - plan.starts[:B])[:, None]
+        slots = plan.slots[(first + torch.arange(T, device=first.device)).clamp(max=n - 1)]
+        served = (count > 0) & (plan.slots[first.clamp(max=n - 1)] >= 0)
+        return torch.where(served, torch.where(count == T, slots, none), -1)
+
     def step(self, X: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
              mask: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
-             slots: Optional[torch.Tensor] = None) -> torch.Tensor:
+             slots: Union[None, torch.Tensor, sq.KVStep] = None) -> torch.Tensor:
         """X: fp16 [B][T][K]; page_table int32 [B][pages]; lengths int32 [B] (the
         context in front of the T tokens); mask as sq.kv_attend's.  positions: int32
         [B][T], what a layer with a rotary turns by (left out: one after the other
         behind the context; of a tree's drafts those with the same depth share one).
-        slots: int64, the B * T tokens' where they are known (sq.kv_plan's).  Returns
-        fp16 [B][T][N]; q, k, v and the attention's output stay in self."""
+        slots: where the tokens go: sq.kv_plan's step, each of whose first B sequences adds
+        T tokens or none; or int64 [B][T] (not a plan's own packed list, in which absent
+        sequences have no place).  A sequence none of whose slots is in the cache is absent
+        from the step.  Left out, the table says where: not behind sq.kv_plan, which leaves pages
+        that were given back in it, and sequences that wait without.  Returns fp16
+        [B][T][N]; q, k, v and the attention's output stay in self."""
         B, T, K = X.shape
+        if slots is None:
+            at = self.slots(page_table, lengths, T)
+        elif isinstance(slots, sq.KVStep):
+            at = self.planned(slots, B, T)
+        elif slots.numel() == B * T:
+            at = slots.reshape(B, T)
+        else:
+            raise ValueError("slots must be a KVStep or int64 [B][T]")
+        seen = lengths
+        if slots is not None:
+            there = ((at >= 0) & (at < self.cache.n_pages * self.cache.page_size)).any(1)
+            lengths = torch.where(there, lengths.clamp(min=0), lengths)       # (one that begins may have a negative length)
+            seen = torch.where(there, lengths, -1)
 
         def where():
             p = lengths[:, None] + torch.arange(T, dtype=torch.int32, device=X.device) if positions is None else positions
@@ -109,8 +142,8 @@ class CachedAttention:
 
         q, k, v = self._heads(X.reshape(B * T, K), where)
         self.q, self.k, self.v = (t.unflatten(0, (B, T)) for t in (q, k, v))
-        sq.kv_write(self.cache, k, v, self.slots(page_table, lengths, T).view(-1) if slots is None else slots)
-        self.o = sq.kv_attend(self.cache, self.q, page_table, lengths, mask)
+        sq.kv_write(self.cache, k, v, at.view(-1))
+        self.o = sq.kv_attend(self.cache, self.q, page_table, seen, mask)
         return self._project(1, self.o.view(B * T, -1)).view(B, T, -1)
 
     def accept(self, path: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor) -> torch.Tensor:

@@ -640,7 +640,8 @@ def kv_plan(pages: KVPages, lengths: torch.Tensor, targets: torch.Tensor, max_to
     tokens (int32 [B]; negative: none yet) holds targets[b] (negative: it leaves);
     pages.table and pages.free are updated, and pages.count, unless count_out (int32)
     is to get the pool's new size.  max_tokens: rows of the step's buffers, at least
-    its tokens (those of sequences beyond it are not served)."""
+    its tokens (those of sequences beyond it are not served).  A sequence that is not
+    served keeps its length; kv_attend is to get -1 for it in that step."""
     B, here = lengths.numel(), _device() if lengths.is_cuda else -2
     i32, table, max_tokens = torch.int32, pages.table, int(max_tokens)
     rows, width = table.shape
