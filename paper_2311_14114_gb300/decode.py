@@ -153,7 +153,7 @@ class CachedAttention:
         B, T = self.k.shape[:2]
         to = torch.full((B, T + 1), -1, dtype=torch.int64, device=path.device)
         to.scatter_(1, torch.where(path >= 0, path, T), self.slots(page_table, lengths, path.shape[1]))
-        sq.kv_write(self.cache, self.k.flatten(0, 1), self.v.flatten(0, 1), to[:, :T].reshape(-1))
+        sq.kv_write(self.cache, self.k.flatten(0, 1), self.v.flatten(0, 1), to[:, :T].reshape(-1).contiguous())
         return torch.where(lengths >= 0, lengths + (path >= 0).sum(1), lengths).to(torch.int32)
 
     def context(self, page_table: torch.Tensor, lengths: torch.Tensor, b: int) -> Tuple[torch.Tensor, torch.Tensor]:
