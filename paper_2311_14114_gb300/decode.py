@@ -51,7 +51,7 @@ class CachedAttention:
         if self.weights[0][1].shape[0] != sum(widths) or self.weights[1][0].K != self.q_heads * v.D:
             raise ValueError("the projections' sizes differ from the heads'")
         self.widths = widths
-        self.q = self.k = self.v = self.o = None
+        self.q = self.k = self.v = self.o = self.at = None
         self.rotary, self.gains, self.eps = rotary, gains or (None, None), eps
 
     def _project(self, which: int, x: torch.Tensor) -> torch.Tensor:
@@ -142,6 +142,7 @@ class CachedAttention:
 
         q, k, v = self._heads(X.reshape(B * T, K), where)
         self.q, self.k, self.v = (t.unflatten(0, (B, T)) for t in (q, k, v))
+        self.at = at
         sq.kv_write(self.cache, k, v, at.view(-1))
         self.o = sq.kv_attend(self.cache, self.q, page_table, seen, mask)
         return self._project(1, self.o.view(B * T, -1)).view(B, T, -1)
@@ -149,12 +150,16 @@ class CachedAttention:
     def accept(self, path: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor) -> torch.Tensor:
         """path: int64 [B][A], the accepted drafts of the last step in their order,
         -1 behind the last.  Their rows become the context's next tokens; returns
-        the new lengths."""
+        the new lengths.  Nothing is written but slots of that step: a sequence that was
+        absent from it (the page behind its context may be another's) keeps its length."""
         B, T = self.k.shape[:2]
+        lengths = torch.where((self.at >= 0).any(1), lengths.clamp(min=0), lengths)
+        slots = self.slots(page_table, lengths, path.shape[1])
+        slots = torch.where((slots[:, :, None] == self.at[:, None]).any(2), slots, -1)
         to = torch.full((B, T + 1), -1, dtype=torch.int64, device=path.device)
-        to.scatter_(1, torch.where(path >= 0, path, T), self.slots(page_table, lengths, path.shape[1]))
+        to.scatter_(1, torch.where(path >= 0, path, T), slots)
         sq.kv_write(self.cache, self.k.flatten(0, 1), self.v.flatten(0, 1), to[:, :T].reshape(-1).contiguous())
-        return torch.where(lengths >= 0, lengths + (path >= 0).sum(1), lengths).to(torch.int32)
+        return (lengths + ((path >= 0) & (slots >= 0)).sum(1)).to(torch.int32)
 
     def context(self, page_table: torch.Tensor, lengths: torch.Tensor, b: int) -> Tuple[torch.Tensor, torch.Tensor]:
         """The keys [n][heads][D] and values that the cache holds of sequence b."""

@@ -119,3 +119,21 @@ def test_a_captured_step(sq):  # noqa: F811
         torch.cuda.synchronize()
         assert torch.equal(got, want) and torch.equal(lengths, a.lengths)
     assert sq.sync_status() == 0
+
+
+@pytest.mark.parametrize("T", [1, 3])
+def test_a_sequence_that_waits_accepts_nothing(sq, T):  # noqa: F811
+    """Its drafts have no slots, and the page behind its context is another's."""
+    s = waiting_pool(sq, 95)
+    n = s.lengths.tolist()
+    plan = sq.kv_plan(s.pages, s.lengths, ints([n[0] + T, n[1] + T, -1, -1, -1]), SEQS * T)
+    s.net.step(s.x(SEQS, T), s.pages.table, s.lengths, slots=plan)
+    path = torch.tensor([list(range(T))] * SEQS, device="cuda")
+    path[1, 1:] = -1
+    new = s.net.accept(path, s.pages.table, s.lengths)
+    assert new.tolist() == [n[0], n[1] + 1, -1, -1, -1]
+    k, v = s.net.k.double().cpu().numpy(), s.net.v.double().cpu().numpy()
+    s.k[1], s.v[1] = np.concatenate([s.k[1], k[1, :1]]), np.concatenate([s.v[1], v[1, :1]])
+    s.lengths = sq.kv_plan(s.pages, plan.lengths, new, 0).lengths
+    s.check_cache()
+    assert sq.sync_status() == 0
