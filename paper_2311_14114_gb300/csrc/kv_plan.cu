@@ -19,6 +19,8 @@
 // the prefix sums' barriers, bisections.  Measured, replayed from a graph (GB300): 8
 // sequences that decode 6.2 us, 1000 of which some leave 12.3, 32 prompts of up to
 // 4000 tokens 10.3.
+#include <atomic>
+
 #include "step_internal.h"
 
 namespace soniq {
@@ -205,13 +207,28 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a) {
     if (tid == 0) a.count_out[0] = (int32_t)min(pool + R - taken, (int64_t)a.n_pages);
 }
 
+constexpr int shared_of(int B) { return 12 * (B + 1) + 9 * B; }
+
+// Asks for the shared memory of the largest call, once per device: the limit is the
+// function's, so one that each call set to its own size would fail other threads' launches.
+cudaError_t prepared() {
+    static std::atomic<bool> done[64];
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const bool known = device >= 0 && device < 64;
+    if (known && done[device].load(std::memory_order_relaxed)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kv_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared_of(kPlanMaxSequences));
+    if (e == cudaSuccess) e = prefer_max_shared(reinterpret_cast<const void*>(kv_plan_kernel));
+    if (e == cudaSuccess && known) done[device].store(true, std::memory_order_relaxed);
+    return e;
+}
+
 }  // namespace
 
 cudaError_t launch_kv_plan(const KvPlanArgs& a, cudaStream_t st) {
-    const int smem = 12 * (a.B + 1) + 9 * a.B;
-    cudaError_t e = prefer_max_shared(reinterpret_cast<const void*>(kv_plan_kernel));
-    if (e == cudaSuccess && smem > 48 * 1024)
-        e = cudaFuncSetAttribute(kv_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    const int smem = shared_of(a.B);
+    const cudaError_t e = prepared();
     if (e != cudaSuccess) return e;
     // two tokens to a thread, or one sequence, whose pages are not known here, to a warp
     const int64_t by_tokens = ((int64_t)a.max_tokens + 2 * kThreads - 1) / (2 * kThreads), by_pages = (a.B + 15) / 16;
