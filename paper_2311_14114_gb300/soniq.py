@@ -696,8 +696,19 @@ class Rotary:
         ratios = [f.as_integer_ratio() for f in self.frequencies]
         turns = [(2 * n * _PI_SCALE * 2 ** 63 + d * _PI) // (2 * d * _PI) % 2 ** 64 for n, d in ratios]
         self.turns = torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turns], dtype=torch.int64, device=device)
-        self.c = CRotary(self.channels, int(self.interleaved), self.magnitude, self.turns.data_ptr() if turns else None)
+        self._refer()
+
+    def _refer(self):
+        self.c = CRotary(self.channels, int(self.interleaved), self.magnitude, self.turns.data_ptr() if self.channels else None)
         self.ref = ctypes.byref(self.c)
+
+    # copies and pickles refer to turns of their own
+    def __getstate__(self):
+        return {name: x for name, x in self.__dict__.items() if name not in ("c", "ref")}
+
+    def __setstate__(self, state):
+        self.__dict__.update(state)
+        self._refer()
 
     @staticmethod
     def _scaled(freq, scaling):
