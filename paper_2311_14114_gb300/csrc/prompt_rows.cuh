@@ -7,6 +7,8 @@
 
 namespace soniq {
 
+constexpr float kMostScale = 2.3e38f;      // up to here scale * log2(e) is within fp32
+
 // The row of query head `head` at token t, over keys first .. end - 1, 32 at a time.
 // VEC: rows are whole 16-byte pieces.  Eight channels to a lane, so the warp takes
 // one, two or four keys (and values) at once.  Weights are relative to the largest
@@ -46,8 +48,9 @@ __device__ __noinline__ void prompt_row(const PromptArgs& a, int head, int t, in
     const uint16_t* values = a.v.p + kv * a.v.head + v_at;
     const int64_t k_token = a.k.token, v_token = a.v.token;
     const int k_left = a.D - k_at, v_left = a.Dv - v_at;
-    // (never 0: what is not there, minus infinity, has no weight at any scale)
-    const float factor = fmaxf(a.scale * kLog2e, 1.4e-45f);
+    // (never 0: what is not there, minus infinity, has no weight at any scale; in two steps where one would pass fp32, of which the tiles have none)
+    const bool whole = VEC || a.scale <= kMostScale;
+    const float factor = whole ? fmaxf(a.scale * kLog2e, 1.4e-45f) : a.scale, rest = whole ? 1.0f : kLog2e;
     const int spare = 32 - __clz(max(end - first - 1, 0));
     float top = -INFINITY, sum = 0.0f, acc[8] = {};
     bool nan = false;
@@ -80,7 +83,7 @@ __device__ __noinline__ void prompt_row(const PromptArgs& a, int head, int t, in
         if (nan) break;
         // (keys of scores minus infinity alone: no weight, and 0 times a value that is not finite is NaN here too)
         const float from = best == -INFINITY ? 0.0f : best;
-        const float down = exp2f((top - from) * factor), w = exp2f((mine - from) * factor), part = ldexpf(w, -spare);
+        const float down = exp2f((top - from) * factor * rest), w = exp2f((mine - from) * factor * rest), part = ldexpf(w, -spare);
         top = best;
         sum = fmaf(sum, down, w);
 #pragma unroll

@@ -861,7 +861,7 @@ bool make_plan(const PromptArgs& a, int tiles, int ctas, PromptPlan* p) {
 }  // namespace
 
 bool prompt_tile_supported(const PromptArgs& a) {
-    return a.D % 8 == 0 && a.Dv % 8 == 0 && (uintptr_t)a.out % 16 == 0 && mapped(a.q, a.n, a.k_heads * a.group, false) &&
+    return a.scale <= kMostScale && a.D % 8 == 0 && a.Dv % 8 == 0 && (uintptr_t)a.out % 16 == 0 && mapped(a.q, a.n, a.k_heads * a.group, false) &&
            mapped(a.k, a.n, a.k_heads, true) && mapped(a.v, a.n, a.k_heads, true);
 }
 
