@@ -615,8 +615,9 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
         const int heads = a.k_heads * a.group;
         float* mine_at = halves + (2 * s + half) * 128 + row;
         const float* other_at = halves + (2 * s + 1 - half) * 128 + row;
-        // Whether it is so in any row of the two warps that share these 32.  (Waits are bounded, but this is not: a warp
-        // whose wait was given up goes on to the next such point, and both leave there.)
+        // Whether it is so in any row of the two warps that share these 32.  Waits are bounded, but this is not: both have to
+        // come to each.  So a warp whose wait was given up goes on to the next one, where both learn of it and leave; and
+        // none stands within a loop over a half's columns, of which the other half may have none.
         auto either = [&](bool x) {
             uint32_t r;
             asm volatile(
