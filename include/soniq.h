@@ -687,7 +687,7 @@ SONIQ_API soniq_status soniq_rotate_heads(const soniq_rotary *rotary, const int3
  * output once.  What a row does not see does not matter, whatever it holds.
  * Pointers need the alignment of their elements.  The tensor cores are used where
  * D and Dv are multiples of 8 and rows are on 16 bytes (pointers, and token and
- * head strides); other rows take a slow kernel.
+ * head strides); other rows, and scales above 2.3e38, take a slow kernel.
  */
 SONIQ_API soniq_status soniq_prompt_attend(const void *Q, int64_t q_token_stride, int64_t q_head_stride, const void *K,
                                            int64_t k_token_stride, int64_t k_head_stride, const void *V,

@@ -8,7 +8,7 @@
 // blocks of 128 tokens.  Its warps:
 //   warp 0 (and 2)   issue the MMAs, each for one tile;
 //   warp 1           copies queries, keys and values by TMA;
-//   warp 3           finds the next unit;
+//   warp 3           finds the next unit, and looks at the clock for all waits;
 //   warps 4-11 and 12-19  softmax of a tile, two threads to a row.
 // Weights go over the scores that they come from.  While one tile's softmax runs,
 // the tensor cores work for the other; a lone tile has two buffers of scores.
@@ -23,8 +23,9 @@
 // leave outputs and begin anew, in code that is not in the instruction cache.
 // Lone tiles (256 channels) have 2048 cycles of MMAs to 1300, and hide the softmax.
 // Measured (GB300, bf16, causal, 32 query heads on 8): 16384 tokens of 128 channels
-// 1.41 ms (1560 TFLOP/s), 8192 of 64, 128, 256: 286, 327, 616 us (960, 1680, 1780),
-// 16 prompts of 410 to 4096 tokens 680 us (1230).
+// 1.42 ms (1550 TFLOP/s), 8192 of 64, 128, 256: 275, 320, 609 us (1000, 1720, 1800),
+// 16 prompts of 410 to 4096 tokens 675 us (1240), 200 of 0 to 200, 12 heads of 64 in
+// fp16, 58 us.
 // Taken and not, at 16384 tokens: blocks of 64 with two buffers of scores 1864 us
 // (their MMAs, N = 64, read 192 bytes of operands a cycle for 128); a thread to a
 // row, 1960; one warp for both tiles' MMAs, 2200, as its instructions between them
@@ -208,7 +209,8 @@ __global__ void __launch_bounds__(128 + 256 * TILES, CTAS)
     // abort flag, which every wait looks at, once none of them has got on for `wait_ns`.  (Not before: a role may wait for
     // as long as the others take over a unit, which with prompts of 2^28 tokens, or rows done again, is longer than any
     // limit.)  These say that they get on: the warp that copies, with each piece, and those that do rows again, with
-    // each 32 keys.
+    // each 32 keys.  (A clock in every wait is code at 35 places: 200 short prompts took 62 us, and 64 with the look at
+    // whether others get on; now 58.)
     auto tick = [progress]() { asm volatile("red.relaxed.cta.shared::cta.add.u32 [%0], 1;" ::"r"(progress) : "memory"); };
     // (one look at a wait that is over costs 20 cycles, the loop 160)
     auto wait = [&](int i, uint32_t parity) {
@@ -870,8 +872,8 @@ cudaError_t launch_prompt_tile(const PromptArgs& a, bool bf16, unsigned* counter
     PromptPlan p{};
     int tiles = 1, ctas = 2;
     // Prompts of 128 rows or less on the average go to two CTAs an SM: the second has the time that the first spends
-    // between units.  (200 prompts x 12 heads, us with one / two: 100 tokens of 64 channels 69 / 45, of 128 74 / 59, 120
-    // of 128 74 / 65; 160 and more of 64 96 / 94.)
+    // between units.  (200 prompts x 12 heads, us with one / two: 100 tokens of 64 channels 52 / 44, of 128 60 / 58, 120
+    // of 128 62 / 63; 160 of 64 79 / 85.)
     const bool small = (int64_t)a.n * (a.group < 128 ? a.group : 128) <= 128 * (int64_t)a.B;
     if (!small || !make_plan(a, 1, 2, &p)) {
         ctas = 1;
